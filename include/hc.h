@@ -456,6 +456,141 @@ hc_status hc_spiral_conv_fwd(const void* x, hc_dtype dt, const int32_t* spiral, 
                              hc_act act, void* y, hc_stream_t stream);
 
 /*
+ * Token operators
+ * ---------------
+ * A token is a row of a compact [capacity, C] matrix; the operators below are
+ * the front of a network over such rows (row embedding, layer norm, the 8-bit
+ * form of the linear layer) and their gradients. The paper has no counterpart.
+ * In all of them `count` is N' on the device (clamped to [0, capacity],
+ * HC_ERR_CAPACITY / HC_ERR_INVALID_INDEX reported when it was outside) or
+ * NULL, which means all `capacity` rows; rows n >= N' are neither read nor
+ * written. Pointers need the alignment of their element type; rows that are
+ * 16-byte aligned (pointer and row size) move in 16-byte pieces. Sums are
+ * taken in fp32 and in a fixed order: results are the same from run to run.
+ */
+
+/*
+ * hc_layer_norm_fwd -- layer norm of every row over its own C channels (the
+ * per-frame norm is hc_sparse_group_norm_fwd):
+ *   mean = sum x / C,  rstd = 1 / sqrt(sum (x - mean)^2 / C + eps)
+ *   y[n][c] = (x[n][c] - mean) * rstd * gamma[c] + beta[c],  n < N'
+ *   x, y      [capacity, C] of dtype dt; y may be x (in place)
+ *   gamma, beta  [C] fp32, or NULL (1 / 0)
+ *   mean, rstd   [capacity] fp32, or NULL: what hc_layer_norm_bwd reads
+ * C >= 1, eps >= 0. With C = 1, or a constant row, and eps = 0 the row is NaN.
+ */
+hc_status hc_layer_norm_fwd(const void* x, hc_dtype dt, const int32_t* count, int capacity, int C,
+                            float eps, const float* gamma, const float* beta, void* y, float* mean,
+                            float* rstd, hc_stream_t stream);
+
+/*
+ * hc_layer_norm_bwd -- its gradient. With xh = (x - mean) * rstd and
+ * g = dy * gamma, over rows n < N':
+ *   dx[n][c]  = rstd * (g - (sum_c g) / C - xh * (sum_c g * xh) / C)
+ *   dgamma[c] = sum_n dy * xh,  dbeta[c] = sum_n dy   (0 when N' = 0)
+ *   x, dy     [capacity, C] of dtype dt; mean, rstd as the forward wrote them
+ *   dx        [capacity, C] of dtype dt, or NULL; may be x or dy (in place)
+ *   dgamma, dbeta  [C] fp32, or NULL each; at least one output is required
+ * Uses the library's per-stream workspace (8 bytes per row and channel sums
+ * of 8 * C bytes for each of at most 16 blocks per SM).
+ */
+hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const int32_t* count,
+                            int capacity, int C, const float* gamma, const float* mean,
+                            const float* rstd, void* dx, float* dgamma, float* dbeta,
+                            hc_stream_t stream);
+
+/*
+ * hc_embedding_fwd -- a table row for every token:
+ *   y[n] = scale * table[ids[n * ids_stride]],  n < N'; zero for the id -1
+ * (padding). Any other id outside [0, V) is reported (HC_ERR_INVALID_INDEX)
+ * and treated as -1.
+ *   table     [V, C] of dtype dt;  y [capacity, C] of dtype dt, rounded once
+ *   ids       int32, ids_stride >= 1 elements apart: 1 for a list of ids, 2
+ *             with ids = coords + 1 for the vertex of every active row of
+ *             hc_mask_compact (a learned vector per vertex)
+ */
+hc_status hc_embedding_fwd(const void* table, hc_dtype dt, int V, int C, const int32_t* ids,
+                           int ids_stride, const int32_t* count, int capacity, float scale,
+                           void* y, hc_stream_t stream);
+
+/*
+ * hc_embedding_sort -- the token positions in ascending order of their id,
+ * equal ids in ascending order of position:
+ *   row_ptr   [V + 1] int32: the tokens of table row v are
+ *             order[row_ptr[v]] .. order[row_ptr[v + 1] - 1]
+ *   order     [capacity] int32; entries from row_ptr[V] on (padding, ids out
+ *             of range, positions n >= N') are written but belong to no row
+ * Computed once per batch and reused by every table indexed with these ids.
+ * Ids out of range other than -1 are reported (HC_ERR_INVALID_INDEX). The
+ * result is unique (bit-exact). Uses the library's per-stream workspace (16
+ * bytes per token and 512 KiB).
+ */
+hc_status hc_embedding_sort(const int32_t* ids, int ids_stride, const int32_t* count, int capacity,
+                            int V, int32_t* row_ptr, int32_t* order, hc_stream_t stream);
+
+/*
+ * hc_embedding_bwd -- the table's gradient:
+ *   dtable[v][c] = scale * sum of dy[order[i]][c], row_ptr[v] <= i < row_ptr[v + 1]
+ * every row written (0 where no token reads it).
+ *   dy        [capacity, C] of dtype dt;  dtable [V, C] fp32
+ *   row_ptr, order  from hc_embedding_sort (same capacity). A range of row_ptr
+ *             that is not inside [0, capacity], or an entry of order that is
+ *             not below capacity, is reported (HC_ERR_INVALID_INDEX) and skipped.
+ */
+hc_status hc_embedding_bwd(const void* dy, hc_dtype dt, const int32_t* row_ptr,
+                           const int32_t* order, int capacity, int V, int C, float scale,
+                           float* dtable, hc_stream_t stream);
+
+/*
+ * The 8-bit form of a matrix: e4m3 values in rows of HC_FP8_PITCH(C) bytes
+ * (C rounded up to 16, the bytes beyond C zero) and one fp32 scale per block
+ * of HC_FP8_BLOCK channels; a value is q * scale.
+ */
+#define HC_FP8_BLOCK 128
+#define HC_FP8_PITCH(C) (((C) + 15) / 16 * 16)
+
+/*
+ * hc_quantize_fp8_rows -- rows into the 8-bit form, a scale per row and block:
+ *   scale = max(amax / 448, 2^-126),  q = e4m3(x / scale)
+ * with amax the largest magnitude of the block's channels, both quotients in
+ * fp32 and each rounding to nearest even. A block that holds a NaN or an
+ * infinity gets a scale that is not finite, so that every product of that row
+ * is NaN.
+ *   x         [capacity, C] of dtype dt
+ *   q         [capacity, HC_FP8_PITCH(C)], 16-byte aligned
+ *   scales    [ceil(C / 128), capacity] fp32 (block-major)
+ */
+hc_status hc_quantize_fp8_rows(const void* x, hc_dtype dt, const int32_t* count, int capacity,
+                               int C, uint8_t* q, float* scales, hc_stream_t stream);
+
+/*
+ * hc_quantize_fp8_weight -- a layer weight W [C_in, C_out] of dtype dt into
+ * the 8-bit form that hc_fp8_linear_fwd reads, a scale per 128 x 128 block:
+ *   wq        [C_out, HC_FP8_PITCH(C_in)], 16-byte aligned (W transposed)
+ *   ws        [ceil(C_out / 128), ceil(C_in / 128)] fp32
+ * Done once per weight. For the input gradient of the layer, quantise W's
+ * transpose: the layer's input gradient is the same product with it.
+ */
+hc_status hc_quantize_fp8_weight(const void* W, hc_dtype dt, int C_in, int C_out, uint8_t* wq,
+                                 float* ws, hc_stream_t stream);
+
+/*
+ * hc_fp8_linear_fwd -- hc_sparse_linear_fwd with both operands in 8 bits:
+ *   y[n][o] = act( bias[o] + sum_b xs[b][n] * ws[o / 128][b] *
+ *                  sum_{c in block b} xq[n][c] * wq[o][c] ),  n < N'
+ *   xq, xs    as hc_quantize_fp8_rows wrote them (same capacity and C_in)
+ *   wq, ws    as hc_quantize_fp8_weight wrote them
+ *   bias      [C_out] fp32, or NULL for zero
+ *   y         [capacity, C_out] of dtype y_dt
+ * Sums in fp32: a block's products are added in the tensor cores'
+ * accumulators, the scaled block sums in registers.
+ */
+hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* count, int capacity,
+                            int C_in, int C_out, const uint8_t* wq, const float* ws,
+                            const float* bias, hc_act act, hc_dtype y_dt, void* y,
+                            hc_stream_t stream);
+
+/*
  * hc_get_device_status -- synchronises `stream`, then reads and clears the
  * current device's sticky status word. Returns HC_OK if no kernel reported a
  * problem since the last read, else the lowest-numbered device error seen

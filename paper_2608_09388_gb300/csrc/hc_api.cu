@@ -666,6 +666,226 @@ hc_status hc_scatter_dense(const void* y, hc_dtype dt, const int32_t* coords,
                           (cudaStream_t)stream);
 }
 
+// Checks shared by the token operators on [capacity, C] rows.
+static hc_status check_rows(const char* fn, hc_dtype dt, int capacity, int C) {
+    HC_REQUIRE(dt == HC_F32 || dt == HC_BF16, "%s: unknown dtype %d", fn, (int)dt);
+    HC_REQUIRE(capacity >= 0, "%s: capacity=%d must be >= 0", fn, capacity);
+    HC_REQUIRE(C >= 1, "%s: C=%d must be >= 1", fn, C);
+    return HC_OK;
+}
+
+static size_t elem_bytes(hc_dtype dt) {
+    return dt == HC_F32 ? 4 : 2;
+}
+
+hc_status hc_layer_norm_fwd(const void* x, hc_dtype dt, const int32_t* count, int capacity, int C,
+                            float eps, const float* gamma, const float* beta, void* y, float* mean,
+                            float* rstd, hc_stream_t stream) {
+    const char* fn = "hc_layer_norm_fwd";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(eps >= 0.f, "%s: eps=%g must be >= 0", fn, (double)eps);
+    if (capacity == 0) return HC_OK;
+    HC_REQUIRE(x && y, "%s: x and y are required", fn);
+    HC_REQUIRE(!misaligned(x, elem_bytes(dt)) && !misaligned(y, elem_bytes(dt)),
+               "%s: x and y must be aligned to the element size", fn);
+    HC_REQUIRE(!misaligned(gamma, 4) && !misaligned(beta, 4) && !misaligned(mean, 4) &&
+                   !misaligned(rstd, 4) && !misaligned(count, 4),
+               "%s: misaligned gamma, beta, mean, rstd or count", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    LayerNormArgs a{};
+    a.x = x;
+    a.dt = dt;
+    a.count = count;
+    a.capacity = capacity;
+    a.C = C;
+    a.eps = eps;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.y = y;
+    a.mean_out = mean;
+    a.rstd_out = rstd;
+    return launch_layer_norm_fwd(ctx, a, (cudaStream_t)stream);
+}
+
+hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const int32_t* count,
+                            int capacity, int C, const float* gamma, const float* mean,
+                            const float* rstd, void* dx, float* dgamma, float* dbeta,
+                            hc_stream_t stream) {
+    const char* fn = "hc_layer_norm_bwd";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(dx || dgamma || dbeta, "%s: at least one of dx, dgamma, dbeta is required", fn);
+    HC_REQUIRE(capacity == 0 || (x && dy && mean && rstd),
+               "%s: x, dy, mean and rstd are required", fn);
+    HC_REQUIRE(!misaligned(x, elem_bytes(dt)) && !misaligned(dy, elem_bytes(dt)) &&
+                   !misaligned(dx, elem_bytes(dt)),
+               "%s: x, dy and dx must be aligned to the element size", fn);
+    HC_REQUIRE(!misaligned(gamma, 4) && !misaligned(mean, 4) && !misaligned(rstd, 4) &&
+                   !misaligned(dgamma, 4) && !misaligned(dbeta, 4) && !misaligned(count, 4),
+               "%s: misaligned gamma, mean, rstd, dgamma, dbeta or count", fn);
+    if (capacity == 0 && !dgamma && !dbeta) return HC_OK;
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    LayerNormArgs a{};
+    a.x = x;
+    a.dy = dy;
+    a.dt = dt;
+    a.count = count;
+    a.capacity = capacity;
+    a.C = C;
+    a.gamma = gamma;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.dx = dx;
+    a.dgamma = dgamma;
+    a.dbeta = dbeta;
+    return launch_layer_norm_bwd(ctx, a, (cudaStream_t)stream);
+}
+
+static hc_status check_ids(const char* fn, const int32_t* ids, int ids_stride, int capacity,
+                           int V, const int32_t* count) {
+    HC_REQUIRE(V >= 0, "%s: V=%d must be >= 0", fn, V);
+    HC_REQUIRE(V < 0x7fffffff, "%s: V=%d must be < 2^31 - 1", fn, V);
+    HC_REQUIRE(ids_stride >= 1, "%s: ids_stride=%d must be >= 1", fn, ids_stride);
+    HC_REQUIRE(capacity == 0 || ids, "%s: ids are required", fn);
+    HC_REQUIRE(!misaligned(ids, 4) && !misaligned(count, 4), "%s: misaligned ids or count", fn);
+    return HC_OK;
+}
+
+hc_status hc_embedding_fwd(const void* table, hc_dtype dt, int V, int C, const int32_t* ids,
+                           int ids_stride, const int32_t* count, int capacity, float scale,
+                           void* y, hc_stream_t stream) {
+    const char* fn = "hc_embedding_fwd";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    st = check_ids(fn, ids, ids_stride, capacity, V, count);
+    if (st != HC_OK) return st;
+    if (capacity == 0) return HC_OK;
+    HC_REQUIRE((table || V == 0) && y, "%s: table and y are required", fn);
+    HC_REQUIRE(!misaligned(table, elem_bytes(dt)) && !misaligned(y, elem_bytes(dt)),
+               "%s: table and y must be aligned to the element size", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    EmbeddingArgs a{dt, ids, ids_stride, count, capacity, V, C, scale};
+    return launch_embedding_fwd(ctx, a, table, y, (cudaStream_t)stream);
+}
+
+hc_status hc_embedding_sort(const int32_t* ids, int ids_stride, const int32_t* count, int capacity,
+                            int V, int32_t* row_ptr, int32_t* order, hc_stream_t stream) {
+    const char* fn = "hc_embedding_sort";
+    t_last_error[0] = 0;
+    HC_REQUIRE(capacity >= 0, "%s: capacity=%d must be >= 0", fn, capacity);
+    hc_status st = check_ids(fn, ids, ids_stride, capacity, V, count);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(row_ptr && (order || capacity == 0), "%s: row_ptr and order are required", fn);
+    HC_REQUIRE(!misaligned(row_ptr, 4) && !misaligned(order, 4), "%s: misaligned row_ptr or order",
+               fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    EmbeddingArgs a{HC_F32, ids, ids_stride, count, capacity, V, 0, 0.f};
+    return launch_embedding_sort(ctx, a, row_ptr, order, (cudaStream_t)stream);
+}
+
+hc_status hc_embedding_bwd(const void* dy, hc_dtype dt, const int32_t* row_ptr,
+                           const int32_t* order, int capacity, int V, int C, float scale,
+                           float* dtable, hc_stream_t stream) {
+    const char* fn = "hc_embedding_bwd";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(V >= 0, "%s: V=%d must be >= 0", fn, V);
+    HC_REQUIRE(V < 0x7fffffff, "%s: V=%d must be < 2^31 - 1", fn, V);
+    if (V == 0) return HC_OK;
+    HC_REQUIRE(row_ptr && dtable && (capacity == 0 || (dy && order)),
+               "%s: dy, row_ptr, order and dtable are required", fn);
+    HC_REQUIRE(!misaligned(dy, elem_bytes(dt)) && !misaligned(row_ptr, 4) &&
+                   !misaligned(order, 4) && !misaligned(dtable, 4),
+               "%s: misaligned dy, row_ptr, order or dtable", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    EmbeddingArgs a{dt, nullptr, 1, nullptr, capacity, V, C, scale};
+    return launch_embedding_bwd(ctx, a, dy, row_ptr, order, dtable, (cudaStream_t)stream);
+}
+
+hc_status hc_quantize_fp8_rows(const void* x, hc_dtype dt, const int32_t* count, int capacity,
+                               int C, uint8_t* q, float* scales, hc_stream_t stream) {
+    const char* fn = "hc_quantize_fp8_rows";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(C <= 0x7fffffff - 127, "%s: C=%d is too large", fn, C);
+    if (capacity == 0) return HC_OK;
+    HC_REQUIRE(x && q && scales, "%s: x, q and scales are required", fn);
+    HC_REQUIRE(!misaligned(x, elem_bytes(dt)) && !misaligned(scales, 4) && !misaligned(count, 4),
+               "%s: misaligned x, scales or count", fn);
+    HC_REQUIRE(!misaligned(q, 16), "%s: q must be 16-byte aligned", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    return launch_quantize_fp8_rows(ctx, x, dt, count, capacity, C, q, scales,
+                                    (cudaStream_t)stream);
+}
+
+hc_status hc_quantize_fp8_weight(const void* W, hc_dtype dt, int C_in, int C_out, uint8_t* wq,
+                                 float* ws, hc_stream_t stream) {
+    const char* fn = "hc_quantize_fp8_weight";
+    t_last_error[0] = 0;
+    HC_REQUIRE(dt == HC_F32 || dt == HC_BF16, "%s: unknown dtype %d", fn, (int)dt);
+    HC_REQUIRE(C_in >= 1 && C_out >= 1, "%s: C_in=%d C_out=%d must be >= 1", fn, C_in, C_out);
+    HC_REQUIRE(C_in <= 0x7fffffff - 127 && C_out <= 0x7fffffff - 127,
+               "%s: C_in=%d or C_out=%d is too large", fn, C_in, C_out);
+    HC_REQUIRE(W && wq && ws, "%s: W, wq and ws are required", fn);
+    HC_REQUIRE(!misaligned(W, elem_bytes(dt)) && !misaligned(ws, 4), "%s: misaligned W or ws", fn);
+    HC_REQUIRE(!misaligned(wq, 16), "%s: wq must be 16-byte aligned", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    return launch_quantize_fp8_weight(ctx, W, dt, C_in, C_out, wq, ws, (cudaStream_t)stream);
+}
+
+hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* count, int capacity,
+                            int C_in, int C_out, const uint8_t* wq, const float* ws,
+                            const float* bias, hc_act act, hc_dtype y_dt, void* y,
+                            hc_stream_t stream) {
+    const char* fn = "hc_fp8_linear_fwd";
+    t_last_error[0] = 0;
+    HC_REQUIRE(y_dt == HC_F32 || y_dt == HC_BF16, "%s: unknown dtype %d", fn, (int)y_dt);
+    HC_REQUIRE(act == HC_ACT_NONE || act == HC_ACT_ELU || act == HC_ACT_RELU,
+               "%s: unknown activation %d", fn, (int)act);
+    HC_REQUIRE(capacity >= 0, "%s: capacity=%d must be >= 0", fn, capacity);
+    HC_REQUIRE(C_in >= 1 && C_out >= 1, "%s: C_in=%d C_out=%d must be >= 1", fn, C_in, C_out);
+    HC_REQUIRE(C_in <= 0x7fffffff - 127 && C_out <= 0x7fffffff - 127,
+               "%s: C_in=%d or C_out=%d is too large", fn, C_in, C_out);
+    if (capacity == 0) return HC_OK;
+    HC_REQUIRE(xq && xs && wq && ws && y, "%s: xq, xs, wq, ws and y are required", fn);
+    HC_REQUIRE(!misaligned(xq, 16) && !misaligned(wq, 16), "%s: xq and wq must be 16-byte aligned",
+               fn);
+    HC_REQUIRE(!misaligned(xs, 4) && !misaligned(ws, 4) && !misaligned(bias, 4) &&
+                   !misaligned(count, 4) && !misaligned(y, elem_bytes(y_dt)),
+               "%s: misaligned xs, ws, bias, count or y", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    Fp8LinearArgs a{};
+    a.xq = xq;
+    a.xs = xs;
+    a.wq = wq;
+    a.ws = ws;
+    a.count = count;
+    a.capacity = capacity;
+    a.C_in = C_in;
+    a.C_out = C_out;
+    a.pitch = HC_FP8_PITCH(C_in);
+    a.bias = bias;
+    a.act = (int)act;
+    a.y_dt = y_dt;
+    a.y = y;
+    a.status = ctx->status;
+    return launch_fp8_linear(ctx, a, (cudaStream_t)stream);
+}
+
 hc_status hc_test_set_option(int option, long long value) {
     t_last_error[0] = 0;
     if (option == HC_TEST_GROUP_NORM_PATH) {

@@ -178,6 +178,63 @@ hc_status launch_scatter(const DeviceCtx* ctx, const void* y, int elem_bytes, co
                          const int32_t* row_of, const int32_t* count, int B, int V, int C,
                          int zero_fill, void* out, cudaStream_t s);
 
+// Token operators on compact rows (layer_norm.cu, embedding.cu,
+// fp8_quant.cu, fp8_linear.cu). count NULL = all `capacity` rows.
+struct LayerNormArgs {
+    const void* x;
+    const void* dy;
+    hc_dtype dt;
+    const int32_t* count;
+    int capacity, C;
+    float eps;
+    const float* gamma;
+    const float* beta;
+    void* y;
+    float* mean_out;  // forward
+    float* rstd_out;
+    const float* mean;  // backward
+    const float* rstd;
+    void* dx;
+    float* dgamma;
+    float* dbeta;
+};
+hc_status launch_layer_norm_fwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s);
+hc_status launch_layer_norm_bwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s);
+struct EmbeddingArgs {
+    hc_dtype dt;  // of the table and y, or of dy
+    const int32_t* ids;
+    long long ids_stride;
+    const int32_t* count;
+    int capacity, V, C;
+    float scale;
+};
+hc_status launch_embedding_fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table,
+                               void* y, cudaStream_t s);
+hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, int32_t* row_ptr,
+                                int32_t* order, cudaStream_t s);
+hc_status launch_embedding_bwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* dy,
+                               const int32_t* row_ptr, const int32_t* order, float* dtable,
+                               cudaStream_t s);
+hc_status launch_quantize_fp8_rows(const DeviceCtx* ctx, const void* x, hc_dtype dt,
+                                   const int32_t* count, int capacity, int C, uint8_t* q,
+                                   float* scales, cudaStream_t s);
+hc_status launch_quantize_fp8_weight(const DeviceCtx* ctx, const void* W, hc_dtype dt, int C_in,
+                                     int C_out, uint8_t* wq, float* ws, cudaStream_t s);
+struct Fp8LinearArgs {
+    const uint8_t* xq;  // [capacity, pitch]
+    const float* xs;    // [blocks of C_in, capacity]
+    const uint8_t* wq;  // [C_out, pitch]
+    const float* ws;    // [blocks of C_out, blocks of C_in]
+    const int32_t* count;
+    int capacity, C_in, C_out, pitch;
+    const float* bias;
+    int act;
+    hc_dtype y_dt;
+    void* y;
+    unsigned* status;
+};
+hc_status launch_fp8_linear(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s);
+
 // ------------------------------------------------------------ launches
 // Every kernel of the library is launched with programmatic stream
 // serialisation: it may be scheduled while the previous kernel on the stream

@@ -21,6 +21,7 @@ HC_F32, HC_BF16 = 0, 1
 HC_ACT_NONE, HC_ACT_ELU, HC_ACT_RELU = 0, 1, 2
 HC_LAYOUT_DENSE, HC_LAYOUT_COMPACT = 0, 1
 HC_MAX_SPIRAL = 32
+HC_FP8_BLOCK = 128
 HC_STATIC_MAX_MASK_BYTES = 4096 * 4096
 HC_TEST_GROUP_NORM_PATH, HC_TEST_WAIT_LIMIT_NS = 1, 2
 
@@ -34,8 +35,10 @@ EXPORTS = ("hc_mask_compact", "hc_mask_compact_static", "hc_sparse_spiral_conv_f
            "hc_sparse_conv_rulebook_fwd_hint", "hc_sparse_linear_fwd",
            "hc_sparse_group_norm_fwd", "hc_sparse_conv_gn_fwd", "hc_mask_score_update", "hc_mask_select_topk",
            "hc_kappa_masks", "hc_gather_rows", "hc_conv_rulebook_transpose",
-           "hc_sparse_conv_rulebook_bwd", "hc_scatter_dense", "hc_spiral_conv_fwd", "hc_get_device_status",
-           "hc_test_set_option", "hc_last_error_string", "hc_version")
+           "hc_sparse_conv_rulebook_bwd", "hc_scatter_dense", "hc_spiral_conv_fwd",
+           "hc_layer_norm_fwd", "hc_layer_norm_bwd", "hc_embedding_fwd", "hc_embedding_sort",
+           "hc_embedding_bwd", "hc_quantize_fp8_rows", "hc_quantize_fp8_weight",
+           "hc_fp8_linear_fwd", "hc_get_device_status", "hc_test_set_option", "hc_last_error_string", "hc_version")
 
 
 class HcError(RuntimeError):
@@ -82,6 +85,14 @@ def load_library(path: str | None = None):
             "hc_gather_rows": [P, I, I, I, I, P, P, I, I, P, P],
             "hc_scatter_dense": [P, I, P, P, P, I, I, I, I, P, P],
             "hc_spiral_conv_fwd": [P, I, P, I, I, I, I, I, P, P, I, P, P],
+            "hc_layer_norm_fwd": [P, I, P, I, I, ctypes.c_float, P, P, P, P, P, P],
+            "hc_layer_norm_bwd": [P, P, I, P, I, I, P, P, P, P, P, P, P],
+            "hc_embedding_fwd": [P, I, I, I, P, I, P, I, ctypes.c_float, P, P],
+            "hc_embedding_sort": [P, I, P, I, I, P, P, P],
+            "hc_embedding_bwd": [P, I, P, P, I, I, I, ctypes.c_float, P, P],
+            "hc_quantize_fp8_rows": [P, I, P, I, I, P, P, P],
+            "hc_quantize_fp8_weight": [P, I, I, I, P, P, P],
+            "hc_fp8_linear_fwd": [P, P, P, I, I, I, P, P, P, I, I, P, P],
             "hc_get_device_status": [P],
             "hc_test_set_option": [I, ctypes.c_longlong],
             "hc_last_error_string": [],
@@ -323,6 +334,158 @@ def hc_spiral_conv_fwd(x, spiral, W, bias, act, y, stream=None):
     _check(load_library().hc_spiral_conv_fwd(
         _p(x), _dt(x), _p(spiral), B, V, L, C_in, C_out, _p(W), _p(bias), act, _p(y),
         _s(stream)), "hc_spiral_conv_fwd")
+
+
+def HC_FP8_PITCH(C: int) -> int:
+    """Bytes of a row of C channels in the 8-bit form."""
+    return (C + 15) // 16 * 16
+
+
+def _want(name, t, shape, dtypes):
+    """A token operator's tensor: None passes; else its shape and dtype must match."""
+    if t is None:
+        return
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+
+
+def _token_types():
+    import torch
+    return (torch.float32,), (torch.int32,), (torch.float8_e4m3fn, torch.uint8)
+
+
+def _p_strided(ids):
+    """A one-dimensional device tensor of any positive stride (a column of a matrix)."""
+    if not ids.is_cuda:
+        raise ValueError("libhc takes device tensors")
+    if ids.dim() != 1 or (ids.shape[0] > 1 and ids.stride(0) < 1):
+        raise ValueError("ids must be one-dimensional, with a stride of at least 1")
+    return ctypes.c_void_p(ids.data_ptr()), max(1, ids.stride(0))
+
+
+def hc_layer_norm_fwd(x, eps, gamma, beta, y, mean=None, rstd=None, count=None, stream=None):
+    """Layer norm of every row n < N' of x [capacity, C] (count int32 [1], or None:
+    all rows) into y (may be x); gamma, beta fp32 [C] or None; mean, rstd fp32
+    [capacity] or None."""
+    capacity, C = x.shape
+    f32, i32, _ = _token_types()
+    _want("y", y, (capacity, C), (x.dtype,))
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        _want(name, t, (C,), f32)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _want(name, t, (capacity,), f32)
+    _want("count", count, (1,), i32)
+    _check(load_library().hc_layer_norm_fwd(
+        _p(x), _dt(x), _p(count), capacity, C, float(eps), _p(gamma), _p(beta), _p(y), _p(mean),
+        _p(rstd), _s(stream)), "hc_layer_norm_fwd")
+
+
+def hc_layer_norm_bwd(x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, count=None,
+                      stream=None):
+    """Gradient of hc_layer_norm_fwd: dx like x (may be x or dy) or None; dgamma,
+    dbeta fp32 [C] or None."""
+    capacity, C = x.shape
+    f32, i32, _ = _token_types()
+    for name, t in (("dy", dy), ("dx", dx)):
+        _want(name, t, (capacity, C), (x.dtype,))
+    for name, t in (("gamma", gamma), ("dgamma", dgamma), ("dbeta", dbeta)):
+        _want(name, t, (C,), f32)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _want(name, t, (capacity,), f32)
+    _want("count", count, (1,), i32)
+    _check(load_library().hc_layer_norm_bwd(
+        _p(x), _p(dy), _dt(x), _p(count), capacity, C, _p(gamma), _p(mean), _p(rstd), _p(dx),
+        _p(dgamma), _p(dbeta), _s(stream)), "hc_layer_norm_bwd")
+
+
+def hc_embedding_fwd(table, ids, scale, y, count=None, stream=None):
+    """y[n] = scale * table[ids[n]] (zero for id -1): table [V, C], ids int32
+    [capacity] of any stride (coords[:, 1] for the vertex of every active row),
+    y [capacity, C]."""
+    V, C = table.shape
+    capacity = ids.shape[0]
+    f32, i32, _ = _token_types()
+    _want("ids", ids, (capacity,), i32)
+    _want("y", y, (capacity, C), (table.dtype,))
+    _want("count", count, (1,), i32)
+    ptr, stride = _p_strided(ids)
+    _check(load_library().hc_embedding_fwd(
+        _p(table), _dt(table), V, C, ptr, stride, _p(count), capacity, float(scale), _p(y),
+        _s(stream)), "hc_embedding_fwd")
+
+
+def hc_embedding_sort(ids, V, row_ptr, order, count=None, stream=None):
+    """Token positions by id, stable: row_ptr int32 [V + 1], order int32 [capacity]."""
+    capacity = ids.shape[0]
+    f32, i32, _ = _token_types()
+    _want("ids", ids, (capacity,), i32)
+    _want("row_ptr", row_ptr, (V + 1,), i32)
+    _want("order", order, (capacity,), i32)
+    _want("count", count, (1,), i32)
+    ptr, stride = _p_strided(ids)
+    _check(load_library().hc_embedding_sort(ptr, stride, _p(count), capacity, V, _p(row_ptr),
+                                            _p(order), _s(stream)), "hc_embedding_sort")
+
+
+def hc_embedding_bwd(dy, row_ptr, order, scale, dtable, stream=None):
+    """dtable[v] = scale * sum of the rows of dy [capacity, C] that read v; dtable
+    fp32 [V, C], every row written."""
+    capacity, C = dy.shape
+    V = dtable.shape[0]
+    f32, i32, _ = _token_types()
+    _want("row_ptr", row_ptr, (V + 1,), i32)
+    _want("order", order, (capacity,), i32)
+    _want("dtable", dtable, (V, C), f32)
+    _check(load_library().hc_embedding_bwd(
+        _p(dy), _dt(dy), _p(row_ptr), _p(order), capacity, V, C, float(scale), _p(dtable),
+        _s(stream)), "hc_embedding_bwd")
+
+
+def hc_quantize_fp8_rows(x, q, scales, count=None, stream=None):
+    """Rows of x [capacity, C] in 8 bits: q e4m3 (or uint8) [capacity,
+    HC_FP8_PITCH(C)], scales fp32 [ceil(C / 128), capacity]."""
+    capacity, C = x.shape
+    f32, i32, q8 = _token_types()
+    _want("q", q, (capacity, HC_FP8_PITCH(C)), q8)
+    _want("scales", scales, ((C + 127) // 128, capacity), f32)
+    _want("count", count, (1,), i32)
+    _check(load_library().hc_quantize_fp8_rows(_p(x), _dt(x), _p(count), capacity, C, _p(q),
+                                               _p(scales), _s(stream)), "hc_quantize_fp8_rows")
+
+
+def hc_quantize_fp8_weight(W, wq, ws, stream=None):
+    """A weight W [C_in, C_out] in 8 bits, transposed: wq e4m3 (or uint8) [C_out,
+    HC_FP8_PITCH(C_in)], ws fp32 [ceil(C_out / 128), ceil(C_in / 128)]."""
+    C_in, C_out = W.shape
+    f32, _, q8 = _token_types()
+    _want("wq", wq, (C_out, HC_FP8_PITCH(C_in)), q8)
+    _want("ws", ws, ((C_out + 127) // 128, (C_in + 127) // 128), f32)
+    _check(load_library().hc_quantize_fp8_weight(_p(W), _dt(W), C_in, C_out, _p(wq), _p(ws),
+                                                 _s(stream)), "hc_quantize_fp8_weight")
+
+
+def hc_fp8_linear_fwd(xq, xs, wq, ws, bias, act, y, count=None, stream=None):
+    """8-bit linear layer: xq, xs from hc_quantize_fp8_rows, wq, ws from
+    hc_quantize_fp8_weight (the same C_in), bias fp32 [C_out] or None, y
+    [capacity, C_out] fp32 or bf16. The zero bytes that fill a row up to its
+    pitch add nothing, so the pitch stands for C_in here."""
+    capacity, pitch = xq.shape
+    C_out = wq.shape[0]
+    f32, i32, q8 = _token_types()
+    nb = (pitch + 127) // 128
+    _want("xq", xq, (capacity, HC_FP8_PITCH(pitch)), q8)
+    _want("xs", xs, (nb, capacity), f32)
+    _want("wq", wq, (C_out, pitch), q8)
+    _want("ws", ws, ((C_out + 127) // 128, nb), f32)
+    _want("bias", bias, (C_out,), f32)
+    if tuple(y.shape) != (capacity, C_out):
+        raise ValueError(f"y has shape {tuple(y.shape)}, expected {(capacity, C_out)}")
+    _want("count", count, (1,), i32)
+    _check(load_library().hc_fp8_linear_fwd(
+        _p(xq), _p(xs), _p(count), capacity, pitch, C_out, _p(wq), _p(ws), _p(bias), act, _dt(y),
+        _p(y), _s(stream)), "hc_fp8_linear_fwd")
 
 
 def hc_test_set_option(option: int, value: int):
