@@ -1,99 +1,474 @@
 // The 8-bit linear layer on compact rows:
 //   y[n][o] = act( bias[o] + sum over blocks b of 128 channels of
 //                  xs[b][n] * ws[o / 128][b] * sum_{c in b} xq[n][c] * wq[o][c] )
-// Products of e4m3 values are exact in fp32 and are summed there; a block's
-// sum is scaled in fp32 and added to the fp32 total.
-#include <cuda_fp8.h>
+// on the tensor cores (tcgen05 kind::f8f6f4, e4m3 x e4m3). Products of e4m3
+// values are exact in fp32; a block's 128 products are summed in the TMEM
+// accumulator, then the block sum is scaled and added to the fp32 total in
+// registers ("promotion"): the scales change from block to block, so an
+// accumulator cannot run on over the blocks.
+//
+// A tile is 128 TMEM lanes x BN columns. Two orientations:
+//   rows on lanes (BN = 128 or 256): lane = token, column = output channel.
+//     The scale of a block is one number per thread.
+//   channels on lanes (BN = 16, 32, 64; at most 64 tokens): lane = output
+//     channel, column = token. A few tokens fill a narrow MMA instead of a
+//     mostly empty 128-row tile, and the weight, which is all the traffic of
+//     such a call, is read once, 128 output channels at a time.
+// With fewer tiles than SMs the channel blocks of a tile are split over a
+// cluster of 2, 4 or 8 CTAs, whose totals are added in rank order through
+// distributed shared memory.
+//
+// Warps: 0-7 promote (warp w: TMEM lanes 32 (w % 4) .. + 31, columns half
+// w / 4), 8 loads both operands of a block with TMA (128 bytes of channels =
+// one swizzled row), 9 issues four MMAs (K = 32 each) a block. A block's
+// accumulator is one of 512 / BN (at most 4) TMEM buffers, so the MMAs of
+// the next blocks, and of the next tile, run while this one is promoted.
+// Every mbarrier wait is bounded; on timeout the CTA records HC_ERR_TIMEOUT,
+// waits for its own copies and MMAs and frees its TMEM.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <mutex>
 
 #include "tokens.cuh"
 
 namespace hc {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64;
-constexpr int kStep = 32;  // channels staged at a time
+constexpr int kLanes = 128;                   // TMEM lanes = rows of the first operand
+constexpr int kKB = 128;                      // channels per block = bytes per smem row
+constexpr int kPromoteWarps = 8;
+constexpr int kLoadWarp = kPromoteWarps;
+constexpr int kMmaWarp = kPromoteWarps + 1;
+constexpr int kThreads = (kPromoteWarps + 2) * 32;
+constexpr int kGroupM = 16;                   // token tiles walked per column of tiles
 
-__device__ __forceinline__ float e4m3_value(uint8_t q) {
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw(q, __NV_E4M3)));
+template <int BN>
+struct Cfg {
+    static constexpr int kStageBytes = (kLanes + BN) * kKB;
+    static constexpr int kStages = 196608 / kStageBytes < 10 ? 196608 / kStageBytes : 10;
+    static constexpr int kBufs = 512 / BN < 4 ? 512 / BN : 4;
+    static constexpr uint32_t kTmemCols = kBufs * BN;
+    static constexpr int kCols = BN / 2;      // columns per promoting thread
+    // kind::f8f6f4 instruction descriptor: D fp32 (bit 4), A and B e4m3 (0 at
+    // bits 7 and 10), both K-major, N >> 3 at 17, M >> 4 at 24.
+    static constexpr uint32_t kIdesc =
+        (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kLanes >> 4) << 24);
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 256;
+    // the split totals [BN][128] fp32 reuse the stages
+    static_assert((size_t)kStages * kStageBytes >= (size_t)BN * kLanes * 4, "split totals");
+};
+
+struct KernelArgs {
+    Fp8LinearArgs a;
+    int nkb;    // blocks of channels
+    int split;  // CTAs of a cluster that share a tile's blocks
+};
+
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr) {
+    // K-major, 128-byte swizzle: 8-row groups 1024 bytes apart, version bits
+    // 46-48 = 0b001
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void tc_mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                            uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) {
+    tmem_ld_32x32b_x32(taddr, r);
+}
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// A float at the same shared-memory offset of another CTA of the cluster.
+__device__ __forceinline__ float lds_cluster_f32(uint32_t addr, uint32_t rank) {
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(at) : "memory");
+    return v;
 }
 
-// 64 rows x 64 output channels per block, 4 x 4 per thread.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) fp8_linear_kernel(const Fp8LinearArgs a) {
-    __shared__ float xt[kStep][kTile + 1], wt[kStep][kTile + 1];
+// The tile t of the walk: token tiles in groups of kGroupM, the tiles of a
+// group column by column, so that a wave of CTAs shares both operands in L2.
+__device__ __forceinline__ void tile_at(long long t, int tm, int tn, int& m, int& n) {
+    const long long per = (long long)kGroupM * tn;
+    const int g = (int)(t / per);
+    const int first = g * kGroupM;
+    const int in = tm - first < kGroupM ? tm - first : kGroupM;
+    const int r = (int)(t - (long long)g * per);
+    n = r / in;
+    m = first + (r - n * in);
+}
+
+template <int BN, bool kSwap, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+    fp8_linear_kernel(const KernelArgs k, const __grid_constant__ CUtensorMap map_x,
+                      const __grid_constant__ CUtensorMap map_w) {
+    using C = Cfg<BN>;
+    const Fp8LinearArgs& a = k.a;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t bars = base + C::kStages * C::kStageBytes;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (C::kStages + s); };
+    auto tfull_bar = [&](int b) { return bars + 8u * (2 * C::kStages + b); };
+    auto tempty_bar = [&](int b) { return bars + 8u * (2 * C::kStages + C::kBufs + b); };
+    const uint32_t fin_bar = bars + 8u * (2 * C::kStages + 2 * C::kBufs);
+    uint8_t* const misc =
+        smem_raw + (bars - raw) + 8 * (2 * C::kStages + 2 * C::kBufs + 1);
+    volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(misc);
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(misc + 4);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::kStages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < C::kBufs; ++b) {
+            mbar_init(tfull_bar(b), 1);
+            mbar_init(tempty_bar(b), kPromoteWarps);
+        }
+        mbar_init(fin_bar, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        prefetch_tensormap(&map_x);
+        prefetch_tensormap(&map_w);
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(smem_u32((const void*)tmem_holder), C::kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
     pdl_wait();
     pdl_trigger();
+
     const long long rows = token_rows(a.count, a.capacity, a.status);
-    const long long n0 = (long long)blockIdx.x * kTile;
-    const int o0 = blockIdx.y * kTile;
-    if (n0 >= rows) return;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int nbi = (a.C_in + 127) / 128;
-    float tot[4][4] = {};
-    for (int b = 0; b < nbi; ++b) {
-        float acc[4][4] = {};
-        for (int k0 = b * 128; k0 < b * 128 + 128 && k0 < a.pitch; k0 += kStep) {
-            __syncthreads();
-            for (int j = threadIdx.x; j < kTile * kStep; j += kThreads) {
-                const int r = j / kStep, k = j % kStep;
-                const bool in = k0 + k < a.pitch;
-                xt[k][r] = in && n0 + r < rows ? e4m3_value(a.xq[(n0 + r) * a.pitch + k0 + k]) : 0.f;
-                wt[k][r] = in && o0 + r < a.C_out
-                               ? e4m3_value(a.wq[(long long)(o0 + r) * a.pitch + k0 + k])
-                               : 0.f;
-            }
-            __syncthreads();
-#pragma unroll 8
-            for (int k = 0; k < kStep; ++k) {
-                float xv[4], wv[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    xv[i] = xt[k][ty * 4 + i];
-                    wv[i] = wt[k][tx * 4 + i];
+    const int tm = (int)((rows + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes));
+    const int tn = (a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN);
+    const long long tiles = (long long)tm * tn;
+    const uint32_t rank = k.split > 1 ? cluster_rank() : 0u;
+    const int kb0 = (int)((long long)k.nkb * rank / k.split);
+    const int kb1 = (int)((long long)k.nkb * (rank + 1) / k.split);
+    const long long first = blockIdx.x / k.split, step = gridDim.x / k.split;
+
+    if (warp == kLoadWarp) {
+        if (lane == 0) {
+            long long it = 0;
+            bool ok = true;
+            for (long long t = first; t < tiles && ok; t += step) {
+                int m, n;
+                tile_at(t, tm, tn, m, n);
+                const int ra = (kSwap ? n : m) * kLanes, rb = (kSwap ? m : n) * BN;
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = (int)(it % C::kStages);
+                    const uint32_t ph = (uint32_t)((it / C::kStages) & 1);
+                    if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, a.status)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t st = base + s * C::kStageBytes;
+                    mbar_arrive_expect_tx(full_bar(s), C::kStageBytes);
+                    tma_load_2d(st, kSwap ? &map_w : &map_x, kb * kKB, ra, full_bar(s));
+                    tma_load_2d(st + kLanes * kKB, kSwap ? &map_x : &map_w, kb * kKB, rb,
+                                full_bar(s));
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xv[i], wv[j], acc[i][j]);
             }
+            // after giving up, the copies already issued end before the CTA does
+            if (!ok)
+                for (long long j = it > C::kStages ? it - C::kStages : 0; j < it; ++j)
+                    mbar_wait_drain(full_bar((int)(j % C::kStages)),
+                                    (uint32_t)((j / C::kStages) & 1), a.status);
         }
-        const float w = a.ws[(long long)(o0 / 128) * nbi + b];  // a tile lies in one block of 128
+        __syncwarp();
+    } else if (warp == kMmaWarp) {
+        if (lane == 0) {
+            long long it = 0;
+            bool ok = true;
+            for (long long t = first; t < tiles && ok; t += step) {
+                for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                    const int s = (int)(it % C::kStages), b = (int)(it % C::kBufs);
+                    if (!mbar_wait(tempty_bar(b), (uint32_t)((it / C::kBufs) & 1) ^ 1u, abort_flag,
+                                   a.status) ||
+                        !mbar_wait(full_bar(s), (uint32_t)((it / C::kStages) & 1), abort_flag,
+                                   a.status)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t st = base + s * C::kStageBytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const long long n = n0 + ty * 4 + i;
-            const float sc = n < rows ? a.xs[(long long)b * a.capacity + n] * w : 0.f;
+                    for (int j = 0; j < kKB / 32; ++j)
+                        tc_mma_e4m3(tmem_base + (uint32_t)(b * BN), desc_sw128(st + j * 32),
+                                    desc_sw128(st + kLanes * kKB + j * 32), C::kIdesc, j != 0);
+                    tc_commit(empty_bar(s));
+                    tc_commit(tfull_bar(b));
+                }
+            }
+            // every MMA issued by this thread has completed once fin_bar fires
+            tc_commit(fin_bar);
+            mbar_wait_drain(fin_bar, 0, a.status);
+        }
+        __syncwarp();
+    } else {
+        const int quarter = warp & 3, half = warp >> 2;
+        const uint32_t tm_lane = (uint32_t)(quarter * 32) << 16;
+        constexpr int kChunk = C::kCols < 32 ? C::kCols : 32;
+        T* const y = static_cast<T*>(a.y);
+        const bool wide = !kSwap && a.C_out % (16 / (int)sizeof(T)) == 0 &&
+                          (reinterpret_cast<uintptr_t>(y) & 15) == 0;
+        long long it = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += step) {
+            int m, n;
+            tile_at(t, tm, tn, m, n);
+            float acc[C::kCols];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) tot[i][j] = fmaf(acc[i][j], sc, tot[i][j]);
+            for (int j = 0; j < C::kCols; ++j) acc[j] = 0.f;
+            // rows on lanes: this thread's token, and the block of its channels;
+            // channels on lanes: lane l holds the scale of the half's token l (+ 32)
+            const long long row =
+                kSwap ? (long long)m * BN + half * C::kCols + lane : (long long)m * kLanes + quarter * 32 + lane;
+            const bool row_in = row < rows && (!kSwap || lane < C::kCols);
+            const float* xs = a.xs + (row_in ? row : 0);
+            const int ob = kSwap ? n : (n * BN + half * C::kCols) / kKB;
+            const int nbo = (a.C_out + kKB - 1) / kKB;
+            const float* ws = a.ws + (long long)(ob < nbo ? ob : 0) * k.nkb;
+            auto scale = [&](int kb) {
+                return kb < kb1 && row_in ? xs[(long long)kb * a.capacity] * ws[kb] : 0.f;
+            };
+            float s0 = scale(kb0), s1 = scale(kb0 + 1);
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const int b = (int)(it % C::kBufs);
+                const float s = s0;
+                s0 = s1;
+                s1 = scale(kb + 2);
+                ok = mbar_wait(tfull_bar(b), (uint32_t)((it / C::kBufs) & 1), abort_flag, a.status);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < C::kCols; c += kChunk) {
+                    uint32_t r[kChunk];
+                    tmem_ld(tmem_base + tm_lane + (uint32_t)(b * BN + half * C::kCols + c), r);
+                    tmem_ld_wait();
+                    if (c + kChunk == C::kCols) {
+                        tc_fence_before();
+                        if (lane == 0) mbar_arrive(tempty_bar(b));
+                    }
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j) {
+                        const float sj = kSwap ? __shfl_sync(0xffffffffu, s, c + j) : s;
+                        acc[c + j] = fmaf(__uint_as_float(r[j]), sj, acc[c + j]);
+                    }
+                }
+            }
+            if (!ok || k.split > 1) {
+                if (k.split > 1 && ok) {
+                    // totals of this CTA's blocks into the (now idle) stages
+#pragma unroll
+                    for (int j = 0; j < C::kCols; ++j)
+                        sts_s32(base + (uint32_t)(((half * C::kCols + j) * kLanes + quarter * 32 + lane) * 4),
+                                __float_as_int(acc[j]));
+                }
+                break;  // a split launch has one tile per cluster
+            }
+            if constexpr (kSwap) {
+                const int o = n * kLanes + quarter * 32 + lane;
+                if (o < a.C_out) {
+                    const float bias = a.bias ? a.bias[o] : 0.f;
+#pragma unroll
+                    for (int j = 0; j < C::kCols; ++j) {
+                        const long long nn = (long long)m * BN + half * C::kCols + j;
+                        if (nn < rows)
+                            y[nn * a.C_out + o] = from_f32<T>(act_apply(acc[j] + bias, a.act));
+                    }
+                }
+            } else if (row < rows) {
+                T* const yr = y + row * a.C_out;
+                const int o0 = n * BN + half * C::kCols;
+                constexpr int kV = 16 / (int)sizeof(T);
+#pragma unroll
+                for (int j = 0; j < C::kCols; j += kV) {
+                    alignas(16) T v[kV];
+#pragma unroll
+                    for (int i = 0; i < kV; ++i) {
+                        const int o = o0 + j + i;
+                        v[i] = from_f32<T>(act_apply(
+                            acc[j + i] + (a.bias && o < a.C_out ? __ldg(a.bias + o) : 0.f), a.act));
+                    }
+                    if (wide) {
+                        if (o0 + j < a.C_out)
+                            *reinterpret_cast<uint4*>(yr + o0 + j) = *reinterpret_cast<uint4*>(v);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kV; ++i)
+                            if (o0 + j + i < a.C_out) yr[o0 + j + i] = v[i];
+                    }
+                }
+            }
         }
     }
-    T* y = static_cast<T*>(a.y);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long n = n0 + ty * 4 + i;
-            const int o = o0 + tx * 4 + j;
-            if (n < rows && o < a.C_out)
-                y[n * a.C_out + o] =
-                    from_f32<T>(act_apply(tot[i][j] + (a.bias ? a.bias[o] : 0.f), a.act));
+    if (k.split > 1) {
+        // every CTA of the cluster passes both barriers, whatever happened above
+        cluster_barrier();
+        if (warp < kPromoteWarps && first < tiles && !*abort_flag) {
+            int m, n;
+            tile_at(first, tm, tn, m, n);
+            const int quarter = warp & 3, half = warp >> 2;
+            T* const y = static_cast<T*>(a.y);
+            const int per = C::kCols / k.split;
+            for (int j = 0; j < per; ++j) {
+                const int col = half * C::kCols + (int)rank * per + j;
+                const int ln = quarter * 32 + lane;
+                float v = 0.f;
+                for (int r = 0; r < k.split; ++r)
+                    v += lds_cluster_f32(base + (uint32_t)((col * kLanes + ln) * 4), (uint32_t)r);
+                const long long nn = kSwap ? (long long)m * BN + col : (long long)m * kLanes + ln;
+                const int o = kSwap ? n * kLanes + ln : n * BN + col;
+                if (nn < rows && o < a.C_out)
+                    y[nn * a.C_out + o] =
+                        from_f32<T>(act_apply(v + (a.bias ? a.bias[o] : 0.f), a.act));
+            }
         }
+        cluster_barrier();
+    } else {
+        __syncthreads();
+    }
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, C::kTmemCols);
+    }
+}
+
+// ---------------------------------------------------------------- host side
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                             &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    });
+    return fn;
+}
+
+// A [rows, pitch] byte matrix in boxes of box_rows x 128 bytes, 128-byte
+// swizzle; what lies outside reads as zero.
+hc_status encode(CUtensorMap* m, const void* base, long long rows, int pitch, int box_rows) {
+    auto enc = tensor_map_encoder();
+    if (!enc) {
+        set_error("cuTensorMapEncodeTiled is unavailable");
+        return HC_ERR_CUDA;
+    }
+    cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {kKB, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r =
+        enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_error("cuTensorMapEncodeTiled failed (%d)", (int)r);
+        return HC_ERR_CUDA;
+    }
+    return HC_OK;
+}
+
+template <int BN, bool kSwap, typename T>
+hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
+    using C = Cfg<BN>;
+    KernelArgs k{a, (a.C_in + kKB - 1) / kKB, 1};
+    CUtensorMap mx, mw;
+    hc_status st = encode(&mx, a.xq, a.capacity, a.pitch, kSwap ? BN : kLanes);
+    if (st != HC_OK) return st;
+    st = encode(&mw, a.wq, a.C_out, a.pitch, kSwap ? kLanes : BN);
+    if (st != HC_OK) return st;
+    const long long tiles =
+        (long long)((a.capacity + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes)) *
+        ((a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN));
+    // split while every CTA still gets an SM of its own and two blocks or more
+    while (k.split < 8 && tiles * k.split * 2 <= ctx->num_sms && k.nkb >= 4 * k.split) k.split *= 2;
+    const long long grid =
+        k.split > 1 ? tiles * k.split : (tiles < ctx->num_sms ? tiles : ctx->num_sms);
+    auto kern = fp8_linear_kernel<BN, kSwap, T>;
+    static bool done[64];
+    if (!done[ctx->device]) {
+        st = check_cuda(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)C::kSmem),
+                        "fp8_linear_kernel");
+        if (st != HC_OK) return st;
+        done[ctx->device] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)k.split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kern, k, mx, mw), "fp8_linear_kernel");
+}
+
+template <typename T>
+hc_status dispatch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
+    if (a.capacity <= 16) return launch<16, true, T>(ctx, a, s);
+    if (a.capacity <= 32) return launch<32, true, T>(ctx, a, s);
+    if (a.capacity <= 64) return launch<64, true, T>(ctx, a, s);
+    // 256 output channels a tile once that still gives every SM a tile
+    const long long tiles256 = (long long)((a.capacity + kLanes - 1) / kLanes) * ((a.C_out + 255) / 256);
+    if (a.C_out > 128 && tiles256 >= ctx->num_sms) return launch<256, false, T>(ctx, a, s);
+    return launch<128, false, T>(ctx, a, s);
 }
 
 }  // namespace
 
-hc_status launch_fp8_linear(const DeviceCtx*, const Fp8LinearArgs& a, cudaStream_t s) {
-    const dim3 grid((unsigned)((a.capacity + kTile - 1) / kTile),
-                    (unsigned)((a.C_out + kTile - 1) / kTile));
-    if (grid.y > 65535u) {
-        set_error("hc_fp8_linear_fwd: C_out=%d is too wide", a.C_out);
-        return HC_ERR_UNSUPPORTED;
-    }
-    return a.y_dt == HC_BF16
-               ? launch_pdl(fp8_linear_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s,
-                            "fp8_linear_kernel", a)
-               : launch_pdl(fp8_linear_kernel<float>, grid, dim3(kThreads), 0, s,
-                            "fp8_linear_kernel", a);
+hc_status launch_fp8_linear(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
+    return a.y_dt == HC_BF16 ? dispatch<__nv_bfloat16>(ctx, a, s) : dispatch<float>(ctx, a, s);
 }
 
 }  // namespace hc
