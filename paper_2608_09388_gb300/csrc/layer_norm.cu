@@ -15,6 +15,205 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// ---------------------------------------------------------------- rows in registers
+// A group of TPR threads holds a whole row: NV pieces of VEC elements each,
+// piece i of thread t at channel (i * TPR + t) * VEC. The row is read once;
+// the next row of the group is loaded before this one is worked on, so that
+// loads are in flight throughout. Groups stride over the rows.
+constexpr int kGroupThreads = 512;  // threads per block: kGroupThreads / TPR groups
+
+template <typename T, int VEC, int TPR, int NV>
+__global__ void __launch_bounds__(kGroupThreads)
+    ln_fwd_rows_kernel(const T* x, const int32_t* count, long long capacity, int C, float eps,
+                       const float* __restrict__ gamma, const float* __restrict__ beta, T* y,
+                       float* mean_out, float* rstd_out, unsigned* status) {
+    __shared__ float sh[2 * kGroupThreads / 32];
+    pdl_wait();
+    pdl_trigger();
+    const long long rows = token_rows(count, capacity, status);
+    constexpr int kGroups = kGroupThreads / TPR;
+    const int t = threadIdx.x % TPR;
+    const long long step = (long long)gridDim.x * kGroups;
+    // every thread of a warp takes part in the shuffles: groups of a warp run
+    // the same number of rounds
+    const long long n0 = (long long)blockIdx.x * kGroups + threadIdx.x / TPR;
+    const long long w0 = TPR < 32 ? n0 - (threadIdx.x & 31) / TPR : n0;
+    Piece<T, VEC> cur[NV], nxt[NV];
+    float ga[NV * VEC], be[NV * VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * VEC;
+        if (n0 < rows && c < C) nxt[i].load(x + n0 * C + c);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            ga[i * VEC + e] = gamma && c < C ? __ldg(gamma + c + e) : 1.f;
+            be[i * VEC + e] = beta && c < C ? __ldg(beta + c + e) : 0.f;
+        }
+    }
+    for (long long w = w0, n = n0; w < rows; w += step, n += step) {
+        const bool in = n < rows;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            cur[i] = nxt[i];
+            const int c = (i * TPR + t) * VEC;
+            if (n + step < rows && c < C) nxt[i].load(x + (n + step) * C + c);
+            if (c < C)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s += cur[i].get(e);
+        }
+        // a quotient, not a product with 1 / C: the mean of a constant row is
+        // then its value, and its differences are zero
+        const float mean = group_sum<TPR>(s, sh, 0) / (float)C;
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((i * TPR + t) * VEC < C)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = cur[i].get(e) - mean;
+                    v += d * d;
+                }
+        const float rstd = 1.f / sqrtf(group_sum<TPR>(v, sh, 1) / (float)C + eps);
+        if (!in) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * VEC;
+            if (c < C) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float xh = (cur[i].get(e) - mean) * rstd;
+                    cur[i].set(e, xh * ga[i * VEC + e] + be[i * VEC + e]);
+                }
+                cur[i].store(y + n * C + c);
+            }
+        }
+        if (t == 0) {
+            if (mean_out) mean_out[n] = mean;
+            if (rstd_out) rstd_out[n] = rstd;
+        }
+    }
+}
+
+// The gradient in the same layout. A thread owns its channels for all its
+// rows, so dgamma and dbeta are summed in registers; the groups of a block
+// are added in shared memory in order, the blocks by ln_param_grad_kernel.
+template <typename T, int VEC, int TPR, int NV>
+__global__ void __launch_bounds__(kGroupThreads)
+    ln_bwd_rows_in_regs_kernel(const T* x, const T* dy, const int32_t* count, long long capacity,
+                               int C, const float* __restrict__ gamma,
+                               const float* __restrict__ mean, const float* __restrict__ rstd,
+                               T* dx, float* __restrict__ part, unsigned* status) {
+    __shared__ float sh[2 * kGroupThreads / 32];
+    extern __shared__ float psum[];  // [2][C] when the block has several groups
+    pdl_wait();
+    pdl_trigger();
+    const long long rows = token_rows(count, capacity, status);
+    constexpr int kGroups = kGroupThreads / TPR;
+    const int t = threadIdx.x % TPR;
+    const long long step = (long long)gridDim.x * kGroups;
+    const long long n0 = (long long)blockIdx.x * kGroups + threadIdx.x / TPR;
+    const long long w0 = TPR < 32 ? n0 - (threadIdx.x & 31) / TPR : n0;
+    const float inv = 1.f / (float)C;
+    Piece<T, VEC> cx[NV], cd[NV], nx[NV], nd[NV];
+    float m1 = 0.f, r1 = 0.f;
+    float ga[NV * VEC], dg[NV * VEC], db[NV * VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            ga[i * VEC + e] = gamma && c < C ? __ldg(gamma + c + e) : 1.f;
+            dg[i * VEC + e] = db[i * VEC + e] = 0.f;
+        }
+        if (n0 < rows && c < C) {
+            nx[i].load(x + n0 * C + c);
+            nd[i].load(dy + n0 * C + c);
+        }
+    }
+    if (n0 < rows) {
+        m1 = mean[n0];
+        r1 = rstd[n0];
+    }
+    for (long long w = w0, n = n0; w < rows; w += step, n += step) {
+        const bool in = n < rows, more = n + step < rows;
+        const float m = m1, r = r1;
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * VEC;
+            cx[i] = nx[i];
+            cd[i] = nd[i];
+            if (more && c < C) {
+                nx[i].load(x + (n + step) * C + c);
+                nd[i].load(dy + (n + step) * C + c);
+            }
+        }
+        if (more) {
+            m1 = mean[n + step];
+            r1 = rstd[n + step];
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (in && (i * TPR + t) * VEC < C)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = cd[i].get(e), xh = (cx[i].get(e) - m) * r;
+                    const float g = d * ga[i * VEC + e];
+                    s1 += g;
+                    s2 += g * xh;
+                    dg[i * VEC + e] += d * xh;
+                    db[i * VEC + e] += d;
+                }
+        if (dx == nullptr) continue;
+        const float c1 = group_sum<TPR>(s1, sh, 0) * inv;
+        const float c2 = group_sum<TPR>(s2, sh, 1) * inv;
+        if (!in) continue;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * VEC;
+            if (c < C) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float xh = (cx[i].get(e) - m) * r;
+                    cx[i].set(e, (cd[i].get(e) * ga[i * VEC + e] - c1 - xh * c2) * r);
+                }
+                cx[i].store(dx + n * C + c);
+            }
+        }
+    }
+    if (part == nullptr) return;
+    float* const out = part + 2ll * blockIdx.x * C;
+    if constexpr (kGroups > 1) {
+        for (int g = 0; g < kGroups; ++g) {
+            if ((int)threadIdx.x / TPR == g)
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const int c = (i * TPR + t) * VEC + e;
+                        if (c < C) {
+                            psum[c] = (g ? psum[c] : 0.f) + dg[i * VEC + e];
+                            psum[C + c] = (g ? psum[C + c] : 0.f) + db[i * VEC + e];
+                        }
+                    }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * C; c += kGroupThreads) out[c] = psum[c];
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const int c = (i * TPR + t) * VEC + e;
+                if (c < C) {
+                    out[c] = dg[i * VEC + e];
+                    out[C + c] = db[i * VEC + e];
+                }
+            }
+    }
+}
+
 // ---------------------------------------------------------------- any width
 // A block per row; the row is read once for the mean, once for the variance
 // and once for the output (the second and third time from the caches).
@@ -107,25 +306,74 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
-// dgamma and dbeta: a thread per channel adds the blocks' sums in order.
-__global__ void __launch_bounds__(kThreads)
+// dgamma and dbeta from the blocks' sums part[parts][2][C]: 32 values per
+// block, 32 warps adding every 32nd part in order, then the warps in order.
+constexpr int kGradWarps = 32;
+
+__global__ void __launch_bounds__(kGradWarps * 32)
     ln_param_grad_kernel(const float* __restrict__ part, int parts, int C, float* dgamma,
                          float* dbeta) {
+    __shared__ float sh[kGradWarps][33];
     pdl_wait();
     pdl_trigger();
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= C) return;
-    float dg = 0.f, db = 0.f;
-    for (int p = 0; p < parts; ++p) {
-        dg += part[(2ll * p) * C + c];
-        db += part[(2ll * p + 1) * C + c];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = blockIdx.x * 32 + lane;  // of the 2 * C sums of a part
+    float v = 0.f;
+    if (c < 2 * C) {
+#pragma unroll 8
+        for (int p = warp; p < parts; p += kGradWarps) v += part[2ll * p * C + c];
     }
-    if (dgamma) dgamma[c] = dg;
-    if (dbeta) dbeta[c] = db;
+    sh[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && c < 2 * C) {
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kGradWarps; ++w) v += sh[w][lane];
+        float* const out = c < C ? dgamma : dbeta;
+        if (out) out[c < C ? c : c - C] = v;
+    }
+}
+
+hc_status param_grad(const LayerNormArgs& a, const float* part, int parts, cudaStream_t s) {
+    const unsigned grid = (unsigned)((2ll * a.C + 31) / 32);
+    return launch_pdl(ln_param_grad_kernel, dim3(grid), dim3(kGradWarps * 32), 0, s,
+                      "ln_param_grad_kernel", part, parts, a.C, a.dgamma, a.dbeta);
+}
+
+template <typename T, int VEC, int TPR, int NV>
+hc_status fwd_rows(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
+    constexpr int kGroups = kGroupThreads / TPR;
+    const long long need = ((long long)a.capacity + kGroups - 1) / kGroups;
+    const long long cap = (long long)ctx->num_sms * 2;  // resident at up to 64 registers
+    return launch_pdl(ln_fwd_rows_kernel<T, VEC, TPR, NV>,
+                      dim3((unsigned)(need < cap ? need : cap)), dim3(kGroupThreads), 0, s,
+                      "ln_fwd_rows_kernel", (const T*)a.x, a.count, (long long)a.capacity, a.C,
+                      a.eps, a.gamma, a.beta, (T*)a.y, a.mean_out, a.rstd_out, ctx->status);
+}
+
+template <typename T, int VEC, int TPR, int NV>
+hc_status bwd_rows(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
+    constexpr int kGroups = kGroupThreads / TPR;
+    const long long need = ((long long)a.capacity + kGroups - 1) / kGroups;
+    const long long cap = (long long)ctx->num_sms;
+    const int grid = (int)(need < 1 ? 1 : need < cap ? need : cap);
+    const bool params = a.dgamma || a.dbeta;
+    float* part = nullptr;
+    if (params) {
+        part = (float*)stream_workspace(s, (size_t)grid * a.C * 8);
+        if (!part) return HC_ERR_CUDA;
+    }
+    const size_t smem = kGroups > 1 && params ? (size_t)a.C * 8 : 0;
+    hc_status st = launch_pdl(ln_bwd_rows_in_regs_kernel<T, VEC, TPR, NV>, dim3((unsigned)grid),
+                              dim3(kGroupThreads), smem, s, "ln_bwd_rows_in_regs_kernel",
+                              (const T*)a.x, (const T*)a.dy, a.count, (long long)a.capacity, a.C,
+                              a.gamma, a.mean, a.rstd, (T*)a.dx, part, ctx->status);
+    if (st != HC_OK || !params) return st;
+    return param_grad(a, part, grid, s);
 }
 
 template <typename T>
-hc_status fwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
+hc_status fwd_wide(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
     const long long cap = (long long)ctx->num_sms * 8;
     const unsigned grid = (unsigned)(a.capacity < cap ? a.capacity : cap);
     return launch_pdl(ln_fwd_kernel<T>, dim3(grid), dim3(kThreads), 0, s, "ln_fwd_kernel",
@@ -134,7 +382,7 @@ hc_status fwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
 }
 
 template <typename T>
-hc_status bwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
+hc_status bwd_wide(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
     const bool params = a.dgamma || a.dbeta;
     const unsigned ctiles = (unsigned)((a.C + kThreads - 1) / kThreads);
     long long parts = (ctx->num_sms * 8 + ctiles - 1) / ctiles;
@@ -158,19 +406,49 @@ hc_status bwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
                     (long long)a.capacity, a.C, a.gamma, a.mean, a.rstd, (const float*)ws,
                     (T*)a.dx, part, ctx->status);
     if (st != HC_OK || !params) return st;
-    return launch_pdl(ln_param_grad_kernel, dim3(ctiles), dim3(kThreads), 0, s,
-                      "ln_param_grad_kernel", (const float*)part, (int)parts, a.C, a.dgamma,
-                      a.dbeta);
+    return param_grad(a, part, (int)parts, s);
+}
+
+template <typename T, int VEC, int TPR, int NV>
+hc_status rows_in_regs(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStream_t s) {
+    return back ? bwd_rows<T, VEC, TPR, NV>(ctx, a, s) : fwd_rows<T, VEC, TPR, NV>(ctx, a, s);
+}
+
+// Rows of at most 8192 channels are held in registers, by the smallest group
+// that does so with two 16-byte pieces a thread (the gradient keeps two rows'
+// pieces, gamma and both sums of every channel); wider rows go through the
+// caches.
+template <typename T>
+hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStream_t s) {
+    constexpr int kVec = 16 / (int)sizeof(T);
+    const int C = a.C;
+    auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    if (C > 8192) return back ? bwd_wide<T>(ctx, a, s) : fwd_wide<T>(ctx, a, s);
+    if (C % kVec == 0 && aligned(a.x) && aligned(a.y) && aligned(a.dy) && aligned(a.dx)) {
+        if (C <= 8 * kVec) return rows_in_regs<T, kVec, 8, 1>(ctx, a, back, s);
+        if (C <= 32 * kVec) return rows_in_regs<T, kVec, 32, 1>(ctx, a, back, s);
+        if (C <= 64 * kVec) return rows_in_regs<T, kVec, 32, 2>(ctx, a, back, s);
+        if (C <= 128 * kVec) return rows_in_regs<T, kVec, 128, 1>(ctx, a, back, s);
+        if (C <= 256 * kVec) return rows_in_regs<T, kVec, 128, 2>(ctx, a, back, s);
+        if (C <= 512 * kVec) return rows_in_regs<T, kVec, 256, 2>(ctx, a, back, s);
+        if (C <= 1024 * kVec) return rows_in_regs<T, kVec, 512, 2>(ctx, a, back, s);
+        if constexpr (kVec == 4) return rows_in_regs<T, kVec, 512, 4>(ctx, a, back, s);
+    }
+    if (C <= 32) return rows_in_regs<T, 1, 8, 4>(ctx, a, back, s);
+    if (C <= 256) return rows_in_regs<T, 1, 32, 8>(ctx, a, back, s);
+    if (C <= 1024) return rows_in_regs<T, 1, 128, 8>(ctx, a, back, s);
+    if (C <= 4096) return rows_in_regs<T, 1, 512, 8>(ctx, a, back, s);
+    return rows_in_regs<T, 1, 512, 16>(ctx, a, back, s);
 }
 
 }  // namespace
 
 hc_status launch_layer_norm_fwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
-    return a.dt == HC_BF16 ? fwd<__nv_bfloat16>(ctx, a, s) : fwd<float>(ctx, a, s);
+    return a.dt == HC_BF16 ? run<__nv_bfloat16>(ctx, a, false, s) : run<float>(ctx, a, false, s);
 }
 
 hc_status launch_layer_norm_bwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
-    return a.dt == HC_BF16 ? bwd<__nv_bfloat16>(ctx, a, s) : bwd<float>(ctx, a, s);
+    return a.dt == HC_BF16 ? run<__nv_bfloat16>(ctx, a, true, s) : run<float>(ctx, a, true, s);
 }
 
 }  // namespace hc

@@ -51,6 +51,75 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// A piece of a row: VEC elements of T as loaded (16 bytes, or one element).
+template <typename T, int VEC>
+struct Piece;
+template <typename T>
+struct Piece<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T* p) { v = *p; }
+    __device__ __forceinline__ void store(T* p) const { *p = v; }
+    __device__ __forceinline__ float get(int) const { return to_f32(v); }
+    __device__ __forceinline__ void set(int, float f) { v = from_f32<T>(f); }
+};
+template <>
+struct Piece<float, 4> {
+    float4 v;
+    __device__ __forceinline__ void load(const float* p) { v = *reinterpret_cast<const float4*>(p); }
+    __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<float4*>(p) = v; }
+    __device__ __forceinline__ float get(int i) const {
+        return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+    }
+    __device__ __forceinline__ void set(int i, float f) {
+        (i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w) = f;
+    }
+};
+template <>
+struct Piece<__nv_bfloat16, 8> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        v = *reinterpret_cast<const uint4*>(p);
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const {
+        *reinterpret_cast<uint4*>(p) = v;
+    }
+    __device__ __forceinline__ uint32_t word(int i) const {
+        return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+    }
+    // bf16 is the upper half of an fp32
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t w = word(i >> 1);
+        return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    }
+    __device__ __forceinline__ void set(int i, float f) {
+        const uint32_t b = __bfloat16_as_ushort(__float2bfloat16_rn(f));
+        uint32_t& w = (i >> 1) == 0 ? v.x : (i >> 1) == 1 ? v.y : (i >> 1) == 2 ? v.z : v.w;
+        w = i & 1 ? (w & 0xffffu) | b << 16 : (w & 0xffff0000u) | b;
+    }
+};
+
+// Sum over a group of TPR threads (a power of two; group g of the block owns
+// threads g * TPR ..), the same value in each of them. A group of several
+// warps passes the warps' sums through sh, [2][warps of the block] floats
+// used in turn (`turn` 0, 1, 0, ..), so that one barrier a call is enough.
+template <int TPR>
+__device__ __forceinline__ float group_sum(float v, float* sh, int turn) {
+#pragma unroll
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1)
+        v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+        constexpr int kWarps = TPR / 32;
+        const int g = threadIdx.x / TPR;
+        float* const at = sh + (turn ? blockDim.x / 32 : 0) + g * kWarps;
+        if ((threadIdx.x & 31) == 0) at[(threadIdx.x % TPR) >> 5] = v;
+        asm volatile("bar.sync %0, %1;\n" ::"r"(g + 1), "r"(TPR) : "memory");
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) v += at[w];
+    }
+    return v;
+}
+
 // Sum over the block, the same value in every thread; sh holds one float per
 // warp and is free again when the next call's first barrier has been passed.
 __device__ __forceinline__ float block_sum(float v, float* sh) {

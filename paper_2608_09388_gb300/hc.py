@@ -38,7 +38,8 @@ EXPORTS = ("hc_mask_compact", "hc_mask_compact_static", "hc_sparse_spiral_conv_f
            "hc_sparse_conv_rulebook_bwd", "hc_scatter_dense", "hc_spiral_conv_fwd",
            "hc_layer_norm_fwd", "hc_layer_norm_bwd", "hc_embedding_fwd", "hc_embedding_sort",
            "hc_embedding_bwd", "hc_quantize_fp8_rows", "hc_quantize_fp8_weight",
-           "hc_fp8_linear_fwd", "hc_get_device_status", "hc_test_set_option", "hc_last_error_string", "hc_version")
+           "hc_fp8_linear_fwd", "hc_get_device_status", "hc_test_set_option",
+           "hc_last_error_string", "hc_version")
 
 
 class HcError(RuntimeError):
@@ -127,9 +128,11 @@ def _p_host_ok(t):
 
 
 def _s(stream):
-    import torch
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # the current stream's handle itself: building the Stream object that
+        # torch.cuda.current_stream() returns takes longer than a launch
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
@@ -341,28 +344,45 @@ def HC_FP8_PITCH(C: int) -> int:
     return (C + 15) // 16 * 16
 
 
-def _want(name, t, shape, dtypes):
-    """A token operator's tensor: None passes; else its shape and dtype must match."""
-    if t is None:
-        return
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+_types = None
 
 
 def _token_types():
-    import torch
-    return (torch.float32,), (torch.int32,), (torch.float8_e4m3fn, torch.uint8)
+    """(fp32, int32, 8-bit, row) dtypes that the token operators take."""
+    global _types
+    if _types is None:
+        import torch
+        _types = ((torch.float32,), (torch.int32,), (torch.float8_e4m3fn, torch.uint8),
+                  (torch.float32, torch.bfloat16))
+    return _types
 
 
-def _p_strided(ids):
-    """A one-dimensional device tensor of any positive stride (a column of a matrix)."""
+def _arg(name, t, shape, dtypes):
+    """Address of a token operator's tensor, once its shape, dtype and memory
+    are what the call needs; None passes."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if not t.is_cuda:
+        raise ValueError("libhc takes device tensors")
+    if not t.is_contiguous():
+        raise ValueError("libhc takes contiguous tensors")
+    return t.data_ptr()
+
+
+def _arg_ids(ids):
+    """Address and stride of a one-dimensional int32 tensor (a column of a matrix has one above 1)."""
+    if ids.dim() != 1 or ids.dtype != _token_types()[1][0]:
+        raise ValueError("ids must be one-dimensional int32")
     if not ids.is_cuda:
         raise ValueError("libhc takes device tensors")
-    if ids.dim() != 1 or (ids.shape[0] > 1 and ids.stride(0) < 1):
-        raise ValueError("ids must be one-dimensional, with a stride of at least 1")
-    return ctypes.c_void_p(ids.data_ptr()), max(1, ids.stride(0))
+    stride = ids.stride(0) if ids.shape[0] > 1 else 1
+    if stride < 1:
+        raise ValueError("ids must have a stride of at least 1")
+    return ids.data_ptr(), stride
 
 
 def hc_layer_norm_fwd(x, eps, gamma, beta, y, mean=None, rstd=None, count=None, stream=None):
@@ -370,16 +390,13 @@ def hc_layer_norm_fwd(x, eps, gamma, beta, y, mean=None, rstd=None, count=None, 
     all rows) into y (may be x); gamma, beta fp32 [C] or None; mean, rstd fp32
     [capacity] or None."""
     capacity, C = x.shape
-    f32, i32, _ = _token_types()
-    _want("y", y, (capacity, C), (x.dtype,))
-    for name, t in (("gamma", gamma), ("beta", beta)):
-        _want(name, t, (C,), f32)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _want(name, t, (capacity,), f32)
-    _want("count", count, (1,), i32)
+    f32, i32, _, row = _token_types()
+    same = (x.dtype,)
     _check(load_library().hc_layer_norm_fwd(
-        _p(x), _dt(x), _p(count), capacity, C, float(eps), _p(gamma), _p(beta), _p(y), _p(mean),
-        _p(rstd), _s(stream)), "hc_layer_norm_fwd")
+        _arg("x", x, (capacity, C), row), _dt(x), _arg("count", count, (1,), i32), capacity, C,
+        eps, _arg("gamma", gamma, (C,), f32), _arg("beta", beta, (C,), f32),
+        _arg("y", y, (capacity, C), same), _arg("mean", mean, (capacity,), f32),
+        _arg("rstd", rstd, (capacity,), f32), _s(stream)), "hc_layer_norm_fwd")
 
 
 def hc_layer_norm_bwd(x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None, count=None,
@@ -387,17 +404,14 @@ def hc_layer_norm_bwd(x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None
     """Gradient of hc_layer_norm_fwd: dx like x (may be x or dy) or None; dgamma,
     dbeta fp32 [C] or None."""
     capacity, C = x.shape
-    f32, i32, _ = _token_types()
-    for name, t in (("dy", dy), ("dx", dx)):
-        _want(name, t, (capacity, C), (x.dtype,))
-    for name, t in (("gamma", gamma), ("dgamma", dgamma), ("dbeta", dbeta)):
-        _want(name, t, (C,), f32)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _want(name, t, (capacity,), f32)
-    _want("count", count, (1,), i32)
+    f32, i32, _, row = _token_types()
+    same = (x.dtype,)
     _check(load_library().hc_layer_norm_bwd(
-        _p(x), _p(dy), _dt(x), _p(count), capacity, C, _p(gamma), _p(mean), _p(rstd), _p(dx),
-        _p(dgamma), _p(dbeta), _s(stream)), "hc_layer_norm_bwd")
+        _arg("x", x, (capacity, C), row), _arg("dy", dy, (capacity, C), same), _dt(x),
+        _arg("count", count, (1,), i32), capacity, C, _arg("gamma", gamma, (C,), f32),
+        _arg("mean", mean, (capacity,), f32), _arg("rstd", rstd, (capacity,), f32),
+        _arg("dx", dx, (capacity, C), same), _arg("dgamma", dgamma, (C,), f32),
+        _arg("dbeta", dbeta, (C,), f32), _s(stream)), "hc_layer_norm_bwd")
 
 
 def hc_embedding_fwd(table, ids, scale, y, count=None, stream=None):
@@ -405,28 +419,24 @@ def hc_embedding_fwd(table, ids, scale, y, count=None, stream=None):
     [capacity] of any stride (coords[:, 1] for the vertex of every active row),
     y [capacity, C]."""
     V, C = table.shape
+    ptr, stride = _arg_ids(ids)
     capacity = ids.shape[0]
-    f32, i32, _ = _token_types()
-    _want("ids", ids, (capacity,), i32)
-    _want("y", y, (capacity, C), (table.dtype,))
-    _want("count", count, (1,), i32)
-    ptr, stride = _p_strided(ids)
+    _, i32, _, row = _token_types()
     _check(load_library().hc_embedding_fwd(
-        _p(table), _dt(table), V, C, ptr, stride, _p(count), capacity, float(scale), _p(y),
-        _s(stream)), "hc_embedding_fwd")
+        _arg("table", table, (V, C), row), _dt(table), V, C, ptr, stride,
+        _arg("count", count, (1,), i32), capacity, scale,
+        _arg("y", y, (capacity, C), (table.dtype,)), _s(stream)), "hc_embedding_fwd")
 
 
 def hc_embedding_sort(ids, V, row_ptr, order, count=None, stream=None):
     """Token positions by id, stable: row_ptr int32 [V + 1], order int32 [capacity]."""
+    ptr, stride = _arg_ids(ids)
     capacity = ids.shape[0]
-    f32, i32, _ = _token_types()
-    _want("ids", ids, (capacity,), i32)
-    _want("row_ptr", row_ptr, (V + 1,), i32)
-    _want("order", order, (capacity,), i32)
-    _want("count", count, (1,), i32)
-    ptr, stride = _p_strided(ids)
-    _check(load_library().hc_embedding_sort(ptr, stride, _p(count), capacity, V, _p(row_ptr),
-                                            _p(order), _s(stream)), "hc_embedding_sort")
+    i32 = _token_types()[1]
+    _check(load_library().hc_embedding_sort(
+        ptr, stride, _arg("count", count, (1,), i32), capacity, V,
+        _arg("row_ptr", row_ptr, (V + 1,), i32), _arg("order", order, (capacity,), i32),
+        _s(stream)), "hc_embedding_sort")
 
 
 def hc_embedding_bwd(dy, row_ptr, order, scale, dtable, stream=None):
@@ -434,36 +444,35 @@ def hc_embedding_bwd(dy, row_ptr, order, scale, dtable, stream=None):
     fp32 [V, C], every row written."""
     capacity, C = dy.shape
     V = dtable.shape[0]
-    f32, i32, _ = _token_types()
-    _want("row_ptr", row_ptr, (V + 1,), i32)
-    _want("order", order, (capacity,), i32)
-    _want("dtable", dtable, (V, C), f32)
+    f32, i32, _, row = _token_types()
     _check(load_library().hc_embedding_bwd(
-        _p(dy), _dt(dy), _p(row_ptr), _p(order), capacity, V, C, float(scale), _p(dtable),
-        _s(stream)), "hc_embedding_bwd")
+        _arg("dy", dy, (capacity, C), row), _dt(dy), _arg("row_ptr", row_ptr, (V + 1,), i32),
+        _arg("order", order, (capacity,), i32), capacity, V, C, scale,
+        _arg("dtable", dtable, (V, C), f32), _s(stream)), "hc_embedding_bwd")
 
 
 def hc_quantize_fp8_rows(x, q, scales, count=None, stream=None):
     """Rows of x [capacity, C] in 8 bits: q e4m3 (or uint8) [capacity,
     HC_FP8_PITCH(C)], scales fp32 [ceil(C / 128), capacity]."""
     capacity, C = x.shape
-    f32, i32, q8 = _token_types()
-    _want("q", q, (capacity, HC_FP8_PITCH(C)), q8)
-    _want("scales", scales, ((C + 127) // 128, capacity), f32)
-    _want("count", count, (1,), i32)
-    _check(load_library().hc_quantize_fp8_rows(_p(x), _dt(x), _p(count), capacity, C, _p(q),
-                                               _p(scales), _s(stream)), "hc_quantize_fp8_rows")
+    f32, i32, q8, row = _token_types()
+    _check(load_library().hc_quantize_fp8_rows(
+        _arg("x", x, (capacity, C), row), _dt(x), _arg("count", count, (1,), i32), capacity, C,
+        _arg("q", q, (capacity, HC_FP8_PITCH(C)), q8),
+        _arg("scales", scales, ((C + 127) // 128, capacity), f32), _s(stream)),
+        "hc_quantize_fp8_rows")
 
 
 def hc_quantize_fp8_weight(W, wq, ws, stream=None):
     """A weight W [C_in, C_out] in 8 bits, transposed: wq e4m3 (or uint8) [C_out,
     HC_FP8_PITCH(C_in)], ws fp32 [ceil(C_out / 128), ceil(C_in / 128)]."""
     C_in, C_out = W.shape
-    f32, _, q8 = _token_types()
-    _want("wq", wq, (C_out, HC_FP8_PITCH(C_in)), q8)
-    _want("ws", ws, ((C_out + 127) // 128, (C_in + 127) // 128), f32)
-    _check(load_library().hc_quantize_fp8_weight(_p(W), _dt(W), C_in, C_out, _p(wq), _p(ws),
-                                                 _s(stream)), "hc_quantize_fp8_weight")
+    f32, _, q8, row = _token_types()
+    _check(load_library().hc_quantize_fp8_weight(
+        _arg("W", W, (C_in, C_out), row), _dt(W), C_in, C_out,
+        _arg("wq", wq, (C_out, HC_FP8_PITCH(C_in)), q8),
+        _arg("ws", ws, ((C_out + 127) // 128, (C_in + 127) // 128), f32), _s(stream)),
+        "hc_quantize_fp8_weight")
 
 
 def hc_fp8_linear_fwd(xq, xs, wq, ws, bias, act, y, count=None, stream=None):
@@ -473,19 +482,14 @@ def hc_fp8_linear_fwd(xq, xs, wq, ws, bias, act, y, count=None, stream=None):
     pitch add nothing, so the pitch stands for C_in here."""
     capacity, pitch = xq.shape
     C_out = wq.shape[0]
-    f32, i32, q8 = _token_types()
+    f32, i32, q8, row = _token_types()
     nb = (pitch + 127) // 128
-    _want("xq", xq, (capacity, HC_FP8_PITCH(pitch)), q8)
-    _want("xs", xs, (nb, capacity), f32)
-    _want("wq", wq, (C_out, pitch), q8)
-    _want("ws", ws, ((C_out + 127) // 128, nb), f32)
-    _want("bias", bias, (C_out,), f32)
-    if tuple(y.shape) != (capacity, C_out):
-        raise ValueError(f"y has shape {tuple(y.shape)}, expected {(capacity, C_out)}")
-    _want("count", count, (1,), i32)
     _check(load_library().hc_fp8_linear_fwd(
-        _p(xq), _p(xs), _p(count), capacity, pitch, C_out, _p(wq), _p(ws), _p(bias), act, _dt(y),
-        _p(y), _s(stream)), "hc_fp8_linear_fwd")
+        _arg("xq", xq, (capacity, HC_FP8_PITCH(pitch)), q8), _arg("xs", xs, (nb, capacity), f32),
+        _arg("count", count, (1,), i32), capacity, pitch, C_out,
+        _arg("wq", wq, (C_out, pitch), q8), _arg("ws", ws, ((C_out + 127) // 128, nb), f32),
+        _arg("bias", bias, (C_out,), f32), act, _dt(y), _arg("y", y, (capacity, C_out), row),
+        _s(stream)), "hc_fp8_linear_fwd")
 
 
 def hc_test_set_option(option: int, value: int):
