@@ -518,8 +518,9 @@ hc_status hc_embedding_fwd(const void* table, hc_dtype dt, int V, int C, const i
  * equal ids in ascending order of position:
  *   row_ptr   [V + 1] int32: the tokens of table row v are
  *             order[row_ptr[v]] .. order[row_ptr[v + 1] - 1]
- *   order     [capacity] int32; entries from row_ptr[V] on (padding, ids out
- *             of range, positions n >= N') are written but belong to no row
+ *   order     [capacity] int32, a permutation of the positions; entries from
+ *             row_ptr[V] on (padding, ids out of range, then n >= N') belong
+ *             to no row
  * Computed once per batch and reused by every table indexed with these ids.
  * Ids out of range other than -1 are reported (HC_ERR_INVALID_INDEX). The
  * result is unique (bit-exact). Uses the library's per-stream workspace (16
@@ -535,7 +536,12 @@ hc_status hc_embedding_sort(const int32_t* ids, int ids_stride, const int32_t* c
  *   dy        [capacity, C] of dtype dt;  dtable [V, C] fp32
  *   row_ptr, order  from hc_embedding_sort (same capacity). A range of row_ptr
  *             that is not inside [0, capacity], or an entry of order that is
- *             not below capacity, is reported (HC_ERR_INVALID_INDEX) and skipped.
+ *             not below capacity, is reported (HC_ERR_INVALID_INDEX) and
+ *             skipped; with a row_ptr that decreases, other rows of more than
+ *             64 tokens are unspecified. No access leaves the buffers.
+ * A row of more than 64 tokens is cut into pieces summed by blocks of their
+ * own and joined in order. Uses the library's per-stream workspace (8 * C
+ * bytes for each 64 tokens, at most for four pieces per SM).
  */
 hc_status hc_embedding_bwd(const void* dy, hc_dtype dt, const int32_t* row_ptr,
                            const int32_t* order, int capacity, int V, int C, float scale,

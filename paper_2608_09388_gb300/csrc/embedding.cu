@@ -14,28 +14,50 @@ namespace {
 constexpr int kThreads = 256;
 
 // ---------------------------------------------------------------- forward
-template <typename T>
+// A group of TPR threads copies NV pieces of TPR * VEC channels of a token's
+// row at a time; all of them are loaded before the first is stored.
+template <typename T, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(kThreads)
     embed_fwd_kernel(const T* __restrict__ table, int V, int C, const int32_t* __restrict__ ids,
-                     long long ids_stride, const int32_t* count, long long capacity, float scale,
-                     T* __restrict__ y, unsigned* status) {
+                     long long ids_stride, const int32_t* count, long long capacity, int slices,
+                     float scale, T* __restrict__ y, unsigned* status) {
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
-    for (long long n = blockIdx.x; n < rows; n += gridDim.x) {
+    const int t = threadIdx.x % TPR;
+    const long long items = rows * slices;
+    const long long step = (long long)gridDim.x * (kThreads / TPR);
+    for (long long it = (long long)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR; it < items;
+         it += step) {
+        int slice;
+        const long long n = div32(it, slices, slice);
         const int id = ids[n * ids_stride];
         const bool ok = id >= 0 && id < V;
-        if (!ok && id != -1 && threadIdx.x == 0) report(status, kErrIndex);
-        for (int c = threadIdx.x; c < C; c += kThreads)
-            y[n * C + c] =
-                from_f32<T>(ok ? to_f32(table[(long long)id * C + c]) * scale : 0.f);
+        if (!ok && id != -1 && t == 0 && slice == 0) report(status, kErrIndex);
+        const int c0 = (slice * NV * TPR + t) * VEC;
+        Piece<T, VEC> p[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = c0 + i * TPR * VEC;
+            if (ok && c < C) p[i].load(table + (long long)id * C + c);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = c0 + i * TPR * VEC;
+            if (c < C) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) p[i].set(e, ok ? p[i].get(e) * scale : 0.f);
+                p[i].store(y + n * C + c);
+            }
+        }
     }
 }
 
 // ---------------------------------------------------------------- sort
-constexpr int kDigitBits = 11;
-constexpr int kDigits = 1 << kDigitBits;
+constexpr int kMaxDigitBits = 11;
+constexpr int kMaxDigits = 1 << kMaxDigitBits;
 constexpr int kMaxTiles = 64;
+constexpr int kMinTile = 2048;
 constexpr int kSortWarps = 8;
 constexpr int kSortThreads = kSortWarps * 32;
 
@@ -45,19 +67,23 @@ struct SortArgs {
     const int32_t* pos_in;
     int32_t* keys_out;
     int32_t* pos_out;
-    int32_t* hist;            // [tiles][kDigits]
+    int32_t* hist;            // [tiles][digits]
     const int32_t* count;
     long long ids_stride;
     long long capacity;
-    long long tile;           // keys per tile, a multiple of kSortThreads
-    int V, shift;
+    int V, shift, bits;       // this pass sorts by key bits [shift, shift + bits)
     unsigned* status;
 };
 
-// Key of entry i of this pass.
-__device__ __forceinline__ int sort_key(const SortArgs& a, long long i, long long rows) {
+// Keys per tile, a multiple of kSortThreads, for at most kMaxTiles tiles.
+__device__ __forceinline__ long long sort_tile(long long rows) {
+    const long long t = (rows + kMaxTiles - 1) / kMaxTiles;
+    return t < kMinTile ? kMinTile : (t + kSortThreads - 1) / kSortThreads * kSortThreads;
+}
+
+// Key of entry i < N' of this pass.
+__device__ __forceinline__ int sort_key(const SortArgs& a, long long i) {
     if (a.ids == nullptr) return a.keys_in[i];
-    if (i >= rows) return a.V;
     const int id = a.ids[i * a.ids_stride];
     if (id >= 0 && id < a.V) return id;
     if (id != -1) report(a.status, kErrIndex);
@@ -65,45 +91,55 @@ __device__ __forceinline__ int sort_key(const SortArgs& a, long long i, long lon
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(const SortArgs a) {
-    __shared__ int h[kDigits];
-    for (int d = threadIdx.x; d < kDigits; d += kSortThreads) h[d] = 0;
+    __shared__ int h[kMaxDigits];
+    const int digits = 1 << a.bits;
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) h[d] = 0;
     pdl_wait();
     pdl_trigger();
     __syncthreads();
     const long long rows = token_rows(a.count, a.capacity, a.status);
-    const long long b = blockIdx.x * a.tile;
-    const long long e = b + a.tile < a.capacity ? b + a.tile : a.capacity;
+    const long long tile = sort_tile(rows);
+    const long long b = blockIdx.x * tile;
+    if (b >= rows) return;
+    const long long e = b + tile < rows ? b + tile : rows;
     for (long long i = b + threadIdx.x; i < e; i += kSortThreads)
-        atomicAdd(&h[(sort_key(a, i, rows) >> a.shift) & (kDigits - 1)], 1);
+        atomicAdd(&h[(sort_key(a, i) >> a.shift) & (digits - 1)], 1);
     __syncthreads();
-    for (int d = threadIdx.x; d < kDigits; d += kSortThreads)
-        a.hist[(long long)blockIdx.x * kDigits + d] = h[d];
+    for (int d = threadIdx.x; d < digits; d += kSortThreads)
+        a.hist[(long long)blockIdx.x * digits + d] = h[d];
 }
 
 // Places a tile's keys: an entry goes to the number of keys with a smaller
 // digit, plus those with its digit in earlier tiles, in earlier warps' shares
 // of this tile and earlier in its own warp's share.
-constexpr size_t kScatterSmem = sizeof(int) * kDigits * (kSortWarps + 1);
+constexpr size_t scatter_smem(int bits) {
+    return (sizeof(int) << bits) * (kSortWarps + 1);
+}
 
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortArgs a) {
     extern __shared__ int sm[];
     __shared__ int sh[kSortWarps];
-    int* const base = sm;                        // [kDigits]
+    const int digits = 1 << a.bits;
+    int* const base = sm;                       // [digits]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int* const cnt = sm + kDigits * (1 + warp);  // this warp's [kDigits]
-    for (int d = threadIdx.x; d < kDigits * kSortWarps; d += kSortThreads) sm[kDigits + d] = 0;
+    int* const cnt = sm + digits * (1 + warp);  // this warp's [digits]
+    for (int d = threadIdx.x; d < digits * kSortWarps; d += kSortThreads) sm[digits + d] = 0;
     pdl_wait();
     pdl_trigger();
+    const long long rows = token_rows(a.count, a.capacity, a.status);
+    const long long tile = sort_tile(rows);
+    const int tiles = (int)((rows + tile - 1) / tile);
+    if ((int)blockIdx.x >= tiles) return;
     // Starts of the digit runs: thread t owns the kPer digits from t * kPer.
-    constexpr int kPer = kDigits / kSortThreads;
+    constexpr int kPer = kMaxDigits / kSortThreads;
     int before[kPer], total[kPer], sum = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) before[j] = total[j] = 0;
-    for (int t = 0; t < (int)gridDim.x; ++t) {
-        const int* h = a.hist + (long long)t * kDigits + threadIdx.x * kPer;
+    for (int t = 0; t < tiles; ++t) {
+        const int* h = a.hist + (long long)t * digits + threadIdx.x * kPer;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            const int v = h[j];
+            const int v = threadIdx.x * kPer + j < digits ? h[j] : 0;
             total[j] += v;
             if (t < (int)blockIdx.x) before[j] += v;
         }
@@ -122,22 +158,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     for (int w = 0; w < warp; ++w) run += sh[w];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        base[threadIdx.x * kPer + j] = run + before[j];
+        if (threadIdx.x * kPer + j < digits) base[threadIdx.x * kPer + j] = run + before[j];
         run += total[j];
     }
     // Digits of each warp's share.
-    const long long rows = token_rows(a.count, a.capacity, a.status);
-    const long long share = a.tile / kSortWarps;  // a multiple of 32
-    const long long b = blockIdx.x * a.tile + warp * share;
-    const long long e = b + share < a.capacity ? b + share : a.capacity;
+    const long long share = tile / kSortWarps;  // a multiple of 32
+    const long long b = blockIdx.x * tile + warp * share;
+    const long long e = b + share < rows ? b + share : rows;
     for (long long i = b + lane; i < e; i += 32)
-        atomicAdd(&cnt[(sort_key(a, i, rows) >> a.shift) & (kDigits - 1)], 1);
+        atomicAdd(&cnt[(sort_key(a, i) >> a.shift) & (digits - 1)], 1);
     __syncthreads();
-    for (int d = threadIdx.x; d < kDigits; d += kSortThreads) {
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
         int at = base[d];
         for (int w = 0; w < kSortWarps; ++w) {
-            const int c = sm[kDigits * (1 + w) + d];
-            sm[kDigits * (1 + w) + d] = at;
+            const int c = sm[digits * (1 + w) + d];
+            sm[digits * (1 + w) + d] = at;
             at += c;
         }
     }
@@ -145,8 +180,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     for (long long i0 = b; i0 < e; i0 += 32) {
         const long long i = i0 + lane;
         const bool in = i < e;
-        const int key = in ? sort_key(a, i, rows) : 0;
-        const int digit = in ? (key >> a.shift) & (kDigits - 1) : kDigits;  // kDigits: no entry
+        const int key = in ? sort_key(a, i) : 0;
+        const int digit = in ? (key >> a.shift) & (digits - 1) : digits;  // digits: no entry
         const unsigned same = __match_any_sync(0xffffffffu, digit);
         const int rank = __popc(same & ((1u << lane) - 1u));
         int at = 0;
@@ -161,68 +196,321 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     }
 }
 
-// row_ptr[v] = entries whose key is below v.
+// row_ptr[v] = entries whose key is below v. Positions from N' on follow the
+// sorted ones in order.
 __global__ void __launch_bounds__(kThreads)
-    sort_ptr_kernel(const int32_t* __restrict__ keys, int capacity, int V,
-                    int32_t* __restrict__ row_ptr) {
+    sort_ptr_kernel(const int32_t* __restrict__ keys, const int32_t* count, int capacity, int V,
+                    int32_t* __restrict__ row_ptr, int32_t* __restrict__ order, unsigned* status) {
     pdl_wait();
     pdl_trigger();
-    const long long v = blockIdx.x * (long long)kThreads + threadIdx.x;
-    if (v > V) return;
-    int lo = 0, hi = capacity;
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (keys[mid] < v)
-            lo = mid + 1;
-        else
-            hi = mid;
+    const int rows = (int)token_rows(count, capacity, status);
+    const long long g = blockIdx.x * (long long)kThreads + threadIdx.x;
+    const long long all = (long long)gridDim.x * kThreads;
+    for (long long v = g; v <= V; v += all) {
+        int lo = 0, hi = rows;
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            if (keys[mid] < v)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        row_ptr[v] = lo;
     }
-    row_ptr[v] = lo;
+    for (long long i = rows + g; i < capacity; i += all) order[i] = (int)i;
 }
 
 // ---------------------------------------------------------------- gradient
-// A block per (table row, 256 channels) adds the row's positions in order.
-template <typename T>
+// Token positions are cut into chunks of sorted entries, at least kMinChunk
+// and so many that there are at most `max_chunks`. A table row of at most one
+// chunk's tokens is summed by one group of threads (embed_bwd_rows_kernel),
+// so that no group walks a frequent token alone. A longer row is summed chunk by chunk, a block
+// each (embed_bwd_chunks_kernel): it holds the chunk's first entry or its
+// last, so a chunk has at most two such sums, slot 0 for the row of its first
+// entry and slot 1 for another row at its end. The chunks' sums of a row are
+// then added in order by the block of the chunk where the row starts
+// (embed_bwd_join_kernel; at most one long row starts in a chunk).
+constexpr int kMinChunk = 64;
+
+struct GradArgs {
+    const int32_t* row_ptr;
+    const int32_t* order;
+    int capacity, V, C;
+    int max_chunks;
+    float scale;
+    float* part;    // [chunks][2][C]
+    float* dtable;
+    unsigned* status;
+};
+
+// Sorted entries in use, and entries per chunk.
+__device__ __forceinline__ int entries(const GradArgs& a) {
+    return min(max(__ldg(a.row_ptr + a.V), 0), a.capacity);
+}
+__device__ __forceinline__ int chunk_of(const GradArgs& a, int total) {
+    return max(kMinChunk, (int)(((long long)total + a.max_chunks - 1) / a.max_chunks));
+}
+
+// Tokens of table row v; empty (and reported) where row_ptr is not a range of
+// the capacity.
+__device__ __forceinline__ int2 tokens_of(const GradArgs& a, int v) {
+    int2 r = make_int2(__ldg(a.row_ptr + v), __ldg(a.row_ptr + v + 1));
+    if (r.x < 0 || r.y < r.x || r.y > a.capacity) {
+        report(a.status, kErrIndex);
+        r = make_int2(0, 0);
+    }
+    return r;
+}
+
+// The table row whose tokens include sorted entry i < row_ptr[V].
+__device__ __forceinline__ int row_at(const GradArgs& a, int i) {
+    int lo = 0, hi = a.V - 1;  // the first row with row_ptr[v + 1] > i
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (__ldg(a.row_ptr + mid + 1) > i)
+            hi = mid;
+        else
+            lo = mid + 1;
+    }
+    return lo;
+}
+
+// acc += dy[order[i]] for i = b, b + step, .. < e, by a group of TPR threads
+// (`mask` of its warp) holding NV pieces of TPR * VEC channels from c0 on. A
+// group reads TPR entries of order at once and keeps kAhead rows in flight.
+template <typename T, int VEC, int TPR, int NV>
+__device__ __forceinline__ void add_tokens(const GradArgs& a, const T* __restrict__ dy, int b, int e,
+                                           int step, int c0, unsigned mask, float (&acc)[NV * VEC]) {
+    constexpr int kAhead = NV >= 4 ? 2 : NV == 2 ? 4 : 8;
+    const int t = threadIdx.x % TPR;
+    for (long long i0 = b; i0 < e; i0 += (long long)TPR * step) {
+        const long long mine = i0 + (long long)t * step;
+        int pos = -1;
+        if (mine < e) {
+            pos = __ldg(a.order + mine);
+            if (pos < 0 || pos >= a.capacity) {
+                report(a.status, kErrIndex);
+                pos = -1;
+            }
+        }
+        const long long left = (e - i0 + step - 1) / step;
+        const int n = left < TPR ? (int)left : TPR;
+        for (int j = 0; j < n; j += kAhead) {
+            Piece<T, VEC> p[kAhead][NV];
+            int at[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                at[u] = __shfl_sync(mask, pos, (j + u) % TPR, TPR);
+                if (j + u >= n) at[u] = -1;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int c = c0 + k * TPR * VEC;
+                    if (at[u] >= 0 && c < a.C) p[u][k].load(dy + (long long)at[u] * a.C + c);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (at[u] >= 0)
+#pragma unroll
+                    for (int k = 0; k < NV; ++k)
+                        if (c0 + k * TPR * VEC < a.C)
+#pragma unroll
+                            for (int v = 0; v < VEC; ++v) acc[k * VEC + v] += p[u][k].get(v);
+        }
+    }
+}
+
+template <int VEC>
+__device__ __forceinline__ void store_floats(float* p, const float* v) {
+    if constexpr (VEC == 1) {
+        *p = *v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4)
+            *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+}
+
+// A group takes `per` consecutive table rows, one slice of channels
+// (blockIdx.y) of each.
+template <typename T, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(kThreads)
-    embed_bwd_kernel(const T* __restrict__ dy, const int32_t* __restrict__ row_ptr,
-                     const int32_t* __restrict__ order, int capacity, int V, int C, float scale,
-                     float* __restrict__ dtable, unsigned* status) {
+    embed_bwd_rows_kernel(const GradArgs a, const T* __restrict__ dy, int per) {
     pdl_wait();
     pdl_trigger();
-    const int c = blockIdx.y * kThreads + threadIdx.x;
-    for (long long v = blockIdx.x; v < V; v += gridDim.x) {
-        int i = row_ptr[v], e = row_ptr[v + 1];
-        if (i < 0 || e < i || e > capacity) {
-            if (threadIdx.x == 0) report(status, kErrIndex);
-            i = e = 0;
-        }
-        float s = 0.f;
-        for (; i < e; ++i) {
-            const int n = order[i];
-            if (n < 0 || n >= capacity) {
-                report(status, kErrIndex);
-                continue;
+    const int t = threadIdx.x % TPR;
+    const unsigned mask =
+        TPR == 32 ? 0xffffffffu : ((1u << (TPR & 31)) - 1u) << (threadIdx.x % 32 / TPR * TPR);
+    const int c0 = (blockIdx.y * NV * TPR + t) * VEC;
+    const long long g = (long long)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
+    const long long v0 = g * per;
+    const int chunk = chunk_of(a, entries(a));
+    for (long long v = v0; v < v0 + per && v < a.V; ++v) {
+        const int2 r = tokens_of(a, (int)v);
+        if (r.y - r.x > chunk) continue;  // the join writes it
+        float acc[NV * VEC];
+#pragma unroll
+        for (int k = 0; k < NV * VEC; ++k) acc[k] = 0.f;
+        add_tokens<T, VEC, TPR, NV>(a, dy, r.x, r.y, 1, c0, mask, acc);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int c = c0 + k * TPR * VEC;
+            if (c < a.C) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[k * VEC + e] *= a.scale;
+                store_floats<VEC>(a.dtable + v * a.C + c, acc + k * VEC);
             }
-            if (c < C) s += to_f32(dy[(long long)n * C + c]);
         }
-        if (c < C) dtable[v * C + c] = s * scale;
     }
+}
+
+// Block (chunk, slice): the sums of the chunk's long rows, warps taking every
+// eighth token, joined in warp order.
+template <typename T, int VEC, int NV>
+__global__ void __launch_bounds__(kThreads)
+    embed_bwd_chunks_kernel(const GradArgs a, const T* __restrict__ dy) {
+    constexpr int kWarps = kThreads / 32, kWidth = NV * VEC * 32;
+    __shared__ float sh[kWarps][kWidth];
+    pdl_wait();
+    pdl_trigger();
+    const int total = entries(a), chunk = chunk_of(a, total);
+    const long long b = (long long)blockIdx.x * chunk;
+    if (b >= total) return;
+    const int p0 = (int)b, p1 = (int)(b + chunk < total ? b + chunk : total);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int s0 = blockIdx.y * kWidth;
+    int row = row_at(a, p0);
+    for (int slot = 0; slot < 2; ++slot) {
+        if (slot == 1) {
+            const int last = row_at(a, p1 - 1);
+            if (last == row) break;
+            row = last;
+        }
+        const int2 r = tokens_of(a, row);
+        if (r.y - r.x <= chunk) continue;
+        const int e = min(r.y, p1);
+        float acc[NV * VEC];
+#pragma unroll
+        for (int k = 0; k < NV * VEC; ++k) acc[k] = 0.f;
+        add_tokens<T, VEC, 32, NV>(a, dy, max(r.x, p0) + warp, e, kWarps, s0 + lane * VEC,
+                                   0xffffffffu, acc);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) sh[warp][(k * 32 + lane) * VEC + v] = acc[k * VEC + v];
+        __syncthreads();
+        float* const out = a.part + (2ll * blockIdx.x + slot) * a.C;
+        for (int c = threadIdx.x; c < kWidth && s0 + c < a.C; c += kThreads) {
+            float s = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) s += sh[w][c];
+            out[s0 + c] = s;
+        }
+    }
+}
+
+// Block (chunk, 256 channels): if a long row starts in the chunk, the sum of
+// its chunks' sums in order, a thread per channel.
+__global__ void __launch_bounds__(kThreads) embed_bwd_join_kernel(const GradArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int total = entries(a), chunk = chunk_of(a, total);
+    const long long b = (long long)blockIdx.x * chunk;
+    if (b >= total) return;
+    const int p1 = (int)(b + chunk < total ? b + chunk : total);
+    const int row = row_at(a, p1 - 1);
+    const int2 r = tokens_of(a, row);
+    if (r.y - r.x <= chunk || r.x < b) return;
+    const int c = blockIdx.y * kThreads + threadIdx.x;
+    if (c >= a.C) return;
+    // the row starts in this chunk: at its first entry (slot 0) or later
+    // (slot 1); it holds the first entry of every later chunk (slot 0)
+    const int k1 = (r.y - 1) / chunk;
+    float s = a.part[(2ll * blockIdx.x + (r.x == b ? 0 : 1)) * a.C + c];
+#pragma unroll 8
+    for (int k = blockIdx.x + 1; k <= k1; ++k) s += a.part[2ll * k * a.C + c];
+    a.dtable[(long long)row * a.C + c] = s * a.scale;
+}
+
+bool aligned16(const void* p) {
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+}
+
+template <typename T, int VEC, int TPR, int NV>
+hc_status fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table, void* y,
+              cudaStream_t s) {
+    const int slices = (a.C + NV * TPR * VEC - 1) / (NV * TPR * VEC);
+    const long long need = ((long long)a.capacity * slices + kThreads / TPR - 1) / (kThreads / TPR);
+    const long long cap = (long long)ctx->num_sms * 8;
+    return launch_pdl(embed_fwd_kernel<T, VEC, TPR, NV>,
+                      dim3((unsigned)(need < cap ? need : cap)), dim3(kThreads), 0, s,
+                      "embed_fwd_kernel", (const T*)table, a.V, a.C, a.ids, a.ids_stride, a.count,
+                      (long long)a.capacity, slices, a.scale, (T*)y, ctx->status);
+}
+
+// 16-byte pieces where the rows allow them; 8 threads a row where that is
+// enough, else a warp with up to 4 pieces each.
+template <typename T>
+hc_status run_fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table, void* y,
+                  cudaStream_t s) {
+    constexpr int kVec = 16 / (int)sizeof(T);
+    if (a.C % kVec == 0 && aligned16(table) && aligned16(y)) {
+        if (a.C <= 8 * kVec) return fwd<T, kVec, 8, 1>(ctx, a, table, y, s);
+        if (a.C <= 32 * kVec) return fwd<T, kVec, 32, 1>(ctx, a, table, y, s);
+        return fwd<T, kVec, 32, 4>(ctx, a, table, y, s);
+    }
+    if (a.C <= 32) return fwd<T, 1, 8, 4>(ctx, a, table, y, s);
+    return fwd<T, 1, 32, 8>(ctx, a, table, y, s);
+}
+
+template <typename T, int VEC, int TPR, int NV>
+hc_status bwd_rows(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStream_t s) {
+    const int slices = (a.C + NV * TPR * VEC - 1) / (NV * TPR * VEC);
+    // consecutive rows per group: one while the groups fill the SMs, then up to 16
+    const long long groups = (long long)ctx->num_sms * 16 * (kThreads / TPR);
+    long long per = ((long long)a.V * slices + groups - 1) / groups;
+    per = per < 1 ? 1 : per > 16 ? 16 : per;
+    const long long blocks = (a.V + per * (kThreads / TPR) - 1) / (per * (kThreads / TPR));
+    return launch_pdl(embed_bwd_rows_kernel<T, VEC, TPR, NV>,
+                      dim3((unsigned)blocks, (unsigned)slices), dim3(kThreads), 0, s,
+                      "embed_bwd_rows_kernel", a, (const T*)dy, (int)per);
+}
+
+template <typename T>
+hc_status run_bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, int chunks,
+                  cudaStream_t s) {
+    constexpr int kVec = 16 / (int)sizeof(T);
+    const bool wide = a.C % kVec == 0 && aligned16(dy) && aligned16(a.dtable);
+    hc_status st;
+    if (chunks > 1) {  // else no row is longer than a chunk
+        const int width = wide ? 32 * kVec : 256;
+        const dim3 grid((unsigned)chunks, (unsigned)((a.C + width - 1) / width));
+        st = wide ? launch_pdl(embed_bwd_chunks_kernel<T, kVec, 1>, grid, dim3(kThreads), 0, s,
+                               "embed_bwd_chunks_kernel", a, (const T*)dy)
+                  : launch_pdl(embed_bwd_chunks_kernel<T, 1, 8>, grid, dim3(kThreads), 0, s,
+                               "embed_bwd_chunks_kernel", a, (const T*)dy);
+        if (st != HC_OK) return st;
+        st = launch_pdl(embed_bwd_join_kernel,
+                        dim3((unsigned)chunks, (unsigned)((a.C + kThreads - 1) / kThreads)),
+                        dim3(kThreads), 0, s, "embed_bwd_join_kernel", a);
+        if (st != HC_OK) return st;
+    }
+    if (wide) {
+        if (a.C <= 8 * kVec) return bwd_rows<T, kVec, 8, 1>(ctx, a, dy, s);
+        if (a.C <= 32 * kVec) return bwd_rows<T, kVec, 32, 1>(ctx, a, dy, s);
+        return bwd_rows<T, kVec, 32, 4>(ctx, a, dy, s);
+    }
+    if (a.C <= 32) return bwd_rows<T, 1, 8, 4>(ctx, a, dy, s);
+    return bwd_rows<T, 1, 32, 8>(ctx, a, dy, s);
 }
 
 }  // namespace
 
 hc_status launch_embedding_fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table,
                                void* y, cudaStream_t s) {
-    const long long cap = (long long)ctx->num_sms * 8;
-    const unsigned grid = (unsigned)(a.capacity < cap ? a.capacity : cap);
-    if (a.dt == HC_BF16)
-        return launch_pdl(embed_fwd_kernel<__nv_bfloat16>, dim3(grid), dim3(kThreads), 0, s,
-                          "embed_fwd_kernel", (const __nv_bfloat16*)table, a.V, a.C, a.ids,
-                          a.ids_stride, a.count, (long long)a.capacity, a.scale,
-                          (__nv_bfloat16*)y, ctx->status);
-    return launch_pdl(embed_fwd_kernel<float>, dim3(grid), dim3(kThreads), 0, s,
-                      "embed_fwd_kernel", (const float*)table, a.V, a.C, a.ids, a.ids_stride,
-                      a.count, (long long)a.capacity, a.scale, (float*)y, ctx->status);
+    return a.dt == HC_BF16 ? run_fwd<__nv_bfloat16>(ctx, a, table, y, s)
+                           : run_fwd<float>(ctx, a, table, y, s);
 }
 
 hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, int32_t* row_ptr,
@@ -235,22 +523,23 @@ hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, in
         if (!done[ctx->device]) {
             st = check_cuda(cudaFuncSetAttribute(sort_scatter_kernel,
                                                  cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)kScatterSmem),
+                                                 (int)scatter_smem(kMaxDigitBits)),
                             "sort_scatter_kernel");
             if (st != HC_OK) return st;
             done[ctx->device] = true;
         }
-        long long tile = (n + kMaxTiles - 1) / kMaxTiles;
-        if (tile < 2048) tile = 2048;
-        tile = (tile + kSortThreads - 1) / kSortThreads * kSortThreads;
-        const unsigned tiles = (unsigned)((n + tile - 1) / tile);
-        int passes = 1;
-        while (passes < 3 && (a.V >> (kDigitBits * passes)) != 0) ++passes;
+        const long long need = (n + kMinTile - 1) / kMinTile;
+        const unsigned tiles = (unsigned)(need < kMaxTiles ? need : kMaxTiles);
+        // the keys 0 .. V in as few passes as 11-bit digits allow, of equal width
+        int key_bits = 1;
+        while (key_bits < 31 && (a.V >> key_bits) != 0) ++key_bits;
+        const int passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits;
+        const int bits = (key_bits + passes - 1) / passes;
         // workspace: histograms, two buffers of keys and two of positions
-        int32_t* ws = (int32_t*)stream_workspace(
-            s, sizeof(int32_t) * ((size_t)kMaxTiles * kDigits + 4 * (size_t)n));
+        const size_t hist = (size_t)kMaxTiles * kMaxDigits;
+        int32_t* ws = (int32_t*)stream_workspace(s, sizeof(int32_t) * (hist + 4 * (size_t)n));
         if (!ws) return HC_ERR_CUDA;
-        int32_t* keys[2] = {ws + (size_t)kMaxTiles * kDigits, ws + (size_t)kMaxTiles * kDigits + n};
+        int32_t* keys[2] = {ws + hist, ws + hist + n};
         int32_t* pos[2] = {keys[1] + n, keys[1] + 2 * n};
         for (int p = 0; p < passes; ++p) {
             SortArgs k{};
@@ -263,42 +552,44 @@ hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, in
             k.count = a.count;
             k.ids_stride = a.ids_stride;
             k.capacity = n;
-            k.tile = tile;
             k.V = a.V;
-            k.shift = p * kDigitBits;
+            k.shift = p * bits;
+            k.bits = bits;
             k.status = ctx->status;
             st = launch_pdl(sort_hist_kernel, dim3(tiles), dim3(kSortThreads), 0, s,
                             "sort_hist_kernel", k);
             if (st != HC_OK) return st;
-            st = launch_pdl(sort_scatter_kernel, dim3(tiles), dim3(kSortThreads), kScatterSmem, s,
-                            "sort_scatter_kernel", k);
+            st = launch_pdl(sort_scatter_kernel, dim3(tiles), dim3(kSortThreads),
+                            scatter_smem(bits), s, "sort_scatter_kernel", k);
             if (st != HC_OK) return st;
             sorted = k.keys_out;
         }
     }
-    const unsigned grid = (unsigned)(((long long)a.V + 1 + kThreads - 1) / kThreads);
-    return launch_pdl(sort_ptr_kernel, dim3(grid), dim3(kThreads), 0, s, "sort_ptr_kernel", sorted,
-                      (int)n, a.V, row_ptr);
+    const long long need = ((a.V + 1ll > n ? a.V + 1ll : n) + kThreads - 1) / kThreads;
+    const long long cap = (long long)ctx->num_sms * 8;
+    return launch_pdl(sort_ptr_kernel, dim3((unsigned)(need < cap ? need : cap)), dim3(kThreads), 0,
+                      s, "sort_ptr_kernel", sorted, a.count, (int)n, a.V, row_ptr, order,
+                      ctx->status);
 }
 
 hc_status launch_embedding_bwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* dy,
                                const int32_t* row_ptr, const int32_t* order, float* dtable,
                                cudaStream_t s) {
-    const unsigned ctiles = (unsigned)((a.C + kThreads - 1) / kThreads);
-    long long gx = (long long)ctx->num_sms * 32;
-    if (gx > a.V) gx = a.V;
-    if (ctiles > 65535u) {
+    // a long row is cut into chunks for four blocks an SM at most
+    const long long need = ((long long)a.capacity + kMinChunk - 1) / kMinChunk;
+    const int chunks = (int)(need < ctx->num_sms * 4 ? need : ctx->num_sms * 4);
+    GradArgs b{row_ptr, order, a.capacity, a.V, a.C, chunks < 1 ? 1 : chunks, a.scale, nullptr,
+               dtable, ctx->status};
+    if ((a.C + 31) / 32 > 65535) {  // the smallest slice of channels, blockIdx.y
         set_error("hc_embedding_bwd: C=%d is too wide", a.C);
         return HC_ERR_UNSUPPORTED;
     }
-    const dim3 grid((unsigned)gx, ctiles);
-    if (a.dt == HC_BF16)
-        return launch_pdl(embed_bwd_kernel<__nv_bfloat16>, grid, dim3(kThreads), 0, s,
-                          "embed_bwd_kernel", (const __nv_bfloat16*)dy, row_ptr, order, a.capacity,
-                          a.V, a.C, a.scale, dtable, ctx->status);
-    return launch_pdl(embed_bwd_kernel<float>, grid, dim3(kThreads), 0, s, "embed_bwd_kernel",
-                      (const float*)dy, row_ptr, order, a.capacity, a.V, a.C, a.scale, dtable,
-                      ctx->status);
+    if (chunks > 1) {
+        b.part = (float*)stream_workspace(s, (size_t)chunks * 2 * a.C * sizeof(float));
+        if (!b.part) return HC_ERR_CUDA;
+    }
+    return a.dt == HC_BF16 ? run_bwd<__nv_bfloat16>(ctx, b, dy, chunks, s)
+                           : run_bwd<float>(ctx, b, dy, chunks, s);
 }
 
 }  // namespace hc
