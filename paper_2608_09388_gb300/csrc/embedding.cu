@@ -57,8 +57,9 @@ __global__ void __launch_bounds__(kThreads)
 constexpr int kMaxDigitBits = 11;
 constexpr int kMaxDigits = 1 << kMaxDigitBits;
 constexpr int kMaxTiles = 64;
-constexpr int kMinTile = 2048;
-constexpr int kSortWarps = 8;
+constexpr int kSortWarps = 16;
+constexpr int kRounds = 8;  // keys per lane held in registers at a time
+constexpr int kMinTile = kSortWarps * 32 * kRounds;
 constexpr int kSortThreads = kSortWarps * 32;
 
 struct SortArgs {
@@ -75,10 +76,10 @@ struct SortArgs {
     unsigned* status;
 };
 
-// Keys per tile, a multiple of kSortThreads, for at most kMaxTiles tiles.
+// Keys per tile, a multiple of kMinTile, for at most kMaxTiles tiles.
 __device__ __forceinline__ long long sort_tile(long long rows) {
     const long long t = (rows + kMaxTiles - 1) / kMaxTiles;
-    return t < kMinTile ? kMinTile : (t + kSortThreads - 1) / kSortThreads * kSortThreads;
+    return t < kMinTile ? kMinTile : (t + kMinTile - 1) / kMinTile * kMinTile;
 }
 
 // Key of entry i < N' of this pass.
@@ -113,39 +114,45 @@ __global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(const SortArgs 
 // digit, plus those with its digit in earlier tiles, in earlier warps' shares
 // of this tile and earlier in its own warp's share.
 constexpr size_t scatter_smem(int bits) {
-    return (sizeof(int) << bits) * (kSortWarps + 1);
+    return (sizeof(int) << bits) * (kSortWarps + 2);
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortArgs a) {
     extern __shared__ int sm[];
     __shared__ int sh[kSortWarps];
     const int digits = 1 << a.bits;
-    int* const base = sm;                       // [digits]
+    int* const base = sm;                       // [digits] starts in this tile
+    int* const tot = sm + digits;               // [digits] over all tiles
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int* const cnt = sm + digits * (1 + warp);  // this warp's [digits]
-    for (int d = threadIdx.x; d < digits * kSortWarps; d += kSortThreads) sm[digits + d] = 0;
+    int* const cnt = sm + digits * (2 + warp);  // [digits] of this warp
+    for (int d = threadIdx.x; d < digits * kSortWarps; d += kSortThreads) sm[digits * 2 + d] = 0;
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(a.count, a.capacity, a.status);
     const long long tile = sort_tile(rows);
     const int tiles = (int)((rows + tile - 1) / tile);
     if ((int)blockIdx.x >= tiles) return;
-    // Starts of the digit runs: thread t owns the kPer digits from t * kPer.
-    constexpr int kPer = kMaxDigits / kSortThreads;
-    int before[kPer], total[kPer], sum = 0;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) before[j] = total[j] = 0;
-    for (int t = 0; t < tiles; ++t) {
-        const int* h = a.hist + (long long)t * digits + threadIdx.x * kPer;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            const int v = threadIdx.x * kPer + j < digits ? h[j] : 0;
-            total[j] += v;
-            if (t < (int)blockIdx.x) before[j] += v;
+    // Starts of the digit runs. Column sums of the tiles' histograms first
+    // (coalesced over the digits), then a scan with kPer digits a thread.
+    for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+        int before = 0, total = 0;
+#pragma unroll 8
+        for (int t = 0; t < tiles; ++t) {
+            const int v = a.hist[(long long)t * digits + d];
+            total += v;
+            before += t < (int)blockIdx.x ? v : 0;
         }
+        base[d] = before;
+        tot[d] = total;
     }
+    __syncthreads();
+    constexpr int kPer = kMaxDigits / kSortThreads;
+    int sum = 0;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) sum += total[j];
+    for (int j = 0; j < kPer; ++j) {
+        const int d = threadIdx.x * kPer + j;
+        sum += d < digits ? tot[d] : 0;
+    }
     int incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -158,56 +165,95 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     for (int w = 0; w < warp; ++w) run += sh[w];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        if (threadIdx.x * kPer + j < digits) base[threadIdx.x * kPer + j] = run + before[j];
-        run += total[j];
+        const int d = threadIdx.x * kPer + j;
+        if (d < digits) {
+            base[d] += run;
+            run += tot[d];
+        }
     }
-    // Digits of each warp's share.
-    const long long share = tile / kSortWarps;  // a multiple of 32
+    // Digits of each warp's share: a multiple of 32 * kRounds entries, that
+    // many at a time in registers (the first batch stays for the placing).
+    const long long share = tile / kSortWarps;
     const long long b = blockIdx.x * tile + warp * share;
     const long long e = b + share < rows ? b + share : rows;
-    for (long long i = b + lane; i < e; i += 32)
-        atomicAdd(&cnt[(sort_key(a, i) >> a.shift) & (digits - 1)], 1);
+    int key[kRounds], pos[kRounds];
+    auto load = [&](long long i0) {
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const long long i = i0 + r * 32 + lane;
+            key[r] = i < e ? sort_key(a, i) : -1;
+            pos[r] = a.ids ? (int)i : i < e ? a.pos_in[i] : 0;
+        }
+    };
+    for (long long i0 = b; i0 < e; i0 += 32 * kRounds) {
+        load(i0);
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+            if (key[r] >= 0) atomicAdd(&cnt[(key[r] >> a.shift) & (digits - 1)], 1);
+    }
     __syncthreads();
     for (int d = threadIdx.x; d < digits; d += kSortThreads) {
         int at = base[d];
+#pragma unroll
         for (int w = 0; w < kSortWarps; ++w) {
-            const int c = sm[digits * (1 + w) + d];
-            sm[digits * (1 + w) + d] = at;
+            const int c = sm[digits * (2 + w) + d];
+            sm[digits * (2 + w) + d] = at;
             at += c;
         }
     }
     __syncthreads();
-    for (long long i0 = b; i0 < e; i0 += 32) {
-        const long long i = i0 + lane;
-        const bool in = i < e;
-        const int key = in ? sort_key(a, i) : 0;
-        const int digit = in ? (key >> a.shift) & (digits - 1) : digits;  // digits: no entry
-        const unsigned same = __match_any_sync(0xffffffffu, digit);
-        const int rank = __popc(same & ((1u << lane) - 1u));
-        int at = 0;
-        if (in) at = cnt[digit] + rank;
-        __syncwarp();
-        if (in && rank == 0) cnt[digit] += __popc(same);
-        __syncwarp();
-        if (in) {
-            a.keys_out[at] = key;
-            a.pos_out[at] = a.ids ? (int)i : a.pos_in[i];
+    for (long long i0 = b; i0 < e; i0 += 32 * kRounds) {
+        if (share > 32 * kRounds) load(i0);  // else the share is still held
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const bool in = key[r] >= 0;
+            const int digit = in ? (key[r] >> a.shift) & (digits - 1) : digits;  // no entry
+            const unsigned same = __match_any_sync(0xffffffffu, digit);
+            const int rank = __popc(same & ((1u << lane) - 1u));
+            int at = 0;
+            if (in) at = cnt[digit] + rank;
+            __syncwarp();
+            if (in && rank == 0) cnt[digit] += __popc(same);
+            __syncwarp();
+            if (in) {
+                a.keys_out[at] = key[r];
+                a.pos_out[at] = pos[r];
+            }
         }
     }
 }
 
-// row_ptr[v] = entries whose key is below v. Positions from N' on follow the
-// sorted ones in order.
+// row_ptr[v] = entries whose key is below v: a binary search that starts
+// among 1024 samples of the keys in shared memory, so that at most 2^-10 of
+// the keys are left for the dependent global loads. Positions from N' on
+// follow the sorted ones in order.
+constexpr int kSampleBits = 10;
+
 __global__ void __launch_bounds__(kThreads)
     sort_ptr_kernel(const int32_t* __restrict__ keys, const int32_t* count, int capacity, int V,
                     int32_t* __restrict__ row_ptr, int32_t* __restrict__ order, unsigned* status) {
+    __shared__ int sample[1 << kSampleBits];
     pdl_wait();
     pdl_trigger();
     const int rows = (int)token_rows(count, capacity, status);
+    const int stride = (rows >> kSampleBits) + 1;  // sample i is keys[i * stride]
+    const int samples = (rows + stride - 1) / stride;
+    for (int i = threadIdx.x; i < samples; i += kThreads) sample[i] = keys[(long long)i * stride];
+    __syncthreads();
     const long long g = blockIdx.x * (long long)kThreads + threadIdx.x;
     const long long all = (long long)gridDim.x * kThreads;
     for (long long v = g; v <= V; v += all) {
-        int lo = 0, hi = rows;
+        int lo = 0, hi = samples;  // samples below v
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (sample[mid] < v)
+                lo = mid + 1;
+            else
+                hi = mid;
+        }
+        // the answer lies after sample lo - 1 and not after sample lo
+        hi = lo == samples ? rows : lo * stride;
+        lo = lo == 0 ? 0 : (lo - 1) * stride + 1;
         while (lo < hi) {
             const int mid = lo + (hi - lo) / 2;
             if (keys[mid] < v)
@@ -221,15 +267,15 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 // ---------------------------------------------------------------- gradient
-// Token positions are cut into chunks of sorted entries, at least kMinChunk
-// and so many that there are at most `max_chunks`. A table row of at most one
-// chunk's tokens is summed by one group of threads (embed_bwd_rows_kernel),
-// so that no group walks a frequent token alone. A longer row is summed chunk by chunk, a block
-// each (embed_bwd_chunks_kernel): it holds the chunk's first entry or its
-// last, so a chunk has at most two such sums, slot 0 for the row of its first
-// entry and slot 1 for another row at its end. The chunks' sums of a row are
-// then added in order by the block of the chunk where the row starts
-// (embed_bwd_join_kernel; at most one long row starts in a chunk).
+// Sorted entries are cut into chunks, of at least kMinChunk entries and at
+// most `max_chunks`. A table row of at most one chunk's tokens is summed by
+// one group of threads, so that no group walks a frequent token alone. A
+// longer row is summed chunk by chunk, a block each: it holds the chunk's
+// first entry or its last, so a chunk has at most two such sums, slot 0 for
+// the row of its first entry and slot 1 for another row at its end. Both
+// kinds of work are blocks of one launch (embed_bwd_kernel). The chunks' sums
+// of a row are then added in order by the block of the chunk where the row
+// starts (embed_bwd_join_kernel; at most one long row starts in a chunk).
 constexpr int kMinChunk = 64;
 
 struct GradArgs {
@@ -262,26 +308,49 @@ __device__ __forceinline__ int2 tokens_of(const GradArgs& a, int v) {
     return r;
 }
 
-// The table row whose tokens include sorted entry i < row_ptr[V].
-__device__ __forceinline__ int row_at(const GradArgs& a, int i) {
-    int lo = 0, hi = a.V - 1;  // the first row with row_ptr[v + 1] > i
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (__ldg(a.row_ptr + mid + 1) > i)
-            hi = mid;
-        else
-            lo = mid + 1;
+// The table rows whose tokens include the sorted entries i.x <= i.y <
+// row_ptr[V], found by a warp with 32 probes a step, both at once (a binary
+// search would be up to 17 dependent loads each).
+__device__ __forceinline__ int2 rows_at(const GradArgs& a, int2 i) {
+    const int lane = threadIdx.x & 31;
+    int lo[2] = {0, 0}, hi[2] = {a.V - 1, a.V - 1};  // the first row with row_ptr[v + 1] > i
+    const int want[2] = {i.x, i.y};
+    while (lo[0] < hi[0] || lo[1] < hi[1]) {
+        long long at[2];
+        bool above[2];
+        int step[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            step[q] = (hi[q] - lo[q]) / 32 + 1;  // probes every `step`, the last past hi
+            at[q] = (long long)lo[q] + (long long)(lane + 1) * step[q] - 1;
+            above[q] = at[q] >= hi[q] || __ldg(a.row_ptr + at[q] + 1) > want[q];
+        }
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int k = __ffs(__ballot_sync(0xffffffffu, above[q])) - 1;
+            const long long top = (long long)lo[q] + (long long)(k + 1) * step[q] - 1;
+            lo[q] += k * step[q];
+            if (top < hi[q]) hi[q] = (int)top;
+        }
     }
-    return lo;
+    return make_int2(lo[0], lo[1]);
 }
+
+// Rows of dy a group keeps in flight: up to 32 registers' worth, 8 at most.
+template <typename T, int VEC, int NV>
+constexpr int kAheadRegs = NV * (VEC * (int)sizeof(T) < 4 ? 1 : VEC * (int)sizeof(T) / 4);
+template <typename T, int VEC, int NV>
+constexpr int kAheadRows = 32 / kAheadRegs<T, VEC, NV> < 8 ? 32 / kAheadRegs<T, VEC, NV> : 8;
 
 // acc += dy[order[i]] for i = b, b + step, .. < e, by a group of TPR threads
 // (`mask` of its warp) holding NV pieces of TPR * VEC channels from c0 on. A
-// group reads TPR entries of order at once and keeps kAhead rows in flight.
+// group reads TPR entries of order at once and keeps kAhead rows in flight:
+// absent rows and channels load from row 0 and channel 0 and add zero, since
+// a load under a condition is moved down to its use, behind the one before.
 template <typename T, int VEC, int TPR, int NV>
 __device__ __forceinline__ void add_tokens(const GradArgs& a, const T* __restrict__ dy, int b, int e,
                                            int step, int c0, unsigned mask, float (&acc)[NV * VEC]) {
-    constexpr int kAhead = NV >= 4 ? 2 : NV == 2 ? 4 : 8;
+    constexpr int kAhead = kAheadRows<T, VEC, NV>;
     const int t = threadIdx.x % TPR;
     for (long long i0 = b; i0 < e; i0 += (long long)TPR * step) {
         const long long mine = i0 + (long long)t * step;
@@ -305,17 +374,14 @@ __device__ __forceinline__ void add_tokens(const GradArgs& a, const T* __restric
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
                     const int c = c0 + k * TPR * VEC;
-                    if (at[u] >= 0 && c < a.C) p[u][k].load(dy + (long long)at[u] * a.C + c);
+                    p[u][k].load(dy + (long long)max(at[u], 0) * a.C + (c < a.C ? c : 0));
                 }
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u)
-                if (at[u] >= 0)
 #pragma unroll
-                    for (int k = 0; k < NV; ++k)
-                        if (c0 + k * TPR * VEC < a.C)
-#pragma unroll
-                            for (int v = 0; v < VEC; ++v) acc[k * VEC + v] += p[u][k].get(v);
+                for (int k = 0; k < NV * VEC; ++k)
+                    acc[k] += at[u] >= 0 ? p[u][k / VEC].get(k % VEC) : 0.f;
         }
     }
 }
@@ -331,106 +397,178 @@ __device__ __forceinline__ void store_floats(float* p, const float* v) {
     }
 }
 
-// A group takes `per` consecutive table rows, one slice of channels
-// (blockIdx.y) of each.
+constexpr int kMaxPer = 16;  // table rows per group at most (below TPR + 1 for 8 threads: 8)
+
+// A group takes `per` consecutive table rows, one slice of channels of each.
+// Their tokens are consecutive sorted entries: they are walked as one list,
+// kAhead rows of dy in flight across the table rows' ends.
 template <typename T, int VEC, int TPR, int NV>
-__global__ void __launch_bounds__(kThreads)
-    embed_bwd_rows_kernel(const GradArgs a, const T* __restrict__ dy, int per) {
-    pdl_wait();
-    pdl_trigger();
+__device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict__ dy, int per,
+                                          long long group, int slice) {
+    constexpr int kAhead = kAheadRows<T, VEC, NV>;
     const int t = threadIdx.x % TPR;
     const unsigned mask =
         TPR == 32 ? 0xffffffffu : ((1u << (TPR & 31)) - 1u) << (threadIdx.x % 32 / TPR * TPR);
-    const int c0 = (blockIdx.y * NV * TPR + t) * VEC;
-    const long long g = (long long)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
-    const long long v0 = g * per;
+    const int c0 = (slice * NV * TPR + t) * VEC;
+    const long long v0 = group * per;
+    if (v0 >= a.V) return;
+    const int mine = a.V - v0 < per ? (int)(a.V - v0) : per;
     const int chunk = chunk_of(a, entries(a));
-    for (long long v = v0; v < v0 + per && v < a.V; ++v) {
-        const int2 r = tokens_of(a, (int)v);
-        if (r.y - r.x > chunk) continue;  // the join writes it
-        float acc[NV * VEC];
+    // thread j < mine: the tokens of row v0 + j
+    int2 r = make_int2(0, 0);
+    if (t < mine) r = tokens_of(a, (int)v0 + t);
+    const bool is_long = r.y - r.x > chunk;  // left to the chunks
+    // one list if the ranges follow each other, else (a long row, or a
+    // row_ptr that is none) a list per row
+    const int next = __shfl_down_sync(mask, r.x, 1, TPR);
+    const unsigned odd = __ballot_sync(mask, is_long || (t + 1 < mine && r.y != next)) & mask;
+    float acc[NV * VEC];
 #pragma unroll
-        for (int k = 0; k < NV * VEC; ++k) acc[k] = 0.f;
-        add_tokens<T, VEC, TPR, NV>(a, dy, r.x, r.y, 1, c0, mask, acc);
+    for (int k = 0; k < NV * VEC; ++k) acc[k] = 0.f;
+    auto flush = [&](int j) {
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int c = c0 + k * TPR * VEC;
             if (c < a.C) {
+                float v[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[k * VEC + e] *= a.scale;
-                store_floats<VEC>(a.dtable + v * a.C + c, acc + k * VEC);
+                for (int e = 0; e < VEC; ++e) {
+                    v[e] = acc[k * VEC + e] * a.scale;
+                    acc[k * VEC + e] = 0.f;
+                }
+                store_floats<VEC>(a.dtable + (v0 + j) * a.C + c, v);
+            }
+        }
+    };
+    if (odd) {
+        for (int j = 0; j < mine; ++j) {
+            const int b = __shfl_sync(mask, r.x, j, TPR), e = __shfl_sync(mask, r.y, j, TPR);
+            if (e - b > chunk) continue;
+            add_tokens<T, VEC, TPR, NV>(a, dy, b, e, 1, c0, mask, acc);
+            flush(j);
+        }
+        return;
+    }
+    const int b = __shfl_sync(mask, r.x, 0, TPR), e = __shfl_sync(mask, r.y, mine - 1, TPR);
+    int j = 0, end = __shfl_sync(mask, r.y, 0, TPR);
+    for (int i0 = b; i0 < e; i0 += TPR) {
+        int pos = -1;
+        if (i0 + t < e) {
+            pos = __ldg(a.order + i0 + t);
+            if (pos < 0 || pos >= a.capacity) {
+                report(a.status, kErrIndex);
+                pos = -1;
+            }
+        }
+        const int n = min(e - i0, TPR);
+        for (int q = 0; q < n; q += kAhead) {
+            Piece<T, VEC> p[kAhead][NV];
+            int at[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                at[u] = __shfl_sync(mask, pos, (q + u) % TPR, TPR);
+                if (q + u >= n) at[u] = -1;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    const int c = c0 + k * TPR * VEC;
+                    p[u][k].load(dy + (long long)max(at[u], 0) * a.C + (c < a.C ? c : 0));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (q + u >= n) break;
+                while (i0 + q + u >= end) {  // this token is of a later row
+                    flush(j);
+                    end = __shfl_sync(mask, r.y, ++j, TPR);
+                }
+#pragma unroll
+                for (int k = 0; k < NV * VEC; ++k)
+                    acc[k] += at[u] >= 0 ? p[u][k / VEC].get(k % VEC) : 0.f;
             }
         }
     }
+    for (; j < mine; ++j) flush(j);
 }
 
-// Block (chunk, slice): the sums of the chunk's long rows, warps taking every
-// eighth token, joined in warp order.
-template <typename T, int VEC, int NV>
-__global__ void __launch_bounds__(kThreads)
-    embed_bwd_chunks_kernel(const GradArgs a, const T* __restrict__ dy) {
-    constexpr int kWarps = kThreads / 32, kWidth = NV * VEC * 32;
-    __shared__ float sh[kWarps][kWidth];
-    pdl_wait();
-    pdl_trigger();
+// The sums of a chunk's long rows. The 8 warps are `sl` slices of 32 * VEC
+// channels times 8 / sl shares of the tokens; shares are joined in order.
+template <typename T, int VEC>
+__device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restrict__ dy, int index,
+                                           float (*sh)[32 * VEC]) {
+    constexpr int kWarps = kThreads / 32, kWidth = 32 * VEC;
     const int total = entries(a), chunk = chunk_of(a, total);
-    const long long b = (long long)blockIdx.x * chunk;
+    const long long b = (long long)index * chunk;
     if (b >= total) return;
     const int p0 = (int)b, p1 = (int)(b + chunk < total ? b + chunk : total);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int s0 = blockIdx.y * kWidth;
-    int row = row_at(a, p0);
-    for (int slot = 0; slot < 2; ++slot) {
-        if (slot == 1) {
-            const int last = row_at(a, p1 - 1);
-            if (last == row) break;
-            row = last;
-        }
-        const int2 r = tokens_of(a, row);
+    const int2 row = rows_at(a, make_int2(p0, p1 - 1));
+    int sl = 1;
+    while (sl < kWarps && sl * kWidth < a.C) sl *= 2;
+    const int shares = kWarps / sl, share = warp / sl;
+    for (int slot = 0; slot < (row.y == row.x ? 1 : 2); ++slot) {
+        const int2 r = tokens_of(a, slot ? row.y : row.x);
         if (r.y - r.x <= chunk) continue;
-        const int e = min(r.y, p1);
-        float acc[NV * VEC];
+        float* const out = a.part + (2ll * index + slot) * a.C;
+        for (int s0 = 0; s0 < a.C; s0 += sl * kWidth) {
+            const int c = s0 + warp % sl * kWidth + lane * VEC;
+            float acc[VEC];
 #pragma unroll
-        for (int k = 0; k < NV * VEC; ++k) acc[k] = 0.f;
-        add_tokens<T, VEC, 32, NV>(a, dy, max(r.x, p0) + warp, e, kWarps, s0 + lane * VEC,
-                                   0xffffffffu, acc);
-        __syncthreads();
+            for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
+            add_tokens<T, VEC, 32, 1>(a, dy, max(r.x, p0) + share, min(r.y, p1), shares, c,
+                                      0xffffffffu, acc);
+            if (shares > 1) {
+                __syncthreads();
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+                for (int v = 0; v < VEC; ++v) sh[warp][lane * VEC + v] = acc[v];
+                __syncthreads();
+                if (share == 0)
+                    for (int q = 1; q < shares; ++q)
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) sh[warp][(k * 32 + lane) * VEC + v] = acc[k * VEC + v];
-        __syncthreads();
-        float* const out = a.part + (2ll * blockIdx.x + slot) * a.C;
-        for (int c = threadIdx.x; c < kWidth && s0 + c < a.C; c += kThreads) {
-            float s = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) s += sh[w][c];
-            out[s0 + c] = s;
+                        for (int v = 0; v < VEC; ++v) acc[v] += sh[warp + q * sl][lane * VEC + v];
+            }
+            if (share == 0 && c < a.C) store_floats<VEC>(out + c, acc);
         }
     }
 }
 
-// Block (chunk, 256 channels): if a long row starts in the chunk, the sum of
-// its chunks' sums in order, a thread per channel.
-__global__ void __launch_bounds__(kThreads) embed_bwd_join_kernel(const GradArgs a) {
+// Blocks [0, chunks): chunks; the others: groups of table rows.
+template <typename T, int VEC, int TPR, int NV>
+__global__ void __launch_bounds__(kThreads)
+    embed_bwd_kernel(const GradArgs a, const T* __restrict__ dy, int chunks, int slices,
+                     int per) {
+    __shared__ float sh[kThreads / 32][32 * VEC];
+    pdl_wait();
+    pdl_trigger();
+    if ((int)blockIdx.x < chunks) {
+        chunk_role<T, VEC>(a, dy, (int)blockIdx.x, sh);
+    } else {
+        int slice;
+        const long long block = div32((int)blockIdx.x - chunks, slices, slice);
+        rows_role<T, VEC, TPR, NV>(a, dy, per, block * (kThreads / TPR) + threadIdx.x / TPR, slice);
+    }
+}
+
+// Block `chunk`: if a long row starts in it, the sum of the row's chunks' sums
+// in order, a thread per channel.
+__global__ void __launch_bounds__(1024) embed_bwd_join_kernel(const GradArgs a) {
     pdl_wait();
     pdl_trigger();
     const int total = entries(a), chunk = chunk_of(a, total);
     const long long b = (long long)blockIdx.x * chunk;
     if (b >= total) return;
     const int p1 = (int)(b + chunk < total ? b + chunk : total);
-    const int row = row_at(a, p1 - 1);
+    const int row = rows_at(a, make_int2(p1 - 1, p1 - 1)).x;
     const int2 r = tokens_of(a, row);
     if (r.y - r.x <= chunk || r.x < b) return;
-    const int c = blockIdx.y * kThreads + threadIdx.x;
-    if (c >= a.C) return;
     // the row starts in this chunk: at its first entry (slot 0) or later
     // (slot 1); it holds the first entry of every later chunk (slot 0)
     const int k1 = (r.y - 1) / chunk;
-    float s = a.part[(2ll * blockIdx.x + (r.x == b ? 0 : 1)) * a.C + c];
+    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+        float s = a.part[(2ll * blockIdx.x + (r.x == b ? 0 : 1)) * a.C + c];
 #pragma unroll 8
-    for (int k = blockIdx.x + 1; k <= k1; ++k) s += a.part[2ll * k * a.C + c];
-    a.dtable[(long long)row * a.C + c] = s * a.scale;
+        for (int k = blockIdx.x + 1; k <= k1; ++k) s += a.part[2ll * k * a.C + c];
+        a.dtable[(long long)row * a.C + c] = s * a.scale;
+    }
 }
 
 bool aligned16(const void* p) {
@@ -465,44 +603,42 @@ hc_status run_fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* tabl
 }
 
 template <typename T, int VEC, int TPR, int NV>
-hc_status bwd_rows(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStream_t s) {
+hc_status bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStream_t s) {
     const int slices = (a.C + NV * TPR * VEC - 1) / (NV * TPR * VEC);
-    // consecutive rows per group: one while the groups fill the SMs, then up to 16
+    const int chunks = a.max_chunks > 1 ? a.max_chunks : 0;  // one chunk: no row is longer
+    // table rows per group: one while the groups fill the SMs
     const long long groups = (long long)ctx->num_sms * 16 * (kThreads / TPR);
     long long per = ((long long)a.V * slices + groups - 1) / groups;
-    per = per < 1 ? 1 : per > 16 ? 16 : per;
+    const int most = TPR < kMaxPer ? TPR : kMaxPer;
+    per = per < 1 ? 1 : per > most ? most : per;
     const long long blocks = (a.V + per * (kThreads / TPR) - 1) / (per * (kThreads / TPR));
-    return launch_pdl(embed_bwd_rows_kernel<T, VEC, TPR, NV>,
-                      dim3((unsigned)blocks, (unsigned)slices), dim3(kThreads), 0, s,
-                      "embed_bwd_rows_kernel", a, (const T*)dy, (int)per);
+    const long long grid = blocks * slices + chunks;
+    if (grid > 0x7fffffffll) {
+        set_error("hc_embedding_bwd: V=%d C=%d is too large", a.V, a.C);
+        return HC_ERR_UNSUPPORTED;
+    }
+    hc_status st = launch_pdl(embed_bwd_kernel<T, VEC, TPR, NV>, dim3((unsigned)grid),
+                              dim3(kThreads), 0, s, "embed_bwd_kernel", a, (const T*)dy, chunks,
+                              slices, (int)per);
+    if (st != HC_OK || chunks == 0) return st;
+    const int threads = a.C >= 1024 ? 1024 : (a.C + 31) / 32 * 32;
+    return launch_pdl(embed_bwd_join_kernel, dim3((unsigned)chunks), dim3((unsigned)threads), 0, s,
+                      "embed_bwd_join_kernel", a);
 }
 
+// Pieces of four channels: the fp32 sums of a warp's pieces then leave as
+// whole 16-byte stores side by side (pieces of eight bf16 channels would
+// store every other 16 bytes at a time).
 template <typename T>
-hc_status run_bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, int chunks,
-                  cudaStream_t s) {
-    constexpr int kVec = 16 / (int)sizeof(T);
-    const bool wide = a.C % kVec == 0 && aligned16(dy) && aligned16(a.dtable);
-    hc_status st;
-    if (chunks > 1) {  // else no row is longer than a chunk
-        const int width = wide ? 32 * kVec : 256;
-        const dim3 grid((unsigned)chunks, (unsigned)((a.C + width - 1) / width));
-        st = wide ? launch_pdl(embed_bwd_chunks_kernel<T, kVec, 1>, grid, dim3(kThreads), 0, s,
-                               "embed_bwd_chunks_kernel", a, (const T*)dy)
-                  : launch_pdl(embed_bwd_chunks_kernel<T, 1, 8>, grid, dim3(kThreads), 0, s,
-                               "embed_bwd_chunks_kernel", a, (const T*)dy);
-        if (st != HC_OK) return st;
-        st = launch_pdl(embed_bwd_join_kernel,
-                        dim3((unsigned)chunks, (unsigned)((a.C + kThreads - 1) / kThreads)),
-                        dim3(kThreads), 0, s, "embed_bwd_join_kernel", a);
-        if (st != HC_OK) return st;
+hc_status run_bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStream_t s) {
+    if (a.C % 4 == 0 && aligned16(dy) && aligned16(a.dtable)) {
+        if (a.C <= 32) return bwd<T, 4, 8, 1>(ctx, a, dy, s);
+        if (a.C <= 128) return bwd<T, 4, 32, 1>(ctx, a, dy, s);
+        if (a.C <= 256) return bwd<T, 4, 32, 2>(ctx, a, dy, s);
+        return bwd<T, 4, 32, 4>(ctx, a, dy, s);
     }
-    if (wide) {
-        if (a.C <= 8 * kVec) return bwd_rows<T, kVec, 8, 1>(ctx, a, dy, s);
-        if (a.C <= 32 * kVec) return bwd_rows<T, kVec, 32, 1>(ctx, a, dy, s);
-        return bwd_rows<T, kVec, 32, 4>(ctx, a, dy, s);
-    }
-    if (a.C <= 32) return bwd_rows<T, 1, 8, 4>(ctx, a, dy, s);
-    return bwd_rows<T, 1, 32, 8>(ctx, a, dy, s);
+    if (a.C <= 32) return bwd<T, 1, 8, 4>(ctx, a, dy, s);
+    return bwd<T, 1, 32, 4>(ctx, a, dy, s);
 }
 
 }  // namespace
@@ -580,16 +716,12 @@ hc_status launch_embedding_bwd(const DeviceCtx* ctx, const EmbeddingArgs& a, con
     const int chunks = (int)(need < ctx->num_sms * 4 ? need : ctx->num_sms * 4);
     GradArgs b{row_ptr, order, a.capacity, a.V, a.C, chunks < 1 ? 1 : chunks, a.scale, nullptr,
                dtable, ctx->status};
-    if ((a.C + 31) / 32 > 65535) {  // the smallest slice of channels, blockIdx.y
-        set_error("hc_embedding_bwd: C=%d is too wide", a.C);
-        return HC_ERR_UNSUPPORTED;
-    }
     if (chunks > 1) {
         b.part = (float*)stream_workspace(s, (size_t)chunks * 2 * a.C * sizeof(float));
         if (!b.part) return HC_ERR_CUDA;
     }
-    return a.dt == HC_BF16 ? run_bwd<__nv_bfloat16>(ctx, b, dy, chunks, s)
-                           : run_bwd<float>(ctx, b, dy, chunks, s);
+    return a.dt == HC_BF16 ? run_bwd<__nv_bfloat16>(ctx, b, dy, s)
+                           : run_bwd<float>(ctx, b, dy, s);
 }
 
 }  // namespace hc

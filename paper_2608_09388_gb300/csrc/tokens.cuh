@@ -75,6 +75,17 @@ struct Piece<float, 4> {
     }
 };
 template <>
+struct Piece<__nv_bfloat16, 4> {
+    uint2 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        v = *reinterpret_cast<const uint2*>(p);
+    }
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t w = i >> 1 ? v.y : v.x;
+        return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    }
+};
+template <>
 struct Piece<__nv_bfloat16, 8> {
     uint4 v;
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
