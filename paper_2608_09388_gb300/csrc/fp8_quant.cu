@@ -28,38 +28,102 @@ __device__ __forceinline__ uint8_t e4m3(float x, float scale) {
     return (uint8_t)__nv_cvt_float_to_fp8(x / scale, __NV_SATFINITE, __NV_E4M3);
 }
 
-// A warp per (row, block of 128 channels).
-template <typename T>
+// The e4m3 bytes of N values x / scale. x * (1 / scale) is within 2^-22 of
+// the fp32 quotient (one rounding each of the reciprocal, the product and the
+// quotient), so both round to the same e4m3 value unless a boundary between
+// two of them is that near: a magnitude from 2^-6 up whose mantissa, cut to
+// three bits, leaves one half give or take 4 units of the last place, or any
+// magnitude below 2^-6, where e4m3 has fewer bits. Only those are divided.
+template <int N>
+__device__ __forceinline__ void to_e4m3(const float (&x)[N], float scale, float inv,
+                                        uint32_t (&w)[N / 4]) {
+    float t[N];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        t[i] = x[i] * inv;
+        const uint32_t m = __float_as_uint(t[i]) & 0x7fffffffu;
+        near |= (m & 0xfffffu) - 0x7fffcu <= 8u || (m < 0x3c800000u && m != 0u);
+    }
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = x[i] / scale;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const uint32_t lo =
+            __nv_cvt_float2_to_fp8x2(make_float2(t[i], t[i + 1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi =
+            __nv_cvt_float2_to_fp8x2(make_float2(t[i + 2], t[i + 3]), __NV_SATFINITE, __NV_E4M3);
+        w[i / 4] = lo | hi << 16;
+    }
+}
+
+// Blocks of 128 channels are numbered row by row. 128 / V lanes hold a block,
+// V channels (16 bytes) each; a warp works on 32 V / 128 blocks at a time and
+// has kAhead such steps in flight. VEC = V where rows allow 16-byte loads,
+// else 1.
+constexpr int kAhead = 4;
+
+template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads)
     quant_rows_kernel(const T* __restrict__ x, const int32_t* count, long long capacity, int C,
                       int pitch, int nb, uint8_t* __restrict__ q, float* __restrict__ scales,
                       unsigned* status) {
+    constexpr int V = 16 / (int)sizeof(T), kLanes = 128 / V, kBlocks = 32 / kLanes;
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
-    const int lane = threadIdx.x & 31;
-    const long long items = rows * nb;
-    for (long long it = (blockIdx.x * (long long)kThreads + threadIdx.x) >> 5; it < items;
-         it += (long long)gridDim.x * (kThreads / 32)) {
+    const int lane = threadIdx.x & 31, sub = lane / kLanes, part = lane % kLanes;
+    const long long blocks = rows * nb;
+    const long long step = (long long)gridDim.x * (kThreads / 32) * kBlocks * kAhead;
+    long long g0 = (long long)((blockIdx.x * kThreads + threadIdx.x) >> 5) * kBlocks * kAhead;
+    for (; g0 < blocks; g0 += step) {
         int b;
-        const long long n = div32(it, nb, b);
-        float v[4], m = 0.f;
+        long long n = div32(g0 + sub, nb, b);
+        Piece<T, VEC> p[kAhead][V / VEC];
+        long long at_n[kAhead];
+        int at_b[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int c = b * 128 + lane * 4 + j;
-            v[j] = c < C ? to_f32(x[n * C + c]) : 0.f;
-            m = max_nan(fabsf(v[j]), m);
+        for (int k = 0; k < kAhead; ++k) {
+            at_n[k] = n;
+            at_b[k] = b;
+            const int c = b * 128 + part * V;
+            const long long row = n < rows ? n : 0;  // absent blocks read row 0
+#pragma unroll
+            for (int v = 0; v < V / VEC; ++v)
+                p[k][v].load(x + row * C + (c + v < C ? c + v : 0));
+            b += kBlocks;
+            while (b >= nb) {
+                b -= nb;
+                ++n;
+            }
         }
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = max_nan(__shfl_xor_sync(0xffffffffu, m, o), m);
-        const float sc = scale_of(m);
-        uint32_t w = 0;
+        for (int k = 0; k < kAhead; ++k) {
+            const int c = at_b[k] * 128 + part * V;
+            float f[V], m = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w |= (b * 128 + lane * 4 + j < C ? (uint32_t)e4m3(v[j], sc) : 0u) << (8 * j);
-        if (b * 128 + lane * 4 < pitch)
-            *reinterpret_cast<uint32_t*>(q + n * pitch + b * 128 + lane * 4) = w;
-        if (lane == 0) scales[(long long)b * capacity + n] = sc;
+            for (int v = 0; v < V; ++v) {
+                f[v] = c + v < C ? p[k][v / VEC].get(v % VEC) : 0.f;
+                m = max_nan(fabsf(f[v]), m);
+            }
+#pragma unroll
+            for (int o = kLanes / 2; o > 0; o >>= 1)
+                m = max_nan(__shfl_xor_sync(0xffffffffu, m, o), m);
+            if (at_n[k] >= rows) continue;
+            const float sc = scale_of(m);
+            uint32_t w[V / 4];
+            to_e4m3<V>(f, sc, 1.f / sc, w);
+            if (c < pitch) {
+                uint8_t* const out = q + at_n[k] * pitch + c;
+                if constexpr (V == 8)
+                    *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+                else
+                    *reinterpret_cast<uint32_t*>(out) = w[0];
+            }
+            if (part == 0) scales[(long long)at_b[k] * capacity + at_n[k]] = sc;
+        }
     }
 }
 
@@ -101,22 +165,34 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
+template <typename T, int VEC>
+hc_status quant_rows_as(const DeviceCtx* ctx, const void* x, const int32_t* count, int capacity,
+                        int C, int pitch, int nb, uint8_t* q, float* scales, cudaStream_t s) {
+    constexpr int kPerBlock = kThreads / 32 * kAhead * 32 / (128 * (int)sizeof(T) / 16);
+    const long long need = ((long long)capacity * nb + kPerBlock - 1) / kPerBlock;
+    const long long cap = (long long)ctx->num_sms * 16;
+    return launch_pdl(quant_rows_kernel<T, VEC>, dim3((unsigned)(need < cap ? need : cap)),
+                      dim3(kThreads), 0, s, "quant_rows_kernel", (const T*)x, count,
+                      (long long)capacity, C, pitch, nb, q, scales, ctx->status);
+}
+
+template <typename T>
+hc_status quant_rows(const DeviceCtx* ctx, const void* x, const int32_t* count, int capacity,
+                     int C, int pitch, int nb, uint8_t* q, float* scales, cudaStream_t s) {
+    constexpr int V = 16 / (int)sizeof(T);
+    if (C % V == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0)
+        return quant_rows_as<T, V>(ctx, x, count, capacity, C, pitch, nb, q, scales, s);
+    return quant_rows_as<T, 1>(ctx, x, count, capacity, C, pitch, nb, q, scales, s);
+}
+
 }  // namespace
 
 hc_status launch_quantize_fp8_rows(const DeviceCtx* ctx, const void* x, hc_dtype dt,
                                    const int32_t* count, int capacity, int C, uint8_t* q,
                                    float* scales, cudaStream_t s) {
     const int pitch = HC_FP8_PITCH(C), nb = (C + 127) / 128;
-    long long blocks = ((long long)capacity * nb + kThreads / 32 - 1) / (kThreads / 32);
-    const long long cap = (long long)ctx->num_sms * 16;
-    if (blocks > cap) blocks = cap;
-    if (dt == HC_BF16)
-        return launch_pdl(quant_rows_kernel<__nv_bfloat16>, dim3((unsigned)blocks), dim3(kThreads),
-                          0, s, "quant_rows_kernel", (const __nv_bfloat16*)x, count,
-                          (long long)capacity, C, pitch, nb, q, scales, ctx->status);
-    return launch_pdl(quant_rows_kernel<float>, dim3((unsigned)blocks), dim3(kThreads), 0, s,
-                      "quant_rows_kernel", (const float*)x, count, (long long)capacity, C, pitch,
-                      nb, q, scales, ctx->status);
+    return dt == HC_BF16 ? quant_rows<__nv_bfloat16>(ctx, x, count, capacity, C, pitch, nb, q, scales, s)
+                         : quant_rows<float>(ctx, x, count, capacity, C, pitch, nb, q, scales, s);
 }
 
 hc_status launch_quantize_fp8_weight(const DeviceCtx*, const void* W, hc_dtype dt, int C_in,
