@@ -27,45 +27,58 @@ __device__ __forceinline__ float scale_of(float amax) {
 __device__ __forceinline__ uint8_t e4m3(float x, float scale) {
     return (uint8_t)__nv_cvt_float_to_fp8(x / scale, __NV_SATFINITE, __NV_E4M3);
 }
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+}
 
-// The e4m3 bytes of N values x / scale. x * (1 / scale) is within 2^-22 of
-// the fp32 quotient (one rounding each of the reciprocal, the product and the
-// quotient), so both round to the same e4m3 value unless a boundary between
-// two of them is that near: a magnitude from 2^-6 up whose mantissa, cut to
-// three bits, leaves one half give or take 4 units of the last place, or any
-// magnitude below 2^-6, where e4m3 has fewer bits. Only those are divided.
+// The e4m3 bytes of N values x / scale. With inv the rounded reciprocal,
+// x * (inv * (1 - 2^-21)) and x * (inv * (1 + 2^-21)) enclose the fp32
+// quotient (four roundings of at most 2^-24 each separate it from x * inv),
+// and rounding to e4m3 is monotonic: where both products round alike, so does
+// the quotient. Only the others are divided.
 template <int N>
 __device__ __forceinline__ void to_e4m3(const float (&x)[N], float scale, float inv,
                                         uint32_t (&w)[N / 4]) {
-    float t[N];
-    bool near = false;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        t[i] = x[i] * inv;
-        const uint32_t m = __float_as_uint(t[i]) & 0x7fffffffu;
-        near |= (m & 0xfffffu) - 0x7fffcu <= 8u || (m < 0x3c800000u && m != 0u);
-    }
-    if (near) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) t[i] = x[i] / scale;
-    }
+    const float below = inv * (1.f - 0x1p-21f), above = inv * (1.f + 0x1p-21f);
+    uint32_t differ = 0;
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-        const uint32_t lo =
-            __nv_cvt_float2_to_fp8x2(make_float2(t[i], t[i + 1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi =
-            __nv_cvt_float2_to_fp8x2(make_float2(t[i + 2], t[i + 3]), __NV_SATFINITE, __NV_E4M3);
-        w[i / 4] = lo | hi << 16;
+        w[i / 4] = pack_e4m3(x[i] * below, x[i + 1] * below, x[i + 2] * below, x[i + 3] * below);
+        differ |= w[i / 4] ^
+                  pack_e4m3(x[i] * above, x[i + 1] * above, x[i + 2] * above, x[i + 3] * above);
+    }
+    if (differ) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            w[i / 4] = pack_e4m3(x[i] / scale, x[i + 1] / scale, x[i + 2] / scale, x[i + 3] / scale);
     }
 }
 
-// Blocks of 128 channels are numbered row by row. 128 / V lanes hold a block,
-// V channels (16 bytes) each; a warp works on 32 V / 128 blocks at a time and
-// has kAhead such steps in flight. VEC = V where rows allow 16-byte loads,
-// else 1.
-constexpr int kAhead = 4;
+// Largest magnitude of a lane's 16 bytes of channels as fp32 bits: magnitudes
+// compare as unsigned numbers, a NaN above all.
+__device__ __forceinline__ uint32_t amax_bits(const Piece<float, 4>& p) {
+    const uint32_t a = max(__float_as_uint(fabsf(p.v.x)), __float_as_uint(fabsf(p.v.y)));
+    const uint32_t b = max(__float_as_uint(fabsf(p.v.z)), __float_as_uint(fabsf(p.v.w)));
+    return max(a, b);
+}
+__device__ __forceinline__ uint32_t amax_bits(const Piece<__nv_bfloat16, 8>& p) {
+    constexpr uint32_t kMag = 0x7fff7fffu;
+    const uint32_t m = __vmaxu2(__vmaxu2(p.v.x & kMag, p.v.y & kMag),
+                                __vmaxu2(p.v.z & kMag, p.v.w & kMag));
+    return max(m << 16, m & 0xffff0000u);
+}
 
-template <typename T, int VEC>
+// Blocks of 128 channels are numbered row by row. 128 / V lanes hold a block,
+// V channels (16 bytes) each; a warp takes 32 V / 128 blocks a step and four
+// steps at a time, so that four loads are in flight and the four steps' scales
+// are found together: the reduction over a block's lanes halves the steps a
+// lane carries at its first two exchanges, after which lane l holds step l % 4
+// and divides for it alone. kWide: rows allow 16-byte loads.
+constexpr int kSteps = 4;
+
+template <typename T, bool kWide>
 __global__ void __launch_bounds__(kThreads)
     quant_rows_kernel(const T* __restrict__ x, const int32_t* count, long long capacity, int C,
                       int pitch, int nb, uint8_t* __restrict__ q, float* __restrict__ scales,
@@ -76,53 +89,71 @@ __global__ void __launch_bounds__(kThreads)
     const long long rows = token_rows(count, capacity, status);
     const int lane = threadIdx.x & 31, sub = lane / kLanes, part = lane % kLanes;
     const long long blocks = rows * nb;
-    const long long step = (long long)gridDim.x * (kThreads / 32) * kBlocks * kAhead;
-    long long g0 = (long long)((blockIdx.x * kThreads + threadIdx.x) >> 5) * kBlocks * kAhead;
+    const long long step = (long long)gridDim.x * (kThreads / 32) * kBlocks * kSteps;
+    long long g0 = (long long)((blockIdx.x * kThreads + threadIdx.x) >> 5) * kBlocks * kSteps;
     for (; g0 < blocks; g0 += step) {
         int b;
         long long n = div32(g0 + sub, nb, b);
-        Piece<T, VEC> p[kAhead][V / VEC];
-        long long at_n[kAhead];
-        int at_b[kAhead];
+        Piece<T, V> p[kSteps];
+        long long at_n[kSteps];
+        int at_c[kSteps];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < kSteps; ++k) {
             at_n[k] = n;
-            at_b[k] = b;
-            const int c = b * 128 + part * V;
-            const long long row = n < rows ? n : 0;  // absent blocks read row 0
+            at_c[k] = b * 128 + part * V;
+            const T* const xr = x + (n < rows ? n : 0) * C;  // absent blocks read row 0
+            if constexpr (kWide) {
+                p[k].load(xr + (at_c[k] < C ? at_c[k] : 0));
+            } else {
 #pragma unroll
-            for (int v = 0; v < V / VEC; ++v)
-                p[k][v].load(x + row * C + (c + v < C ? c + v : 0));
+                for (int v = 0; v < V; ++v) {
+                    const int c = at_c[k] + v;
+                    p[k].set(v, c < C ? to_f32(xr[c]) : 0.f);
+                }
+            }
             b += kBlocks;
             while (b >= nb) {
                 b -= nb;
                 ++n;
             }
         }
+        uint32_t m[kSteps];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int c = at_b[k] * 128 + part * V;
-            float f[V], m = 0.f;
+        for (int k = 0; k < kSteps; ++k) m[k] = at_c[k] < C ? amax_bits(p[k]) : 0u;
+        const bool b0 = lane & 1, b1 = lane & 2;
+        const uint32_t m01 =
+            max(b0 ? m[1] : m[0], __shfl_xor_sync(0xffffffffu, b0 ? m[0] : m[1], 1));
+        const uint32_t m23 =
+            max(b0 ? m[3] : m[2], __shfl_xor_sync(0xffffffffu, b0 ? m[2] : m[3], 1));
+        uint32_t top = max(b1 ? m23 : m01, __shfl_xor_sync(0xffffffffu, b1 ? m01 : m23, 2));
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                f[v] = c + v < C ? p[k][v / VEC].get(v % VEC) : 0.f;
-                m = max_nan(fabsf(f[v]), m);
-            }
+        for (int o = 4; o < kLanes; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float my_scale = scale_of(__uint_as_float(top)), my_inv = 1.f / my_scale;
+        if (part < kSteps) {
+            const long long mine = g0 + sub + (long long)part * kBlocks;
+            int mb;
+            const long long mn = div32(mine, nb, mb);
+            if (mn < rows) scales[(long long)mb * capacity + mn] = my_scale;
+        }
 #pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1)
-                m = max_nan(__shfl_xor_sync(0xffffffffu, m, o), m);
-            if (at_n[k] >= rows) continue;
-            const float sc = scale_of(m);
+        for (int k = 0; k < kSteps; ++k) {
+            const float sc = __shfl_sync(0xffffffffu, my_scale, sub * kLanes + k);
+            const float inv = __shfl_sync(0xffffffffu, my_inv, sub * kLanes + k);
+            if (at_n[k] >= rows || at_c[k] >= pitch) continue;
+            float f[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) f[v] = p[k].get(v);
             uint32_t w[V / 4];
-            to_e4m3<V>(f, sc, 1.f / sc, w);
-            if (c < pitch) {
-                uint8_t* const out = q + at_n[k] * pitch + c;
-                if constexpr (V == 8)
-                    *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
-                else
-                    *reinterpret_cast<uint32_t*>(out) = w[0];
+            to_e4m3<V>(f, sc, inv, w);
+            if (at_c[k] >= C) {
+#pragma unroll
+                for (int v = 0; v < V / 4; ++v) w[v] = 0u;  // beyond C
             }
-            if (part == 0) scales[(long long)at_b[k] * capacity + at_n[k]] = sc;
+            uint8_t* const out = q + at_n[k] * pitch + at_c[k];
+            if constexpr (V == 8)
+                *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+            else
+                *reinterpret_cast<uint32_t*>(out) = w[0];
         }
     }
 }
@@ -165,24 +196,17 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
-template <typename T, int VEC>
-hc_status quant_rows_as(const DeviceCtx* ctx, const void* x, const int32_t* count, int capacity,
-                        int C, int pitch, int nb, uint8_t* q, float* scales, cudaStream_t s) {
-    constexpr int kPerBlock = kThreads / 32 * kAhead * 32 / (128 * (int)sizeof(T) / 16);
-    const long long need = ((long long)capacity * nb + kPerBlock - 1) / kPerBlock;
-    const long long cap = (long long)ctx->num_sms * 16;
-    return launch_pdl(quant_rows_kernel<T, VEC>, dim3((unsigned)(need < cap ? need : cap)),
-                      dim3(kThreads), 0, s, "quant_rows_kernel", (const T*)x, count,
-                      (long long)capacity, C, pitch, nb, q, scales, ctx->status);
-}
-
 template <typename T>
 hc_status quant_rows(const DeviceCtx* ctx, const void* x, const int32_t* count, int capacity,
                      int C, int pitch, int nb, uint8_t* q, float* scales, cudaStream_t s) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (C % V == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0)
-        return quant_rows_as<T, V>(ctx, x, count, capacity, C, pitch, nb, q, scales, s);
-    return quant_rows_as<T, 1>(ctx, x, count, capacity, C, pitch, nb, q, scales, s);
+    constexpr int V = 16 / (int)sizeof(T), kPerBlock = kThreads / 32 * kSteps * 32 * V / 128;
+    const long long need = ((long long)capacity * nb + kPerBlock - 1) / kPerBlock;
+    const long long cap = (long long)ctx->num_sms * 16;
+    const bool wide = C % V == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    return launch_pdl(wide ? quant_rows_kernel<T, true> : quant_rows_kernel<T, false>,
+                      dim3((unsigned)(need < cap ? need : cap)), dim3(kThreads), 0, s,
+                      "quant_rows_kernel", (const T*)x, count, (long long)capacity, C, pitch, nb,
+                      q, scales, ctx->status);
 }
 
 }  // namespace
