@@ -54,7 +54,12 @@ struct Cfg {
     // bits 7 and 10), both K-major, N >> 3 at 17, M >> 4 at 24.
     static constexpr uint32_t kIdesc =
         (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kLanes >> 4) << 24);
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + 256;
+    // after the stages: bias of each promoting warp's columns, output staging
+    // (32 rows x 64 bytes a warp), barriers
+    static constexpr int kBiasBytes = kPromoteWarps * kCols * 4;
+    static constexpr int kOutBytes = kPromoteWarps * 32 * 64;
+    static constexpr size_t kSmem =
+        1024 + (size_t)kStages * kStageBytes + kBiasBytes + kOutBytes + 256;
     // the split totals [BN][128] fp32 reuse the stages
     static_assert((size_t)kStages * kStageBytes >= (size_t)BN * kLanes * 4, "split totals");
 };
@@ -100,6 +105,34 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[8]) {
         : "r"(taddr)
         : "memory");
 }
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile(
+        "{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(e));
+    return e != 0;
+}
+// (a0, a1) += (v0, v1) * (s, s), one instruction for both.
+__device__ __forceinline__ void fma_pair(float& a0, float& a1, uint32_t v0, uint32_t v1, float s) {
+    unsigned long long a, v, ss;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(a) : "f"(a0), "f"(a1));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(v0), "r"(v1));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(ss) : "f"(s));
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(v), "l"(ss));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(a));
+}
+// A pipeline wait of this kernel, by a whole warp. A few tries first: the
+// shared bounded wait reads its limit from global memory once a try has
+// failed, longer than most waits here last.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                         unsigned* status, unsigned long long limit) {
+    bool ok = false;
+#pragma unroll 1
+    for (int i = 0; i < 16 && !ok; ++i) ok = mbar_try_wait(bar, parity);
+    if (!ok) ok = mbar_wait_for(bar, parity, abort_flag, status, limit);
+    return __all_sync(0xffffffffu, ok);
+}
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
 }
@@ -129,6 +162,72 @@ __device__ __forceinline__ void tile_at(long long t, int tm, int tn, int& m, int
     m = first + (r - n * in);
 }
 
+template <int kAct>
+struct Act {
+    static constexpr int value = kAct;
+};
+
+// Bias, activation and store of a warp's 32 rows (one per lane, from row r0
+// on) x kCols channels from o0 on. 64 bytes of every row at a time go through
+// the warp's staging buffer (16-byte pieces swizzled so that neither side has
+// bank conflicts) and leave as whole 64-byte pieces of rows: straight from
+// the registers a store would touch 32 rows with 16 bytes each.
+template <typename T, int kCols, int kAct>
+__device__ __forceinline__ void store_tile(const float (&acc)[kCols], const float* bias,
+                                           uint32_t stage, T* y, long long r0, long long rows,
+                                           int o0, int C_out) {
+    constexpr int kV = 16 / (int)sizeof(T), kPass = 64 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+    const bool wide = C_out % kV == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0;
+#pragma unroll
+    for (int p = 0; p < kCols; p += kPass) {
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = p + q * kV + i * (kV / 4);
+                if constexpr (sizeof(T) == 4) {
+                    w[i] = __float_as_uint(act_fixed<kAct>(acc[j] + bias[j]));
+                } else {
+                    const __nv_bfloat162 v =
+                        __floats2bfloat162_rn(act_fixed<kAct>(acc[j] + bias[j]),
+                                              act_fixed<kAct>(acc[j + 1] + bias[j + 1]));
+                    w[i] = *reinterpret_cast<const uint32_t*>(&v);
+                }
+            }
+            sts_v4(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4),
+                   make_uint4(w[0], w[1], w[2], w[3]));
+        }
+        __syncwarp();
+        if (wide) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2), q = lane & 3;
+                const int o = o0 + p + q * kV;
+                const uint4 v = lds_u4(stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
+                if (r0 + r < rows && o < C_out)
+                    *reinterpret_cast<uint4*>(y + (r0 + r) * C_out + o) = v;
+            }
+        } else {
+            for (int i = lane; i < 32 * kPass; i += 32) {
+                const int r = i / kPass, j = i % kPass, q = j / kV;
+                const uint32_t at = stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4) + j % kV * (int)sizeof(T);
+                T v;
+                if constexpr (sizeof(T) == 4) {
+                    v = __int_as_float(lds_s32(at));
+                } else {
+                    uint16_t b;
+                    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(b) : "r"(at) : "memory");
+                    v = __ushort_as_bfloat16(b);
+                }
+                if (r0 + r < rows && o0 + p + j < C_out) y[(r0 + r) * C_out + o0 + p + j] = v;
+            }
+        }
+    }
+}
+
 template <int BN, bool kSwap, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
     fp8_linear_kernel(const KernelArgs k, const __grid_constant__ CUtensorMap map_x,
@@ -138,7 +237,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t bars = base + C::kStages * C::kStageBytes;
+    const uint32_t bias_at = base + C::kStages * C::kStageBytes;
+    const uint32_t out_at = bias_at + C::kBiasBytes;
+    const uint32_t bars = out_at + C::kOutBytes;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (C::kStages + s); };
     auto tfull_bar = [&](int b) { return bars + 8u * (2 * C::kStages + b); };
@@ -176,6 +277,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_wait();
     pdl_trigger();
 
+    const unsigned long long limit =
+        reinterpret_cast<const volatile DeviceWord*>(a.status)->wait_limit_ns;
     const long long rows = token_rows(a.count, a.capacity, a.status);
     const int tm = (int)((rows + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes));
     const int tn = (a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN);
@@ -185,60 +288,62 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int kb1 = (int)((long long)k.nkb * (rank + 1) / k.split);
     const long long first = blockIdx.x / k.split, step = gridDim.x / k.split;
 
+    // In all roles every lane of the warp walks the loop, so that its state is
+    // uniform; the copies and MMAs are issued by one lane.
     if (warp == kLoadWarp) {
-        if (lane == 0) {
-            long long it = 0;
-            bool ok = true;
-            for (long long t = first; t < tiles && ok; t += step) {
-                int m, n;
-                tile_at(t, tm, tn, m, n);
-                const int ra = (kSwap ? n : m) * kLanes, rb = (kSwap ? m : n) * BN;
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = (int)(it % C::kStages);
-                    const uint32_t ph = (uint32_t)((it / C::kStages) & 1);
-                    if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag, a.status)) {
-                        ok = false;
-                        break;
-                    }
+        const bool leader = elect_one();
+        uint32_t it = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += step) {
+            int m, n;
+            tile_at(t, tm, tn, m, n);
+            const int ra = (kSwap ? n : m) * kLanes, rb = (kSwap ? m : n) * BN;
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const uint32_t s = it % C::kStages;
+                ok = wait_bar(empty_bar(s), ((it / C::kStages) & 1) ^ 1u, abort_flag, a.status,
+                              limit);
+                if (!ok) break;
+                if (leader) {
                     const uint32_t st = base + s * C::kStageBytes;
                     mbar_arrive_expect_tx(full_bar(s), C::kStageBytes);
                     tma_load_2d(st, kSwap ? &map_w : &map_x, kb * kKB, ra, full_bar(s));
                     tma_load_2d(st + kLanes * kKB, kSwap ? &map_x : &map_w, kb * kKB, rb,
                                 full_bar(s));
                 }
+                __syncwarp();
             }
-            // after giving up, the copies already issued end before the CTA does
-            if (!ok)
-                for (long long j = it > C::kStages ? it - C::kStages : 0; j < it; ++j)
-                    mbar_wait_drain(full_bar((int)(j % C::kStages)),
-                                    (uint32_t)((j / C::kStages) & 1), a.status);
         }
+        // after giving up, the copies already issued end before the CTA does
+        if (!ok && leader)
+            for (uint32_t j = it > C::kStages ? it - C::kStages : 0; j < it; ++j)
+                mbar_wait_drain(full_bar(j % C::kStages), (j / C::kStages) & 1, a.status);
         __syncwarp();
     } else if (warp == kMmaWarp) {
-        if (lane == 0) {
-            long long it = 0;
-            bool ok = true;
-            for (long long t = first; t < tiles && ok; t += step) {
-                for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                    const int s = (int)(it % C::kStages), b = (int)(it % C::kBufs);
-                    if (!mbar_wait(tempty_bar(b), (uint32_t)((it / C::kBufs) & 1) ^ 1u, abort_flag,
-                                   a.status) ||
-                        !mbar_wait(full_bar(s), (uint32_t)((it / C::kStages) & 1), abort_flag,
-                                   a.status)) {
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t st = base + s * C::kStageBytes;
+        const bool leader = elect_one();
+        uint32_t it = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += step) {
+            for (int kb = kb0; kb < kb1; ++kb, ++it) {
+                const uint32_t s = it % C::kStages, b = it % C::kBufs;
+                ok = wait_bar(tempty_bar(b), ((it / C::kBufs) & 1) ^ 1u, abort_flag, a.status,
+                              limit) &&
+                     wait_bar(full_bar(s), (it / C::kStages) & 1, abort_flag, a.status, limit);
+                if (!ok) break;
+                tc_fence_after();
+                if (leader) {
+                    const uint64_t da = desc_sw128(base + s * C::kStageBytes);
+                    const uint64_t db = desc_sw128(base + s * C::kStageBytes + kLanes * kKB);
 #pragma unroll
-                    for (int j = 0; j < kKB / 32; ++j)
-                        tc_mma_e4m3(tmem_base + (uint32_t)(b * BN), desc_sw128(st + j * 32),
-                                    desc_sw128(st + kLanes * kKB + j * 32), C::kIdesc, j != 0);
+                    for (int j = 0; j < kKB / 32; ++j)  // 32 bytes of channels further on
+                        tc_mma_e4m3(tmem_base + b * BN, da + 2 * j, db + 2 * j, C::kIdesc, j != 0);
                     tc_commit(empty_bar(s));
                     tc_commit(tfull_bar(b));
                 }
+                __syncwarp();
             }
-            // every MMA issued by this thread has completed once fin_bar fires
+        }
+        // every MMA issued by this thread has completed once fin_bar fires
+        if (leader) {
             tc_commit(fin_bar);
             mbar_wait_drain(fin_bar, 0, a.status);
         }
@@ -246,11 +351,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t tm_lane = (uint32_t)(quarter * 32) << 16;
-        constexpr int kChunk = C::kCols < 32 ? C::kCols : 32;
+        // TMEM columns read at a time: more would not fit beside the totals
+        constexpr int kChunk = C::kCols < 16 ? C::kCols : 16;
         T* const y = static_cast<T*>(a.y);
-        const bool wide = !kSwap && a.C_out % (16 / (int)sizeof(T)) == 0 &&
-                          (reinterpret_cast<uintptr_t>(y) & 15) == 0;
-        long long it = 0;
+        float* const bias_s =
+            reinterpret_cast<float*>(smem_raw + (bias_at - raw)) + warp * C::kCols;
+        const int nbo = (a.C_out + kKB - 1) / kKB;
+        uint32_t it = 0;
         bool ok = true;
         for (long long t = first; t < tiles && ok; t += step) {
             int m, n;
@@ -258,53 +365,78 @@ __global__ void __launch_bounds__(kThreads, 1)
             float acc[C::kCols];
 #pragma unroll
             for (int j = 0; j < C::kCols; ++j) acc[j] = 0.f;
+            if constexpr (!kSwap) {
+                __syncwarp();  // the last tile's bias has been read
+#pragma unroll
+                for (int j = 0; j < C::kCols; j += 32) {
+                    const int o = n * BN + half * C::kCols + j + lane;
+                    bias_s[j + lane] = a.bias && o < a.C_out ? __ldg(a.bias + o) : 0.f;
+                }
+                __syncwarp();
+            }
             // rows on lanes: this thread's token, and the block of its channels;
-            // channels on lanes: lane l holds the scale of the half's token l (+ 32)
-            const long long row =
-                kSwap ? (long long)m * BN + half * C::kCols + lane : (long long)m * kLanes + quarter * 32 + lane;
+            // channels on lanes: lane l holds the scale of the half's token l
+            const long long row = kSwap ? (long long)m * BN + half * C::kCols + lane
+                                        : (long long)m * kLanes + quarter * 32 + lane;
             const bool row_in = row < rows && (!kSwap || lane < C::kCols);
             const float* xs = a.xs + (row_in ? row : 0);
             const int ob = kSwap ? n : (n * BN + half * C::kCols) / kKB;
-            const int nbo = (a.C_out + kKB - 1) / kKB;
             const float* ws = a.ws + (long long)(ob < nbo ? ob : 0) * k.nkb;
-            auto scale = [&](int kb) {
-                return kb < kb1 && row_in ? xs[(long long)kb * a.capacity] * ws[kb] : 0.f;
+            // The two factors of a block's scale are loaded two blocks ahead and
+            // multiplied when they are used (formed at once, the product would
+            // wait for its loads); unrolled by two, so that no copy from one
+            // set to the other waits either.
+            float fx[2], fw[2];
+            auto load_scale = [&](int kb, int u) {
+                const bool in = kb < kb1 && row_in;
+                fx[u] = in ? __ldg(xs + (long long)kb * a.capacity) : 0.f;
+                fw[u] = in ? __ldg(ws + kb) : 0.f;
             };
-            float s0 = scale(kb0), s1 = scale(kb0 + 1);
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const int b = (int)(it % C::kBufs);
-                const float s = s0;
-                s0 = s1;
-                s1 = scale(kb + 2);
-                ok = mbar_wait(tfull_bar(b), (uint32_t)((it / C::kBufs) & 1), abort_flag, a.status);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tc_fence_after();
+            load_scale(kb0, 0);
+            load_scale(kb0 + 1, 1);
+            for (int k2 = kb0; k2 < kb1 && ok; k2 += 2) {
 #pragma unroll
-                for (int c = 0; c < C::kCols; c += kChunk) {
-                    uint32_t r[kChunk];
-                    tmem_ld(tmem_base + tm_lane + (uint32_t)(b * BN + half * C::kCols + c), r);
-                    tmem_ld_wait();
-                    if (c + kChunk == C::kCols) {
-                        tc_fence_before();
-                        if (lane == 0) mbar_arrive(tempty_bar(b));
-                    }
+                for (int u = 0; u < 2; ++u) {
+                    const int kb = k2 + u;
+                    if (kb >= kb1 || !ok) break;
+                    const uint32_t b = it % C::kBufs;
+                    const float s = fx[u] * fw[u];
+                    load_scale(kb + 2, u);
+                    ok = wait_bar(tfull_bar(b), (it / C::kBufs) & 1, abort_flag, a.status, limit);
+                    ++it;
+                    if (!ok) break;
+                    tc_fence_after();
 #pragma unroll
-                    for (int j = 0; j < kChunk; ++j) {
-                        const float sj = kSwap ? __shfl_sync(0xffffffffu, s, c + j) : s;
-                        acc[c + j] = fmaf(__uint_as_float(r[j]), sj, acc[c + j]);
+                    for (int c = 0; c < C::kCols; c += kChunk) {
+                        uint32_t r[kChunk];
+                        tmem_ld(tmem_base + tm_lane + b * BN + (uint32_t)(half * C::kCols + c), r);
+                        tmem_ld_wait();
+                        if (c + kChunk == C::kCols) {
+                            tc_fence_before();
+                            if (lane == 0) mbar_arrive(tempty_bar(b));
+                        }
+                        if constexpr (kSwap) {
+#pragma unroll
+                            for (int j = 0; j < kChunk; ++j)
+                                acc[c + j] = fmaf(__uint_as_float(r[j]),
+                                                  __shfl_sync(0xffffffffu, s, c + j), acc[c + j]);
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kChunk; j += 2)
+                                fma_pair(acc[c + j], acc[c + j + 1], r[j], r[j + 1], s);
+                        }
                     }
                 }
             }
-            if (!ok || k.split > 1) {
-                if (k.split > 1 && ok) {
-                    // totals of this CTA's blocks into the (now idle) stages
+            if (!ok) break;
+            if (k.split > 1) {
+                // totals of this CTA's blocks into the (now idle) stages; a split
+                // launch has one tile per cluster
 #pragma unroll
-                    for (int j = 0; j < C::kCols; ++j)
-                        sts_s32(base + (uint32_t)(((half * C::kCols + j) * kLanes + quarter * 32 + lane) * 4),
-                                __float_as_int(acc[j]));
-                }
-                break;  // a split launch has one tile per cluster
+                for (int j = 0; j < C::kCols; ++j)
+                    sts_s32(base + (uint32_t)(((half * C::kCols + j) * kLanes + quarter * 32 + lane) * 4),
+                            __float_as_int(acc[j]));
+                break;
             }
             if constexpr (kSwap) {
                 const int o = n * kLanes + quarter * 32 + lane;
@@ -317,28 +449,19 @@ __global__ void __launch_bounds__(kThreads, 1)
                             y[nn * a.C_out + o] = from_f32<T>(act_apply(acc[j] + bias, a.act));
                     }
                 }
-            } else if (row < rows) {
-                T* const yr = y + row * a.C_out;
-                const int o0 = n * BN + half * C::kCols;
-                constexpr int kV = 16 / (int)sizeof(T);
-#pragma unroll
-                for (int j = 0; j < C::kCols; j += kV) {
-                    alignas(16) T v[kV];
-#pragma unroll
-                    for (int i = 0; i < kV; ++i) {
-                        const int o = o0 + j + i;
-                        v[i] = from_f32<T>(act_apply(
-                            acc[j + i] + (a.bias && o < a.C_out ? __ldg(a.bias + o) : 0.f), a.act));
-                    }
-                    if (wide) {
-                        if (o0 + j < a.C_out)
-                            *reinterpret_cast<uint4*>(yr + o0 + j) = *reinterpret_cast<uint4*>(v);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kV; ++i)
-                            if (o0 + j + i < a.C_out) yr[o0 + j + i] = v[i];
-                    }
-                }
+            } else {
+                auto finish = [&](auto act) {
+                    store_tile<T, C::kCols, decltype(act)::value>(
+                        acc, bias_s, out_at + (uint32_t)warp * 2048u, y,
+                        (long long)m * kLanes + quarter * 32, rows, n * BN + half * C::kCols,
+                        a.C_out);
+                };
+                if (a.act == HC_ACT_ELU)
+                    finish(Act<HC_ACT_ELU>{});
+                else if (a.act == HC_ACT_RELU)
+                    finish(Act<HC_ACT_RELU>{});
+                else
+                    finish(Act<HC_ACT_NONE>{});
             }
         }
     }
