@@ -39,14 +39,19 @@ constexpr int kLanes = 128;                   // TMEM lanes = rows of the first 
 constexpr int kKB = 128;                      // channels per block = bytes per smem row
 constexpr int kPromoteWarps = 8;
 constexpr int kLoadWarp = kPromoteWarps;
-constexpr int kMmaWarp = kPromoteWarps + 1;
-constexpr int kThreads = (kPromoteWarps + 2) * 32;
+constexpr int kMmaWarp = kPromoteWarps + 1;  // and the next: even and odd blocks
+constexpr int kMmaWarps = 2;
+constexpr int kThreads = (kPromoteWarps + 4) * 32;  // three warpgroups; the last warp idles
+// Registers of the third warpgroup and of the promoting ones: launched with
+// 168 each (64512 in all), 128 * 88 + 256 * 208 = 64512 after the exchange.
+constexpr int kRoleRegs = 88, kPromoteRegs = 208;
 constexpr int kGroupM = 16;                   // token tiles walked per column of tiles
 
 template <int BN>
 struct Cfg {
     static constexpr int kStageBytes = (kLanes + BN) * kKB;
-    static constexpr int kStages = 196608 / kStageBytes < 10 ? 196608 / kStageBytes : 10;
+    // even: a stage's blocks then all belong to one MMA warp
+    static constexpr int kStages = (196608 / kStageBytes < 10 ? 196608 / kStageBytes : 10) & ~1;
     static constexpr int kBufs = 512 / BN < 4 ? 512 / BN : 4;
     static constexpr uint32_t kTmemCols = kBufs * BN;
     static constexpr int kCols = BN / 2;      // columns per promoting thread
@@ -132,6 +137,15 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile
     for (int i = 0; i < 16 && !ok; ++i) ok = mbar_try_wait(bar, parity);
     if (!ok) ok = mbar_wait_for(bar, parity, abort_flag, status, limit);
     return __all_sync(0xffffffffu, ok);
+}
+// Both phases, looked at together before either is waited for.
+__device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint32_t bar1,
+                                          uint32_t parity1, volatile int* abort_flag,
+                                          unsigned* status, unsigned long long limit) {
+    const bool a = mbar_try_wait(bar0, parity0), b = mbar_try_wait(bar1, parity1);
+    if (__all_sync(0xffffffffu, a && b)) return true;
+    return wait_bar(bar0, parity0, abort_flag, status, limit) &&
+           wait_bar(bar1, parity1, abort_flag, status, limit);
 }
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
@@ -260,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(tfull_bar(b), 1);
             mbar_init(tempty_bar(b), kPromoteWarps);
         }
-        mbar_init(fin_bar, 1);
+        mbar_init(fin_bar, kMmaWarps);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
         prefetch_tensormap(&map_x);
@@ -290,6 +304,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     // In all roles every lane of the warp walks the loop, so that its state is
     // uniform; the copies and MMAs are issued by one lane.
+    if (warp >= kPromoteWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRoleRegs));
     if (warp == kLoadWarp) {
         const bool leader = elect_one();
         uint32_t it = 0;
@@ -318,37 +334,38 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (uint32_t j = it > C::kStages ? it - C::kStages : 0; j < it; ++j)
                 mbar_wait_drain(full_bar(j % C::kStages), (j / C::kStages) & 1, a.status);
         __syncwarp();
-    } else if (warp == kMmaWarp) {
+    } else if (warp < kMmaWarp + kMmaWarps) {
         const bool leader = elect_one();
-        uint32_t it = 0;
+        const uint32_t mine = (uint32_t)(warp - kMmaWarp);
+        // this CTA's blocks, all tiles one after another
+        const uint32_t total = (uint32_t)((tiles > first ? (tiles - first + step - 1) / step : 0) * (kb1 - kb0));
         bool ok = true;
-        for (long long t = first; t < tiles && ok; t += step) {
-            for (int kb = kb0; kb < kb1; ++kb, ++it) {
-                const uint32_t s = it % C::kStages, b = it % C::kBufs;
-                ok = wait_bar(tempty_bar(b), ((it / C::kBufs) & 1) ^ 1u, abort_flag, a.status,
-                              limit) &&
-                     wait_bar(full_bar(s), (it / C::kStages) & 1, abort_flag, a.status, limit);
-                if (!ok) break;
-                tc_fence_after();
-                if (leader) {
-                    const uint64_t da = desc_sw128(base + s * C::kStageBytes);
-                    const uint64_t db = desc_sw128(base + s * C::kStageBytes + kLanes * kKB);
+        for (uint32_t it = mine; it < total; it += kMmaWarps) {
+            const uint32_t s = it % C::kStages, b = it % C::kBufs;
+            const uint64_t da = desc_sw128(base + s * C::kStageBytes);
+            const uint64_t db = desc_sw128(base + s * C::kStageBytes + kLanes * kKB);
+            ok = wait_bars(full_bar(s), (it / C::kStages) & 1, tempty_bar(b),
+                           ((it / C::kBufs) & 1) ^ 1u, abort_flag, a.status, limit);
+            if (!ok) break;
+            tc_fence_after();
+            if (leader) {
 #pragma unroll
-                    for (int j = 0; j < kKB / 32; ++j)  // 32 bytes of channels further on
-                        tc_mma_e4m3(tmem_base + b * BN, da + 2 * j, db + 2 * j, C::kIdesc, j != 0);
-                    tc_commit(empty_bar(s));
-                    tc_commit(tfull_bar(b));
-                }
-                __syncwarp();
+                for (int j = 0; j < kKB / 32; ++j)  // 32 bytes of channels further on
+                    tc_mma_e4m3(tmem_base + b * BN, da + 2 * j, db + 2 * j, C::kIdesc, j != 0);
+                tc_commit(tfull_bar(b));
+                tc_commit(empty_bar(s));
             }
+            __syncwarp();
         }
-        // every MMA issued by this thread has completed once fin_bar fires
+        // every MMA issued by these threads has completed once fin_bar fires
         if (leader) {
             tc_commit(fin_bar);
             mbar_wait_drain(fin_bar, 0, a.status);
         }
         __syncwarp();
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPromoteRegs));
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t tm_lane = (uint32_t)(quarter * 32) << 16;
         // TMEM columns read at a time: more would not fit beside the totals
