@@ -18,16 +18,33 @@ constexpr int kThreads = 256;
 // ---------------------------------------------------------------- rows in registers
 // A group of TPR threads holds a whole row: NV pieces of VEC elements each,
 // piece i of thread t at channel (i * TPR + t) * VEC. The row is read once;
-// the next row of the group is loaded before this one is worked on, so that
+// the next rows of the group are loaded before this one is worked on, so that
 // loads are in flight throughout. Groups stride over the rows.
 constexpr int kGroupThreads = 512;  // threads per block: kGroupThreads / TPR groups
+constexpr int kFwdAhead = 2;        // rows of a group in flight in the forward pass
+
+// p[c .. c + VEC), 16-byte aligned when VEC > 1, or `none` without a p.
+template <int VEC>
+__device__ __forceinline__ void load_floats(const float* __restrict__ p, int c, float none,
+                                            float (&v)[VEC]) {
+    if constexpr (VEC == 1) {
+        v[0] = p ? __ldg(p + c) : none;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4) {
+            const float4 f = p ? __ldg(reinterpret_cast<const float4*>(p + c + i))
+                               : make_float4(none, none, none, none);
+            v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+        }
+    }
+}
 
 template <typename T, int VEC, int TPR, int NV>
-__global__ void __launch_bounds__(kGroupThreads)
+__global__ void __launch_bounds__(kGroupThreads, 2)
     ln_fwd_rows_kernel(const T* x, const int32_t* count, long long capacity, int C, float eps,
                        const float* __restrict__ gamma, const float* __restrict__ beta, T* y,
                        float* mean_out, float* rstd_out, unsigned* status) {
-    __shared__ float sh[2 * kGroupThreads / 32];
+    __shared__ __align__(16) float sh[2 * kGroupThreads / 32];
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
@@ -38,59 +55,66 @@ __global__ void __launch_bounds__(kGroupThreads)
     // the same number of rounds
     const long long n0 = (long long)blockIdx.x * kGroups + threadIdx.x / TPR;
     const long long w0 = TPR < 32 ? n0 - (threadIdx.x & 31) / TPR : n0;
-    Piece<T, VEC> cur[NV], nxt[NV];
-    float ga[NV * VEC], be[NV * VEC];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + t) * VEC;
-        if (n0 < rows && c < C) nxt[i].load(x + n0 * C + c);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            ga[i * VEC + e] = gamma && c < C ? __ldg(gamma + c + e) : 1.f;
-            be[i * VEC + e] = beta && c < C ? __ldg(beta + c + e) : 0.f;
-        }
-    }
-    for (long long w = w0, n = n0; w < rows; w += step, n += step) {
-        const bool in = n < rows;
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            cur[i] = nxt[i];
-            const int c = (i * TPR + t) * VEC;
-            if (n + step < rows && c < C) nxt[i].load(x + (n + step) * C + c);
-            if (c < C)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) s += cur[i].get(e);
-        }
-        // a quotient, not a product with 1 / C: the mean of a constant row is
-        // then its value, and its differences are zero
-        const float mean = group_sum<TPR>(s, sh, 0) / (float)C;
-        float v = 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if ((i * TPR + t) * VEC < C)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float d = cur[i].get(e) - mean;
-                    v += d * d;
-                }
-        const float rstd = 1.f / sqrtf(group_sum<TPR>(v, sh, 1) / (float)C + eps);
-        if (!in) continue;
+    const float inv = 1.f / (float)C;
+    Piece<T, VEC> cur[NV], ring[kFwdAhead][NV];
+    auto load = [&](long long n, Piece<T, VEC>(&p)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * VEC;
-            if (c < C) {
+            if (n < rows && c < C) p[i].load(x + n * C + c);
+        }
+    };
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float xh = (cur[i].get(e) - mean) * rstd;
-                    cur[i].set(e, xh * ga[i * VEC + e] + be[i * VEC + e]);
+    for (int u = 0; u < kFwdAhead; ++u) load(n0 + u * step, ring[u]);
+    for (long long w = w0, n = n0; w < rows;) {
+#pragma unroll
+        for (int u = 0; u < kFwdAhead; ++u, w += step, n += step) {
+            if (w >= rows) break;
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) cur[i] = ring[u][i];
+            load(n + kFwdAhead * step, ring[u]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((i * TPR + t) * VEC < C)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) s += cur[i].get(e);
+            // the product with 1 / C, corrected by its residual: the mean of a
+            // constant row is then its value, and its differences are zero
+            s = group_sum<TPR>(s, sh, 0);
+            float mean = s * inv;
+            mean = fmaf(fmaf(-mean, (float)C, s), inv, mean);
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((i * TPR + t) * VEC < C)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float d = cur[i].get(e) - mean;
+                        v += d * d;
+                    }
+            const float rstd = rsqrtf(fmaf(group_sum<TPR>(v, sh, 1), inv, eps));
+            if (n >= rows) continue;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + t) * VEC;
+                if (c < C) {
+                    // gamma and beta come from L1 for every row: in registers
+                    // they would cost a row in flight
+                    float ga[VEC], be[VEC];
+                    load_floats<VEC>(gamma, c, 1.f, ga);
+                    load_floats<VEC>(beta, c, 0.f, be);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        be[e] = fmaf((cur[i].get(e) - mean) * rstd, ga[e], be[e]);
+                    cur[i].set_all(be);
+                    cur[i].store(y + n * C + c);
                 }
-                cur[i].store(y + n * C + c);
             }
-        }
-        if (t == 0) {
-            if (mean_out) mean_out[n] = mean;
-            if (rstd_out) rstd_out[n] = rstd;
+            if (t == 0) {
+                if (mean_out) mean_out[n] = mean;
+                if (rstd_out) rstd_out[n] = rstd;
+            }
         }
     }
 }
@@ -104,7 +128,7 @@ __global__ void __launch_bounds__(kGroupThreads)
                                int C, const float* __restrict__ gamma,
                                const float* __restrict__ mean, const float* __restrict__ rstd,
                                T* dx, float* __restrict__ part, unsigned* status) {
-    __shared__ float sh[2 * kGroupThreads / 32];
+    __shared__ __align__(16) float sh[2 * kGroupThreads / 32];
     extern __shared__ float psum[];  // [2][C] when the block has several groups
     pdl_wait();
     pdl_trigger();
@@ -173,11 +197,13 @@ __global__ void __launch_bounds__(kGroupThreads)
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * VEC;
             if (c < C) {
+                float f[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const float xh = (cx[i].get(e) - m) * r;
-                    cx[i].set(e, (cd[i].get(e) * ga[i * VEC + e] - c1 - xh * c2) * r);
+                    f[e] = (cd[i].get(e) * ga[i * VEC + e] - c1 - xh * c2) * r;
                 }
+                cx[i].set_all(f);
                 cx[i].store(dx + n * C + c);
             }
         }
@@ -424,7 +450,8 @@ hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStrea
     const int C = a.C;
     auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
     if (C > 8192) return back ? bwd_wide<T>(ctx, a, s) : fwd_wide<T>(ctx, a, s);
-    if (C % kVec == 0 && aligned(a.x) && aligned(a.y) && aligned(a.dy) && aligned(a.dx)) {
+    if (C % kVec == 0 && aligned(a.x) && aligned(a.y) && aligned(a.dy) && aligned(a.dx) &&
+        aligned(a.gamma) && aligned(a.beta)) {
         if (C <= 8 * kVec) return rows_in_regs<T, kVec, 8, 1>(ctx, a, back, s);
         if (C <= 32 * kVec) return rows_in_regs<T, kVec, 32, 1>(ctx, a, back, s);
         if (C <= 64 * kVec) return rows_in_regs<T, kVec, 32, 2>(ctx, a, back, s);

@@ -61,6 +61,7 @@ struct Piece<T, 1> {
     __device__ __forceinline__ void store(T* p) const { *p = v; }
     __device__ __forceinline__ float get(int) const { return to_f32(v); }
     __device__ __forceinline__ void set(int, float f) { v = from_f32<T>(f); }
+    __device__ __forceinline__ void set_all(const float (&f)[1]) { v = from_f32<T>(f[0]); }
 };
 template <>
 struct Piece<float, 4> {
@@ -72,6 +73,9 @@ struct Piece<float, 4> {
     }
     __device__ __forceinline__ void set(int i, float f) {
         (i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w) = f;
+    }
+    __device__ __forceinline__ void set_all(const float (&f)[4]) {
+        v = make_float4(f[0], f[1], f[2], f[3]);
     }
 };
 template <>
@@ -107,6 +111,14 @@ struct Piece<__nv_bfloat16, 8> {
         uint32_t& w = (i >> 1) == 0 ? v.x : (i >> 1) == 1 ? v.y : (i >> 1) == 2 ? v.z : v.w;
         w = i & 1 ? (w & 0xffffu) | b << 16 : (w & 0xffff0000u) | b;
     }
+    // two values to a word in one conversion
+    __device__ __forceinline__ void set_all(const float (&f)[8]) {
+        v = make_uint4(pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7]));
+    }
+    static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&b);
+    }
 };
 
 // Sum over a group of TPR threads (a power of two; group g of the block owns
@@ -120,13 +132,17 @@ __device__ __forceinline__ float group_sum(float v, float* sh, int turn) {
         v += __shfl_xor_sync(0xffffffffu, v, o);
     if constexpr (TPR > 32) {
         constexpr int kWarps = TPR / 32;
+        static_assert(kWarps % 4 == 0, "the warps' sums are read four at a time");
         const int g = threadIdx.x / TPR;
-        float* const at = sh + (turn ? blockDim.x / 32 : 0) + g * kWarps;
+        float* const at = sh + (turn ? blockDim.x / 32 : 0) + g * kWarps;  // 16-byte aligned
         if ((threadIdx.x & 31) == 0) at[(threadIdx.x % TPR) >> 5] = v;
         asm volatile("bar.sync %0, %1;\n" ::"r"(g + 1), "r"(TPR) : "memory");
         v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) v += at[w];
+        for (int w = 0; w < kWarps; w += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(at + w);
+            v += (f.x + f.y) + (f.z + f.w);
+        }
     }
     return v;
 }
