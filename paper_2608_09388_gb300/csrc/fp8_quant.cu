@@ -27,6 +27,16 @@ __device__ __forceinline__ float scale_of(float amax) {
 __device__ __forceinline__ uint8_t e4m3(float x, float scale) {
     return (uint8_t)__nv_cvt_float_to_fp8(x / scale, __NV_SATFINITE, __NV_E4M3);
 }
+// (a, b) * (s, s), one instruction for both.
+__device__ __forceinline__ float2 mul_pair(float a, float b, float s) {
+    unsigned long long v, ss;
+    float2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(ss) : "f"(s));
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(ss));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
     const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
     const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
@@ -45,9 +55,10 @@ __device__ __forceinline__ void to_e4m3(const float (&x)[N], float scale, float 
     uint32_t differ = 0;
 #pragma unroll
     for (int i = 0; i < N; i += 4) {
-        w[i / 4] = pack_e4m3(x[i] * below, x[i + 1] * below, x[i + 2] * below, x[i + 3] * below);
-        differ |= w[i / 4] ^
-                  pack_e4m3(x[i] * above, x[i + 1] * above, x[i + 2] * above, x[i + 3] * above);
+        const float2 a = mul_pair(x[i], x[i + 1], below), b = mul_pair(x[i + 2], x[i + 3], below);
+        const float2 c = mul_pair(x[i], x[i + 1], above), d = mul_pair(x[i + 2], x[i + 3], above);
+        w[i / 4] = pack_e4m3(a.x, a.y, b.x, b.y);
+        differ |= w[i / 4] ^ pack_e4m3(c.x, c.y, d.x, d.y);
     }
     if (differ) {
 #pragma unroll
@@ -75,10 +86,15 @@ __device__ __forceinline__ uint32_t amax_bits(const Piece<__nv_bfloat16, 8>& p) 
 // steps at a time, so that four loads are in flight and the four steps' scales
 // are found together: the reduction over a block's lanes halves the steps a
 // lane carries at its first two exchanges, after which lane l holds step l % 4
-// and divides for it alone. kWide: rows allow 16-byte loads.
+// and divides for it alone.
 constexpr int kSteps = 4;
+enum RowLoads {
+    kScalar,  // elements one by one
+    kWide,    // rows allow 16-byte loads
+    kFlat     // and hold whole blocks: block g lies at x + 128 g, whatever its row
+};
 
-template <typename T, bool kWide>
+template <typename T, RowLoads kLoads>
 __global__ void __launch_bounds__(kThreads)
     quant_rows_kernel(const T* __restrict__ x, const int32_t* count, long long capacity, int C,
                       int pitch, int nb, uint8_t* __restrict__ q, float* __restrict__ scales,
@@ -92,34 +108,40 @@ __global__ void __launch_bounds__(kThreads)
     const long long step = (long long)gridDim.x * (kThreads / 32) * kBlocks * kSteps;
     long long g0 = (long long)((blockIdx.x * kThreads + threadIdx.x) >> 5) * kBlocks * kSteps;
     for (; g0 < blocks; g0 += step) {
-        int b;
-        long long n = div32(g0 + sub, nb, b);
         Piece<T, V> p[kSteps];
-        long long at_n[kSteps];
-        int at_c[kSteps];
+        long long at[kSteps];   // of the lane's piece in q, -1: no such block
+        uint32_t used = 0;      // bit k: the piece holds channels, not the row's end
+        int b = 0;
+        long long n = 0;
+        if constexpr (kLoads != kFlat) n = div32(g0 + sub, nb, b);
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) {
-            at_n[k] = n;
-            at_c[k] = b * 128 + part * V;
-            const T* const xr = x + (n < rows ? n : 0) * C;  // absent blocks read row 0
-            if constexpr (kWide) {
-                p[k].load(xr + (at_c[k] < C ? at_c[k] : 0));
+            if constexpr (kLoads == kFlat) {
+                const long long g = g0 + sub + k * kBlocks;
+                at[k] = g < blocks ? g * 128 + part * V : -1;
+                used |= 1u << k;
+                p[k].load(x + (g < blocks ? at[k] : 0));  // absent blocks read the first
             } else {
+                const int c = b * 128 + part * V;
+                at[k] = n < rows && c < pitch ? n * pitch + c : -1;
+                used |= (c < C ? 1u : 0u) << k;
+                const T* const xr = x + (n < rows ? n : 0) * C;
+                if constexpr (kLoads == kWide) {
+                    p[k].load(xr + (c < C ? c : 0));
+                } else {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int c = at_c[k] + v;
-                    p[k].set(v, c < C ? to_f32(xr[c]) : 0.f);
+                    for (int v = 0; v < V; ++v) p[k].set(v, c + v < C ? to_f32(xr[c + v]) : 0.f);
                 }
-            }
-            b += kBlocks;
-            while (b >= nb) {
-                b -= nb;
-                ++n;
+                b += kBlocks;
+                while (b >= nb) {
+                    b -= nb;
+                    ++n;
+                }
             }
         }
         uint32_t m[kSteps];
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) m[k] = at_c[k] < C ? amax_bits(p[k]) : 0u;
+        for (int k = 0; k < kSteps; ++k) m[k] = used >> k & 1u ? amax_bits(p[k]) : 0u;
         const bool b0 = lane & 1, b1 = lane & 2;
         const uint32_t m01 =
             max(b0 ? m[1] : m[0], __shfl_xor_sync(0xffffffffu, b0 ? m[0] : m[1], 1));
@@ -139,21 +161,20 @@ __global__ void __launch_bounds__(kThreads)
         for (int k = 0; k < kSteps; ++k) {
             const float sc = __shfl_sync(0xffffffffu, my_scale, sub * kLanes + k);
             const float inv = __shfl_sync(0xffffffffu, my_inv, sub * kLanes + k);
-            if (at_n[k] >= rows || at_c[k] >= pitch) continue;
+            if (at[k] < 0) continue;
             float f[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) f[v] = p[k].get(v);
             uint32_t w[V / 4];
             to_e4m3<V>(f, sc, inv, w);
-            if (at_c[k] >= C) {
+            if (kLoads != kFlat && !(used >> k & 1u)) {
 #pragma unroll
                 for (int v = 0; v < V / 4; ++v) w[v] = 0u;  // beyond C
             }
-            uint8_t* const out = q + at_n[k] * pitch + at_c[k];
             if constexpr (V == 8)
-                *reinterpret_cast<uint2*>(out) = make_uint2(w[0], w[1]);
+                *reinterpret_cast<uint2*>(q + at[k]) = make_uint2(w[0], w[1]);
             else
-                *reinterpret_cast<uint32_t*>(out) = w[0];
+                *reinterpret_cast<uint32_t*>(q + at[k]) = w[0];
         }
     }
 }
@@ -203,7 +224,9 @@ hc_status quant_rows(const DeviceCtx* ctx, const void* x, const int32_t* count, 
     const long long need = ((long long)capacity * nb + kPerBlock - 1) / kPerBlock;
     const long long cap = (long long)ctx->num_sms * 16;
     const bool wide = C % V == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
-    return launch_pdl(wide ? quant_rows_kernel<T, true> : quant_rows_kernel<T, false>,
+    return launch_pdl(wide && C % 128 == 0 ? quant_rows_kernel<T, kFlat>
+                      : wide               ? quant_rows_kernel<T, kWide>
+                                           : quant_rows_kernel<T, kScalar>,
                       dim3((unsigned)(need < cap ? need : cap)), dim3(kThreads), 0, s,
                       "quant_rows_kernel", (const T*)x, count, (long long)capacity, C, pitch, nb,
                       q, scales, ctx->status);
