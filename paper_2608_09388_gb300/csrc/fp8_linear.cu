@@ -130,13 +130,18 @@ __device__ __forceinline__ void fma_pair(float& a0, float& a1, uint32_t v0, uint
 // A pipeline wait of this kernel, by a whole warp. A few tries first: the
 // shared bounded wait reads its limit from global memory once a try has
 // failed, longer than most waits here last.
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                         unsigned* status, unsigned long long limit) {
+__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                          unsigned* status, unsigned long long limit) {
     bool ok = false;
 #pragma unroll 1
     for (int i = 0; i < 16 && !ok; ++i) ok = mbar_try_wait(bar, parity);
     if (!ok) ok = mbar_wait_for(bar, parity, abort_flag, status, limit);
     return __all_sync(0xffffffffu, ok);
+}
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                         unsigned* status, unsigned long long limit) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return wait_slow(bar, parity, abort_flag, status, limit);
 }
 // Both phases, looked at together before either is waited for.
 __device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint32_t bar1,
@@ -144,8 +149,8 @@ __device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint3
                                           unsigned* status, unsigned long long limit) {
     const bool a = mbar_try_wait(bar0, parity0), b = mbar_try_wait(bar1, parity1);
     if (__all_sync(0xffffffffu, a && b)) return true;
-    return wait_bar(bar0, parity0, abort_flag, status, limit) &&
-           wait_bar(bar1, parity1, abort_flag, status, limit);
+    return wait_slow(bar0, parity0, abort_flag, status, limit) &&
+           wait_slow(bar1, parity1, abort_flag, status, limit);
 }
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
@@ -166,14 +171,14 @@ __device__ __forceinline__ float lds_cluster_f32(uint32_t addr, uint32_t rank) {
 
 // The tile t of the walk: token tiles in groups of kGroupM, the tiles of a
 // group column by column, so that a wave of CTAs shares both operands in L2.
-__device__ __forceinline__ void tile_at(long long t, int tm, int tn, int& m, int& n) {
-    const long long per = (long long)kGroupM * tn;
-    const int g = (int)(t / per);
-    const int first = g * kGroupM;
-    const int in = tm - first < kGroupM ? tm - first : kGroupM;
-    const int r = (int)(t - (long long)g * per);
-    n = r / in;
-    m = first + (r - n * in);
+__device__ __forceinline__ void tile_at(uint32_t t, int tm, int tn, int& m, int& n) {
+    const uint32_t per = (uint32_t)kGroupM * (uint32_t)tn;
+    const uint32_t g = t / per;
+    const int first = (int)g * kGroupM;
+    const uint32_t in = (uint32_t)(tm - first < kGroupM ? tm - first : kGroupM);
+    const uint32_t r = t - g * per;
+    n = (int)(r / in);
+    m = first + (int)(r - (uint32_t)n * in);
 }
 
 template <int kAct>
@@ -293,14 +298,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     const unsigned long long limit =
         reinterpret_cast<const volatile DeviceWord*>(a.status)->wait_limit_ns;
-    const long long rows = token_rows(a.count, a.capacity, a.status);
-    const int tm = (int)((rows + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes));
-    const int tn = (a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN);
-    const long long tiles = (long long)tm * tn;
+    const int rows = (int)token_rows(a.count, a.capacity, a.status);
+    constexpr int kTileRows = kSwap ? BN : kLanes, kTileOut = kSwap ? kLanes : BN;
+    const int tm = (int)(((long long)rows + kTileRows - 1) / kTileRows);
+    const int tn = (int)(((long long)a.C_out + kTileOut - 1) / kTileOut);
+    const uint32_t tiles = (uint32_t)tm * (uint32_t)tn;  // below 2^31 (checked by the host)
     const uint32_t rank = k.split > 1 ? cluster_rank() : 0u;
     const int kb0 = (int)((long long)k.nkb * rank / k.split);
     const int kb1 = (int)((long long)k.nkb * (rank + 1) / k.split);
-    const long long first = blockIdx.x / k.split, step = gridDim.x / k.split;
+    const uint32_t first = blockIdx.x / (uint32_t)k.split, step = gridDim.x / (uint32_t)k.split;
 
     // In all roles every lane of the warp walks the loop, so that its state is
     // uniform; the copies and MMAs are issued by one lane.
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool leader = elect_one();
         uint32_t it = 0;
         bool ok = true;
-        for (long long t = first; t < tiles && ok; t += step) {
+        for (uint32_t t = first; t < tiles && ok; t += step) {
             int m, n;
             tile_at(t, tm, tn, m, n);
             const int ra = (kSwap ? n : m) * kLanes, rb = (kSwap ? m : n) * BN;
@@ -338,7 +344,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool leader = elect_one();
         const uint32_t mine = (uint32_t)(warp - kMmaWarp);
         // this CTA's blocks, all tiles one after another
-        const uint32_t total = (uint32_t)((tiles > first ? (tiles - first + step - 1) / step : 0) * (kb1 - kb0));
+        const uint32_t total =
+            (tiles > first ? (tiles - first + step - 1) / step : 0u) * (uint32_t)(kb1 - kb0);
         bool ok = true;
         for (uint32_t it = mine; it < total; it += kMmaWarps) {
             const uint32_t s = it % C::kStages, b = it % C::kBufs;
@@ -376,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int nbo = (a.C_out + kKB - 1) / kKB;
         uint32_t it = 0;
         bool ok = true;
-        for (long long t = first; t < tiles && ok; t += step) {
+        for (uint32_t t = first; t < tiles && ok; t += step) {
             int m, n;
             tile_at(t, tm, tn, m, n);
             float acc[C::kCols];
@@ -393,40 +400,46 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             // rows on lanes: this thread's token, and the block of its channels;
             // channels on lanes: lane l holds the scale of the half's token l
-            const long long row = kSwap ? (long long)m * BN + half * C::kCols + lane
-                                        : (long long)m * kLanes + quarter * 32 + lane;
+            const int row = kSwap ? m * BN + half * C::kCols + lane
+                                  : m * kLanes + quarter * 32 + lane;
             const bool row_in = row < rows && (!kSwap || lane < C::kCols);
-            const float* xs = a.xs + (row_in ? row : 0);
             const int ob = kSwap ? n : (n * BN + half * C::kCols) / kKB;
-            const float* ws = a.ws + (long long)(ob < nbo ? ob : 0) * k.nkb;
+            const float* xs = a.xs + (long long)kb0 * a.capacity + (row_in ? row : 0);
+            const float* ws = a.ws + (long long)(ob < nbo ? ob : 0) * k.nkb + kb0;
             // The two factors of a block's scale are loaded two blocks ahead and
             // multiplied when they are used (formed at once, the product would
             // wait for its loads); unrolled by two, so that no copy from one
-            // set to the other waits either.
+            // set to the other waits either. A row that is not in use takes
+            // row 0's scales and is not stored. The last block's are loaded
+            // again rather than any past it.
             float fx[2], fw[2];
-            auto load_scale = [&](int kb, int u) {
-                const bool in = kb < kb1 && row_in;
-                fx[u] = in ? __ldg(xs + (long long)kb * a.capacity) : 0.f;
-                fw[u] = in ? __ldg(ws + kb) : 0.f;
+            const float* const xs_last = xs + (long long)(kb1 - kb0 - 1) * a.capacity;
+            auto load_scale = [&](int u) {
+                fx[u] = __ldg(xs);
+                fw[u] = __ldg(ws);
+                if (xs < xs_last) {
+                    xs += a.capacity;
+                    ++ws;
+                }
             };
-            load_scale(kb0, 0);
-            load_scale(kb0 + 1, 1);
-            for (int k2 = kb0; k2 < kb1 && ok; k2 += 2) {
+            load_scale(0);
+            load_scale(1);
+            for (int left = kb1 - kb0; left > 0 && ok; left -= 2) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int kb = k2 + u;
-                    if (kb >= kb1 || !ok) break;
-                    const uint32_t b = it % C::kBufs;
+                    if (u == 1 && (left < 2 || !ok)) break;
+                    const uint32_t b = it % C::kBufs, ph = (it / C::kBufs) & 1;
                     const float s = fx[u] * fw[u];
-                    load_scale(kb + 2, u);
-                    ok = wait_bar(tfull_bar(b), (it / C::kBufs) & 1, abort_flag, a.status, limit);
+                    load_scale(u);
+                    ok = wait_bar(tfull_bar(b), ph, abort_flag, a.status, limit);
                     ++it;
                     if (!ok) break;
                     tc_fence_after();
+                    const uint32_t at = tmem_base + tm_lane + b * BN + (uint32_t)(half * C::kCols);
 #pragma unroll
                     for (int c = 0; c < C::kCols; c += kChunk) {
                         uint32_t r[kChunk];
-                        tmem_ld(tmem_base + tm_lane + b * BN + (uint32_t)(half * C::kCols + c), r);
+                        tmem_ld(at + (uint32_t)c, r);
                         tmem_ld_wait();
                         if (c + kChunk == C::kCols) {
                             tc_fence_before();
@@ -566,6 +579,10 @@ hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
         ((a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN));
     // split while every CTA still gets an SM of its own and two blocks or more
     while (k.split < 8 && tiles * k.split * 2 <= ctx->num_sms && k.nkb >= 4 * k.split) k.split *= 2;
+    if (tiles > 0x7fffffffll) {
+        set_error("hc_fp8_linear_fwd: capacity=%d C_out=%d is too large", a.capacity, a.C_out);
+        return HC_ERR_UNSUPPORTED;
+    }
     const long long grid =
         k.split > 1 ? tiles * k.split : (tiles < ctx->num_sms ? tiles : ctx->num_sms);
     auto kern = fp8_linear_kernel<BN, kSwap, T>;
