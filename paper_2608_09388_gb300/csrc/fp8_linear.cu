@@ -89,9 +89,6 @@ __device__ __forceinline__ void tc_mma_e4m3(uint32_t d_tmem, uint64_t a_desc, ui
         "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[32]) {
-    tmem_ld_32x32b_x32(taddr, r);
-}
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -127,27 +124,47 @@ __device__ __forceinline__ void fma_pair(float& a0, float& a1, uint32_t v0, uint
     asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(v), "l"(ss));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(a));
 }
-// A pipeline wait of this kernel, by a whole warp. A few tries first: the
-// shared bounded wait reads its limit from global memory once a try has
-// failed, longer than most waits here last.
+// A pipeline wait of this kernel, by a whole warp: one try, then polling with
+// a look at the abort flag and the clock every eight polls. (mbar_wait reads
+// its limit from global memory whenever its first try has failed, longer than
+// most waits here last; and a suspended try would outlast a lowered limit.)
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n"
+        " mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                           unsigned* status, unsigned long long limit) {
+    const unsigned long long t0 = globaltimer_ns();
     bool ok = false;
+    for (;;) {
 #pragma unroll 1
-    for (int i = 0; i < 16 && !ok; ++i) ok = mbar_try_wait(bar, parity);
-    if (!ok) ok = mbar_wait_for(bar, parity, abort_flag, status, limit);
+        for (int i = 0; i < 8 && !ok; ++i) ok = mbar_test_wait(bar, parity);
+        if (ok || *abort_flag) break;
+        if (globaltimer_ns() - t0 > limit) {
+            *abort_flag = 1;
+            report(status, kErrTimeout);
+            break;
+        }
+    }
     return __all_sync(0xffffffffu, ok);
 }
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                          unsigned* status, unsigned long long limit) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
     return wait_slow(bar, parity, abort_flag, status, limit);
 }
 // Both phases, looked at together before either is waited for.
 __device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint32_t bar1,
                                           uint32_t parity1, volatile int* abort_flag,
                                           unsigned* status, unsigned long long limit) {
-    const bool a = mbar_try_wait(bar0, parity0), b = mbar_try_wait(bar1, parity1);
+    const bool a = mbar_test_wait(bar0, parity0), b = mbar_test_wait(bar1, parity1);
     if (__all_sync(0xffffffffu, a && b)) return true;
     return wait_slow(bar0, parity0, abort_flag, status, limit) &&
            wait_slow(bar1, parity1, abort_flag, status, limit);
@@ -335,8 +352,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 __syncwarp();
             }
         }
-        // after giving up, the copies already issued end before the CTA does
-        if (!ok && leader)
+        // the copies already issued end before the CTA does, also where another
+        // role gave up and nobody waits for them
+        if (leader)
             for (uint32_t j = it > C::kStages ? it - C::kStages : 0; j < it; ++j)
                 mbar_wait_drain(full_bar(j % C::kStages), (j / C::kStages) & 1, a.status);
         __syncwarp();
