@@ -124,11 +124,14 @@ __device__ __forceinline__ void fma_pair(float& a0, float& a1, uint32_t v0, uint
     asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(v), "l"(ss));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(a));
 }
-// A pipeline wait of this kernel, by a whole warp: one try, then polling with
-// a look at the abort flag and the clock every eight polls. (mbar_wait reads
-// its limit from global memory whenever its first try has failed, longer than
-// most waits here last; and a suspended try would outlast a lowered limit.)
-__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+// A pipeline wait of this kernel, by a whole warp: a look at the phase, then
+// tries that may suspend the warp, the abort flag and the clock after each.
+// (mbar_wait reads its limit from global memory whenever its first try has
+// failed, longer than most waits here last. Polling all the time instead drew
+// power: 1.5% on the largest products, which run at the power limit. A limit
+// lowered below a try's longest suspension is kept by polling.)
+constexpr unsigned long long kLongestTryNs = 100000;
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n .reg .pred p;\n"
@@ -142,10 +145,9 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                           unsigned* status, unsigned long long limit) {
     const unsigned long long t0 = globaltimer_ns();
-    bool ok = false;
+    bool ok;
     for (;;) {
-#pragma unroll 1
-        for (int i = 0; i < 8 && !ok; ++i) ok = mbar_test_wait(bar, parity);
+        ok = limit > kLongestTryNs ? mbar_try_wait(bar, parity) : mbar_test(bar, parity);
         if (ok || *abort_flag) break;
         if (globaltimer_ns() - t0 > limit) {
             *abort_flag = 1;
@@ -157,14 +159,14 @@ __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatil
 }
 __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                          unsigned* status, unsigned long long limit) {
-    if (__all_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
     return wait_slow(bar, parity, abort_flag, status, limit);
 }
 // Both phases, looked at together before either is waited for.
 __device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint32_t bar1,
                                           uint32_t parity1, volatile int* abort_flag,
                                           unsigned* status, unsigned long long limit) {
-    const bool a = mbar_test_wait(bar0, parity0), b = mbar_test_wait(bar1, parity1);
+    const bool a = mbar_test(bar0, parity0), b = mbar_test(bar1, parity1);
     if (__all_sync(0xffffffffu, a && b)) return true;
     return wait_slow(bar0, parity0, abort_flag, status, limit) &&
            wait_slow(bar1, parity1, abort_flag, status, limit);
