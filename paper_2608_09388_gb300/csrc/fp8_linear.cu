@@ -46,12 +46,17 @@ constexpr int kThreads = (kPromoteWarps + 4) * 32;  // three warpgroups; the las
 // 168 each (64512 in all), 128 * 88 + 256 * 208 = 64512 after the exchange.
 constexpr int kRoleRegs = 88, kPromoteRegs = 208;
 constexpr int kGroupM = 16;                   // token tiles walked per column of tiles
+constexpr int kPrefetch = 8;                  // weight blocks of a CTA asked into L2 ahead
 
 template <int BN>
 struct Cfg {
     static constexpr int kStageBytes = (kLanes + BN) * kKB;
     // even: a stage's blocks then all belong to one MMA warp
-    static constexpr int kStages = (196608 / kStageBytes < 10 ? 196608 / kStageBytes : 10) & ~1;
+    // Channels on the lanes: two CTAs an SM, so that the next call's are there,
+    // and its first weights on their way into L2, while this one's finish.
+    static constexpr bool kTwo = BN <= 64;
+    static constexpr int kRing = kTwo ? 100 * 1024 : 192 * 1024;
+    static constexpr int kStages = (kRing / kStageBytes < 10 ? kRing / kStageBytes : 10) & ~1;
     static constexpr int kBufs = 512 / BN < 4 ? 512 / BN : 4;
     static constexpr uint32_t kTmemCols = kBufs * BN;
     static constexpr int kCols = BN / 2;      // columns per promoting thread
@@ -61,12 +66,15 @@ struct Cfg {
         (1u << 4) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kLanes >> 4) << 24);
     // after the stages: bias of each promoting warp's columns, output staging
     // (32 rows x 64 bytes a warp), barriers
-    static constexpr int kBiasBytes = kPromoteWarps * kCols * 4;
-    static constexpr int kOutBytes = kPromoteWarps * 32 * 64;
+    static constexpr int kBiasBytes = kTwo ? 0 : kPromoteWarps * kCols * 4;
+    static constexpr int kOutBytes = kTwo ? 0 : kPromoteWarps * 32 * 64;
     static constexpr size_t kSmem =
         1024 + (size_t)kStages * kStageBytes + kBiasBytes + kOutBytes + 256;
-    // the split totals [BN][128] fp32 reuse the stages
-    static_assert((size_t)kStages * kStageBytes >= (size_t)BN * kLanes * 4, "split totals");
+    // The totals of a split tile reuse the stages: [BN][128] fp32 with channels
+    // on the lanes, [128][kTotalPitch] with tokens on the lanes (4 more than BN,
+    // so that eight rows' 16-byte pieces fall into different banks).
+    static constexpr int kTotalPitch = BN + 4;
+    static_assert((size_t)kStages * kStageBytes >= (size_t)kTotalPitch * kLanes * 4, "split totals");
 };
 
 struct KernelArgs {
@@ -106,6 +114,13 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[8]) {
           "=r"(r[7])
         : "r"(taddr)
         : "memory");
+}
+// A box of the tensor map into L2.
+__device__ __forceinline__ void tma_prefetch_2d(const void* tmap, int c0, int c1) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];\n" ::"l"(
+                     reinterpret_cast<uint64_t>(tmap)),
+                 "r"(c0), "r"(c1)
+                 : "memory");
 }
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
@@ -188,6 +203,17 @@ __device__ __forceinline__ float lds_cluster_f32(uint32_t addr, uint32_t rank) {
     return v;
 }
 
+__device__ __forceinline__ float4 lds_cluster_f4(uint32_t addr, uint32_t rank) {
+    uint32_t at;
+    float4 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(at)
+                 : "memory");
+    return v;
+}
+
 // The tile t of the walk: token tiles in groups of kGroupM, the tiles of a
 // group column by column, so that a wave of CTAs shares both operands in L2.
 __device__ __forceinline__ void tile_at(uint32_t t, int tm, int tn, int& m, int& n) {
@@ -267,7 +293,7 @@ __device__ __forceinline__ void store_tile(const float (&acc)[kCols], const floa
 }
 
 template <int BN, bool kSwap, typename T>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
     fp8_linear_kernel(const KernelArgs k, const __grid_constant__ CUtensorMap map_x,
                       const __grid_constant__ CUtensorMap map_w) {
     using C = Cfg<BN>;
@@ -312,6 +338,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_holder;
+    const uint32_t rank = k.split > 1 ? cluster_rank() : 0u;
+    const int kb0 = (int)((long long)k.nkb * rank / k.split);
+    const int kb1 = (int)((long long)k.nkb * (rank + 1) / k.split);
+    const uint32_t first = blockIdx.x / (uint32_t)k.split, step = gridDim.x / (uint32_t)k.split;
+    if constexpr (kSwap) {
+        // The weight is all the traffic of these calls, and which tile a CTA
+        // starts with does not depend on N': its first boxes are asked into L2
+        // while the kernel before (the quantisation of the tokens, as a rule)
+        // still runs. That kernel's writes land in L2 too: the loads below see
+        // them whatever was asked for before.
+        if (warp == kLoadWarp && first < (uint32_t)((a.C_out + kLanes - 1) / kLanes))
+            for (int kb = kb0 + lane; kb < kb1 && kb < kb0 + kPrefetch; kb += 32)
+                tma_prefetch_2d(&map_w, kb * kKB, (int)first * kLanes);
+    }
     pdl_wait();
     pdl_trigger();
 
@@ -322,15 +362,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int tm = (int)(((long long)rows + kTileRows - 1) / kTileRows);
     const int tn = (int)(((long long)a.C_out + kTileOut - 1) / kTileOut);
     const uint32_t tiles = (uint32_t)tm * (uint32_t)tn;  // below 2^31 (checked by the host)
-    const uint32_t rank = k.split > 1 ? cluster_rank() : 0u;
-    const int kb0 = (int)((long long)k.nkb * rank / k.split);
-    const int kb1 = (int)((long long)k.nkb * (rank + 1) / k.split);
-    const uint32_t first = blockIdx.x / (uint32_t)k.split, step = gridDim.x / (uint32_t)k.split;
 
     // In all roles every lane of the warp walks the loop, so that its state is
     // uniform; the copies and MMAs are issued by one lane.
     if (warp >= kPromoteWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRoleRegs));
+    if constexpr (!C::kTwo) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRoleRegs));
     if (warp == kLoadWarp) {
         const bool leader = elect_one();
         uint32_t it = 0;
@@ -392,7 +428,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
     }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPromoteRegs));
+        if constexpr (!C::kTwo)
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kPromoteRegs));
         const int quarter = warp & 3, half = warp >> 2;
         const uint32_t tm_lane = (uint32_t)(quarter * 32) << 16;
         // TMEM columns read at a time: more would not fit beside the totals
@@ -482,10 +519,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (k.split > 1) {
                 // totals of this CTA's blocks into the (now idle) stages; a split
                 // launch has one tile per cluster
+                if constexpr (kSwap) {
 #pragma unroll
-                for (int j = 0; j < C::kCols; ++j)
-                    sts_s32(base + (uint32_t)(((half * C::kCols + j) * kLanes + quarter * 32 + lane) * 4),
-                            __float_as_int(acc[j]));
+                    for (int j = 0; j < C::kCols; ++j)
+                        sts_s32(base + (uint32_t)(((half * C::kCols + j) * kLanes + quarter * 32 + lane) * 4),
+                                __float_as_int(acc[j]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < C::kCols; j += 4)
+                        sts_v4(base + (uint32_t)((quarter * 32 + lane) * C::kTotalPitch + half * C::kCols + j) * 4u,
+                               make_uint4(__float_as_uint(acc[j]), __float_as_uint(acc[j + 1]),
+                                          __float_as_uint(acc[j + 2]), __float_as_uint(acc[j + 3])));
+                }
                 break;
             }
             if constexpr (kSwap) {
@@ -521,20 +566,59 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (warp < kPromoteWarps && first < tiles && !*abort_flag) {
             int m, n;
             tile_at(first, tm, tn, m, n);
-            const int quarter = warp & 3, half = warp >> 2;
             T* const y = static_cast<T*>(a.y);
-            const int per = C::kCols / k.split;
-            for (int j = 0; j < per; ++j) {
-                const int col = half * C::kCols + (int)rank * per + j;
-                const int ln = quarter * 32 + lane;
-                float v = 0.f;
-                for (int r = 0; r < k.split; ++r)
-                    v += lds_cluster_f32(base + (uint32_t)((col * kLanes + ln) * 4), (uint32_t)r);
-                const long long nn = kSwap ? (long long)m * BN + col : (long long)m * kLanes + ln;
-                const int o = kSwap ? n * kLanes + ln : n * BN + col;
-                if (nn < rows && o < a.C_out)
-                    y[nn * a.C_out + o] =
-                        from_f32<T>(act_apply(v + (a.bias ? a.bias[o] : 0.f), a.act));
+            if constexpr (kSwap) {
+                // a share of the tokens each, a channel per lane
+                const int quarter = warp & 3, half = warp >> 2;
+                const int per = C::kCols / k.split, ln = quarter * 32 + lane;
+                const int o = n * kLanes + ln;
+                const float bias = a.bias && o < a.C_out ? __ldg(a.bias + o) : 0.f;
+                for (int j = 0; j < per; ++j) {
+                    const int col = half * C::kCols + (int)rank * per + j;
+                    float v = 0.f;
+                    for (int r = 0; r < k.split; ++r)
+                        v += lds_cluster_f32(base + (uint32_t)((col * kLanes + ln) * 4), (uint32_t)r);
+                    const long long nn = (long long)m * BN + col;
+                    if (nn < rows && o < a.C_out)
+                        y[nn * a.C_out + o] = from_f32<T>(act_apply(v + bias, a.act));
+                }
+            } else {
+                // a share of the tokens each, a warp per token, 4 channels per lane
+                const int per = kLanes / k.split;
+                const bool wide = a.C_out % 4 == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0;
+                for (int c = lane * 4; c < BN; c += 128) {
+                    const int o = n * BN + c;
+                    float bias[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        bias[i] = a.bias && o + i < a.C_out ? __ldg(a.bias + o + i) : 0.f;
+#pragma unroll 4
+                    for (int q = warp; q < per; q += kPromoteWarps) {
+                        const int ln = (int)rank * per + q;
+                        const long long nn = (long long)m * kLanes + ln;
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                        for (int r = 0; r < k.split; ++r) {
+                            const float4 f = lds_cluster_f4(
+                                base + (uint32_t)(ln * C::kTotalPitch + c) * 4u, (uint32_t)r);
+                            v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+                        }
+                        if (nn >= rows) continue;
+                        const float w[4] = {act_apply(v.x + bias[0], a.act), act_apply(v.y + bias[1], a.act),
+                                            act_apply(v.z + bias[2], a.act), act_apply(v.w + bias[3], a.act)};
+                        T* const yr = y + nn * a.C_out + o;
+                        if (wide && o < a.C_out) {
+                            if constexpr (sizeof(T) == 4)
+                                *reinterpret_cast<float4*>(yr) = make_float4(w[0], w[1], w[2], w[3]);
+                            else
+                                *reinterpret_cast<uint2*>(yr) =
+                                    make_uint2(Piece<T, 8>::pair(w[0], w[1]), Piece<T, 8>::pair(w[2], w[3]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (o + i < a.C_out) yr[i] = from_f32<T>(w[i]);
+                        }
+                    }
+                }
             }
         }
         cluster_barrier();
@@ -598,13 +682,14 @@ hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
         (long long)((a.capacity + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes)) *
         ((a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN));
     // split while every CTA still gets an SM of its own and two blocks or more
-    while (k.split < 8 && tiles * k.split * 2 <= ctx->num_sms && k.nkb >= 4 * k.split) k.split *= 2;
+    const int slots = ctx->num_sms * (C::kTwo ? 2 : 1);
+    while (k.split < 8 && tiles * k.split * 2 <= slots && k.nkb >= 4 * k.split) k.split *= 2;
     if (tiles > 0x7fffffffll) {
         set_error("hc_fp8_linear_fwd: capacity=%d C_out=%d is too large", a.capacity, a.C_out);
         return HC_ERR_UNSUPPORTED;
     }
     const long long grid =
-        k.split > 1 ? tiles * k.split : (tiles < ctx->num_sms ? tiles : ctx->num_sms);
+        k.split > 1 ? tiles * k.split : (tiles < slots ? tiles : slots);
     auto kern = fp8_linear_kernel<BN, kSwap, T>;
     static bool done[64];
     if (!done[ctx->device]) {
