@@ -223,6 +223,110 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     }
 }
 
+// All passes of a sort of at most kMinTile entries by one block, the keys and
+// positions handed from pass to pass through shared memory.
+constexpr size_t small_smem(int bits) {
+    return (sizeof(int) << bits) * (kSortWarps + 1) + 2 * sizeof(int) * kMinTile;
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs a, int passes) {
+    extern __shared__ int sm[];
+    __shared__ int sh[kSortWarps];
+    const int digits = 1 << a.bits;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int* const base = sm;                         // [digits]
+    int* const cnt = sm + digits * (1 + warp);    // [digits] of this warp
+    int* const skey = sm + digits * (1 + kSortWarps);
+    int* const spos = skey + kMinTile;
+    pdl_wait();
+    pdl_trigger();
+    const int rows = (int)token_rows(a.count, a.capacity, a.status);
+    const int i0 = warp * 32 * kRounds + lane;
+    int key[kRounds], pos[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        pos[r] = i0 + r * 32;
+        key[r] = pos[r] < rows ? sort_key(a, pos[r]) : -1;
+    }
+    for (int p = 0; p < passes; ++p) {
+        const int shift = p * a.bits;
+        for (int d = threadIdx.x; d < digits * kSortWarps; d += kSortThreads) sm[digits + d] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
+            if (key[r] >= 0) atomicAdd(&cnt[(key[r] >> shift) & (digits - 1)], 1);
+        __syncthreads();
+        // starts of the warps within a digit, then of the digits
+        for (int d = threadIdx.x; d < digits; d += kSortThreads) {
+            int at = 0;
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) {
+                const int c = sm[digits * (1 + w) + d];
+                sm[digits * (1 + w) + d] = at;
+                at += c;
+            }
+            base[d] = at;
+        }
+        __syncthreads();
+        constexpr int kPer = kMaxDigits / kSortThreads;
+        int tot[kPer], sum = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int d = threadIdx.x * kPer + j;
+            tot[j] = d < digits ? base[d] : 0;
+            sum += tot[j];
+        }
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) sh[warp] = incl;
+        __syncthreads();
+        int run = incl - sum;
+        for (int w = 0; w < warp; ++w) run += sh[w];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const int d = threadIdx.x * kPer + j;
+            if (d < digits) base[d] = run;
+            run += tot[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const bool in = key[r] >= 0;
+            const int digit = in ? (key[r] >> shift) & (digits - 1) : digits;  // no entry
+            const unsigned same = __match_any_sync(0xffffffffu, digit);
+            const int rank = __popc(same & ((1u << lane) - 1u));
+            int at = 0;
+            if (in) at = base[digit] + cnt[digit] + rank;
+            __syncwarp();
+            if (in && rank == 0) cnt[digit] += __popc(same);
+            __syncwarp();
+            if (in) {
+                skey[at] = key[r];
+                spos[at] = pos[r];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const int i = i0 + r * 32;
+            key[r] = i < rows ? skey[i] : -1;
+            pos[r] = i < rows ? spos[i] : 0;
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int i = i0 + r * 32;
+        if (i < rows) {
+            a.keys_out[i] = key[r];
+            a.pos_out[i] = pos[r];
+        }
+    }
+}
+
 // row_ptr[v] = entries whose key is below v: a binary search that starts
 // among 1024 samples of the keys in shared memory, so that at most 2^-10 of
 // the keys are left for the dependent global loads. Positions from N' on
@@ -665,6 +769,11 @@ hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, in
                                                  (int)scatter_smem(kMaxDigitBits)),
                             "sort_scatter_kernel");
             if (st != HC_OK) return st;
+            st = check_cuda(cudaFuncSetAttribute(sort_small_kernel,
+                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 (int)small_smem(kMaxDigitBits)),
+                            "sort_small_kernel");
+            if (st != HC_OK) return st;
             done[ctx->device] = true;
         }
         const long long need = (n + kMinTile - 1) / kMinTile;
@@ -680,28 +789,40 @@ hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, in
         if (!ws) return HC_ERR_CUDA;
         int32_t* keys[2] = {ws + hist, ws + hist + n};
         int32_t* pos[2] = {keys[1] + n, keys[1] + 2 * n};
-        for (int p = 0; p < passes; ++p) {
-            SortArgs k{};
-            k.ids = p == 0 ? a.ids : nullptr;
-            k.keys_in = keys[(p + 1) & 1];
-            k.pos_in = pos[(p + 1) & 1];
-            k.keys_out = keys[p & 1];
-            k.pos_out = p == passes - 1 ? order : pos[p & 1];
-            k.hist = ws;
-            k.count = a.count;
-            k.ids_stride = a.ids_stride;
-            k.capacity = n;
-            k.V = a.V;
-            k.shift = p * bits;
-            k.bits = bits;
-            k.status = ctx->status;
-            st = launch_pdl(sort_hist_kernel, dim3(tiles), dim3(kSortThreads), 0, s,
-                            "sort_hist_kernel", k);
+        SortArgs k{};
+        k.ids = a.ids;
+        k.hist = ws;
+        k.count = a.count;
+        k.ids_stride = a.ids_stride;
+        k.capacity = n;
+        k.V = a.V;
+        k.bits = bits;
+        k.status = ctx->status;
+        if (n <= kMinTile) {
+            // one launch instead of two a pass: 3132 ids in two passes took
+            // 19.9 us that way, most of it launches and their round trips
+            k.keys_out = keys[0];
+            k.pos_out = order;
+            st = launch_pdl(sort_small_kernel, dim3(1), dim3(kSortThreads), small_smem(bits), s,
+                            "sort_small_kernel", k, passes);
             if (st != HC_OK) return st;
-            st = launch_pdl(sort_scatter_kernel, dim3(tiles), dim3(kSortThreads),
-                            scatter_smem(bits), s, "sort_scatter_kernel", k);
-            if (st != HC_OK) return st;
-            sorted = k.keys_out;
+            sorted = keys[0];
+        } else {
+            for (int p = 0; p < passes; ++p) {
+                k.ids = p == 0 ? a.ids : nullptr;
+                k.keys_in = keys[(p + 1) & 1];
+                k.pos_in = pos[(p + 1) & 1];
+                k.keys_out = keys[p & 1];
+                k.pos_out = p == passes - 1 ? order : pos[p & 1];
+                k.shift = p * bits;
+                st = launch_pdl(sort_hist_kernel, dim3(tiles), dim3(kSortThreads), 0, s,
+                                "sort_hist_kernel", k);
+                if (st != HC_OK) return st;
+                st = launch_pdl(sort_scatter_kernel, dim3(tiles), dim3(kSortThreads),
+                                scatter_smem(bits), s, "sort_scatter_kernel", k);
+                if (st != HC_OK) return st;
+                sorted = k.keys_out;
+            }
         }
     }
     const long long need = ((a.V + 1ll > n ? a.V + 1ll : n) + kThreads - 1) / kThreads;

@@ -248,21 +248,20 @@ __device__ __forceinline__ void store_tile(const float (&acc)[kCols], const floa
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            uint32_t w[4];
+            float f[kV];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = p + q * kV + i * (kV / 4);
-                if constexpr (sizeof(T) == 4) {
-                    w[i] = __float_as_uint(act_fixed<kAct>(acc[j] + bias[j]));
-                } else {
-                    const __nv_bfloat162 v =
-                        __floats2bfloat162_rn(act_fixed<kAct>(acc[j] + bias[j]),
-                                              act_fixed<kAct>(acc[j + 1] + bias[j + 1]));
-                    w[i] = *reinterpret_cast<const uint32_t*>(&v);
-                }
+            for (int i = 0; i < kV; i += 4) {
+                const int j = p + q * kV + i;
+                const float4 b = *reinterpret_cast<const float4*>(bias + j);
+                f[i] = act_fixed<kAct>(acc[j] + b.x);
+                f[i + 1] = act_fixed<kAct>(acc[j + 1] + b.y);
+                f[i + 2] = act_fixed<kAct>(acc[j + 2] + b.z);
+                f[i + 3] = act_fixed<kAct>(acc[j + 3] + b.w);
             }
+            Piece<T, kV> w;
+            w.set_all(f);
             sts_v4(stage + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4),
-                   make_uint4(w[0], w[1], w[2], w[3]));
+                   *reinterpret_cast<const uint4*>(&w.v));
         }
         __syncwarp();
         if (wide) {
@@ -275,18 +274,25 @@ __device__ __forceinline__ void store_tile(const float (&acc)[kCols], const floa
                     *reinterpret_cast<uint4*>(y + (r0 + r) * C_out + o) = v;
             }
         } else {
-            for (int i = lane; i < 32 * kPass; i += 32) {
-                const int r = i / kPass, j = i % kPass, q = j / kV;
-                const uint32_t at = stage + r * 64 + ((q ^ ((r >> 1) & 3)) << 4) + j % kV * (int)sizeof(T);
+            // element by element, kPass lanes side by side in a row
+            constexpr int kRows = 32 / kPass;  // rows at a time
+            const int j = lane % kPass, q = j / kV, rl = lane / kPass;
+            const bool in = o0 + p + j < C_out;
+            T* at = y + (r0 + rl) * C_out + o0 + p + j;
+            const uint32_t from = stage + rl * 64 + j % kV * (int)sizeof(T);
+#pragma unroll
+            for (int r = 0; r < 32; r += kRows) {
+                const uint32_t a = from + r * 64 + ((q ^ (((r + rl) >> 1) & 3)) << 4);
                 T v;
                 if constexpr (sizeof(T) == 4) {
-                    v = __int_as_float(lds_s32(at));
+                    v = __int_as_float(lds_s32(a));
                 } else {
                     uint16_t b;
-                    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(b) : "r"(at) : "memory");
+                    asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(b) : "r"(a) : "memory");
                     v = __ushort_as_bfloat16(b);
                 }
-                if (r0 + r < rows && o0 + p + j < C_out) y[(r0 + r) * C_out + o0 + p + j] = v;
+                if (in && r0 + r + rl < rows) *at = v;
+                at += (long long)kRows * C_out;
             }
         }
     }

@@ -90,6 +90,7 @@ __device__ __forceinline__ uint32_t amax_bits(const Piece<__nv_bfloat16, 8>& p) 
 constexpr int kSteps = 4;
 enum RowLoads {
     kScalar,  // elements one by one
+    kWords,   // bf16 rows allow 4-byte loads
     kWide,    // rows allow 16-byte loads
     kFlat     // and hold whole blocks: block g lies at x + 128 g, whatever its row
 };
@@ -125,12 +126,26 @@ __global__ void __launch_bounds__(kThreads)
                 const int c = b * 128 + part * V;
                 at[k] = n < rows && c < pitch ? n * pitch + c : -1;
                 used |= (c < C ? 1u : 0u) << k;
-                const T* const xr = x + (n < rows ? n : 0) * C;
+                const long long xr = (n < rows ? n : 0) * C;
                 if constexpr (kLoads == kWide) {
-                    p[k].load(xr + (c < C ? c : 0));
-                } else {
+                    p[k].load(x + xr + (c < C ? c : 0));
+                } else if constexpr (kLoads == kWords) {
+                    uint32_t w[4];
 #pragma unroll
-                    for (int v = 0; v < V; ++v) p[k].set(v, c + v < C ? to_f32(xr[c + v]) : 0.f);
+                    for (int v = 0; v < 4; ++v) {
+                        const int at_c = c + 2 * v;  // both elements of a word exist, or neither
+                        w[v] = *reinterpret_cast<const uint32_t*>(x + xr + (at_c < C ? at_c : 0));
+                        w[v] = at_c < C ? w[v] : 0u;
+                    }
+                    p[k].v = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+                    float f[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        f[v] = to_f32(x[xr + (c + v < C ? c + v : 0)]);
+                        f[v] = c + v < C ? f[v] : 0.f;
+                    }
+                    p[k].set_all(f);
                 }
                 b += kBlocks;
                 while (b >= nb) {
@@ -223,10 +238,14 @@ hc_status quant_rows(const DeviceCtx* ctx, const void* x, const int32_t* count, 
     constexpr int V = 16 / (int)sizeof(T), kPerBlock = kThreads / 32 * kSteps * 32 * V / 128;
     const long long need = ((long long)capacity * nb + kPerBlock - 1) / kPerBlock;
     const long long cap = (long long)ctx->num_sms * 16;
-    const bool wide = C % V == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
-    return launch_pdl(wide && C % 128 == 0 ? quant_rows_kernel<T, kFlat>
-                      : wide               ? quant_rows_kernel<T, kWide>
-                                           : quant_rows_kernel<T, kScalar>,
+    const uintptr_t at = reinterpret_cast<uintptr_t>(x);
+    const bool wide = C % V == 0 && at % 16 == 0;
+    auto kern = wide && C % 128 == 0 ? quant_rows_kernel<T, kFlat>
+                : wide               ? quant_rows_kernel<T, kWide>
+                                     : quant_rows_kernel<T, kScalar>;
+    if constexpr (sizeof(T) == 2)
+        if (!wide && C % 2 == 0 && at % 4 == 0) kern = quant_rows_kernel<T, kWords>;
+    return launch_pdl(kern,
                       dim3((unsigned)(need < cap ? need : cap)), dim3(kThreads), 0, s,
                       "quant_rows_kernel", (const T*)x, count, (long long)capacity, C, pitch, nb,
                       q, scales, ctx->status);

@@ -21,7 +21,9 @@ constexpr int kThreads = 256;
 // the next rows of the group are loaded before this one is worked on, so that
 // loads are in flight throughout. Groups stride over the rows.
 constexpr int kGroupThreads = 512;  // threads per block: kGroupThreads / TPR groups
-constexpr int kFwdAhead = 2;        // rows of a group in flight in the forward pass
+// Rows of a group in flight in the forward pass, within its 64 registers.
+template <typename T, int VEC, int NV>
+constexpr int kFwdAhead = NV * (VEC == 1 ? 1 : 4) <= 8 ? 2 : 1;
 
 // p[c .. c + VEC), 16-byte aligned when VEC > 1, or `none` without a p.
 template <int VEC>
@@ -56,7 +58,8 @@ __global__ void __launch_bounds__(kGroupThreads, 2)
     const long long n0 = (long long)blockIdx.x * kGroups + threadIdx.x / TPR;
     const long long w0 = TPR < 32 ? n0 - (threadIdx.x & 31) / TPR : n0;
     const float inv = 1.f / (float)C;
-    Piece<T, VEC> cur[NV], ring[kFwdAhead][NV];
+    constexpr int kAhead = kFwdAhead<T, VEC, NV>;
+    Piece<T, VEC> cur[NV], ring[kAhead][NV];
     auto load = [&](long long n, Piece<T, VEC>(&p)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -65,15 +68,15 @@ __global__ void __launch_bounds__(kGroupThreads, 2)
         }
     };
 #pragma unroll
-    for (int u = 0; u < kFwdAhead; ++u) load(n0 + u * step, ring[u]);
+    for (int u = 0; u < kAhead; ++u) load(n0 + u * step, ring[u]);
     for (long long w = w0, n = n0; w < rows;) {
 #pragma unroll
-        for (int u = 0; u < kFwdAhead; ++u, w += step, n += step) {
+        for (int u = 0; u < kAhead; ++u, w += step, n += step) {
             if (w >= rows) break;
             float s = 0.f;
 #pragma unroll
             for (int i = 0; i < NV; ++i) cur[i] = ring[u][i];
-            load(n + kFwdAhead * step, ring[u]);
+            load(n + kAhead * step, ring[u]);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if ((i * TPR + t) * VEC < C)
@@ -121,7 +124,7 @@ __global__ void __launch_bounds__(kGroupThreads, 2)
 
 // The gradient in the same layout. A thread owns its channels for all its
 // rows, so dgamma and dbeta are summed in registers; the groups of a block
-// are added in shared memory in order, the blocks by ln_param_grad_kernel.
+// are added in order through shared memory, the blocks by ln_param_grad_kernel.
 template <typename T, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(kGroupThreads)
     ln_bwd_rows_in_regs_kernel(const T* x, const T* dy, const int32_t* count, long long capacity,
@@ -129,7 +132,7 @@ __global__ void __launch_bounds__(kGroupThreads)
                                const float* __restrict__ mean, const float* __restrict__ rstd,
                                T* dx, float* __restrict__ part, unsigned* status) {
     __shared__ __align__(16) float sh[2 * kGroupThreads / 32];
-    extern __shared__ float psum[];  // [2][C] when the block has several groups
+    extern __shared__ float psum[];  // [groups][2][C] when the block has several groups
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
@@ -211,21 +214,24 @@ __global__ void __launch_bounds__(kGroupThreads)
     if (part == nullptr) return;
     float* const out = part + 2ll * blockIdx.x * C;
     if constexpr (kGroups > 1) {
-        for (int g = 0; g < kGroups; ++g) {
-            if ((int)threadIdx.x / TPR == g)
+        float* const mine = psum + (threadIdx.x / TPR) * 2 * C;
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const int c = (i * TPR + t) * VEC + e;
-                        if (c < C) {
-                            psum[c] = (g ? psum[c] : 0.f) + dg[i * VEC + e];
-                            psum[C + c] = (g ? psum[C + c] : 0.f) + db[i * VEC + e];
-                        }
-                    }
-            __syncthreads();
+            for (int e = 0; e < VEC; ++e) {
+                const int c = (i * TPR + t) * VEC + e;
+                if (c < C) {
+                    mine[c] = dg[i * VEC + e];
+                    mine[C + c] = db[i * VEC + e];
+                }
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < 2 * C; c += kGroupThreads) {
+            float v = 0.f;
+#pragma unroll 8
+            for (int g = 0; g < kGroups; ++g) v += psum[g * 2 * C + c];
+            out[c] = v;
         }
-        for (int c = threadIdx.x; c < 2 * C; c += kGroupThreads) out[c] = psum[c];
     } else {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -389,10 +395,21 @@ hc_status bwd_rows(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s)
         part = (float*)stream_workspace(s, (size_t)grid * a.C * 8);
         if (!part) return HC_ERR_CUDA;
     }
-    const size_t smem = kGroups > 1 && params ? (size_t)a.C * 8 : 0;
-    hc_status st = launch_pdl(ln_bwd_rows_in_regs_kernel<T, VEC, TPR, NV>, dim3((unsigned)grid),
-                              dim3(kGroupThreads), smem, s, "ln_bwd_rows_in_regs_kernel",
-                              (const T*)a.x, (const T*)a.dy, a.count, (long long)a.capacity, a.C,
+    // the groups' sums: at most 64 KiB, two 4-byte sums for each of the
+    // kGroups * C <= 512 * 16 channels held
+    const size_t smem = kGroups > 1 && params ? (size_t)kGroups * a.C * 8 : 0;
+    auto kern = ln_bwd_rows_in_regs_kernel<T, VEC, TPR, NV>;
+    static bool done[64];
+    if (smem > 48 * 1024 && !done[ctx->device]) {
+        const hc_status st = check_cuda(
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 kGroupThreads * NV * VEC * 8),
+            "ln_bwd_rows_in_regs_kernel");
+        if (st != HC_OK) return st;
+        done[ctx->device] = true;
+    }
+    hc_status st = launch_pdl(kern, dim3((unsigned)grid), dim3(kGroupThreads), smem, s,
+                              "ln_bwd_rows_in_regs_kernel", (const T*)a.x, (const T*)a.dy, a.count, (long long)a.capacity, a.C,
                               a.gamma, a.mean, a.rstd, (T*)a.dx, part, ctx->status);
     if (st != HC_OK || !params) return st;
     return param_grad(a, part, grid, s);
@@ -462,7 +479,9 @@ hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStrea
         if constexpr (kVec == 4) return rows_in_regs<T, kVec, 512, 4>(ctx, a, back, s);
     }
     if (C <= 32) return rows_in_regs<T, 1, 8, 4>(ctx, a, back, s);
+    if (C <= 64) return rows_in_regs<T, 1, 8, 8>(ctx, a, back, s);
     if (C <= 256) return rows_in_regs<T, 1, 32, 8>(ctx, a, back, s);
+    if (C <= 512) return rows_in_regs<T, 1, 32, 16>(ctx, a, back, s);
     if (C <= 1024) return rows_in_regs<T, 1, 128, 8>(ctx, a, back, s);
     if (C <= 4096) return rows_in_regs<T, 1, 512, 8>(ctx, a, back, s);
     return rows_in_regs<T, 1, 512, 16>(ctx, a, back, s);
