@@ -21,28 +21,34 @@ constexpr int kThreads = 256;
 // the next rows of the group are loaded before this one is worked on, so that
 // loads are in flight throughout. Groups stride over the rows.
 constexpr int kGroupThreads = 512;  // threads per block: kGroupThreads / TPR groups
-// Rows of a group in flight in the forward pass, within its 64 registers.
+// Rows of a group in flight in the forward pass: 32 registers' worth, four at
+// most. One block an SM then has 64 KB on the way, and gamma and beta stay in
+// registers (read from L1 for every row they took 85% of its data path:
+// 65536 x 2048 bf16 103 us).
 template <typename T, int VEC, int NV>
-constexpr int kFwdAhead = NV * (VEC == 1 ? 1 : 4) <= 8 ? 2 : 1;
+constexpr int kRowRegs = NV * (VEC == 1 ? 1 : 4);
+template <typename T, int VEC, int NV>
+constexpr int kFwdAhead = 32 / kRowRegs<T, VEC, NV> < 4 ? 32 / kRowRegs<T, VEC, NV> : 4;
 
 // p[c .. c + VEC), 16-byte aligned when VEC > 1, or `none` without a p.
 template <int VEC>
-__device__ __forceinline__ void load_floats(const float* __restrict__ p, int c, float none,
-                                            float (&v)[VEC]) {
+__device__ __forceinline__ void load_units(const float* __restrict__ p, int c, float none,
+                                           typename UnitOf<VEC>::type (&u)[UnitOf<VEC>::count]) {
     if constexpr (VEC == 1) {
-        v[0] = p ? __ldg(p + c) : none;
+        u[0].v = p ? __ldg(p + c) : none;
     } else {
 #pragma unroll
-        for (int i = 0; i < VEC; i += 4) {
-            const float4 f = p ? __ldg(reinterpret_cast<const float4*>(p + c + i))
+        for (int i = 0; i < VEC / 2; i += 2) {
+            const float4 f = p ? __ldg(reinterpret_cast<const float4*>(p + c + 2 * i))
                                : make_float4(none, none, none, none);
-            v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+            u[i] = make_f2(f.x, f.y);
+            u[i + 1] = make_f2(f.z, f.w);
         }
     }
 }
 
 template <typename T, int VEC, int TPR, int NV>
-__global__ void __launch_bounds__(kGroupThreads, 2)
+__global__ void __launch_bounds__(kGroupThreads)
     ln_fwd_rows_kernel(const T* x, const int32_t* count, long long capacity, int C, float eps,
                        const float* __restrict__ gamma, const float* __restrict__ beta, T* y,
                        float* mean_out, float* rstd_out, unsigned* status) {
@@ -57,9 +63,20 @@ __global__ void __launch_bounds__(kGroupThreads, 2)
     // the same number of rounds
     const long long n0 = (long long)blockIdx.x * kGroups + threadIdx.x / TPR;
     const long long w0 = TPR < 32 ? n0 - (threadIdx.x & 31) / TPR : n0;
+    using Unit = UnitOf<VEC>;
+    using U = typename Unit::type;
     const float inv = 1.f / (float)C;
     constexpr int kAhead = kFwdAhead<T, VEC, NV>;
-    Piece<T, VEC> cur[NV], ring[kAhead][NV];
+    Piece<T, VEC> ring[kAhead][NV];
+    U ga[NV][Unit::count], be[NV][Unit::count];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + t) * VEC;
+        if (c < C) {
+            load_units<VEC>(gamma, c, 1.f, ga[i]);
+            load_units<VEC>(beta, c, 0.f, be[i]);
+        }
+    }
     auto load = [&](long long n, Piece<T, VEC>(&p)[NV]) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -73,45 +90,45 @@ __global__ void __launch_bounds__(kGroupThreads, 2)
 #pragma unroll
         for (int u = 0; u < kAhead; ++u, w += step, n += step) {
             if (w >= rows) break;
-            float s = 0.f;
+            // the row as fp32, then its differences from the mean
+            U s = Unit::splat(0.f), v = s, d[NV][Unit::count];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) cur[i] = ring[u][i];
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < Unit::count; ++e) d[i][e] = ring[u][i].unit(e);
             load(n + kAhead * step, ring[u]);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if ((i * TPR + t) * VEC < C)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) s += cur[i].get(e);
+                    for (int e = 0; e < Unit::count; ++e) s = add(s, d[i][e]);
             // the product with 1 / C, corrected by its residual: the mean of a
             // constant row is then its value, and its differences are zero
-            s = group_sum<TPR>(s, sh, 0);
-            float mean = s * inv;
-            mean = fmaf(fmaf(-mean, (float)C, s), inv, mean);
-            float v = 0.f;
+            const float sum = group_sum<TPR>(total(s), sh, 0);
+            float mean = sum * inv;
+            mean = fmaf(fmaf(-mean, (float)C, sum), inv, mean);
+            const U less = Unit::splat(-mean);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if ((i * TPR + t) * VEC < C)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float d = cur[i].get(e) - mean;
-                        v += d * d;
+                    for (int e = 0; e < Unit::count; ++e) {
+                        d[i][e] = add(d[i][e], less);
+                        v = fma(d[i][e], d[i][e], v);
                     }
-            const float rstd = rsqrtf(fmaf(group_sum<TPR>(v, sh, 1), inv, eps));
+            const float rstd = rsqrtf(fmaf(group_sum<TPR>(total(v), sh, 1), inv, eps));
             if (n >= rows) continue;
+            const U times = Unit::splat(rstd);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * TPR + t) * VEC;
                 if (c < C) {
-                    // gamma and beta come from L1 for every row: in registers
-                    // they would cost a row in flight
-                    float ga[VEC], be[VEC];
-                    load_floats<VEC>(gamma, c, 1.f, ga);
-                    load_floats<VEC>(beta, c, 0.f, be);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        be[e] = fmaf((cur[i].get(e) - mean) * rstd, ga[e], be[e]);
-                    cur[i].set_all(be);
-                    cur[i].store(y + n * C + c);
+                    for (int e = 0; e < Unit::count; ++e)
+                        d[i][e] = fma(mul(d[i][e], times), ga[i][e], be[i][e]);
+                    Piece<T, VEC> out;
+                    out.set_units(d[i]);
+                    out.store(y + n * C + c);
                 }
             }
             if (t == 0) {
@@ -141,18 +158,19 @@ __global__ void __launch_bounds__(kGroupThreads)
     const long long step = (long long)gridDim.x * kGroups;
     const long long n0 = (long long)blockIdx.x * kGroups + threadIdx.x / TPR;
     const long long w0 = TPR < 32 ? n0 - (threadIdx.x & 31) / TPR : n0;
+    using Unit = UnitOf<VEC>;
+    using U = typename Unit::type;
+    constexpr int kU = Unit::count;
     const float inv = 1.f / (float)C;
     Piece<T, VEC> cx[NV], cd[NV], nx[NV], nd[NV];
     float m1 = 0.f, r1 = 0.f;
-    float ga[NV * VEC], dg[NV * VEC], db[NV * VEC];
+    U ga[NV][kU], dg[NV][kU], db[NV][kU];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + t) * VEC;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            ga[i * VEC + e] = gamma && c < C ? __ldg(gamma + c + e) : 1.f;
-            dg[i * VEC + e] = db[i * VEC + e] = 0.f;
-        }
+        for (int e = 0; e < kU; ++e) ga[i][e] = Unit::splat(1.f), dg[i][e] = db[i][e] = Unit::splat(0.f);
+        if (c < C) load_units<VEC>(gamma, c, 1.f, ga[i]);
         if (n0 < rows && c < C) {
             nx[i].load(x + n0 * C + c);
             nd[i].load(dy + n0 * C + c);
@@ -164,8 +182,8 @@ __global__ void __launch_bounds__(kGroupThreads)
     }
     for (long long w = w0, n = n0; w < rows; w += step, n += step) {
         const bool in = n < rows, more = n + step < rows;
-        const float m = m1, r = r1;
-        float s1 = 0.f, s2 = 0.f;
+        const U less = Unit::splat(-m1), times = Unit::splat(r1);
+        U s1 = Unit::splat(0.f), s2 = s1;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * VEC;
@@ -184,29 +202,30 @@ __global__ void __launch_bounds__(kGroupThreads)
         for (int i = 0; i < NV; ++i)
             if (in && (i * TPR + t) * VEC < C)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float d = cd[i].get(e), xh = (cx[i].get(e) - m) * r;
-                    const float g = d * ga[i * VEC + e];
-                    s1 += g;
-                    s2 += g * xh;
-                    dg[i * VEC + e] += d * xh;
-                    db[i * VEC + e] += d;
+                for (int e = 0; e < kU; ++e) {
+                    const U d = cd[i].unit(e), xh = mul(add(cx[i].unit(e), less), times);
+                    const U g = mul(d, ga[i][e]);
+                    s1 = add(s1, g);
+                    s2 = fma(g, xh, s2);
+                    dg[i][e] = fma(d, xh, dg[i][e]);
+                    db[i][e] = add(db[i][e], d);
                 }
         if (dx == nullptr) continue;
-        const float c1 = group_sum<TPR>(s1, sh, 0) * inv;
-        const float c2 = group_sum<TPR>(s2, sh, 1) * inv;
+        const float c1 = group_sum<TPR>(total(s1), sh, 0) * inv;
+        const float c2 = group_sum<TPR>(total(s2), sh, 1) * inv;
         if (!in) continue;
+        const U less1 = Unit::splat(-c1), less2 = Unit::splat(-c2);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * VEC;
             if (c < C) {
-                float f[VEC];
+                U f[kU];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float xh = (cx[i].get(e) - m) * r;
-                    f[e] = (cd[i].get(e) * ga[i * VEC + e] - c1 - xh * c2) * r;
+                for (int e = 0; e < kU; ++e) {
+                    const U xh = mul(add(cx[i].unit(e), less), times);
+                    f[e] = mul(fma(xh, less2, fma(cd[i].unit(e), ga[i][e], less1)), times);
                 }
-                cx[i].set_all(f);
+                cx[i].set_units(f);
                 cx[i].store(dx + n * C + c);
             }
         }
@@ -218,11 +237,11 @@ __global__ void __launch_bounds__(kGroupThreads)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const int c = (i * TPR + t) * VEC + e;
+            for (int e = 0; e < kU; ++e) {
+                const int c = (i * TPR + t) * VEC + e * (VEC / kU);
                 if (c < C) {
-                    mine[c] = dg[i * VEC + e];
-                    mine[C + c] = db[i * VEC + e];
+                    Unit::store(mine + c, dg[i][e]);
+                    Unit::store(mine + C + c, db[i][e]);
                 }
             }
         __syncthreads();
@@ -236,11 +255,11 @@ __global__ void __launch_bounds__(kGroupThreads)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const int c = (i * TPR + t) * VEC + e;
+            for (int e = 0; e < kU; ++e) {
+                const int c = (i * TPR + t) * VEC + e * (VEC / kU);
                 if (c < C) {
-                    out[c] = dg[i * VEC + e];
-                    out[C + c] = db[i * VEC + e];
+                    Unit::store(out + c, dg[i][e]);
+                    Unit::store(out + C + c, db[i][e]);
                 }
             }
     }
@@ -376,7 +395,7 @@ template <typename T, int VEC, int TPR, int NV>
 hc_status fwd_rows(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
     constexpr int kGroups = kGroupThreads / TPR;
     const long long need = ((long long)a.capacity + kGroups - 1) / kGroups;
-    const long long cap = (long long)ctx->num_sms * 2;  // resident at up to 64 registers
+    const long long cap = (long long)ctx->num_sms;
     return launch_pdl(ln_fwd_rows_kernel<T, VEC, TPR, NV>,
                       dim3((unsigned)(need < cap ? need : cap)), dim3(kGroupThreads), 0, s,
                       "ln_fwd_rows_kernel", (const T*)a.x, a.count, (long long)a.capacity, a.C,

@@ -51,6 +51,74 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// Arithmetic units of a piece: two fp32 values that one instruction adds,
+// multiplies or accumulates, or one where a piece is a single element.
+struct F1 {
+    float v;
+};
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 make_f2(float a, float b) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 split(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F1 add(F1 a, F1 b) {
+    return {a.v + b.v};
+}
+__device__ __forceinline__ F1 mul(F1 a, F1 b) {
+    return {a.v * b.v};
+}
+__device__ __forceinline__ F1 fma(F1 a, F1 b, F1 c) {
+    return {fmaf(a.v, b.v, c.v)};
+}
+__device__ __forceinline__ float total(F1 a) {
+    return a.v;
+}
+__device__ __forceinline__ F2 add(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float total(F2 a) {
+    const float2 f = split(a);
+    return f.x + f.y;
+}
+template <int VEC>
+struct UnitOf {
+    using type = F2;
+    static constexpr int count = VEC / 2;
+    static __device__ __forceinline__ F2 splat(float v) { return make_f2(v, v); }
+    static __device__ __forceinline__ void store(float* p, F2 u) {
+        const float2 f = split(u);
+        p[0] = f.x;
+        p[1] = f.y;
+    }
+};
+template <>
+struct UnitOf<1> {
+    using type = F1;
+    static constexpr int count = 1;
+    static __device__ __forceinline__ F1 splat(float v) { return {v}; }
+    static __device__ __forceinline__ void store(float* p, F1 u) { *p = u.v; }
+};
+
 // A piece of a row: VEC elements of T as loaded (16 bytes, or one element).
 template <typename T, int VEC>
 struct Piece;
@@ -62,6 +130,8 @@ struct Piece<T, 1> {
     __device__ __forceinline__ float get(int) const { return to_f32(v); }
     __device__ __forceinline__ void set(int, float f) { v = from_f32<T>(f); }
     __device__ __forceinline__ void set_all(const float (&f)[1]) { v = from_f32<T>(f[0]); }
+    __device__ __forceinline__ F1 unit(int) const { return {to_f32(v)}; }
+    __device__ __forceinline__ void set_units(const F1 (&u)[1]) { v = from_f32<T>(u[0].v); }
 };
 template <>
 struct Piece<float, 4> {
@@ -76,6 +146,13 @@ struct Piece<float, 4> {
     }
     __device__ __forceinline__ void set_all(const float (&f)[4]) {
         v = make_float4(f[0], f[1], f[2], f[3]);
+    }
+    __device__ __forceinline__ F2 unit(int i) const {
+        return i ? make_f2(v.z, v.w) : make_f2(v.x, v.y);
+    }
+    __device__ __forceinline__ void set_units(const F2 (&u)[2]) {
+        const float2 a = split(u[0]), b = split(u[1]);
+        v = make_float4(a.x, a.y, b.x, b.y);
     }
 };
 template <>
@@ -114,6 +191,13 @@ struct Piece<__nv_bfloat16, 8> {
     // two values to a word in one conversion
     __device__ __forceinline__ void set_all(const float (&f)[8]) {
         v = make_uint4(pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7]));
+    }
+    __device__ __forceinline__ F2 unit(int i) const {
+        return make_f2(get(2 * i), get(2 * i + 1));
+    }
+    __device__ __forceinline__ void set_units(const F2 (&u)[4]) {
+        const float2 a = split(u[0]), b = split(u[1]), c = split(u[2]), d = split(u[3]);
+        v = make_uint4(pair(a.x, a.y), pair(b.x, b.y), pair(c.x, c.y), pair(d.x, d.y));
     }
     static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
         const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
