@@ -657,8 +657,9 @@ __global__ void __launch_bounds__(kThreads, 3)
 }
 
 // Block `chunk`: if a long row starts in it, the sum of the row's chunks' sums
-// in order, a thread per channel.
-__global__ void __launch_bounds__(1024) embed_bwd_join_kernel(const GradArgs a) {
+// in order, V channels a thread.
+template <int V>
+__global__ void __launch_bounds__(kThreads) embed_bwd_join_kernel(const GradArgs a) {
     pdl_wait();
     pdl_trigger();
     const int total = entries(a), chunk = chunk_of(a, total);
@@ -671,11 +672,20 @@ __global__ void __launch_bounds__(1024) embed_bwd_join_kernel(const GradArgs a) 
     // the row starts in this chunk: at its first entry (slot 0) or later
     // (slot 1); it holds the first entry of every later chunk (slot 0)
     const int k1 = (r.y - 1) / chunk;
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-        float s = a.part[(2ll * blockIdx.x + (r.x == b ? 0 : 1)) * a.C + c];
+    const float* const first = a.part + (2ll * blockIdx.x + (r.x == b ? 0 : 1)) * a.C;
+    for (int c = threadIdx.x * V; c < a.C; c += kThreads * V) {
+        Piece<float, V> s;
+        s.load(first + c);
 #pragma unroll 8
-        for (int k = blockIdx.x + 1; k <= k1; ++k) s += a.part[2ll * k * a.C + c];
-        a.dtable[(long long)row * a.C + c] = s * a.scale;
+        for (int k = blockIdx.x + 1; k <= k1; ++k) {
+            Piece<float, V> f;
+            f.load(a.part + 2ll * k * a.C + c);
+#pragma unroll
+            for (int v = 0; v < V; ++v) s.set(v, s.get(v) + f.get(v));
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) s.set(v, s.get(v) * a.scale);
+        s.store(a.dtable + (long long)row * a.C + c);
     }
 }
 
@@ -729,9 +739,8 @@ hc_status bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStrea
                               dim3(kThreads), 0, s, "embed_bwd_kernel", a, (const T*)dy, chunks,
                               slices, (int)per);
     if (st != HC_OK || chunks == 0) return st;
-    const int threads = a.C >= 1024 ? 1024 : (a.C + 31) / 32 * 32;
-    return launch_pdl(embed_bwd_join_kernel, dim3((unsigned)chunks), dim3((unsigned)threads), 0, s,
-                      "embed_bwd_join_kernel", a);
+    return launch_pdl(VEC == 4 ? embed_bwd_join_kernel<4> : embed_bwd_join_kernel<1>,
+                      dim3((unsigned)chunks), dim3(kThreads), 0, s, "embed_bwd_join_kernel", a);
 }
 
 // Pieces of four channels: the fp32 sums of a warp's pieces then leave as

@@ -186,30 +186,18 @@ __device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint3
     return wait_slow(bar0, parity0, abort_flag, status, limit) &&
            wait_slow(bar1, parity1, abort_flag, status, limit);
 }
-__device__ __forceinline__ void cluster_barrier() {
-    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
 // A float at the same shared-memory offset of another CTA of the cluster.
 __device__ __forceinline__ float lds_cluster_f32(uint32_t addr, uint32_t rank) {
-    uint32_t at;
     float v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(cluster_map(addr, rank)) : "memory");
     return v;
 }
 
 __device__ __forceinline__ float4 lds_cluster_f4(uint32_t addr, uint32_t rank) {
-    uint32_t at;
     float4 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];\n"
                  : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(at)
+                 : "r"(cluster_map(addr, rank))
                  : "memory");
     return v;
 }
@@ -705,21 +693,8 @@ hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
         if (st != HC_OK) return st;
         done[ctx->device] = true;
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = C::kSmem;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)k.split;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return check_cuda(cudaLaunchKernelEx(&cfg, kern, k, mx, mw), "fp8_linear_kernel");
+    return launch_cluster(kern, (unsigned)grid, (unsigned)k.split, kThreads, C::kSmem, s,
+                          "fp8_linear_kernel", k, mx, mw);
 }
 
 template <typename T>

@@ -11,6 +11,44 @@ namespace hc {
 
 #if defined(__CUDACC__)
 
+// launch_pdl with `cluster` neighbouring blocks of the grid to a cluster.
+template <typename... KArgs, typename... Args>
+hc_status launch_cluster(void (*kernel)(KArgs...), unsigned blocks, unsigned cluster, int threads,
+                         size_t smem, cudaStream_t s, const char* what, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...), what);
+}
+
+// Every thread of every block of the cluster; what was written before it, to
+// shared or global memory, is seen after it by all of them.
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The shared-memory address of block `rank` of the cluster that `addr` is here.
+__device__ __forceinline__ uint32_t cluster_map(uint32_t addr, uint32_t rank) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
+    return at;
+}
+
 // Rows in use: *count clamped to [0, capacity] (reported when it was
 // outside), or every row when count is NULL.
 __device__ __forceinline__ long long token_rows(const int32_t* count, long long capacity,
