@@ -484,10 +484,18 @@ hc_status rows_in_regs(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, 
     return back ? bwd_rows<T, VEC, TPR, NV>(ctx, a, s) : fwd_rows<T, VEC, TPR, NV>(ctx, a, s);
 }
 
-// Rows of at most 8192 channels are held in registers, by the smallest group
-// that does so with two 16-byte pieces a thread (the gradient keeps two rows'
-// pieces, gamma and both sums of every channel); wider rows go through the
-// caches.
+// Rows of at most 8192 channels are held in registers (16384 x 8192 bf16:
+// forward 100 us, gradient 170; through the caches 171 and 637), by the
+// smallest group that does so with two 16-byte pieces a thread (four for the
+// widest fp32 rows): the gradient keeps two rows' pieces, gamma and both sums
+// of every channel. Twice the threads for a row cost more than they hide
+// (65536 x 2048 bf16: 135 and 183 us against 89 and 136; 65536 x 64: 14 and 18
+// against 5 and 9), four pieces a thread slow the gradient (65536 x 256 bf16:
+// 48 us against 22). Rows that allow no 16-byte loads are read element by
+// element (65536 x 2048 bf16 would then take 250 and 280 us); there the
+// forward holds 16 elements a thread from 257 channels on (32768 x 2047 bf16:
+// 75 us against 127 with 8), the gradient at most 8 (144 against 252) up to
+// 4096.
 template <typename T>
 hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStream_t s) {
     constexpr int kVec = 16 / (int)sizeof(T);
@@ -507,10 +515,18 @@ hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStrea
     }
     if (C <= 32) return rows_in_regs<T, 1, 8, 4>(ctx, a, back, s);
     if (C <= 64) return rows_in_regs<T, 1, 8, 8>(ctx, a, back, s);
+    if (C <= 128) return rows_in_regs<T, 1, 32, 4>(ctx, a, back, s);
     if (C <= 256) return rows_in_regs<T, 1, 32, 8>(ctx, a, back, s);
-    if (C <= 512) return rows_in_regs<T, 1, 32, 16>(ctx, a, back, s);
-    if (C <= 1024) return rows_in_regs<T, 1, 128, 8>(ctx, a, back, s);
-    if (C <= 4096) return rows_in_regs<T, 1, 512, 8>(ctx, a, back, s);
+    if (C > 512 && C <= 1024) return rows_in_regs<T, 1, 128, 8>(ctx, a, back, s);
+    if (back) {
+        if (C <= 512) return bwd_rows<T, 1, 128, 4>(ctx, a, s);
+        if (C <= 2048) return bwd_rows<T, 1, 256, 8>(ctx, a, s);
+        if (C <= 4096) return bwd_rows<T, 1, 512, 8>(ctx, a, s);
+    } else {
+        if (C <= 512) return fwd_rows<T, 1, 32, 16>(ctx, a, s);
+        if (C <= 2048) return fwd_rows<T, 1, 128, 16>(ctx, a, s);
+        if (C <= 4096) return fwd_rows<T, 1, 256, 16>(ctx, a, s);
+    }
     return rows_in_regs<T, 1, 512, 16>(ctx, a, back, s);
 }
 
