@@ -682,9 +682,15 @@ hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
     const long long tiles =
         (long long)((a.capacity + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes)) *
         ((a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN));
-    // split while every CTA still gets an SM of its own and two blocks or more
+    // Split while every CTA still gets an SM (or half) of its own and two blocks
+    // or more: 1 x 8192 x 8192 takes 13.5 us, unsplit 22. Clusters of 8 find room
+    // late unless they leave half of it free: 128 x 2048 x 2048 (16 tiles) 14.0
+    // us, 7.1 with clusters of 4, 1 x 4096 x 4096 6.1 and 5.5; 128 x 8192 x 1024
+    // (8 tiles) 8.9 against 9.8.
     const int slots = ctx->num_sms * (C::kTwo ? 2 : 1);
-    while (k.split < 8 && tiles * k.split * 2 <= slots && k.nkb >= 4 * k.split) k.split *= 2;
+    while (k.split < 8 && tiles * k.split * (k.split == 4 ? 4 : 2) <= slots &&
+           k.nkb >= 4 * k.split)
+        k.split *= 2;
     if (tiles > 0x7fffffffll) {
         set_error("hc_fp8_linear_fwd: capacity=%d C_out=%d is too large", a.capacity, a.C_out);
         return HC_ERR_UNSUPPORTED;
@@ -706,12 +712,20 @@ hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
 
 template <typename T>
 hc_status dispatch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
+    // Few tokens on the columns, the narrowest that holds them: 16 x 4096 x 4096
+    // 6.2 us, 10.8 with 64 columns, 10.1 with tokens on the lanes. At 33 to 64
+    // both orientations are near: 37 x 2000 x 1001 6.2 and 7.7 us, 64 x 8192 x
+    // 8192 18.1 and 18.8, 64 x 2048 x 8192 10.2 and 9.1.
     if (a.capacity <= 16) return launch<16, true, T>(ctx, a, s);
     if (a.capacity <= 32) return launch<32, true, T>(ctx, a, s);
     if (a.capacity <= 64) return launch<64, true, T>(ctx, a, s);
-    // 256 output channels a tile once that still gives every SM a tile
-    const long long tiles256 = (long long)((a.capacity + kLanes - 1) / kLanes) * ((a.C_out + 255) / 256);
-    if (a.C_out > 128 && tiles256 >= ctx->num_sms) return launch<256, false, T>(ctx, a, s);
+    // A tile of 256 output channels takes 1.6 times as long as one of 128 (one
+    // wave of each, 1024 x 4096 x 4096: 17.4 us against 22.1 for two waves of
+    // 128): the width whose waves take less.
+    const long long m = (a.capacity + kLanes - 1) / kLanes, sms = ctx->num_sms;
+    const long long waves128 = (m * ((a.C_out + 127) / 128) + sms - 1) / sms;
+    const long long waves256 = (m * ((a.C_out + 255) / 256) + sms - 1) / sms;
+    if (a.C_out > 128 && 8 * waves256 <= 5 * waves128) return launch<256, false, T>(ctx, a, s);
     return launch<128, false, T>(ctx, a, s);
 }
 
