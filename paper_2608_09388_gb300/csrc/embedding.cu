@@ -8,9 +8,9 @@
 // order: results are the same from run to run.
 //
 // Forward and gradient are bound by memory (rows gathered, a table of fp32
-// written whole), the sort by the round trips of its five launches (two and a
-// half a pass). 65536 Zipf-distributed ids into 131072 x 1024 bf16 (GB300):
-// forward 32 us (26 at the copy rate), sort 26 us, gradient 132 us (99).
+// written whole), the sort by the round trips of its five launches (two a
+// pass, one for row_ptr). 65536 Zipf-distributed ids into 131072 x 1024 bf16 (GB300):
+// forward 32 us (26 at the copy rate), sort 26 us, gradient 124 us (99).
 #include "tokens.cuh"
 
 namespace hc {
@@ -383,9 +383,15 @@ __global__ void __launch_bounds__(kThreads)
 // first entry or its last, so a chunk has at most two such sums, slot 0 for
 // the row of its first entry and slot 1 for another row at its end. Both
 // kinds of work are blocks of one launch (embed_bwd_kernel). The chunks' sums
-// of a row are then added in order by the block of the chunk where the row
-// starts (embed_bwd_join_kernel; at most one long row starts in a chunk).
+// of a row are then added in a fixed order by the blocks of the chunk where
+// the row starts (embed_bwd_join_kernel; at most one long row starts in a
+// chunk, noted in `starts`).
+// Fewer chunks leave frequent tokens to few groups, more mean more sums to join:
+// 65536 ids of a 32000 x 512 bf16 table, frequent rows side by side, 60 us with 8
+// chunks an SM (79 with 4, 59 with 16), 16763 of 10475 x 128 fp32, frequent rows
+// scattered, 14.3 (13.7, 16.3).
 constexpr int kMinChunk = 64;
+constexpr int kChunksPerSM = 8;
 
 struct GradArgs {
     const int32_t* row_ptr;
@@ -394,6 +400,7 @@ struct GradArgs {
     int max_chunks;
     float scale;
     float* part;    // [chunks][2][C]
+    int* starts;    // [chunks] the long row that starts there, or -1
     float* dtable;
     unsigned* status;
 };
@@ -608,10 +615,17 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
     constexpr int kWarps = kThreads / 32, kWidth = 32 * VEC;
     const int total = entries(a), chunk = chunk_of(a, total);
     const long long b = (long long)index * chunk;
-    if (b >= total) return;
+    if (b >= total) {
+        if (threadIdx.x == 0) a.starts[index] = -1;
+        return;
+    }
     const int p0 = (int)b, p1 = (int)(b + chunk < total ? b + chunk : total);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int2 row = rows_at(a, make_int2(p0, p1 - 1));
+    if (threadIdx.x == 0) {
+        const int2 r = tokens_of(a, row.y);
+        a.starts[index] = r.y - r.x > chunk && r.x >= p0 ? row.y : -1;
+    }
     int sl = 1;
     while (sl < kWarps && sl * kWidth < a.C) sl *= 2;
     const int shares = kWarps / sl, share = warp / sl;
@@ -643,7 +657,7 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
 
 // Blocks [0, chunks): chunks; the others: groups of table rows.
 // Three blocks an SM: with fewer registers a thread and 256 channels a group
-// the 131072 x 1024 bf16 table of 65536 tokens takes 135 us, with 512 channels
+// the 131072 x 1024 bf16 table of 65536 tokens took 135 us, with 512 channels
 // and two blocks 147 us (loads in flight per warp against warps).
 template <typename T, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(kThreads, 3)
@@ -661,37 +675,50 @@ __global__ void __launch_bounds__(kThreads, 3)
     }
 }
 
-// Block `chunk`: if a long row starts in it, the sum of the row's chunks' sums
-// in order, V channels a thread.
+// Block (slice, chunk): if a long row starts in the chunk, 32 * V channels of
+// the sum of the row's chunks' sums. Warp w adds every 8th from the w-th on,
+// then the warps' sums are added in order. (One block a row, each thread walking
+// all sums of its channels: 131 us instead of 125 for the gradient of 131072 x
+// 1024, 21 instead of 17 for 65536 tokens of 10475 x 128 fp32.)
 template <int V>
 __global__ void __launch_bounds__(kThreads) embed_bwd_join_kernel(const GradArgs a) {
+    constexpr int kWarps = kThreads / 32;
+    __shared__ float sh[kWarps][32 * V];
     pdl_wait();
     pdl_trigger();
-    const int total = entries(a), chunk = chunk_of(a, total);
-    const long long b = (long long)blockIdx.x * chunk;
-    if (b >= total) return;
-    const int p1 = (int)(b + chunk < total ? b + chunk : total);
-    const int row = rows_at(a, make_int2(p1 - 1, p1 - 1)).x;
+    const int row = __ldg(a.starts + blockIdx.y);
+    if (row < 0) return;
+    const int chunk = chunk_of(a, entries(a));
     const int2 r = tokens_of(a, row);
-    if (r.y - r.x <= chunk || r.x < b) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int c = ((int)blockIdx.x * 32 + lane) * V;
     // the row starts in this chunk: at its first entry (slot 0) or later
     // (slot 1); it holds the first entry of every later chunk (slot 0)
-    const int k1 = (r.y - 1) / chunk;
-    const float* const first = a.part + (2ll * blockIdx.x + (r.x == b ? 0 : 1)) * a.C;
-    for (int c = threadIdx.x * V; c < a.C; c += kThreads * V) {
-        Piece<float, V> s;
-        s.load(first + c);
-#pragma unroll 8
-        for (int k = blockIdx.x + 1; k <= k1; ++k) {
+    const int k0 = (int)blockIdx.y, k1 = (r.y - 1) / chunk;
+    const int slot0 = r.x == (long long)k0 * chunk ? 0 : 1;
+    Piece<float, V> s;
+#pragma unroll
+    for (int v = 0; v < V; ++v) s.set(v, 0.f);
+    if (c < a.C) {
+#pragma unroll 4
+        for (int k = k0 + warp; k <= k1; k += kWarps) {
             Piece<float, V> f;
-            f.load(a.part + 2ll * k * a.C + c);
+            f.load(a.part + (2ll * k + (k == k0 ? slot0 : 0)) * a.C + c);
 #pragma unroll
             for (int v = 0; v < V; ++v) s.set(v, s.get(v) + f.get(v));
         }
-#pragma unroll
-        for (int v = 0; v < V; ++v) s.set(v, s.get(v) * a.scale);
-        s.store(a.dtable + (long long)row * a.C + c);
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) sh[warp][lane * V + v] = s.get(v);
+    __syncthreads();
+    if (warp != 0 || c >= a.C) return;
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) s.set(v, s.get(v) + sh[w][lane * V + v]);
+#pragma unroll
+    for (int v = 0; v < V; ++v) s.set(v, s.get(v) * a.scale);
+    s.store(a.dtable + (long long)row * a.C + c);
 }
 
 bool aligned16(const void* p) {
@@ -710,8 +737,10 @@ hc_status fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table, v
                       (long long)a.capacity, slices, a.scale, (T*)y, ctx->status);
 }
 
-// 16-byte pieces where the rows allow them; 8 threads a row where that is
-// enough, else a warp with up to 4 pieces each.
+// 16-byte pieces where the rows allow them (65536 of 131072 x 1024 bf16: 36 us,
+// 57 element by element); 8 threads a row where that is enough (65536 of 10475 x
+// 32 fp32: 3.7 us, 7.8 with a warp), else a warp with up to 4 pieces each (one:
+// 39 us).
 template <typename T>
 hc_status run_fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table, void* y,
                   cudaStream_t s) {
@@ -729,7 +758,8 @@ template <typename T, int VEC, int TPR, int NV>
 hc_status bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStream_t s) {
     const int slices = (a.C + NV * TPR * VEC - 1) / (NV * TPR * VEC);
     const int chunks = a.max_chunks > 1 ? a.max_chunks : 0;  // one chunk: no row is longer
-    // table rows per group: one while the groups fill the SMs
+    // table rows per group: one while the groups fill the SMs (always one: 302
+    // us instead of 225 for 65536 tokens of 131072 x 1024 bf16)
     const long long groups = (long long)ctx->num_sms * 16 * (kThreads / TPR);
     long long per = ((long long)a.V * slices + groups - 1) / groups;
     const int most = TPR < kMaxPer ? TPR : kMaxPer;
@@ -744,13 +774,16 @@ hc_status bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStrea
                               dim3(kThreads), 0, s, "embed_bwd_kernel", a, (const T*)dy, chunks,
                               slices, (int)per);
     if (st != HC_OK || chunks == 0) return st;
-    return launch_pdl(VEC == 4 ? embed_bwd_join_kernel<4> : embed_bwd_join_kernel<1>,
-                      dim3((unsigned)chunks), dim3(kThreads), 0, s, "embed_bwd_join_kernel", a);
+    return launch_pdl(embed_bwd_join_kernel<VEC>,
+                      dim3((unsigned)((a.C + 32 * VEC - 1) / (32 * VEC)), (unsigned)chunks),
+                      dim3(kThreads), 0, s, "embed_bwd_join_kernel", a);
 }
 
 // Pieces of four channels: the fp32 sums of a warp's pieces then leave as
 // whole 16-byte stores side by side (pieces of eight bf16 channels would
-// store every other 16 bytes at a time).
+// store every other 16 bytes at a time); element by element the 225 us of 65536
+// tokens of 131072 x 1024 bf16 were 295. 8 threads a row of up to 32 channels:
+// 16763 tokens of 10475 x 32 fp32 take 8 us, with a warp 11.
 template <typename T>
 hc_status run_bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStream_t s) {
     if (a.C % 4 == 0 && aligned16(dy) && aligned16(a.dtable)) {
@@ -849,14 +882,14 @@ hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, in
 hc_status launch_embedding_bwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* dy,
                                const int32_t* row_ptr, const int32_t* order, float* dtable,
                                cudaStream_t s) {
-    // a long row is cut into chunks for four blocks an SM at most
     const long long need = ((long long)a.capacity + kMinChunk - 1) / kMinChunk;
-    const int chunks = (int)(need < ctx->num_sms * 4 ? need : ctx->num_sms * 4);
+    const int chunks = (int)(need < ctx->num_sms * kChunksPerSM ? need : ctx->num_sms * kChunksPerSM);
     GradArgs b{row_ptr, order, a.capacity, a.V, a.C, chunks < 1 ? 1 : chunks, a.scale, nullptr,
-               dtable, ctx->status};
+               nullptr, dtable, ctx->status};
     if (chunks > 1) {
-        b.part = (float*)stream_workspace(s, (size_t)chunks * 2 * a.C * sizeof(float));
+        b.part = (float*)stream_workspace(s, (size_t)chunks * (2 * (size_t)a.C + 1) * sizeof(float));
         if (!b.part) return HC_ERR_CUDA;
+        b.starts = (int*)(b.part + (size_t)chunks * 2 * a.C);
     }
     return a.dt == HC_BF16 ? run_bwd<__nv_bfloat16>(ctx, b, dy, s)
                            : run_bwd<float>(ctx, b, dy, s);
