@@ -491,8 +491,9 @@ hc_status hc_layer_norm_fwd(const void* x, hc_dtype dt, const int32_t* count, in
  *   x, dy     [capacity, C] of dtype dt; mean, rstd as the forward wrote them
  *   dx        [capacity, C] of dtype dt, or NULL; may be x or dy (in place)
  *   dgamma, dbeta  [C] fp32, or NULL each; at least one output is required
- * Uses the library's per-stream workspace (8 bytes per row and channel sums
- * of 8 * C bytes for each of at most 16 blocks per SM).
+ * Uses the library's per-stream workspace (channel sums of 8 * C bytes for
+ * each of at most one block per SM; rows of more than 8192 channels: 8 bytes
+ * per row and 2 KB for each of at most 8 blocks per SM and one per 256 channels).
  */
 hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const int32_t* count,
                             int capacity, int C, const float* gamma, const float* mean,
@@ -541,7 +542,7 @@ hc_status hc_embedding_sort(const int32_t* ids, int ids_stride, const int32_t* c
  *             64 tokens are unspecified. No access leaves the buffers.
  * A row of more than 64 tokens is cut into pieces summed by blocks of their
  * own and joined in order. Uses the library's per-stream workspace (8 * C
- * bytes for each 64 tokens, at most for four pieces per SM).
+ * + 4 bytes for each 64 tokens, at most for eight pieces per SM).
  */
 hc_status hc_embedding_bwd(const void* dy, hc_dtype dt, const int32_t* row_ptr,
                            const int32_t* order, int capacity, int V, int C, float scale,

@@ -28,9 +28,11 @@
 // CTA records HC_ERR_TIMEOUT, waits for its own copies and MMAs and frees its
 // TMEM.
 //
-// Measured on a GB300: 16384 x 8192 x 8192 in 755 us (2.9 PFLOP/s, tensor pipe
-// 64% of elapsed) while the clock holds, 880 us when it runs on at the 1.4 kW
-// limit (1.6 GHz); the MMAs alone with their loads take 612 us. 1 x 8192 x
+// Measured on a GB300: 16384 x 8192 x 8192 in 745 us (2.95 PFLOP/s, tensor pipe
+// 64% of elapsed) while the clock holds, 825 to 870 us when it runs on at the 1.4 kW
+// limit (1.6 GHz); the MMAs alone with their loads take 612 us. A tile of few blocks pays for its
+// first scales and its epilogue, about 2 us (16384 x 640 x 4096: 69 us, 41 without
+// the stores and what leads to them). 1 x 8192 x
 // 8192 takes 14 us, 9.9 of them the weight at the copy rate.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -441,20 +443,34 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
         const int nbo = (a.C_out + kKB - 1) / kKB;
         uint32_t it = 0;
         bool ok = true;
-        for (uint32_t t = first; t < tiles && ok; t += step) {
+        // The two factors of a block's scale are loaded two blocks ahead and
+        // multiplied when they are used (formed at once, the product would
+        // wait for its loads); unrolled by two, so that no copy from one
+        // set to the other waits either. A row that is not in use takes
+        // row 0's scales and is not stored. The last block's are loaded
+        // again rather than any past it.
+        float fx[2], fw[2];
+        const float *xs, *xs_last, *ws;
+        float bias_r[C::kCols / 32 + 1];
+        auto load_scale = [&](int u) {
+            fx[u] = __ldg(xs);
+            fw[u] = __ldg(ws);
+            if (xs < xs_last) {
+                xs += a.capacity;
+                ++ws;
+            }
+        };
+        // the first scales and the bias of tile t, asked for before the tile
+        // before it is stored
+        auto begin = [&](uint32_t t) {
             int m, n;
             tile_at(t, tm, tn, m, n);
-            float acc[C::kCols];
-#pragma unroll
-            for (int j = 0; j < C::kCols; ++j) acc[j] = 0.f;
             if constexpr (!kSwap) {
-                __syncwarp();  // the last tile's bias has been read
 #pragma unroll
                 for (int j = 0; j < C::kCols; j += 32) {
                     const int o = n * BN + half * C::kCols + j + lane;
-                    bias_s[j + lane] = a.bias && o < a.C_out ? __ldg(a.bias + o) : 0.f;
+                    bias_r[j / 32] = a.bias && o < a.C_out ? __ldg(a.bias + o) : 0.f;
                 }
-                __syncwarp();
             }
             // rows on lanes: this thread's token, and the block of its channels;
             // channels on lanes: lane l holds the scale of the half's token l
@@ -462,26 +478,23 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
                                   : m * kLanes + quarter * 32 + lane;
             const bool row_in = row < rows && (!kSwap || lane < C::kCols);
             const int ob = kSwap ? n : (n * BN + half * C::kCols) / kKB;
-            const float* xs = a.xs + (long long)kb0 * a.capacity + (row_in ? row : 0);
-            const float* ws = a.ws + (long long)(ob < nbo ? ob : 0) * k.nkb + kb0;
-            // The two factors of a block's scale are loaded two blocks ahead and
-            // multiplied when they are used (formed at once, the product would
-            // wait for its loads); unrolled by two, so that no copy from one
-            // set to the other waits either. A row that is not in use takes
-            // row 0's scales and is not stored. The last block's are loaded
-            // again rather than any past it.
-            float fx[2], fw[2];
-            const float* const xs_last = xs + (long long)(kb1 - kb0 - 1) * a.capacity;
-            auto load_scale = [&](int u) {
-                fx[u] = __ldg(xs);
-                fw[u] = __ldg(ws);
-                if (xs < xs_last) {
-                    xs += a.capacity;
-                    ++ws;
-                }
-            };
+            xs = a.xs + (long long)kb0 * a.capacity + (row_in ? row : 0);
+            xs_last = xs + (long long)(kb1 - kb0 - 1) * a.capacity;
+            ws = a.ws + (long long)(ob < nbo ? ob : 0) * k.nkb + kb0;
             load_scale(0);
             load_scale(1);
+        };
+        if (first < tiles) begin(first);
+        for (uint32_t t = first; t < tiles && ok; t += step) {
+            float acc[C::kCols];
+#pragma unroll
+            for (int j = 0; j < C::kCols; ++j) acc[j] = 0.f;
+            if constexpr (!kSwap) {
+                __syncwarp();  // the last tile's bias has been read
+#pragma unroll
+                for (int j = 0; j < C::kCols; j += 32) bias_s[j + lane] = bias_r[j / 32];
+                __syncwarp();
+            }
             for (int left = kb1 - kb0; left > 0 && ok; left -= 2) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -534,6 +547,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
                 }
                 break;
             }
+            int m, n;
+            tile_at(t, tm, tn, m, n);
+            if (t + step < tiles) begin(t + step);
             if constexpr (kSwap) {
                 const int o = n * kLanes + quarter * 32 + lane;
                 if (o < a.C_out) {
