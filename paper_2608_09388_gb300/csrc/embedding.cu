@@ -8,9 +8,9 @@
 // order: results are the same from run to run.
 //
 // Forward and gradient are bound by memory (rows gathered, a table of fp32
-// written whole), the sort by the round trips of its five launches (two a
-// pass, one for row_ptr). 65536 Zipf-distributed ids into 131072 x 1024 bf16 (GB300):
-// forward 32 us (26 at the copy rate), sort 26 us, gradient 124 us (99).
+// written whole), the sort by the round trips of its launches (two a pass, one
+// for row_ptr). 65536 Zipf-distributed ids into 131072 x 1024 bf16 (GB300):
+// forward 32 us (26 at the copy rate), sort 24 us, gradient 125 us (99).
 #include "tokens.cuh"
 
 namespace hc {
@@ -63,9 +63,8 @@ constexpr int kMaxDigitBits = 11;
 constexpr int kMaxDigits = 1 << kMaxDigitBits;
 constexpr int kMaxTiles = 64;
 constexpr int kSortWarps = 16;
-constexpr int kRounds = 8;  // keys per lane held in registers at a time
-constexpr int kMinTile = kSortWarps * 32 * kRounds;
 constexpr int kSortThreads = kSortWarps * 32;
+constexpr int kSmallSort = 4 * kSortThreads;  // entries of a sort by one block
 
 struct SortArgs {
     const int32_t* ids;       // first pass: the ids themselves
@@ -81,8 +80,16 @@ struct SortArgs {
     unsigned* status;
 };
 
-// Keys per tile, a multiple of kMinTile, for at most kMaxTiles tiles.
+// Keys per tile, a multiple of R a thread, for at most kMaxTiles tiles. R keys a
+// lane are held in registers at a time and placed one after another: few keys a
+// tile shorten that chain, many tiles lengthen the sum of their histograms. With
+// row_ptr 16763 ids take 16.4 us with R = 2, 17.8 with 4, 23.6 with 8, 65536 of
+// 131072 rows 25.7, 23.7 and 26.2, 262144 of 32000 35, 35 and 31: R is 2 while
+// that is 32 tiles at most, else 4 (8 would suit a large capacity that is used
+// whole, but N' is often a small part of it).
+template <int R>
 __device__ __forceinline__ long long sort_tile(long long rows) {
+    constexpr int kMinTile = kSortThreads * R;
     const long long t = (rows + kMaxTiles - 1) / kMaxTiles;
     return t < kMinTile ? kMinTile : (t + kMinTile - 1) / kMinTile * kMinTile;
 }
@@ -96,6 +103,7 @@ __device__ __forceinline__ int sort_key(const SortArgs& a, long long i) {
     return a.V;
 }
 
+template <int R>
 __global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(const SortArgs a) {
     __shared__ int h[kMaxDigits];
     const int digits = 1 << a.bits;
@@ -104,7 +112,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_hist_kernel(const SortArgs 
     pdl_trigger();
     __syncthreads();
     const long long rows = token_rows(a.count, a.capacity, a.status);
-    const long long tile = sort_tile(rows);
+    const long long tile = sort_tile<R>(rows);
     const long long b = blockIdx.x * tile;
     if (b >= rows) return;
     const long long e = b + tile < rows ? b + tile : rows;
@@ -122,6 +130,7 @@ constexpr size_t scatter_smem(int bits) {
     return (sizeof(int) << bits) * (kSortWarps + 2);
 }
 
+template <int R>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortArgs a) {
     extern __shared__ int sm[];
     __shared__ int sh[kSortWarps];
@@ -134,7 +143,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(a.count, a.capacity, a.status);
-    const long long tile = sort_tile(rows);
+    const long long tile = sort_tile<R>(rows);
     const int tiles = (int)((rows + tile - 1) / tile);
     if ((int)blockIdx.x >= tiles) return;
     // Starts of the digit runs. Column sums of the tiles' histograms first
@@ -176,24 +185,24 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
             run += tot[d];
         }
     }
-    // Digits of each warp's share: a multiple of 32 * kRounds entries, that
+    // Digits of each warp's share: a multiple of 32 * R entries, that
     // many at a time in registers (the first batch stays for the placing).
     const long long share = tile / kSortWarps;
     const long long b = blockIdx.x * tile + warp * share;
     const long long e = b + share < rows ? b + share : rows;
-    int key[kRounds], pos[kRounds];
+    int key[R], pos[R];
     auto load = [&](long long i0) {
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
+        for (int r = 0; r < R; ++r) {
             const long long i = i0 + r * 32 + lane;
             key[r] = i < e ? sort_key(a, i) : -1;
             pos[r] = a.ids ? (int)i : i < e ? a.pos_in[i] : 0;
         }
     };
-    for (long long i0 = b; i0 < e; i0 += 32 * kRounds) {
+    for (long long i0 = b; i0 < e; i0 += 32 * R) {
         load(i0);
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r)
+        for (int r = 0; r < R; ++r)
             if (key[r] >= 0) atomicAdd(&cnt[(key[r] >> a.shift) & (digits - 1)], 1);
     }
     __syncthreads();
@@ -207,10 +216,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
         }
     }
     __syncthreads();
-    for (long long i0 = b; i0 < e; i0 += 32 * kRounds) {
-        if (share > 32 * kRounds) load(i0);  // else the share is still held
+    for (long long i0 = b; i0 < e; i0 += 32 * R) {
+        if (share > 32 * R) load(i0);  // else the share is still held
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
+        for (int r = 0; r < R; ++r) {
             const bool in = key[r] >= 0;
             const int digit = in ? (key[r] >> a.shift) & (digits - 1) : digits;  // no entry
             const unsigned same = __match_any_sync(0xffffffffu, digit);
@@ -228,12 +237,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const SortAr
     }
 }
 
-// All passes of a sort of at most kMinTile entries by one block, the keys and
+// All passes of a sort of at most R * kSortThreads entries by one block, the keys and
 // positions handed from pass to pass through shared memory.
+template <int R>
 constexpr size_t small_smem(int bits) {
-    return (sizeof(int) << bits) * (kSortWarps + 1) + 2 * sizeof(int) * kMinTile;
+    return (sizeof(int) << bits) * (kSortWarps + 1) + 2 * sizeof(int) * R * kSortThreads;
 }
 
+template <int R>
 __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs a, int passes) {
     extern __shared__ int sm[];
     __shared__ int sh[kSortWarps];
@@ -242,14 +253,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs
     int* const base = sm;                         // [digits]
     int* const cnt = sm + digits * (1 + warp);    // [digits] of this warp
     int* const skey = sm + digits * (1 + kSortWarps);
-    int* const spos = skey + kMinTile;
+    int* const spos = skey + R * kSortThreads;
     pdl_wait();
     pdl_trigger();
     const int rows = (int)token_rows(a.count, a.capacity, a.status);
-    const int i0 = warp * 32 * kRounds + lane;
-    int key[kRounds], pos[kRounds];
+    const int i0 = warp * 32 * R + lane;
+    int key[R], pos[R];
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < R; ++r) {
         pos[r] = i0 + r * 32;
         key[r] = pos[r] < rows ? sort_key(a, pos[r]) : -1;
     }
@@ -258,7 +269,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs
         for (int d = threadIdx.x; d < digits * kSortWarps; d += kSortThreads) sm[digits + d] = 0;
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r)
+        for (int r = 0; r < R; ++r)
             if (key[r] >= 0) atomicAdd(&cnt[(key[r] >> shift) & (digits - 1)], 1);
         __syncthreads();
         // starts of the warps within a digit, then of the digits
@@ -299,7 +310,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
+        for (int r = 0; r < R; ++r) {
             const bool in = key[r] >= 0;
             const int digit = in ? (key[r] >> shift) & (digits - 1) : digits;  // no entry
             const unsigned same = __match_any_sync(0xffffffffu, digit);
@@ -316,14 +327,14 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const SortArgs
         }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kRounds; ++r) {
+        for (int r = 0; r < R; ++r) {
             const int i = i0 + r * 32;
             key[r] = i < rows ? skey[i] : -1;
             pos[r] = i < rows ? spos[i] : 0;
         }
     }
 #pragma unroll
-    for (int r = 0; r < kRounds; ++r) {
+    for (int r = 0; r < R; ++r) {
         const int i = i0 + r * 32;
         if (i < rows) {
             a.keys_out[i] = key[r];
@@ -725,6 +736,66 @@ bool aligned16(const void* p) {
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
+hc_status sort_smem(const DeviceCtx* ctx, const void* kern, size_t bytes, bool (&done)[64],
+                    const char* name) {
+    if (done[ctx->device]) return HC_OK;
+    const hc_status st = check_cuda(
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes), name);
+    done[ctx->device] = st == HC_OK;
+    return st;
+}
+
+template <int R>
+hc_status sort_small(const DeviceCtx* ctx, SortArgs k, int passes, int32_t* order,
+                     const int32_t** sorted, cudaStream_t s) {
+    static bool done[64];
+    auto kern = sort_small_kernel<R>;
+    hc_status st = sort_smem(ctx, (const void*)kern, small_smem<R>(kMaxDigitBits), done,
+                             "sort_small_kernel");
+    if (st != HC_OK) return st;
+    k.keys_out = (int32_t*)stream_workspace(s, sizeof(int32_t) * (size_t)k.capacity);
+    if (!k.keys_out) return HC_ERR_CUDA;
+    k.pos_out = order;
+    *sorted = k.keys_out;
+    return launch_pdl(kern, dim3(1), dim3(kSortThreads), small_smem<R>(k.bits), s,
+                      "sort_small_kernel", k, passes);
+}
+
+template <int R>
+hc_status sort_tiles(const DeviceCtx* ctx, SortArgs k, int passes, int32_t* order,
+                     const int32_t** sorted, cudaStream_t s) {
+    static bool done[64];
+    auto scatter = sort_scatter_kernel<R>;
+    hc_status st = sort_smem(ctx, (const void*)scatter, scatter_smem(kMaxDigitBits), done,
+                             "sort_scatter_kernel");
+    if (st != HC_OK) return st;
+    const long long n = k.capacity, need = (n + R * kSortThreads - 1) / (R * kSortThreads);
+    const unsigned tiles = (unsigned)(need < kMaxTiles ? need : kMaxTiles);
+    // workspace: histograms, two buffers of keys and two of positions
+    const size_t hist = (size_t)kMaxTiles * kMaxDigits;
+    int32_t* ws = (int32_t*)stream_workspace(s, sizeof(int32_t) * (hist + 4 * (size_t)n));
+    if (!ws) return HC_ERR_CUDA;
+    int32_t* keys[2] = {ws + hist, ws + hist + n};
+    int32_t* pos[2] = {keys[1] + n, keys[1] + 2 * n};
+    k.hist = ws;
+    for (int p = 0; p < passes; ++p) {
+        if (p > 0) k.ids = nullptr;
+        k.keys_in = keys[(p + 1) & 1];
+        k.pos_in = pos[(p + 1) & 1];
+        k.keys_out = keys[p & 1];
+        k.pos_out = p == passes - 1 ? order : pos[p & 1];
+        k.shift = p * k.bits;
+        st = launch_pdl(sort_hist_kernel<R>, dim3(tiles), dim3(kSortThreads), 0, s,
+                        "sort_hist_kernel", k);
+        if (st != HC_OK) return st;
+        st = launch_pdl(scatter, dim3(tiles), dim3(kSortThreads), scatter_smem(k.bits), s,
+                        "sort_scatter_kernel", k);
+        if (st != HC_OK) return st;
+        *sorted = k.keys_out;
+    }
+    return HC_OK;
+}
+
 template <typename T, int VEC, int TPR, int NV>
 hc_status fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, const void* table, void* y,
               cudaStream_t s) {
@@ -806,71 +877,28 @@ hc_status launch_embedding_fwd(const DeviceCtx* ctx, const EmbeddingArgs& a, con
 hc_status launch_embedding_sort(const DeviceCtx* ctx, const EmbeddingArgs& a, int32_t* row_ptr,
                                 int32_t* order, cudaStream_t s) {
     const long long n = a.capacity;
-    hc_status st;
     const int32_t* sorted = nullptr;
     if (n > 0) {
-        static bool done[64];
-        if (!done[ctx->device]) {
-            st = check_cuda(cudaFuncSetAttribute(sort_scatter_kernel,
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)scatter_smem(kMaxDigitBits)),
-                            "sort_scatter_kernel");
-            if (st != HC_OK) return st;
-            st = check_cuda(cudaFuncSetAttribute(sort_small_kernel,
-                                                 cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 (int)small_smem(kMaxDigitBits)),
-                            "sort_small_kernel");
-            if (st != HC_OK) return st;
-            done[ctx->device] = true;
-        }
-        const long long need = (n + kMinTile - 1) / kMinTile;
-        const unsigned tiles = (unsigned)(need < kMaxTiles ? need : kMaxTiles);
         // the keys 0 .. V in as few passes as 11-bit digits allow, of equal width
         int key_bits = 1;
         while (key_bits < 31 && (a.V >> key_bits) != 0) ++key_bits;
         const int passes = (key_bits + kMaxDigitBits - 1) / kMaxDigitBits;
-        const int bits = (key_bits + passes - 1) / passes;
-        // workspace: histograms, two buffers of keys and two of positions
-        const size_t hist = (size_t)kMaxTiles * kMaxDigits;
-        int32_t* ws = (int32_t*)stream_workspace(s, sizeof(int32_t) * (hist + 4 * (size_t)n));
-        if (!ws) return HC_ERR_CUDA;
-        int32_t* keys[2] = {ws + hist, ws + hist + n};
-        int32_t* pos[2] = {keys[1] + n, keys[1] + 2 * n};
         SortArgs k{};
         k.ids = a.ids;
-        k.hist = ws;
         k.count = a.count;
         k.ids_stride = a.ids_stride;
         k.capacity = n;
         k.V = a.V;
-        k.bits = bits;
+        k.bits = (key_bits + passes - 1) / passes;
         k.status = ctx->status;
-        if (n <= kMinTile) {
-            // one launch instead of two a pass: 3132 ids in two passes took
-            // 19.9 us that way, most of it launches and their round trips
-            k.keys_out = keys[0];
-            k.pos_out = order;
-            st = launch_pdl(sort_small_kernel, dim3(1), dim3(kSortThreads), small_smem(bits), s,
-                            "sort_small_kernel", k, passes);
-            if (st != HC_OK) return st;
-            sorted = keys[0];
-        } else {
-            for (int p = 0; p < passes; ++p) {
-                k.ids = p == 0 ? a.ids : nullptr;
-                k.keys_in = keys[(p + 1) & 1];
-                k.pos_in = pos[(p + 1) & 1];
-                k.keys_out = keys[p & 1];
-                k.pos_out = p == passes - 1 ? order : pos[p & 1];
-                k.shift = p * bits;
-                st = launch_pdl(sort_hist_kernel, dim3(tiles), dim3(kSortThreads), 0, s,
-                                "sort_hist_kernel", k);
-                if (st != HC_OK) return st;
-                st = launch_pdl(sort_scatter_kernel, dim3(tiles), dim3(kSortThreads),
-                                scatter_smem(bits), s, "sort_scatter_kernel", k);
-                if (st != HC_OK) return st;
-                sorted = k.keys_out;
-            }
-        }
+        // One launch instead of two a pass while a block holds the keys: 2000 ids
+        // 10.5 us with row_ptr, 13.2 with tiles. 4000 by one block would take
+        // 15.5, with tiles 14.1.
+        const hc_status st = n <= 2 * kSortThreads    ? sort_small<2>(ctx, k, passes, order, &sorted, s)
+                             : n <= kSmallSort        ? sort_small<4>(ctx, k, passes, order, &sorted, s)
+                             : n <= 64 * kSortThreads ? sort_tiles<2>(ctx, k, passes, order, &sorted, s)
+                                                      : sort_tiles<4>(ctx, k, passes, order, &sorted, s);
+        if (st != HC_OK) return st;
     }
     const long long need = ((a.V + 1ll > n ? a.V + 1ll : n) + kThreads - 1) / kThreads;
     const long long cap = (long long)ctx->num_sms * 8;

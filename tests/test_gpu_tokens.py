@@ -142,6 +142,13 @@ def test_layer_norm(C, dtype):
     assert (dx[n:] == 77).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("C", [65, 127, 129, 255, 301, 511, 513, 1025, 2047, 2051, 4095, 4099, 8191])
+def test_layer_norm_odd_widths(C, dtype):
+    """Rows without 16-byte loads at the widths where their layout changes."""
+    test_layer_norm(C, dtype)
+
+
 @pytest.mark.parametrize("n", [0, 1, 2, 3, 127, 128, 129, 5000])
 @pytest.mark.parametrize("C,dtype", [(64, BF), (131, F), (1024, BF), (4096, F)])
 def test_layer_norm_rows(n, C, dtype):
@@ -326,6 +333,33 @@ def test_embedding(n, slack, V, C, kind, dtype):
     table, dy = randn(g, V, C, dtype=dtype), randn(g, cap, C, dtype=dtype)
     out = embed_all(table, ids, 1.7, dy, cap, n)
     check_embed(table, ids, 1.7, dy, cap, n, out)
+
+
+@pytest.mark.parametrize("cap", [1023, 1024, 1025, 2047, 2048, 2049, 32768, 32769, 65536, 65537,
+                                 131073])
+def test_embedding_sort_sizes(cap):
+    """The sort at the sizes where its tiles change, all rows used and fewer."""
+    for n in (cap, cap // 2 + 1):
+        for V, kind in ((3, "uniform"), (10475, "zipf")):
+            ids = ids_of(gen(cap + V), cap, V, kind).cuda()
+            row_ptr = torch.full((V + 1,), 77, dtype=torch.int32, device="cuda")
+            order = torch.full((cap,), 77, dtype=torch.int32, device="cuda")
+            hc.hc_embedding_sort(ids, V, row_ptr, order, count=count_of(n))
+            rp, od = sort_ref(ids, n, V)
+            assert np.array_equal(row_ptr.cpu().numpy(), rp)
+            assert np.array_equal(order.cpu().numpy(), od)
+
+
+@pytest.mark.parametrize("n,V,C,dtype", [(9000, 500, 45, BF), (20000, 40, 520, F)])
+def test_embedding_frequent_rows_side_by_side(n, V, C, dtype):
+    """Low ids far more frequent than the others: most tokens belong to rows
+    that are cut into pieces, several of them next to each other."""
+    g = gen(n + V)
+    ids = (torch.rand(n, generator=g, device="cuda").pow(4) * V).int().clamp_(0, V - 1)
+    table, dy = randn(g, V, C, dtype=dtype), randn(g, n, C, dtype=dtype)
+    out = embed_all(table, ids, 0.3, dy, n)
+    check_embed(table, ids, 0.3, dy, n, n, out)
+    assert all(torch.equal(a, b) for a, b in zip(out, embed_all(table, ids, 0.3, dy, n)))
 
 
 def test_embedding_column_of_coordinates():
@@ -534,6 +568,15 @@ def test_fp8_linear(n, slack, K, N, act, out):
     ref, tol = linear_ref(q[:n], s[:, :n], w, ws, K, bias, act)
     within(y[:n], ref, tol + rounding(out, ref), "y")
     assert (y[n:] == 77).all()
+
+
+@pytest.mark.parametrize("n,slack,K,N,act,out", [
+    (2400, 30, 392, 2000, 1, BF), (4700, 0, 136, 1001, 2, F), (4700, 150, 520, 2050, 0, BF),
+    (9000, 0, 260, 3000, 0, F), (128, 0, 1024, 2048, 0, BF), (90, 3, 4096, 1030, 1, F)])
+def test_fp8_linear_tiles(n, slack, K, N, act, out):
+    """Tiles of 256 output channels, one and several a block, with whole and
+    ragged ends; tiles split over clusters of four and eight."""
+    test_fp8_linear(n, slack, K, N, act, out)
 
 
 def test_fp8_linear_forms():
