@@ -29,11 +29,11 @@
 // TMEM.
 //
 // Measured on a GB300: 16384 x 8192 x 8192 in 745 us (2.95 PFLOP/s, tensor pipe
-// 64% of elapsed) while the clock holds, 825 to 870 us when it runs on at the 1.4 kW
-// limit (1.6 GHz); the MMAs alone with their loads take 612 us. A tile of few blocks pays for its
-// first scales and its epilogue, about 2 us (16384 x 640 x 4096: 69 us, 41 without
-// the stores and what leads to them). 1 x 8192 x
-// 8192 takes 14 us, 9.9 of them the weight at the copy rate.
+// 64% of elapsed) while the clock holds, 825 to 870 us when it runs on at the
+// 1.4 kW limit (1.6 GHz); the MMAs alone with their loads take 612 us. A tile of
+// few blocks pays for its first scales and its epilogue, about 2 us (16384 x 640
+// x 4096: 69 us, 41 without the stores and what leads to them). 1 x 8192 x 8192
+// takes 14 us, 9.9 of them the weight at the copy rate.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
