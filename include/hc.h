@@ -492,8 +492,8 @@ hc_status hc_layer_norm_fwd(const void* x, hc_dtype dt, const int32_t* count, in
  *   dx        [capacity, C] of dtype dt, or NULL; may be x or dy (in place)
  *   dgamma, dbeta  [C] fp32, or NULL each; at least one output is required
  * Uses the library's per-stream workspace (channel sums of 8 * C bytes for
- * each of at most one block per SM; rows of more than 8192 channels: 8 bytes
- * per row and 2 KB for each of at most 8 blocks per SM and one per 256 channels).
+ * each of at most three blocks per SM; rows of more than 8192 channels: 8 bytes
+ * per row besides).
  */
 hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const int32_t* count,
                             int capacity, int C, const float* gamma, const float* mean,

@@ -21,7 +21,7 @@
 namespace hc {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 
 // ---------------------------------------------------------------- rows in registers
 // A group of TPR threads holds a whole row: NV pieces of VEC elements each,
@@ -51,6 +51,24 @@ __device__ __forceinline__ void load_units(const float* __restrict__ p, int c, f
                                : make_float4(none, none, none, none);
             u[i] = make_f2(f.x, f.y);
             u[i + 1] = make_f2(f.z, f.w);
+        }
+    }
+}
+
+// The same as plain numbers.
+template <int VEC>
+__device__ __forceinline__ void load_floats(const float* __restrict__ p, int c, float none,
+                                            float (&f)[VEC]) {
+    typename UnitOf<VEC>::type u[UnitOf<VEC>::count];
+    load_units<VEC>(p, c, none, u);
+    if constexpr (VEC == 1) {
+        f[0] = u[0].v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            const float2 v = split(u[i]);
+            f[2 * i] = v.x;
+            f[2 * i + 1] = v.y;
         }
     }
 }
@@ -273,10 +291,12 @@ __global__ void __launch_bounds__(kGroupThreads)
     }
 }
 
-// ---------------------------------------------------------------- any width
+// ---------------------------------------------------------------- wide rows
 // A block per row; the row is read once for the mean, once for the variance
 // and once for the output (the second and third time from the caches).
-template <typename T>
+// 16384 x 16384 bf16: forward 249 us, gradient 457 (158 and 237 at the copy
+// rate; element by element 404 and 1115; forward with 256 threads 283).
+template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads)
     ln_fwd_kernel(const T* x, const int32_t* count, long long capacity, int C, float eps,
                   const float* __restrict__ gamma, const float* __restrict__ beta, T* y,
@@ -289,17 +309,36 @@ __global__ void __launch_bounds__(kThreads)
         const T* xr = x + n * C;
         T* yr = y + n * C;
         float s = 0.f;
-        for (int c = threadIdx.x; c < C; c += kThreads) s += to_f32(xr[c]);
+#pragma unroll 4
+        for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+            Piece<T, VEC> p;
+            p.load(xr + c);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s += p.get(e);
+        }
         const float mean = block_sum(s, sh) / (float)C;
         float v = 0.f;
-        for (int c = threadIdx.x; c < C; c += kThreads) {
-            const float d = to_f32(xr[c]) - mean;
-            v += d * d;
+#pragma unroll 4
+        for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+            Piece<T, VEC> p;
+            p.load(xr + c);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float d = p.get(e) - mean;
+                v += d * d;
+            }
         }
         const float rstd = 1.f / sqrtf(block_sum(v, sh) / (float)C + eps);
-        for (int c = threadIdx.x; c < C; c += kThreads) {
-            const float xh = (to_f32(xr[c]) - mean) * rstd;
-            yr[c] = from_f32<T>(xh * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f));
+        for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+            Piece<T, VEC> p;
+            p.load(xr + c);
+            float w[VEC], b[VEC], f[VEC];
+            load_floats<VEC>(gamma, c, 1.f, w);
+            load_floats<VEC>(beta, c, 0.f, b);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = (p.get(e) - mean) * rstd * w[e] + b[e];
+            p.set_all(f);
+            p.store(yr + c);
         }
         if (threadIdx.x == 0) {
             if (mean_out) mean_out[n] = mean;
@@ -310,7 +349,7 @@ __global__ void __launch_bounds__(kThreads)
 
 // The two means of a row's gradient: sums[2n] = sum g / C, sums[2n + 1] =
 // sum (g * xh) / C.
-template <typename T>
+template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads)
     ln_bwd_rows_kernel(const T* x, const T* dy, const int32_t* count, long long capacity, int C,
                        const float* __restrict__ gamma, const float* __restrict__ mean,
@@ -323,10 +362,19 @@ __global__ void __launch_bounds__(kThreads)
     for (long long n = blockIdx.x; n < rows; n += gridDim.x) {
         const float m = mean[n], r = rstd[n];
         float s1 = 0.f, s2 = 0.f;
-        for (int c = threadIdx.x; c < C; c += kThreads) {
-            const float g = to_f32(dy[n * C + c]) * (gamma ? gamma[c] : 1.f);
-            s1 += g;
-            s2 += g * ((to_f32(x[n * C + c]) - m) * r);
+#pragma unroll 2
+        for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+            Piece<T, VEC> p, d;
+            float w[VEC];
+            p.load(x + n * C + c);
+            d.load(dy + n * C + c);
+            load_floats<VEC>(gamma, c, 1.f, w);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float g = d.get(e) * w[e];
+                s1 += g;
+                s2 += g * ((p.get(e) - m) * r);
+            }
         }
         s1 = block_sum(s1, sh);
         s2 = block_sum(s2, sh);
@@ -337,9 +385,13 @@ __global__ void __launch_bounds__(kThreads)
     }
 }
 
-// A thread per channel walks the rows blockIdx.y, + gridDim.y, ...: dx, and
-// its own sums of dy * xh and dy into part[blockIdx.y][2][C].
-template <typename T>
+// A thread per piece of VEC channels walks the rows blockIdx.y, + gridDim.y,
+// ...: dx, and its own sums of dy * xh and dy into part[blockIdx.y][2][C].
+// kColRows rows are loaded before the first is worked on: dx may be x or dy,
+// so no load would be moved up over a store.
+constexpr int kColRows = 4;
+
+template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads)
     ln_bwd_cols_kernel(const T* x, const T* dy, const int32_t* count, long long capacity, int C,
                        const float* __restrict__ gamma, const float* __restrict__ mean,
@@ -348,20 +400,50 @@ __global__ void __launch_bounds__(kThreads)
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
-    const int c = blockIdx.x * kThreads + threadIdx.x;
+    const int c = (int)(blockIdx.x * kThreads + threadIdx.x) * VEC;
     if (c >= C) return;
-    const float w = gamma ? gamma[c] : 1.f;
-    float dg = 0.f, db = 0.f;
-    for (long long n = blockIdx.y; n < rows; n += gridDim.y) {
-        const float d = to_f32(dy[n * C + c]);
-        const float xh = (to_f32(x[n * C + c]) - mean[n]) * rstd[n];
-        if (dx) dx[n * C + c] = from_f32<T>((d * w - sums[2 * n] - xh * sums[2 * n + 1]) * rstd[n]);
-        dg += d * xh;
-        db += d;
+    float w[VEC], dg[VEC], db[VEC];
+    load_floats<VEC>(gamma, c, 1.f, w);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) dg[e] = db[e] = 0.f;
+    for (long long n0 = blockIdx.y; n0 < rows; n0 += (long long)kColRows * gridDim.y) {
+        Piece<T, VEC> p[kColRows], d[kColRows];
+        float m[kColRows], r[kColRows], s1[kColRows], s2[kColRows];
+#pragma unroll
+        for (int u = 0; u < kColRows; ++u) {
+            // a row past the end is loaded as the first and not used
+            const long long at = n0 + (long long)u * gridDim.y, n = at < rows ? at : n0;
+            p[u].load(x + n * C + c);
+            d[u].load(dy + n * C + c);
+            m[u] = mean[n];
+            r[u] = rstd[n];
+            s1[u] = dx ? sums[2 * n] : 0.f;
+            s2[u] = dx ? sums[2 * n + 1] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < kColRows; ++u) {
+            const long long n = n0 + (long long)u * gridDim.y;
+            if (n >= rows) break;
+            float f[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float g = d[u].get(e), xh = (p[u].get(e) - m[u]) * r[u];
+                f[e] = (g * w[e] - s1[u] - xh * s2[u]) * r[u];
+                dg[e] += g * xh;
+                db[e] += g;
+            }
+            if (dx) {
+                p[u].set_all(f);
+                p[u].store(dx + n * C + c);
+            }
+        }
     }
     if (part) {
-        part[(2ll * blockIdx.y) * C + c] = dg;
-        part[(2ll * blockIdx.y + 1) * C + c] = db;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            part[(2ll * blockIdx.y) * C + c + e] = dg[e];
+            part[(2ll * blockIdx.y + 1) * C + c + e] = db[e];
+        }
     }
 }
 
@@ -442,19 +524,19 @@ hc_status bwd_rows(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s)
     return param_grad(a, part, grid, s);
 }
 
-template <typename T>
+template <typename T, int VEC>
 hc_status fwd_wide(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
     const long long cap = (long long)ctx->num_sms * 8;
     const unsigned grid = (unsigned)(a.capacity < cap ? a.capacity : cap);
-    return launch_pdl(ln_fwd_kernel<T>, dim3(grid), dim3(kThreads), 0, s, "ln_fwd_kernel",
+    return launch_pdl(ln_fwd_kernel<T, VEC>, dim3(grid), dim3(kThreads), 0, s, "ln_fwd_kernel",
                       (const T*)a.x, a.count, (long long)a.capacity, a.C, a.eps, a.gamma, a.beta,
                       (T*)a.y, a.mean_out, a.rstd_out, ctx->status);
 }
 
-template <typename T>
+template <typename T, int VEC>
 hc_status bwd_wide(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s) {
     const bool params = a.dgamma || a.dbeta;
-    const unsigned ctiles = (unsigned)((a.C + kThreads - 1) / kThreads);
+    const unsigned ctiles = (unsigned)((a.C + kThreads * VEC - 1) / (kThreads * VEC));
     long long parts = (ctx->num_sms * 8 + ctiles - 1) / ctiles;
     if (parts > a.capacity) parts = a.capacity;
     if (parts < 1) parts = 1;
@@ -465,13 +547,13 @@ hc_status bwd_wide(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s)
     const long long cap = (long long)ctx->num_sms * 8;
     hc_status st;
     if (a.capacity > 0 && a.dx) {
-        st = launch_pdl(ln_bwd_rows_kernel<T>, dim3((unsigned)(a.capacity < cap ? a.capacity : cap)),
+        st = launch_pdl(ln_bwd_rows_kernel<T, VEC>, dim3((unsigned)(a.capacity < cap ? a.capacity : cap)),
                         dim3(kThreads), 0, s, "ln_bwd_rows_kernel", (const T*)a.x, (const T*)a.dy,
                         a.count, (long long)a.capacity, a.C, a.gamma, a.mean, a.rstd, ws,
                         ctx->status);
         if (st != HC_OK) return st;
     }
-    st = launch_pdl(ln_bwd_cols_kernel<T>, dim3(ctiles, (unsigned)parts), dim3(kThreads), 0, s,
+    st = launch_pdl(ln_bwd_cols_kernel<T, VEC>, dim3(ctiles, (unsigned)parts), dim3(kThreads), 0, s,
                     "ln_bwd_cols_kernel", (const T*)a.x, (const T*)a.dy, a.count,
                     (long long)a.capacity, a.C, a.gamma, a.mean, a.rstd, (const float*)ws,
                     (T*)a.dx, part, ctx->status);
@@ -485,7 +567,7 @@ hc_status rows_in_regs(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, 
 }
 
 // Rows of at most 8192 channels are held in registers (16384 x 8192 bf16:
-// forward 100 us, gradient 170; through the caches 171 and 637), by the
+// forward 100 us, gradient 170; through the caches 145 and 244), by the
 // smallest group that does so with two 16-byte pieces a thread (four for the
 // widest fp32 rows): the gradient keeps two rows' pieces, gamma and both sums
 // of every channel. Twice the threads for a row cost more than they hide
@@ -501,9 +583,13 @@ hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStrea
     constexpr int kVec = 16 / (int)sizeof(T);
     const int C = a.C;
     auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
-    if (C > 8192) return back ? bwd_wide<T>(ctx, a, s) : fwd_wide<T>(ctx, a, s);
-    if (C % kVec == 0 && aligned(a.x) && aligned(a.y) && aligned(a.dy) && aligned(a.dx) &&
-        aligned(a.gamma) && aligned(a.beta)) {
+    const bool wide = C % kVec == 0 && aligned(a.x) && aligned(a.y) && aligned(a.dy) &&
+                      aligned(a.dx) && aligned(a.gamma) && aligned(a.beta);
+    if (C > 8192) {
+        if (wide) return back ? bwd_wide<T, kVec>(ctx, a, s) : fwd_wide<T, kVec>(ctx, a, s);
+        return back ? bwd_wide<T, 1>(ctx, a, s) : fwd_wide<T, 1>(ctx, a, s);
+    }
+    if (wide) {
         if (C <= 8 * kVec) return rows_in_regs<T, kVec, 8, 1>(ctx, a, back, s);
         if (C <= 32 * kVec) return rows_in_regs<T, kVec, 32, 1>(ctx, a, back, s);
         if (C <= 64 * kVec) return rows_in_regs<T, kVec, 32, 2>(ctx, a, back, s);
