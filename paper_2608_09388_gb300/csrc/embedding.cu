@@ -699,13 +699,14 @@ __global__ void __launch_bounds__(kThreads) embed_bwd_join_kernel(const GradArgs
     pdl_trigger();
     const int row = __ldg(a.starts + blockIdx.y);
     if (row < 0) return;
-    const int chunk = chunk_of(a, entries(a));
+    const int total = entries(a), chunk = chunk_of(a, total);
     const int2 r = tokens_of(a, row);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int c = ((int)blockIdx.x * 32 + lane) * V;
     // the row starts in this chunk: at its first entry (slot 0) or later
-    // (slot 1); it holds the first entry of every later chunk (slot 0)
-    const int k0 = (int)blockIdx.y, k1 = (r.y - 1) / chunk;
+    // (slot 1); it holds the first entry of every later chunk (slot 0). Where
+    // row_ptr decreases, its end may lie behind the last chunk.
+    const int k0 = (int)blockIdx.y, k1 = (min(r.y, total) - 1) / chunk;
     const int slot0 = r.x == (long long)k0 * chunk ? 0 : 1;
     Piece<float, V> s;
 #pragma unroll

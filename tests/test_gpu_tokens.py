@@ -483,6 +483,24 @@ def quantise_weight(W):
     return q, s
 
 
+def test_embedding_bwd_end_behind_entries():
+    """A row_ptr that decreases, a row's end far behind the entries in use: it
+    is reported, the chunks' sums stay within their buffer, and the next call
+    is right."""
+    g = gen(7)
+    V, C, cap = 2, 64, 200000
+    dy = randn(g, cap, C)
+    ids = torch.zeros(cap, dtype=torch.int32, device="cuda")
+    _, row_ptr, order, good = embed_all(randn(g, V, C), ids, 1.0, dy, cap)
+    bad = torch.tensor([0, cap, 64], dtype=torch.int32, device="cuda")
+    dt = torch.empty(V, C, device="cuda")
+    hc.hc_embedding_bwd(dy, bad, order, 1.0, dt)
+    assert hc.hc_get_device_status() == hc.HC_ERR_INVALID_INDEX
+    assert (dt[1] == 0).all()
+    hc.hc_embedding_bwd(dy, row_ptr, order, 1.0, dt)
+    assert torch.equal(dt, good) and hc.hc_get_device_status() == hc.HC_OK
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("n,slack,K", [(0, 3, 40), (1, 0, 1), (1, 0, 8192), (7, 2, 15), (33, 7, 16),
                                        (64, 0, 127), (65, 1, 128), (100, 0, 129), (31, 0, 1000),
