@@ -574,10 +574,9 @@ hc_status rows_in_regs(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, 
 // (65536 x 2048 bf16: 135 and 183 us against 89 and 136; 65536 x 64: 14 and 18
 // against 5 and 9), four pieces a thread slow the gradient (65536 x 256 bf16:
 // 48 us against 22). Rows that allow no 16-byte loads are read element by
-// element (65536 x 2048 bf16 would then take 250 and 280 us); there the
-// forward holds 16 elements a thread from 257 channels on (32768 x 2047 bf16:
-// 75 us against 127 with 8), the gradient at most 8 (144 against 252) up to
-// 4096.
+// element (32768 x 2047 bf16 75 and 143 us, half of 89 and 136 at 2048
+// channels); there the forward holds 16 elements a thread from 257 channels on
+// (8: 127 us), the gradient at most 8 (16: 252) up to 4096.
 template <typename T>
 hc_status run(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, cudaStream_t s) {
     constexpr int kVec = 16 / (int)sizeof(T);
