@@ -538,8 +538,9 @@ hc_status hc_embedding_sort(const int32_t* ids, int ids_stride, const int32_t* c
  *   row_ptr, order  from hc_embedding_sort (same capacity). A range of row_ptr
  *             that is not inside [0, capacity], or an entry of order that is
  *             not below capacity, is reported (HC_ERR_INVALID_INDEX) and
- *             skipped; with a row_ptr that decreases, other rows of more than
- *             64 tokens are unspecified. No access leaves the buffers.
+ *             skipped; with a row_ptr that decreases, other rows that have more
+ *             than 64 tokens, or share them with up to 15 neighbours in a
+ *             large table, are unspecified. No access leaves the buffers.
  * A row of more than 64 tokens is cut into pieces summed by blocks of their
  * own and joined in order. Uses the library's per-stream workspace (8 * C
  * + 4 bytes for each 64 tokens, at most for eight pieces per SM).

@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(kThreads)
 // the row starts (embed_bwd_join_kernel; at most one long row starts in a
 // chunk, noted in `starts`).
 // Fewer chunks leave frequent tokens to few groups, more mean more sums to join:
-// 65536 ids of a 32000 x 512 bf16 table, frequent rows side by side, 60 us with 8
+// 65536 ids of a 32000 x 512 bf16 table, frequent rows side by side, took 60 us with 8
 // chunks an SM (79 with 4, 59 with 16), 16763 of 10475 x 128 fp32, frequent rows
 // scattered, 14.3 (13.7, 16.3).
 constexpr int kMinChunk = 64;
@@ -433,6 +433,17 @@ __device__ __forceinline__ int2 tokens_of(const GradArgs& a, int v) {
         r = make_int2(0, 0);
     }
     return r;
+}
+
+// Whether the short rows of a group of `per` > 1 table rows are left to the
+// chunks too, each to the chunk that its tokens start in: the group holds more
+// than a chunk's tokens. Frequent rows are often neighbours (ids by falling
+// frequency), and their group would end last: 65536 tokens of 131072 x 1024
+// bf16 178 us so, 121 with this, of 32000 x 512 59 and 40.
+__device__ __forceinline__ bool is_heavy(const GradArgs& a, int per, long long group, int chunk) {
+    if (per == 1 || a.max_chunks == 1) return false;
+    const long long v0 = group * per, v1 = v0 + per < a.V ? v0 + per : a.V;
+    return (long long)__ldg(a.row_ptr + v1) - __ldg(a.row_ptr + v0) > chunk;
 }
 
 // The table rows whose tokens include the sorted entries i.x <= i.y <
@@ -546,6 +557,7 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
     int2 r = make_int2(0, 0);
     if (t < mine) r = tokens_of(a, (int)v0 + t);
     const bool is_long = r.y - r.x > chunk;  // left to the chunks
+    const bool heavy = is_heavy(a, per, group, chunk);
     // one list if the ranges follow each other, else (a long row, or a
     // row_ptr that is none) a list per row
     const int next = __shfl_down_sync(mask, r.x, 1, TPR);
@@ -568,6 +580,12 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
             }
         }
     };
+    if (heavy) {
+        for (unsigned none = __ballot_sync(mask, t < mine && r.x == r.y) & mask; none != 0;
+             none &= none - 1)
+            flush((__ffs(none) - 1) % TPR);
+        return;
+    }
     if (odd) {
         for (int j = 0; j < mine; ++j) {
             const int b = __shfl_sync(mask, r.x, j, TPR), e = __shfl_sync(mask, r.y, j, TPR);
@@ -618,11 +636,13 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
     for (; j < mine; ++j) flush(j);
 }
 
-// The sums of a chunk's long rows. The 8 warps are `sl` slices of 32 * VEC
-// channels times 8 / sl shares of the tokens; shares are joined in order.
+// The sums of a chunk's long rows, then its short rows of heavy groups. For a
+// long row the 8 warps are `sl` slices of 32 * VEC channels times 8 / sl shares
+// of the tokens; shares are joined in order. A short row's slices go to the
+// warps in turn.
 template <typename T, int VEC>
 __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restrict__ dy, int index,
-                                           float (*sh)[32 * VEC]) {
+                                           int per, float (*sh)[32 * VEC]) {
     constexpr int kWarps = kThreads / 32, kWidth = 32 * VEC;
     const int total = entries(a), chunk = chunk_of(a, total);
     const long long b = (long long)index * chunk;
@@ -664,6 +684,35 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
             if (share == 0 && c < a.C) store_floats<VEC>(out + c, acc);
         }
     }
+    // a heavy group holds more entries than a chunk: none lies between the
+    // groups of the chunk's first and last entry
+    const int pieces = (a.C + kWidth - 1) / kWidth;
+    int turn = 0;
+    for (int q = 0; q < 2; ++q) {
+        const int group = (q ? row.y : row.x) / per;
+        if (q && group == row.x / per) break;
+        if (!is_heavy(a, per, group, chunk)) continue;
+        const long long v0 = (long long)group * per;
+        int2 r = make_int2(0, 0);
+        if (lane < per && v0 + lane < a.V) r = tokens_of(a, (int)v0 + lane);
+        unsigned which = __ballot_sync(
+            0xffffffffu, r.x < r.y && r.y - r.x <= chunk && r.x >= p0 && r.x < p1);
+        for (; which != 0; which &= which - 1) {
+            const int j = __ffs(which) - 1;
+            const int b0 = __shfl_sync(0xffffffffu, r.x, j), e0 = __shfl_sync(0xffffffffu, r.y, j);
+            for (int p = 0; p < pieces; ++p, ++turn) {
+                if (turn % kWarps != warp) continue;
+                const int c = p * kWidth + lane * VEC;
+                float acc[VEC];
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
+                add_tokens<T, VEC, 32, 1>(a, dy, b0, e0, 1, c, 0xffffffffu, acc);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) acc[k] *= a.scale;
+                if (c < a.C) store_floats<VEC>(a.dtable + (v0 + j) * a.C + c, acc);
+            }
+        }
+    }
 }
 
 // Blocks [0, chunks): chunks; the others: groups of table rows.
@@ -678,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 3)
     pdl_wait();
     pdl_trigger();
     if ((int)blockIdx.x < chunks) {
-        chunk_role<T, VEC>(a, dy, (int)blockIdx.x, sh);
+        chunk_role<T, VEC>(a, dy, (int)blockIdx.x, per, sh);
     } else {
         int slice;
         const long long block = div32((int)blockIdx.x - chunks, slices, slice);

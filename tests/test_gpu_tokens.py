@@ -350,7 +350,9 @@ def test_embedding_sort_sizes(cap):
             assert np.array_equal(order.cpu().numpy(), od)
 
 
-@pytest.mark.parametrize("n,V,C,dtype", [(9000, 500, 45, BF), (20000, 40, 520, F)])
+@pytest.mark.parametrize("n,V,C,dtype", [
+    (9000, 500, 45, BF), (20000, 40, 520, F), (20000, 60000, 40, BF), (30000, 50000, 136, F),
+    (15000, 200000, 13, BF), (15000, 200000, 24, F), (3000, 40000, 520, BF)])
 def test_embedding_frequent_rows_side_by_side(n, V, C, dtype):
     """Low ids far more frequent than the others: most tokens belong to rows
     that are cut into pieces, several of them next to each other."""
