@@ -639,21 +639,23 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
 // The sums of a chunk's long rows, then its short rows of heavy groups. For a
 // long row the 8 warps are `sl` slices of 32 * VEC channels times 8 / sl shares
 // of the tokens; shares are joined in order. A short row's slices go to the
-// warps in turn.
+// warps in turn. Rows of more than 8 slices are `part`s of them, a block each
+// (3517 tokens of 895 x 3038 fp32 22 us, 69 by one block; 16384 of 32000 x 4096
+// bf16 117 and 139).
 template <typename T, int VEC>
 __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restrict__ dy, int index,
-                                           int per, float (*sh)[32 * VEC]) {
+                                           int part, int per, float (*sh)[32 * VEC]) {
     constexpr int kWarps = kThreads / 32, kWidth = 32 * VEC;
     const int total = entries(a), chunk = chunk_of(a, total);
     const long long b = (long long)index * chunk;
     if (b >= total) {
-        if (threadIdx.x == 0) a.starts[index] = -1;
+        if (threadIdx.x == 0 && part == 0) a.starts[index] = -1;
         return;
     }
     const int p0 = (int)b, p1 = (int)(b + chunk < total ? b + chunk : total);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int2 row = rows_at(a, make_int2(p0, p1 - 1));
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && part == 0) {
         const int2 r = tokens_of(a, row.y);
         a.starts[index] = r.y - r.x > chunk && r.x >= p0 ? row.y : -1;
     }
@@ -664,29 +666,27 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
         const int2 r = tokens_of(a, slot ? row.y : row.x);
         if (r.y - r.x <= chunk) continue;
         float* const out = a.part + (2ll * index + slot) * a.C;
-        for (int s0 = 0; s0 < a.C; s0 += sl * kWidth) {
-            const int c = s0 + warp % sl * kWidth + lane * VEC;
-            float acc[VEC];
+        const int c = (part * sl + warp % sl) * kWidth + lane * VEC;
+        float acc[VEC];
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
-            add_tokens<T, VEC, 32, 1>(a, dy, max(r.x, p0) + share, min(r.y, p1), shares, c,
-                                      0xffffffffu, acc);
-            if (shares > 1) {
-                __syncthreads();
+        for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
+        add_tokens<T, VEC, 32, 1>(a, dy, max(r.x, p0) + share, min(r.y, p1), shares, c,
+                                  0xffffffffu, acc);
+        if (shares > 1) {
+            __syncthreads();
 #pragma unroll
-                for (int v = 0; v < VEC; ++v) sh[warp][lane * VEC + v] = acc[v];
-                __syncthreads();
-                if (share == 0)
-                    for (int q = 1; q < shares; ++q)
+            for (int v = 0; v < VEC; ++v) sh[warp][lane * VEC + v] = acc[v];
+            __syncthreads();
+            if (share == 0)
+                for (int q = 1; q < shares; ++q)
 #pragma unroll
-                        for (int v = 0; v < VEC; ++v) acc[v] += sh[warp + q * sl][lane * VEC + v];
-            }
-            if (share == 0 && c < a.C) store_floats<VEC>(out + c, acc);
+                    for (int v = 0; v < VEC; ++v) acc[v] += sh[warp + q * sl][lane * VEC + v];
         }
+        if (share == 0 && c < a.C) store_floats<VEC>(out + c, acc);
     }
     // a heavy group holds more entries than a chunk: none lies between the
     // groups of the chunk's first and last entry
-    const int pieces = (a.C + kWidth - 1) / kWidth;
+    const int from = part * kWarps, pieces = min((a.C + kWidth - 1) / kWidth, from + kWarps);
     int turn = 0;
     for (int q = 0; q < 2; ++q) {
         const int group = (q ? row.y : row.x) / per;
@@ -700,7 +700,7 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
         for (; which != 0; which &= which - 1) {
             const int j = __ffs(which) - 1;
             const int b0 = __shfl_sync(0xffffffffu, r.x, j), e0 = __shfl_sync(0xffffffffu, r.y, j);
-            for (int p = 0; p < pieces; ++p, ++turn) {
+            for (int p = from; p < pieces; ++p, ++turn) {
                 if (turn % kWarps != warp) continue;
                 const int c = p * kWidth + lane * VEC;
                 float acc[VEC];
@@ -715,22 +715,24 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
     }
 }
 
-// Blocks [0, chunks): chunks; the others: groups of table rows.
+// Blocks [0, chunks * parts): chunks; the others: groups of table rows.
 // Three blocks an SM: with fewer registers a thread and 256 channels a group
 // the 131072 x 1024 bf16 table of 65536 tokens took 135 us, with 512 channels
 // and two blocks 147 us (loads in flight per warp against warps).
 template <typename T, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(kThreads, 3)
-    embed_bwd_kernel(const GradArgs a, const T* __restrict__ dy, int chunks, int slices,
-                     int per) {
+    embed_bwd_kernel(const GradArgs a, const T* __restrict__ dy, int chunks, int parts,
+                     int slices, int per) {
     __shared__ float sh[kThreads / 32][32 * VEC];
     pdl_wait();
     pdl_trigger();
-    if ((int)blockIdx.x < chunks) {
-        chunk_role<T, VEC>(a, dy, (int)blockIdx.x, per, sh);
+    if ((int)blockIdx.x < chunks * parts) {
+        int part;
+        const int index = div32((int)blockIdx.x, parts, part);
+        chunk_role<T, VEC>(a, dy, index, part, per, sh);
     } else {
         int slice;
-        const long long block = div32((int)blockIdx.x - chunks, slices, slice);
+        const long long block = div32((int)blockIdx.x - chunks * parts, slices, slice);
         rows_role<T, VEC, TPR, NV>(a, dy, per, block * (kThreads / TPR) + threadIdx.x / TPR, slice);
     }
 }
@@ -886,14 +888,16 @@ hc_status bwd(const DeviceCtx* ctx, const GradArgs& a, const void* dy, cudaStrea
     const int most = TPR < kMaxPer ? TPR : kMaxPer;
     per = per < 1 ? 1 : per > most ? most : per;
     const long long blocks = (a.V + per * (kThreads / TPR) - 1) / (per * (kThreads / TPR));
-    const long long grid = blocks * slices + chunks;
+    constexpr int kPart = kThreads * VEC;  // channels of a chunk's block
+    const int parts = (int)(((long long)a.C + kPart - 1) / kPart);
+    const long long grid = blocks * slices + (long long)chunks * parts;
     if (grid > 0x7fffffffll) {
         set_error("hc_embedding_bwd: V=%d C=%d is too large", a.V, a.C);
         return HC_ERR_UNSUPPORTED;
     }
     hc_status st = launch_pdl(embed_bwd_kernel<T, VEC, TPR, NV>, dim3((unsigned)grid),
                               dim3(kThreads), 0, s, "embed_bwd_kernel", a, (const T*)dy, chunks,
-                              slices, (int)per);
+                              parts, slices, (int)per);
     if (st != HC_OK || chunks == 0) return st;
     return launch_pdl(embed_bwd_join_kernel<VEC>,
                       dim3((unsigned)((a.C + 32 * VEC - 1) / (32 * VEC)), (unsigned)chunks),
