@@ -590,8 +590,9 @@ hc_status hc_quantize_fp8_weight(const void* W, hc_dtype dt, int C_in, int C_out
  *   wq, ws    as hc_quantize_fp8_weight wrote them
  *   bias      [C_out] fp32, or NULL for zero
  *   y         [capacity, C_out] of dtype y_dt
- * Sums in fp32: a block's products are added in the tensor cores'
- * accumulators, the scaled block sums in registers.
+ * A NaN stays one behind either activation. Sums in fp32: a block's products
+ * are added in the tensor cores' accumulators, the scaled block sums in
+ * registers.
  */
 hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* count, int capacity,
                             int C_in, int C_out, const uint8_t* wq, const float* ws,

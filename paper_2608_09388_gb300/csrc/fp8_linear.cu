@@ -228,6 +228,20 @@ struct Act {
     static constexpr int value = kAct;
 };
 
+// Activation of an output. A NaN stays one: it marks a row whose 8-bit form
+// holds a NaN or an infinity (fmaxf would make a zero of it).
+template <int kAct>
+__device__ __forceinline__ float activate(float z) {
+    if (kAct == HC_ACT_ELU) return z > 0.f ? z : __expf(z) - 1.f;
+    if (kAct == HC_ACT_RELU) return z < 0.f ? 0.f : z;
+    return z;
+}
+__device__ __forceinline__ float activate(float z, int act) {
+    if (act == HC_ACT_ELU) return activate<HC_ACT_ELU>(z);
+    if (act == HC_ACT_RELU) return activate<HC_ACT_RELU>(z);
+    return z;
+}
+
 // Bias, activation and store of a warp's 32 rows (one per lane, from row r0
 // on) x kCols channels from o0 on. 64 bytes of every row at a time go through
 // the warp's staging buffer (16-byte pieces swizzled so that neither side has
@@ -250,10 +264,10 @@ __device__ __forceinline__ void store_tile(const float (&acc)[kCols], const floa
             for (int i = 0; i < kV; i += 4) {
                 const int j = p + q * kV + i;
                 const float4 b = *reinterpret_cast<const float4*>(bias + j);
-                f[i] = act_fixed<kAct>(acc[j] + b.x);
-                f[i + 1] = act_fixed<kAct>(acc[j + 1] + b.y);
-                f[i + 2] = act_fixed<kAct>(acc[j + 2] + b.z);
-                f[i + 3] = act_fixed<kAct>(acc[j + 3] + b.w);
+                f[i] = activate<kAct>(acc[j] + b.x);
+                f[i + 1] = activate<kAct>(acc[j + 1] + b.y);
+                f[i + 2] = activate<kAct>(acc[j + 2] + b.z);
+                f[i + 3] = activate<kAct>(acc[j + 3] + b.w);
             }
             Piece<T, kV> w;
             w.set_all(f);
@@ -558,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
                     for (int j = 0; j < C::kCols; ++j) {
                         const long long nn = (long long)m * BN + half * C::kCols + j;
                         if (nn < rows)
-                            y[nn * a.C_out + o] = from_f32<T>(act_apply(acc[j] + bias, a.act));
+                            y[nn * a.C_out + o] = from_f32<T>(activate(acc[j] + bias, a.act));
                     }
                 }
             } else {
@@ -597,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
                         v += lds_cluster_f32(base + (uint32_t)((col * kLanes + ln) * 4), (uint32_t)r);
                     const long long nn = (long long)m * BN + col;
                     if (nn < rows && o < a.C_out)
-                        y[nn * a.C_out + o] = from_f32<T>(act_apply(v + bias, a.act));
+                        y[nn * a.C_out + o] = from_f32<T>(activate(v + bias, a.act));
                 }
             } else {
                 // a share of the tokens each, a warp per token, 4 channels per lane
@@ -620,8 +634,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
                             v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
                         }
                         if (nn >= rows) continue;
-                        const float w[4] = {act_apply(v.x + bias[0], a.act), act_apply(v.y + bias[1], a.act),
-                                            act_apply(v.z + bias[2], a.act), act_apply(v.w + bias[3], a.act)};
+                        const float w[4] = {activate(v.x + bias[0], a.act), activate(v.y + bias[1], a.act),
+                                            activate(v.z + bias[2], a.act), activate(v.w + bias[3], a.act)};
                         T* const yr = y + nn * a.C_out + o;
                         if (wide && o < a.C_out) {
                             if constexpr (sizeof(T) == 4)

@@ -1,0 +1,78 @@
+"""The token operators on values at the edge of their arithmetic: what an
+activation does with NaN and with values near zero, rows without a spread,
+rows with a NaN in a ragged block. Bounds as in test_gpu_tokens.py: U = 2^-24
+is the unit roundoff of fp32, a bf16 result is rounded once more by at most
+2^-8 of its value."""
+import pytest
+
+from paper_2608_09388_gb300 import hc
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+U = 2.0 ** -24
+BF, F, D64 = torch.bfloat16, torch.float32, torch.float64
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_09388_gb300 import build
+    build.build()
+    hc.load_library()
+    assert hc.hc_get_device_status() == hc.HC_OK
+
+
+@pytest.fixture(autouse=True)
+def _status_clean():
+    yield
+    assert hc.hc_get_device_status() == hc.HC_OK
+
+
+def randn(seed, *shape, dtype=F):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, device="cuda").to(dtype)
+
+
+def quantise(x):
+    n, K = x.shape
+    q = torch.full((n, hc.HC_FP8_PITCH(K)), 0x55, dtype=torch.uint8, device="cuda")
+    s = torch.full(((K + 127) // 128, n), 77.0, device="cuda")
+    hc.hc_quantize_fp8_rows(x, q, s)
+    return q, s
+
+
+def quantise_weight(W):
+    K, N = W.shape
+    q = torch.full((N, hc.HC_FP8_PITCH(K)), 0x55, dtype=torch.uint8, device="cuda")
+    s = torch.full(((N + 127) // 128, (K + 127) // 128), 77.0, device="cuda")
+    hc.hc_quantize_fp8_weight(W, q, s)
+    return q, s
+
+
+# The four ways a tile leaves the 8-bit product: tokens or channels on the
+# lanes, the channel blocks by one CTA (K below 512: fewer than four blocks) or
+# joined over a cluster; and tokens on the lanes with 256 channels a tile.
+EPILOGUES = [(300, 136, 200), (128, 1024, 256), (5, 136, 200), (40, 136, 70), (5, 1024, 200),
+             (2400, 392, 2000)]
+
+
+@pytest.mark.parametrize("out", [BF, F])
+@pytest.mark.parametrize("n,K,N", EPILOGUES)
+@pytest.mark.parametrize("act", [hc.HC_ACT_NONE, hc.HC_ACT_ELU, hc.HC_ACT_RELU])
+def test_linear_keeps_nan(n, K, N, act, out):
+    """Every output of a row that holds a NaN or an infinity is NaN, behind an
+    activation too, and no other row's is."""
+    x = randn(n, n, K)
+    x[1, 3], x[2, K - 1], x[n - 2, 0] = float("nan"), float("inf"), float("-inf")
+    q, s = quantise(x)
+    w, ws = quantise_weight(randn(K, K, N))
+    y = torch.empty(n, N, dtype=out, device="cuda")
+    hc.hc_fp8_linear_fwd(q, s, w, ws, randn(N, N), act, y)
+    bad = torch.zeros(n, dtype=torch.bool, device="cuda")
+    bad[[1, 2, n - 2]] = True
+    assert y[bad].isnan().all()
+    assert y[~bad].isfinite().all()
