@@ -229,10 +229,22 @@ struct Act {
 };
 
 // Activation of an output. A NaN stays one: it marks a row whose 8-bit form
-// holds a NaN or an infinity (fmaxf would make a zero of it).
+// holds a NaN or an infinity (fmaxf would make a zero of it). ELU's exp(z) - 1
+// is taken from the fast exponential where z < -1/8: its two units in the last
+// place are there at most 18 * 2^-24 of the difference. Nearer to zero, where
+// nothing of a small z would be left, from the first five terms of its series (the sixth is
+// below 2^-24 of the sum). 16384 x 640 x 4096 105 us so, with expm1f 195, 96
+// with the exponential alone.
 template <int kAct>
 __device__ __forceinline__ float activate(float z) {
-    if (kAct == HC_ACT_ELU) return z > 0.f ? z : __expf(z) - 1.f;
+    if (kAct == HC_ACT_ELU) {
+        float p = fmaf(z, 1.f / 120.f, 1.f / 24.f);
+        p = fmaf(z, p, 1.f / 6.f);
+        p = fmaf(z, p, 0.5f);
+        p = fmaf(z * z, p, z);
+        p = z < -0.125f ? __expf(z) - 1.f : p;
+        return z > 0.f ? z : p;
+    }
     if (kAct == HC_ACT_RELU) return z < 0.f ? 0.f : z;
     return z;
 }

@@ -76,3 +76,28 @@ def test_linear_keeps_nan(n, K, N, act, out):
     bad[[1, 2, n - 2]] = True
     assert y[bad].isnan().all()
     assert y[~bad].isfinite().all()
+
+
+@pytest.mark.parametrize("out", [BF, F])
+@pytest.mark.parametrize("n,K,N", EPILOGUES)
+def test_linear_elu_near_zero(n, K, N, out):
+    """ELU of small negative sums keeps their leading bits. All products have
+    one sign, so the sum's bound (128 products a block and the scaled block
+    sums, each addition off by at most 2 U) is relative to the sum; ELU's slope
+    is at most 1, and its exponential minus one is off by at most 20 U of the
+    result (two units in the last place of a fast exponential below exp(-1/8),
+    against 1 - exp(-1/8))."""
+    x = randn(n, n, K).abs() * torch.logspace(-9, 1, n, device="cuda")[:, None]
+    q, s = quantise(x)
+    w, ws = quantise_weight(-randn(K, K, N).abs() * K ** -0.5)
+    y = torch.empty(n, N, dtype=out, device="cuda")
+    hc.hc_fp8_linear_fwd(q, s, w, ws, None, hc.HC_ACT_ELU, y)
+    xv = q.view(torch.float8_e4m3fn).to(D64)[:, :K] * s.to(D64).t().repeat_interleave(128, 1)[:, :K]
+    wv = w.view(torch.float8_e4m3fn).to(D64)[:, :K] \
+        * ws.to(D64).repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K]
+    z = xv @ wv.t()
+    ref = torch.expm1(z)
+    tol = (2 * 128 + 2 * (K // 128 + 1) + 8) * U * z.abs() + 20 * U * ref.abs() \
+        + (2.0 ** -8 if out == BF else U) * ref.abs()
+    bad = (y.to(D64) - ref).abs() > tol
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off"
