@@ -82,7 +82,10 @@ typedef enum {
  * kept until process exit. Make the first call on each device and stream
  * outside stream capture; later calls allocate nothing unless a larger mask
  * is seen. Calls on one stream are ordered; calls on different streams use
- * different workspaces.
+ * different workspaces. All operators share a stream's workspace: a call that
+ * needs a larger one synchronises the stream and replaces it. A workspace that
+ * was in use during a capture then stays allocated beside the new one, so a
+ * graph may be replayed after larger calls on its stream.
  */
 hc_status hc_mask_compact(const uint8_t* mask, int B, int V, int32_t* coords,
                           int32_t* row_of, int32_t* batch_offsets, int32_t* count,

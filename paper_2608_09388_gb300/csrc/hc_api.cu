@@ -73,6 +73,7 @@ const DeviceCtx* device_ctx() {
 struct Workspace {
     void* ptr = nullptr;
     size_t bytes = 0;
+    bool captured = false;  // handed out while the stream was being captured
 };
 static std::map<std::pair<int, cudaStream_t>, Workspace> g_ws;
 static std::mutex g_ws_mutex;
@@ -80,22 +81,30 @@ static std::mutex g_ws_mutex;
 void* stream_workspace(cudaStream_t s, size_t bytes) {
     int dev = -1;
     if (check_cuda(cudaGetDevice(&dev), "cudaGetDevice") != HC_OK) return nullptr;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (check_cuda(cudaStreamIsCapturing(s, &capture), "cudaStreamIsCapturing") != HC_OK)
+        return nullptr;
     std::lock_guard<std::mutex> lock(g_ws_mutex);
     Workspace& w = g_ws[std::make_pair(dev, s)];
-    if (w.bytes >= bytes) return w.ptr;
-    size_t want = bytes < 4096 ? 4096 : bytes;
-    if (w.ptr) {
-        // The old buffer may still be read by work queued on this stream.
-        if (check_cuda(cudaStreamSynchronize(s), "cudaStreamSynchronize") != HC_OK) return nullptr;
-        cudaFree(w.ptr);
-        w.ptr = nullptr;
-        w.bytes = 0;
+    if (w.bytes < bytes) {
+        // The old buffer may still be read by work queued on this stream. One whose
+        // address a captured graph holds stays allocated until exit: the graph may be
+        // replayed at any time.
+        if (w.ptr && !w.captured) {
+            if (check_cuda(cudaStreamSynchronize(s), "cudaStreamSynchronize") != HC_OK)
+                return nullptr;
+            cudaFree(w.ptr);
+            w = Workspace{};
+        }
+        const size_t want = bytes < 4096 ? 4096 : bytes;
+        void* p = nullptr;
+        if (check_cuda(cudaMalloc(&p, want), "cudaMalloc(workspace)") != HC_OK) return nullptr;
+        w.ptr = p;
+        w.bytes = want;
+        w.captured = false;
     }
-    void* p = nullptr;
-    if (check_cuda(cudaMalloc(&p, want), "cudaMalloc(workspace)") != HC_OK) return nullptr;
-    w.ptr = p;
-    w.bytes = want;
-    return p;
+    w.captured = w.captured || capture != cudaStreamCaptureStatusNone;
+    return w.ptr;
 }
 
 static bool misaligned(const void* p, size_t a) {

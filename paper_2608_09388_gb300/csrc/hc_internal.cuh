@@ -49,7 +49,8 @@ const DeviceCtx* device_ctx();
 void set_error(const char* fmt, ...);
 hc_status check_cuda(cudaError_t e, const char* what);
 // Per-(device, stream) scratch of at least `bytes`, grown on demand and kept
-// until exit. nullptr after recording an error.
+// until exit; a buffer that was handed out during a stream capture is never
+// freed, so that its graph stays valid. nullptr after recording an error.
 void* stream_workspace(cudaStream_t s, size_t bytes);
 
 // ------------------------------------------------------------ operator modes
