@@ -86,6 +86,8 @@ typedef enum {
  * needs a larger one synchronises the stream and replaces it. A workspace that
  * was in use during a capture then stays allocated beside the new one, so a
  * graph may be replayed after larger calls on its stream.
+ * A call holds its stream's workspace until its last launch: calls of several
+ * threads on one stream follow each other whole.
  */
 hc_status hc_mask_compact(const uint8_t* mask, int B, int V, int32_t* coords,
                           int32_t* row_of, int32_t* batch_offsets, int32_t* count,

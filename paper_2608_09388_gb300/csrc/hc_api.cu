@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <atomic>
+#include <exception>
 #include <map>
 #include <mutex>
 #include <utility>
@@ -70,41 +71,62 @@ const DeviceCtx* device_ctx() {
     return &g_ctx[dev];
 }
 
-struct Workspace {
+struct StreamScratch {
+    // held by a call from before it asks for the buffer until its last launch
+    std::recursive_mutex in_use;
     void* ptr = nullptr;
     size_t bytes = 0;
     bool captured = false;  // handed out while the stream was being captured
 };
-static std::map<std::pair<int, cudaStream_t>, Workspace> g_ws;
-static std::mutex g_ws_mutex;
+static std::map<std::pair<int, cudaStream_t>, StreamScratch> g_scratch;
+static std::mutex g_scratch_mutex;
 
-void* stream_workspace(cudaStream_t s, size_t bytes) {
+// Entries stay where they are until exit. nullptr after recording an error.
+static StreamScratch* scratch_of(cudaStream_t s) {
     int dev = -1;
     if (check_cuda(cudaGetDevice(&dev), "cudaGetDevice") != HC_OK) return nullptr;
+    try {
+        std::lock_guard<std::mutex> lock(g_scratch_mutex);
+        return &g_scratch[std::make_pair(dev, s)];
+    } catch (const std::exception& e) {
+        set_error("workspace: %s", e.what());
+        return nullptr;
+    }
+}
+
+StreamLock::StreamLock(cudaStream_t s) : scratch_(scratch_of(s)) {
+    if (scratch_) scratch_->in_use.lock();
+}
+StreamLock::~StreamLock() {
+    if (scratch_) scratch_->in_use.unlock();
+}
+
+void* stream_workspace(cudaStream_t s, size_t bytes) {
+    StreamScratch* const w = scratch_of(s);
+    if (!w) return nullptr;
     cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
     if (check_cuda(cudaStreamIsCapturing(s, &capture), "cudaStreamIsCapturing") != HC_OK)
         return nullptr;
-    std::lock_guard<std::mutex> lock(g_ws_mutex);
-    Workspace& w = g_ws[std::make_pair(dev, s)];
-    if (w.bytes < bytes) {
+    if (w->bytes < bytes) {
         // The old buffer may still be read by work queued on this stream. One whose
         // address a captured graph holds stays allocated until exit: the graph may be
         // replayed at any time.
-        if (w.ptr && !w.captured) {
+        if (w->ptr && !w->captured) {
             if (check_cuda(cudaStreamSynchronize(s), "cudaStreamSynchronize") != HC_OK)
                 return nullptr;
-            cudaFree(w.ptr);
-            w = Workspace{};
+            cudaFree(w->ptr);
+            w->ptr = nullptr;
+            w->bytes = 0;
         }
         const size_t want = bytes < 4096 ? 4096 : bytes;
         void* p = nullptr;
         if (check_cuda(cudaMalloc(&p, want), "cudaMalloc(workspace)") != HC_OK) return nullptr;
-        w.ptr = p;
-        w.bytes = want;
-        w.captured = false;
+        w->ptr = p;
+        w->bytes = want;
+        w->captured = false;
     }
-    w.captured = w.captured || capture != cudaStreamCaptureStatusNone;
-    return w.ptr;
+    w->captured = w->captured || capture != cudaStreamCaptureStatusNone;
+    return w->ptr;
 }
 
 static bool misaligned(const void* p, size_t a) {
@@ -115,6 +137,7 @@ static bool misaligned(const void* p, size_t a) {
 // CUDA cores otherwise.
 hc_status dispatch_conv(const DeviceCtx* ctx, ConvArgs& a, hc_dtype dt, cudaStream_t s) {
     a.status = ctx->status;
+    StreamLock lock(s);
     if (conv_tc_supported(a, dt)) {
         if (const size_t pb = conv_tc_pad_bytes(a)) {
             a.pad_ws = stream_workspace(s, pb);
@@ -157,6 +180,7 @@ hc_status hc_mask_compact(const uint8_t* mask, int B, int V, int32_t* coords, in
                "hc_mask_compact: mask and coords are required");
     const DeviceCtx* ctx = device_ctx();
     if (!ctx) return HC_ERR_CUDA;
+    StreamLock lock((cudaStream_t)stream);
     return launch_compact(ctx, mask, B, V, coords, row_of, batch_offsets, count,
                           (cudaStream_t)stream);
 }
@@ -327,6 +351,7 @@ hc_status hc_mask_compact_rulebook(const uint8_t* mask, int B, int V, const int3
     const DeviceCtx* ctx = device_ctx();
     if (!ctx) return HC_ERR_CUDA;
     const cudaStream_t s = (cudaStream_t)stream;
+    StreamLock lock(s);
     if ((long long)B * V > 0 && compact_map_supported(B, V, L))
         return launch_compact_map(ctx, mask, B, V, spiral, L, (int)x_layout, coords, row_of,
                                   batch_offsets, count, rulebook, s);
@@ -426,6 +451,7 @@ hc_status hc_sparse_group_norm_fwd(const void* x, hc_dtype dt, const int32_t* ba
     HC_REQUIRE(!misaligned(x, eb) && !misaligned(y, eb), "%s: misaligned x/y", fn);
     const DeviceCtx* ctx = device_ctx();
     if (!ctx) return HC_ERR_CUDA;
+    StreamLock lock((cudaStream_t)stream);
     return launch_group_norm(ctx, x, dt, batch_offsets, B, capacity, C, G, eps, gamma, beta,
                              (int)act, y, (cudaStream_t)stream);
 }
@@ -469,6 +495,7 @@ hc_status hc_sparse_conv_gn_fwd(const void* x, hc_dtype dt, int x_rows, const in
     a.mode = kRulebook;
     a.act = HC_ACT_NONE;  // the activation follows the normalisation
     a.status = ctx->status;
+    StreamLock lock(s);
     const int cpg = C_out / G;
     // channels per group a power of two from 8 to the tile's width
     if (conv_tc_supported(a, dt) && cpg >= 8 && (cpg & (cpg - 1)) == 0 && cpg <= conv_tc_tile_n(a) &&
@@ -518,6 +545,7 @@ hc_status hc_conv_rulebook_transpose(const int32_t* rulebook, const int32_t* cou
     if (x_rows == 0)
         return check_cuda(cudaMemsetAsync(row_ptr, 0, sizeof(int32_t), (cudaStream_t)stream),
                           "cudaMemsetAsync(row_ptr)");
+    StreamLock lock((cudaStream_t)stream);
     return launch_rulebook_transpose(ctx, rulebook, count, capacity, L, x_rows, row_ptr, taps,
                                      (cudaStream_t)stream);
 }
@@ -584,6 +612,7 @@ hc_status hc_sparse_conv_rulebook_bwd(const void* x, hc_dtype dt, int x_rows,
     b.dx = x_rows > 0 ? dx : nullptr;
     b.dW = dW;
     b.dbias = dbias;
+    StreamLock lock(s);
     return launch_conv_bwd(ctx, b, s);
 }
 
@@ -604,6 +633,7 @@ hc_status hc_mask_score_update(const void* O, hc_dtype dt, int K, int N, int D,
     HC_REQUIRE(!misaligned(O, dt == HC_F32 ? 4 : 2), "%s: misaligned O", fn);
     const DeviceCtx* ctx = device_ctx();
     if (!ctx) return HC_ERR_CUDA;
+    StreamLock lock((cudaStream_t)stream);
     return launch_mask_score(ctx, O, dt, K, N, D, alpha_in, alpha_out, sim, (cudaStream_t)stream);
 }
 
@@ -752,6 +782,7 @@ hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const in
     a.dx = dx;
     a.dgamma = dgamma;
     a.dbeta = dbeta;
+    StreamLock lock((cudaStream_t)stream);
     return launch_layer_norm_bwd(ctx, a, (cudaStream_t)stream);
 }
 
@@ -797,6 +828,7 @@ hc_status hc_embedding_sort(const int32_t* ids, int ids_stride, const int32_t* c
     const DeviceCtx* ctx = device_ctx();
     if (!ctx) return HC_ERR_CUDA;
     EmbeddingArgs a{HC_F32, ids, ids_stride, count, capacity, V, 0, 0.f};
+    StreamLock lock((cudaStream_t)stream);
     return launch_embedding_sort(ctx, a, row_ptr, order, (cudaStream_t)stream);
 }
 
@@ -818,6 +850,7 @@ hc_status hc_embedding_bwd(const void* dy, hc_dtype dt, const int32_t* row_ptr,
     const DeviceCtx* ctx = device_ctx();
     if (!ctx) return HC_ERR_CUDA;
     EmbeddingArgs a{dt, nullptr, 1, nullptr, capacity, V, C, scale};
+    StreamLock lock((cudaStream_t)stream);
     return launch_embedding_bwd(ctx, a, dy, row_ptr, order, dtable, (cudaStream_t)stream);
 }
 

@@ -50,8 +50,22 @@ void set_error(const char* fmt, ...);
 hc_status check_cuda(cudaError_t e, const char* what);
 // Per-(device, stream) scratch of at least `bytes`, grown on demand and kept
 // until exit; a buffer that was handed out during a stream capture is never
-// freed, so that its graph stays valid. nullptr after recording an error.
+// freed, so that its graph stays valid. nullptr after recording an error. The
+// caller holds a StreamLock from before this call until its last launch that
+// uses the buffer: calls of other threads on the stream, whose launches would
+// come in between or who would replace the buffer, wait for it.
 void* stream_workspace(cudaStream_t s, size_t bytes);
+struct StreamScratch;
+class StreamLock {
+public:
+    explicit StreamLock(cudaStream_t s);
+    ~StreamLock();
+    StreamLock(const StreamLock&) = delete;
+    StreamLock& operator=(const StreamLock&) = delete;
+
+private:
+    StreamScratch* scratch_;
+};
 
 // ------------------------------------------------------------ operator modes
 enum RowMode : int {

@@ -1,5 +1,7 @@
 """The workspace that the operators of a stream share: a captured graph keeps
-the one it was captured with."""
+the one it was captured with, and threads that share a stream do not share it at one time."""
+import threading
+
 import pytest
 
 from paper_2608_09388_gb300 import hc
@@ -85,4 +87,37 @@ def test_graph_after_a_larger_call():
             graph.replay()
             assert same(small.result(), want[0])
         assert int(guard.count_nonzero()) == 0
+    assert hc.hc_get_device_status() == hc.HC_OK
+
+
+def test_threads_on_one_stream():
+    """Threads that call on one stream at the same time, with sizes that need
+    workspaces of different sizes: each gets its own results."""
+    steps = [Step(3000, 900, 24, 4), Step(50000, 300, 64, 5), Step(120000, 2000, 40, 6),
+             Step(20000, 70, 200, 7)]
+    want = []
+    for s in steps:
+        s.run()
+        want.append(s.result())
+        s.forget()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    start, failed = threading.Barrier(len(steps)), []
+
+    def work(s):
+        try:
+            start.wait(60)
+            for _ in range(200):
+                s.run(side)
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(s,)) for s in steps]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(120)
+    assert not failed and not any(t.is_alive() for t in threads)
+    for s, w in zip(steps, want):
+        assert same(s.result(), w)
     assert hc.hc_get_device_status() == hc.HC_OK
