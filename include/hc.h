@@ -482,7 +482,8 @@ hc_status hc_spiral_conv_fwd(const void* x, hc_dtype dt, const int32_t* spiral, 
  *   x, y      [capacity, C] of dtype dt; y may be x (in place)
  *   gamma, beta  [C] fp32, or NULL (1 / 0)
  *   mean, rstd   [capacity] fp32, or NULL: what hc_layer_norm_bwd reads
- * C >= 1, eps >= 0. With C = 1, or a constant row, and eps = 0 the row is NaN.
+ * C >= 1, eps >= 0. A row of one value (C = 1 too) has that value as its mean
+ * and y = beta exactly, whatever its size; with eps = 0 the row is NaN.
  */
 hc_status hc_layer_norm_fwd(const void* x, hc_dtype dt, const int32_t* count, int capacity, int C,
                             float eps, const float* gamma, const float* beta, void* y, float* mean,

@@ -5,7 +5,8 @@
 // and backwards, with xh = (x - mean) * rstd and g = dy * gamma:
 //   dx     = rstd * (g - sum g / C - xh * sum (g * xh) / C)
 //   dgamma = sum over rows of dy * xh,  dbeta = sum over rows of dy
-// All sums in fp32; the variance is taken around the mean. dgamma and dbeta
+// All sums in fp32; the variance is taken around the mean, which is refined
+// where it is far from zero against the row's spread. dgamma and dbeta
 // are summed per block of rows and the blocks' sums joined in a fixed order,
 // so every result is the same from run to run.
 //
@@ -13,7 +14,7 @@
 // rows and writes one. Rows of up to 8192 channels therefore stay in registers
 // between the passes over their channels, and the loads of the next rows are
 // issued before this one is reduced. At 65536 x 2048 bf16 (GB300) the forward
-// takes 89 us (79 at the copy rate) and the gradient 137 us (119), 4 us of it
+// takes 91 us (79 at the copy rate) and the gradient 137 us (119), 4 us of it
 // the joining of dgamma and dbeta; before the arithmetic went in pairs the
 // issue slots bound it (103 us).
 #include "tokens.cuh"
@@ -73,6 +74,21 @@ __device__ __forceinline__ void load_floats(const float* __restrict__ p, int c, 
     }
 }
 
+// Whether a row's mean is so far from zero, against the spread that its sum of
+// squared differences shows, that the rounding of its sum may matter: 16 times.
+// The mean of the differences is then taken off them as well. A row of one
+// value is always so unless it is zero: its differences, all alike and a few
+// units in the last place of the value, then vanish.
+__device__ __forceinline__ bool is_far(float mean, float sum2, float inv) {
+    return mean * mean >= sum2 * (256.f * inv) && mean != 0.f;
+}
+// sum / C with inv the rounded 1 / C: the product, corrected by its residual,
+// is the quotient where that is an fp32 number.
+__device__ __forceinline__ float mean_of(float sum, int C, float inv) {
+    const float q = sum * inv;
+    return fmaf(fmaf(-q, (float)C, sum), inv, q);
+}
+
 template <typename T, int VEC, int TPR, int NV>
 __global__ void __launch_bounds__(kGroupThreads)
     ln_fwd_rows_kernel(const T* x, const int32_t* count, long long capacity, int C, float eps,
@@ -93,6 +109,9 @@ __global__ void __launch_bounds__(kGroupThreads)
     using U = typename Unit::type;
     const float inv = 1.f / (float)C;
     constexpr int kAhead = kFwdAhead<T, VEC, NV>;
+    // The second look at a row that is far from zero reads it again where single
+    // elements fill the registers (keeping it spills: 32768 x 2047 bf16 230 us, 76 so).
+    constexpr bool kReread = VEC == 1;
     Piece<T, VEC> ring[kAhead][NV];
     U ga[NV][Unit::count], be[NV][Unit::count];
 #pragma unroll
@@ -128,11 +147,9 @@ __global__ void __launch_bounds__(kGroupThreads)
                 if ((i * TPR + t) * VEC < C)
 #pragma unroll
                     for (int e = 0; e < Unit::count; ++e) s = add(s, d[i][e]);
-            // the product with 1 / C, corrected by its residual: the mean of a
-            // constant row is then its value, and its differences are zero
-            const float sum = group_sum<TPR>(total(s), sh, 0);
-            float mean = sum * inv;
-            mean = fmaf(fmaf(-mean, (float)C, sum), inv, mean);
+            // a product that is not fused into the differences: they are taken from
+            // the number that is kept
+            float mean = __fmul_rn(group_sum<TPR>(total(s), sh, 0), inv);
             const U less = Unit::splat(-mean);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
@@ -142,7 +159,45 @@ __global__ void __launch_bounds__(kGroupThreads)
                         d[i][e] = add(d[i][e], less);
                         v = fma(d[i][e], d[i][e], v);
                     }
-            const float rstd = rsqrtf(fmaf(group_sum<TPR>(total(v), sh, 1), inv, eps));
+            float sum2 = group_sum<TPR>(total(v), sh, 1);
+            const bool far = n < rows && is_far(mean, sum2, inv);
+            if (TPR < 32 ? __any_sync(0xffffffffu, far) : far) {
+                s = v = Unit::splat(0.f);
+                if constexpr (kReread) {
+#pragma unroll 1
+                    for (int c = t; far && c < C; c += TPR) {
+                        Piece<T, VEC> p;
+                        p.load(x + n * C + c);
+                        s = add(s, add(p.unit(0), less));
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+                        if ((i * TPR + t) * VEC < C)
+#pragma unroll
+                            for (int e = 0; e < Unit::count; ++e) s = add(s, d[i][e]);
+                }
+                const float off = mean_of(group_sum<TPR>(total(s), sh, 0), C, inv);
+                if (far) {
+                    mean += off;
+                    const U less2 = Unit::splat(kReread ? -mean : -off);
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        const int c = (i * TPR + t) * VEC;
+                        if (c >= C) continue;
+                        Piece<T, VEC> p;
+                        if constexpr (kReread) p.load(x + n * C + c);
+#pragma unroll
+                        for (int e = 0; e < Unit::count; ++e) {
+                            d[i][e] = add(kReread ? p.unit(e) : d[i][e], less2);
+                            v = fma(d[i][e], d[i][e], v);
+                        }
+                    }
+                }
+                const float again = group_sum<TPR>(total(v), sh, 1);
+                sum2 = far ? again : sum2;
+            }
+            const float rstd = rsqrtf(fmaf(sum2, inv, eps));
             if (n >= rows) continue;
             const U times = Unit::splat(rstd);
 #pragma unroll
@@ -294,7 +349,7 @@ __global__ void __launch_bounds__(kGroupThreads)
 // ---------------------------------------------------------------- wide rows
 // A block per row; the row is read once for the mean, once for the variance
 // and once for the output (the second and third time from the caches).
-// 16384 x 16384 bf16: forward 249 us, gradient 457 (158 and 237 at the copy
+// 16384 x 16384 bf16: forward 257 us, gradient 457 (158 and 237 at the copy
 // rate; element by element 404 and 1115; forward with 256 threads 283).
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kThreads)
@@ -316,19 +371,33 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) s += p.get(e);
         }
-        const float mean = block_sum(s, sh) / (float)C;
-        float v = 0.f;
+        float mean = block_sum(s, sh) / (float)C;
+        float v;
+        for (bool again = false;; again = true) {
+            v = 0.f;
 #pragma unroll 4
-        for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
-            Piece<T, VEC> p;
-            p.load(xr + c);
+            for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+                Piece<T, VEC> p;
+                p.load(xr + c);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = p.get(e) - mean;
-                v += d * d;
+                for (int e = 0; e < VEC; ++e) {
+                    const float d = p.get(e) - mean;
+                    v += d * d;
+                }
             }
+            v = block_sum(v, sh);
+            if (again || !is_far(mean, v, 1.f / (float)C)) break;
+            s = 0.f;
+#pragma unroll 1
+            for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+                Piece<T, VEC> p;
+                p.load(xr + c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s += p.get(e) - mean;
+            }
+            mean += block_sum(s, sh) / (float)C;
         }
-        const float rstd = 1.f / sqrtf(block_sum(v, sh) / (float)C + eps);
+        const float rstd = 1.f / sqrtf(v / (float)C + eps);
         for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
             Piece<T, VEC> p;
             p.load(xr + c);
@@ -567,14 +636,14 @@ hc_status rows_in_regs(const DeviceCtx* ctx, const LayerNormArgs& a, bool back, 
 }
 
 // Rows of at most 8192 channels are held in registers (16384 x 8192 bf16:
-// forward 100 us, gradient 170; through the caches 145 and 244), by the
+// forward 104 us, gradient 170; through the caches 145 and 244), by the
 // smallest group that does so with two 16-byte pieces a thread (four for the
 // widest fp32 rows): the gradient keeps two rows' pieces, gamma and both sums
 // of every channel. Twice the threads for a row cost more than they hide
-// (65536 x 2048 bf16: 135 and 183 us against 89 and 136; 65536 x 64: 14 and 18
+// (65536 x 2048 bf16: 135 and 183 us against 91 and 136; 65536 x 64: 14 and 18
 // against 5 and 9), four pieces a thread slow the gradient (65536 x 256 bf16:
 // 48 us against 22). Rows that allow no 16-byte loads are read element by
-// element (32768 x 2047 bf16 75 and 143 us, half of 89 and 136 at 2048
+// element (32768 x 2047 bf16 75 and 143 us, half of 91 and 136 at 2048
 // channels); there the forward holds 16 elements a thread from 257 channels on
 // (8: 127 us), the gradient at most 8 (16: 252) up to 4096.
 template <typename T>

@@ -101,3 +101,51 @@ def test_linear_elu_near_zero(n, K, N, out):
         + (2.0 ** -8 if out == BF else U) * ref.abs()
     bad = (y.to(D64) - ref).abs() > tol
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off"
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("C", [1, 2, 7, 24, 131, 264, 500, 1000, 2048, 2051, 4104, 8192, 8200, 20001])
+def test_layer_norm_constant_rows(C, dtype):
+    """A row of one value has that value as its mean and no differences from
+    it, whatever the rounding of its sum: beta exactly, with the gradient's
+    xh = 0 exactly as well (dgamma = 0)."""
+    v = torch.cat([torch.tensor([0.1, 56188.883, -3.3e-3, 1e30, -7.7e-30, 0.0]),
+                   1e4 + 9e4 * torch.rand(60, generator=torch.Generator().manual_seed(C))])
+    x = v.cuda()[:, None].expand(-1, C).to(dtype).contiguous()
+    gamma, beta = 1 + randn(1, C).abs(), randn(2, C)
+    y, mean, rstd = torch.empty_like(x), torch.empty(len(v), device="cuda"), torch.empty(len(v), device="cuda")
+    hc.hc_layer_norm_fwd(x, 1e-5, gamma, beta, y, mean=mean, rstd=rstd)
+    assert torch.equal(mean, x[:, 0].float())
+    assert torch.equal(y, beta.to(dtype).expand(len(v), C))
+    dg = torch.empty(C, device="cuda")
+    hc.hc_layer_norm_bwd(x, torch.ones_like(x), gamma, mean, rstd, dgamma=dg)
+    assert (dg == 0).all()
+
+
+@pytest.mark.parametrize("C", [8, 131, 264, 2048, 2051, 8200])
+def test_layer_norm_mean_of_infinities(C):
+    """The saved mean of a row with infinities of one sign is that infinity
+    (sum x / C); the row's norm is NaN."""
+    x = randn(C, 5, C)
+    x[1, C - 1], x[2, 0], x[3, 1], x[3, 2] = float("inf"), float("-inf"), float("inf"), float("-inf")
+    y, mean, rstd = torch.empty_like(x), torch.empty(5, device="cuda"), torch.empty(5, device="cuda")
+    hc.hc_layer_norm_fwd(x, 1e-5, None, None, y, mean=mean, rstd=rstd)
+    assert mean[1] == float("inf") and mean[2] == float("-inf") and mean[3].isnan()
+    assert y[1:4].isnan().all() and rstd[1:4].isnan().all()
+    assert y[[0, 4]].isfinite().all() and mean[[0, 4]].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("C", [7, 24, 64, 131, 264, 2048, 8200])
+def test_layer_norm_rows_apart(C, dtype):
+    """A row gives the same bits beside rows far from zero as alone, and such
+    rows the same bits as alone."""
+    x = randn(C, 40, C, dtype=dtype)
+    x[1::3] = (3000 + 4 * randn(C + 1, 13, C)).to(dtype)
+    x[2::3] = 1234.5
+    y, mean, rstd = torch.empty_like(x), torch.empty(40, device="cuda"), torch.empty(40, device="cuda")
+    hc.hc_layer_norm_fwd(x, 1e-5, None, None, y, mean=mean, rstd=rstd)
+    one, m, r = torch.empty_like(x[:1]), torch.empty(1, device="cuda"), torch.empty(1, device="cuda")
+    for n in range(40):
+        hc.hc_layer_norm_fwd(x[n:n + 1].clone(), 1e-5, None, None, one, mean=m, rstd=r)
+        assert torch.equal(one[0], y[n]) and m[0] == mean[n] and r[0] == rstd[n], n
