@@ -45,6 +45,11 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
     return lo | hi << 16;
 }
 
+// The first n of a word's four bytes.
+__device__ __forceinline__ uint32_t first_bytes(int n) {
+    return n >= 4 ? 0xffffffffu : n > 0 ? (1u << 8 * n) - 1u : 0u;
+}
+
 // The e4m3 bytes of N values x / scale. With inv the rounded reciprocal,
 // x * (inv * (1 - 2^-21)) and x * (inv * (1 + 2^-21)) enclose the fp32
 // quotient (four roundings of at most 2^-24 each separate it from x * inv),
@@ -188,6 +193,15 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
                 for (int v = 0; v < V / 4; ++v) w[v] = 0u;  // beyond C
             }
+            if constexpr (kLoads == kScalar || kLoads == kWords) {
+                // a piece that holds the row's end: the zeros behind it have no
+                // quotient where the scale is a NaN
+                if (sc != sc) {
+                    const int left = C - (int)(at[k] % pitch);
+#pragma unroll
+                    for (int v = 0; v < V / 4; ++v) w[v] &= first_bytes(left - 4 * v);
+                }
+            }
             if constexpr (V == 8)
                 *reinterpret_cast<uint2*>(q + at[k]) = make_uint2(w[0], w[1]);
             else
@@ -240,8 +254,7 @@ __global__ void __launch_bounds__(kThreads)
         to_e4m3<16>(v, sc, inv, w);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int left = C_in - (i0 + k + 4 * q);  // zero from C_in on
-            if (left < 4) w[q] &= left > 0 ? (1u << 8 * left) - 1u : 0u;
+            w[q] &= first_bytes(C_in - (i0 + k + 4 * q));  // zero from C_in on
         }
         *reinterpret_cast<uint4*>(to + k) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -254,9 +267,9 @@ hc_status quant_rows(const DeviceCtx* ctx, const void* x, const int32_t* count, 
     const long long need = ((long long)capacity * nb + kPerBlock - 1) / kPerBlock;
     const long long cap = (long long)ctx->num_sms * 16;
     const uintptr_t at = reinterpret_cast<uintptr_t>(x);
-    // 16-byte loads (16384 x 8192 bf16: 81 us, 165 element by element), without a
+    // 16-byte loads (16384 x 8192 bf16: 81 us, 169 element by element), without a
     // division a block to find its row where rows hold whole blocks (98 with it);
-    // 4-byte loads of even bf16 rows (16384 x 4932: 83 us, 105 by elements)
+    // 4-byte loads of even bf16 rows (16384 x 4932: 85 us, 107 by elements)
     const bool wide = C % V == 0 && at % 16 == 0;
     auto kern = wide && C % 128 == 0 ? quant_rows_kernel<T, kFlat>
                 : wide               ? quant_rows_kernel<T, kWide>

@@ -149,3 +149,20 @@ def test_layer_norm_rows_apart(C, dtype):
     for n in range(40):
         hc.hc_layer_norm_fwd(x[n:n + 1].clone(), 1e-5, None, None, one, mean=m, rstd=r)
         assert torch.equal(one[0], y[n]) and m[0] == mean[n] and r[0] == rstd[n], n
+
+
+@pytest.mark.parametrize("dtype,C", [(F, 131), (F, 2001), (F, 300), (BF, 131), (BF, 2001),
+                                     (BF, 130), (BF, 300), (BF, 2002), (BF, 1), (F, 2)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_quantize_rows_padding_is_zero(dtype, C, value):
+    """The bytes of a row beyond C are zero, also where its last block holds a
+    NaN or an infinity (the block's channels are then not numbers, or zero)."""
+    x = randn(C, 5, C, dtype=dtype)
+    x[1, C - 1] = value
+    x[3, (C - 1) // 128 * 128] = value
+    for t in (x, torch.empty(x.numel() + 1, dtype=dtype, device="cuda")[1:].view(x.shape).copy_(x)):
+        q, s = quantise(t)
+        assert (q[:, C:] == 0).all()
+        assert not s[-1, [1, 3]].isfinite().any() and s[:, [0, 2, 4]].isfinite().all()
+        last = q[:, :C].view(torch.float8_e4m3fn).float()
+        assert last[1, C - 1].isnan() and last[3, (C - 1) // 128 * 128].isnan()
