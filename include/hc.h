@@ -470,7 +470,8 @@ hc_status hc_spiral_conv_fwd(const void* x, hc_dtype dt, const int32_t* spiral, 
  * HC_ERR_CAPACITY / HC_ERR_INVALID_INDEX reported when it was outside) or
  * NULL, which means all `capacity` rows; rows n >= N' are neither read nor
  * written. Pointers need the alignment of their element type; rows that are
- * 16-byte aligned (pointer and row size) move in 16-byte pieces. Sums are
+ * 16-byte aligned (pointer and row size) move in 16-byte pieces. Rows of more
+ * than 2^31 - 8193 channels are refused (HC_ERR_INVALID_ARG). Sums are
  * taken in fp32 and in a fixed order: results are the same from run to run.
  */
 

@@ -705,11 +705,16 @@ hc_status hc_scatter_dense(const void* y, hc_dtype dt, const int32_t* coords,
                           (cudaStream_t)stream);
 }
 
+// The kernels' int channel counters run past a row's end by less than a
+// block's stride: 512 threads of eight channels, or a slice of 1024.
+static constexpr int kMaxChannels = 0x7fffffff - 8192;
+
 // Checks shared by the token operators on [capacity, C] rows.
 static hc_status check_rows(const char* fn, hc_dtype dt, int capacity, int C) {
     HC_REQUIRE(dt == HC_F32 || dt == HC_BF16, "%s: unknown dtype %d", fn, (int)dt);
     HC_REQUIRE(capacity >= 0, "%s: capacity=%d must be >= 0", fn, capacity);
     HC_REQUIRE(C >= 1, "%s: C=%d must be >= 1", fn, C);
+    HC_REQUIRE(C <= kMaxChannels, "%s: C=%d is too large", fn, C);
     return HC_OK;
 }
 
@@ -860,7 +865,6 @@ hc_status hc_quantize_fp8_rows(const void* x, hc_dtype dt, const int32_t* count,
     t_last_error[0] = 0;
     hc_status st = check_rows(fn, dt, capacity, C);
     if (st != HC_OK) return st;
-    HC_REQUIRE(C <= 0x7fffffff - 127, "%s: C=%d is too large", fn, C);
     if (capacity == 0) return HC_OK;
     HC_REQUIRE(x && q && scales, "%s: x, q and scales are required", fn);
     HC_REQUIRE(!misaligned(x, elem_bytes(dt)) && !misaligned(scales, 4) && !misaligned(count, 4),
@@ -878,7 +882,7 @@ hc_status hc_quantize_fp8_weight(const void* W, hc_dtype dt, int C_in, int C_out
     t_last_error[0] = 0;
     HC_REQUIRE(dt == HC_F32 || dt == HC_BF16, "%s: unknown dtype %d", fn, (int)dt);
     HC_REQUIRE(C_in >= 1 && C_out >= 1, "%s: C_in=%d C_out=%d must be >= 1", fn, C_in, C_out);
-    HC_REQUIRE(C_in <= 0x7fffffff - 127 && C_out <= 0x7fffffff - 127,
+    HC_REQUIRE(C_in <= kMaxChannels && C_out <= kMaxChannels,
                "%s: C_in=%d or C_out=%d is too large", fn, C_in, C_out);
     HC_REQUIRE(W && wq && ws, "%s: W, wq and ws are required", fn);
     HC_REQUIRE(!misaligned(W, elem_bytes(dt)) && !misaligned(ws, 4), "%s: misaligned W or ws", fn);
@@ -899,7 +903,7 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
                "%s: unknown activation %d", fn, (int)act);
     HC_REQUIRE(capacity >= 0, "%s: capacity=%d must be >= 0", fn, capacity);
     HC_REQUIRE(C_in >= 1 && C_out >= 1, "%s: C_in=%d C_out=%d must be >= 1", fn, C_in, C_out);
-    HC_REQUIRE(C_in <= 0x7fffffff - 127 && C_out <= 0x7fffffff - 127,
+    HC_REQUIRE(C_in <= kMaxChannels && C_out <= kMaxChannels,
                "%s: C_in=%d or C_out=%d is too large", fn, C_in, C_out);
     if (capacity == 0) return HC_OK;
     HC_REQUIRE(xq && xs && wq && ws && y, "%s: xq, xs, wq, ws and y are required", fn);
