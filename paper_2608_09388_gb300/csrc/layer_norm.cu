@@ -527,15 +527,15 @@ __global__ void __launch_bounds__(kGradWarps * 32)
     pdl_wait();
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int c = blockIdx.x * 32 + lane;  // of the 2 * C sums of a part
+    const long long c = blockIdx.x * 32ll + lane;  // of the 2 * C sums of a part
     float v = 0.f;
-    if (c < 2 * C) {
+    if (c < 2ll * C) {
 #pragma unroll 8
         for (int p = warp; p < parts; p += kGradWarps) v += part[2ll * p * C + c];
     }
     sh[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && c < 2 * C) {
+    if (warp == 0 && c < 2ll * C) {
         v = 0.f;
 #pragma unroll
         for (int w = 0; w < kGradWarps; ++w) v += sh[w][lane];
