@@ -721,9 +721,9 @@ hc_status launch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
     if (st != HC_OK) return st;
     st = encode(&mw, a.wq, a.C_out, a.pitch, kSwap ? kLanes : BN);
     if (st != HC_OK) return st;
-    const long long tiles =
-        (long long)((a.capacity + (kSwap ? BN : kLanes) - 1) / (kSwap ? BN : kLanes)) *
-        ((a.C_out + (kSwap ? kLanes : BN) - 1) / (kSwap ? kLanes : BN));
+    constexpr int kTileRows = kSwap ? BN : kLanes, kTileOut = kSwap ? kLanes : BN;
+    const long long tiles = (((long long)a.capacity + kTileRows - 1) / kTileRows) *
+                            (((long long)a.C_out + kTileOut - 1) / kTileOut);
     // Split while every CTA still gets an SM (or half) of its own and two blocks
     // or more: 1 x 8192 x 8192 takes 13.5 us, unsplit 22. Clusters of 8 find room
     // late unless they leave half of it free: 128 x 2048 x 2048 (16 tiles) 14.0
@@ -764,7 +764,7 @@ hc_status dispatch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s)
     // A tile of 256 output channels takes 1.6 times as long as one of 128 (one
     // wave of each, 1024 x 4096 x 4096: 17.4 us against 22.1 for two waves of
     // 128): the width whose waves take less.
-    const long long m = (a.capacity + kLanes - 1) / kLanes, sms = ctx->num_sms;
+    const long long m = ((long long)a.capacity + kLanes - 1) / kLanes, sms = ctx->num_sms;
     const long long waves128 = (m * ((a.C_out + 127) / 128) + sms - 1) / sms;
     const long long waves256 = (m * ((a.C_out + 255) / 256) + sms - 1) / sms;
     if (a.C_out > 128 && 8 * waves256 <= 5 * waves128) return launch<256, false, T>(ctx, a, s);

@@ -33,7 +33,26 @@ def layer_norm_wide():
     assert int((dg[3:-3] == 0).sum()) == C - 6 and int((db[3:-3] == 2).sum()) == C - 6
 
 
-CASES = [layer_norm_wide]
+def linear_rows():
+    """An 8-bit product of as many rows as an int counts: the first rows and the last
+    ones, which the others, all zero, are not."""
+    n, K, N = 2 ** 31 - 1, 16, 8
+    q = torch.zeros(n, K, dtype=torch.uint8, device="cuda")
+    s = torch.full((1, n), 0.5, device="cuda")
+    one, two = 0x38, 0x40  # e4m3
+    q[:3], q[-300:] = two, one
+    w = torch.full((N, K), one, dtype=torch.uint8, device="cuda")
+    ws = torch.full((1, 1), 2.0, device="cuda")
+    bias = torch.arange(N, device="cuda").float()
+    y = torch.full((n, N), 77.0, dtype=BF, device="cuda")
+    hc.hc_fp8_linear_fwd(q, s, w, ws, bias, hc.HC_ACT_NONE, y)
+    b = bias.to(BF)
+    assert (y[:3] == b + 32).all() and (y[-300:] == b + 16).all()
+    for at in range(3, n - 300, 2 ** 28):  # in parts: a comparison of all would take as much memory
+        assert (y[at:min(at + 2 ** 28, n - 300)] == b).all(), at
+
+
+CASES = [layer_norm_wide, linear_rows]
 
 
 @pytest.mark.parametrize("case", [c.__name__ for c in CASES])
