@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kThreads)
     pdl_trigger();
     const int rows = (int)token_rows(count, capacity, status);
     const int stride = (rows >> kSampleBits) + 1;  // sample i is keys[i * stride]
-    const int samples = (rows + stride - 1) / stride;
+    const int samples = (int)(((long long)rows + stride - 1) / stride);
     for (int i = threadIdx.x; i < samples; i += kThreads) sample[i] = keys[(long long)i * stride];
     __syncthreads();
     const long long g = blockIdx.x * (long long)kThreads + threadIdx.x;
@@ -487,8 +487,8 @@ constexpr int kAheadRows = 32 / kAheadRegs<T, VEC, NV> < 8 ? 32 / kAheadRegs<T, 
 // absent rows and channels load from row 0 and channel 0 and add zero, since
 // a load under a condition is moved down to its use, behind the one before.
 template <typename T, int VEC, int TPR, int NV>
-__device__ __forceinline__ void add_tokens(const GradArgs& a, const T* __restrict__ dy, int b, int e,
-                                           int step, int c0, unsigned mask, float (&acc)[NV * VEC]) {
+__device__ __forceinline__ void add_tokens(const GradArgs& a, const T* __restrict__ dy, long long b,
+                                           int e, int step, int c0, unsigned mask, float (&acc)[NV * VEC]) {
     constexpr int kAhead = kAheadRows<T, VEC, NV>;
     const int t = threadIdx.x % TPR;
     for (long long i0 = b; i0 < e; i0 += (long long)TPR * step) {
@@ -597,16 +597,18 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
     }
     const int b = __shfl_sync(mask, r.x, 0, TPR), e = __shfl_sync(mask, r.y, mine - 1, TPR);
     int j = 0, end = __shfl_sync(mask, r.y, 0, TPR);
-    for (int i0 = b; i0 < e; i0 += TPR) {
+    // unsigned: the step behind the last entry may pass the largest int
+    unsigned i0 = (unsigned)b;
+    for (int left = e - b; left > 0; left -= TPR, i0 += TPR) {
         int pos = -1;
-        if (i0 + t < e) {
+        if (t < left) {
             pos = __ldg(a.order + i0 + t);
             if (pos < 0 || pos >= a.capacity) {
                 report(a.status, kErrIndex);
                 pos = -1;
             }
         }
-        const int n = min(e - i0, TPR);
+        const int n = min(left, TPR);
         for (int q = 0; q < n; q += kAhead) {
             Piece<T, VEC> p[kAhead][NV];
             int at[kAhead];
@@ -623,7 +625,7 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (q + u >= n) break;
-                while (i0 + q + u >= end) {  // this token is of a later row
+                while (i0 + q + u >= (unsigned)end) {  // this token is of a later row
                     flush(j);
                     end = __shfl_sync(mask, r.y, ++j, TPR);
                 }
@@ -670,7 +672,7 @@ __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restric
         float acc[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) acc[k] = 0.f;
-        add_tokens<T, VEC, 32, 1>(a, dy, max(r.x, p0) + share, min(r.y, p1), shares, c,
+        add_tokens<T, VEC, 32, 1>(a, dy, (long long)max(r.x, p0) + share, min(r.y, p1), shares, c,
                                   0xffffffffu, acc);
         if (shares > 1) {
             __syncthreads();

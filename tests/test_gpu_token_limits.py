@@ -52,7 +52,36 @@ def linear_rows():
         assert (y[at:min(at + 2 ** 28, n - 300)] == b).all(), at
 
 
-CASES = [layer_norm_wide, linear_rows]
+def embedding_tokens():
+    """As many tokens as an int counts, nearly all of them one id: the ends of
+    the sorted entries, and of the rows' ranges, are the largest int."""
+    n, V = 2 ** 31 - 1, 5
+    ids = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ids[-61:-41], ids[-41:-21], ids[-21:-1], ids[5] = 1, 3, 4, 4
+    rp = torch.empty(V + 1, dtype=torch.int32, device="cuda")
+    od = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    hc.hc_embedding_sort(ids, V, rp, od)
+    assert rp.tolist() == [0, n - 61, n - 41, n - 41, n - 21, n]
+    last = torch.arange(n - 61, n, device="cuda")
+    assert torch.equal(od[n - 61:n - 21].long(), last[:40]) and od[n - 21] == 5
+    assert torch.equal(od[n - 20:].long(), last[40:60])
+    assert torch.equal(od[:5].long(), last[:5] - (n - 61)) and od[5] == 6 and od[n - 62] == n - 1
+    del ids
+    dy = torch.ones(n, 1, dtype=BF, device="cuda")
+    dy[-61:] = 3
+    dt = torch.full((V, 1), 77.0, device="cuda")
+    hc.hc_embedding_bwd(dy, rp, od, 0.5, dt)
+    assert dt[1:, 0].tolist() == [30.0, 0.0, 30.0, 30.5]
+    # chunks' sums are exact (below 2^24), their join is not: 1300 additions
+    assert abs(float(dt[0, 0]) - 0.5 * (n - 62 + 3)) <= 1300 * 2.0 ** -24 * n
+    y = torch.empty(n, 1, dtype=BF, device="cuda")
+    ids = torch.ones(n, dtype=torch.int32, device="cuda")
+    ids[-3:] = 2
+    hc.hc_embedding_fwd(torch.tensor([[5.0], [6.0], [7.0]], dtype=BF, device="cuda"), ids, 1.0, y)
+    assert (y[-3:] == 7).all() and y[n - 4] == 6 and int((y[:-3] == 6).sum()) == n - 3
+
+
+CASES = [layer_norm_wide, linear_rows, embedding_tokens]
 
 
 @pytest.mark.parametrize("case", [c.__name__ for c in CASES])
