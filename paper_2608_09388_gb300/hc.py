@@ -357,6 +357,11 @@ def _token_types():
     return _types
 
 
+def _too_large(*sizes):
+    """The library counts in 32 bits, and ctypes would pass the low bits of more."""
+    raise ValueError(f"sizes {sizes} must be below 2^31")
+
+
 def _arg(name, t, shape, dtypes):
     """Address of a token operator's tensor, once its shape, dtype and memory
     are what the call needs; None passes."""
@@ -377,11 +382,13 @@ def _arg_ids(ids):
     """Address and stride of a one-dimensional int32 tensor (a column of a matrix has one above 1)."""
     if ids.dim() != 1 or ids.dtype != _token_types()[1][0]:
         raise ValueError("ids must be one-dimensional int32")
-    if not ids.is_cuda:
-        raise ValueError("libhc takes device tensors")
     stride = ids.stride(0) if ids.shape[0] > 1 else 1
     if stride < 1:
         raise ValueError("ids must have a stride of at least 1")
+    if stride >> 31:
+        _too_large(stride)
+    if not ids.is_cuda:
+        raise ValueError("libhc takes device tensors")
     return ids.data_ptr(), stride
 
 
@@ -390,6 +397,8 @@ def hc_layer_norm_fwd(x, eps, gamma, beta, y, mean=None, rstd=None, count=None, 
     all rows) into y (may be x); gamma, beta fp32 [C] or None; mean, rstd fp32
     [capacity] or None."""
     capacity, C = x.shape
+    if (capacity | C) >> 31:
+        _too_large(capacity, C)
     f32, i32, _, row = _token_types()
     same = (x.dtype,)
     _check(load_library().hc_layer_norm_fwd(
@@ -404,6 +413,8 @@ def hc_layer_norm_bwd(x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None
     """Gradient of hc_layer_norm_fwd: dx like x (may be x or dy) or None; dgamma,
     dbeta fp32 [C] or None."""
     capacity, C = x.shape
+    if (capacity | C) >> 31:
+        _too_large(capacity, C)
     f32, i32, _, row = _token_types()
     same = (x.dtype,)
     _check(load_library().hc_layer_norm_bwd(
@@ -419,8 +430,10 @@ def hc_embedding_fwd(table, ids, scale, y, count=None, stream=None):
     [capacity] of any stride (coords[:, 1] for the vertex of every active row),
     y [capacity, C]."""
     V, C = table.shape
-    ptr, stride = _arg_ids(ids)
     capacity = ids.shape[0]
+    if (V | C | capacity) >> 31:
+        _too_large(V, C, capacity)
+    ptr, stride = _arg_ids(ids)
     _, i32, _, row = _token_types()
     _check(load_library().hc_embedding_fwd(
         _arg("table", table, (V, C), row), _dt(table), V, C, ptr, stride,
@@ -430,8 +443,10 @@ def hc_embedding_fwd(table, ids, scale, y, count=None, stream=None):
 
 def hc_embedding_sort(ids, V, row_ptr, order, count=None, stream=None):
     """Token positions by id, stable: row_ptr int32 [V + 1], order int32 [capacity]."""
-    ptr, stride = _arg_ids(ids)
     capacity = ids.shape[0]
+    if V >= 0 and (V | capacity) >> 31:
+        _too_large(V, capacity)
+    ptr, stride = _arg_ids(ids)
     i32 = _token_types()[1]
     _check(load_library().hc_embedding_sort(
         ptr, stride, _arg("count", count, (1,), i32), capacity, V,
@@ -444,6 +459,8 @@ def hc_embedding_bwd(dy, row_ptr, order, scale, dtable, stream=None):
     fp32 [V, C], every row written."""
     capacity, C = dy.shape
     V = dtable.shape[0]
+    if (capacity | C | V) >> 31:
+        _too_large(capacity, C, V)
     f32, i32, _, row = _token_types()
     _check(load_library().hc_embedding_bwd(
         _arg("dy", dy, (capacity, C), row), _dt(dy), _arg("row_ptr", row_ptr, (V + 1,), i32),
@@ -455,6 +472,8 @@ def hc_quantize_fp8_rows(x, q, scales, count=None, stream=None):
     """Rows of x [capacity, C] in 8 bits: q e4m3 (or uint8) [capacity,
     HC_FP8_PITCH(C)], scales fp32 [ceil(C / 128), capacity]."""
     capacity, C = x.shape
+    if (capacity | C) >> 31:
+        _too_large(capacity, C)
     f32, i32, q8, row = _token_types()
     _check(load_library().hc_quantize_fp8_rows(
         _arg("x", x, (capacity, C), row), _dt(x), _arg("count", count, (1,), i32), capacity, C,
@@ -467,6 +486,8 @@ def hc_quantize_fp8_weight(W, wq, ws, stream=None):
     """A weight W [C_in, C_out] in 8 bits, transposed: wq e4m3 (or uint8) [C_out,
     HC_FP8_PITCH(C_in)], ws fp32 [ceil(C_out / 128), ceil(C_in / 128)]."""
     C_in, C_out = W.shape
+    if (C_in | C_out) >> 31:
+        _too_large(C_in, C_out)
     f32, _, q8, row = _token_types()
     _check(load_library().hc_quantize_fp8_weight(
         _arg("W", W, (C_in, C_out), row), _dt(W), C_in, C_out,
@@ -482,6 +503,8 @@ def hc_fp8_linear_fwd(xq, xs, wq, ws, bias, act, y, count=None, stream=None):
     pitch add nothing, so the pitch stands for C_in here."""
     capacity, pitch = xq.shape
     C_out = wq.shape[0]
+    if (capacity | pitch | C_out) >> 31:
+        _too_large(capacity, pitch, C_out)
     f32, i32, q8, row = _token_types()
     nb = (pitch + 127) // 128
     _check(load_library().hc_fp8_linear_fwd(
