@@ -468,10 +468,12 @@ hc_status hc_spiral_conv_fwd(const void* x, hc_dtype dt, const int32_t* spiral, 
  * form of the linear layer) and their gradients. The paper has no counterpart.
  * In all of them `count` is N' on the device (clamped to [0, capacity],
  * HC_ERR_CAPACITY / HC_ERR_INVALID_INDEX reported when it was outside) or
- * NULL, which means all `capacity` rows; rows n >= N' are neither read nor
- * written. Pointers need the alignment of their element type; rows that are
+ * NULL, which means all `capacity` rows; rows n >= N' are not written, and
+ * what they hold has no effect (the 8-bit product copies whole tiles: it reads
+ * up to 127 of them). Pointers need the alignment of their element type; rows that are
  * 16-byte aligned (pointer and row size) move in 16-byte pieces. Rows of more
- * than 2^31 - 8193 channels are refused (HC_ERR_INVALID_ARG). Sums are
+ * than 2^31 - 8193 channels are refused (HC_ERR_INVALID_ARG), and so is a weight
+ * of more than 65535 * 128 output channels (HC_ERR_UNSUPPORTED). Sums are
  * taken in fp32 and in a fixed order: results are the same from run to run.
  */
 

@@ -643,7 +643,9 @@ __device__ __forceinline__ void rows_role(const GradArgs& a, const T* __restrict
 // of the tokens; shares are joined in order. A short row's slices go to the
 // warps in turn. Rows of more than 8 slices are `part`s of them, a block each
 // (3517 tokens of 895 x 3038 fp32 22 us, 69 by one block; 16384 of 32000 x 4096
-// bf16 117 and 139).
+// bf16 117 and 139). Where the last part is narrow it loses: its warps share the
+// slices of the whole row, not of what is left (34421 tokens of 336 x 543 bf16,
+// three parts of 256 channels, 41 us, 35 by one block).
 template <typename T, int VEC>
 __device__ __forceinline__ void chunk_role(const GradArgs& a, const T* __restrict__ dy, int index,
                                            int part, int per, float (*sh)[32 * VEC]) {

@@ -28,9 +28,9 @@
 // CTA records HC_ERR_TIMEOUT, waits for its own copies and MMAs and frees its
 // TMEM.
 //
-// Measured on a GB300: 16384 x 8192 x 8192 in 745 us (2.95 PFLOP/s, tensor pipe
-// 64% of elapsed) while the clock holds, 825 to 870 us when it runs on at the
-// 1.4 kW limit (1.6 GHz); the MMAs alone with their loads take 612 us. A tile of
+// Measured on a GB300: 16384 x 8192 x 8192 in 825 to 870 us when it runs on at
+// the 1.4 kW limit (1.6 GHz), 745 us in a burst (2.95 PFLOP/s, tensor pipe 64%
+// of elapsed); the MMAs alone with their loads take 612 us. A tile of
 // few blocks pays for its first scales and its epilogue, about 2 us (16384 x 640
 // x 4096: 69 us, 41 without the stores and what leads to them). 1 x 8192 x 8192
 // takes 14 us, 9.9 of them the weight at the copy rate.
@@ -756,8 +756,9 @@ template <typename T>
 hc_status dispatch(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s) {
     // Few tokens on the columns, the narrowest that holds them: 16 x 4096 x 4096
     // 6.2 us, 10.8 with 64 columns, 10.1 with tokens on the lanes. At 33 to 64
-    // both orientations are near: 37 x 2000 x 1001 6.2 and 7.7 us, 64 x 8192 x
-    // 8192 18.1 and 18.8, 64 x 2048 x 8192 10.2 and 9.1.
+    // it goes by the shape: 37 x 2000 x 1001 6.2 and 7.7 us, 64 x 8192 x 8192
+    // 18.1 and 18.8, but 64 x 2048 x 8192 10.2 and 9.1, 64 x 4096 x 16384 19.8
+    // and 15.6: wide outputs lose.
     if (a.capacity <= 16) return launch<16, true, T>(ctx, a, s);
     if (a.capacity <= 32) return launch<32, true, T>(ctx, a, s);
     if (a.capacity <= 64) return launch<64, true, T>(ctx, a, s);

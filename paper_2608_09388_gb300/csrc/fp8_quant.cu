@@ -213,8 +213,8 @@ __global__ void __launch_bounds__(kThreads)
 // A block per 128 x 128 block of W [C_in, C_out], written transposed: a thread
 // holds 64 channels in of one channel out, all loaded before the first is
 // used, and writes them as 64 bytes of that row. W is read once (8192 x 8192
-// bf16: 78 us, 30 at the copy rate; read twice and transposed through shared
-// memory 126).
+// bf16: 78 to 97 us, 30 at the copy rate; read twice and transposed through shared
+// memory 126; a warp's 16-byte stores go to 32 rows).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
     quant_weight_kernel(const T* __restrict__ W, int C_in, int C_out, int pitch, int nbi,
