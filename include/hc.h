@@ -85,7 +85,9 @@ typedef enum {
  * different workspaces. All operators share a stream's workspace: a call that
  * needs a larger one synchronises the stream and replaces it. A workspace that
  * was in use during a capture then stays allocated beside the new one, so a
- * graph may be replayed after larger calls on its stream.
+ * graph may be replayed after larger calls on its stream. A graph uses the
+ * workspace of the stream it was captured on, wherever it is replayed: replays
+ * of such graphs and calls on that stream must not overlap.
  * A call holds its stream's workspace until its last launch: calls of several
  * threads on one stream follow each other whole.
  */
