@@ -243,6 +243,41 @@ struct Piece<__nv_bfloat16, 8> {
     }
 };
 
+// p[c .. c + VEC), 16-byte aligned when VEC > 1, or `none` without a p.
+template <int VEC>
+__device__ __forceinline__ void load_units(const float* __restrict__ p, int c, float none,
+                                           typename UnitOf<VEC>::type (&u)[UnitOf<VEC>::count]) {
+    if constexpr (VEC == 1) {
+        u[0].v = p ? __ldg(p + c) : none;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; i += 2) {
+            const float4 f = p ? __ldg(reinterpret_cast<const float4*>(p + c + 2 * i))
+                               : make_float4(none, none, none, none);
+            u[i] = make_f2(f.x, f.y);
+            u[i + 1] = make_f2(f.z, f.w);
+        }
+    }
+}
+
+// The same as plain numbers.
+template <int VEC>
+__device__ __forceinline__ void load_floats(const float* __restrict__ p, int c, float none,
+                                            float (&f)[VEC]) {
+    typename UnitOf<VEC>::type u[UnitOf<VEC>::count];
+    load_units<VEC>(p, c, none, u);
+    if constexpr (VEC == 1) {
+        f[0] = u[0].v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) {
+            const float2 v = split(u[i]);
+            f[2 * i] = v.x;
+            f[2 * i + 1] = v.y;
+        }
+    }
+}
+
 // Sum over a group of TPR threads (a power of two; group g of the block owns
 // threads g * TPR ..), the same value in each of them. A group of several
 // warps passes the warps' sums through sh, [2][warps of the block] floats
