@@ -34,6 +34,7 @@
 #ifndef HC_H
 #define HC_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -466,8 +467,9 @@ hc_status hc_spiral_conv_fwd(const void* x, hc_dtype dt, const int32_t* spiral, 
  * Token operators
  * ---------------
  * A token is a row of a compact [capacity, C] matrix; the operators below are
- * the front of a network over such rows (row embedding, layer norm, the 8-bit
- * form of the linear layer) and their gradients. The paper has no counterpart.
+ * the parts of a network over such rows (row embedding, layer norm,
+ * root-mean-square norm with the residual's addition, the 8-bit form of the
+ * linear layer) and their gradients. The paper has no counterpart.
  * In all of them `count` is N' on the device (clamped to [0, capacity],
  * HC_ERR_CAPACITY / HC_ERR_INVALID_INDEX reported when it was outside) or
  * NULL, which means all `capacity` rows; rows n >= N' are not written, and
@@ -510,6 +512,49 @@ hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const in
                             int capacity, int C, const float* gamma, const float* mean,
                             const float* rstd, void* dx, float* dgamma, float* dbeta,
                             hc_stream_t stream);
+
+/*
+ * hc_rms_norm_fwd -- the residual's addition and the root-mean-square norm of
+ * the sum, in the rows' type and/or in 8 bits for hc_fp8_linear_fwd:
+ *   h = x + res, rounded to dt (h = x where res is NULL)
+ *   rstd = 1 / sqrt(sum h^2 / C + eps)
+ *   v = h * rstd * gamma;  y = v rounded to dt;  q, scales = the 8-bit form of
+ *   v (as hc_quantize_fp8_rows makes it of fp32 rows),  n < N'
+ *   x, res    [capacity, C] of dtype dt; res may be NULL
+ *   gamma     [C] fp32, or NULL (1)
+ *   h         [capacity, C] of dtype dt, or NULL: the residual stream after
+ *             this layer, and what hc_rms_norm_bwd reads; may be x or res
+ *   y         [capacity, C] of dtype dt, or NULL; may be x or res (h may not
+ *             be the same one)
+ *   rstd      [capacity] fp32, or NULL: for hc_rms_norm_bwd
+ *   q         [capacity, HC_FP8_PITCH(C)], 16-byte aligned, and scales
+ *             [ceil(C / 128), capacity] fp32, or both NULL
+ * One of y and q is required. C >= 1, eps >= 0. Rows whose squares would pass
+ * the range of fp32 are summed with their values scaled by a power of two. A
+ * row of zeros gives zeros; with eps = 0 it is NaN.
+ */
+hc_status hc_rms_norm_fwd(const void* x, const void* res, hc_dtype dt, const int32_t* count,
+                          int capacity, int C, float eps, const float* gamma, void* h, void* y,
+                          float* rstd, uint8_t* q, float* scales, hc_stream_t stream);
+
+/*
+ * hc_rms_norm_bwd -- its gradient. With hh = h * rstd and g = dy * gamma, over
+ * rows n < N':
+ *   dx[n][c]  = dres[n][c] + rstd * (g - hh * (sum_c g * hh) / C)
+ *   dgamma[c] = sum_n dy * hh   (0 when N' = 0)
+ * dx is the gradient of x and of res alike.
+ *   h, dy     [capacity, C] of dtype dt; rstd as the forward wrote it
+ *   dres      [capacity, C] of dtype dt: the gradient that reaches h on the
+ *             residual stream, or NULL (0)
+ *   dx        [capacity, C] of dtype dt, or NULL; may be h, dy or dres
+ *   dgamma    [C] fp32, or NULL; at least one output is required
+ * Uses the library's per-stream workspace (channel sums of 4 * C bytes for
+ * each of at most four blocks per SM; rows of more than 8192 channels: 4 bytes
+ * per row besides).
+ */
+hc_status hc_rms_norm_bwd(const void* h, const void* dy, const void* dres, hc_dtype dt,
+                          const int32_t* count, int capacity, int C, const float* gamma,
+                          const float* rstd, void* dx, float* dgamma, hc_stream_t stream);
 
 /*
  * hc_embedding_fwd -- a table row for every token:
@@ -609,6 +654,48 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
                             int C_in, int C_out, const uint8_t* wq, const float* ws,
                             const float* bias, hc_act act, hc_dtype y_dt, void* y,
                             hc_stream_t stream);
+
+/*
+ * A list of tensors of any sizes and either type, gone over as one: a table in
+ * device memory, made once for tensors that stay where they are.
+ * hc_tensor_list_fill writes the table of n tensors, hc_tensor_list_bytes(n)
+ * bytes, to host memory and fills in *list for the copy of it that the caller
+ * then makes at device_table (both 8-byte aligned); the copy has to be there
+ * before the first call with the list, and to stay. No GPU call is made.
+ *   in, out   n device addresses each, aligned to their element type; out NULL:
+ *             in place. No output may overlap another output or another
+ *             tensor's input (HC_ERR_INVALID_ARG), or its own unless it is it
+ *   numel     elements of each, 0 allowed;  dt  an hc_dtype each
+ */
+typedef struct hc_tensor_list {
+    const void* table; /* the device copy */
+    long long units;
+    int tensors;
+} hc_tensor_list;
+size_t hc_tensor_list_bytes(int n);
+hc_status hc_tensor_list_fill(const void* const* in, void* const* out, const long long* numel,
+                              const int* dt, int n, void* host_table, const void* device_table,
+                              hc_tensor_list* list);
+
+/*
+ * hc_grad_norm -- the norm over all inputs of a list:
+ *   norm = sqrt(sum over all tensors of in^2)      (one fp32; 0 for no elements)
+ * Sums behind the first 32 squares are taken in more than fp32 and in a fixed
+ * order; squares above the range of fp32 are taken in 64 bits, what is smaller
+ * than 2^-75 counts as 0. Uses the library's per-stream workspace (4096 bytes).
+ */
+hc_status hc_grad_norm(const hc_tensor_list* list, float* norm, hc_stream_t stream);
+
+/*
+ * hc_grad_clip -- the list's inputs scaled so that their norm is at most
+ * max_norm, rounded once:
+ *   out = in * (norm <= max_norm ? 1 : max_norm / norm)
+ * norm is read on the device: hc_grad_norm's, or one that a caller has combined
+ * from several. An infinite norm gives 0 (NaN where in is infinite), a NaN fills
+ * all outputs. Tensors in place whose norm is not above max_norm are not touched.
+ */
+hc_status hc_grad_clip(const hc_tensor_list* list, const float* norm, float max_norm,
+                       hc_stream_t stream);
 
 /*
  * hc_get_device_status -- synchronises `stream`, then reads and clears the

@@ -791,6 +791,79 @@ hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const in
     return launch_layer_norm_bwd(ctx, a, (cudaStream_t)stream);
 }
 
+hc_status hc_rms_norm_fwd(const void* x, const void* res, hc_dtype dt, const int32_t* count,
+                          int capacity, int C, float eps, const float* gamma, void* h, void* y,
+                          float* rstd, uint8_t* q, float* scales, hc_stream_t stream) {
+    const char* fn = "hc_rms_norm_fwd";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(eps >= 0.f, "%s: eps=%g must be >= 0", fn, (double)eps);
+    HC_REQUIRE(!q == !scales, "%s: q and scales go together", fn);
+    if (capacity == 0) return HC_OK;
+    HC_REQUIRE(x && (y || q), "%s: x and one of y and q are required", fn);
+    const size_t e = elem_bytes(dt);
+    HC_REQUIRE(!misaligned(x, e) && !misaligned(res, e) && !misaligned(h, e) && !misaligned(y, e),
+               "%s: x, res, h and y must be aligned to the element size", fn);
+    HC_REQUIRE(!misaligned(gamma, 4) && !misaligned(rstd, 4) && !misaligned(scales, 4) &&
+                   !misaligned(count, 4),
+               "%s: misaligned gamma, rstd, scales or count", fn);
+    HC_REQUIRE(!misaligned(q, 16), "%s: q must be 16-byte aligned", fn);
+    HC_REQUIRE(!h || h != y, "%s: h and y must be different buffers", fn);
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    RmsNormArgs a{};
+    a.x = x;
+    a.res = res;
+    a.dt = dt;
+    a.count = count;
+    a.capacity = capacity;
+    a.C = C;
+    a.eps = eps;
+    a.gamma = gamma;
+    a.h = h;
+    a.y = y;
+    a.rstd_out = rstd;
+    a.q = q;
+    a.scales = scales;
+    return launch_rms_norm_fwd(ctx, a, (cudaStream_t)stream);
+}
+
+hc_status hc_rms_norm_bwd(const void* h, const void* dy, const void* dres, hc_dtype dt,
+                          const int32_t* count, int capacity, int C, const float* gamma,
+                          const float* rstd, void* dx, float* dgamma, hc_stream_t stream) {
+    const char* fn = "hc_rms_norm_bwd";
+    t_last_error[0] = 0;
+    hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(dx || dgamma, "%s: at least one of dx and dgamma is required", fn);
+    HC_REQUIRE(capacity == 0 || (h && dy && rstd), "%s: h, dy and rstd are required", fn);
+    const size_t e = elem_bytes(dt);
+    HC_REQUIRE(!misaligned(h, e) && !misaligned(dy, e) && !misaligned(dres, e) &&
+                   !misaligned(dx, e),
+               "%s: h, dy, dres and dx must be aligned to the element size", fn);
+    HC_REQUIRE(!misaligned(gamma, 4) && !misaligned(rstd, 4) && !misaligned(dgamma, 4) &&
+                   !misaligned(count, 4),
+               "%s: misaligned gamma, rstd, dgamma or count", fn);
+    if (capacity == 0 && !dgamma) return HC_OK;
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    RmsNormArgs a{};
+    a.x = h;
+    a.res = dres;
+    a.dy = dy;
+    a.dt = dt;
+    a.count = count;
+    a.capacity = capacity;
+    a.C = C;
+    a.gamma = gamma;
+    a.rstd = rstd;
+    a.dx = dx;
+    a.dgamma = dgamma;
+    StreamLock lock((cudaStream_t)stream);
+    return launch_rms_norm_bwd(ctx, a, (cudaStream_t)stream);
+}
+
 static hc_status check_ids(const char* fn, const int32_t* ids, int ids_stride, int capacity,
                            int V, const int32_t* count) {
     HC_REQUIRE(V >= 0, "%s: V=%d must be >= 0", fn, V);
@@ -930,6 +1003,79 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
     a.y = y;
     a.status = ctx->status;
     return launch_fp8_linear(ctx, a, (cudaStream_t)stream);
+}
+
+size_t hc_tensor_list_bytes(int n) {
+    return n < 0 ? 0 : tensor_list_bytes(n);
+}
+
+hc_status hc_tensor_list_fill(const void* const* in, void* const* out, const long long* numel,
+                              const int* dt, int n, void* host_table, const void* device_table,
+                              hc_tensor_list* list) {
+    const char* fn = "hc_tensor_list_fill";
+    t_last_error[0] = 0;
+    HC_REQUIRE(n >= 0 && n < 0x7fffffff, "%s: n=%d must be >= 0 and < 2^31 - 1", fn, n);
+    HC_REQUIRE(host_table && device_table && list, "%s: both tables and list are required", fn);
+    HC_REQUIRE(!misaligned(host_table, 8) && !misaligned(device_table, 8),
+               "%s: tables must be 8-byte aligned", fn);
+    HC_REQUIRE(n == 0 || (in && numel && dt), "%s: in, numel and dt are required", fn);
+    long long total = 0;
+    for (int i = 0; i < n; ++i) {
+        HC_REQUIRE(dt[i] == HC_F32 || dt[i] == HC_BF16, "%s: tensor %d has unknown dtype %d", fn, i,
+                   dt[i]);
+        HC_REQUIRE(numel[i] >= 0 && numel[i] < (1ll << 48) && (total += numel[i]) < (1ll << 48),
+                   "%s: tensor %d has %lld elements", fn, i, numel[i]);
+        const size_t e = elem_bytes((hc_dtype)dt[i]);
+        HC_REQUIRE(numel[i] == 0 || (in[i] && (!out || out[i])), "%s: tensor %d is missing", fn, i);
+        HC_REQUIRE(!misaligned(in[i], e) && !(out && misaligned(out[i], e)),
+                   "%s: tensor %d is not aligned to its element size", fn, i);
+    }
+    long long units = 0;
+    int bad = 0;
+    try {
+        HC_REQUIRE(fill_tensor_list(in, out, numel, dt, n, host_table, &units, &bad),
+                   "%s: tensor %d overlaps another one's output", fn, bad);
+    } catch (const std::exception& e) {
+        set_error("%s: %s", fn, e.what());
+        return HC_ERR_CUDA;
+    }
+    list->table = device_table;
+    list->units = units;
+    list->tensors = n;
+    return HC_OK;
+}
+
+static hc_status check_list(const char* fn, const hc_tensor_list* list, const float* norm) {
+    HC_REQUIRE(list && list->table && list->tensors >= 0 && list->units >= 0,
+               "%s: a list from hc_tensor_list_fill is required", fn);
+    HC_REQUIRE(norm && !misaligned(norm, 4), "%s: norm is missing or misaligned", fn);
+    return HC_OK;
+}
+
+hc_status hc_grad_norm(const hc_tensor_list* list, float* norm, hc_stream_t stream) {
+    const char* fn = "hc_grad_norm";
+    t_last_error[0] = 0;
+    const hc_status st = check_list(fn, list, norm);
+    if (st != HC_OK) return st;
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    StreamLock lock((cudaStream_t)stream);
+    return launch_grad_norm(ctx, list->table, list->tensors, list->units, norm,
+                            (cudaStream_t)stream);
+}
+
+hc_status hc_grad_clip(const hc_tensor_list* list, const float* norm, float max_norm,
+                       hc_stream_t stream) {
+    const char* fn = "hc_grad_clip";
+    t_last_error[0] = 0;
+    const hc_status st = check_list(fn, list, norm);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(max_norm >= 0.f, "%s: max_norm=%g must be >= 0", fn, (double)max_norm);
+    if (list->units == 0) return HC_OK;
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    return launch_grad_clip(ctx, list->table, list->tensors, list->units, norm, max_norm,
+                            (cudaStream_t)stream);
 }
 
 hc_status hc_test_set_option(int option, long long value) {

@@ -193,7 +193,7 @@ hc_status launch_scatter(const DeviceCtx* ctx, const void* y, int elem_bytes, co
                          const int32_t* row_of, const int32_t* count, int B, int V, int C,
                          int zero_fill, void* out, cudaStream_t s);
 
-// Token operators on compact rows (layer_norm.cu, embedding.cu,
+// Token operators on compact rows (layer_norm.cu, rms_norm.cu, embedding.cu,
 // fp8_quant.cu, fp8_linear.cu). count NULL = all `capacity` rows.
 struct LayerNormArgs {
     const void* x;
@@ -215,6 +215,29 @@ struct LayerNormArgs {
 };
 hc_status launch_layer_norm_fwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s);
 hc_status launch_layer_norm_bwd(const DeviceCtx* ctx, const LayerNormArgs& a, cudaStream_t s);
+struct RmsNormArgs {
+    const void* x;    // forward: x; backward: the stored row h
+    const void* res;  // forward: the residual; backward: its gradient dres
+    const void* dy;
+    hc_dtype dt;
+    const int32_t* count;
+    int capacity, C;
+    float eps;
+    const float* gamma;
+    void* h;
+    void* y;
+    float* rstd_out;  // forward
+    uint8_t* q;
+    float* scales;
+    const float* rstd;  // backward
+    void* dx;
+    float* dgamma;
+};
+hc_status launch_rms_norm_fwd(const DeviceCtx* ctx, const RmsNormArgs& a, cudaStream_t s);
+hc_status launch_rms_norm_bwd(const DeviceCtx* ctx, const RmsNormArgs& a, cudaStream_t s);
+// out[c] = sum over p < parts of part[p * pitch + c], in a fixed order.
+hc_status launch_column_sum(const float* part, int parts, long long pitch, int C, float* out,
+                            cudaStream_t s);
 struct EmbeddingArgs {
     hc_dtype dt;  // of the table and y, or of dy
     const int32_t* ids;
@@ -249,6 +272,15 @@ struct Fp8LinearArgs {
     unsigned* status;
 };
 hc_status launch_fp8_linear(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s);
+
+// Lists of tensors (grad_clip.cu). fill_tensor_list may throw std::bad_alloc.
+size_t tensor_list_bytes(int n);
+bool fill_tensor_list(const void* const* in, void* const* out, const long long* numel,
+                      const int* dt, int n, void* table, long long* units, int* bad);
+hc_status launch_grad_norm(const DeviceCtx* ctx, const void* table, int n, long long units,
+                           float* norm, cudaStream_t s);
+hc_status launch_grad_clip(const DeviceCtx* ctx, const void* table, int n, long long units,
+                           const float* norm, float max_norm, cudaStream_t s);
 
 // ------------------------------------------------------------ launches
 // Every kernel of the library is launched with programmatic stream

@@ -36,9 +36,10 @@ EXPORTS = ("hc_mask_compact", "hc_mask_compact_static", "hc_sparse_spiral_conv_f
            "hc_sparse_group_norm_fwd", "hc_sparse_conv_gn_fwd", "hc_mask_score_update", "hc_mask_select_topk",
            "hc_kappa_masks", "hc_gather_rows", "hc_conv_rulebook_transpose",
            "hc_sparse_conv_rulebook_bwd", "hc_scatter_dense", "hc_spiral_conv_fwd",
-           "hc_layer_norm_fwd", "hc_layer_norm_bwd", "hc_embedding_fwd", "hc_embedding_sort",
+           "hc_layer_norm_fwd", "hc_layer_norm_bwd", "hc_rms_norm_fwd", "hc_rms_norm_bwd", "hc_embedding_fwd", "hc_embedding_sort",
            "hc_embedding_bwd", "hc_quantize_fp8_rows", "hc_quantize_fp8_weight",
-           "hc_fp8_linear_fwd", "hc_get_device_status", "hc_test_set_option",
+           "hc_fp8_linear_fwd", "hc_tensor_list_bytes", "hc_tensor_list_fill", "hc_grad_norm",
+           "hc_grad_clip", "hc_get_device_status", "hc_test_set_option",
            "hc_last_error_string", "hc_version")
 
 
@@ -88,12 +89,18 @@ def load_library(path: str | None = None):
             "hc_spiral_conv_fwd": [P, I, P, I, I, I, I, I, P, P, I, P, P],
             "hc_layer_norm_fwd": [P, I, P, I, I, ctypes.c_float, P, P, P, P, P, P],
             "hc_layer_norm_bwd": [P, P, I, P, I, I, P, P, P, P, P, P, P],
+            "hc_rms_norm_fwd": [P, P, I, P, I, I, ctypes.c_float, P, P, P, P, P, P, P],
+            "hc_rms_norm_bwd": [P, P, P, I, P, I, I, P, P, P, P, P],
             "hc_embedding_fwd": [P, I, I, I, P, I, P, I, ctypes.c_float, P, P],
             "hc_embedding_sort": [P, I, P, I, I, P, P, P],
             "hc_embedding_bwd": [P, I, P, P, I, I, I, ctypes.c_float, P, P],
             "hc_quantize_fp8_rows": [P, I, P, I, I, P, P, P],
             "hc_quantize_fp8_weight": [P, I, I, I, P, P, P],
             "hc_fp8_linear_fwd": [P, P, P, I, I, I, P, P, P, I, I, P, P],
+            "hc_tensor_list_bytes": [I],
+            "hc_tensor_list_fill": [P, P, P, P, I, P, P, P],
+            "hc_grad_norm": [P, P, P],
+            "hc_grad_clip": [P, P, ctypes.c_float, P],
             "hc_get_device_status": [P],
             "hc_test_set_option": [I, ctypes.c_longlong],
             "hc_last_error_string": [],
@@ -102,7 +109,8 @@ def load_library(path: str | None = None):
         for name, args in sig.items():
             fn = getattr(lib, name)
             fn.argtypes = args
-            fn.restype = ctypes.c_char_p if name in ("hc_last_error_string", "hc_version") else I
+            fn.restype = (ctypes.c_char_p if name in ("hc_last_error_string", "hc_version") else
+                          ctypes.c_size_t if name == "hc_tensor_list_bytes" else I)
         _lib = lib
         return lib
 
@@ -425,6 +433,43 @@ def hc_layer_norm_bwd(x, dy, gamma, mean, rstd, dx=None, dgamma=None, dbeta=None
         _arg("dbeta", dbeta, (C,), f32), _s(stream)), "hc_layer_norm_bwd")
 
 
+def hc_rms_norm_fwd(x, eps, gamma, res=None, h=None, y=None, rstd=None, q=None, scales=None,
+                    count=None, stream=None):
+    """h = x + res (rounded to their type; x alone without res), then the
+    root-mean-square norm of every row n < N' of h [capacity, C] into y and/or,
+    in 8 bits, into q [capacity, HC_FP8_PITCH(C)] and scales fp32 [ceil(C / 128),
+    capacity]; gamma fp32 [C] or None, rstd fp32 [capacity] or None. h and y may
+    each be x or res."""
+    capacity, C = x.shape
+    if (capacity | C) >> 31:
+        _too_large(capacity, C)
+    f32, i32, q8, row = _token_types()
+    same = (x.dtype,)
+    _check(load_library().hc_rms_norm_fwd(
+        _arg("x", x, (capacity, C), row), _arg("res", res, (capacity, C), same), _dt(x),
+        _arg("count", count, (1,), i32), capacity, C, eps, _arg("gamma", gamma, (C,), f32),
+        _arg("h", h, (capacity, C), same), _arg("y", y, (capacity, C), same),
+        _arg("rstd", rstd, (capacity,), f32), _arg("q", q, (capacity, HC_FP8_PITCH(C)), q8),
+        _arg("scales", scales, ((C + 127) // 128, capacity), f32), _s(stream)), "hc_rms_norm_fwd")
+
+
+def hc_rms_norm_bwd(h, dy, gamma, rstd, dres=None, dx=None, dgamma=None, count=None, stream=None):
+    """Gradient of hc_rms_norm_fwd: dx (of x and of res) like h, with dres, the
+    gradient that reaches h by itself, added; may be h, dy or dres, or None;
+    dgamma fp32 [C] or None."""
+    capacity, C = h.shape
+    if (capacity | C) >> 31:
+        _too_large(capacity, C)
+    f32, i32, _, row = _token_types()
+    same = (h.dtype,)
+    _check(load_library().hc_rms_norm_bwd(
+        _arg("h", h, (capacity, C), row), _arg("dy", dy, (capacity, C), same),
+        _arg("dres", dres, (capacity, C), same), _dt(h), _arg("count", count, (1,), i32), capacity,
+        C, _arg("gamma", gamma, (C,), f32), _arg("rstd", rstd, (capacity,), f32),
+        _arg("dx", dx, (capacity, C), same), _arg("dgamma", dgamma, (C,), f32), _s(stream)),
+        "hc_rms_norm_bwd")
+
+
 def hc_embedding_fwd(table, ids, scale, y, count=None, stream=None):
     """y[n] = scale * table[ids[n]] (zero for id -1): table [V, C], ids int32
     [capacity] of any stride (coords[:, 1] for the vertex of every active row),
@@ -513,6 +558,67 @@ def hc_fp8_linear_fwd(xq, xs, wq, ws, bias, act, y, count=None, stream=None):
         _arg("wq", wq, (C_out, pitch), q8), _arg("ws", ws, ((C_out + 127) // 128, nb), f32),
         _arg("bias", bias, (C_out,), f32), act, _dt(y), _arg("y", y, (capacity, C_out), row),
         _s(stream)), "hc_fp8_linear_fwd")
+
+
+class hc_tensor_list(ctypes.Structure):
+    """A list of tensors for hc_grad_norm and hc_grad_clip, made once: grads (fp32
+    or bf16, any shapes, contiguous, on one device) and outs like them (None: in
+    place). It holds them and its table on their device. Waits for the table's
+    copy, so that every stream may use it; not to be made during a capture."""
+    _fields_ = [("table", ctypes.c_void_p), ("units", ctypes.c_longlong),
+                ("tensors", ctypes.c_int)]
+
+    def __init__(self, grads, outs=None):
+        super().__init__()
+        import torch
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        if len(self.outs) != len(self.grads):
+            raise ValueError(f"{len(self.grads)} grads and {len(self.outs)} outs")
+        n = len(self.grads)
+        row = _token_types()[3]
+        index = {t.device.index for t in self.grads + self.outs if t.is_cuda}
+        if len(index) > 1:
+            raise ValueError(f"tensors on devices {sorted(index)}: a list is of one")
+        ins, out = (ctypes.c_void_p * n)(), (ctypes.c_void_p * n)()
+        numel, dt = (ctypes.c_longlong * n)(), (ctypes.c_int * n)()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            ins[i] = _arg(f"grads[{i}]", g, g.shape, row)
+            out[i] = _arg(f"outs[{i}]", o, g.shape, (g.dtype,))
+            numel[i], dt[i] = g.numel(), _dt(g)
+        self.device = index.pop() if index else torch.cuda.current_device()
+        lib = load_library()
+        host = torch.empty(lib.hc_tensor_list_bytes(n), dtype=torch.uint8)
+        self.memory = torch.empty(host.shape, dtype=torch.uint8, device=f"cuda:{self.device}")
+        _check(lib.hc_tensor_list_fill(ins, out, numel, dt, n, host.data_ptr(),
+                                       self.memory.data_ptr(), ctypes.byref(self)),
+               "hc_tensor_list_fill")
+        self.memory.copy_(host)
+        torch.cuda.current_stream(self.device).synchronize()
+
+
+def _list(tensors):
+    import torch
+    if not isinstance(tensors, hc_tensor_list):
+        raise TypeError("an hc_tensor_list is expected")
+    if tensors.device != torch._C._cuda_getDevice():
+        raise ValueError(f"the list is of device {tensors.device}, which is not the current one")
+    return ctypes.byref(tensors)
+
+
+def hc_grad_norm(tensors, norm, stream=None):
+    """norm fp32 [1] = the norm over all grads of an hc_tensor_list."""
+    f32 = _token_types()[0]
+    _check(load_library().hc_grad_norm(_list(tensors), _arg("norm", norm, (1,), f32), _s(stream)),
+           "hc_grad_norm")
+
+
+def hc_grad_clip(tensors, norm, max_norm, stream=None):
+    """outs = grads * min(1, max_norm / norm) for an hc_tensor_list; norm fp32 [1]
+    on the device."""
+    f32 = _token_types()[0]
+    _check(load_library().hc_grad_clip(_list(tensors), _arg("norm", norm, (1,), f32), max_norm,
+                                       _s(stream)), "hc_grad_clip")
 
 
 def hc_test_set_option(option: int, value: int):

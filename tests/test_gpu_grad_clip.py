@@ -1,0 +1,206 @@
+"""The norm over a list of tensors and the clipping by it, against 64-bit sums.
+
+Tolerances. U = 2^-24. A thread sums 32 squares in two chains of 16 and adds
+the two: 17 U of a sum of positive numbers. Their sums are kept in a pair of
+fp32 numbers whose lower one takes at most 2^-24 of the upper one a step and
+rounds it to 2^-24 of that; for the up to 2^12 steps of a thread here that is
+below U. Then 64 bits, a square root and one rounding: the norm is off by at most
+(17 + 1) U / 2 + U = 10 U of itself. The scale is a quotient of it (1 U more),
+an output one product (1 U) and its rounding."""
+import math
+
+import pytest
+
+from paper_2608_09388_gb300 import hc
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+from _tokens import BF, D64, F, U, full, gen, randn, rounding, shifted, within  # noqa: E402
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2608_09388_gb300 import build
+    build.build()
+    hc.load_library()
+    assert hc.hc_get_device_status() == hc.HC_OK
+
+
+@pytest.fixture(autouse=True)
+def _status_clean():
+    yield
+    assert hc.hc_get_device_status() == hc.HC_OK
+
+
+def norm_ref(ts):
+    return math.sqrt(sum(float((t.to(D64) ** 2).sum()) for t in ts))
+
+
+def check(grads, outs, norm, max_norm, before=None):
+    ref = norm_ref(before or grads)
+    assert abs(float(norm) - ref) <= 10 * U * ref
+    scale = 1.0 if float(norm) <= max_norm else max_norm / ref
+    for i, (g, o) in enumerate(zip(before or grads, outs)):
+        want = g.to(D64) * scale
+        within(o, want, 0 if scale == 1 else 13 * U * want.abs() + rounding(g.dtype, want), i)
+
+
+# one element, pieces that are not full, the border of a unit and of the units
+# a block loads together, more units than blocks
+SIZES = [[1], [0, 3], [7, 8, 9], [4095, 4096, 4097], [16384, 16385, 1, 65536],
+         [1000] * 300, [3000000, 5, 0, 70001], [12345678]]
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("sizes", SIZES)
+def test_norm_and_clip(sizes, kind):
+    g = gen(len(sizes) + sizes[0])
+    types = {"f32": [F], "bf16": [BF], "mixed": [F, BF]}[kind]
+    grads = [randn(g, n, dtype=types[i % len(types)]) for i, n in enumerate(sizes)]
+    outs = [full((n,), t.dtype) for n, t in zip(sizes, grads)]
+    lst = hc.hc_tensor_list(grads, outs)
+    norm = full((1,))
+    hc.hc_grad_norm(lst, norm)
+    ref = norm_ref(grads)
+    for max_norm in (0.7 * ref, 1.3 * ref):
+        for o in outs:
+            o.fill_(77)
+        hc.hc_grad_clip(lst, norm, max_norm)
+        check(grads, outs, norm, max_norm)
+    again = full((1,))
+    hc.hc_grad_norm(lst, again)
+    assert torch.equal(again, norm)
+    # in place: the same bits, and untouched where the norm is not above
+    want = [o.clone() for o in outs]
+    here = [t.clone() for t in grads]
+    inp = hc.hc_tensor_list(here)
+    hc.hc_grad_clip(inp, norm, 1.3 * ref)
+    assert all(torch.equal(a, b) for a, b in zip(here, grads))
+    hc.hc_grad_clip(lst, norm, 0.3 * ref)
+    hc.hc_grad_clip(inp, norm, 0.3 * ref)
+    assert all(torch.equal(a, b) for a, b in zip(here, outs)) and len(want) == len(here)
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_neighbours_and_alignment(dtype):
+    """Tensors one after another in one buffer, at every alignment, into outputs
+    of other alignments: what lies between and around them stays."""
+    g = gen(3)
+    sizes = [1, 2, 3, 5, 8, 13, 4095, 4099, 8190, 31, 1, 1]
+    total = sum(sizes) + len(sizes) + 9
+    src, dst = randn(g, total, dtype=dtype), full((total + 3,), dtype)
+    keep = src.clone()
+    grads, outs, spans, at = [], [], [], 1
+    for n in sizes:
+        grads.append(src[at:at + n])
+        outs.append(dst[at + 2:at + 2 + n])
+        spans.append((at + 2, n))
+        at += n + (1 if n % 2 else 0)
+    lst = hc.hc_tensor_list(grads, outs)
+    norm = full((1,))
+    hc.hc_grad_norm(lst, norm)
+    hc.hc_grad_clip(lst, norm, 1.0)
+    check(grads, outs, norm, 1.0)
+    assert torch.equal(src, keep)
+    mine = torch.zeros(total + 3, dtype=torch.bool, device="cuda")
+    for a, n in spans:
+        mine[a:a + n] = True
+    assert (dst[~mine] == 77).all()
+    before = [t.clone() for t in grads]
+    hc.hc_grad_clip(hc.hc_tensor_list(grads), norm, 1.0)
+    assert all(torch.equal(a, b) for a, b in zip(grads, outs)) and len(before) == len(outs)
+    gap = torch.ones(total, dtype=torch.bool, device="cuda")
+    for a, n in spans:
+        gap[a - 2:a - 2 + n] = False
+    assert torch.equal(src[gap], keep[gap])
+
+
+def clip_of(ts, max_norm):
+    outs = [torch.full_like(t, 77) for t in ts]
+    lst, norm = hc.hc_tensor_list(ts, outs), full((1,))
+    hc.hc_grad_norm(lst, norm)
+    hc.hc_grad_clip(lst, norm, max_norm)
+    return norm, outs
+
+
+def test_values():
+    g = gen(5)
+    a, b = randn(g, 5000), randn(g, 70000, dtype=BF)
+    # squares above the range of fp32
+    big = [a * 2.0 ** 100, (b.float() * 2.0 ** 90).to(BF)]
+    norm, outs = clip_of(big, 1.0)
+    check(big, outs, norm, 1.0)
+    # zeros, no elements, no tensors: norm 0, outputs as the inputs
+    for ts in ([torch.zeros(5000, device="cuda")], [a[:0]], []):
+        norm, outs = clip_of(ts, 0.0)
+        assert norm.item() == 0 and all(torch.equal(o, t) for o, t in zip(outs, ts))
+    # an infinity, a NaN
+    c = a.clone()
+    c[4321] = float("-inf")
+    norm, outs = clip_of([c, b], 1.0)
+    assert norm.item() == math.inf and outs[0][4321].isnan() and int(outs[0].isnan().sum()) == 1
+    assert (outs[0].nan_to_num() == 0).all() and (outs[1] == 0).all()
+    c[17] = float("nan")
+    norm, outs = clip_of([c, b], 1.0)
+    assert norm.isnan() and outs[0].isnan().all() and outs[1].isnan().all()
+    # exact sums: the norm exactly at the border is not clipped
+    d = torch.full((4096, 4), 2.0, device="cuda")
+    norm, outs = clip_of([d], 256.0)
+    assert norm.item() == 256 and torch.equal(outs[0], d)
+    norm, outs = clip_of([d], 64.0)
+    assert (outs[0] == 0.5).all()
+    norm, outs = clip_of([a], 0.0)
+    assert (outs[0] == 0).all()
+    norm, outs = clip_of([a], math.inf)
+    assert torch.equal(outs[0], a)
+
+
+def test_long_sum():
+    """2^28 equal values: a plain fp32 chain would stop growing."""
+    t = torch.full((2 ** 28,), 0.1, device="cuda")
+    norm = full((1,))
+    hc.hc_grad_norm(hc.hc_tensor_list([t]), norm)
+    ref = math.sqrt(2 ** 28 * float(t[0]) ** 2)
+    assert abs(norm.item() - ref) <= 10 * U * ref
+
+
+def test_stream_graph_and_shapes():
+    """Another stream, a captured pass replayed on other gradients, two lists
+    at a time on two streams, tensors of several dimensions."""
+    g = gen(7)
+    sets = [[randn(g, 300, 70), randn(g, 64, 3, 3, 3, dtype=BF), randn(g, 1)] for _ in range(2)]
+    outs = [[torch.full_like(t, 77) for t in s] for s in sets]
+    lists = [hc.hc_tensor_list(s, o) for s, o in zip(sets, outs)]
+    norms = [full((1,)) for _ in sets]
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for l, n, s in zip(lists, norms, streams):
+            hc.hc_grad_norm(l, n, stream=s)
+            hc.hc_grad_clip(l, n, 1.0, stream=s)
+    torch.cuda.synchronize()
+    for s, o, n in zip(sets, outs, norms):
+        check(s, o, n, 1.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        hc.hc_grad_norm(lists[0], norms[0], stream=streams[0])
+        hc.hc_grad_clip(lists[0], norms[0], 1.0, stream=streams[0])
+    for by in (3.0, 1e-3):
+        for t in sets[0]:
+            t.mul_(by)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(sets[0], outs[0], norms[0], 1.0)
+    assert shifted(sets[0][0]).shape == sets[0][0].shape
+
+
+def test_other_device_is_refused():
+    lst = hc.hc_tensor_list([torch.zeros(3, device="cuda")])
+    lst.device += 1
+    with pytest.raises(ValueError):
+        hc.hc_grad_norm(lst, full((1,)))
