@@ -656,6 +656,53 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
                             hc_stream_t stream);
 
 /*
+ * hc_linear_cross_entropy_fwd -- softmax cross entropy of the logits of a
+ * linear layer, which are never kept. For n < N' with targets[n] >= 0:
+ *   l[v] = sum_c x[n][c] * W[v][c] + bias[v]
+ *   lse[n] = log sum_v exp(l[v]),  loss[n] = lse[n] - l[targets[n]]
+ * A token with the target -1 takes no part: its loss and lse are 0. Any other
+ * target outside [0, V) is reported (HC_ERR_INVALID_INDEX) and treated as -1.
+ *   x         [capacity, C] of dtype dt
+ *   W         [V, C] of dtype dt: a row per class, as an embedding table has
+ *             (the same table may serve both)
+ *   bias      [V] fp32, or NULL (0); -infinity excludes a class
+ *   targets   [capacity] int32
+ *   loss, lse [capacity] fp32, or NULL each; at least one is required. lse is
+ *             what hc_linear_cross_entropy_bwd reads
+ * fp32 operands keep fp32's precision: each is split into three bf16 numbers,
+ * and the products that matter are summed. Uses the library's per-stream workspace:
+ * with planes = 1 (bf16) or 3 (fp32), 2 * planes * C + 16 bytes a row of the
+ * capacity (rounded up to 256 rows), 8 bytes a row and 128 classes, and
+ * 2 * planes * C bytes a class for fp32 and for rows of W that are not 16-byte aligned.
+ */
+hc_status hc_linear_cross_entropy_fwd(const void* x, const void* W, hc_dtype dt, const float* bias,
+                                      const int32_t* targets, const int32_t* count, int capacity,
+                                      int C, int V, float* loss, float* lse, hc_stream_t stream);
+
+/*
+ * hc_linear_cross_entropy_bwd -- its gradients. With
+ *   G[n][v] = dloss[n] * (exp(l[v] - lse[n]) - (v == targets[n]))
+ * for the tokens that take part, 0 for the others:
+ *   dx[n][c] = sum_v G[n][v] * W[v][c]          (n < N')
+ *   dW[v][c] = sum_n G[n][v] * x[n][c],  dbias[v] = sum_n G[n][v]
+ * Every row of dW and dbias is written (0 where no token takes part).
+ *   lse       [capacity] fp32, as the forward wrote it
+ *   dloss     [capacity] fp32: the gradient of each token's loss (1 / tokens for
+ *             their mean); not read where the target is -1
+ *   dx        [capacity, C] of dtype dt, or NULL; may be x
+ *   dW        [V, C] of dtype dt, or NULL; may not overlap W
+ *   dbias     [V] fp32, or NULL; at least one output is required
+ * G is held in bf16 for bf16 operands (a rounding of 2^-8 at most), in three bf16
+ * numbers for fp32; sums are in fp32. The vocabulary is taken in pieces whose G
+ * takes at most 512 MiB of the workspace (2048 classes at least); the sums of dx
+ * take up to four times 4 * C bytes a row of the capacity more than the forward.
+ */
+hc_status hc_linear_cross_entropy_bwd(const void* x, const void* W, hc_dtype dt, const float* bias,
+                                      const int32_t* targets, const float* lse, const float* dloss,
+                                      const int32_t* count, int capacity, int C, int V, void* dx,
+                                      void* dW, float* dbias, hc_stream_t stream);
+
+/*
  * A list of tensors of any sizes and either type, gone over as one: a table in
  * device memory, made once for tensors that stay where they are.
  * hc_tensor_list_fill writes the table of n tensors, hc_tensor_list_bytes(n)

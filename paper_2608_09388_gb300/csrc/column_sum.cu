@@ -12,12 +12,13 @@ constexpr int kWarps = 32;
 
 __global__ void __launch_bounds__(kWarps * 32)
     column_sum_kernel(const float* __restrict__ part, int parts, long long pitch, int C,
-                      float* __restrict__ out) {
+                      float* __restrict__ out, const int* rows) {
     __shared__ float sh[kWarps][33];
     pdl_wait();
     pdl_trigger();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long c = blockIdx.x * 32ll + lane;
+    if (rows) parts = min(parts, (int)((*rows + 31ll) / 32));
     float v = 0.f;
     if (c < C) {
 #pragma unroll 8
@@ -36,10 +37,10 @@ __global__ void __launch_bounds__(kWarps * 32)
 }  // namespace
 
 hc_status launch_column_sum(const float* part, int parts, long long pitch, int C, float* out,
-                            cudaStream_t s) {
+                            cudaStream_t s, const int* rows) {
     const unsigned grid = (unsigned)(((long long)C + 31) / 32);
     return launch_pdl(column_sum_kernel, dim3(grid), dim3(kWarps * 32), 0, s, "column_sum_kernel",
-                      part, parts, pitch, C, out);
+                      part, parts, pitch, C, out, rows);
 }
 
 }  // namespace hc

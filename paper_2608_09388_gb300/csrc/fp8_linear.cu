@@ -34,12 +34,7 @@
 // few blocks pays for its first scales and its epilogue, about 2 us (16384 x 640
 // x 4096: 69 us, 41 without the stores and what leads to them). 1 x 8192 x 8192
 // takes 14 us, 9.9 of them the weight at the copy rate.
-#include <cuda.h>
-#include <cudaTypedefs.h>
-
-#include <mutex>
-
-#include "tokens.cuh"
+#include "pipeline.cuh"
 
 namespace hc {
 namespace {
@@ -131,14 +126,6 @@ __device__ __forceinline__ void tma_prefetch_2d(const void* tmap, int c0, int c1
                  "r"(c0), "r"(c1)
                  : "memory");
 }
-// One lane of a converged warp.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t e;
-    asm volatile(
-        "{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(e));
-    return e != 0;
-}
 // (a0, a1) += (v0, v1) * (s, s), one instruction for both.
 __device__ __forceinline__ void fma_pair(float& a0, float& a1, uint32_t v0, uint32_t v1, float s) {
     unsigned long long a, v, ss;
@@ -147,53 +134,6 @@ __device__ __forceinline__ void fma_pair(float& a0, float& a1, uint32_t v0, uint
     asm("mov.b64 %0, {%1, %1};" : "=l"(ss) : "f"(s));
     asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(a) : "l"(v), "l"(ss));
     asm("mov.b64 {%0, %1}, %2;" : "=f"(a0), "=f"(a1) : "l"(a));
-}
-// A pipeline wait of this kernel, by a whole warp: a look at the phase, then
-// tries that may suspend the warp, the abort flag and the clock after each.
-// (mbar_wait reads its limit from global memory whenever its first try has
-// failed, longer than most waits here last. Polling all the time instead drew
-// power: 1.5% on the largest products, which run at the power limit. A limit
-// lowered below a try's longest suspension is kept by polling.)
-constexpr unsigned long long kLongestTryNs = 100000;
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n"
-        " mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        " selp.u32 %0, 1, 0, p;\n}\n"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                          unsigned* status, unsigned long long limit) {
-    const unsigned long long t0 = globaltimer_ns();
-    bool ok;
-    for (;;) {
-        ok = limit > kLongestTryNs ? mbar_try_wait(bar, parity) : mbar_test(bar, parity);
-        if (ok || *abort_flag) break;
-        if (globaltimer_ns() - t0 > limit) {
-            *abort_flag = 1;
-            report(status, kErrTimeout);
-            break;
-        }
-    }
-    return __all_sync(0xffffffffu, ok);
-}
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag,
-                                         unsigned* status, unsigned long long limit) {
-    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-    return wait_slow(bar, parity, abort_flag, status, limit);
-}
-// Both phases, looked at together before either is waited for.
-__device__ __forceinline__ bool wait_bars(uint32_t bar0, uint32_t parity0, uint32_t bar1,
-                                          uint32_t parity1, volatile int* abort_flag,
-                                          unsigned* status, unsigned long long limit) {
-    const bool a = mbar_test(bar0, parity0), b = mbar_test(bar1, parity1);
-    if (__all_sync(0xffffffffu, a && b)) return true;
-    return wait_slow(bar0, parity0, abort_flag, status, limit) &&
-           wait_slow(bar1, parity1, abort_flag, status, limit);
 }
 // A float at the same shared-memory offset of another CTA of the cluster.
 __device__ __forceinline__ float lds_cluster_f32(uint32_t addr, uint32_t rank) {
@@ -675,20 +615,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<BN>::kTwo ? 2 : 1)
 }
 
 // ---------------------------------------------------------------- host side
-PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-    static std::once_flag once;
-    std::call_once(once, [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                             &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    });
-    return fn;
-}
-
 // A [rows, pitch] byte matrix in boxes of box_rows x 128 bytes, 128-byte
 // swizzle; what lies outside reads as zero.
 hc_status encode(CUtensorMap* m, const void* base, long long rows, int pitch, int box_rows) {

@@ -1005,6 +1005,85 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
     return launch_fp8_linear(ctx, a, (cudaStream_t)stream);
 }
 
+static hc_status check_xent(const char* fn, const void* x, const void* W, hc_dtype dt,
+                            const float* bias, const int32_t* targets, const int32_t* count,
+                            int capacity, int C, int V) {
+    const hc_status st = check_rows(fn, dt, capacity, C);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(V >= 1 && V <= kMaxChannels, "%s: V=%d must be >= 1 and <= %d", fn, V, kMaxChannels);
+    HC_REQUIRE(W && (capacity == 0 || (x && targets)), "%s: x, W and targets are required", fn);
+    HC_REQUIRE(!misaligned(x, elem_bytes(dt)) && !misaligned(W, elem_bytes(dt)),
+               "%s: x and W must be aligned to the element size", fn);
+    HC_REQUIRE(!misaligned(bias, 4) && !misaligned(targets, 4) && !misaligned(count, 4),
+               "%s: misaligned bias, targets or count", fn);
+    return HC_OK;
+}
+
+hc_status hc_linear_cross_entropy_fwd(const void* x, const void* W, hc_dtype dt, const float* bias,
+                                      const int32_t* targets, const int32_t* count, int capacity,
+                                      int C, int V, float* loss, float* lse, hc_stream_t stream) {
+    const char* fn = "hc_linear_cross_entropy_fwd";
+    t_last_error[0] = 0;
+    const hc_status st = check_xent(fn, x, W, dt, bias, targets, count, capacity, C, V);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(loss || lse, "%s: at least one of loss and lse is required", fn);
+    HC_REQUIRE(!misaligned(loss, 4) && !misaligned(lse, 4), "%s: misaligned loss or lse", fn);
+    if (capacity == 0) return HC_OK;
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    LinearXentArgs a{};
+    a.x = x;
+    a.W = W;
+    a.dt = dt;
+    a.bias = bias;
+    a.targets = targets;
+    a.count = count;
+    a.capacity = capacity;
+    a.C = C;
+    a.V = V;
+    a.loss_out = loss;
+    a.lse_out = lse;
+    StreamLock lock((cudaStream_t)stream);
+    return launch_linear_xent_fwd(ctx, a, (cudaStream_t)stream);
+}
+
+hc_status hc_linear_cross_entropy_bwd(const void* x, const void* W, hc_dtype dt, const float* bias,
+                                      const int32_t* targets, const float* lse, const float* dloss,
+                                      const int32_t* count, int capacity, int C, int V, void* dx,
+                                      void* dW, float* dbias, hc_stream_t stream) {
+    const char* fn = "hc_linear_cross_entropy_bwd";
+    t_last_error[0] = 0;
+    const hc_status st = check_xent(fn, x, W, dt, bias, targets, count, capacity, C, V);
+    if (st != HC_OK) return st;
+    HC_REQUIRE(dx || dW || dbias, "%s: at least one of dx, dW and dbias is required", fn);
+    HC_REQUIRE(capacity == 0 || (lse && dloss), "%s: lse and dloss are required", fn);
+    HC_REQUIRE(!misaligned(dx, elem_bytes(dt)) && !misaligned(dW, elem_bytes(dt)),
+               "%s: dx and dW must be aligned to the element size", fn);
+    HC_REQUIRE(!misaligned(lse, 4) && !misaligned(dloss, 4) && !misaligned(dbias, 4),
+               "%s: misaligned lse, dloss or dbias", fn);
+    HC_REQUIRE(!dW || dW != W, "%s: dW may not be W", fn);
+    if (capacity == 0 && !dW && !dbias) return HC_OK;
+    const DeviceCtx* ctx = device_ctx();
+    if (!ctx) return HC_ERR_CUDA;
+    LinearXentArgs a{};
+    a.x = x;
+    a.W = W;
+    a.dt = dt;
+    a.bias = bias;
+    a.targets = targets;
+    a.count = count;
+    a.capacity = capacity;
+    a.C = C;
+    a.V = V;
+    a.lse = lse;
+    a.dloss = dloss;
+    a.dx = dx;
+    a.dW = dW;
+    a.dbias = dbias;
+    StreamLock lock((cudaStream_t)stream);
+    return launch_linear_xent_bwd(ctx, a, (cudaStream_t)stream);
+}
+
 size_t hc_tensor_list_bytes(int n) {
     return n < 0 ? 0 : tensor_list_bytes(n);
 }

@@ -194,7 +194,7 @@ hc_status launch_scatter(const DeviceCtx* ctx, const void* y, int elem_bytes, co
                          int zero_fill, void* out, cudaStream_t s);
 
 // Token operators on compact rows (layer_norm.cu, rms_norm.cu, embedding.cu,
-// fp8_quant.cu, fp8_linear.cu). count NULL = all `capacity` rows.
+// fp8_quant.cu, fp8_linear.cu, linear_xent.cu). count NULL = all `capacity` rows.
 struct LayerNormArgs {
     const void* x;
     const void* dy;
@@ -235,9 +235,11 @@ struct RmsNormArgs {
 };
 hc_status launch_rms_norm_fwd(const DeviceCtx* ctx, const RmsNormArgs& a, cudaStream_t s);
 hc_status launch_rms_norm_bwd(const DeviceCtx* ctx, const RmsNormArgs& a, cudaStream_t s);
-// out[c] = sum over p < parts of part[p * pitch + c], in a fixed order.
+// out[c] = sum over p < parts of part[p * pitch + c], in a fixed order. With
+// `rows` (on the device), part p is of the rows 32 p .. and the ones behind
+// *rows are not read.
 hc_status launch_column_sum(const float* part, int parts, long long pitch, int C, float* out,
-                            cudaStream_t s);
+                            cudaStream_t s, const int* rows = nullptr);
 struct EmbeddingArgs {
     hc_dtype dt;  // of the table and y, or of dy
     const int32_t* ids;
@@ -272,6 +274,25 @@ struct Fp8LinearArgs {
     unsigned* status;
 };
 hc_status launch_fp8_linear(const DeviceCtx* ctx, const Fp8LinearArgs& a, cudaStream_t s);
+
+struct LinearXentArgs {
+    const void* x;
+    const void* W;  // [V, C]
+    hc_dtype dt;
+    const float* bias;
+    const int32_t* targets;
+    const int32_t* count;
+    int capacity, C, V;
+    float* loss_out;  // forward
+    float* lse_out;
+    const float* lse;  // backward
+    const float* dloss;
+    void* dx;
+    void* dW;
+    float* dbias;
+};
+hc_status launch_linear_xent_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
+hc_status launch_linear_xent_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
 
 // Lists of tensors (grad_clip.cu). fill_tensor_list may throw std::bad_alloc.
 size_t tensor_list_bytes(int n);

@@ -1,0 +1,1044 @@
+// Softmax cross entropy behind a linear layer, and its gradients, without the
+// logits ever being kept. For every token n < N' with a class t[n] >= 0:
+//   l[v] = x[n] . W[v] + bias[v],  lse = log sum_v exp(l[v]),  loss = lse - l[t]
+//   G[n][v] = dloss[n] * (exp(l[v] - lse) - (v == t))
+//   dx = G W,  dW = G^T x,  dbias[v] = sum_n G[n][v]
+// The tokens that take part are gathered first, in their order, into M rows
+// of the workspace. Forward, a tile of logits leaves a (largest, sum of
+// exponentials) pair per row and half tile, joined by a last kernel. Backward,
+// the vocabulary is taken in pieces: the logits of a piece are formed again,
+// G of the piece is written to the workspace in 16 bits, and both products
+// with it follow; dx is summed over the pieces in fp32.
+//
+// All four products are tcgen05 products of bf16 with fp32 accumulators. fp32
+// operands (and then G) are held as three bf16 numbers whose sum is the value
+// to 2^-24 of it, and six of the nine partial products are summed, the small
+// ones first: what is left out is below 2^-24 of a product. For bf16 operands
+// G is rounded to bf16 once (2^-9 of a value, as its factors are): its sums
+// over tokens and classes stay in fp32.
+//
+// The products run on pairs of CTAs (cta_group::2): a tile of 256 x 256, 128
+// rows of both operands in each CTA's shared memory, and 2 x 256 columns of
+// TMEM, so that a tile's epilogue runs under the next one's products.
+#include "pipeline.cuh"
+
+namespace hc {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 2^v, 2 units in the last place; results below the normal numbers are zero.
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// ---------------------------------------------------------------- layout of a call
+struct Rows {
+    int* m;            // tokens that take part
+    int* row_of;       // [capacity] their row, -1 for the others
+    int* token_of;     // [capacity]
+    int* target;       // [mpad]
+    float* lse;        // [mpad] backward
+    float* dloss;      // [mpad] backward
+    float* at_target;  // [mpad] forward: the target's logit
+    __nv_bfloat16* x;  // [planes][mpad][pitch]
+};
+
+// ---------------------------------------------------------------- gather
+__device__ __forceinline__ void planes_of(float v, __nv_bfloat16 (&p)[3]) {
+    p[0] = __float2bfloat16_rn(v);
+    const float r = v - __bfloat162float(p[0]);
+    // an infinity or a NaN is all in the first
+    const bool plain = fabsf(v) < __int_as_float(0x7f800000) && fabsf(r) < __int_as_float(0x7f800000);
+    p[1] = __float2bfloat16_rn(plain ? r : 0.f);
+    p[2] = __float2bfloat16_rn(plain ? r - __bfloat162float(p[1]) : 0.f);
+}
+
+constexpr int kGatherThreads = 256;
+
+// Sum over the block of small counts.
+__device__ __forceinline__ int block_count(int v, int* sh) {
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < kGatherThreads / 32; ++w) v += sh[w];
+    return v;
+}
+
+struct GatherArgs {
+    const void* x;
+    const int32_t* targets;
+    const int32_t* count;
+    long long capacity, mpad;
+    int C, V;
+    long long pitch;        // of a gathered row
+    const float* lse;       // backward
+    const float* dloss;
+    float* loss_out;        // forward: zero for tokens that take no part
+    float* lse_out;
+    unsigned* status;
+};
+
+// Block b takes the tokens [N' b / blocks, N' (b + 1) / blocks): it counts the
+// ones that take part before them, then gives its own their rows in order. The
+// last block zeroes the rows up to the next multiple of 64 (a block of the
+// products over tokens).
+template <typename T>
+__global__ void __launch_bounds__(kGatherThreads)
+    xent_gather_kernel(const GatherArgs a, const Rows r) {
+    constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+    __shared__ int sh[kGatherThreads / 32];
+    __shared__ int token[kGatherThreads];
+    pdl_wait();
+    pdl_trigger();
+    const long long rows = token_rows(a.count, a.capacity, a.status);
+    const long long n0 = rows * blockIdx.x / gridDim.x, n1 = rows * (blockIdx.x + 1) / gridDim.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto valid = [&](long long n) {
+        const int t = a.targets[n];
+        return t >= 0 && t < a.V;
+    };
+    int before = 0;
+#pragma unroll 8
+    for (long long n = threadIdx.x; n < n0; n += kGatherThreads) before += valid(n);
+    long long at = block_count(before, sh);
+    const T* const x = static_cast<const T*>(a.x);
+    const bool wide = a.C % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    for (long long first = n0; first < n1; first += kGatherThreads) {
+        const long long n = first + threadIdx.x;
+        int t = -1;
+        if (n < n1) {
+            t = a.targets[n];
+            if (t < -1 || t >= a.V) {
+                report(a.status, kErrIndex);
+                t = -1;
+            }
+            if (t < 0) {
+                r.row_of[n] = -1;
+                if (a.loss_out) a.loss_out[n] = 0.f;
+                if (a.lse_out) a.lse_out[n] = 0.f;
+            }
+        }
+        const unsigned mask = __ballot_sync(0xffffffffu, t >= 0);
+        __syncthreads();
+        if (lane == 0) sh[warp] = __popc(mask);
+        __syncthreads();
+        int mine = __popc(mask & ((1u << lane) - 1u)), all = 0;
+#pragma unroll
+        for (int w = 0; w < kGatherThreads / 32; ++w) {
+            if (w < warp) mine += sh[w];
+            all += sh[w];
+        }
+        if (t >= 0) {
+            const long long row = at + mine;
+            token[mine] = (int)n;
+            r.row_of[n] = (int)row;
+            r.token_of[row] = (int)n;
+            r.target[row] = t;
+            if (a.dloss) {
+                r.lse[row] = a.lse[n];
+                r.dloss[row] = a.dloss[n];
+            }
+        }
+        __syncthreads();
+        for (int j = warp; j < all; j += kGatherThreads / 32) {
+            const T* const from = x + (long long)token[j] * a.C;
+            __nv_bfloat16* const to = r.x + (at + j) * a.pitch;
+            if (wide && kPlanes == 1) {
+                for (int c = lane * 8; c < a.C; c += 256)
+                    *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(from + c);
+            } else {
+                for (int c = lane; c < a.C; c += 32) {
+                    __nv_bfloat16 p[3];
+                    if constexpr (kPlanes == 1)
+                        p[0] = from[c];
+                    else
+                        planes_of(from[c], p);
+#pragma unroll
+                    for (int k = 0; k < kPlanes; ++k) to[k * a.mpad * a.pitch + c] = p[k];
+                }
+            }
+        }
+        at += all;
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+        if (threadIdx.x == 0) *r.m = (int)at;
+        const long long end = (at + 63) / 64 * 64;
+        for (int k = 0; k < kPlanes; ++k) {
+            __nv_bfloat16* const p = r.x + k * a.mpad * a.pitch;
+            for (long long i = at * a.pitch + threadIdx.x; i < end * a.pitch; i += kGatherThreads)
+                p[i] = __float2bfloat16_rn(0.f);
+        }
+    }
+}
+
+// W in the form the products read where it is not: three planes of bf16, or
+// rows with a pitch that is a multiple of 16 bytes.
+template <typename T>
+__global__ void __launch_bounds__(256)
+    xent_weight_kernel(const T* __restrict__ W, int V, int C, long long pitch,
+                       __nv_bfloat16* __restrict__ out) {
+    constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+    pdl_wait();
+    pdl_trigger();
+    const int warp = (int)((blockIdx.x * 256 + threadIdx.x) >> 5), lane = threadIdx.x & 31;
+    for (long long v = warp; v < V; v += (long long)gridDim.x * 8)
+        for (int c = lane; c < C; c += 32) {
+            __nv_bfloat16 p[3];
+            if constexpr (kPlanes == 1)
+                p[0] = W[v * C + c];
+            else
+                planes_of(W[v * C + c], p);
+#pragma unroll
+            for (int k = 0; k < kPlanes; ++k) out[(k * (long long)V + v) * pitch + c] = p[k];
+        }
+}
+
+// ---------------------------------------------------------------- products
+enum Product {
+    kStats,   // x W^T -> the pairs of the forward pass
+    kGrad,    // x W^T -> G of a piece
+    kInput,   // G W -> fp32 slabs of dx
+    kWeight,  // G^T x -> rows of dW
+};
+
+constexpr int kTile = 256;                       // rows of a tile, 128 in each CTA
+constexpr int kHalf = 128;
+constexpr int kKB = 64;                          // elements per block of the sum: 128 bytes
+constexpr int kOperandBytes = kHalf * kKB * 2;   // 16 KiB
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kStages = 6;
+constexpr int kStoreWarps = 8;
+constexpr int kLoadWarp = kStoreWarps;
+constexpr int kMmaWarp = kStoreWarps + 1;
+constexpr int kThreads = (kStoreWarps + 2) * 32;
+constexpr int kOutBytes = 32 * 128;              // staging of a storing warp
+constexpr int kGroupM = 16;                      // row tiles walked per column of tiles
+constexpr int kBars = 2 * kStages + 5;
+constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreWarps * kOutBytes + kBars * 8 + 64;
+
+struct ProductArgs {
+    const int* m;        // rows of x and G
+    int rows;            // kWeight: rows of the piece (the others: *m)
+    int cols;            // columns of the result
+    int depth;           // length of the sum (kWeight: *m)
+    int bn;              // columns of a tile: 64 (kStats), 128 or 256
+    int split;           // kInput: parts of the sum
+    int planes;          // 1, or 3: six products a block
+    int v0, V;           // first class of the piece, classes in all
+    const float* bias;
+    const int* target;
+    const float* lse;
+    const float* dloss;
+    float2* pairs;       // kStats: [half tiles][mpad]
+    float* at_target;
+    float* dbias_part;   // kGrad: [mpad / 32][piece], or NULL
+    long long mpad, piece;
+    bool add;            // kInput: onto what earlier pieces left
+    void* dw;            // kWeight: rows from v0 on, [.., cols]
+    bool wide;           // its rows are 16-byte aligned: stored by TMA
+    unsigned* status;
+};
+
+__device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo) {
+    // 128-byte swizzle, groups of 8 rows 1024 bytes apart; MN-major: the next
+    // 64 columns lbo bytes further on
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) |
+           ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc,
+                                         uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Arrive on `bar` of both CTAs once the products issued so far are done.
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64"
+        " [%0], %1;\n" ::"r"(bar),
+        "h"((unsigned short)3)
+        : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar)
+                 : "memory");
+}
+// A box of this CTA's, whose bytes are counted by the pair's first CTA.
+__device__ __forceinline__ void load_pair(uint32_t dst, const void* tmap, int c0, int c1, int c2,
+                                          uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4}], [%5];\n" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void store_box(const void* tmap, uint32_t src, int c0, int c1, int c2,
+                                          bool add) {
+    if (add)
+        asm volatile(
+            "cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group"
+            " [%0, {%2, %3, %4}], [%1];\n" ::"l"(reinterpret_cast<uint64_t>(tmap)),
+            "r"(src), "r"(c0), "r"(c1), "r"(c2)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group"
+            " [%0, {%2, %3, %4}], [%1];\n" ::"l"(reinterpret_cast<uint64_t>(tmap)),
+            "r"(src), "r"(c0), "r"(c1), "r"(c2)
+            : "memory");
+    asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
+}
+
+// The tile t of the walk: row tiles in groups of kGroupM, the tiles of a group
+// column by column, so that the pairs at work share both operands in L2.
+__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tm, uint32_t tn, int& m, int& n) {
+    const uint32_t per = (uint32_t)kGroupM * tn;
+    const uint32_t g = t / per, first = g * kGroupM;
+    const uint32_t in = tm - first < (uint32_t)kGroupM ? tm - first : (uint32_t)kGroupM;
+    const uint32_t r = t - g * per;
+    n = (int)(r / in);
+    m = (int)(first + r % in);
+}
+
+// The planes of operand A and B in product p of six, small ones first.
+__device__ __forceinline__ int plane_a(int planes, int p) {
+    return planes == 1 ? 0 : (0x021010 >> (4 * (5 - p))) & 3;
+}
+__device__ __forceinline__ int plane_b(int planes, int p) {
+    return planes == 1 ? 0 : (0x201100 >> (4 * (5 - p))) & 3;
+}
+
+// Sums of v[i] over the warp's lanes, column i in lane i.
+__device__ __forceinline__ float column_sums(float (&v)[32]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+            const float send = up ? v[i] : v[i + o], keep = up ? v[i + o] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+        }
+    }
+    return v[0];
+}
+
+template <Product kP, typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+    xent_product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a,
+                        const __grid_constant__ CUtensorMap map_b,
+                        const __grid_constant__ CUtensorMap map_out) {
+    constexpr bool kAMn = kP == kWeight, kBMn = kP == kInput || kP == kWeight;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t out_at = base + kStages * kStageBytes;
+    const uint32_t bars = out_at + kStoreWarps * kOutBytes;
+    auto full_bar = [&](uint32_t s) { return bars + 8u * s; };
+    auto empty_bar = [&](uint32_t s) { return bars + 8u * (kStages + s); };
+    auto tfull_bar = [&](uint32_t b) { return bars + 8u * (2 * kStages + b); };
+    auto tempty_bar = [&](uint32_t b) { return bars + 8u * (2 * kStages + 2 + b); };
+    const uint32_t fin_bar = bars + 8u * (2 * kStages + 4);
+    uint8_t* const misc = smem_raw + (bars - raw) + 8 * kBars;
+    volatile uint32_t* const tmem_holder = reinterpret_cast<volatile uint32_t*>(misc);
+    volatile int* const abort_flag = reinterpret_cast<volatile int*>(misc + 4);
+    const uint32_t issued_at = bars + 8u * kBars + 8u;  // copies issued, read by the first CTA
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(tfull_bar(b), 1);
+            mbar_init(tempty_bar(b), 2 * kStoreWarps);
+        }
+        mbar_init(fin_bar, 1);
+        *abort_flag = 0;
+        sts_s32(issued_at, 0);
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        prefetch_tensormap(&map_a);
+        prefetch_tensormap(&map_b);
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(
+                         smem_u32((const void*)tmem_holder)),
+                     "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_barrier();  // both CTAs' barriers are there
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
+    pdl_wait();
+    pdl_trigger();
+
+    const unsigned long long limit =
+        reinterpret_cast<const volatile DeviceWord*>(a.status)->wait_limit_ns;
+    const int M = *a.m;
+    const int rows = kP == kWeight ? a.rows : M;
+    const int depth = kP == kWeight ? M : a.depth;
+    const uint32_t tm = (uint32_t)(((long long)rows + kTile - 1) / kTile);
+    const uint32_t tn = (uint32_t)(((long long)a.cols + a.bn - 1) / a.bn);
+    const uint32_t units = tm * tn * (uint32_t)a.split;  // below 2^31 (checked by the host)
+    const int blocks = (int)(((long long)depth + kKB - 1) / kKB);
+    const int products = a.planes == 1 ? 1 : 6;
+    const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+    // Unit u: its tile, and its blocks [k0, k1) of the sum.
+    auto unit_at = [&](uint32_t u, int& m, int& n, int& part, int& k0, int& k1) {
+        part = 0;
+        k0 = 0;
+        k1 = blocks;
+        if constexpr (kP == kInput) {
+            const uint32_t tiles = tm * tn;
+            part = (int)(u / tiles);
+            u -= (uint32_t)part * tiles;
+            k0 = (int)((long long)blocks * part / a.split);
+            k1 = (int)((long long)blocks * (part + 1) / a.split);
+        }
+        tile_at(u, tm, tn, m, n);
+    };
+
+    // In all roles every lane of the warp walks the loop, so that its state is
+    // uniform; the copies and products are issued by one lane.
+    uint32_t issued = 0;
+    if (warp == kLoadWarp) {
+        const bool leader = elect_one();
+        const uint32_t full0 = cluster_map(full_bar(0), 0);  // the first CTA's
+        // a box of B holds its rows (the channels are innermost: bn / 2 rows),
+        // or 64 columns of 64 rows each
+        const uint32_t b_bytes = (uint32_t)a.bn / 2 * kKB * 2;
+        const uint32_t both = 2 * (kOperandBytes + b_bytes);
+        bool ok = true;
+        for (uint32_t u = first; u < units && ok; u += step) {
+            int m, n, part, k0, k1;
+            unit_at(u, m, n, part, k0, k1);
+            const int row = m * kTile + (int)rank * kHalf, col = n * a.bn + (int)rank * a.bn / 2;
+            for (int p = 0; p < products && ok; ++p) {
+                const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
+                for (int k = k0; k < k1; ++k, ++issued) {
+                    const uint32_t s = issued % kStages;
+                    ok = wait_bar(empty_bar(s), ((issued / kStages) & 1) ^ 1u, abort_flag, a.status,
+                                  limit);
+                    if (!ok) break;
+                    if (leader) {
+                        const uint32_t sa = base + s * kStageBytes, sb = sa + kOperandBytes;
+                        const uint32_t bar = full0 + 8u * s;
+                        if (rank == 0) mbar_arrive_expect_tx(full_bar(s), both);
+                        if constexpr (kAMn) {
+                            load_pair(sa, &map_a, row, k * kKB, pa, bar);
+                            load_pair(sa + kOperandBytes / 2, &map_a, row + 64, k * kKB, pa, bar);
+                        } else {
+                            load_pair(sa, &map_a, k * kKB, row, pa, bar);
+                        }
+                        // kInput: the classes of the piece start at v0
+                        if constexpr (kBMn) {
+                            const int at = k * kKB + (kP == kInput ? a.v0 : 0);
+                            load_pair(sb, &map_b, col, at, pb, bar);
+                            if (a.bn == 256)
+                                load_pair(sb + kOperandBytes / 2, &map_b, col + 64, at, pb, bar);
+                        } else {
+                            load_pair(sb, &map_b, k * kKB, a.v0 + col, pb, bar);
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) sts_s32(issued_at, (int)issued);
+    } else if (warp == kMmaWarp) {
+        if (rank == 0) {
+            const bool leader = elect_one();
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (kAMn ? 1u << 15 : 0u) |
+                                   (kBMn ? 1u << 16 : 0u) | ((uint32_t)(a.bn >> 3) << 17) |
+                                   ((uint32_t)(kTile >> 4) << 24);
+            uint32_t it = 0, tile = 0;
+            bool ok = true;
+            for (uint32_t u = first; u < units && ok; u += step, ++tile) {
+                int m, n, part, k0, k1;
+                unit_at(u, m, n, part, k0, k1);
+                const uint32_t b = tile & 1;
+                ok = wait_bar(tempty_bar(b), ((tile >> 1) & 1) ^ 1u, abort_flag, a.status, limit);
+                if (!ok) break;
+                tc_fence_after();
+                const int total = (k1 - k0) * products;
+                for (int k = 0; k < total; ++k, ++it) {
+                    const uint32_t s = it % kStages;
+                    ok = wait_bar(full_bar(s), (it / kStages) & 1, abort_flag, a.status, limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (leader) {
+                        const uint32_t sa = base + s * kStageBytes;
+                        const uint64_t da = desc_sw128(sa, kAMn ? kOperandBytes / 2 : 16);
+                        const uint64_t db = desc_sw128(sa + kOperandBytes, kBMn ? kOperandBytes / 2 : 16);
+#pragma unroll
+                        for (int j = 0; j < kKB / 16; ++j)  // 16 elements of the sum further on
+                            mma_pair(tmem_base + b * 256u, da + (kAMn ? 128 : 2) * j,
+                                     db + (kBMn ? 128 : 2) * j, idesc, (k | j) != 0 ? 1u : 0u);
+                        commit_pair(empty_bar(s));
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (leader) commit_pair(tfull_bar(b));
+                __syncwarp();
+            }
+            // every product issued here, and every arrival before this one, has
+            // completed once fin_bar fires, in both CTAs
+            if (leader) commit_pair(fin_bar);
+            __syncwarp();
+        }
+    } else {
+        const int quarter = warp & 3, half = warp >> 2, hc = a.bn / 2;
+        const uint32_t stage = out_at + (uint32_t)warp * kOutBytes;
+        uint32_t tile = 0;
+        for (uint32_t u = first; u < units; u += step, ++tile) {
+            int m, n, part, k0, k1;
+            unit_at(u, m, n, part, k0, k1);
+            const uint32_t b = tile & 1;
+            const bool ok = wait_bar(tfull_bar(b), (tile >> 1) & 1, abort_flag, a.status, limit);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * 256u + half * hc;
+            const uint32_t tempty = cluster_map(tempty_bar(b), 0);
+            // 32 columns of this lane's row
+            auto load = [&](int c, float (&f)[32]) {
+                uint32_t r[32];
+                tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
+                tmem_ld_wait();
+                if (c + 32 >= hc) {
+                    tc_fence_before();
+                    if (lane == 0) arrive_cluster(tempty);
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) f[i] = k1 > k0 ? __uint_as_float(r[i]) : 0.f;
+            };
+            const int row0 = m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+            const int col0 = n * a.bn + half * hc;
+            // 128 bytes of each of the warp's rows, swizzled, then one box
+            auto staging_free = [&] {
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
+                __syncwarp();
+            };
+            auto put = [&](int q, uint4 v) { sts_v4(stage + lane * 128 + ((q ^ (lane & 7)) << 4), v); };
+            auto send = [&](int c0, int c1, int c2, bool add) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) store_box(&map_out, stage, c0, c1, c2, add);
+            };
+            auto pack = [](float lo, float hi) { return Piece<__nv_bfloat16, 8>::pair(lo, hi); };
+
+            if constexpr (kP == kStats) {
+                const int target = row < M ? a.target[row] - a.v0 : -1;
+                float top = -__int_as_float(0x7f800000), sum = 0.f;
+                for (int c = 0; c < hc; c += 32) {
+                    float f[32];
+                    load(c, f);
+                    const int col = col0 + c;
+                    if (a.bias) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (col + i < a.cols) f[i] += __ldg(a.bias + a.v0 + col + i);
+                    }
+                    if (col + 32 > a.cols) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (col + i >= a.cols) f[i] = -__int_as_float(0x7f800000);
+                    }
+                    float most = top;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) most = fmaxf(most, f[i]);
+                    if (target >= col && target < col + 32) {
+                        float v = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v = col + i == target ? f[i] : v;
+                        a.at_target[row] = v;
+                    }
+                    // classes masked with -infinity leave it at that; a NaN
+                    // goes past fmaxf and into the sum
+                    const float from = most == -__int_as_float(0x7f800000) ? 0.f : most;
+                    sum *= ex2((top - from) * kLog2e);
+                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) s4[i & 3] += ex2((f[i] - from) * kLog2e);
+                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    top = most;
+                }
+                if (row < M && col0 < a.cols)
+                    a.pairs[(long long)(n * 2 + half) * a.mpad + row] = make_float2(top, sum);
+            } else if constexpr (kP == kGrad) {
+                const bool in = row < M;
+                const float lse = in ? a.lse[row] : 0.f, dloss = in ? a.dloss[row] : 0.f;
+                const int target = in ? a.target[row] - a.v0 : -1;
+                for (int c = 0; c < hc; c += 64) {
+                    float f[64];
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        float g[32];
+                        load(c + h, g);
+                        const int col = col0 + c + h;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const bool there = in && col + i < a.cols;
+                            if (a.bias && col + i < a.cols) g[i] += __ldg(a.bias + a.v0 + col + i);
+                            float p = ex2((g[i] - lse) * kLog2e);
+                            p -= col + i == target ? 1.f : 0.f;
+                            g[i] = there ? p * dloss : 0.f;
+                            f[h + i] = g[i];
+                        }
+                        if (a.dbias_part) {
+                            const float s = column_sums(g);
+                            if (col + lane < a.cols)
+                                a.dbias_part[(long long)(row0 / 32) * a.piece + col + lane] = s;
+                        }
+                    }
+                    const int planes = sizeof(T) == 4 ? 3 : 1;
+#pragma unroll
+                    for (int k = 0; k < planes; ++k) {
+                        staging_free();
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
+                            float v[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                v[i] = __bfloat162float(__float2bfloat16_rn(f[8 * q + i]));
+                                f[8 * q + i] -= v[i];  // what the next plane holds
+                            }
+                            put(q, make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]),
+                                              pack(v[6], v[7])));
+                        }
+                        send(col0 + c, row0, k, false);
+                    }
+                }
+            } else if constexpr (kP == kInput || sizeof(T) == 4) {
+                // fp32 results, 32 columns at a time
+                for (int c = 0; c < hc; c += 32) {
+                    float f[32];
+                    load(c, f);
+                    staging_free();
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        put(q, make_uint4(__float_as_uint(f[4 * q]), __float_as_uint(f[4 * q + 1]),
+                                          __float_as_uint(f[4 * q + 2]), __float_as_uint(f[4 * q + 3])));
+                    const int col = col0 + c;
+                    if (kP == kInput) {
+                        if (col < a.cols) send(col, row0, part, a.add);
+                    } else if (a.wide) {
+                        if (col < a.cols && row0 < rows) send(col, a.v0 + row0, 0, false);
+                    } else {
+                        __syncwarp();
+                        for (int r = 0; r < 32; ++r) {
+                            const uint32_t at = stage + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4;
+                            if (row0 + r < rows && col + lane < a.cols)
+                                static_cast<float*>(a.dw)[(long long)(a.v0 + row0 + r) * a.cols + col + lane] =
+                                    __int_as_float(lds_s32(at));
+                        }
+                        __syncwarp();
+                    }
+                }
+            } else {
+                // bf16 results, 64 columns at a time
+                for (int c = 0; c < hc; c += 64) {
+                    staging_free();
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        float f[32];
+                        load(c + h, f);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            put(h / 8 + q,
+                                make_uint4(pack(f[8 * q], f[8 * q + 1]), pack(f[8 * q + 2], f[8 * q + 3]),
+                                           pack(f[8 * q + 4], f[8 * q + 5]), pack(f[8 * q + 6], f[8 * q + 7])));
+                    }
+                    const int col = col0 + c;
+                    if (a.wide) {
+                        if (col < a.cols && row0 < rows) send(col, a.v0 + row0, 0, false);
+                    } else {
+                        __syncwarp();
+                        for (int r = 0; r < 32; ++r) {
+                            if (row0 + r >= rows) break;
+                            __nv_bfloat16* const to =
+                                static_cast<__nv_bfloat16*>(a.dw) + (long long)(a.v0 + row0 + r) * a.cols;
+#pragma unroll
+                            for (int h = 0; h < 64; h += 32) {
+                                const int j = h + lane;
+                                const uint32_t at = stage + r * 128 + (((j >> 3) ^ (r & 7)) << 4) + (j & 7) * 2;
+                                uint16_t v;
+                                asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(at) : "memory");
+                                if (col + j < a.cols) to[col + j] = __ushort_as_bfloat16(v);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
+        __syncwarp();
+    }
+
+    // The copies already issued land before either CTA ends, also where a role
+    // gave up: the first CTA's barriers count the bytes of both. A copy that one
+    // CTA issued and the other did not is counted for both by hand.
+    __syncthreads();
+    cluster_barrier();
+    if (warp == kMmaWarp && lane == 0) mbar_wait_drain(fin_bar, 0, a.status);
+    if (rank == 0 && warp == kLoadWarp && lane == 0) {
+        const uint32_t mine = (uint32_t)lds_s32(issued_at);
+        uint32_t other;
+        asm volatile("ld.shared::cluster.u32 %0, [%1];\n"
+                     : "=r"(other)
+                     : "r"(cluster_map(issued_at, 1))
+                     : "memory");
+        const uint32_t most = mine > other ? mine : other;
+        const uint32_t one = kOperandBytes + (uint32_t)a.bn / 2 * kKB * 2;
+        for (uint32_t j = most > kStages ? most - kStages : 0; j < most; ++j) {
+            const uint32_t bar = full_bar(j % kStages);
+            if (j >= mine)
+                mbar_arrive_expect_tx(bar, one);
+            else if (j >= other)
+                asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;\n" ::"r"(
+                                 bar),
+                             "r"(one)
+                             : "memory");
+            mbar_wait_drain(bar, (j / kStages) & 1, a.status);
+        }
+    }
+    __syncwarp();
+    cluster_barrier();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem_base),
+                     "r"(512)
+                     : "memory");
+    }
+}
+
+// ---------------------------------------------------------------- joins
+// The pairs of a row -> loss and lse: 32 rows a block, every 32nd pair a warp,
+// then the warps in order.
+__global__ void __launch_bounds__(1024)
+    xent_loss_kernel(const Rows r, const float2* __restrict__ pairs, int halves, long long mpad,
+                     float* loss, float* lse) {
+    __shared__ float2 sh[32][32];
+    pdl_wait();
+    pdl_trigger();
+    const int M = *r.m, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float least = -__int_as_float(0x7f800000);
+    // (top, sum) and another pair as one; tops of -infinity hold nothing, a NaN stays
+    auto join = [&](float2 a, float2 b) {
+        const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
+        return make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
+    };
+    for (long long row0 = blockIdx.x * 32ll; row0 < M; row0 += gridDim.x * 32ll) {
+        const long long row = row0 + lane;
+        float2 p = make_float2(least, 0.f);
+        if (row < M) {
+#pragma unroll 4
+            for (int h = warp; h < halves; h += 32) p = join(p, pairs[h * mpad + row]);
+        }
+        __syncthreads();
+        sh[warp][lane] = p;
+        __syncthreads();
+        if (warp == 0 && row < M) {
+            for (int w = 1; w < 32; ++w) p = join(p, sh[w][lane]);
+            const float all = p.x + logf(p.y);
+            const int n = r.token_of[row];
+            if (lse) lse[n] = all;
+            if (loss) loss[n] = all - r.at_target[row];
+        }
+    }
+}
+
+// dx from the slabs of its row, zero for tokens that take no part.
+template <typename T>
+__global__ void __launch_bounds__(256)
+    xent_input_kernel(const int32_t* count, long long capacity, const int* row_of,
+                      const float* __restrict__ slabs, int split, long long mpad, long long pitch,
+                      int C, T* dx, unsigned* status) {
+    pdl_wait();
+    pdl_trigger();
+    const long long rows = token_rows(count, capacity, status);
+    const int lane = threadIdx.x & 31;
+    for (long long n = (blockIdx.x * 256 + threadIdx.x) >> 5; n < rows; n += (long long)gridDim.x * 8) {
+        const int row = row_of[n];
+        for (int c = lane; c < C; c += 32) {
+            float v = 0.f;
+            if (row >= 0)
+                for (int s = 0; s < split; ++s) v += slabs[(s * mpad + row) * pitch + c];
+            dx[n * C + c] = from_f32<T>(v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host side
+// A 3-D map over [planes][rows][cols] elements, boxes of box_rows x 128 bytes
+// with 128-byte swizzle; what lies outside reads as zero and is not written.
+hc_status encode(CUtensorMap* m, CUtensorMapDataType type, const void* base, long long cols,
+                 long long rows, int planes, long long pitch, int box_rows) {
+    auto enc = tensor_map_encoder();
+    if (!enc) {
+        set_error("cuTensorMapEncodeTiled is unavailable");
+        return HC_ERR_CUDA;
+    }
+    const int e = type == CU_TENSOR_MAP_DATA_TYPE_FLOAT32 ? 4 : 2;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)(pitch * e), (cuuint64_t)(pitch * e * rows)};
+    cuuint32_t box[3] = {(cuuint32_t)(128 / e), (cuuint32_t)box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(m, type, 3, const_cast<void*>(base), dims, strides, box, estr,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_error("cuTensorMapEncodeTiled failed (%d)", (int)r);
+        return HC_ERR_CUDA;
+    }
+    return HC_OK;
+}
+constexpr CUtensorMapDataType kBf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+constexpr CUtensorMapDataType kF32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+
+template <Product kP, typename T>
+hc_status product(const DeviceCtx* ctx, const ProductArgs& a, long long units, const CUtensorMap& ma,
+                  const CUtensorMap& mb, const CUtensorMap& mo, cudaStream_t s) {
+    if (units > 0x7fffffffll) {
+        set_error("cross entropy: %lld tiles are too many", units);
+        return HC_ERR_UNSUPPORTED;
+    }
+    const long long pairs = ctx->num_sms / 2;
+    const unsigned grid = (unsigned)(2 * (units < 1 ? 1 : units < pairs ? units : pairs));
+    auto kern = xent_product_kernel<kP, T>;
+    static bool done[64];
+    if (!done[ctx->device]) {
+        const hc_status st = check_cuda(
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem),
+            "xent_product_kernel");
+        if (st != HC_OK) return st;
+        done[ctx->device] = true;
+    }
+    return launch_cluster(kern, grid, 2, kThreads, kSmem, s, "xent_product_kernel", a, ma, mb, mo);
+}
+
+long long up(long long v, long long to) {
+    return (v + to - 1) / to * to;
+}
+
+// The workspace of a call, laid out part by part: once to count, once to place.
+struct Layout {
+    uint8_t* base;
+    size_t used = 0;
+    template <typename P>
+    P* take(size_t n) {
+        P* const p = reinterpret_cast<P*>(base + used);
+        used = (used + n * sizeof(P) + 255) / 256 * 256;
+        return p;
+    }
+};
+
+template <typename T>
+struct Call {
+    static constexpr int kPlanes = sizeof(T) == 4 ? 3 : 1;
+    const DeviceCtx* ctx;
+    const LinearXentArgs& a;
+    cudaStream_t s;
+    long long mpad, pitch;
+    bool direct;         // the products read W where it is
+    Rows r{};
+    __nv_bfloat16* w = nullptr;
+
+    Call(const DeviceCtx* ctx_, const LinearXentArgs& a_, cudaStream_t s_) : ctx(ctx_), a(a_), s(s_) {
+        mpad = up(a.capacity < 1 ? 1 : a.capacity, kTile);
+        pitch = up(a.C, 8);
+        direct = kPlanes == 1 && a.C % 8 == 0 && (reinterpret_cast<uintptr_t>(a.W) & 15) == 0;
+    }
+    void rows(Layout& l, bool back) {
+        r.m = l.take<int>(1);
+        r.row_of = l.take<int>(mpad);
+        r.token_of = l.take<int>(mpad);
+        r.target = l.take<int>(mpad);
+        if (back) {
+            r.lse = l.take<float>(mpad);
+            r.dloss = l.take<float>(mpad);
+        } else {
+            r.at_target = l.take<float>(mpad);
+        }
+        r.x = l.take<__nv_bfloat16>((size_t)kPlanes * mpad * pitch);
+        if (!direct) w = l.take<__nv_bfloat16>((size_t)kPlanes * a.V * pitch);
+    }
+    hc_status gather(bool back) {
+        GatherArgs g{a.x, a.targets, a.count, a.capacity, mpad, a.C, a.V, pitch,
+                     back ? a.lse : nullptr, back ? a.dloss : nullptr, back ? nullptr : a.loss_out,
+                     back ? nullptr : a.lse_out, ctx->status};
+        const long long need = ((long long)a.capacity + 31) / 32, cap = 2ll * ctx->num_sms;
+        hc_status st = launch_pdl(xent_gather_kernel<T>,
+                                  dim3((unsigned)(need < 1 ? 1 : need < cap ? need : cap)),
+                                  dim3(kGatherThreads), 0, s, "xent_gather_kernel", g, r);
+        if (st != HC_OK || direct) return st;
+        const long long wneed = ((long long)a.V + 7) / 8, wcap = 8ll * ctx->num_sms;
+        return launch_pdl(xent_weight_kernel<T>, dim3((unsigned)(wneed < wcap ? wneed : wcap)),
+                          dim3(256), 0, s, "xent_weight_kernel", (const T*)a.W, a.V, a.C, pitch, w);
+    }
+    hc_status map_x(CUtensorMap* m, int box) {
+        return encode(m, kBf16, r.x, a.C, mpad, kPlanes, pitch, box);
+    }
+    hc_status map_w(CUtensorMap* m, int box) {
+        return encode(m, kBf16, direct ? a.W : (const void*)w, a.C, a.V, kPlanes,
+                      direct ? a.C : pitch, box);
+    }
+
+    hc_status forward() {
+        const int bn = a.V <= 64 ? 64 : a.V <= 128 ? 128 : 256;
+        const int halves = (int)up((a.V + bn / 2 - 1) / (bn / 2), 2);
+        float2* pairs = nullptr;
+        auto place = [&](Layout l) {
+            rows(l, false);
+            pairs = l.take<float2>((size_t)halves * mpad);
+            return l.used;
+        };
+        uint8_t* const ws = (uint8_t*)stream_workspace(s, place({nullptr}));
+        if (!ws) return HC_ERR_CUDA;
+        place({ws});
+        hc_status st = gather(false);
+        if (st != HC_OK) return st;
+        CUtensorMap mx, mw;
+        if ((st = map_x(&mx, kHalf)) != HC_OK || (st = map_w(&mw, bn / 2)) != HC_OK) return st;
+        ProductArgs p{};
+        p.m = r.m;
+        p.cols = a.V;
+        p.depth = a.C;
+        p.bn = bn;
+        p.split = 1;
+        p.planes = kPlanes;
+        p.V = a.V;
+        p.bias = a.bias;
+        p.target = r.target;
+        p.pairs = pairs;
+        p.at_target = r.at_target;
+        p.mpad = mpad;
+        p.status = ctx->status;
+        const long long units = mpad / kTile * ((a.V + (long long)bn - 1) / bn);
+        st = product<kStats, T>(ctx, p, units, mx, mw, mw, s);
+        if (st != HC_OK) return st;
+        const long long need = mpad / 32, cap = 2ll * ctx->num_sms;
+        return launch_pdl(xent_loss_kernel, dim3((unsigned)(need < cap ? need : cap)), dim3(1024), 0, s,
+                          "xent_loss_kernel", r, (const float2*)pairs,
+                          (int)(((long long)a.V + bn / 2 - 1) / (bn / 2)), mpad, a.loss_out, a.lse_out);
+    }
+
+    hc_status backward() {
+        // pieces of the vocabulary: G of one takes at most 512 MiB, or 2048 classes
+        const long long all = up(a.V, kTile);
+        long long most = (512ll << 20) / (mpad * 2 * kPlanes) / kTile * kTile;
+        if (most < 2048) most = 2048;
+        const long long pieces = (all + most - 1) / most;
+        const long long piece = up((all + pieces - 1) / pieces, kTile);
+        const long long xpitch = up(a.C, 4);
+        const int bn_v = a.V <= 128 ? 128 : 256, bn_c = a.C <= 128 ? 128 : 256;
+        const long long tiles = mpad / kTile * ((a.C + bn_c - 1) / bn_c);
+        // dx has few tiles with long sums: parts of them, 1024 classes at least
+        const int pairs = ctx->num_sms / 2;
+        long long split = (3 * pairs + tiles - 1) / tiles;
+        if (split > piece / 1024) split = piece / 1024;
+        if (split < 1 || !a.dx) split = 1;
+        __nv_bfloat16* G = nullptr;
+        float *slabs = nullptr, *part = nullptr;
+        auto place = [&](Layout l) {
+            rows(l, true);
+            G = l.take<__nv_bfloat16>((size_t)kPlanes * mpad * piece);
+            if (a.dx) slabs = l.take<float>((size_t)split * mpad * xpitch);
+            if (a.dbias) part = l.take<float>((size_t)(mpad / 32) * piece);
+            return l.used;
+        };
+        uint8_t* const ws = (uint8_t*)stream_workspace(s, place({nullptr}));
+        if (!ws) return HC_ERR_CUDA;
+        place({ws});
+        hc_status st = gather(true);
+        if (st != HC_OK) return st;
+        CUtensorMap mx, mw, mx_mn, mw_mn, mg, mg_mn, mg_out, mdx{}, mdw{};
+        const bool wide = (a.C * sizeof(T)) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.dW) & 15) == 0;
+        if ((st = map_x(&mx, kHalf)) != HC_OK || (st = map_w(&mw, bn_v / 2)) != HC_OK ||
+            (st = map_x(&mx_mn, kKB)) != HC_OK || (st = map_w(&mw_mn, kKB)) != HC_OK ||
+            (st = encode(&mg, kBf16, G, piece, mpad, kPlanes, piece, kHalf)) != HC_OK ||
+            (st = encode(&mg_mn, kBf16, G, piece, mpad, kPlanes, piece, kKB)) != HC_OK ||
+            (st = encode(&mg_out, kBf16, G, piece, mpad, kPlanes, piece, 32)) != HC_OK)
+            return st;
+        if (a.dx && (st = encode(&mdx, kF32, slabs, a.C, mpad, (int)split, xpitch, 32)) != HC_OK) return st;
+        if (a.dW && wide &&
+            (st = encode(&mdw, sizeof(T) == 4 ? kF32 : kBf16, a.dW, a.C, a.V, 1, a.C, 32)) != HC_OK)
+            return st;
+        ProductArgs p{};
+        p.m = r.m;
+        p.planes = kPlanes;
+        p.V = a.V;
+        p.bias = a.bias;
+        p.target = r.target;
+        p.lse = r.lse;
+        p.dloss = r.dloss;
+        p.dbias_part = part;
+        p.mpad = mpad;
+        p.piece = piece;
+        p.dw = a.dW;
+        p.wide = wide;
+        p.status = ctx->status;
+        for (long long v0 = 0; v0 < a.V; v0 += piece) {
+            const int classes = (int)(a.V - v0 < piece ? a.V - v0 : piece);
+            p.v0 = (int)v0;
+            p.cols = classes;
+            p.depth = a.C;
+            p.bn = bn_v;
+            p.split = 1;
+            st = product<kGrad, T>(ctx, p, mpad / kTile * ((classes + bn_v - 1) / bn_v), mx, mw, mg_out, s);
+            if (st != HC_OK) return st;
+            if (a.dbias) {
+                st = launch_column_sum(part, (int)(mpad / 32), piece, classes, a.dbias + v0, s, r.m);
+                if (st != HC_OK) return st;
+            }
+            p.bn = bn_c;
+            p.cols = a.C;
+            if (a.dx) {
+                p.depth = classes;
+                p.split = (int)split;
+                p.add = v0 > 0;
+                st = product<kInput, T>(ctx, p, tiles * split, mg, mw_mn, mdx, s);
+                if (st != HC_OK) return st;
+            }
+            if (a.dW) {
+                p.rows = classes;
+                p.split = 1;
+                const long long units = ((long long)classes + kTile - 1) / kTile * ((a.C + bn_c - 1) / bn_c);
+                st = product<kWeight, T>(ctx, p, units, mg_mn, mx_mn, mdw, s);
+                if (st != HC_OK) return st;
+            }
+        }
+        if (!a.dx || a.capacity == 0) return HC_OK;
+        const long long need = ((long long)a.capacity + 7) / 8, cap = 8ll * ctx->num_sms;
+        return launch_pdl(xent_input_kernel<T>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0,
+                          s, "xent_input_kernel", a.count, (long long)a.capacity, (const int*)r.row_of,
+                          (const float*)slabs, (int)split, mpad, xpitch, a.C, (T*)a.dx, ctx->status);
+    }
+};
+
+}  // namespace
+
+hc_status launch_linear_xent_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
+    return a.dt == HC_BF16 ? Call<__nv_bfloat16>(ctx, a, s).forward() : Call<float>(ctx, a, s).forward();
+}
+
+hc_status launch_linear_xent_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
+    return a.dt == HC_BF16 ? Call<__nv_bfloat16>(ctx, a, s).backward() : Call<float>(ctx, a, s).backward();
+}
+
+}  // namespace hc

@@ -38,7 +38,8 @@ EXPORTS = ("hc_mask_compact", "hc_mask_compact_static", "hc_sparse_spiral_conv_f
            "hc_sparse_conv_rulebook_bwd", "hc_scatter_dense", "hc_spiral_conv_fwd",
            "hc_layer_norm_fwd", "hc_layer_norm_bwd", "hc_rms_norm_fwd", "hc_rms_norm_bwd", "hc_embedding_fwd", "hc_embedding_sort",
            "hc_embedding_bwd", "hc_quantize_fp8_rows", "hc_quantize_fp8_weight",
-           "hc_fp8_linear_fwd", "hc_tensor_list_bytes", "hc_tensor_list_fill", "hc_grad_norm",
+           "hc_fp8_linear_fwd", "hc_linear_cross_entropy_fwd", "hc_linear_cross_entropy_bwd",
+           "hc_tensor_list_bytes", "hc_tensor_list_fill", "hc_grad_norm",
            "hc_grad_clip", "hc_get_device_status", "hc_test_set_option",
            "hc_last_error_string", "hc_version")
 
@@ -97,6 +98,8 @@ def load_library(path: str | None = None):
             "hc_quantize_fp8_rows": [P, I, P, I, I, P, P, P],
             "hc_quantize_fp8_weight": [P, I, I, I, P, P, P],
             "hc_fp8_linear_fwd": [P, P, P, I, I, I, P, P, P, I, I, P, P],
+            "hc_linear_cross_entropy_fwd": [P, P, I, P, P, P, I, I, I, P, P, P],
+            "hc_linear_cross_entropy_bwd": [P, P, I, P, P, P, P, P, I, I, I, P, P, P, P],
             "hc_tensor_list_bytes": [I],
             "hc_tensor_list_fill": [P, P, P, P, I, P, P, P],
             "hc_grad_norm": [P, P, P],
@@ -558,6 +561,44 @@ def hc_fp8_linear_fwd(xq, xs, wq, ws, bias, act, y, count=None, stream=None):
         _arg("wq", wq, (C_out, pitch), q8), _arg("ws", ws, ((C_out + 127) // 128, nb), f32),
         _arg("bias", bias, (C_out,), f32), act, _dt(y), _arg("y", y, (capacity, C_out), row),
         _s(stream)), "hc_fp8_linear_fwd")
+
+
+def hc_linear_cross_entropy_fwd(x, W, bias, targets, loss=None, lse=None, count=None,
+                                stream=None):
+    """loss[n] = log sum_v exp(l[v]) - l[targets[n]] with l = x[n] W^T + bias, and that
+    logarithm as lse[n]; 0 both for the target -1. x [capacity, C], W [V, C] of the
+    same type, bias fp32 [V] or None, targets int32 [capacity], loss and lse fp32
+    [capacity] (one may be None)."""
+    capacity, C = x.shape
+    V = W.shape[0]
+    if (capacity | C | V) >> 31:
+        _too_large(capacity, C, V)
+    f32, i32, _, row = _token_types()
+    _check(load_library().hc_linear_cross_entropy_fwd(
+        _arg("x", x, (capacity, C), row), _arg("W", W, (V, C), (x.dtype,)), _dt(x),
+        _arg("bias", bias, (V,), f32), _arg("targets", targets, (capacity,), i32),
+        _arg("count", count, (1,), i32), capacity, C, V, _arg("loss", loss, (capacity,), f32),
+        _arg("lse", lse, (capacity,), f32), _s(stream)), "hc_linear_cross_entropy_fwd")
+
+
+def hc_linear_cross_entropy_bwd(x, W, bias, targets, lse, dloss, dx=None, dW=None, dbias=None,
+                                count=None, stream=None):
+    """Gradients of hc_linear_cross_entropy_fwd: lse as it wrote it, dloss fp32
+    [capacity] the gradient of each token's loss; dx like x (may be x), dW like
+    W, dbias fp32 [V], or None each."""
+    capacity, C = x.shape
+    V = W.shape[0]
+    if (capacity | C | V) >> 31:
+        _too_large(capacity, C, V)
+    f32, i32, _, row = _token_types()
+    same = (x.dtype,)
+    _check(load_library().hc_linear_cross_entropy_bwd(
+        _arg("x", x, (capacity, C), row), _arg("W", W, (V, C), same), _dt(x),
+        _arg("bias", bias, (V,), f32), _arg("targets", targets, (capacity,), i32),
+        _arg("lse", lse, (capacity,), f32), _arg("dloss", dloss, (capacity,), f32),
+        _arg("count", count, (1,), i32), capacity, C, V, _arg("dx", dx, (capacity, C), same),
+        _arg("dW", dW, (V, C), same), _arg("dbias", dbias, (V,), f32), _s(stream)),
+        "hc_linear_cross_entropy_bwd")
 
 
 class hc_tensor_list(ctypes.Structure):
