@@ -122,6 +122,12 @@ __device__ __forceinline__ double block_sum_f64(double v, double* sh) {
     return v;
 }
 
+// Whether units u .. u + n - 1 lie wholly inside their tensor.
+__device__ __forceinline__ bool inside(const Entry& e, long long u, int n) {
+    const long long at = (u - e.first) * kUnit - e.off;
+    return at >= 0 && at + (long long)n * kUnit <= e.numel;
+}
+
 // The block's units [first, last): part[blockIdx.x] = the sum of their squares.
 __global__ void __launch_bounds__(kThreads, 2)
     sum_squares_kernel(const Entry* __restrict__ table, int n, long long units,
@@ -132,19 +138,53 @@ __global__ void __launch_bounds__(kThreads, 2)
     const long long u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
     float hi = 0.f, lo = 0.f;
     double far = 0.0;  // squares that fp32 does not hold
-    int t = u0 < u1 ? find_entry(table, n, u0) : 0;
+    if (u0 >= u1) {
+        if (threadIdx.x == 0) part[blockIdx.x] = 0.0;
+        return;
+    }
+    int t = find_entry(table, n, u0);
+    Entry e = table[t];
+    long long end = table[t + 1].first;
     for (long long u = u0; u < u1; u += kAhead) {
         Elems r[kAhead];
         bool bf16[kAhead];
+        while (end <= u) {
+            e = table[++t];
+            end = table[t + 1].first;
+        }
+        if (u + kAhead <= u1 && inside(e, u, kAhead)) {
+            // the rule: no look at the ends, all loads at once
+            if (e.dt == HC_BF16) {
+                const uint4* const at = reinterpret_cast<const uint4*>(
+                    static_cast<const __nv_bfloat16*>(e.in) + piece_at(e, u, 0));
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            bf16[k] = true;
-            r[k].a[0] = make_uint4(0u, 0u, 0u, 0u);
-            if (u + k < u1) {
-                while (table[t + 1].first <= u + k) ++t;
-                const Entry e = table[t];
-                bf16[k] = e.dt == HC_BF16;
-                r[k] = load_unit(e, u + k);
+                for (int k = 0; k < kAhead; ++k) {
+                    bf16[k] = true;
+                    r[k].a[0] = at[k * kThreads];
+                }
+            } else {
+                const uint4* const at = reinterpret_cast<const uint4*>(
+                    static_cast<const float*>(e.in) + piece_at(e, u, 0));
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) {
+                    bf16[k] = false;
+                    r[k].a[0] = at[2 * k * kThreads];
+                    r[k].a[1] = at[(2 * k + 1) * kThreads];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                bf16[k] = true;
+                r[k].a[0] = make_uint4(0u, 0u, 0u, 0u);
+                if (u + k < u1) {
+                    while (end <= u + k) {
+                        e = table[++t];
+                        end = table[t + 1].first;
+                    }
+                    bf16[k] = e.dt == HC_BF16;
+                    r[k] = load_unit(e, u + k);
+                }
             }
         }
         F2 s = make_f2(0.f, 0.f);
@@ -189,6 +229,27 @@ __global__ void __launch_bounds__(kThreads)
     if (threadIdx.x == 0) *norm = (float)sqrt(v);
 }
 
+// kAhead units wholly inside a tensor, input and output aligned alike.
+template <typename T>
+__device__ __forceinline__ void scale_units(const Entry& e, long long u, float scale) {
+    constexpr int V = 16 / (int)sizeof(T), kPieces = kPer / V;
+    const long long at = piece_at(e, u, 0);
+    const T* const in = static_cast<const T*>(e.in) + at;
+    T* const out = static_cast<T*>(e.out) + at;
+    Piece<T, V> p[kAhead * kPieces];
+#pragma unroll
+    for (int k = 0; k < kAhead * kPieces; ++k) p[k].load(in + k * kThreads * V);
+#pragma unroll
+    for (int k = 0; k < kAhead * kPieces; ++k) {
+        float f[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = p[k].get(i) * scale;
+        p[k].set_all(f);
+        p[k].store(out + k * kThreads * V);
+    }
+}
+
+// The same units as sum_squares_kernel's block, from the last one down.
 __global__ void __launch_bounds__(kThreads, 2)
     scale_kernel(const Entry* __restrict__ table, int n, long long units, const float* norm,
                  float max_norm) {
@@ -197,16 +258,30 @@ __global__ void __launch_bounds__(kThreads, 2)
     const float size = *norm;
     const float scale = size <= max_norm ? 1.f : max_norm / size;  // a NaN passes
     const long long u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
-    int t = u0 < u1 ? find_entry(table, n, u1 - 1) : 0;
-    for (long long u = u1 - 1; u >= u0; u -= kAhead) {
+    if (u0 >= u1) return;
+    int t = find_entry(table, n, u1 - 1);
+    Entry e = table[t];
+    auto wide = [](const Entry& e) {
+        return ((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15) == 0;
+    };
+    for (long long u = u1 - 1; u >= u0; u -= kAhead) {  // u and the ones below
+        while (e.first > u) e = table[--t];
+        const long long lo = u - (kAhead - 1);
+        if (lo >= u0 && lo >= e.first && inside(e, lo, kAhead) && wide(e)) {
+            if (scale == 1.f && e.in == e.out) continue;
+            if (e.dt == HC_BF16)
+                scale_units<__nv_bfloat16>(e, lo, scale);
+            else
+                scale_units<float>(e, lo, scale);
+            continue;
+        }
         Elems r[kAhead];
         int at[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             at[k] = -1;
             if (u - k >= u0) {
-                while (table[t].first > u - k) --t;
-                const Entry e = table[t];
+                while (e.first > u - k) e = table[--t];
                 if (scale != 1.f || e.in != e.out) {
                     at[k] = t;
                     r[k] = load_unit(e, u - k);
@@ -216,27 +291,25 @@ __global__ void __launch_bounds__(kThreads, 2)
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (at[k] < 0) continue;
-            const Entry e = table[at[k]];
-            const bool bf16 = e.dt == HC_BF16;
+            const Entry o = table[at[k]];
+            const bool bf16 = o.dt == HC_BF16;
             float f[kPer];
             as_floats(r[k], bf16, f);
 #pragma unroll
             for (int i = 0; i < kPer; ++i) f[i] *= scale;
-            const bool wide = ((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15) == 0;
             if (bf16) {
                 Piece<__nv_bfloat16, 8> p;
                 p.set_all(f);
-                store_piece(static_cast<__nv_bfloat16*>(e.out), piece_at(e, u - k, 0), e.numel, p.v,
-                            wide);
+                store_piece(static_cast<__nv_bfloat16*>(o.out), piece_at(o, u - k, 0), o.numel, p.v,
+                            wide(o));
             } else {
-                float* const o = static_cast<float*>(e.out);
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    store_piece(o, piece_at(e, u - k, j), e.numel,
+                    store_piece(static_cast<float*>(o.out), piece_at(o, u - k, j), o.numel,
                                 make_uint4(__float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]),
                                            __float_as_uint(f[4 * j + 2]),
                                            __float_as_uint(f[4 * j + 3])),
-                                wide);
+                                wide(o));
             }
         }
     }

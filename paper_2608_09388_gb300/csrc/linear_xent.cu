@@ -150,9 +150,11 @@ __global__ void __launch_bounds__(kGatherThreads)
             const T* const from = x + (long long)token[j] * a.C;
             __nv_bfloat16* const to = r.x + (at + j) * a.pitch;
             if (wide && kPlanes == 1) {
+#pragma unroll 4
                 for (int c = lane * 8; c < a.C; c += 256)
                     *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(from + c);
             } else {
+#pragma unroll 4
                 for (int c = lane; c < a.C; c += 32) {
                     __nv_bfloat16 p[3];
                     if constexpr (kPlanes == 1)
@@ -188,6 +190,7 @@ __global__ void __launch_bounds__(256)
     pdl_trigger();
     const int warp = (int)((blockIdx.x * 256 + threadIdx.x) >> 5), lane = threadIdx.x & 31;
     for (long long v = warp; v < V; v += (long long)gridDim.x * 8)
+#pragma unroll 4
         for (int c = lane; c < C; c += 32) {
             __nv_bfloat16 p[3];
             if constexpr (kPlanes == 1)
@@ -204,7 +207,7 @@ enum Product {
     kStats,   // x W^T -> the pairs of the forward pass
     kGrad,    // x W^T -> G of a piece
     kInput,   // G W -> fp32 slabs of dx
-    kWeight,  // G^T x -> rows of dW
+    kWeight,  // G^T x -> rows of dW, or fp32 slabs of them
 };
 
 constexpr int kTile = 256;                       // rows of a tile, 128 in each CTA
@@ -219,6 +222,10 @@ constexpr int kMmaWarp = kStoreWarps + 1;
 constexpr int kThreads = (kStoreWarps + 2) * 32;
 constexpr int kOutBytes = 32 * 128;              // staging of a storing warp
 constexpr int kGroupM = 16;                      // row tiles walked per column of tiles
+// fp32 operands: blocks of the sum behind which the accumulator is added to
+// fp32 registers. The tensor cores truncate at every step of 16, always
+// towards zero: 784 steps at full size left 1.7e-5 of a weight's gradient.
+constexpr int kChain = 4;
 constexpr int kBars = 2 * kStages + 5;
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreWarps * kOutBytes + kBars * 8 + 64;
 
@@ -228,7 +235,7 @@ struct ProductArgs {
     int cols;            // columns of the result
     int depth;           // length of the sum (kWeight: *m)
     int bn;              // columns of a tile: 64 (kStats), 128 or 256
-    int split;           // kInput: parts of the sum
+    int split;           // kInput, kWeight: parts of the sum, a slab of the result each
     int planes;          // 1, or 3: six products a block
     int v0, V;           // first class of the piece, classes in all
     const float* bias;
@@ -337,6 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const __grid_constant__ CUtensorMap map_b,
                         const __grid_constant__ CUtensorMap map_out) {
     constexpr bool kAMn = kP == kWeight, kBMn = kP == kInput || kP == kWeight;
+    constexpr bool kPromote = sizeof(T) == 4;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -397,12 +405,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int products = a.planes == 1 ? 1 : 6;
     const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
 
-    // Unit u: its tile, and its blocks [k0, k1) of the sum.
+    // Unit u: its tile, and its blocks [k0, k1) of the sum, taken in chains.
     auto unit_at = [&](uint32_t u, int& m, int& n, int& part, int& k0, int& k1) {
         part = 0;
         k0 = 0;
         k1 = blocks;
-        if constexpr (kP == kInput) {
+        if constexpr (kP == kInput || kP == kWeight) {
             const uint32_t tiles = tm * tn;
             part = (int)(u / tiles);
             u -= (uint32_t)part * tiles;
@@ -427,9 +435,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             int m, n, part, k0, k1;
             unit_at(u, m, n, part, k0, k1);
             const int row = m * kTile + (int)rank * kHalf, col = n * a.bn + (int)rank * a.bn / 2;
+            const int chain = kPromote ? kChain : k1 - k0;
+            for (int kc = k0; kc < k1 && ok; kc += chain)
             for (int p = 0; p < products && ok; ++p) {
                 const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
-                for (int k = k0; k < k1; ++k, ++issued) {
+                const int end = k1 - kc < chain ? k1 : kc + chain;
+                for (int k = kc; k < end; ++k, ++issued) {
                     const uint32_t s = issued % kStages;
                     ok = wait_bar(empty_bar(s), ((issued / kStages) & 1) ^ 1u, abort_flag, a.status,
                                   limit);
@@ -467,34 +478,42 @@ __global__ void __launch_bounds__(kThreads, 1)
                                    ((uint32_t)(kTile >> 4) << 24);
             uint32_t it = 0, tile = 0;
             bool ok = true;
-            for (uint32_t u = first; u < units && ok; u += step, ++tile) {
+            for (uint32_t u = first; u < units && ok; u += step) {
                 int m, n, part, k0, k1;
                 unit_at(u, m, n, part, k0, k1);
-                const uint32_t b = tile & 1;
-                ok = wait_bar(tempty_bar(b), ((tile >> 1) & 1) ^ 1u, abort_flag, a.status, limit);
-                if (!ok) break;
-                tc_fence_after();
-                const int total = (k1 - k0) * products;
-                for (int k = 0; k < total; ++k, ++it) {
-                    const uint32_t s = it % kStages;
-                    ok = wait_bar(full_bar(s), (it / kStages) & 1, abort_flag, a.status, limit);
+                const int chain = kPromote ? kChain : k1 - k0;
+                int kc = k0;
+                do {  // an empty sum of bf16 operands still passes its accumulator on
+                    if (kPromote && kc >= k1) break;
+                    const uint32_t b = tile & 1;
+                    ok = wait_bar(tempty_bar(b), ((tile >> 1) & 1) ^ 1u, abort_flag, a.status, limit);
                     if (!ok) break;
                     tc_fence_after();
-                    if (leader) {
-                        const uint32_t sa = base + s * kStageBytes;
-                        const uint64_t da = desc_sw128(sa, kAMn ? kOperandBytes / 2 : 16);
-                        const uint64_t db = desc_sw128(sa + kOperandBytes, kBMn ? kOperandBytes / 2 : 16);
+                    const int total = (k1 - kc < chain ? k1 - kc : chain) * products;
+                    for (int k = 0; k < total; ++k, ++it) {
+                        const uint32_t s = it % kStages;
+                        ok = wait_bar(full_bar(s), (it / kStages) & 1, abort_flag, a.status, limit);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (leader) {
+                            const uint32_t sa = base + s * kStageBytes;
+                            const uint64_t da = desc_sw128(sa, kAMn ? kOperandBytes / 2 : 16);
+                            const uint64_t db =
+                                desc_sw128(sa + kOperandBytes, kBMn ? kOperandBytes / 2 : 16);
 #pragma unroll
-                        for (int j = 0; j < kKB / 16; ++j)  // 16 elements of the sum further on
-                            mma_pair(tmem_base + b * 256u, da + (kAMn ? 128 : 2) * j,
-                                     db + (kBMn ? 128 : 2) * j, idesc, (k | j) != 0 ? 1u : 0u);
-                        commit_pair(empty_bar(s));
+                            for (int j = 0; j < kKB / 16; ++j)  // 16 elements of the sum further on
+                                mma_pair(tmem_base + b * 256u, da + (kAMn ? 128 : 2) * j,
+                                         db + (kBMn ? 128 : 2) * j, idesc, (k | j) != 0 ? 1u : 0u);
+                            commit_pair(empty_bar(s));
+                        }
+                        __syncwarp();
                     }
+                    if (!ok) break;
+                    if (leader) commit_pair(tfull_bar(b));
                     __syncwarp();
-                }
-                if (!ok) break;
-                if (leader) commit_pair(tfull_bar(b));
-                __syncwarp();
+                    ++tile;
+                    kc += chain;
+                } while (kc < k1);
             }
             // every product issued here, and every arrival before this one, has
             // completed once fin_bar fires, in both CTAs
@@ -505,26 +524,62 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int quarter = warp & 3, half = warp >> 2, hc = a.bn / 2;
         const uint32_t stage = out_at + (uint32_t)warp * kOutBytes;
         uint32_t tile = 0;
-        for (uint32_t u = first; u < units; u += step, ++tile) {
+        bool ok = true;
+        for (uint32_t u = first; u < units; u += step) {
             int m, n, part, k0, k1;
             unit_at(u, m, n, part, k0, k1);
-            const uint32_t b = tile & 1;
-            const bool ok = wait_bar(tfull_bar(b), (tile >> 1) & 1, abort_flag, a.status, limit);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * 256u + half * hc;
-            const uint32_t tempty = cluster_map(tempty_bar(b), 0);
-            // 32 columns of this lane's row
-            auto load = [&](int c, float (&f)[32]) {
-                uint32_t r[32];
-                tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
-                tmem_ld_wait();
-                if (c + 32 >= hc) {
-                    tc_fence_before();
-                    if (lane == 0) arrive_cluster(tempty);
-                }
+            // the next accumulator: where it is, and the barrier that gives it back
+            uint32_t acc = 0, tempty = 0;
+            auto next = [&] {
+                const uint32_t b = tile & 1;
+                ok = wait_bar(tfull_bar(b), (tile >> 1) & 1, abort_flag, a.status, limit);
+                tc_fence_after();
+                acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * 256u + half * hc;
+                tempty = cluster_map(tempty_bar(b), 0);
+                ++tile;
+            };
+            float sums[kPromote ? 128 : 1];  // of this lane's row
+            if constexpr (kPromote) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) f[i] = k1 > k0 ? __uint_as_float(r[i]) : 0.f;
+                for (int i = 0; i < 128; ++i) sums[i] = 0.f;
+                for (int kc = k0; kc < k1 && ok; kc += kChain) {
+                    next();
+                    if (!ok) break;
+#pragma unroll
+                    for (int c = 0; c < 128; c += 32) {
+                        if (c >= hc) break;
+                        uint32_t r[32];
+                        tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
+                        tmem_ld_wait();
+                        if (c + 32 >= hc) {
+                            tc_fence_before();
+                            if (lane == 0) arrive_cluster(tempty);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sums[c + i] += __uint_as_float(r[i]);
+                    }
+                }
+            } else {
+                next();
+            }
+            if (!ok) break;
+            // 32 columns of this lane's row
+            constexpr int kCols = 128;
+            auto load = [&](int c, float (&f)[32]) {
+                if constexpr (kPromote) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = sums[c + i];
+                } else {
+                    uint32_t r[32];
+                    tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
+                    tmem_ld_wait();
+                    if (c + 32 >= hc) {
+                        tc_fence_before();
+                        if (lane == 0) arrive_cluster(tempty);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = k1 > k0 ? __uint_as_float(r[i]) : 0.f;
+                }
             };
             const int row0 = m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
             const int col0 = n * a.bn + half * hc;
@@ -544,7 +599,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (kP == kStats) {
                 const int target = row < M ? a.target[row] - a.v0 : -1;
                 float top = -__int_as_float(0x7f800000), sum = 0.f;
-                for (int c = 0; c < hc; c += 32) {
+#pragma unroll(kPromote ? 4 : 1)
+                for (int c = 0; c < kCols; c += 32) {
+                    if (c >= hc) break;
                     float f[32];
                     load(c, f);
                     const int col = col0 + c;
@@ -583,7 +640,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const bool in = row < M;
                 const float lse = in ? a.lse[row] : 0.f, dloss = in ? a.dloss[row] : 0.f;
                 const int target = in ? a.target[row] - a.v0 : -1;
-                for (int c = 0; c < hc; c += 64) {
+#pragma unroll(kPromote ? 2 : 1)
+                for (int c = 0; c < kCols; c += 64) {
+                    if (c >= hc) break;
                     float f[64];
 #pragma unroll
                     for (int h = 0; h < 64; h += 32) {
@@ -623,9 +682,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                         send(col0 + c, row0, k, false);
                     }
                 }
-            } else if constexpr (kP == kInput || sizeof(T) == 4) {
+            } else if (kP == kInput || sizeof(T) == 4 || a.split > 1) {
                 // fp32 results, 32 columns at a time
-                for (int c = 0; c < hc; c += 32) {
+                const bool slab = kP == kInput || a.split > 1;
+#pragma unroll(kPromote ? 4 : 1)
+                for (int c = 0; c < kCols; c += 32) {
+                    if (c >= hc) break;
                     float f[32];
                     load(c, f);
                     staging_free();
@@ -634,8 +696,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         put(q, make_uint4(__float_as_uint(f[4 * q]), __float_as_uint(f[4 * q + 1]),
                                           __float_as_uint(f[4 * q + 2]), __float_as_uint(f[4 * q + 3])));
                     const int col = col0 + c;
-                    if (kP == kInput) {
-                        if (col < a.cols) send(col, row0, part, a.add);
+                    if (slab) {
+                        if (col < a.cols) send(col, row0, part, kP == kInput && a.add);
                     } else if (a.wide) {
                         if (col < a.cols && row0 < rows) send(col, a.v0 + row0, 0, false);
                     } else {
@@ -727,6 +789,131 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
+// ---------------------------------------------------------------- few tokens
+// Up to kFew tokens (a scoring or decoding step): bound by the one read of W,
+// so the sums are taken on the CUDA cores straight from the rows as they are. A
+// warp takes kFewRows classes at a time, 16 bytes of each a lane, against the
+// tokens' rows in shared memory (fp32; the 16-byte pieces of a lane's channels
+// lie 512 bytes apart, so that neither side has bank conflicts).
+constexpr int kFew = 4;
+constexpr int kFewThreads = 256;
+constexpr int kFewRows = 4;
+
+template <typename T, int VEC>
+__device__ __forceinline__ int few_at(int c) {
+    if (VEC < 8) return c;
+    return (c & ~255) + (c & 4) * 32 + ((c & 255) >> 3) * 4 + (c & 3);
+}
+
+template <typename T, int VEC, int kTokens>
+__global__ void __launch_bounds__(kFewThreads)
+    xent_few_kernel(const T* __restrict__ x, const T* __restrict__ W, const float* __restrict__ bias,
+                    const int32_t* targets, int C, int V, float2* __restrict__ pairs,
+                    float* __restrict__ at_target) {
+    extern __shared__ __align__(16) float rows[];  // [kTokens][up to a multiple of 256]
+    __shared__ float2 sh[kFewThreads / 32][kTokens];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int pitch = (C + 255) & ~255;
+    const float least = -__int_as_float(0x7f800000);
+    pdl_wait();
+    pdl_trigger();
+    int target[kTokens];
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) {
+        target[t] = targets[t];
+        for (int c = threadIdx.x; c < C; c += kFewThreads)
+            rows[t * pitch + few_at<T, VEC>(c)] = to_f32(x[(long long)t * C + c]);
+    }
+    __syncthreads();
+    float2 all[kTokens];
+#pragma unroll
+    for (int t = 0; t < kTokens; ++t) all[t] = make_float2(least, 0.f);
+    const long long step = (long long)gridDim.x * (kFewThreads / 32) * kFewRows;
+    for (long long v0 = ((long long)blockIdx.x * (kFewThreads / 32) + warp) * kFewRows; v0 < V; v0 += step) {
+        float s[kFewRows][kTokens] = {};
+        const T* w[kFewRows];
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r) w[r] = W + (v0 + r < V ? v0 + r : v0) * C;
+#pragma unroll 4
+        for (int c = lane * VEC; c < C; c += 32 * VEC) {
+            Piece<T, VEC> p[kFewRows];
+#pragma unroll
+            for (int r = 0; r < kFewRows; ++r) p[r].load(w[r] + c);
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) {
+                float f[VEC];
+                if constexpr (VEC == 1) {
+                    f[0] = rows[t * pitch + c];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < VEC; e += 4) {
+                        const float4 q = *reinterpret_cast<const float4*>(rows + t * pitch + few_at<T, VEC>(c + e));
+                        f[e] = q.x, f[e + 1] = q.y, f[e + 2] = q.z, f[e + 3] = q.w;
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < kFewRows; ++r)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) s[r][t] = fmaf(p[r].get(e), f[e], s[r][t]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kFewRows; ++r) {
+            if (v0 + r >= V) break;
+            const float b = bias ? __ldg(bias + v0 + r) : 0.f;
+#pragma unroll
+            for (int t = 0; t < kTokens; ++t) {
+                const float l = warp_sum(s[r][t]) + b;
+                if (lane == 0 && v0 + r == target[t]) at_target[t] = l;
+                const float top = fmaxf(all[t].x, l), from = top == least ? 0.f : top;
+                all[t] = make_float2(top, all[t].y * ex2((all[t].x - from) * kLog2e) + ex2((l - from) * kLog2e));
+            }
+        }
+    }
+    if (lane == 0)
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) sh[warp][t] = all[t];
+    __syncthreads();
+    if (threadIdx.x < kTokens) {
+        float2 a = sh[0][threadIdx.x];
+        for (int w = 1; w < kFewThreads / 32; ++w) {
+            const float2 b = sh[w][threadIdx.x];
+            const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
+            a = make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
+        }
+        pairs[(long long)blockIdx.x * kFew + threadIdx.x] = a;
+    }
+}
+
+// The blocks' pairs of a token -> loss and lse, a warp per token.
+__global__ void __launch_bounds__(kFew * 32)
+    xent_few_join_kernel(const int32_t* count, long long capacity, const int32_t* targets, int V,
+                         const float2* __restrict__ pairs, int blocks, const float* at_target, float* loss,
+                         float* lse, unsigned* status) {
+    pdl_wait();
+    pdl_trigger();
+    const float least = -__int_as_float(0x7f800000);
+    const int n = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (n >= token_rows(count, capacity, status)) return;
+    const int t = targets[n];
+    const bool in = t >= 0 && t < V;
+    if (!in && t != -1 && lane == 0) report(status, kErrIndex);
+    auto join = [&](float2 a, float2 b) {
+        const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
+        return make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
+    };
+    float2 p = make_float2(least, 0.f);
+#pragma unroll 4
+    for (int b = lane; b < blocks; b += 32) p = join(p, pairs[(long long)b * kFew + n]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        p = join(p, make_float2(__shfl_xor_sync(0xffffffffu, p.x, o), __shfl_xor_sync(0xffffffffu, p.y, o)));
+    if (lane != 0) return;
+    const float all = p.x + logf(p.y);
+    if (lse) lse[n] = in ? all : 0.f;
+    if (loss) loss[n] = in ? all - at_target[n] : 0.f;
+}
+
 // ---------------------------------------------------------------- joins
 // The pairs of a row -> loss and lse: 32 rows a block, every 32nd pair a warp,
 // then the warps in order.
@@ -763,23 +950,45 @@ __global__ void __launch_bounds__(1024)
     }
 }
 
-// dx from the slabs of its row, zero for tokens that take no part.
+// Rows of a result from its slabs. dx: the rows n < N', zero for tokens that
+// take no part; a piece of dW: all its rows. Four channels a lane.
 template <typename T>
 __global__ void __launch_bounds__(256)
-    xent_input_kernel(const int32_t* count, long long capacity, const int* row_of,
-                      const float* __restrict__ slabs, int split, long long mpad, long long pitch,
-                      int C, T* dx, unsigned* status) {
+    xent_slabs_kernel(const int32_t* count, long long capacity, const int* row_of,
+                      const float* __restrict__ slabs, int split, long long slab_rows, long long pitch,
+                      int C, bool wide, T* out, unsigned* status) {
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
-    const int lane = threadIdx.x & 31;
-    for (long long n = (blockIdx.x * 256 + threadIdx.x) >> 5; n < rows; n += (long long)gridDim.x * 8) {
-        const int row = row_of[n];
-        for (int c = lane; c < C; c += 32) {
-            float v = 0.f;
-            if (row >= 0)
-                for (int s = 0; s < split; ++s) v += slabs[(s * mpad + row) * pitch + c];
-            dx[n * C + c] = from_f32<T>(v);
+    // a row's pieces of 128 channels, one after another
+    const int lane = threadIdx.x & 31, per = (C + 127) / 128;
+    const long long step = (long long)gridDim.x * 8;
+    for (long long i = (blockIdx.x * 256 + threadIdx.x) >> 5; i < rows * per; i += step) {
+        int k;
+        const long long n = div32(i, per, k);
+        const int c = k * 128 + lane * 4;
+        const long long row = row_of ? row_of[n] : n;
+        if (c >= C) continue;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (row >= 0) {
+#pragma unroll 4
+            for (int s = 0; s < split; ++s) {
+                const float4 f = *reinterpret_cast<const float4*>(slabs + (s * slab_rows + row) * pitch + c);
+                v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+            }
+        }
+        T* const to = out + n * C + c;
+        if (wide) {
+            if constexpr (sizeof(T) == 4)
+                *reinterpret_cast<float4*>(to) = v;
+            else
+                *reinterpret_cast<uint2*>(to) = make_uint2(Piece<__nv_bfloat16, 8>::pair(v.x, v.y),
+                                                           Piece<__nv_bfloat16, 8>::pair(v.z, v.w));
+        } else {
+            const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c + e < C) to[e] = from_f32<T>(f[e]);
         }
     }
 }
@@ -882,7 +1091,7 @@ struct Call {
         GatherArgs g{a.x, a.targets, a.count, a.capacity, mpad, a.C, a.V, pitch,
                      back ? a.lse : nullptr, back ? a.dloss : nullptr, back ? nullptr : a.loss_out,
                      back ? nullptr : a.lse_out, ctx->status};
-        const long long need = ((long long)a.capacity + 31) / 32, cap = 2ll * ctx->num_sms;
+        const long long need = ((long long)a.capacity + 15) / 16, cap = 6ll * ctx->num_sms;
         hc_status st = launch_pdl(xent_gather_kernel<T>,
                                   dim3((unsigned)(need < 1 ? 1 : need < cap ? need : cap)),
                                   dim3(kGatherThreads), 0, s, "xent_gather_kernel", g, r);
@@ -899,7 +1108,51 @@ struct Call {
                       direct ? a.C : pitch, box);
     }
 
+    template <int VEC, int kTokens>
+    hc_status few_tokens(float2* pairs, float* at_target, int blocks) {
+        const size_t smem = (size_t)kTokens * ((a.C + 255) / 256 * 256) * 4;
+        return launch_pdl(xent_few_kernel<T, VEC, kTokens>, dim3((unsigned)blocks), dim3(kFewThreads), smem, s,
+                          "xent_few_kernel", (const T*)a.x, (const T*)a.W, a.bias, a.targets, a.C, a.V, pairs,
+                          at_target);
+    }
+    template <int VEC>
+    hc_status few_tokens(float2* pairs, float* at_target, int blocks) {
+        switch (a.capacity) {
+            case 1: return few_tokens<VEC, 1>(pairs, at_target, blocks);
+            case 2: return few_tokens<VEC, 2>(pairs, at_target, blocks);
+            case 3: return few_tokens<VEC, 3>(pairs, at_target, blocks);
+            default: return few_tokens<VEC, 4>(pairs, at_target, blocks);
+        }
+    }
+    hc_status forward_few() {
+        constexpr int kVec = 16 / (int)sizeof(T);
+        const long long need = ((long long)a.V + kFewRows * kFewThreads / 32 - 1) / (kFewRows * kFewThreads / 32);
+        const long long cap = 4ll * ctx->num_sms;
+        const int blocks = (int)(need < cap ? need : cap);
+        float2* const pairs = (float2*)stream_workspace(s, ((size_t)blocks * kFew + kFew) * sizeof(float2));
+        if (!pairs) return HC_ERR_CUDA;
+        float* const at_target = reinterpret_cast<float*>(pairs + (size_t)blocks * kFew);
+        const bool wide = a.C % kVec == 0 && (reinterpret_cast<uintptr_t>(a.W) & 15) == 0;
+        const hc_status st = wide ? few_tokens<kVec>(pairs, at_target, blocks) : few_tokens<1>(pairs, at_target, blocks);
+        if (st != HC_OK) return st;
+        return launch_pdl(xent_few_join_kernel, dim3(1), dim3(kFew * 32), 0, s, "xent_few_join_kernel", a.count,
+                          (long long)a.capacity, a.targets, a.V, (const float2*)pairs, blocks,
+                          (const float*)at_target, a.loss_out, a.lse_out, ctx->status);
+    }
+
+    // The rows of `out` from `split` slabs (row_of: dx, else a piece of dW).
+    hc_status join(const int32_t* count, long long rows_, const int* row_of, const float* slabs, int split,
+                   long long slab_rows, long long xpitch, T* out) {
+        const bool wide = a.C % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0;
+        const long long need = (rows_ * ((a.C + 127) / 128) + 7) / 8, cap = 8ll * ctx->num_sms;
+        return launch_pdl(xent_slabs_kernel<T>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0, s,
+                          "xent_slabs_kernel", count, rows_, row_of, slabs, split, slab_rows, xpitch, a.C,
+                          wide, out, ctx->status);
+    }
+
     hc_status forward() {
+        // their rows have to fit the 48 KiB of shared memory that every launch may have
+        if (a.capacity <= kFew && (long long)a.capacity * up(a.C, 256) * 4 <= 47 * 1024) return forward_few();
         const int bn = a.V <= 64 ? 64 : a.V <= 128 ? 128 : 256;
         const int halves = (int)up((a.V + bn / 2 - 1) / (bn / 2), 2);
         float2* pairs = nullptr;
@@ -953,12 +1206,18 @@ struct Call {
         long long split = (3 * pairs + tiles - 1) / tiles;
         if (split > piece / 1024) split = piece / 1024;
         if (split < 1 || !a.dx) split = 1;
+        // so has dW with few classes; 256 tokens at least
+        const long long wtiles = piece / kTile * ((a.C + bn_c - 1) / bn_c);
+        long long wsplit = pairs / wtiles;
+        if (wsplit > a.capacity / 256) wsplit = a.capacity / 256;
+        if (wsplit < 1 || !a.dW) wsplit = 1;
         __nv_bfloat16* G = nullptr;
-        float *slabs = nullptr, *part = nullptr;
+        float *slabs = nullptr, *wslabs = nullptr, *part = nullptr;
         auto place = [&](Layout l) {
             rows(l, true);
             G = l.take<__nv_bfloat16>((size_t)kPlanes * mpad * piece);
             if (a.dx) slabs = l.take<float>((size_t)split * mpad * xpitch);
+            if (wsplit > 1) wslabs = l.take<float>((size_t)wsplit * piece * xpitch);
             if (a.dbias) part = l.take<float>((size_t)(mpad / 32) * piece);
             return l.used;
         };
@@ -976,7 +1235,10 @@ struct Call {
             (st = encode(&mg_out, kBf16, G, piece, mpad, kPlanes, piece, 32)) != HC_OK)
             return st;
         if (a.dx && (st = encode(&mdx, kF32, slabs, a.C, mpad, (int)split, xpitch, 32)) != HC_OK) return st;
-        if (a.dW && wide &&
+        if (wsplit > 1 &&
+            (st = encode(&mdw, kF32, wslabs, a.C, piece, (int)wsplit, xpitch, 32)) != HC_OK)
+            return st;
+        if (a.dW && wide && wsplit == 1 &&
             (st = encode(&mdw, sizeof(T) == 4 ? kF32 : kBf16, a.dW, a.C, a.V, 1, a.C, 32)) != HC_OK)
             return st;
         ProductArgs p{};
@@ -1017,17 +1279,19 @@ struct Call {
             }
             if (a.dW) {
                 p.rows = classes;
-                p.split = 1;
+                p.split = (int)wsplit;
                 const long long units = ((long long)classes + kTile - 1) / kTile * ((a.C + bn_c - 1) / bn_c);
-                st = product<kWeight, T>(ctx, p, units, mg_mn, mx_mn, mdw, s);
+                st = product<kWeight, T>(ctx, p, units * wsplit, mg_mn, mx_mn, mdw, s);
                 if (st != HC_OK) return st;
+                if (wsplit > 1) {
+                    st = join(nullptr, classes, nullptr, wslabs, (int)wsplit, piece, xpitch,
+                              (T*)a.dW + v0 * a.C);
+                    if (st != HC_OK) return st;
+                }
             }
         }
         if (!a.dx || a.capacity == 0) return HC_OK;
-        const long long need = ((long long)a.capacity + 7) / 8, cap = 8ll * ctx->num_sms;
-        return launch_pdl(xent_input_kernel<T>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0,
-                          s, "xent_input_kernel", a.count, (long long)a.capacity, (const int*)r.row_of,
-                          (const float*)slabs, (int)split, mpad, xpitch, a.C, (T*)a.dx, ctx->status);
+        return join(a.count, a.capacity, r.row_of, slabs, (int)split, mpad, xpitch, (T*)a.dx);
     }
 };
 
