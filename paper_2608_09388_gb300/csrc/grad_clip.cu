@@ -1,17 +1,21 @@
 // The norm over all gradients of a network, and the gradients scaled so that
 // it is at most max_norm:
 //   norm = sqrt(sum over all tensors of g^2),  out = g * min(1, max_norm / norm)
-// The tensors are cut into units of 4096 elements, numbered tensor after
-// tensor; a block takes a range of units, whatever tensors they lie in.
+// The tensors are cut into units of 16 KiB, numbered tensor after tensor; a
+// block takes a range of units, whatever tensors they lie in.
 //
-// Squares are summed 32 at a time in fp32, those sums in a pair of fp32
-// numbers that keeps what each addition rounds off, the threads' and blocks'
-// sums in 64 bits: the norm of 10^9 values is off by a few units of fp32. The
-// order is fixed by the sizes alone, so the result is the same from run to run.
+// A thread's squares of a unit (8 fp32, 16 bf16) are summed in fp32, those sums in a
+// pair of fp32 numbers that keeps what each addition rounds off, the threads'
+// and blocks' sums in 64 bits: the norm of 10^9 values is off by a few units of
+// fp32. The order is fixed by the sizes alone, so the result is the same from
+// run to run.
 //
 // Bound by memory: the norm reads every value, the scaling reads it again (what
 // the caches still hold of it: the units are walked in the other direction) and
-// writes it.
+// writes it. One compact loop for both types: what a short call waits for is
+// the table, the first loads and the code itself, which come from memory too
+// (71 MB in 60 tensors: unrolled paths for whole and for ragged units took 20
+// us more).
 #include <algorithm>
 #include <exception>
 #include <vector>
@@ -22,92 +26,72 @@ namespace hc {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kPer = 8;                      // elements of a unit per thread
-constexpr int kUnit = kThreads * kPer;
-constexpr int kAhead = 4;                    // units loaded before the first is worked on
+constexpr int kResident = 3;                 // blocks an SM
+constexpr int kPieces = 2;                   // 16-byte pieces of a unit per thread
+constexpr int kUnit = kThreads * kPieces * 16;
+// Blocks of the grid: as many as run at a time, or several times that (up to
+// kBlocks an SM) where each still gets kShare units: ranges that are taken as SMs
+// get free even out what they wait.
+constexpr int kBlocks = 32, kShare = 8;
 
-// One tensor. Units count from the 16-byte boundary at or below `in`, `off`
-// elements before its first; `first` numbers its first unit.
+// One tensor. Units count from the 16-byte boundary at or below `in`; `first`
+// numbers its first unit.
 struct Entry {
-    const void* in;
-    void* out;
-    long long numel;
+    const char* in;
+    char* out;
+    long long bytes;
     long long first;
-    int off;
-    int dt;
+    int bf16;
+    int pad;
 };
 
-// A thread's elements of a unit: 16 bytes of bf16, or two times 16 bytes of fp32.
-struct Elems {
-    uint4 a[2];
-};
-
-template <typename T>
-__device__ __forceinline__ uint4 load_piece(const T* p, long long at, long long numel) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (at >= 0 && at + V <= numel) return *reinterpret_cast<const uint4*>(p + at);
-    alignas(16) T v[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = at + i >= 0 && at + i < numel ? p[at + i] : from_f32<T>(0.f);
-    return *reinterpret_cast<const uint4*>(v);
-}
-template <typename T>
-__device__ __forceinline__ void store_piece(T* p, long long at, long long numel, uint4 v, bool wide) {
-    constexpr int V = 16 / (int)sizeof(T);
-    if (wide && at >= 0 && at + V <= numel) {
-        *reinterpret_cast<uint4*>(p + at) = v;
-        return;
-    }
-    alignas(16) T f[V];
-    *reinterpret_cast<uint4*>(f) = v;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (at + i >= 0 && at + i < numel) p[at + i] = f[i];
-}
-
-// First element (of the tensor) of this thread's piece j of unit u.
-__device__ __forceinline__ long long piece_at(const Entry& e, long long u, int j) {
-    const long long base = (u - e.first) * kUnit - e.off;
-    return e.dt == HC_BF16 ? base + threadIdx.x * 8 : base + j * (kUnit / 2) + threadIdx.x * 4;
-}
-__device__ __forceinline__ Elems load_unit(const Entry& e, long long u) {
-    Elems r;
-    if (e.dt == HC_BF16) {
-        r.a[0] = load_piece(static_cast<const __nv_bfloat16*>(e.in), piece_at(e, u, 0), e.numel);
-    } else {
-        const float* p = static_cast<const float*>(e.in);
-        r.a[0] = load_piece(p, piece_at(e, u, 0), e.numel);
-        r.a[1] = load_piece(p, piece_at(e, u, 1), e.numel);
-    }
-    return r;
-}
-__device__ __forceinline__ void as_floats(const Elems& r, bool bf16, float (&f)[kPer]) {
-    const uint32_t w[4] = {r.a[0].x, r.a[0].y, r.a[0].z, r.a[0].w};
-    if (bf16) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f[i] = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-    } else {
-        const uint32_t z[4] = {r.a[1].x, r.a[1].y, r.a[1].z, r.a[1].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[i] = __uint_as_float(w[i]);
-            f[4 + i] = __uint_as_float(z[i]);
-        }
-    }
-}
-
-// The entry of unit u: the last one whose first unit is not above u.
+// The last entry whose first unit is not above u, the same in every thread: all
+// entries looked at together, or by halves where they are many.
 __device__ __forceinline__ int find_entry(const Entry* table, int n, long long u) {
+    if (n <= kThreads)
+        return __syncthreads_count((int)threadIdx.x < n && table[threadIdx.x].first <= u) - 1;
     int lo = 0, hi = n - 1;
     while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
+        const int mid = (int)(((long long)lo + hi + 1) >> 1);
         if (table[mid].first <= u)
             lo = mid;
         else
             hi = mid - 1;
     }
     return lo;
+}
+
+// A thread's 16 bytes at `at`, zero where they lie outside [from, to).
+__device__ __forceinline__ uint4 load_piece(const char* at, const char* from, const char* to) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (at >= from && at + 16 <= to) {
+        v = *reinterpret_cast<const uint4*>(at);
+    } else if (at < to && at + 16 > from) {
+        // both types as halves of words: an element is inside or outside as a whole
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const char* const p = at + 2 * i;
+            if (p >= from && p < to)
+                w[i >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16 * (i & 1);
+        }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return v;
+}
+__device__ __forceinline__ void store_piece(char* at, const char* from, const char* to, uint4 v,
+                                            bool wide) {
+    if (wide && at >= from && at + 16 <= to) {
+        *reinterpret_cast<uint4*>(at) = v;
+    } else if (at < to && at + 16 > from) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            char* const p = at + 2 * i;
+            if (p >= from && p < to)
+                *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[i >> 1] >> 16 * (i & 1));
+        }
+    }
 }
 
 __device__ __forceinline__ double block_sum_f64(double v, double* sh) {
@@ -122,96 +106,63 @@ __device__ __forceinline__ double block_sum_f64(double v, double* sh) {
     return v;
 }
 
-// Whether units u .. u + n - 1 lie wholly inside their tensor.
-__device__ __forceinline__ bool inside(const Entry& e, long long u, int n) {
-    const long long at = (u - e.first) * kUnit - e.off;
-    return at >= 0 && at + (long long)n * kUnit <= e.numel;
+// The two values of a word.
+__device__ __forceinline__ float2 halves(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 
-// The block's units [first, last): part[blockIdx.x] = the sum of their squares.
-__global__ void __launch_bounds__(kThreads, 2)
+// part[b] = the sum of the squares in the units [units * b / blocks, ..).
+__global__ void __launch_bounds__(kThreads, kResident)
     sum_squares_kernel(const Entry* __restrict__ table, int n, long long units,
                        double* __restrict__ part) {
     __shared__ double sh[kThreads / 32];
     pdl_wait();
     pdl_trigger();
-    const long long u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
+    const long long u1 = units * (blockIdx.x + 1) / gridDim.x;
+    long long u = units * blockIdx.x / gridDim.x;
     float hi = 0.f, lo = 0.f;
     double far = 0.0;  // squares that fp32 does not hold
-    if (u0 >= u1) {
-        if (threadIdx.x == 0) part[blockIdx.x] = 0.0;
-        return;
-    }
-    int t = find_entry(table, n, u0);
-    Entry e = table[t];
-    long long end = table[t + 1].first;
-    for (long long u = u0; u < u1; u += kAhead) {
-        Elems r[kAhead];
-        bool bf16[kAhead];
-        while (end <= u) {
-            e = table[++t];
-            end = table[t + 1].first;
-        }
-        if (u + kAhead <= u1 && inside(e, u, kAhead)) {
-            // the rule: no look at the ends, all loads at once
-            if (e.dt == HC_BF16) {
-                const uint4* const at = reinterpret_cast<const uint4*>(
-                    static_cast<const __nv_bfloat16*>(e.in) + piece_at(e, u, 0));
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    bf16[k] = true;
-                    r[k].a[0] = at[k * kThreads];
-                }
-            } else {
-                const uint4* const at = reinterpret_cast<const uint4*>(
-                    static_cast<const float*>(e.in) + piece_at(e, u, 0));
-#pragma unroll
-                for (int k = 0; k < kAhead; ++k) {
-                    bf16[k] = false;
-                    r[k].a[0] = at[2 * k * kThreads];
-                    r[k].a[1] = at[(2 * k + 1) * kThreads];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                bf16[k] = true;
-                r[k].a[0] = make_uint4(0u, 0u, 0u, 0u);
-                if (u + k < u1) {
-                    while (end <= u + k) {
-                        e = table[++t];
-                        end = table[t + 1].first;
-                    }
-                    bf16[k] = e.dt == HC_BF16;
-                    r[k] = load_unit(e, u + k);
-                }
-            }
-        }
-        F2 s = make_f2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            float f[kPer];
-            as_floats(r[k], bf16[k], f);
-#pragma unroll
-            for (int i = 0; i < kPer; i += 2) {
-                const F2 v = make_f2(f[i], f[i + 1]);
-                s = fma(v, v, s);
-            }
-        }
-        const float p = total(s);
-        if (p < __int_as_float(0x7f800000)) {
-            // hi + p, and what the addition rounds off
-            const float sum = hi + p, b = sum - hi;
-            lo += (hi - (sum - b)) + (p - b);
-            hi = sum;
-        } else {
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) {
-                float f[kPer];
-                as_floats(r[k], bf16[k], f);
+    if (u < u1) {
+        int t = find_entry(table, n, u);
+        while (u < u1) {
+            const char *const from = table[t].in, *const to = from + table[t].bytes;
+            const bool bf16 = table[t].bf16;
+            const long long next = table[t + 1].first, end = next < u1 ? next : u1;
+            const char* at = from - (reinterpret_cast<uintptr_t>(from) & 15) +
+                             (u - table[t].first) * kUnit + threadIdx.x * 16;
 #pragma unroll 1
-                for (int i = 0; i < kPer; ++i) far += (double)f[i] * (double)f[i];
+            for (; u < end; ++u, at += kUnit) {
+                uint4 v[kPieces];
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) v[j] = load_piece(at + j * (kThreads * 16), from, to);
+                float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j) {
+                    const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = bf16 ? halves(w[i]) : make_float2(__uint_as_float(w[i]), 0.f);
+                        s0 = fmaf(f.x, f.x, s0);
+                        s1 = fmaf(f.y, f.y, s1);
+                    }
+                }
+                const float s = s0 + s1;
+                if (s < __int_as_float(0x7f800000)) {
+                    // hi + s, and what the addition rounds off
+                    const float sum = hi + s, b = sum - hi;
+                    lo += (hi - (sum - b)) + (s - b);
+                    hi = sum;
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < 4 * kPieces; ++i) {
+                        const uint4 q = i < 4 ? v[0] : v[1];
+                        const uint32_t w = (i & 2) ? ((i & 1) ? q.w : q.z) : ((i & 1) ? q.y : q.x);
+                        const float2 f = bf16 ? halves(w) : make_float2(__uint_as_float(w), 0.f);
+                        far += (double)f.x * f.x + (double)f.y * f.y;
+                    }
+                }
             }
+            ++t;
         }
     }
     const double v = block_sum_f64((double)hi + (double)lo + far, sh);
@@ -229,95 +180,57 @@ __global__ void __launch_bounds__(kThreads)
     if (threadIdx.x == 0) *norm = (float)sqrt(v);
 }
 
-// kAhead units wholly inside a tensor, input and output aligned alike.
-template <typename T>
-__device__ __forceinline__ void scale_units(const Entry& e, long long u, float scale) {
-    constexpr int V = 16 / (int)sizeof(T), kPieces = kPer / V;
-    const long long at = piece_at(e, u, 0);
-    const T* const in = static_cast<const T*>(e.in) + at;
-    T* const out = static_cast<T*>(e.out) + at;
-    Piece<T, V> p[kAhead * kPieces];
-#pragma unroll
-    for (int k = 0; k < kAhead * kPieces; ++k) p[k].load(in + k * kThreads * V);
-#pragma unroll
-    for (int k = 0; k < kAhead * kPieces; ++k) {
-        float f[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = p[k].get(i) * scale;
-        p[k].set_all(f);
-        p[k].store(out + k * kThreads * V);
-    }
-}
-
-// The same units as sum_squares_kernel's block, from the last one down.
-__global__ void __launch_bounds__(kThreads, 2)
+// The units of sum_squares_kernel's blocks, from the last one down: what the
+// norm has read last is in the caches.
+__global__ void __launch_bounds__(kThreads, kResident)
     scale_kernel(const Entry* __restrict__ table, int n, long long units, const float* norm,
                  float max_norm) {
     pdl_wait();
     pdl_trigger();
+    const long long b = gridDim.x - 1 - blockIdx.x;
+    const long long u0 = units * b / gridDim.x;
+    long long u = units * (b + 1) / gridDim.x;  // the units below it are left
+    if (u <= u0) return;
     const float size = *norm;
     const float scale = size <= max_norm ? 1.f : max_norm / size;  // a NaN passes
-    const long long u0 = units * blockIdx.x / gridDim.x, u1 = units * (blockIdx.x + 1) / gridDim.x;
-    if (u0 >= u1) return;
-    int t = find_entry(table, n, u1 - 1);
-    Entry e = table[t];
-    auto wide = [](const Entry& e) {
-        return ((reinterpret_cast<uintptr_t>(e.in) ^ reinterpret_cast<uintptr_t>(e.out)) & 15) == 0;
-    };
-    for (long long u = u1 - 1; u >= u0; u -= kAhead) {  // u and the ones below
-        while (e.first > u) e = table[--t];
-        const long long lo = u - (kAhead - 1);
-        if (lo >= u0 && lo >= e.first && inside(e, lo, kAhead) && wide(e)) {
-            if (scale == 1.f && e.in == e.out) continue;
-            if (e.dt == HC_BF16)
-                scale_units<__nv_bfloat16>(e, lo, scale);
-            else
-                scale_units<float>(e, lo, scale);
-            continue;
-        }
-        Elems r[kAhead];
-        int at[kAhead];
+    int t = find_entry(table, n, u - 1);
+    for (; u > u0; --t) {
+        const char *const from = table[t].in, *const to = from + table[t].bytes;
+        const bool bf16 = table[t].bf16;
+        const long long first = table[t].first, end = first > u0 ? first : u0;
+        const ptrdiff_t off = table[t].out - from;
+        const bool wide = (off & 15) == 0;
+        if (scale == 1.f && off == 0) u = end < u ? end : u;
+        const char* at = from - (reinterpret_cast<uintptr_t>(from) & 15) + (u - 1 - first) * kUnit +
+                         threadIdx.x * 16;
+#pragma unroll 1
+        for (; u > end; --u, at -= kUnit) {
+            uint4 v[kPieces];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            at[k] = -1;
-            if (u - k >= u0) {
-                while (e.first > u - k) e = table[--t];
-                if (scale != 1.f || e.in != e.out) {
-                    at[k] = t;
-                    r[k] = load_unit(e, u - k);
+            for (int j = 0; j < kPieces; ++j) v[j] = load_piece(at + j * (kThreads * 16), from, to);
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = halves(w[i]);
+                    w[i] = bf16 ? Piece<__nv_bfloat16, 8>::pair(f.x * scale, f.y * scale)
+                                : __float_as_uint(__uint_as_float(w[i]) * scale);
                 }
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            if (at[k] < 0) continue;
-            const Entry o = table[at[k]];
-            const bool bf16 = o.dt == HC_BF16;
-            float f[kPer];
-            as_floats(r[k], bf16, f);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) f[i] *= scale;
-            if (bf16) {
-                Piece<__nv_bfloat16, 8> p;
-                p.set_all(f);
-                store_piece(static_cast<__nv_bfloat16*>(o.out), piece_at(o, u - k, 0), o.numel, p.v,
-                            wide(o));
-            } else {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    store_piece(static_cast<float*>(o.out), piece_at(o, u - k, j), o.numel,
-                                make_uint4(__float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]),
-                                           __float_as_uint(f[4 * j + 2]),
-                                           __float_as_uint(f[4 * j + 3])),
-                                wide(o));
+                store_piece(const_cast<char*>(at) + j * (kThreads * 16) + off, from + off, to + off,
+                            make_uint4(w[0], w[1], w[2], w[3]), wide);
             }
         }
     }
 }
 
 unsigned grid_of(const DeviceCtx* ctx, long long units) {
-    const long long cap = 2ll * ctx->num_sms;
-    return (unsigned)(units < 1 ? 1 : units < cap ? units : cap);
+    const long long once = (long long)kResident * ctx->num_sms, cap = (long long)kBlocks * ctx->num_sms;
+    long long grid = units / kShare;
+    if (grid < 4 * once) grid = once;  // a short second round would cost as much as the first
+    if (grid > cap) grid = cap;
+    if (grid > units) grid = units;
+    return (unsigned)(grid < 1 ? 1 : grid);
 }
 
 }  // namespace
@@ -339,11 +252,12 @@ bool fill_tensor_list(const void* const* in, void* const* out, const long long* 
     long long first = 0;
     for (int i = 0; i < n; ++i) {
         const int size = dt[i] == HC_BF16 ? 2 : 4;
-        const int off = (int)((reinterpret_cast<uintptr_t>(in[i]) & 15) / size);
+        const long long off = (long long)(reinterpret_cast<uintptr_t>(in[i]) & 15);
+        const long long bytes = numel[i] * size;
         void* const o = out ? out[i] : const_cast<void*>(in[i]);
-        e[i] = Entry{in[i], o, numel[i], first, off, dt[i]};
-        if (numel[i] == 0) continue;
-        first += (numel[i] + off + kUnit - 1) / kUnit;
+        e[i] = Entry{(const char*)in[i], (char*)o, bytes, first, dt[i] == HC_BF16, 0};
+        if (bytes == 0) continue;
+        first += (bytes + off + kUnit - 1) / kUnit;
         const uintptr_t at = reinterpret_cast<uintptr_t>(o);
         outs.push_back({at, at + (uintptr_t)numel[i] * size, i});
     }

@@ -1,7 +1,7 @@
 """The norm over a list of tensors and the clipping by it, against 64-bit sums.
 
-Tolerances. U = 2^-24. A thread sums 32 squares in two chains of 16 and adds
-the two: 17 U of a sum of positive numbers. Their sums are kept in a pair of
+Tolerances. U = 2^-24. A thread sums up to 32 squares in two chains of 16 and
+adds the two: 17 U of a sum of positive numbers. Their sums are kept in a pair of
 fp32 numbers whose lower one takes at most 2^-24 of the upper one a step and
 rounds it to 2^-24 of that; for the up to 2^12 steps of a thread here that is
 below U. Then 64 bits, a square root and one rounding: the norm is off by at most
@@ -51,7 +51,7 @@ def check(grads, outs, norm, max_norm, before=None):
 
 # one element, pieces that are not full, the border of a unit and of the units
 # a block loads together, more units than blocks
-SIZES = [[1], [0, 3], [7, 8, 9], [4095, 4096, 4097], [16384, 16385, 1, 65536],
+SIZES = [[1], [0, 3], [7, 8, 9], [4095, 4096, 4097], [8191, 8192, 8193], [16384, 16385, 1, 65536],
          [1000] * 300, [3000000, 5, 0, 70001], [12345678]]
 
 

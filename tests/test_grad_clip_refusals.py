@@ -9,7 +9,7 @@ from paper_2608_09388_gb300 import build, hc
 torch = pytest.importorskip("torch")
 
 P = ctypes.c_void_p
-UNIT = 4096  # elements, as the table counts them
+UNIT = 4096  # fp32 elements, 8192 bf16: 16 KiB
 
 
 @pytest.fixture(scope="module")
@@ -38,12 +38,12 @@ def fill(lib, tensors, in_place=False, n=None, host=None, device=0x5000, drop=()
 def test_units(lib):
     """A tensor's units count from the 16-byte boundary at or below it."""
     for numel, dt, at, units in ((0, 0, 0, 0), (1, 0, 0x1000, 1), (UNIT, 0, 0x1000, 1),
-                                 (UNIT + 1, 1, 0x1000, 2), (UNIT, 1, 0x1002, 2),
+                                 (2 * UNIT + 1, 1, 0x1000, 2), (2 * UNIT, 1, 0x1002, 2),
                                  (UNIT - 3, 0, 0x100c, 1), (UNIT - 2, 0, 0x100c, 2),
-                                 (2 ** 40, 1, 0x1000, 2 ** 28)):
+                                 (2 ** 40, 1, 0x1000, 2 ** 27)):
         st, d = fill(lib, [(at, at, numel, dt)])
         assert st == hc.HC_OK and (d.units, d.tensors, d.table) == (units, 1, 0x5000)
-    st, d = fill(lib, [(0x1000, 0x9000, 5, 0), (0, 0, 0, 1), (0x2000, 0xa000, UNIT, 1)])
+    st, d = fill(lib, [(0x1000, 0x9000, 5, 0), (0, 0, 0, 1), (0x2000, 0xa000, 2 * UNIT, 1)])
     assert st == hc.HC_OK and d.units == 2 and d.tensors == 3
     st, d = fill(lib, [])
     assert st == hc.HC_OK and d.units == 0
