@@ -204,10 +204,9 @@ __global__ void __launch_bounds__(256)
 
 // ---------------------------------------------------------------- products
 enum Product {
-    kStats,   // x W^T -> the pairs of the forward pass
-    kGrad,    // x W^T -> G of a piece
-    kInput,   // G W -> fp32 slabs of dx
-    kWeight,  // G^T x -> rows of dW, or fp32 slabs of them
+    kStats,  // x W^T -> the pairs of the forward pass
+    kGrad,   // x W^T -> G of a piece
+    kBack,   // G W -> fp32 slabs of dx, and G^T x -> rows of dW or fp32 slabs of them
 };
 
 constexpr int kTile = 256;                       // rows of a tile, 128 in each CTA
@@ -215,8 +214,12 @@ constexpr int kHalf = 128;
 constexpr int kKB = 64;                          // elements per block of the sum: 128 bytes
 constexpr int kOperandBytes = kHalf * kKB * 2;   // 16 KiB
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 6;
-constexpr int kStoreWarps = 8;
+constexpr int kStages = 5;
+// Sixteen warps take a tile from TMEM, 32 rows and kCols columns each: with eight
+// the loads, exponentials and stores of a tile of G, one behind the other,
+// took longer than its products up to a depth of 1600.
+constexpr int kStoreWarps = 16;
+constexpr int kCols = 64;
 constexpr int kLoadWarp = kStoreWarps;
 constexpr int kMmaWarp = kStoreWarps + 1;
 constexpr int kThreads = (kStoreWarps + 2) * 32;
@@ -228,28 +231,32 @@ constexpr int kGroupM = 16;                      // row tiles walked per column 
 constexpr int kChain = 4;
 constexpr int kBars = 2 * kStages + 5;
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreWarps * kOutBytes + kBars * 8 + 64;
+static_assert(kSmem <= 232448, "shared memory of a block");
 
 struct ProductArgs {
     const int* m;        // rows of x and G
-    int rows;            // kWeight: rows of the piece (the others: *m)
-    int cols;            // columns of the result
-    int depth;           // length of the sum (kWeight: *m)
-    int bn;              // columns of a tile: 64 (kStats), 128 or 256
-    int split;           // kInput, kWeight: parts of the sum, a slab of the result each
+    int cols;            // classes of the piece
+    int C;
+    int bn;              // columns of a tile, 128 or 256
     int planes;          // 1, or 3: six products a block
-    int v0, V;           // first class of the piece, classes in all
+    int v0;              // first class of the piece
     const float* bias;
     const int* target;
     const float* lse;
     const float* dloss;
-    float2* pairs;       // kStats: [half tiles][mpad]
+    float2* pairs;       // kStats: [classes / kCols][mpad]
     float* at_target;
     float* dbias_part;   // kGrad: [mpad / 32][piece], or NULL
     long long mpad, piece;
-    bool add;            // kInput: onto what earlier pieces left
-    void* dw;            // kWeight: rows from v0 on, [.., cols]
-    bool wide;           // its rows are 16-byte aligned: stored by TMA
+    int split;           // kBack: parts of the sums of dx, a slab each; 0: no dx
+    int wsplit;          // of dW; 1: its rows directly; 0: no dW
+    bool add;            // dx: onto what earlier pieces left
+    void* dw;            // rows from v0 on
+    bool wide;           // they are 16-byte aligned: stored by TMA
     unsigned* status;
+};
+struct Maps {
+    CUtensorMap a, b, bx, out, out_w;
 };
 
 __device__ __forceinline__ uint64_t desc_sw128(uint32_t saddr, uint32_t lbo) {
@@ -338,13 +345,36 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
     return v[0];
 }
 
+// What the pair does: a tile of one of the results, and the blocks [k0, k1)
+// of its sum.
+struct Work {
+    bool weight;  // kBack: of dW
+    int m, n, part, k0, k1;
+};
+
+// The i-th work of pair p of P. kBack has two lists, `first` units that cost
+// about `times` as much as the `second` ones: the long ones go round the pairs,
+// the pairs that got one less make up for it with short ones, and the rest
+// of those goes round again. Returns the unit, counted through both lists.
+__device__ __forceinline__ uint32_t scheduled(uint32_t i, uint32_t p, uint32_t P, uint32_t first,
+                                              uint32_t second, uint32_t times) {
+    const uint32_t r = first % P, mine = first / P + (p < r ? 1u : 0u);
+    if (i < mine) return p + i * P;
+    i -= mine;
+    const uint32_t more = r && p >= r ? times : 0u;
+    uint32_t u;
+    if (i < more)
+        u = p - r + i * (P - r);
+    else
+        u = (r ? times * (P - r) : 0u) + (p + P - r) % P + (i - more) * P;
+    return u < second ? first + u : first + second;
+}
+
 template <Product kP, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
-    xent_product_kernel(const ProductArgs a, const __grid_constant__ CUtensorMap map_a,
-                        const __grid_constant__ CUtensorMap map_b,
-                        const __grid_constant__ CUtensorMap map_out) {
-    constexpr bool kAMn = kP == kWeight, kBMn = kP == kInput || kP == kWeight;
+    xent_product_kernel(const ProductArgs a, const __grid_constant__ Maps maps) {
     constexpr bool kPromote = sizeof(T) == 4;
+    constexpr bool kBMn = kP == kBack;  // B's rows are along the sum
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
@@ -375,8 +405,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         *abort_flag = 0;
         sts_s32(issued_at, 0);
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-        prefetch_tensormap(&map_a);
-        prefetch_tensormap(&map_b);
+        prefetch_tensormap(&maps.a);
+        prefetch_tensormap(&maps.b);
     }
     if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(
@@ -396,33 +426,50 @@ __global__ void __launch_bounds__(kThreads, 1)
     const unsigned long long limit =
         reinterpret_cast<const volatile DeviceWord*>(a.status)->wait_limit_ns;
     const int M = *a.m;
-    const int rows = kP == kWeight ? a.rows : M;
-    const int depth = kP == kWeight ? M : a.depth;
-    const uint32_t tm = (uint32_t)(((long long)rows + kTile - 1) / kTile);
-    const uint32_t tn = (uint32_t)(((long long)a.cols + a.bn - 1) / a.bn);
-    const uint32_t units = tm * tn * (uint32_t)a.split;  // below 2^31 (checked by the host)
-    const int blocks = (int)(((long long)depth + kKB - 1) / kKB);
+    auto tiles_of = [](long long n, int by) { return (uint32_t)((n + by - 1) / by); };
     const int products = a.planes == 1 ? 1 : 6;
-    const uint32_t first = blockIdx.x >> 1, step = gridDim.x >> 1;
+    const uint32_t pair = blockIdx.x >> 1, P = gridDim.x >> 1;
+    // tiles and blocks of the logits or of dx, and of dW; unit counts are
+    // below 2^31 (checked by the host)
+    const uint32_t tm = tiles_of(M, kTile), tn = tiles_of(kP == kBack ? a.C : a.cols, a.bn);
+    const uint32_t tmw = tiles_of(a.cols, kTile);
+    const int blocks = (int)tiles_of(kP == kBack ? a.cols : a.C, kKB), wblocks = (int)tiles_of(M, kKB);
+    const uint32_t units = tm * tn * (kP == kBack ? (uint32_t)a.split : 1u);
+    const uint32_t wunits = kP == kBack ? tmw * tn * (uint32_t)a.wsplit : 0u;
+    // the list with the longer units goes first
+    const int each = a.split > 0 ? blocks / a.split : 0, weach = a.wsplit > 0 ? wblocks / a.wsplit : 0;
+    const bool weight_first = kP == kBack && weach > each;
+    const uint32_t times =
+        (uint32_t)(weight_first ? weach / (each < 1 ? 1 : each) : each / (weach < 1 ? 1 : weach));
 
-    // Unit u: its tile, and its blocks [k0, k1) of the sum, taken in chains.
-    auto unit_at = [&](uint32_t u, int& m, int& n, int& part, int& k0, int& k1) {
-        part = 0;
-        k0 = 0;
-        k1 = blocks;
-        if constexpr (kP == kInput || kP == kWeight) {
-            const uint32_t tiles = tm * tn;
-            part = (int)(u / tiles);
-            u -= (uint32_t)part * tiles;
-            k0 = (int)((long long)blocks * part / a.split);
-            k1 = (int)((long long)blocks * (part + 1) / a.split);
+    auto work_at = [&](uint32_t i, Work& w) -> bool {
+        w.weight = false;
+        w.part = 0;
+        uint32_t u;
+        if constexpr (kP == kBack) {
+            u = weight_first ? scheduled(i, pair, P, wunits, units, times)
+                             : scheduled(i, pair, P, units, wunits, times);
+            if (u >= units + wunits) return false;
+            w.weight = weight_first ? u < wunits : u >= units;
+            if (w.weight != weight_first) u -= weight_first ? wunits : units;
+            const uint32_t tiles = (w.weight ? tmw : tm) * tn;
+            const int split = w.weight ? a.wsplit : a.split, all = w.weight ? wblocks : blocks;
+            w.part = (int)(u / tiles);
+            u -= (uint32_t)w.part * tiles;
+            w.k0 = (int)((long long)all * w.part / split);
+            w.k1 = (int)((long long)all * (w.part + 1) / split);
+        } else {
+            u = pair + i * P;
+            if (u >= units) return false;
+            w.k0 = 0;
+            w.k1 = blocks;
         }
-        tile_at(u, tm, tn, m, n);
+        tile_at(u, w.weight ? tmw : tm, tn, w.m, w.n);
+        return true;
     };
 
     // In all roles every lane of the warp walks the loop, so that its state is
     // uniform; the copies and products are issued by one lane.
-    uint32_t issued = 0;
     if (warp == kLoadWarp) {
         const bool leader = elect_one();
         const uint32_t full0 = cluster_map(full_bar(0), 0);  // the first CTA's
@@ -430,66 +477,71 @@ __global__ void __launch_bounds__(kThreads, 1)
         // or 64 columns of 64 rows each
         const uint32_t b_bytes = (uint32_t)a.bn / 2 * kKB * 2;
         const uint32_t both = 2 * (kOperandBytes + b_bytes);
+        uint32_t issued = 0;
         bool ok = true;
-        for (uint32_t u = first; u < units && ok; u += step) {
-            int m, n, part, k0, k1;
-            unit_at(u, m, n, part, k0, k1);
-            const int row = m * kTile + (int)rank * kHalf, col = n * a.bn + (int)rank * a.bn / 2;
-            const int chain = kPromote ? kChain : k1 - k0;
-            for (int kc = k0; kc < k1 && ok; kc += chain)
-            for (int p = 0; p < products && ok; ++p) {
-                const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
-                const int end = k1 - kc < chain ? k1 : kc + chain;
-                for (int k = kc; k < end; ++k, ++issued) {
-                    const uint32_t s = issued % kStages;
-                    ok = wait_bar(empty_bar(s), ((issued / kStages) & 1) ^ 1u, abort_flag, a.status,
-                                  limit);
-                    if (!ok) break;
-                    if (leader) {
-                        const uint32_t sa = base + s * kStageBytes, sb = sa + kOperandBytes;
-                        const uint32_t bar = full0 + 8u * s;
-                        if (rank == 0) mbar_arrive_expect_tx(full_bar(s), both);
-                        if constexpr (kAMn) {
-                            load_pair(sa, &map_a, row, k * kKB, pa, bar);
-                            load_pair(sa + kOperandBytes / 2, &map_a, row + 64, k * kKB, pa, bar);
-                        } else {
-                            load_pair(sa, &map_a, k * kKB, row, pa, bar);
+        Work w;
+        for (uint32_t i = 0; ok && work_at(i, w); ++i) {
+            const int row = w.m * kTile + (int)rank * kHalf, col = w.n * a.bn + (int)rank * a.bn / 2;
+            const int chain = kPromote ? kChain : w.k1 - w.k0;
+            for (int kc = w.k0; kc < w.k1 && ok; kc += chain)
+                for (int p = 0; p < products && ok; ++p) {
+                    const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
+                    const int end = w.k1 - kc < chain ? w.k1 : kc + chain;
+                    for (int k = kc; k < end; ++k, ++issued) {
+                        const uint32_t s = issued % kStages;
+                        ok = wait_bar(empty_bar(s), ((issued / kStages) & 1) ^ 1u, abort_flag,
+                                      a.status, limit);
+                        if (!ok) break;
+                        if (leader) {
+                            const uint32_t sa = base + s * kStageBytes, sb = sa + kOperandBytes;
+                            const uint32_t bar = full0 + 8u * s;
+                            const int at = k * kKB;
+                            if (rank == 0) mbar_arrive_expect_tx(full_bar(s), both);
+                            if constexpr (kP == kBack) {
+                                // boxes of 64 rows both ways: G's rows or columns
+                                if (w.weight) {
+                                    load_pair(sa, &maps.a, row, at, pa, bar);
+                                    load_pair(sa + kOperandBytes / 2, &maps.a, row + 64, at, pa, bar);
+                                } else {
+                                    load_pair(sa, &maps.a, at, row, pa, bar);
+                                    load_pair(sa + kOperandBytes / 2, &maps.a, at, row + 64, pa, bar);
+                                }
+                                const CUtensorMap* const mb = w.weight ? &maps.bx : &maps.b;
+                                const int from = w.weight ? at : a.v0 + at;
+                                load_pair(sb, mb, col, from, pb, bar);
+                                if (a.bn == 256)
+                                    load_pair(sb + kOperandBytes / 2, mb, col + 64, from, pb, bar);
+                            } else {
+                                load_pair(sa, &maps.a, at, row, pa, bar);
+                                load_pair(sb, &maps.b, at, a.v0 + col, pb, bar);
+                            }
                         }
-                        // kInput: the classes of the piece start at v0
-                        if constexpr (kBMn) {
-                            const int at = k * kKB + (kP == kInput ? a.v0 : 0);
-                            load_pair(sb, &map_b, col, at, pb, bar);
-                            if (a.bn == 256)
-                                load_pair(sb + kOperandBytes / 2, &map_b, col + 64, at, pb, bar);
-                        } else {
-                            load_pair(sb, &map_b, k * kKB, a.v0 + col, pb, bar);
-                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                 }
-            }
         }
         if (lane == 0) sts_s32(issued_at, (int)issued);
     } else if (warp == kMmaWarp) {
         if (rank == 0) {
             const bool leader = elect_one();
-            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (kAMn ? 1u << 15 : 0u) |
-                                   (kBMn ? 1u << 16 : 0u) | ((uint32_t)(a.bn >> 3) << 17) |
-                                   ((uint32_t)(kTile >> 4) << 24);
+            const uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | (kBMn ? 1u << 16 : 0u) |
+                                    ((uint32_t)(a.bn >> 3) << 17) | ((uint32_t)(kTile >> 4) << 24);
             uint32_t it = 0, tile = 0;
             bool ok = true;
-            for (uint32_t u = first; u < units && ok; u += step) {
-                int m, n, part, k0, k1;
-                unit_at(u, m, n, part, k0, k1);
-                const int chain = kPromote ? kChain : k1 - k0;
-                int kc = k0;
+            Work w;
+            for (uint32_t i = 0; ok && work_at(i, w); ++i) {
+                // A of dW is G read along its columns
+                const uint32_t idesc = idesc0 | (w.weight ? 1u << 15 : 0u);
+                const uint32_t lbo = w.weight ? kOperandBytes / 2 : 16, step = w.weight ? 128 : 2;
+                const int chain = kPromote ? kChain : w.k1 - w.k0;
+                int kc = w.k0;
                 do {  // an empty sum of bf16 operands still passes its accumulator on
-                    if (kPromote && kc >= k1) break;
+                    if (kPromote && kc >= w.k1) break;
                     const uint32_t b = tile & 1;
                     ok = wait_bar(tempty_bar(b), ((tile >> 1) & 1) ^ 1u, abort_flag, a.status, limit);
                     if (!ok) break;
                     tc_fence_after();
-                    const int total = (k1 - kc < chain ? k1 - kc : chain) * products;
+                    const int total = (w.k1 - kc < chain ? w.k1 - kc : chain) * products;
                     for (int k = 0; k < total; ++k, ++it) {
                         const uint32_t s = it % kStages;
                         ok = wait_bar(full_bar(s), (it / kStages) & 1, abort_flag, a.status, limit);
@@ -497,13 +549,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tc_fence_after();
                         if (leader) {
                             const uint32_t sa = base + s * kStageBytes;
-                            const uint64_t da = desc_sw128(sa, kAMn ? kOperandBytes / 2 : 16);
+                            const uint64_t da = desc_sw128(sa, lbo);
                             const uint64_t db =
                                 desc_sw128(sa + kOperandBytes, kBMn ? kOperandBytes / 2 : 16);
 #pragma unroll
                             for (int j = 0; j < kKB / 16; ++j)  // 16 elements of the sum further on
-                                mma_pair(tmem_base + b * 256u, da + (kAMn ? 128 : 2) * j,
-                                         db + (kBMn ? 128 : 2) * j, idesc, (k | j) != 0 ? 1u : 0u);
+                                mma_pair(tmem_base + b * 256u, da + step * j, db + (kBMn ? 128 : 2) * j,
+                                         idesc, (k | j) != 0 ? 1u : 0u);
                             commit_pair(empty_bar(s));
                         }
                         __syncwarp();
@@ -513,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     __syncwarp();
                     ++tile;
                     kc += chain;
-                } while (kc < k1);
+                } while (kc < w.k1);
             }
             // every product issued here, and every arrival before this one, has
             // completed once fin_bar fires, in both CTAs
@@ -521,173 +573,208 @@ __global__ void __launch_bounds__(kThreads, 1)
             __syncwarp();
         }
     } else {
-        const int quarter = warp & 3, half = warp >> 2, hc = a.bn / 2;
+        const int quarter = warp & 3, group = warp >> 2;
+        const bool mine = group * kCols < a.bn;  // a narrow tile leaves some warps idle
         const uint32_t stage = out_at + (uint32_t)warp * kOutBytes;
+        const uint32_t tempty0 = cluster_map(tempty_bar(0), 0);
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         uint32_t tile = 0;
         bool ok = true;
-        for (uint32_t u = first; u < units; u += step) {
-            int m, n, part, k0, k1;
-            unit_at(u, m, n, part, k0, k1);
+        Work w;
+        for (uint32_t i = 0; work_at(i, w); ++i) {
             // the next accumulator: where it is, and the barrier that gives it back
             uint32_t acc = 0, tempty = 0;
             auto next = [&] {
                 const uint32_t b = tile & 1;
                 ok = wait_bar(tfull_bar(b), (tile >> 1) & 1, abort_flag, a.status, limit);
                 tc_fence_after();
-                acc = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * 256u + half * hc;
-                tempty = cluster_map(tempty_bar(b), 0);
+                acc = tmem_base + lanes + b * 256u + (uint32_t)(group * kCols);
+                tempty = tempty0 + 8u * b;
                 ++tile;
             };
-            float sums[kPromote ? 128 : 1];  // of this lane's row
+            auto give_back = [&] {
+                tc_fence_before();
+                if (lane == 0) arrive_cluster(tempty);
+            };
+            float sums[kPromote ? kCols : 1];  // of this lane's row
             if constexpr (kPromote) {
 #pragma unroll
-                for (int i = 0; i < 128; ++i) sums[i] = 0.f;
-                for (int kc = k0; kc < k1 && ok; kc += kChain) {
+                for (int j = 0; j < kCols; ++j) sums[j] = 0.f;
+                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain) {
                     next();
                     if (!ok) break;
+                    if (mine) {
 #pragma unroll
-                    for (int c = 0; c < 128; c += 32) {
-                        if (c >= hc) break;
-                        uint32_t r[32];
-                        tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
-                        tmem_ld_wait();
-                        if (c + 32 >= hc) {
-                            tc_fence_before();
-                            if (lane == 0) arrive_cluster(tempty);
+                        for (int c = 0; c < kCols; c += 32) {
+                            uint32_t r[32];
+                            tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
+                            tmem_ld_wait();
+                            if (c + 32 == kCols) give_back();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sums[c + j] += __uint_as_float(r[j]);
                         }
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) sums[c + i] += __uint_as_float(r[i]);
+                    } else {
+                        give_back();
                     }
                 }
             } else {
                 next();
             }
             if (!ok) break;
+            if (!mine) {
+                if (!kPromote) give_back();
+                continue;
+            }
             // 32 columns of this lane's row
-            constexpr int kCols = 128;
             auto load = [&](int c, float (&f)[32]) {
                 if constexpr (kPromote) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = sums[c + i];
+                    for (int j = 0; j < 32; ++j) f[j] = sums[c + j];
                 } else {
                     uint32_t r[32];
                     tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
                     tmem_ld_wait();
-                    if (c + 32 >= hc) {
-                        tc_fence_before();
-                        if (lane == 0) arrive_cluster(tempty);
-                    }
+                    if (c + 32 == kCols) give_back();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = k1 > k0 ? __uint_as_float(r[i]) : 0.f;
+                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(r[j]);
+                    if (kP == kBack && w.k1 == w.k0) {  // an empty sum
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] = 0.f;
+                    }
                 }
             };
-            const int row0 = m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
-            const int col0 = n * a.bn + half * hc;
+            const int row0 = w.m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+            const int col0 = w.n * a.bn + group * kCols;
             // 128 bytes of each of the warp's rows, swizzled, then one box
             auto staging_free = [&] {
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;\n" ::: "memory");
                 __syncwarp();
             };
             auto put = [&](int q, uint4 v) { sts_v4(stage + lane * 128 + ((q ^ (lane & 7)) << 4), v); };
-            auto send = [&](int c0, int c1, int c2, bool add) {
+            auto send = [&](const CUtensorMap* map, int c0, int c1, int c2, bool add) {
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) store_box(&map_out, stage, c0, c1, c2, add);
+                if (lane == 0) store_box(map, stage, c0, c1, c2, add);
             };
             auto pack = [](float lo, float hi) { return Piece<__nv_bfloat16, 8>::pair(lo, hi); };
 
             if constexpr (kP == kStats) {
-                const int target = row < M ? a.target[row] - a.v0 : -1;
-                float top = -__int_as_float(0x7f800000), sum = 0.f;
-#pragma unroll(kPromote ? 4 : 1)
+                const int target = row < M ? a.target[row] : -1;
+                const float least = -__int_as_float(0x7f800000);
+                float top = least, sum = 0.f;
+#pragma unroll
                 for (int c = 0; c < kCols; c += 32) {
-                    if (c >= hc) break;
                     float f[32];
                     load(c, f);
                     const int col = col0 + c;
                     if (a.bias) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col + i < a.cols) f[i] += __ldg(a.bias + a.v0 + col + i);
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j < a.cols) f[j] += __ldg(a.bias + col + j);
                     }
                     if (col + 32 > a.cols) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col + i >= a.cols) f[i] = -__int_as_float(0x7f800000);
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j >= a.cols) f[j] = least;
                     }
-                    float most = top;
+                    float m4[4] = {top, least, least, least};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) most = fmaxf(most, f[i]);
+                    for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], f[j]);
+                    const float most = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
                     if (target >= col && target < col + 32) {
                         float v = 0.f;
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v = col + i == target ? f[i] : v;
+                        for (int j = 0; j < 32; ++j) v = col + j == target ? f[j] : v;
                         a.at_target[row] = v;
                     }
                     // classes masked with -infinity leave it at that; a NaN
                     // goes past fmaxf and into the sum
-                    const float from = most == -__int_as_float(0x7f800000) ? 0.f : most;
+                    const float from = most == least ? 0.f : most;
                     sum *= ex2((top - from) * kLog2e);
                     float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s4[i & 3] += ex2((f[i] - from) * kLog2e);
+                    for (int j = 0; j < 32; ++j) s4[j & 3] += ex2((f[j] - from) * kLog2e);
                     sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
                     top = most;
                 }
                 if (row < M && col0 < a.cols)
-                    a.pairs[(long long)(n * 2 + half) * a.mpad + row] = make_float2(top, sum);
+                    a.pairs[(long long)(col0 / kCols) * a.mpad + row] = make_float2(top, sum);
             } else if constexpr (kP == kGrad) {
                 const bool in = row < M;
                 const float lse = in ? a.lse[row] : 0.f, dloss = in ? a.dloss[row] : 0.f;
                 const int target = in ? a.target[row] - a.v0 : -1;
-#pragma unroll(kPromote ? 2 : 1)
-                for (int c = 0; c < kCols; c += 64) {
-                    if (c >= hc) break;
-                    float f[64];
+                // the whole of it inside: no looks at rows and columns
+                const bool whole = row0 + 32 <= M && col0 + kCols <= a.cols;
+                float keep[kPromote ? kCols : 1];
+                if (!kPromote) staging_free();
 #pragma unroll
-                    for (int h = 0; h < 64; h += 32) {
-                        float g[32];
-                        load(c + h, g);
-                        const int col = col0 + c + h;
+                for (int c = 0; c < kCols; c += 32) {
+                    float f[32];
+                    load(c, f);
+                    const int col = col0 + c;
+                    if (a.bias) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const bool there = in && col + i < a.cols;
-                            if (a.bias && col + i < a.cols) g[i] += __ldg(a.bias + a.v0 + col + i);
-                            float p = ex2((g[i] - lse) * kLog2e);
-                            p -= col + i == target ? 1.f : 0.f;
-                            g[i] = there ? p * dloss : 0.f;
-                            f[h + i] = g[i];
-                        }
-                        if (a.dbias_part) {
-                            const float s = column_sums(g);
-                            if (col + lane < a.cols)
-                                a.dbias_part[(long long)(row0 / 32) * a.piece + col + lane] = s;
-                        }
+                        for (int j = 0; j < 32; ++j)
+                            if (col + j < a.cols) f[j] += __ldg(a.bias + a.v0 + col + j);
                     }
-                    const int planes = sizeof(T) == 4 ? 3 : 1;
 #pragma unroll
-                    for (int k = 0; k < planes; ++k) {
+                    for (int j = 0; j < 32; ++j) f[j] = ex2((f[j] - lse) * kLog2e);
+                    if (target >= col && target < col + 32) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] -= col + j == target ? 1.f : 0.f;
+                    }
+                    if (whole) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] *= dloss;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j)
+                            f[j] = in && col + j < a.cols ? f[j] * dloss : 0.f;
+                    }
+                    if constexpr (kPromote) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) keep[c + j] = f[j];
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            put(c / 8 + q,
+                                make_uint4(pack(f[8 * q], f[8 * q + 1]), pack(f[8 * q + 2], f[8 * q + 3]),
+                                           pack(f[8 * q + 4], f[8 * q + 5]), pack(f[8 * q + 6], f[8 * q + 7])));
+                    }
+                    if (a.dbias_part) {
+                        const float s = column_sums(f);
+                        if (col + lane < a.cols)
+                            a.dbias_part[(long long)(row0 / 32) * a.piece + col + lane] = s;
+                    }
+                }
+                if constexpr (kPromote) {
+                    // three planes, each what the ones before leave
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
                         staging_free();
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
                             float v[8];
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                v[i] = __bfloat162float(__float2bfloat16_rn(f[8 * q + i]));
-                                f[8 * q + i] -= v[i];  // what the next plane holds
+                            for (int j = 0; j < 8; ++j) {
+                                v[j] = __bfloat162float(__float2bfloat16_rn(keep[8 * q + j]));
+                                keep[8 * q + j] -= v[j];
                             }
                             put(q, make_uint4(pack(v[0], v[1]), pack(v[2], v[3]), pack(v[4], v[5]),
                                               pack(v[6], v[7])));
                         }
-                        send(col0 + c, row0, k, false);
+                        send(&maps.out, col0, row0, k, false);
                     }
+                } else {
+                    send(&maps.out, col0, row0, 0, false);
                 }
-            } else if (kP == kInput || sizeof(T) == 4 || a.split > 1) {
+            } else if (!w.weight || kPromote || a.wsplit > 1) {
                 // fp32 results, 32 columns at a time
-                const bool slab = kP == kInput || a.split > 1;
-#pragma unroll(kPromote ? 4 : 1)
+                const bool slab = !w.weight || a.wsplit > 1;
+                const CUtensorMap* const map = w.weight ? &maps.out_w : &maps.out;
+                const int rows = w.weight ? a.cols : M;
+#pragma unroll
                 for (int c = 0; c < kCols; c += 32) {
-                    if (c >= hc) break;
                     float f[32];
                     load(c, f);
                     staging_free();
@@ -697,54 +784,51 @@ __global__ void __launch_bounds__(kThreads, 1)
                                           __float_as_uint(f[4 * q + 2]), __float_as_uint(f[4 * q + 3])));
                     const int col = col0 + c;
                     if (slab) {
-                        if (col < a.cols) send(col, row0, part, kP == kInput && a.add);
+                        if (col < a.C) send(map, col, row0, w.part, !w.weight && a.add);
                     } else if (a.wide) {
-                        if (col < a.cols && row0 < rows) send(col, a.v0 + row0, 0, false);
+                        if (col < a.C && row0 < rows) send(map, col, a.v0 + row0, 0, false);
                     } else {
                         __syncwarp();
                         for (int r = 0; r < 32; ++r) {
                             const uint32_t at = stage + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4;
-                            if (row0 + r < rows && col + lane < a.cols)
-                                static_cast<float*>(a.dw)[(long long)(a.v0 + row0 + r) * a.cols + col + lane] =
+                            if (row0 + r < rows && col + lane < a.C)
+                                static_cast<float*>(a.dw)[(long long)(a.v0 + row0 + r) * a.C + col + lane] =
                                     __int_as_float(lds_s32(at));
                         }
                         __syncwarp();
                     }
                 }
             } else {
-                // bf16 results, 64 columns at a time
-                for (int c = 0; c < hc; c += 64) {
-                    staging_free();
+                // bf16 rows of dW, 64 columns
+                staging_free();
 #pragma unroll
-                    for (int h = 0; h < 64; h += 32) {
-                        float f[32];
-                        load(c + h, f);
+                for (int c = 0; c < kCols; c += 32) {
+                    float f[32];
+                    load(c, f);
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            put(h / 8 + q,
-                                make_uint4(pack(f[8 * q], f[8 * q + 1]), pack(f[8 * q + 2], f[8 * q + 3]),
-                                           pack(f[8 * q + 4], f[8 * q + 5]), pack(f[8 * q + 6], f[8 * q + 7])));
-                    }
-                    const int col = col0 + c;
-                    if (a.wide) {
-                        if (col < a.cols && row0 < rows) send(col, a.v0 + row0, 0, false);
-                    } else {
-                        __syncwarp();
-                        for (int r = 0; r < 32; ++r) {
-                            if (row0 + r >= rows) break;
-                            __nv_bfloat16* const to =
-                                static_cast<__nv_bfloat16*>(a.dw) + (long long)(a.v0 + row0 + r) * a.cols;
+                    for (int q = 0; q < 4; ++q)
+                        put(c / 8 + q,
+                            make_uint4(pack(f[8 * q], f[8 * q + 1]), pack(f[8 * q + 2], f[8 * q + 3]),
+                                       pack(f[8 * q + 4], f[8 * q + 5]), pack(f[8 * q + 6], f[8 * q + 7])));
+                }
+                if (a.wide) {
+                    if (col0 < a.C && row0 < a.cols) send(&maps.out_w, col0, a.v0 + row0, 0, false);
+                } else {
+                    __syncwarp();
+                    for (int r = 0; r < 32; ++r) {
+                        if (row0 + r >= a.cols) break;
+                        __nv_bfloat16* const to =
+                            static_cast<__nv_bfloat16*>(a.dw) + (long long)(a.v0 + row0 + r) * a.C;
 #pragma unroll
-                            for (int h = 0; h < 64; h += 32) {
-                                const int j = h + lane;
-                                const uint32_t at = stage + r * 128 + (((j >> 3) ^ (r & 7)) << 4) + (j & 7) * 2;
-                                uint16_t v;
-                                asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(at) : "memory");
-                                if (col + j < a.cols) to[col + j] = __ushort_as_bfloat16(v);
-                            }
+                        for (int h = 0; h < 64; h += 32) {
+                            const int j = h + lane;
+                            const uint32_t at = stage + r * 128 + (((j >> 3) ^ (r & 7)) << 4) + (j & 7) * 2;
+                            uint16_t v;
+                            asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(at) : "memory");
+                            if (col0 + j < a.C) to[col0 + j] = __ushort_as_bfloat16(v);
                         }
-                        __syncwarp();
                     }
+                    __syncwarp();
                 }
             }
         }
@@ -1021,8 +1105,7 @@ constexpr CUtensorMapDataType kBf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
 constexpr CUtensorMapDataType kF32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
 
 template <Product kP, typename T>
-hc_status product(const DeviceCtx* ctx, const ProductArgs& a, long long units, const CUtensorMap& ma,
-                  const CUtensorMap& mb, const CUtensorMap& mo, cudaStream_t s) {
+hc_status product(const DeviceCtx* ctx, const ProductArgs& a, long long units, const Maps& maps, cudaStream_t s) {
     if (units > 0x7fffffffll) {
         set_error("cross entropy: %lld tiles are too many", units);
         return HC_ERR_UNSUPPORTED;
@@ -1038,7 +1121,7 @@ hc_status product(const DeviceCtx* ctx, const ProductArgs& a, long long units, c
         if (st != HC_OK) return st;
         done[ctx->device] = true;
     }
-    return launch_cluster(kern, grid, 2, kThreads, kSmem, s, "xent_product_kernel", a, ma, mb, mo);
+    return launch_cluster(kern, grid, 2, kThreads, kSmem, s, "xent_product_kernel", a, maps);
 }
 
 long long up(long long v, long long to) {
@@ -1153,12 +1236,12 @@ struct Call {
     hc_status forward() {
         // their rows have to fit the 48 KiB of shared memory that every launch may have
         if (a.capacity <= kFew && (long long)a.capacity * up(a.C, 256) * 4 <= 47 * 1024) return forward_few();
-        const int bn = a.V <= 64 ? 64 : a.V <= 128 ? 128 : 256;
-        const int halves = (int)up((a.V + bn / 2 - 1) / (bn / 2), 2);
+        const int bn = a.V <= 128 ? 128 : 256;
+        const int parts = (int)(((long long)a.V + kCols - 1) / kCols);
         float2* pairs = nullptr;
         auto place = [&](Layout l) {
             rows(l, false);
-            pairs = l.take<float2>((size_t)halves * mpad);
+            pairs = l.take<float2>((size_t)parts * mpad);
             return l.used;
         };
         uint8_t* const ws = (uint8_t*)stream_workspace(s, place({nullptr}));
@@ -1166,29 +1249,25 @@ struct Call {
         place({ws});
         hc_status st = gather(false);
         if (st != HC_OK) return st;
-        CUtensorMap mx, mw;
-        if ((st = map_x(&mx, kHalf)) != HC_OK || (st = map_w(&mw, bn / 2)) != HC_OK) return st;
+        Maps maps{};
+        if ((st = map_x(&maps.a, kHalf)) != HC_OK || (st = map_w(&maps.b, bn / 2)) != HC_OK) return st;
         ProductArgs p{};
         p.m = r.m;
         p.cols = a.V;
-        p.depth = a.C;
+        p.C = a.C;
         p.bn = bn;
-        p.split = 1;
         p.planes = kPlanes;
-        p.V = a.V;
         p.bias = a.bias;
         p.target = r.target;
         p.pairs = pairs;
         p.at_target = r.at_target;
         p.mpad = mpad;
         p.status = ctx->status;
-        const long long units = mpad / kTile * ((a.V + (long long)bn - 1) / bn);
-        st = product<kStats, T>(ctx, p, units, mx, mw, mw, s);
+        st = product<kStats, T>(ctx, p, mpad / kTile * ((a.V + (long long)bn - 1) / bn), maps, s);
         if (st != HC_OK) return st;
         const long long need = mpad / 32, cap = 2ll * ctx->num_sms;
         return launch_pdl(xent_loss_kernel, dim3((unsigned)(need < cap ? need : cap)), dim3(1024), 0, s,
-                          "xent_loss_kernel", r, (const float2*)pairs,
-                          (int)(((long long)a.V + bn / 2 - 1) / (bn / 2)), mpad, a.loss_out, a.lse_out);
+                          "xent_loss_kernel", r, (const float2*)pairs, parts, mpad, a.loss_out, a.lse_out);
     }
 
     hc_status backward() {
@@ -1226,25 +1305,23 @@ struct Call {
         place({ws});
         hc_status st = gather(true);
         if (st != HC_OK) return st;
-        CUtensorMap mx, mw, mx_mn, mw_mn, mg, mg_mn, mg_out, mdx{}, mdw{};
+        Maps grad{}, back{};
         const bool wide = (a.C * sizeof(T)) % 16 == 0 && (reinterpret_cast<uintptr_t>(a.dW) & 15) == 0;
-        if ((st = map_x(&mx, kHalf)) != HC_OK || (st = map_w(&mw, bn_v / 2)) != HC_OK ||
-            (st = map_x(&mx_mn, kKB)) != HC_OK || (st = map_w(&mw_mn, kKB)) != HC_OK ||
-            (st = encode(&mg, kBf16, G, piece, mpad, kPlanes, piece, kHalf)) != HC_OK ||
-            (st = encode(&mg_mn, kBf16, G, piece, mpad, kPlanes, piece, kKB)) != HC_OK ||
-            (st = encode(&mg_out, kBf16, G, piece, mpad, kPlanes, piece, 32)) != HC_OK)
+        if ((st = map_x(&grad.a, kHalf)) != HC_OK || (st = map_w(&grad.b, bn_v / 2)) != HC_OK ||
+            (st = encode(&grad.out, kBf16, G, piece, mpad, kPlanes, piece, 32)) != HC_OK ||
+            (st = encode(&back.a, kBf16, G, piece, mpad, kPlanes, piece, kKB)) != HC_OK ||
+            (st = map_w(&back.b, kKB)) != HC_OK || (st = map_x(&back.bx, kKB)) != HC_OK)
             return st;
-        if (a.dx && (st = encode(&mdx, kF32, slabs, a.C, mpad, (int)split, xpitch, 32)) != HC_OK) return st;
-        if (wsplit > 1 &&
-            (st = encode(&mdw, kF32, wslabs, a.C, piece, (int)wsplit, xpitch, 32)) != HC_OK)
-            return st;
-        if (a.dW && wide && wsplit == 1 &&
-            (st = encode(&mdw, sizeof(T) == 4 ? kF32 : kBf16, a.dW, a.C, a.V, 1, a.C, 32)) != HC_OK)
-            return st;
+        if (a.dx && (st = encode(&back.out, kF32, slabs, a.C, mpad, (int)split, xpitch, 32)) != HC_OK) return st;
+        if (wsplit > 1)
+            st = encode(&back.out_w, kF32, wslabs, a.C, piece, (int)wsplit, xpitch, 32);
+        else if (a.dW && wide)
+            st = encode(&back.out_w, sizeof(T) == 4 ? kF32 : kBf16, a.dW, a.C, a.V, 1, a.C, 32);
+        if (st != HC_OK) return st;
         ProductArgs p{};
         p.m = r.m;
+        p.C = a.C;
         p.planes = kPlanes;
-        p.V = a.V;
         p.bias = a.bias;
         p.target = r.target;
         p.lse = r.lse;
@@ -1252,6 +1329,8 @@ struct Call {
         p.dbias_part = part;
         p.mpad = mpad;
         p.piece = piece;
+        p.split = a.dx ? (int)split : 0;
+        p.wsplit = a.dW ? (int)wsplit : 0;
         p.dw = a.dW;
         p.wide = wide;
         p.status = ctx->status;
@@ -1259,35 +1338,24 @@ struct Call {
             const int classes = (int)(a.V - v0 < piece ? a.V - v0 : piece);
             p.v0 = (int)v0;
             p.cols = classes;
-            p.depth = a.C;
             p.bn = bn_v;
-            p.split = 1;
-            st = product<kGrad, T>(ctx, p, mpad / kTile * ((classes + bn_v - 1) / bn_v), mx, mw, mg_out, s);
+            p.add = v0 > 0;
+            st = product<kGrad, T>(ctx, p, mpad / kTile * ((classes + bn_v - 1) / bn_v), grad, s);
             if (st != HC_OK) return st;
             if (a.dbias) {
                 st = launch_column_sum(part, (int)(mpad / 32), piece, classes, a.dbias + v0, s, r.m);
                 if (st != HC_OK) return st;
             }
+            if (!a.dx && !a.dW) continue;
             p.bn = bn_c;
-            p.cols = a.C;
-            if (a.dx) {
-                p.depth = classes;
-                p.split = (int)split;
-                p.add = v0 > 0;
-                st = product<kInput, T>(ctx, p, tiles * split, mg, mw_mn, mdx, s);
+            const long long units = tiles * p.split + ((long long)classes + kTile - 1) / kTile *
+                                                          ((a.C + bn_c - 1) / bn_c) * p.wsplit;
+            st = product<kBack, T>(ctx, p, units, back, s);
+            if (st != HC_OK) return st;
+            if (p.wsplit > 1) {
+                st = join(nullptr, classes, nullptr, wslabs, (int)wsplit, piece, xpitch,
+                          (T*)a.dW + v0 * a.C);
                 if (st != HC_OK) return st;
-            }
-            if (a.dW) {
-                p.rows = classes;
-                p.split = (int)wsplit;
-                const long long units = ((long long)classes + kTile - 1) / kTile * ((a.C + bn_c - 1) / bn_c);
-                st = product<kWeight, T>(ctx, p, units * wsplit, mg_mn, mx_mn, mdw, s);
-                if (st != HC_OK) return st;
-                if (wsplit > 1) {
-                    st = join(nullptr, classes, nullptr, wslabs, (int)wsplit, piece, xpitch,
-                              (T*)a.dW + v0 * a.C);
-                    if (st != HC_OK) return st;
-                }
             }
         }
         if (!a.dx || a.capacity == 0) return HC_OK;
