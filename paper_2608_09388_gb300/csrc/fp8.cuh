@@ -13,18 +13,21 @@ namespace hc {
 constexpr float kE4m3Max = 448.f;
 constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
 
+// amax / 448 by Markstein's correction (see to_e4m3), divided where a
+// residual would leave the range of fp32.
 __device__ __forceinline__ float scale_of(float amax) {
+    constexpr float kInv = 1.f / kE4m3Max;
+    if (amax >= 0x1p-90f && amax < __int_as_float(0x7f800000)) {
+        const float q = amax * kInv;
+        return fmaf(fmaf(q, -kE4m3Max, amax), kInv, q);
+    }
     const float s = amax / kE4m3Max;
     return s < kMinScale ? kMinScale : s;  // a NaN passes
 }
-// (a, b) * (s, s), one instruction for both.
-__device__ __forceinline__ float2 mul_pair(float a, float b, float s) {
-    unsigned long long v, ss;
-    float2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
-    asm("mov.b64 %0, {%1, %1};" : "=l"(ss) : "f"(s));
-    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(ss));
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+// The largest magnitude of three, a NaN if one of them is.
+__device__ __forceinline__ float max_mag(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
@@ -38,24 +41,29 @@ __device__ __forceinline__ uint32_t first_bytes(int n) {
     return n >= 4 ? 0xffffffffu : n > 0 ? (1u << 8 * n) - 1u : 0u;
 }
 
-// The e4m3 bytes of N values x / scale. With inv the rounded reciprocal,
-// x * (inv * (1 - 2^-21)) and x * (inv * (1 + 2^-21)) enclose the fp32
-// quotient (four roundings of at most 2^-24 each separate it from x * inv),
-// and rounding to e4m3 is monotonic: where both products round alike, so does
-// the quotient. Only the others are divided.
+// The e4m3 bytes of N values x / scale, inv the rounded reciprocal of scale. The
+// quotient is q - (q * scale - x) * inv with q = x * inv (Markstein's
+// correction): the residual is exact, and with a correctly rounded inv the
+// result is the correctly rounded quotient, as the division gives it, also
+// for a zero of either sign. Where the residual would leave the range of fp32
+// (or scale is infinite or a NaN) the values are divided.
 template <int N>
 __device__ __forceinline__ void to_e4m3(const float (&x)[N], float scale, float inv,
                                         uint32_t (&w)[N / 4]) {
-    const float below = inv * (1.f - 0x1p-21f), above = inv * (1.f + 0x1p-21f);
-    uint32_t differ = 0;
+    if (scale >= 0x1p-90f && scale < __int_as_float(0x7f800000)) {
+        const F2 s = make_f2(scale, scale), i1 = make_f2(inv, inv), i2 = make_f2(-inv, -inv);
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        const float2 a = mul_pair(x[i], x[i + 1], below), b = mul_pair(x[i + 2], x[i + 3], below);
-        const float2 c = mul_pair(x[i], x[i + 1], above), d = mul_pair(x[i + 2], x[i + 3], above);
-        w[i / 4] = pack_e4m3(a.x, a.y, b.x, b.y);
-        differ |= w[i / 4] ^ pack_e4m3(c.x, c.y, d.x, d.y);
-    }
-    if (differ) {
+        for (int i = 0; i < N; i += 4) {
+            float2 f[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float a = x[i + 2 * h], b = x[i + 2 * h + 1];
+                const F2 q = mul(make_f2(a, b), i1);
+                f[h] = split(fma(fma(q, s, make_f2(-a, -b)), i2, q));
+            }
+            w[i / 4] = pack_e4m3(f[0].x, f[0].y, f[1].x, f[1].y);
+        }
+    } else {
 #pragma unroll
         for (int i = 0; i < N; i += 4)
             w[i / 4] = pack_e4m3(x[i] / scale, x[i + 1] / scale, x[i + 2] / scale, x[i + 3] / scale);

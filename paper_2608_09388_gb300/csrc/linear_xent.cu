@@ -103,6 +103,8 @@ __global__ void __launch_bounds__(kGatherThreads)
         const int t = a.targets[n];
         return t >= 0 && t < a.V;
     };
+    // the block's first targets are on their way while the ones before are counted
+    int ahead = n0 + threadIdx.x < n1 ? a.targets[n0 + threadIdx.x] : -1;
     int before = 0;
 #pragma unroll 8
     for (long long n = threadIdx.x; n < n0; n += kGatherThreads) before += valid(n);
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(kGatherThreads)
         const long long n = first + threadIdx.x;
         int t = -1;
         if (n < n1) {
-            t = a.targets[n];
+            t = first == n0 ? ahead : a.targets[n];
             if (t < -1 || t >= a.V) {
                 report(a.status, kErrIndex);
                 t = -1;
@@ -873,6 +875,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
+// (top, sum) and another pair as one; tops of -infinity hold nothing, a NaN stays.
+__device__ __forceinline__ float2 join_pairs(float2 a, float2 b) {
+    const float least = -__int_as_float(0x7f800000);
+    const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
+    return make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
+}
+__device__ __forceinline__ float2 join_warp(float2 p) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+        p = join_pairs(p, make_float2(__shfl_xor_sync(0xffffffffu, p.x, o),
+                                      __shfl_xor_sync(0xffffffffu, p.y, o)));
+    return p;
+}
+
 // ---------------------------------------------------------------- few tokens
 // Up to kFew tokens (a scoring or decoding step): bound by the one read of W,
 // so the sums are taken on the CUDA cores straight from the rows as they are. A
@@ -890,7 +906,7 @@ __device__ __forceinline__ int few_at(int c) {
 }
 
 template <typename T, int VEC, int kTokens>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(kFewThreads, kTokens <= 2 ? 3 : 2)
     xent_few_kernel(const T* __restrict__ x, const T* __restrict__ W, const float* __restrict__ bias,
                     const int32_t* targets, int C, int V, float2* __restrict__ pairs,
                     float* __restrict__ at_target) {
@@ -912,17 +928,22 @@ __global__ void __launch_bounds__(kFewThreads)
     float2 all[kTokens];
 #pragma unroll
     for (int t = 0; t < kTokens; ++t) all[t] = make_float2(least, 0.f);
-    const long long step = (long long)gridDim.x * (kFewThreads / 32) * kFewRows;
-    for (long long v0 = ((long long)blockIdx.x * (kFewThreads / 32) + warp) * kFewRows; v0 < V; v0 += step) {
+    // whole rounds of kFewRows classes a warp, then what is left in one round of
+    // as few as it takes: every warp ends at the same time
+    const int W_ = gridDim.x * (kFewThreads / 32), w_ = (int)blockIdx.x * (kFewThreads / 32) + warp;
+    const int whole = V / (W_ * kFewRows), left = V - whole * W_ * kFewRows;
+    const int last = (left + W_ - 1) / W_;
+    for (int i = 0; i <= whole; ++i) {
+        const int take = i < whole ? kFewRows : last;
+        const long long v0 = (long long)i * W_ * kFewRows + (long long)w_ * take;
+        if (v0 >= V || take == 0) break;
         float s[kFewRows][kTokens] = {};
-        const T* w[kFewRows];
-#pragma unroll
-        for (int r = 0; r < kFewRows; ++r) w[r] = W + (v0 + r < V ? v0 + r : v0) * C;
 #pragma unroll 4
         for (int c = lane * VEC; c < C; c += 32 * VEC) {
             Piece<T, VEC> p[kFewRows];
 #pragma unroll
-            for (int r = 0; r < kFewRows; ++r) p[r].load(w[r] + c);
+            for (int r = 0; r < kFewRows; ++r)
+                if (r < take && v0 + r < V) p[r].load(W + (v0 + r) * C + c);
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) {
                 float f[VEC];
@@ -943,14 +964,13 @@ __global__ void __launch_bounds__(kFewThreads)
         }
 #pragma unroll
         for (int r = 0; r < kFewRows; ++r) {
-            if (v0 + r >= V) break;
+            if (r >= take || v0 + r >= V) break;
             const float b = bias ? __ldg(bias + v0 + r) : 0.f;
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) {
                 const float l = warp_sum(s[r][t]) + b;
                 if (lane == 0 && v0 + r == target[t]) at_target[t] = l;
-                const float top = fmaxf(all[t].x, l), from = top == least ? 0.f : top;
-                all[t] = make_float2(top, all[t].y * ex2((all[t].x - from) * kLog2e) + ex2((l - from) * kLog2e));
+                all[t] = join_pairs(all[t], make_float2(l, 1.f));
             }
         }
     }
@@ -959,13 +979,9 @@ __global__ void __launch_bounds__(kFewThreads)
         for (int t = 0; t < kTokens; ++t) sh[warp][t] = all[t];
     __syncthreads();
     if (threadIdx.x < kTokens) {
-        float2 a = sh[0][threadIdx.x];
-        for (int w = 1; w < kFewThreads / 32; ++w) {
-            const float2 b = sh[w][threadIdx.x];
-            const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
-            a = make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
-        }
-        pairs[(long long)blockIdx.x * kFew + threadIdx.x] = a;
+        float2 p = sh[0][threadIdx.x];
+        for (int w = 1; w < kFewThreads / 32; ++w) p = join_pairs(p, sh[w][threadIdx.x]);
+        pairs[(long long)blockIdx.x * kFew + threadIdx.x] = p;
     }
 }
 
@@ -982,16 +998,10 @@ __global__ void __launch_bounds__(kFew * 32)
     const int t = targets[n];
     const bool in = t >= 0 && t < V;
     if (!in && t != -1 && lane == 0) report(status, kErrIndex);
-    auto join = [&](float2 a, float2 b) {
-        const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
-        return make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
-    };
     float2 p = make_float2(least, 0.f);
-#pragma unroll 4
-    for (int b = lane; b < blocks; b += 32) p = join(p, pairs[(long long)b * kFew + n]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        p = join(p, make_float2(__shfl_xor_sync(0xffffffffu, p.x, o), __shfl_xor_sync(0xffffffffu, p.y, o)));
+#pragma unroll 8
+    for (int b = lane; b < blocks; b += 32) p = join_pairs(p, pairs[(long long)b * kFew + n]);
+    p = join_warp(p);
     if (lane != 0) return;
     const float all = p.x + logf(p.y);
     if (lse) lse[n] = in ? all : 0.f;
@@ -999,33 +1009,36 @@ __global__ void __launch_bounds__(kFew * 32)
 }
 
 // ---------------------------------------------------------------- joins
-// The pairs of a row -> loss and lse: 32 rows a block, every 32nd pair a warp,
-// then the warps in order.
+// The pairs of a row -> loss and lse: 32 rows a block, every 32nd pair a warp;
+// then a warp per row.
 __global__ void __launch_bounds__(1024)
-    xent_loss_kernel(const Rows r, const float2* __restrict__ pairs, int halves, long long mpad,
+    xent_loss_kernel(const Rows r, const float2* __restrict__ pairs, int parts, long long mpad,
                      float* loss, float* lse) {
-    __shared__ float2 sh[32][32];
+    __shared__ float2 sh[32][33];
     pdl_wait();
     pdl_trigger();
     const int M = *r.m, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float least = -__int_as_float(0x7f800000);
-    // (top, sum) and another pair as one; tops of -infinity hold nothing, a NaN stays
-    auto join = [&](float2 a, float2 b) {
-        const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
-        return make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
-    };
     for (long long row0 = blockIdx.x * 32ll; row0 < M; row0 += gridDim.x * 32ll) {
-        const long long row = row0 + lane;
         float2 p = make_float2(least, 0.f);
-        if (row < M) {
-#pragma unroll 4
-            for (int h = warp; h < halves; h += 32) p = join(p, pairs[h * mpad + row]);
+        if (row0 + lane < M) {
+            constexpr int kLoads = 8;
+            for (int h = warp; h < parts; h += 32 * kLoads) {
+                float2 q[kLoads];
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k)
+                    q[k] = h + 32 * k < parts ? pairs[(h + 32ll * k) * mpad + row0 + lane]
+                                              : make_float2(least, 0.f);
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) p = join_pairs(p, q[k]);
+            }
         }
         __syncthreads();
         sh[warp][lane] = p;
         __syncthreads();
-        if (warp == 0 && row < M) {
-            for (int w = 1; w < 32; ++w) p = join(p, sh[w][lane]);
+        p = join_warp(sh[lane][warp]);
+        const long long row = row0 + warp;
+        if (lane == 0 && row < M) {
             const float all = p.x + logf(p.y);
             const int n = r.token_of[row];
             if (lse) lse[n] = all;
@@ -1174,7 +1187,7 @@ struct Call {
         GatherArgs g{a.x, a.targets, a.count, a.capacity, mpad, a.C, a.V, pitch,
                      back ? a.lse : nullptr, back ? a.dloss : nullptr, back ? nullptr : a.loss_out,
                      back ? nullptr : a.lse_out, ctx->status};
-        const long long need = ((long long)a.capacity + 15) / 16, cap = 6ll * ctx->num_sms;
+        const long long need = ((long long)a.capacity + 7) / 8, cap = 8ll * ctx->num_sms;
         hc_status st = launch_pdl(xent_gather_kernel<T>,
                                   dim3((unsigned)(need < 1 ? 1 : need < cap ? need : cap)),
                                   dim3(kGatherThreads), 0, s, "xent_gather_kernel", g, r);
@@ -1209,8 +1222,9 @@ struct Call {
     }
     hc_status forward_few() {
         constexpr int kVec = 16 / (int)sizeof(T);
-        const long long need = ((long long)a.V + kFewRows * kFewThreads / 32 - 1) / (kFewRows * kFewThreads / 32);
-        const long long cap = 4ll * ctx->num_sms;
+        // as many blocks as run at a time, a class a warp at least
+        const long long need = ((long long)a.V + kFewThreads / 32 - 1) / (kFewThreads / 32);
+        const long long cap = (a.capacity <= 2 ? 3ll : 2ll) * ctx->num_sms;
         const int blocks = (int)(need < cap ? need : cap);
         float2* const pairs = (float2*)stream_workspace(s, ((size_t)blocks * kFew + kFew) * sizeof(float2));
         if (!pairs) return HC_ERR_CUDA;
@@ -1272,17 +1286,23 @@ struct Call {
 
     hc_status backward() {
         // pieces of the vocabulary: G of one takes at most 512 MiB, or 2048 classes
-        const long long all = up(a.V, kTile);
+        const long long classes_all = up(a.V, kTile);
         long long most = (512ll << 20) / (mpad * 2 * kPlanes) / kTile * kTile;
         if (most < 2048) most = 2048;
-        const long long pieces = (all + most - 1) / most;
-        const long long piece = up((all + pieces - 1) / pieces, kTile);
+        const long long pieces = (classes_all + most - 1) / most;
+        const long long piece = up((classes_all + pieces - 1) / pieces, kTile);
         const long long xpitch = up(a.C, 4);
         const int bn_v = a.V <= 128 ? 128 : 256, bn_c = a.C <= 128 ? 128 : 256;
         const long long tiles = mpad / kTile * ((a.C + bn_c - 1) / bn_c);
-        // dx has few tiles with long sums: parts of them, 1024 classes at least
+        // dx may have few tiles with long sums. They go first and the tiles of dW
+        // fill up behind them, so that a part of a sum may be as long as two thirds of
+        // a pair's whole work (2048 of 32000 x 1024: two parts; eight of them
+        // cost 15 us for the slabs alone); 1024 classes at least. The same parts
+        // without dW, so that dx does not depend on what else is asked for.
         const int pairs = ctx->num_sms / 2;
-        long long split = (3 * pairs + tiles - 1) / tiles;
+        const long long sum = piece / kKB;
+        const long long all = tiles * sum + piece / kTile * ((a.C + bn_c - 1) / bn_c) * (mpad / kKB);
+        long long split = (3 * sum * pairs + 2 * all - 1) / (2 * all);
         if (split > piece / 1024) split = piece / 1024;
         if (split < 1 || !a.dx) split = 1;
         // so has dW with few classes; 256 tokens at least

@@ -129,12 +129,7 @@ __global__ void __launch_bounds__(kGroupThreads)
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * TPR + t) * VEC;
-                if (res) {
-#pragma unroll
-                    for (int e = 0; e < kU; ++e)
-                        d[i][e] = add(ring[u][i].unit(e), ringr[u][i].unit(e));
-                    ring[u][i].set_units(d[i]);  // rounded to the rows' type
-                }
+                if (res) ring[u][i] = sum_of(ring[u][i], ringr[u][i]);
 #pragma unroll
                 for (int e = 0; e < kU; ++e) d[i][e] = ring[u][i].unit(e);
                 if (c < C) {
@@ -183,25 +178,55 @@ __global__ void __launch_bounds__(kGroupThreads)
             }
             if constexpr (kQ && VEC > 1) {
                 constexpr int kBlockLanes = 128 / VEC < TPR ? 128 / VEC : TPR;
+                float v[NV][VEC];
+                uint32_t top[NV];
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    const int c = (i * TPR + t) * VEC;
-                    float v[VEC];
+                    const bool there = (i * TPR + t) * VEC < C;
 #pragma unroll
                     for (int e = 0; e < kU; ++e) {
                         const float2 f = split(d[i][e]);
-                        v[2 * e] = c < C ? f.x : 0.f;
-                        v[2 * e + 1] = c < C ? f.y : 0.f;
+                        v[i][2 * e] = there ? f.x : 0.f;
+                        v[i][2 * e + 1] = there ? f.y : 0.f;
                     }
-                    uint32_t top = 0;
+                    float most = 0.f;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) top = max(top, mag(v[e]));
+                    for (int e = 0; e < VEC; e += 2) most = max_mag(most, v[i][e], v[i][e + 1]);
+                    top[i] = __float_as_uint(most);
+                }
+                // the maxima of a lane's NV blocks: each exchange leaves it with
+                // half of them, after which lane l goes on with block l % NV
+                const int own = lane % NV;
+                uint32_t m = top[0];
+                if constexpr (NV == 2) {
+                    m = max(own ? top[1] : top[0],
+                            __shfl_xor_sync(0xffffffffu, own ? top[0] : top[1], 1));
+                } else if constexpr (NV == 4) {
+                    const bool b0 = lane & 1, b1 = lane & 2;
+                    const uint32_t m01 = max(b0 ? top[1] : top[0],
+                                             __shfl_xor_sync(0xffffffffu, b0 ? top[0] : top[1], 1));
+                    const uint32_t m23 = max(b0 ? top[3] : top[2],
+                                             __shfl_xor_sync(0xffffffffu, b0 ? top[2] : top[3], 1));
+                    m = max(b1 ? m23 : m01, __shfl_xor_sync(0xffffffffu, b1 ? m01 : m23, 2));
+                }
+                static_assert(NV == 1 || NV == 2 || NV == 4, "blocks of a lane");
 #pragma unroll
-                    for (int o = 1; o < kBlockLanes; o <<= 1)
-                        top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    const float scale = scale_of(__uint_as_float(top));
+                for (int o = NV; o < kBlockLanes; o <<= 1)
+                    m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const float my_scale = scale_of(__uint_as_float(m)), my_inv = 1.f / my_scale;
+                {
+                    const int c = (own * TPR + t) * VEC;
+                    if (in && lane % kBlockLanes < NV && (c & ~127) < C)
+                        o8.scales[(long long)(c / 128) * capacity + n] = my_scale;
+                }
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int c = (i * TPR + t) * VEC;
+                    const int from = (lane & ~(kBlockLanes - 1)) + i;
+                    const float scale = NV == 1 ? my_scale : __shfl_sync(0xffffffffu, my_scale, from);
+                    const float inv = NV == 1 ? my_inv : __shfl_sync(0xffffffffu, my_inv, from);
                     uint32_t word[VEC / 4];
-                    to_e4m3<VEC>(v, scale, 1.f / scale, word);
+                    to_e4m3<VEC>(v[i], scale, inv, word);
                     if (c >= C) {
 #pragma unroll
                         for (int k = 0; k < VEC / 4; ++k) word[k] = 0u;  // the pitch's end
@@ -213,8 +238,6 @@ __global__ void __launch_bounds__(kGroupThreads)
                         else
                             *reinterpret_cast<uint32_t*>(at) = word[0];
                     }
-                    if (in && c < C && c % 128 == 0)
-                        o8.scales[(long long)(c / 128) * capacity + n] = scale;
                 }
             }
             if constexpr (kQ && VEC == 1) {

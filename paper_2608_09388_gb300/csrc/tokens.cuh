@@ -278,6 +278,34 @@ __device__ __forceinline__ void load_floats(const float* __restrict__ p, int c, 
     }
 }
 
+// a + b, rounded to their type. (bf16 pairs in one instruction: one rounding,
+// as a sum in fp32 rounded again gives it too, since that one is exact wherever the
+// smaller number reaches the last place of the result.)
+template <typename P>
+__device__ __forceinline__ P sum_of(const P& a, const P& b) {
+    P r;
+    r.v = a.v;
+    if constexpr (sizeof(r.v) == 16) {
+        r.v = make_float4(a.v.x + b.v.x, a.v.y + b.v.y, a.v.z + b.v.z, a.v.w + b.v.w);
+    } else {
+        const float f[1] = {a.get(0) + b.get(0)};
+        r.set_all(f);
+    }
+    return r;
+}
+__device__ __forceinline__ uint32_t sum_words(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 s = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&a),
+                                     *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&s);
+}
+__device__ __forceinline__ Piece<__nv_bfloat16, 8> sum_of(const Piece<__nv_bfloat16, 8>& a,
+                                                          const Piece<__nv_bfloat16, 8>& b) {
+    Piece<__nv_bfloat16, 8> r;
+    r.v = make_uint4(sum_words(a.v.x, b.v.x), sum_words(a.v.y, b.v.y), sum_words(a.v.z, b.v.z),
+                     sum_words(a.v.w, b.v.w));
+    return r;
+}
+
 // Sum over a group of TPR threads (a power of two; group g of the block owns
 // threads g * TPR ..), the same value in each of them. A group of several
 // warps passes the warps' sums through sh, [2][warps of the block] floats

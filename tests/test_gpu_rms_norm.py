@@ -233,6 +233,27 @@ def test_values(C, dtype):
     assert y[0].isnan().all() and (y[1:5].isfinite()).all() and (y[7:].isfinite()).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("C", [64, 131])
+def test_stored_sums(C, dtype):
+    """The stored sum over all exponents: terms far apart, of opposite signs,
+    halfway cases, numbers below the normal range, zeros of both signs."""
+    g = gen(C)
+    n = 4096
+    e = torch.randint(-149, 120, (2, n, C), generator=g, device="cuda")
+    e[1, ::2] = e[0, ::2] - torch.randint(0, 12, (n // 2, C), generator=g, device="cuda")
+    x, res = ((1 + torch.rand(n, C, generator=g, device="cuda")).double().ldexp(k).float()
+              * torch.randint(0, 2, (n, C), generator=g, device="cuda").mul(2).sub(1) for k in e)
+    x, res = x.to(dtype), res.to(dtype)
+    x[5], res[5] = 0.0, -0.0
+    x[6], res[6] = -0.0, -0.0
+    h, y = torch.empty_like(x), torch.empty_like(x)
+    hc.hc_rms_norm_fwd(x, 1e-5, None, res=res, h=h, y=y)
+    want = stored(x, res)
+    bits = torch.int16 if dtype == BF else torch.int32
+    assert torch.equal(h.view(bits), want.view(bits))
+
+
 def test_differences():
     """dx (with the residual's share) and dgamma against central differences of
     the 64-bit forward, step h = 2^-12: the differences' own error is below h^2
