@@ -294,6 +294,11 @@ struct LinearXentArgs {
 hc_status launch_linear_xent_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
 hc_status launch_linear_xent_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
 
+// The same for few classes of few channels (xent_small.cu).
+bool xent_small_supported(const LinearXentArgs& a);
+hc_status launch_xent_small_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
+hc_status launch_xent_small_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
+
 // Lists of tensors (grad_clip.cu). fill_tensor_list may throw std::bad_alloc.
 size_t tensor_list_bytes(int n);
 bool fill_tensor_list(const void* const* in, void* const* out, const long long* numel,

@@ -21,18 +21,10 @@
 // rows of both operands in each CTA's shared memory, and 2 x 256 columns of
 // TMEM, so that a tile's epilogue runs under the next one's products.
 #include "pipeline.cuh"
+#include "xent.cuh"
 
 namespace hc {
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-// 2^v, 2 units in the last place; results below the normal numbers are zero.
-__device__ __forceinline__ float ex2(float v) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 
 // ---------------------------------------------------------------- layout of a call
 struct Rows {
@@ -875,20 +867,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-// (top, sum) and another pair as one; tops of -infinity hold nothing, a NaN stays.
-__device__ __forceinline__ float2 join_pairs(float2 a, float2 b) {
-    const float least = -__int_as_float(0x7f800000);
-    const float top = fmaxf(a.x, b.x), from = top == least ? 0.f : top;
-    return make_float2(top, a.y * ex2((a.x - from) * kLog2e) + b.y * ex2((b.x - from) * kLog2e));
-}
-__device__ __forceinline__ float2 join_warp(float2 p) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        p = join_pairs(p, make_float2(__shfl_xor_sync(0xffffffffu, p.x, o),
-                                      __shfl_xor_sync(0xffffffffu, p.y, o)));
-    return p;
-}
-
 // ---------------------------------------------------------------- few tokens
 // Up to kFew tokens (a scoring or decoding step): bound by the one read of W,
 // so the sums are taken on the CUDA cores straight from the rows as they are. A
@@ -906,7 +884,7 @@ __device__ __forceinline__ int few_at(int c) {
 }
 
 template <typename T, int VEC, int kTokens>
-__global__ void __launch_bounds__(kFewThreads, kTokens <= 2 ? 3 : 2)
+__global__ void __launch_bounds__(kFewThreads, kTokens == 1 ? 4 : kTokens == 2 ? 3 : 2)
     xent_few_kernel(const T* __restrict__ x, const T* __restrict__ W, const float* __restrict__ bias,
                     const int32_t* targets, int C, int V, float2* __restrict__ pairs,
                     float* __restrict__ at_target) {
@@ -930,15 +908,15 @@ __global__ void __launch_bounds__(kFewThreads, kTokens <= 2 ? 3 : 2)
     for (int t = 0; t < kTokens; ++t) all[t] = make_float2(least, 0.f);
     // whole rounds of kFewRows classes a warp, then what is left in one round of
     // as few as it takes: every warp ends at the same time
-    const int W_ = gridDim.x * (kFewThreads / 32), w_ = (int)blockIdx.x * (kFewThreads / 32) + warp;
-    const int whole = V / (W_ * kFewRows), left = V - whole * W_ * kFewRows;
-    const int last = (left + W_ - 1) / W_;
+    const int warps = gridDim.x * (kFewThreads / 32), w = (int)blockIdx.x * (kFewThreads / 32) + warp;
+    const int whole = V / (warps * kFewRows), left = V - whole * warps * kFewRows;
+    const int last = (left + warps - 1) / warps;
     for (int i = 0; i <= whole; ++i) {
         const int take = i < whole ? kFewRows : last;
-        const long long v0 = (long long)i * W_ * kFewRows + (long long)w_ * take;
+        const long long v0 = (long long)i * warps * kFewRows + (long long)w * take;
         if (v0 >= V || take == 0) break;
         float s[kFewRows][kTokens] = {};
-#pragma unroll 4
+#pragma unroll 2
         for (int c = lane * VEC; c < C; c += 32 * VEC) {
             Piece<T, VEC> p[kFewRows];
 #pragma unroll
@@ -1001,7 +979,7 @@ __global__ void __launch_bounds__(kFew * 32)
     float2 p = make_float2(least, 0.f);
 #pragma unroll 8
     for (int b = lane; b < blocks; b += 32) p = join_pairs(p, pairs[(long long)b * kFew + n]);
-    p = join_warp(p);
+    p = join_lanes<32>(p);
     if (lane != 0) return;
     const float all = p.x + logf(p.y);
     if (lse) lse[n] = in ? all : 0.f;
@@ -1036,7 +1014,7 @@ __global__ void __launch_bounds__(1024)
         __syncthreads();
         sh[warp][lane] = p;
         __syncthreads();
-        p = join_warp(sh[lane][warp]);
+        p = join_lanes<32>(sh[lane][warp]);
         const long long row = row0 + warp;
         if (lane == 0 && row < M) {
             const float all = p.x + logf(p.y);
@@ -1224,7 +1202,7 @@ struct Call {
         constexpr int kVec = 16 / (int)sizeof(T);
         // as many blocks as run at a time, a class a warp at least
         const long long need = ((long long)a.V + kFewThreads / 32 - 1) / (kFewThreads / 32);
-        const long long cap = (a.capacity <= 2 ? 3ll : 2ll) * ctx->num_sms;
+        const long long cap = (a.capacity == 1 ? 4ll : a.capacity == 2 ? 3ll : 2ll) * ctx->num_sms;
         const int blocks = (int)(need < cap ? need : cap);
         float2* const pairs = (float2*)stream_workspace(s, ((size_t)blocks * kFew + kFew) * sizeof(float2));
         if (!pairs) return HC_ERR_CUDA;
@@ -1386,10 +1364,12 @@ struct Call {
 }  // namespace
 
 hc_status launch_linear_xent_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
+    if (xent_small_supported(a)) return launch_xent_small_fwd(ctx, a, s);
     return a.dt == HC_BF16 ? Call<__nv_bfloat16>(ctx, a, s).forward() : Call<float>(ctx, a, s).forward();
 }
 
 hc_status launch_linear_xent_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
+    if (xent_small_supported(a)) return launch_xent_small_bwd(ctx, a, s);
     return a.dt == HC_BF16 ? Call<__nv_bfloat16>(ctx, a, s).backward() : Call<float>(ctx, a, s).backward();
 }
 

@@ -57,6 +57,8 @@ _lock = threading.Lock()
 def load_library(path: str | None = None):
     """Load libhc.so (built by paper_2608_09388_gb300.build). Raises if absent."""
     global _lib
+    if _lib is not None:  # every call asks: the lock alone takes 0.2 us
+        return _lib
     with _lock:
         if _lib is not None:
             return _lib
