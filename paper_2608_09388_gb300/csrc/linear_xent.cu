@@ -5,7 +5,7 @@
 //   dx = G W,  dW = G^T x,  dbias[v] = sum_n G[n][v]
 // The tokens that take part are gathered first, in their order, into M rows
 // of the workspace. Forward, a tile of logits leaves a (largest, sum of
-// exponentials) pair per row and half tile, joined by a last kernel. Backward,
+// exponentials) pair per row and 64 classes, joined by a last kernel. Backward,
 // the vocabulary is taken in pieces: the logits of a piece are formed again,
 // G of the piece is written to the workspace in 16 bits, and both products
 // with it follow; dx is summed over the pieces in fp32.
@@ -14,8 +14,11 @@
 // operands (and then G) are held as three bf16 numbers whose sum is the value
 // to 2^-24 of it, and six of the nine partial products are summed, the small
 // ones first: what is left out is below 2^-24 of a product. For bf16 operands
-// G is rounded to bf16 once (2^-9 of a value, as its factors are): its sums
-// over tokens and classes stay in fp32.
+// G is rounded to bf16 once, as its factors are; its sums over tokens and classes
+// stay in fp32. In dx one value of a row may outweigh all others, its target's: what
+// the rounding takes off that one is kept in fp32 and added with the row of W
+// at the end (8192 of 131072 x 2048: dx off by 0.0027 of its size without, 0.0017
+// is the rounding of dx itself).
 //
 // The products run on pairs of CTAs (cta_group::2): a tile of 256 x 256, 128
 // rows of both operands in each CTA's shared memory, and 2 x 256 columns of
@@ -35,6 +38,7 @@ struct Rows {
     float* lse;        // [mpad] backward
     float* dloss;      // [mpad] backward
     float* at_target;  // [mpad] forward: the target's logit
+    float* rest;       // [mpad] backward, bf16: what rounding took off the target's G
     __nv_bfloat16* x;  // [planes][mpad][pitch]
 };
 
@@ -147,6 +151,22 @@ __global__ void __launch_bounds__(kGatherThreads)
 #pragma unroll 4
                 for (int c = lane * 8; c < a.C; c += 256)
                     *reinterpret_cast<uint4*>(to + c) = *reinterpret_cast<const uint4*>(from + c);
+            } else if (wide) {
+#pragma unroll 4
+                for (int c = lane * 4; c < a.C; c += 128) {
+                    const float4 f = *reinterpret_cast<const float4*>(from + c);
+                    __nv_bfloat16 p[4][3];
+                    planes_of(f.x, p[0]);
+                    planes_of(f.y, p[1]);
+                    planes_of(f.z, p[2]);
+                    planes_of(f.w, p[3]);
+#pragma unroll
+                    for (int k = 0; k < kPlanes; ++k) {
+                        alignas(8) __nv_bfloat16 q[4] = {p[0][k], p[1][k], p[2][k], p[3][k]};
+                        *reinterpret_cast<uint2*>(to + k * a.mpad * a.pitch + c) =
+                            *reinterpret_cast<const uint2*>(q);
+                    }
+                }
             } else {
 #pragma unroll 4
                 for (int c = lane; c < a.C; c += 32) {
@@ -166,9 +186,10 @@ __global__ void __launch_bounds__(kGatherThreads)
         if (threadIdx.x == 0) *r.m = (int)at;
         const long long end = (at + 63) / 64 * 64;
         for (int k = 0; k < kPlanes; ++k) {
-            __nv_bfloat16* const p = r.x + k * a.mpad * a.pitch;
-            for (long long i = at * a.pitch + threadIdx.x; i < end * a.pitch; i += kGatherThreads)
-                p[i] = __float2bfloat16_rn(0.f);
+            // (rows are a multiple of 16 bytes apart)
+            uint4* const p = reinterpret_cast<uint4*>(r.x + k * a.mpad * a.pitch);
+            for (long long i = at * a.pitch / 8 + threadIdx.x; i < end * a.pitch / 8; i += kGatherThreads)
+                p[i] = make_uint4(0u, 0u, 0u, 0u);
         }
     }
 }
@@ -219,10 +240,15 @@ constexpr int kMmaWarp = kStoreWarps + 1;
 constexpr int kThreads = (kStoreWarps + 2) * 32;
 constexpr int kOutBytes = 32 * 128;              // staging of a storing warp
 constexpr int kGroupM = 16;                      // row tiles walked per column of tiles
-// fp32 operands: blocks of the sum behind which the accumulator is added to
-// fp32 registers. The tensor cores truncate at every step of 16, always
-// towards zero: 784 steps at full size left 1.7e-5 of a weight's gradient.
-constexpr int kChain = 4;
+// Blocks of the sum behind which the accumulator is added to fp32 registers,
+// with fp32 operands and for logits. The tensor cores truncate at every step of 16,
+// always towards zero: 784 steps at full size left 1.7e-5 of a weight's
+// gradient, 128 steps 1.6e-6 of a loss (1.25e-8 a step). Results that are rounded to
+// bf16 keep one accumulator.
+template <Product kP, typename T>
+constexpr bool kPromoted = sizeof(T) == 4 || kP != kBack;
+template <typename T>
+constexpr int kChain = sizeof(T) == 4 ? 4 : 8;
 constexpr int kBars = 2 * kStages + 5;
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreWarps * kOutBytes + kBars * 8 + 64;
 static_assert(kSmem <= 232448, "shared memory of a block");
@@ -231,13 +257,14 @@ struct ProductArgs {
     const int* m;        // rows of x and G
     int cols;            // classes of the piece
     int C;
-    int bn;              // columns of a tile, 128 or 256
+    int bn;              // columns of a tile: 256, 128 or (logits) 64
     int planes;          // 1, or 3: six products a block
     int v0;              // first class of the piece
     const float* bias;
     const int* target;
     const float* lse;
     const float* dloss;
+    float* rest;         // kGrad, bf16
     float2* pairs;       // kStats: [classes / kCols][mpad]
     float* at_target;
     float* dbias_part;   // kGrad: [mpad / 32][piece], or NULL
@@ -324,6 +351,27 @@ __device__ __forceinline__ int plane_b(int planes, int p) {
     return planes == 1 ? 0 : (0x201100 >> (4 * (5 - p))) & 3;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// f[j] += bias[j] for the `left` of 32 classes that there are; the same ones
+// in every lane, 16 bytes at a time where their address allows it.
+__device__ __forceinline__ void add_bias(float (&f)[32], const float* bias, int left) {
+    if (left >= 32 && (reinterpret_cast<uintptr_t>(bias) & 15) == 0) {
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            const float4 b = __ldg(reinterpret_cast<const float4*>(bias + j));
+            f[j] += b.x, f[j + 1] += b.y, f[j + 2] += b.z, f[j + 3] += b.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < left) f[j] += __ldg(bias + j);
+    }
+}
+
 // Sums of v[i] over the warp's lanes, column i in lane i.
 __device__ __forceinline__ float column_sums(float (&v)[32]) {
     const int lane = threadIdx.x & 31;
@@ -367,7 +415,7 @@ __device__ __forceinline__ uint32_t scheduled(uint32_t i, uint32_t p, uint32_t P
 template <Product kP, typename T>
 __global__ void __launch_bounds__(kThreads, 1)
     xent_product_kernel(const ProductArgs a, const __grid_constant__ Maps maps) {
-    constexpr bool kPromote = sizeof(T) == 4;
+    constexpr bool kPromote = kPromoted<kP, T>, kPlanes3 = sizeof(T) == 4;
     constexpr bool kBMn = kP == kBack;  // B's rows are along the sum
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -476,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         Work w;
         for (uint32_t i = 0; ok && work_at(i, w); ++i) {
             const int row = w.m * kTile + (int)rank * kHalf, col = w.n * a.bn + (int)rank * a.bn / 2;
-            const int chain = kPromote ? kChain : w.k1 - w.k0;
+            const int chain = kPromote ? kChain<T> : w.k1 - w.k0;
             for (int kc = w.k0; kc < w.k1 && ok; kc += chain)
                 for (int p = 0; p < products && ok; ++p) {
                     const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
@@ -527,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // A of dW is G read along its columns
                 const uint32_t idesc = idesc0 | (w.weight ? 1u << 15 : 0u);
                 const uint32_t lbo = w.weight ? kOperandBytes / 2 : 16, step = w.weight ? 128 : 2;
-                const int chain = kPromote ? kChain : w.k1 - w.k0;
+                const int chain = kPromote ? kChain<T> : w.k1 - w.k0;
                 int kc = w.k0;
                 do {  // an empty sum of bf16 operands still passes its accumulator on
                     if (kPromote && kc >= w.k1) break;
@@ -594,18 +642,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (kPromote) {
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) sums[j] = 0.f;
-                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain) {
+                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<T>) {
                     next();
                     if (!ok) break;
                     if (mine) {
 #pragma unroll
-                        for (int c = 0; c < kCols; c += 32) {
-                            uint32_t r[32];
-                            tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
+                        for (int c = 0; c < kCols; c += 16) {
+                            uint32_t r[16];
+                            tmem_ld(acc + (uint32_t)c, r);
                             tmem_ld_wait();
-                            if (c + 32 == kCols) give_back();
+                            if (c + 16 == kCols) give_back();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sums[c + j] += __uint_as_float(r[j]);
+                            for (int j = 0; j < 16; ++j) sums[c + j] += __uint_as_float(r[j]);
                         }
                     } else {
                         give_back();
@@ -661,11 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float f[32];
                     load(c, f);
                     const int col = col0 + c;
-                    if (a.bias) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j < a.cols) f[j] += __ldg(a.bias + col + j);
-                    }
+                    if (a.bias) add_bias(f, a.bias + col, a.cols - col);
                     if (col + 32 > a.cols) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
@@ -673,8 +717,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     float m4[4] = {top, least, least, least};
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) m4[j & 3] = fmaxf(m4[j & 3], f[j]);
-                    const float most = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                    for (int j = 0; j < 32; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], f[j], f[j + 1]);
+                    const float most = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]);
                     if (target >= col && target < col + 32) {
                         float v = 0.f;
 #pragma unroll
@@ -682,13 +726,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                         a.at_target[row] = v;
                     }
                     // classes masked with -infinity leave it at that; a NaN
-                    // goes past fmaxf and into the sum
+                    // goes past the maximum and into the sum
                     const float from = most == least ? 0.f : most;
                     sum *= ex2((top - from) * kLog2e);
-                    float s4[4] = {0.f, 0.f, 0.f, 0.f};
+                    const F2 less = make_f2(-from, -from), scale = make_f2(kLog2e, kLog2e);
+                    F2 s2[2] = {make_f2(0.f, 0.f), make_f2(0.f, 0.f)};
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) s4[j & 3] += ex2((f[j] - from) * kLog2e);
-                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 e = split(mul(add(make_f2(f[j], f[j + 1]), less), scale));
+                        s2[j / 2 & 1] = add(s2[j / 2 & 1], make_f2(ex2(e.x), ex2(e.y)));
+                    }
+                    sum += total(add(s2[0], s2[1]));
                     top = most;
                 }
                 if (row < M && col0 < a.cols)
@@ -699,36 +747,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int target = in ? a.target[row] - a.v0 : -1;
                 // the whole of it inside: no looks at rows and columns
                 const bool whole = row0 + 32 <= M && col0 + kCols <= a.cols;
-                float keep[kPromote ? kCols : 1];
-                if (!kPromote) staging_free();
+                float keep[kPlanes3 ? kCols : 1];
+                if (!kPlanes3) staging_free();
 #pragma unroll
                 for (int c = 0; c < kCols; c += 32) {
                     float f[32];
                     load(c, f);
                     const int col = col0 + c;
-                    if (a.bias) {
+                    if (a.bias) add_bias(f, a.bias + a.v0 + col, a.cols - col);
+                    const F2 less = make_f2(-lse, -lse), scale = make_f2(kLog2e, kLog2e);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j < a.cols) f[j] += __ldg(a.bias + a.v0 + col + j);
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 e = split(mul(add(make_f2(f[j], f[j + 1]), less), scale));
+                        f[j] = ex2(e.x);
+                        f[j + 1] = ex2(e.y);
                     }
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = ex2((f[j] - lse) * kLog2e);
                     if (target >= col && target < col + 32) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) f[j] -= col + j == target ? 1.f : 0.f;
                     }
                     if (whole) {
+                        const F2 times = make_f2(dloss, dloss);
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) f[j] *= dloss;
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 e = split(mul(make_f2(f[j], f[j + 1]), times));
+                            f[j] = e.x;
+                            f[j + 1] = e.y;
+                        }
                     } else {
 #pragma unroll
                         for (int j = 0; j < 32; ++j)
                             f[j] = in && col + j < a.cols ? f[j] * dloss : 0.f;
                     }
-                    if constexpr (kPromote) {
+                    if constexpr (kPlanes3) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) keep[c + j] = f[j];
                     } else {
+                        if (target >= col && target < col + 32) {
+                            float v = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v = col + j == target ? f[j] : v;
+                            a.rest[row] = v - __bfloat162float(__float2bfloat16_rn(v));
+                        }
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
                             put(c / 8 + q,
@@ -741,7 +801,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             a.dbias_part[(long long)(row0 / 32) * a.piece + col + lane] = s;
                     }
                 }
-                if constexpr (kPromote) {
+                if constexpr (kPlanes3) {
                     // three planes, each what the ones before leave
 #pragma unroll
                     for (int k = 0; k < 3; ++k) {
@@ -903,9 +963,15 @@ __global__ void __launch_bounds__(kFewThreads, kTokens == 1 ? 4 : kTokens == 2 ?
             rows[t * pitch + few_at<T, VEC>(c)] = to_f32(x[(long long)t * C + c]);
     }
     __syncthreads();
-    float2 all[kTokens];
+    // Of the kValues sums of a round (class r, token t) a lane keeps one, the
+    // lane's upper bits being r and t: its class's running pair
+    constexpr int kT = kTokens == 3 ? 4 : kTokens, kValues = kFewRows * kT;
+    constexpr int kSame = 32 / kValues;  // lanes with the same value
+    const int my_r = lane / (32 / kFewRows), my_t = lane / kSame % kT;
+    int my_target = -1;
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t) all[t] = make_float2(least, 0.f);
+    for (int t = 0; t < kTokens; ++t) my_target = my_t == t ? target[t] : my_target;
+    float2 mine = make_float2(least, 0.f);
     // whole rounds of kFewRows classes a warp, then what is left in one round of
     // as few as it takes: every warp ends at the same time
     const int warps = gridDim.x * (kFewThreads / 32), w = (int)blockIdx.x * (kFewThreads / 32) + warp;
@@ -940,21 +1006,34 @@ __global__ void __launch_bounds__(kFewThreads, kTokens == 1 ? 4 : kTokens == 2 ?
                     for (int e = 0; e < VEC; ++e) s[r][t] = fmaf(p[r].get(e), f[e], s[r][t]);
             }
         }
+        // sums over the lanes, half of the values left to each at every step
+        float v[kValues];
 #pragma unroll
-        for (int r = 0; r < kFewRows; ++r) {
-            if (r >= take || v0 + r >= V) break;
-            const float b = bias ? __ldg(bias + v0 + r) : 0.f;
+        for (int k = 0; k < kValues; ++k) v[k] = k % kT < kTokens ? s[k / kT][k % kT] : 0.f;
+        int o = 16;
 #pragma unroll
-            for (int t = 0; t < kTokens; ++t) {
-                const float l = warp_sum(s[r][t]) + b;
-                if (lane == 0 && v0 + r == target[t]) at_target[t] = l;
-                all[t] = join_pairs(all[t], make_float2(l, 1.f));
+        for (int half = kValues / 2; half > 0; half /= 2, o /= 2) {
+            const bool up = lane & o;
+#pragma unroll
+            for (int k = 0; k < half; ++k) {
+                const float send = up ? v[k] : v[k + half], keep = up ? v[k + half] : v[k];
+                v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
             }
         }
-    }
-    if (lane == 0)
 #pragma unroll
-        for (int t = 0; t < kTokens; ++t) sh[warp][t] = all[t];
+        for (int q = kSame / 2; q > 0; q /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], q);
+        const long long cls = v0 + my_r;
+        if (my_r < take && cls < V && my_t < kTokens) {
+            const float l = v[0] + (bias ? __ldg(bias + cls) : 0.f);
+            if (lane % kSame == 0 && cls == my_target) at_target[my_t] = l;
+            mine = join_pairs(mine, make_float2(l, 1.f));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o >= 32 / kFewRows; o /= 2)  // the classes of a token
+        mine = join_pairs(mine, make_float2(__shfl_xor_sync(0xffffffffu, mine.x, o),
+                                            __shfl_xor_sync(0xffffffffu, mine.y, o)));
+    if (my_r == 0 && lane % kSame == 0 && my_t < kTokens) sh[warp][my_t] = mine;
     __syncthreads();
     if (threadIdx.x < kTokens) {
         float2 p = sh[0][threadIdx.x];
@@ -987,51 +1066,63 @@ __global__ void __launch_bounds__(kFew * 32)
 }
 
 // ---------------------------------------------------------------- joins
-// The pairs of a row -> loss and lse: 32 rows a block, every 32nd pair a warp;
-// then a warp per row.
-__global__ void __launch_bounds__(1024)
+// The pairs of a row -> loss and lse: 8 rows a block (64 neighbouring bytes of a
+// part), every 128th part a thread; then a warp per row. Rows may be few
+// and parts many: 1152 rows of 1261 parts took 25 us with 32 rows a block.
+constexpr int kLossRows = 8, kLossThreads = 1024, kLossParts = kLossThreads / kLossRows;
+
+__global__ void __launch_bounds__(kLossThreads)
     xent_loss_kernel(const Rows r, const float2* __restrict__ pairs, int parts, long long mpad,
                      float* loss, float* lse) {
-    __shared__ float2 sh[32][33];
+    __shared__ float2 sh[kLossRows][kLossParts + 1];
     pdl_wait();
     pdl_trigger();
-    const int M = *r.m, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int M = *r.m, sub = threadIdx.x % kLossRows, first = threadIdx.x / kLossRows;
     const float least = -__int_as_float(0x7f800000);
-    for (long long row0 = blockIdx.x * 32ll; row0 < M; row0 += gridDim.x * 32ll) {
+    for (long long row0 = blockIdx.x * (long long)kLossRows; row0 < M;
+         row0 += gridDim.x * (long long)kLossRows) {
         float2 p = make_float2(least, 0.f);
-        if (row0 + lane < M) {
-            constexpr int kLoads = 8;
-            for (int h = warp; h < parts; h += 32 * kLoads) {
+        if (row0 + sub < M) {
+            constexpr int kLoads = 4;
+            for (int h = first; h < parts; h += kLossParts * kLoads) {
                 float2 q[kLoads];
 #pragma unroll
                 for (int k = 0; k < kLoads; ++k)
-                    q[k] = h + 32 * k < parts ? pairs[(h + 32ll * k) * mpad + row0 + lane]
-                                              : make_float2(least, 0.f);
-#pragma unroll
-                for (int k = 0; k < kLoads; ++k) p = join_pairs(p, q[k]);
+                    q[k] = h + kLossParts * k < parts
+                               ? pairs[(h + (long long)kLossParts * k) * mpad + row0 + sub]
+                               : make_float2(least, 0.f);
+                p = join_pairs(p, join_pairs(join_pairs(q[0], q[1]), join_pairs(q[2], q[3])));
             }
         }
         __syncthreads();
-        sh[warp][lane] = p;
+        sh[sub][first] = p;
         __syncthreads();
-        p = join_lanes<32>(sh[lane][warp]);
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         const long long row = row0 + warp;
-        if (lane == 0 && row < M) {
-            const float all = p.x + logf(p.y);
-            const int n = r.token_of[row];
-            if (lse) lse[n] = all;
-            if (loss) loss[n] = all - r.at_target[row];
+        if (warp < kLossRows && row < M) {
+            p = sh[warp][lane];
+#pragma unroll
+            for (int k = 32; k < kLossParts; k += 32) p = join_pairs(p, sh[warp][lane + k]);
+            p = join_lanes<32>(p);
+            if (lane == 0) {
+                const float all = p.x + logf(p.y);
+                const int n = r.token_of[row];
+                if (lse) lse[n] = all;
+                if (loss) loss[n] = all - r.at_target[row];
+            }
         }
     }
 }
 
 // Rows of a result from its slabs. dx: the rows n < N', zero for tokens that
-// take no part; a piece of dW: all its rows. Four channels a lane.
+// take no part, with the `rest` of the target's G times its row of W where there
+// is one; a piece of dW: all its rows. Four channels a lane.
 template <typename T>
 __global__ void __launch_bounds__(256)
     xent_slabs_kernel(const int32_t* count, long long capacity, const int* row_of,
                       const float* __restrict__ slabs, int split, long long slab_rows, long long pitch,
-                      int C, bool wide, T* out, unsigned* status) {
+                      int C, bool wide, const float* __restrict__ rest, const int* __restrict__ target,
+                      const T* __restrict__ W, T* out, unsigned* status) {
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
@@ -1046,10 +1137,26 @@ __global__ void __launch_bounds__(256)
         if (c >= C) continue;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (row >= 0) {
-#pragma unroll 4
+#pragma unroll 8
             for (int s = 0; s < split; ++s) {
                 const float4 f = *reinterpret_cast<const float4*>(slabs + (s * slab_rows + row) * pitch + c);
                 v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
+            }
+            if (rest) {
+                const float by = rest[row];
+                const T* const w = W + (long long)target[row] * C + c;
+                float f[4];
+                if (wide) {
+                    Piece<T, 4> q;
+                    q.load(w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] = q.get(e);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] = c + e < C ? to_f32(w[e]) : 0.f;
+                }
+                v.x = fmaf(by, f[0], v.x), v.y = fmaf(by, f[1], v.y);
+                v.z = fmaf(by, f[2], v.z), v.w = fmaf(by, f[3], v.w);
             }
         }
         T* const to = out + n * C + c;
@@ -1155,6 +1262,7 @@ struct Call {
         if (back) {
             r.lse = l.take<float>(mpad);
             r.dloss = l.take<float>(mpad);
+            r.rest = l.take<float>(mpad);
         } else {
             r.at_target = l.take<float>(mpad);
         }
@@ -1215,20 +1323,38 @@ struct Call {
                           (const float*)at_target, a.loss_out, a.lse_out, ctx->status);
     }
 
+    // Columns of a tile of logits: the ones whose rounds over the pairs of SMs take
+    // least. A block of the sum takes 512 clocks with 256 columns, about 380 and
+    // 320 with 128 and 64, which the loads bound (79 tokens of 113 x 2036 fp32: 63 us in
+    // one tile of 256, 50 in two of 64).
+    int columns(long long classes) const {
+        const long long pairs = ctx->num_sms / 2;
+        auto cost = [&](int bn) {
+            const long long units = mpad / kTile * ((classes + bn - 1) / bn);
+            return (units + pairs - 1) / pairs * (bn == 256 ? 8 : bn == 128 ? 6 : 5);
+        };
+        int bn = 256;
+        if (cost(128) < cost(bn)) bn = 128;
+        if (cost(64) < cost(bn)) bn = 64;
+        return bn;
+    }
+
     // The rows of `out` from `split` slabs (row_of: dx, else a piece of dW).
     hc_status join(const int32_t* count, long long rows_, const int* row_of, const float* slabs, int split,
                    long long slab_rows, long long xpitch, T* out) {
-        const bool wide = a.C % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0;
+        const float* const rest = row_of && kPlanes == 1 ? r.rest : nullptr;
+        auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & (4 * sizeof(T) - 1)) == 0; };
+        const bool wide = a.C % 4 == 0 && aligned(out) && (!rest || aligned(a.W));
         const long long need = (rows_ * ((a.C + 127) / 128) + 7) / 8, cap = 8ll * ctx->num_sms;
         return launch_pdl(xent_slabs_kernel<T>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0, s,
                           "xent_slabs_kernel", count, rows_, row_of, slabs, split, slab_rows, xpitch, a.C,
-                          wide, out, ctx->status);
+                          wide, rest, (const int*)r.target, (const T*)a.W, out, ctx->status);
     }
 
     hc_status forward() {
         // their rows have to fit the 48 KiB of shared memory that every launch may have
         if (a.capacity <= kFew && (long long)a.capacity * up(a.C, 256) * 4 <= 47 * 1024) return forward_few();
-        const int bn = a.V <= 128 ? 128 : 256;
+        const int bn = columns(a.V);
         const int parts = (int)(((long long)a.V + kCols - 1) / kCols);
         float2* pairs = nullptr;
         auto place = [&](Layout l) {
@@ -1257,8 +1383,8 @@ struct Call {
         p.status = ctx->status;
         st = product<kStats, T>(ctx, p, mpad / kTile * ((a.V + (long long)bn - 1) / bn), maps, s);
         if (st != HC_OK) return st;
-        const long long need = mpad / 32, cap = 2ll * ctx->num_sms;
-        return launch_pdl(xent_loss_kernel, dim3((unsigned)(need < cap ? need : cap)), dim3(1024), 0, s,
+        const long long need = ((long long)a.capacity + kLossRows - 1) / kLossRows, cap = 2ll * ctx->num_sms;
+        return launch_pdl(xent_loss_kernel, dim3((unsigned)(need < cap ? need : cap)), dim3(kLossThreads), 0, s,
                           "xent_loss_kernel", r, (const float2*)pairs, parts, mpad, a.loss_out, a.lse_out);
     }
 
@@ -1270,7 +1396,7 @@ struct Call {
         const long long pieces = (classes_all + most - 1) / most;
         const long long piece = up((classes_all + pieces - 1) / pieces, kTile);
         const long long xpitch = up(a.C, 4);
-        const int bn_v = a.V <= 128 ? 128 : 256, bn_c = a.C <= 128 ? 128 : 256;
+        const int bn_v = columns(piece < a.V ? piece : a.V), bn_c = a.C <= 128 ? 128 : 256;
         const long long tiles = mpad / kTile * ((a.C + bn_c - 1) / bn_c);
         // dx may have few tiles with long sums. They go first and the tiles of dW
         // fill up behind them, so that a part of a sum may be as long as two thirds of
@@ -1324,6 +1450,7 @@ struct Call {
         p.target = r.target;
         p.lse = r.lse;
         p.dloss = r.dloss;
+        p.rest = r.rest;
         p.dbias_part = part;
         p.mpad = mpad;
         p.piece = piece;
