@@ -244,11 +244,13 @@ constexpr int kGroupM = 16;                      // row tiles walked per column 
 // with fp32 operands and for logits. The tensor cores truncate at every step of 16,
 // always towards zero: 784 steps at full size left 1.7e-5 of a weight's
 // gradient, 128 steps 1.6e-6 of a loss (1.25e-8 a step). Results that are rounded to
-// bf16 keep one accumulator.
+// bf16 keep one accumulator; the logits of G, which is rounded too, are taken
+// in chains twice as long as those of the loss (8 blocks: 2048 of 32000 x 1024
+// 94 us, 16: 86).
 template <Product kP, typename T>
 constexpr bool kPromoted = sizeof(T) == 4 || kP != kBack;
-template <typename T>
-constexpr int kChain = sizeof(T) == 4 ? 4 : 8;
+template <Product kP, typename T>
+constexpr int kChain = sizeof(T) == 4 ? 4 : kP == kStats ? 8 : 16;
 constexpr int kBars = 2 * kStages + 5;
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreWarps * kOutBytes + kBars * 8 + 64;
 static_assert(kSmem <= 232448, "shared memory of a block");
@@ -385,6 +387,18 @@ __device__ __forceinline__ float column_sums(float (&v)[32]) {
         }
     }
     return v[0];
+}
+
+// G of bf16 operands is held divided by a number in [1, 2) that takes the
+// mantissa off the first row's dloss. Where all tokens have the same dloss (a mean
+// over tokens), a target far from sure then is a power of two to the last
+// place, and rounding it costs nothing; with the mantissa, all of them were
+// rounded by the same part (dW off by 0.0019 to 0.0027 of its size by what
+// the number of tokens happened to be). Products with G are multiplied by it.
+__device__ __forceinline__ float scale_of_g(const float* dloss, int M) {
+    if (M <= 0) return 1.f;
+    const uint32_t b = __float_as_uint(__ldg(dloss)), e = b & 0x7f800000u;
+    return e == 0u || e == 0x7f800000u ? 1.f : __uint_as_float((b & 0x007fffffu) | 0x3f800000u);
 }
 
 // What the pair does: a tile of one of the results, and the blocks [k0, k1)
@@ -524,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         Work w;
         for (uint32_t i = 0; ok && work_at(i, w); ++i) {
             const int row = w.m * kTile + (int)rank * kHalf, col = w.n * a.bn + (int)rank * a.bn / 2;
-            const int chain = kPromote ? kChain<T> : w.k1 - w.k0;
+            const int chain = kPromote ? kChain<kP, T> : w.k1 - w.k0;
             for (int kc = w.k0; kc < w.k1 && ok; kc += chain)
                 for (int p = 0; p < products && ok; ++p) {
                     const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
@@ -575,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // A of dW is G read along its columns
                 const uint32_t idesc = idesc0 | (w.weight ? 1u << 15 : 0u);
                 const uint32_t lbo = w.weight ? kOperandBytes / 2 : 16, step = w.weight ? 128 : 2;
-                const int chain = kPromote ? kChain<T> : w.k1 - w.k0;
+                const int chain = kPromote ? kChain<kP, T> : w.k1 - w.k0;
                 int kc = w.k0;
                 do {  // an empty sum of bf16 operands still passes its accumulator on
                     if (kPromote && kc >= w.k1) break;
@@ -620,6 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t stage = out_at + (uint32_t)warp * kOutBytes;
         const uint32_t tempty0 = cluster_map(tempty_bar(0), 0);
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const float g_scale = kP != kStats && !kPlanes3 ? scale_of_g(a.dloss, M) : 1.f;
         uint32_t tile = 0;
         bool ok = true;
         Work w;
@@ -642,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if constexpr (kPromote) {
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) sums[j] = 0.f;
-                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<T>) {
+                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<kP, T>) {
                     next();
                     if (!ok) break;
                     if (mine) {
@@ -652,8 +667,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                             tmem_ld(acc + (uint32_t)c, r);
                             tmem_ld_wait();
                             if (c + 16 == kCols) give_back();
+                            if (kc == w.k0) {
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) sums[c + j] += __uint_as_float(r[j]);
+                                for (int j = 0; j < 16; ++j) sums[c + j] = __uint_as_float(r[j]);
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) sums[c + j] += __uint_as_float(r[j]);
+                            }
                         }
                     } else {
                         give_back();
@@ -743,7 +763,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     a.pairs[(long long)(col0 / kCols) * a.mpad + row] = make_float2(top, sum);
             } else if constexpr (kP == kGrad) {
                 const bool in = row < M;
-                const float lse = in ? a.lse[row] : 0.f, dloss = in ? a.dloss[row] : 0.f;
+                const float lse = in ? a.lse[row] : 0.f;
+                const float dloss = in ? a.dloss[row] / g_scale : 0.f;
                 const int target = in ? a.target[row] - a.v0 : -1;
                 // the whole of it inside: no looks at rows and columns
                 const bool whole = row0 + 32 <= M && col0 + kCols <= a.cols;
@@ -787,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             float v = 0.f;
 #pragma unroll
                             for (int j = 0; j < 32; ++j) v = col + j == target ? f[j] : v;
-                            a.rest[row] = v - __bfloat162float(__float2bfloat16_rn(v));
+                            a.rest[row] = (v - __bfloat162float(__float2bfloat16_rn(v))) * g_scale;
                         }
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
@@ -798,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (a.dbias_part) {
                         const float s = column_sums(f);
                         if (col + lane < a.cols)
-                            a.dbias_part[(long long)(row0 / 32) * a.piece + col + lane] = s;
+                            a.dbias_part[(long long)(row0 / 32) * a.piece + col + lane] = s * g_scale;
                     }
                 }
                 if constexpr (kPlanes3) {
@@ -859,6 +880,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int c = 0; c < kCols; c += 32) {
                     float f[32];
                     load(c, f);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] *= g_scale;
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
                         put(c / 8 + q,
@@ -1122,12 +1145,14 @@ __global__ void __launch_bounds__(256)
     xent_slabs_kernel(const int32_t* count, long long capacity, const int* row_of,
                       const float* __restrict__ slabs, int split, long long slab_rows, long long pitch,
                       int C, bool wide, const float* __restrict__ rest, const int* __restrict__ target,
-                      const T* __restrict__ W, T* out, unsigned* status) {
+                      const T* __restrict__ W, const float* __restrict__ dloss, const int* m, T* out,
+                      unsigned* status) {
     pdl_wait();
     pdl_trigger();
     const long long rows = token_rows(count, capacity, status);
     // a row's pieces of 128 channels, one after another
     const int lane = threadIdx.x & 31, per = (C + 127) / 128;
+    const float g_scale = sizeof(T) == 4 ? 1.f : scale_of_g(dloss, *m);
     const long long step = (long long)gridDim.x * 8;
     for (long long i = (blockIdx.x * 256 + threadIdx.x) >> 5; i < rows * per; i += step) {
         int k;
@@ -1142,6 +1167,7 @@ __global__ void __launch_bounds__(256)
                 const float4 f = *reinterpret_cast<const float4*>(slabs + (s * slab_rows + row) * pitch + c);
                 v.x += f.x, v.y += f.y, v.z += f.z, v.w += f.w;
             }
+            v.x *= g_scale, v.y *= g_scale, v.z *= g_scale, v.w *= g_scale;
             if (rest) {
                 const float by = rest[row];
                 const T* const w = W + (long long)target[row] * C + c;
@@ -1348,7 +1374,8 @@ struct Call {
         const long long need = (rows_ * ((a.C + 127) / 128) + 7) / 8, cap = 8ll * ctx->num_sms;
         return launch_pdl(xent_slabs_kernel<T>, dim3((unsigned)(need < cap ? need : cap)), dim3(256), 0, s,
                           "xent_slabs_kernel", count, rows_, row_of, slabs, split, slab_rows, xpitch, a.C,
-                          wide, rest, (const int*)r.target, (const T*)a.W, out, ctx->status);
+                          wide, rest, (const int*)r.target, (const T*)a.W, (const float*)r.dloss, (const int*)r.m, out,
+                          ctx->status);
     }
 
     hc_status forward() {
