@@ -52,7 +52,7 @@ def check(grads, outs, norm, max_norm, before=None):
 # one element, pieces that are not full, the border of a unit and of the units
 # a block loads together, more units than blocks
 SIZES = [[1], [0, 3], [7, 8, 9], [4095, 4096, 4097], [8191, 8192, 8193], [16384, 16385, 1, 65536],
-         [1000] * 300, [3000000, 5, 0, 70001], [12345678]]
+         [1000] * 300, [37, 4100] * 400, [3000000, 5, 0, 70001], [12345678]]
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16", "mixed"])

@@ -84,7 +84,8 @@ def bwd_ref(x, W, b, t, lse, dloss):
     G = G * dloss.to(D64)[:, None]
     xd, Wd = x.to(D64), W.to(D64)
     half = 2.0 ** -8 if x.dtype == BF else 2.0 ** -24
-    tg16 = tg + half * G.abs()
+    # the products may take a number below the normal range as zero: all of it is off
+    tg16 = tg + half * G.abs() + torch.where(G.abs() < 2.0 ** -126, G.abs(), 0.0)
     dx, dW, db = G @ Wd, G.t() @ xd, G.sum(0)
     Sx, Sw = G.abs() @ Wd.abs(), G.abs().t() @ xd.abs()
     tdx = tg16 @ Wd.abs() + sum_tol(W.shape[0], x.dtype, Sx) + rounding(x.dtype, dx)
@@ -273,6 +274,50 @@ def test_targets_out_of_range():
     hc.hc_linear_cross_entropy_fwd(x, W, b, clean, got["loss"], count=count_of(n + 1))
     assert hc.hc_get_device_status() == hc.HC_ERR_CAPACITY
     assert torch.equal(got["loss"], want["loss"])
+
+
+def test_equal_weights():
+    """A mean over tokens that are far from sure: G's target entries, p - 1 times
+    one number, are held to p of it (below 2^-9, p - 1 rounds to -1), the others to
+    2^-8 of themselves, whatever that number's mantissa; dx has the target's
+    rounding given back."""
+    n, V, C = 700, 3000, 264
+    x, W, b, t, _ = inputs(12, n, V, C, BF, bias=False, ignored=0.0)
+    x = (x.float() * 0.05).to(BF)
+    for weight in (1 / 700, -1.9921875 / 512, 3e-30, 1.0):
+        dloss = full((n,), value=weight)
+        o = run_all(x, W, b, t, dloss, None)
+        l, T = logits_ref(x, W, b)
+        d = l - o["lse"].to(D64)[:, None]
+        p = torch.exp(d)
+        assert float(p.max()) < 2.0 ** -9
+        w = dloss.to(D64).abs()[:, None]
+        tp = p * (T + 2.0 ** -21 + 4 * U * (d.abs() + o["lse"].to(D64).abs()[:, None]))
+        at = torch.zeros_like(p).scatter_(1, t.long()[:, None], 1.0)
+        G = (p - at) * dloss.to(D64)[:, None]
+        tg = (tp + 4 * U * at + 2.0 ** -8 * p) * w
+        xd, Wd = x.to(D64), W.to(D64)
+        dx, dW = G @ Wd, G.t() @ xd
+        within(o["dx"], dx, tg @ Wd.abs() + sum_tol(V, BF, G.abs() @ Wd.abs()) + rounding(BF, dx), "dx")
+        within(o["dW"], dW, (tg + p * at * w).t() @ xd.abs() + sum_tol(n, BF, G.abs().t() @ xd.abs())
+               + rounding(BF, dW), "dW")
+        within(o["dbias"], G.sum(0), ((tp + 4 * U * at) * w).sum(0) + (n + 8) * U * G.abs().sum(0), "dbias")
+
+
+def test_first_weight_special():
+    """The first token's dloss of zero, infinite, or below the normal numbers:
+    the others' gradients are as without it."""
+    n, V, C = 300, 500, 136
+    x, W, b, t, dloss = inputs(13, n, V, C, BF, ignored=0.0)
+    dloss[0] = 0
+    want = run_all(x, W, b, t, dloss, None)
+    check(x, W, b, t, dloss, n, want)
+    for first in (2.0 ** -140, -2.0 ** -149):
+        dloss[0] = first
+        check(x, W, b, t, dloss, n, run_all(x, W, b, t, dloss, None))
+    dloss[0] = float("inf")
+    o = run_all(x, W, b, t, dloss, None)
+    assert torch.equal(o["dx"][1:], want["dx"][1:]) and not o["dx"][0].isfinite().any()
 
 
 def test_differences():
