@@ -665,7 +665,8 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
  *   x         [capacity, C] of dtype dt
  *   W         [V, C] of dtype dt: a row per class, as an embedding table has
  *             (the same table may serve both)
- *   bias      [V] fp32, or NULL (0); -infinity excludes a class
+ *   bias      [V] fp32, or NULL (0); -infinity excludes a class (a token whose
+ *             classes are all excluded has the loss NaN)
  *   targets   [capacity] int32
  *   loss, lse [capacity] fp32, or NULL each; at least one is required. lse is
  *             what hc_linear_cross_entropy_bwd reads

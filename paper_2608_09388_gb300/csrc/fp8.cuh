@@ -13,16 +13,17 @@ namespace hc {
 constexpr float kE4m3Max = 448.f;
 constexpr float kMinScale = 1.17549435e-38f;  // 2^-126
 
-// amax / 448 by Markstein's correction (see to_e4m3), divided where a
-// residual would leave the range of fp32.
+// Where a number lies below this, its block is worked on 2^64 times as large:
+// a residual (see to_e4m3) would leave the range of fp32.
+constexpr float kTiny = 0x1p-90f, kUp = 0x1p64f, kDown = 0x1p-64f;
+
+// max(amax / 448, 2^-126) by Markstein's correction; an infinity or a NaN passes.
 __device__ __forceinline__ float scale_of(float amax) {
     constexpr float kInv = 1.f / kE4m3Max;
-    if (amax >= 0x1p-90f && amax < __int_as_float(0x7f800000)) {
-        const float q = amax * kInv;
-        return fmaf(fmaf(q, -kE4m3Max, amax), kInv, q);
-    }
-    const float s = amax / kE4m3Max;
-    return s < kMinScale ? kMinScale : s;  // a NaN passes
+    const bool tiny = amax < kTiny;
+    const float a = tiny ? amax * kUp : amax, q = a * kInv;
+    const float c = fmaf(fmaf(q, -kE4m3Max, a), kInv, q), s = tiny ? c * kDown : c;
+    return !(amax < __int_as_float(0x7f800000)) ? amax : s < kMinScale ? kMinScale : s;
 }
 // The largest magnitude of three, a NaN if one of them is.
 __device__ __forceinline__ float max_mag(float a, float b, float c) {
@@ -45,19 +46,28 @@ __device__ __forceinline__ uint32_t first_bytes(int n) {
 // quotient is q - (q * scale - x) * inv with q = x * inv (Markstein's
 // correction): the residual is exact, and with a correctly rounded inv the
 // result is the correctly rounded quotient, as the division gives it, also
-// for a zero of either sign. Where the residual would leave the range of fp32
-// (or scale is infinite or a NaN) the values are divided.
+// for a zero of either sign. Under a scale that is infinite or a NaN the
+// values are divided.
 template <int N>
 __device__ __forceinline__ void to_e4m3(const float (&x)[N], float scale, float inv,
                                         uint32_t (&w)[N / 4]) {
-    if (scale >= 0x1p-90f && scale < __int_as_float(0x7f800000)) {
-        const F2 s = make_f2(scale, scale), i1 = make_f2(inv, inv), i2 = make_f2(-inv, -inv);
+    if (scale < __int_as_float(0x7f800000)) {
+        const bool tiny = scale < kTiny;
+        const float sc = tiny ? scale * kUp : scale, in = tiny ? inv * kDown : inv;
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = x[i];
+        if (tiny) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] *= kUp;
+        }
+        const F2 s = make_f2(sc, sc), i1 = make_f2(in, in), i2 = make_f2(-in, -in);
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
             float2 f[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float a = x[i + 2 * h], b = x[i + 2 * h + 1];
+                const float a = v[i + 2 * h], b = v[i + 2 * h + 1];
                 const F2 q = mul(make_f2(a, b), i1);
                 f[h] = split(fma(fma(q, s, make_f2(-a, -b)), i2, q));
             }

@@ -155,7 +155,9 @@ __global__ void __launch_bounds__(kThreads, kResident)
                 } else {
 #pragma unroll 1
                     for (int i = 0; i < 4 * kPieces; ++i) {
-                        const uint4 q = i < 4 ? v[0] : v[1];
+                        uint4 q = v[0];
+#pragma unroll
+                        for (int j = 1; j < kPieces; ++j) q = i >> 2 == j ? v[j] : q;
                         const uint32_t w = (i & 2) ? ((i & 1) ? q.w : q.z) : ((i & 1) ? q.y : q.x);
                         const float2 f = bf16 ? halves(w) : make_float2(__uint_as_float(w), 0.f);
                         far += (double)f.x * f.x + (double)f.y * f.y;

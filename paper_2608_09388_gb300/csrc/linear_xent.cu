@@ -44,12 +44,13 @@ struct Rows {
 
 // ---------------------------------------------------------------- gather
 __device__ __forceinline__ void planes_of(float v, __nv_bfloat16 (&p)[3]) {
-    p[0] = __float2bfloat16_rn(v);
-    const float r = v - __bfloat162float(p[0]);
-    // an infinity or a NaN is all in the first
-    const bool plain = fabsf(v) < __int_as_float(0x7f800000) && fabsf(r) < __int_as_float(0x7f800000);
-    p[1] = __float2bfloat16_rn(plain ? r : 0.f);
-    p[2] = __float2bfloat16_rn(plain ? r - __bfloat162float(p[1]) : 0.f);
+    // an infinity or a NaN is all in the first; what would round to an
+    // infinity is cut
+    const bool plain = fabsf(v) < __int_as_float(0x7f800000);
+    p[0] = fabsf(v) > 0x1.fep127f && plain ? __float2bfloat16_rz(v) : __float2bfloat16_rn(v);
+    const float r = plain ? v - __bfloat162float(p[0]) : 0.f;
+    p[1] = __float2bfloat16_rn(r);
+    p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
 }
 
 constexpr int kGatherThreads = 256;

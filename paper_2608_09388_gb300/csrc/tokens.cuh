@@ -194,6 +194,25 @@ struct Piece<float, 4> {
     }
 };
 template <>
+struct Piece<__nv_bfloat16, 2> {
+    uint32_t v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        v = *reinterpret_cast<const uint32_t*>(p);
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const {
+        *reinterpret_cast<uint32_t*>(p) = v;
+    }
+    __device__ __forceinline__ float get(int i) const {
+        return __uint_as_float(i ? v & 0xffff0000u : v << 16);
+    }
+    __device__ __forceinline__ F2 unit(int) const { return make_f2(get(0), get(1)); }
+    __device__ __forceinline__ void set_units(const F2 (&u)[1]) {
+        const float2 a = split(u[0]);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(a.x, a.y);
+        v = *reinterpret_cast<const uint32_t*>(&b);
+    }
+};
+template <>
 struct Piece<__nv_bfloat16, 4> {
     uint2 v;
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
@@ -243,12 +262,14 @@ struct Piece<__nv_bfloat16, 8> {
     }
 };
 
-// p[c .. c + VEC), 16-byte aligned when VEC > 1, or `none` without a p.
+// p[c .. c + VEC), 16-byte aligned when VEC > 2, or `none` without a p.
 template <int VEC>
 __device__ __forceinline__ void load_units(const float* __restrict__ p, int c, float none,
                                            typename UnitOf<VEC>::type (&u)[UnitOf<VEC>::count]) {
     if constexpr (VEC == 1) {
         u[0].v = p ? __ldg(p + c) : none;
+    } else if constexpr (VEC == 2) {
+        u[0] = p ? make_f2(__ldg(p + c), __ldg(p + c + 1)) : make_f2(none, none);
     } else {
 #pragma unroll
         for (int i = 0; i < VEC / 2; i += 2) {
@@ -297,6 +318,12 @@ __device__ __forceinline__ uint32_t sum_words(uint32_t a, uint32_t b) {
     const __nv_bfloat162 s = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&a),
                                      *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&s);
+}
+__device__ __forceinline__ Piece<__nv_bfloat16, 2> sum_of(const Piece<__nv_bfloat16, 2>& a,
+                                                          const Piece<__nv_bfloat16, 2>& b) {
+    Piece<__nv_bfloat16, 2> r;
+    r.v = sum_words(a.v, b.v);
+    return r;
 }
 __device__ __forceinline__ Piece<__nv_bfloat16, 8> sum_of(const Piece<__nv_bfloat16, 8>& a,
                                                           const Piece<__nv_bfloat16, 8>& b) {

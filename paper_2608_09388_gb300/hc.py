@@ -391,6 +391,23 @@ def _arg(name, t, shape, dtypes):
     return t.data_ptr()
 
 
+_devices = None
+
+
+def _on_current_device(*tensors):
+    """Refuses tensors of another device than the current one, where there is one:
+    the kernels would run on the current device with addresses of the other's."""
+    global _devices
+    import torch
+    if _devices is None:
+        _devices = torch.cuda.device_count()
+    if _devices > 1:
+        current = torch._C._cuda_getDevice()
+        for t in tensors:
+            if t is not None and t.get_device() != current:
+                raise ValueError(f"a tensor is on device {t.get_device()}, the current one is {current}")
+
+
 def _arg_ids(ids):
     """Address and stride of a one-dimensional int32 tensor (a column of a matrix has one above 1)."""
     if ids.dim() != 1 or ids.dtype != _token_types()[1][0]:
@@ -450,6 +467,7 @@ def hc_rms_norm_fwd(x, eps, gamma, res=None, h=None, y=None, rstd=None, q=None, 
         _too_large(capacity, C)
     f32, i32, q8, row = _token_types()
     same = (x.dtype,)
+    _on_current_device(x, gamma, res, h, y, rstd, q, scales, count)
     _check(load_library().hc_rms_norm_fwd(
         _arg("x", x, (capacity, C), row), _arg("res", res, (capacity, C), same), _dt(x),
         _arg("count", count, (1,), i32), capacity, C, eps, _arg("gamma", gamma, (C,), f32),
@@ -467,6 +485,7 @@ def hc_rms_norm_bwd(h, dy, gamma, rstd, dres=None, dx=None, dgamma=None, count=N
         _too_large(capacity, C)
     f32, i32, _, row = _token_types()
     same = (h.dtype,)
+    _on_current_device(h, dy, gamma, rstd, dres, dx, dgamma, count)
     _check(load_library().hc_rms_norm_bwd(
         _arg("h", h, (capacity, C), row), _arg("dy", dy, (capacity, C), same),
         _arg("dres", dres, (capacity, C), same), _dt(h), _arg("count", count, (1,), i32), capacity,
@@ -576,6 +595,7 @@ def hc_linear_cross_entropy_fwd(x, W, bias, targets, loss=None, lse=None, count=
     if (capacity | C | V) >> 31:
         _too_large(capacity, C, V)
     f32, i32, _, row = _token_types()
+    _on_current_device(x, W, bias, targets, loss, lse, count)
     _check(load_library().hc_linear_cross_entropy_fwd(
         _arg("x", x, (capacity, C), row), _arg("W", W, (V, C), (x.dtype,)), _dt(x),
         _arg("bias", bias, (V,), f32), _arg("targets", targets, (capacity,), i32),
@@ -594,6 +614,7 @@ def hc_linear_cross_entropy_bwd(x, W, bias, targets, lse, dloss, dx=None, dW=Non
         _too_large(capacity, C, V)
     f32, i32, _, row = _token_types()
     same = (x.dtype,)
+    _on_current_device(x, W, bias, targets, lse, dloss, dx, dW, dbias, count)
     _check(load_library().hc_linear_cross_entropy_bwd(
         _arg("x", x, (capacity, C), row), _arg("W", W, (V, C), same), _dt(x),
         _arg("bias", bias, (V,), f32), _arg("targets", targets, (capacity,), i32),
@@ -652,6 +673,7 @@ def _list(tensors):
 def hc_grad_norm(tensors, norm, stream=None):
     """norm fp32 [1] = the norm over all grads of an hc_tensor_list."""
     f32 = _token_types()[0]
+    _on_current_device(norm)
     _check(load_library().hc_grad_norm(_list(tensors), _arg("norm", norm, (1,), f32), _s(stream)),
            "hc_grad_norm")
 
@@ -660,6 +682,7 @@ def hc_grad_clip(tensors, norm, max_norm, stream=None):
     """outs = grads * min(1, max_norm / norm) for an hc_tensor_list; norm fp32 [1]
     on the device."""
     f32 = _token_types()[0]
+    _on_current_device(norm)
     _check(load_library().hc_grad_clip(_list(tensors), _arg("norm", norm, (1,), f32), max_norm,
                                        _s(stream)), "hc_grad_clip")
 

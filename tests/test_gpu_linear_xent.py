@@ -261,6 +261,22 @@ def test_shifted_rows(dtype):
     check(x, W, b, t, dloss, n, o)
 
 
+def test_fp32_range():
+    """fp32 operands up to the largest number: what bf16 would round to an
+    infinity does not become one; exact products, so exact logits."""
+    V, C = 300, 136
+    W, x = torch.zeros(V, C, device="cuda"), torch.zeros(6, C, device="cuda")
+    top = torch.finfo(F).max
+    W[200, 3], x[:, 3] = 2.0 ** -126, torch.tensor([top, -top, 1.0, 2.0 ** 127, 0.0, -1.5], device="cuda")
+    t = full((6,), torch.int32, 200)
+    loss, lse = full((6,)), full((6,))
+    hc.hc_linear_cross_entropy_fwd(x, W, None, t, loss, lse)
+    l = x[:, 3].to(D64) * 2.0 ** -126
+    want = torch.log(torch.exp(l) + (V - 1))
+    within(lse, want, 2.0 ** -20 * want, "lse")
+    within(loss, want - l, 2.0 ** -20 * want, "loss")
+
+
 def test_targets_out_of_range():
     n, V, C = 50, 40, 24
     x, W, b, t, dloss = inputs(7, n, V, C, F)

@@ -68,3 +68,19 @@ def test_binding_checks_shapes_and_types(lib):
             hc.hc_rms_norm_bwd(x, y, None, z(6), **kw)
     with pytest.raises((ValueError, TypeError)):
         hc.hc_rms_norm_bwd(x, y, z(7), z(6), dx=x)
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class Far:
+        def get_device(self):
+            return 1
+
+    class Near:
+        def get_device(self):
+            return 0
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(hc, "_devices", 2)
+    hc._on_current_device(Near(), None, Near())
+    with pytest.raises(ValueError, match="device 1"):
+        hc._on_current_device(Near(), Far())
