@@ -329,10 +329,14 @@ __global__ void __launch_bounds__(kGroupThreads)
         for (int e = 0; e < kU; ++e) ga[i][e] = Unit::splat(1.f), dg[i][e] = Unit::splat(0.f);
         if (c < C) load_units<VEC>(gamma, c, 1.f, ga[i]);
     }
-    load(n0);
+    // the next row is on its way while this one is worked on; 16 single elements
+    // of three inputs twice would spill (16384 x 5001 bf16 951 us so)
+    constexpr bool kNext = !(VEC == 1 && NV == 16);
+    if (kNext) load(n0);
     int turn = 0;
     for (long long w = w0, n = n0; w < rows; w += step, n += step) {
         const bool in = n < rows;
+        if (!kNext) load(n);
         const U times = Unit::splat(r1);
         U s = Unit::splat(0.f);
 #pragma unroll
@@ -341,7 +345,7 @@ __global__ void __launch_bounds__(kGroupThreads)
             cd[i] = nd[i];
             cr[i] = nr[i];
         }
-        load(n + step);
+        if (kNext) load(n + step);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (in && (i * TPR + t) * VEC < C)
@@ -693,7 +697,8 @@ hc_status run(const DeviceCtx* ctx, const RmsNormArgs& a, bool back, cudaStream_
         if (C <= 8 * kVec) return rows_in_regs<T, kVec, 8, 1>(ctx, a, back, s);
         if (C <= 32 * kVec) return rows_in_regs<T, kVec, 32, 1>(ctx, a, back, s);
         if (C <= 64 * kVec) return rows_in_regs<T, kVec, 32, 2>(ctx, a, back, s);
-        if (C <= 128 * kVec) return rows_in_regs<T, kVec, 128, 1>(ctx, a, back, s);
+        if (C <= 128 * kVec)
+            return back ? bwd_rows<T, kVec, 128, 1>(ctx, a, s) : fwd_rows<T, kVec, 32, 4>(ctx, a, s);
         if (C <= 256 * kVec) return rows_in_regs<T, kVec, 128, 2>(ctx, a, back, s);
         if (C <= 512 * kVec) return rows_in_regs<T, kVec, 256, 2>(ctx, a, back, s);
         if (C <= 1024 * kVec) {
@@ -712,21 +717,33 @@ hc_status run(const DeviceCtx* ctx, const RmsNormArgs& a, bool back, cudaStream_
             if (C <= 128) return rows_in_regs<T, 2, 8, 8>(ctx, a, back, s);
             if (C <= 256) return rows_in_regs<T, 2, 32, 4>(ctx, a, back, s);
             if (C <= 512) return rows_in_regs<T, 2, 32, 8>(ctx, a, back, s);
-            if (C <= 1024) return rows_in_regs<T, 2, 128, 4>(ctx, a, back, s);
-            if (C <= 2048) return rows_in_regs<T, 2, 128, 8>(ctx, a, back, s);
-            if (C <= 4096) return rows_in_regs<T, 2, 256, 8>(ctx, a, back, s);
-            return rows_in_regs<T, 2, 512, 8>(ctx, a, back, s);
+            if (!back) {
+                if (C <= 1024) return fwd_rows<T, 2, 32, 16>(ctx, a, s);
+                if (C <= 4096) return fwd_rows<T, 2, 128, 16>(ctx, a, s);
+                return fwd_rows<T, 2, 256, 16>(ctx, a, s);
+            }
+            if (C <= 1024) return bwd_rows<T, 2, 128, 4>(ctx, a, s);
+            if (C <= 2048) return bwd_rows<T, 2, 128, 8>(ctx, a, s);
+            if (C <= 4096) return bwd_rows<T, 2, 256, 8>(ctx, a, s);
+            return bwd_rows<T, 2, 512, 8>(ctx, a, s);
         }
     }
     if (C <= 32) return rows_in_regs<T, 1, 8, 4>(ctx, a, back, s);
     if (C <= 64) return rows_in_regs<T, 1, 8, 8>(ctx, a, back, s);
     if (C <= 128) return rows_in_regs<T, 1, 32, 4>(ctx, a, back, s);
     if (C <= 256) return rows_in_regs<T, 1, 32, 8>(ctx, a, back, s);
-    if (C <= 512) return rows_in_regs<T, 1, 128, 4>(ctx, a, back, s);
-    if (C <= 1024) return rows_in_regs<T, 1, 128, 8>(ctx, a, back, s);
-    if (C <= 2048) return rows_in_regs<T, 1, 256, 8>(ctx, a, back, s);
-    if (C <= 4096) return rows_in_regs<T, 1, 512, 8>(ctx, a, back, s);
-    return rows_in_regs<T, 1, 512, 16>(ctx, a, back, s);
+    if (!back) {
+        if (C <= 512) return fwd_rows<T, 1, 32, 16>(ctx, a, s);
+        if (C <= 1024) return fwd_rows<T, 1, 128, 8>(ctx, a, s);
+        if (C <= 2048) return fwd_rows<T, 1, 128, 16>(ctx, a, s);
+        if (C <= 4096) return fwd_rows<T, 1, 256, 16>(ctx, a, s);
+        return fwd_rows<T, 1, 512, 16>(ctx, a, s);
+    }
+    if (C <= 512) return bwd_rows<T, 1, 128, 4>(ctx, a, s);
+    if (C <= 1024) return bwd_rows<T, 1, 128, 8>(ctx, a, s);
+    if (C <= 2048) return bwd_rows<T, 1, 256, 8>(ctx, a, s);
+    if (C <= 4096) return bwd_rows<T, 1, 512, 8>(ctx, a, s);
+    return bwd_rows<T, 1, 512, 16>(ctx, a, s);
 }
 
 }  // namespace
