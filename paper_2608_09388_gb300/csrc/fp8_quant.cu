@@ -7,9 +7,10 @@
 // scale infinity, its infinities held as NaN: products of such a row are NaN.
 //
 // Bound by memory once the quotients are not divided one by one: 16384 x 8192
-// bf16 takes 81 us (60 at the copy rate; 231 us with a division per value, 153
-// with four scales a warp found one after another), 16384 x 4932, whose rows
-// allow 4-byte loads only, 85 us (36).
+// bf16 takes 65 to 67 us (60 at the copy rate; 231 us with a division per value, 153
+// with four scales a warp found one after another, 81 with two products that
+// enclose the quotient in place of its correction), 16384 x 4932, whose rows
+// allow 4-byte loads only, 67 to 72 us (36).
 #include "fp8.cuh"
 
 namespace hc {
@@ -146,7 +147,7 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 // A block per 128 x 128 block of W [C_in, C_out], written transposed: a thread
 // holds 64 channels in of one channel out, all loaded before the first is
 // used, and writes them as 64 bytes of that row. W is read once (8192 x 8192
-// bf16: 78 to 97 us, 30 at the copy rate; read twice and transposed through shared
+// bf16: 67 us, 30 at the copy rate; read twice and transposed through shared
 // memory 126; a warp's 16-byte stores go to 32 rows).
 template <typename T>
 __global__ void __launch_bounds__(kThreads)

@@ -14,7 +14,9 @@
 // Bound by memory: forward reads two rows and writes two (8 bits: one and a
 // half), the gradient reads three and writes one. Rows of up to 8192 channels
 // stay in registers between the sum of squares and the output, and the next
-// rows are on their way before this one is reduced.
+// rows are on their way before this one is reduced. At 65536 x 2048 bf16 (GB300)
+// forward and gradient take 327 us (317 at the copy rate), 16384 x 8192 bf16 to 8
+// bits 156 (139), 1 x 4096 to 8 bits 2.5.
 #include "fp8.cuh"
 
 namespace hc {
@@ -682,6 +684,13 @@ hc_status bwd_wide(const DeviceCtx* ctx, const RmsNormArgs& a, cudaStream_t s) {
     return launch_column_sum(part, (int)parts, a.C, a.C, a.dgamma, s);
 }
 
+// Rows of at most 8192 channels are held in registers by the smallest group that
+// does so without spilling: forward up to 64 bytes a lane of a warp (300 to 1024 bf16
+// channels by a warp each, which waits for no other: 600 channels 168 us for 268 MB
+// in and out, by 128 threads with a barrier a row 229; to 8 bits 162 and 316), the
+// gradient, which keeps three rows' pieces twice, gamma and its sums, half of
+// that. Rows without 16-byte loads are read in 4-byte pieces where they allow it (602
+// bf16 channels 188 us, 2050 258), else element by element (2047 bf16 265, fp32 165).
 template <typename T>
 hc_status run(const DeviceCtx* ctx, const RmsNormArgs& a, bool back, cudaStream_t s) {
     constexpr int kVec = 16 / (int)sizeof(T);
