@@ -202,8 +202,9 @@ __global__ void __launch_bounds__(kGatherThreads)
 }
 
 // W in the form the products read where it is not: three planes of bf16, or
-// rows with a pitch that is a multiple of 16 bytes.
-template <typename T>
+// rows with a pitch that is a multiple of 16 bytes. kN channels a lane, where
+// rows of fp32 allow it.
+template <typename T, int kN>
 __global__ void __launch_bounds__(256)
     xent_weight_kernel(const T* __restrict__ W, int V, int C, long long pitch,
                        __nv_bfloat16* __restrict__ out) {
@@ -213,14 +214,34 @@ __global__ void __launch_bounds__(256)
     const int warp = (int)((blockIdx.x * 256 + threadIdx.x) >> 5), lane = threadIdx.x & 31;
     for (long long v = warp; v < V; v += (long long)gridDim.x * 8)
 #pragma unroll 4
-        for (int c = lane; c < C; c += 32) {
-            __nv_bfloat16 p[3];
-            if constexpr (kPlanes == 1)
-                p[0] = W[v * C + c];
-            else
-                planes_of(W[v * C + c], p);
+        for (int c = lane * kN; c < C; c += 32 * kN) {
+            __nv_bfloat16 p[kN][3];
+            if constexpr (kPlanes == 1) {
+                p[0][0] = W[v * C + c];
+            } else {
+                alignas(16) float f[kN];
+                if constexpr (kN == 4)
+                    *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(W + v * C + c);
+                else if constexpr (kN == 2)
+                    *reinterpret_cast<float2*>(f) = *reinterpret_cast<const float2*>(W + v * C + c);
+                else
+                    f[0] = W[v * C + c];
 #pragma unroll
-            for (int k = 0; k < kPlanes; ++k) out[(k * (long long)V + v) * pitch + c] = p[k];
+                for (int i = 0; i < kN; ++i) planes_of(f[i], p[i]);
+            }
+#pragma unroll
+            for (int k = 0; k < kPlanes; ++k) {
+                __nv_bfloat16* const to = out + (k * (long long)V + v) * pitch + c;
+                alignas(8) __nv_bfloat16 q[kN];
+#pragma unroll
+                for (int i = 0; i < kN; ++i) q[i] = p[i][k];
+                if constexpr (kN == 4)
+                    *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(q);
+                else if constexpr (kN == 2)
+                    *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(q);
+                else
+                    *to = q[0];
+            }
         }
 }
 
@@ -311,8 +332,11 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "h"((unsigned short)3)
         : "memory");
 }
+// An arrival that orders no memory: what it tells has been read from TMEM (and
+// waited for) already. With release semantics it waited for the global stores
+// of the tile before, 1000 clocks a tile.
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar)
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar)
                  : "memory");
 }
 // A box of this CTA's, whose bytes are counted by the pair's first CTA.
@@ -341,16 +365,35 @@ __device__ __forceinline__ void store_box(const void* tmap, uint32_t src, int c0
     asm volatile("cp.async.bulk.commit_group;\n" ::: "memory");
 }
 
-// The tile t of the walk: row tiles in groups of kGroupM, the tiles of a group
-// column by column, so that the pairs at work share both operands in L2.
-__device__ __forceinline__ void tile_at(uint32_t t, uint32_t tm, uint32_t tn, int& m, int& n) {
-    const uint32_t per = (uint32_t)kGroupM * tn;
-    const uint32_t g = t / per, first = g * kGroupM;
-    const uint32_t in = tm - first < (uint32_t)kGroupM ? tm - first : (uint32_t)kGroupM;
-    const uint32_t r = t - g * per;
-    n = (int)(r / in);
-    m = (int)(first + r % in);
-}
+// The tiles, walked in groups of kGroupM row tiles, the tiles of a group column by
+// column, so that the pairs at work share both operands in L2. `at` is the tile's
+// place in its group; going on needs no division but in the last group.
+struct Walk {
+    uint32_t tm, tn, first, in, at;
+    __device__ __forceinline__ Walk(uint32_t tm_, uint32_t tn_, uint32_t t) : tm(tm_), tn(tn_) {
+        const uint32_t g = t / ((uint32_t)kGroupM * tn);
+        first = g * kGroupM;
+        at = t - first * tn;
+        size();
+    }
+    __device__ __forceinline__ void size() {
+        in = tm - first < (uint32_t)kGroupM ? tm - first : (uint32_t)kGroupM;
+    }
+    // false behind the last tile
+    __device__ __forceinline__ bool go(uint32_t by) {
+        at += by;
+        while (first < tm && at >= in * tn) {
+            at -= in * tn;
+            first += kGroupM;
+            if (first < tm) size();
+        }
+        return first < tm;
+    }
+    __device__ __forceinline__ void tile(int& m, int& n) const {
+        n = (int)(in == (uint32_t)kGroupM ? at / (uint32_t)kGroupM : at / in);
+        m = (int)(first + at - (uint32_t)n * in);
+    }
+};
 
 // The planes of operand A and B in product p of six, small ones first.
 __device__ __forceinline__ int plane_a(int planes, int p) {
@@ -505,12 +548,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t times =
         (uint32_t)(weight_first ? weach / (each < 1 ? 1 : each) : each / (weach < 1 ? 1 : weach));
 
+    // the logits' tiles go round the pairs
+    Walk walk(tm, tn < 1 ? 1 : tn, pair);
     auto work_at = [&](uint32_t i, Work& w) -> bool {
         w.weight = false;
         w.part = 0;
-        uint32_t u;
         if constexpr (kP == kBack) {
-            u = weight_first ? scheduled(i, pair, P, wunits, units, times)
+            uint32_t u = weight_first ? scheduled(i, pair, P, wunits, units, times)
                              : scheduled(i, pair, P, units, wunits, times);
             if (u >= units + wunits) return false;
             w.weight = weight_first ? u < wunits : u >= units;
@@ -521,13 +565,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             u -= (uint32_t)w.part * tiles;
             w.k0 = (int)((long long)all * w.part / split);
             w.k1 = (int)((long long)all * (w.part + 1) / split);
+            const Walk at(w.weight ? tmw : tm, tn, u);
+            at.tile(w.m, w.n);
         } else {
-            u = pair + i * P;
-            if (u >= units) return false;
+            if (i == 0 ? pair >= units : !walk.go(P)) return false;
             w.k0 = 0;
             w.k1 = blocks;
+            walk.tile(w.m, w.n);
         }
-        tile_at(u, w.weight ? tmw : tm, tn, w.m, w.n);
         return true;
     };
 
@@ -660,56 +705,18 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tc_fence_before();
                 if (lane == 0) arrive_cluster(tempty);
             };
-            float sums[kPromote ? kCols : 1];  // of this lane's row
-            if constexpr (kPromote) {
+            // 32 columns of this lane's row from the accumulator, which is given
+            // back with the last ones
+            auto direct = [&](int c, float (&f)[32]) {
+                uint32_t r[32];
+                tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
+                tmem_ld_wait();
+                if (c + 32 == kCols) give_back();
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) sums[j] = 0.f;
-                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<kP, T>) {
-                    next();
-                    if (!ok) break;
-                    if (mine) {
+                for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(r[j]);
+                if (kP == kBack && w.k1 == w.k0) {  // an empty sum
 #pragma unroll
-                        for (int c = 0; c < kCols; c += 16) {
-                            uint32_t r[16];
-                            tmem_ld(acc + (uint32_t)c, r);
-                            tmem_ld_wait();
-                            if (c + 16 == kCols) give_back();
-                            if (kc == w.k0) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) sums[c + j] = __uint_as_float(r[j]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) sums[c + j] += __uint_as_float(r[j]);
-                            }
-                        }
-                    } else {
-                        give_back();
-                    }
-                }
-            } else {
-                next();
-            }
-            if (!ok) break;
-            if (!mine) {
-                if (!kPromote) give_back();
-                continue;
-            }
-            // 32 columns of this lane's row
-            auto load = [&](int c, float (&f)[32]) {
-                if constexpr (kPromote) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = sums[c + j];
-                } else {
-                    uint32_t r[32];
-                    tmem_ld_32x32b_x32(acc + (uint32_t)c, r);
-                    tmem_ld_wait();
-                    if (c + 32 == kCols) give_back();
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(r[j]);
-                    if (kP == kBack && w.k1 == w.k0) {  // an empty sum
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) f[j] = 0.f;
-                    }
+                    for (int j = 0; j < 32; ++j) f[j] = 0.f;
                 }
             };
             const int row0 = w.m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
@@ -727,45 +734,43 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             auto pack = [](float lo, float hi) { return Piece<__nv_bfloat16, 8>::pair(lo, hi); };
 
+            auto finish = [&](auto load, auto load_all) {
             if constexpr (kP == kStats) {
                 const int target = row < M ? a.target[row] : -1;
                 const float least = -__int_as_float(0x7f800000);
-                float top = least, sum = 0.f;
-#pragma unroll
-                for (int c = 0; c < kCols; c += 32) {
-                    float f[32];
-                    load(c, f);
-                    const int col = col0 + c;
-                    if (a.bias) add_bias(f, a.bias + col, a.cols - col);
-                    if (col + 32 > a.cols) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (col + j >= a.cols) f[j] = least;
-                    }
-                    float m4[4] = {top, least, least, least};
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], f[j], f[j + 1]);
-                    const float most = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]);
-                    if (target >= col && target < col + 32) {
-                        float v = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v = col + j == target ? f[j] : v;
-                        a.at_target[row] = v;
-                    }
-                    // classes masked with -infinity leave it at that; a NaN
-                    // goes past the maximum and into the sum
-                    const float from = most == least ? 0.f : most;
-                    sum *= ex2((top - from) * kLog2e);
-                    const F2 less = make_f2(-from, -from), scale = make_f2(kLog2e, kLog2e);
-                    F2 s2[2] = {make_f2(0.f, 0.f), make_f2(0.f, 0.f)};
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const float2 e = split(mul(add(make_f2(f[j], f[j + 1]), less), scale));
-                        s2[j / 2 & 1] = add(s2[j / 2 & 1], make_f2(ex2(e.x), ex2(e.y)));
-                    }
-                    sum += total(add(s2[0], s2[1]));
-                    top = most;
+                float f[kCols];
+                load_all(f);
+                if (a.bias) {
+                    add_bias(reinterpret_cast<float (&)[32]>(f[0]), a.bias + col0, a.cols - col0);
+                    add_bias(reinterpret_cast<float (&)[32]>(f[32]), a.bias + col0 + 32, a.cols - col0 - 32);
                 }
+                if (col0 + kCols > a.cols) {
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j)
+                        if (col0 + j >= a.cols) f[j] = least;
+                }
+                float m4[4] = {least, least, least, least};
+#pragma unroll
+                for (int j = 0; j < kCols; j += 2) m4[j / 2 & 3] = max3(m4[j / 2 & 3], f[j], f[j + 1]);
+                const float top = max3(fmaxf(m4[0], m4[1]), m4[2], m4[3]);
+                if (target >= col0 && target < col0 + kCols) {
+                    float v = 0.f;
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) v = col0 + j == target ? f[j] : v;
+                    a.at_target[row] = v;
+                }
+                // classes masked with -infinity leave it at that; a NaN goes
+                // past the maximum and into the sum
+                const float from = top == least ? 0.f : top;
+                const F2 less = make_f2(-from, -from), scale = make_f2(kLog2e, kLog2e);
+                F2 s4[4];
+#pragma unroll
+                for (int j = 0; j < kCols; j += 2) {
+                    const float2 e = split(mul(add(make_f2(f[j], f[j + 1]), less), scale));
+                    const F2 p = make_f2(ex2(e.x), ex2(e.y));
+                    s4[j / 2 & 3] = j < 8 ? p : add(s4[j / 2 & 3], p);
+                }
+                const float sum = total(add(add(s4[0], s4[1]), add(s4[2], s4[3])));
                 if (row < M && col0 < a.cols)
                     a.pairs[(long long)(col0 / kCols) * a.mpad + row] = make_float2(top, sum);
             } else if constexpr (kP == kGrad) {
@@ -775,7 +780,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int target = in ? a.target[row] - a.v0 : -1;
                 // the whole of it inside: no looks at rows and columns
                 const bool whole = row0 + 32 <= M && col0 + kCols <= a.cols;
-                float keep[kPlanes3 ? kCols : 1];
+                [[maybe_unused]] float keep[kPlanes3 ? kCols : 1];
                 if (!kPlanes3) staging_free();
 #pragma unroll
                 for (int c = 0; c < kCols; c += 32) {
@@ -914,6 +919,59 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     __syncwarp();
                 }
+            }
+            };
+            // one accumulator holds the whole sum, or its chains are added up here
+            if (!kPromote || (w.k1 > w.k0 && w.k1 - w.k0 <= kChain<kP, T>)) {
+                next();
+                if (!ok) break;
+                if (mine)
+                    finish(direct, [&](float (&f)[kCols]) {
+                        uint32_t r0[32], r1[32];
+                        tmem_ld_32x32b_x32(acc, r0);
+                        tmem_ld_32x32b_x32(acc + 32u, r1);
+                        tmem_ld_wait();
+                        give_back();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            f[j] = __uint_as_float(r0[j]);
+                            f[32 + j] = __uint_as_float(r1[j]);
+                        }
+                    });
+                else
+                    give_back();
+            } else {
+                float sums[kCols];
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) sums[j] = 0.f;
+                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<kP, T>) {
+                    next();
+                    if (!ok) break;
+                    if (!mine) {
+                        give_back();
+                        continue;
+                    }
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 16) {
+                        uint32_t r[16];
+                        tmem_ld(acc + (uint32_t)c, r);
+                        tmem_ld_wait();
+                        if (c + 16 == kCols) give_back();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) sums[c + j] += __uint_as_float(r[j]);
+                    }
+                }
+                if (!ok) break;
+                if (mine)
+                    finish(
+                        [&](int c, float (&f)[32]) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) f[j] = sums[c + j];
+                        },
+                        [&](float (&f)[kCols]) {
+#pragma unroll
+                            for (int j = 0; j < kCols; ++j) f[j] = sums[j];
+                        });
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;\n" ::: "memory");
@@ -1312,8 +1370,16 @@ struct Call {
                                   dim3(kGatherThreads), 0, s, "xent_gather_kernel", g, r);
         if (st != HC_OK || direct) return st;
         const long long wneed = ((long long)a.V + 7) / 8, wcap = 8ll * ctx->num_sms;
-        return launch_pdl(xent_weight_kernel<T>, dim3((unsigned)(wneed < wcap ? wneed : wcap)),
-                          dim3(256), 0, s, "xent_weight_kernel", (const T*)a.W, a.V, a.C, pitch, w);
+        const uintptr_t at = reinterpret_cast<uintptr_t>(a.W);
+        auto kern = xent_weight_kernel<T, 1>;
+        if constexpr (kPlanes == 3) {
+            if (a.C % 4 == 0 && a.C >= 128 && at % 16 == 0)
+                kern = xent_weight_kernel<T, 4>;
+            else if (a.C % 2 == 0 && a.C >= 64 && at % 8 == 0)
+                kern = xent_weight_kernel<T, 2>;
+        }
+        return launch_pdl(kern, dim3((unsigned)(wneed < wcap ? wneed : wcap)), dim3(256), 0, s,
+                          "xent_weight_kernel", (const T*)a.W, a.V, a.C, pitch, w);
     }
     hc_status map_x(CUtensorMap* m, int box) {
         return encode(m, kBf16, r.x, a.C, mpad, kPlanes, pitch, box);

@@ -41,6 +41,8 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
 }
 __device__ __forceinline__ bool wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                           unsigned* status, unsigned long long limit) {
+    // one try before the clock is looked at
+    if (limit > kLongestTryNs && __all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
     const unsigned long long t0 = globaltimer_ns();
     bool ok;
     for (;;) {
