@@ -682,7 +682,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
     } else {
         const int quarter = warp & 3, group = warp >> 2;
-        const bool mine = group * kCols < a.bn;  // a narrow tile leaves some warps idle
+        // rows that are used: of G those that the products over tokens take too,
+        // whole blocks of them
+        const int used = kP == kGrad ? (int)(((long long)M + kKB - 1) / kKB * kKB) : M;
         const uint32_t stage = out_at + (uint32_t)warp * kOutBytes;
         const uint32_t tempty0 = cluster_map(tempty_bar(0), 0);
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
@@ -691,6 +693,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool ok = true;
         Work w;
         for (uint32_t i = 0; work_at(i, w); ++i) {
+            const int row0 = w.m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+            // a narrow tile, or one with few rows, leaves some warps idle
+            const bool mine = group * kCols < a.bn && row0 < (w.weight ? a.cols : used);
             // the next accumulator: where it is, and the barrier that gives it back
             uint32_t acc = 0, tempty = 0;
             auto next = [&] {
@@ -719,7 +724,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int j = 0; j < 32; ++j) f[j] = 0.f;
                 }
             };
-            const int row0 = w.m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
             const int col0 = w.n * a.bn + group * kCols;
             // 128 bytes of each of the warp's rows, swizzled, then one box
             auto staging_free = [&] {
@@ -904,18 +908,26 @@ __global__ void __launch_bounds__(kThreads, 1)
                     if (col0 < a.C && row0 < a.cols) send(&maps.out_w, col0, a.v0 + row0, 0, false);
                 } else {
                     __syncwarp();
+                    // two values a lane where the row's place in memory allows it; with
+                    // the row one off, its first and last go by themselves
+                    auto value = [&](int r, int j) {
+                        const uint32_t at = stage + r * 128 + (((j >> 3) ^ (r & 7)) << 4) + (j & 7) * 2;
+                        uint16_t v;
+                        asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(at) : "memory");
+                        return v;
+                    };
                     for (int r = 0; r < 32; ++r) {
                         if (row0 + r >= a.cols) break;
-                        __nv_bfloat16* const to =
-                            static_cast<__nv_bfloat16*>(a.dw) + (long long)(a.v0 + row0 + r) * a.C;
-#pragma unroll
-                        for (int h = 0; h < 64; h += 32) {
-                            const int j = h + lane;
-                            const uint32_t at = stage + r * 128 + (((j >> 3) ^ (r & 7)) << 4) + (j & 7) * 2;
-                            uint16_t v;
-                            asm volatile("ld.shared.u16 %0, [%1];\n" : "=h"(v) : "r"(at) : "memory");
-                            if (col0 + j < a.C) to[col0 + j] = __ushort_as_bfloat16(v);
-                        }
+                        uint16_t* const to = static_cast<uint16_t*>(a.dw) +
+                                             (long long)(a.v0 + row0 + r) * a.C + col0;
+                        const int left = a.C - col0, off = (int)(reinterpret_cast<uintptr_t>(to) >> 1 & 1);
+                        const int j = 2 * lane + off;
+                        const uint16_t lo = value(r, j), hi = value(r, j + 1 < kCols ? j + 1 : 0);
+                        if (j + 1 < kCols && j + 1 < left)
+                            *reinterpret_cast<uint32_t*>(to + j) = (uint32_t)hi << 16 | lo;
+                        else if (j < left)
+                            to[j] = lo;
+                        if (j + 1 == kCols && left > 0) to[0] = hi;
                     }
                     __syncwarp();
                 }
