@@ -116,14 +116,16 @@ __global__ void __launch_bounds__(kThreads, kResident)
     sum_squares_kernel(const Entry* __restrict__ table, int n, long long units,
                        double* __restrict__ part) {
     __shared__ double sh[kThreads / 32];
-    pdl_wait();
     pdl_trigger();
     const long long u1 = units * (blockIdx.x + 1) / gridDim.x;
     long long u = units * blockIdx.x / gridDim.x;
     float hi = 0.f, lo = 0.f;
     double far = 0.0;  // squares that fp32 does not hold
+    // the table has been there since before the first call: its look-up runs
+    // while the kernel before ends
+    int t = u < u1 ? find_entry(table, n, u) : 0;
+    pdl_wait();
     if (u < u1) {
-        int t = find_entry(table, n, u);
         while (u < u1) {
             const char *const from = table[t].in, *const to = from + table[t].bytes;
             const bool bf16 = table[t].bf16;
@@ -187,15 +189,15 @@ __global__ void __launch_bounds__(kThreads)
 __global__ void __launch_bounds__(kThreads, kResident)
     scale_kernel(const Entry* __restrict__ table, int n, long long units, const float* norm,
                  float max_norm) {
-    pdl_wait();
     pdl_trigger();
     const long long b = gridDim.x - 1 - blockIdx.x;
     const long long u0 = units * b / gridDim.x;
     long long u = units * (b + 1) / gridDim.x;  // the units below it are left
+    int t = u > u0 ? find_entry(table, n, u - 1) : 0;  // see sum_squares_kernel
+    pdl_wait();
     if (u <= u0) return;
     const float size = *norm;
     const float scale = size <= max_norm ? 1.f : max_norm / size;  // a NaN passes
-    int t = find_entry(table, n, u - 1);
     for (; u > u0; --t) {
         const char *const from = table[t].in, *const to = from + table[t].bytes;
         const bool bf16 = table[t].bf16;
