@@ -271,14 +271,14 @@ constexpr int kGroupM = 16;                      // row tiles walked per column 
 // Blocks of the sum behind which the accumulator is added to fp32 registers,
 // with fp32 operands and for logits. The tensor cores truncate at every step of 16,
 // always towards zero: 784 steps at full size left 1.7e-5 of a weight's
-// gradient, 128 steps 1.6e-6 of a loss (1.25e-8 a step). Results that are rounded to
-// bf16 keep one accumulator; the logits of G, which is rounded too, are taken
-// in chains twice as long as those of the loss (8 blocks: 2048 of 32000 x 1024
-// 94 us, 16: 86).
+// gradient, 128 steps 1.6e-6 of a loss (1.25e-8 a step). The logits of G are taken
+// in the loss's chains, so that what is left in them is in lse too: in chains
+// twice as long (2048 of 32000 x 1024 84 us, 88 so) dbias was off by 4e-6, not 5e-7.
+// Results that are rounded to bf16 keep one accumulator.
 template <Product kP, typename T>
 constexpr bool kPromoted = sizeof(T) == 4 || kP != kBack;
-template <Product kP, typename T>
-constexpr int kChain = sizeof(T) == 4 ? 4 : kP == kStats ? 8 : 16;
+template <typename T>
+constexpr int kChain = sizeof(T) == 4 ? 4 : 8;
 constexpr int kBars = 2 * kStages + 5;
 constexpr size_t kSmem = 1024 + (size_t)kStages * kStageBytes + kStoreWarps * kOutBytes + kBars * 8 + 64;
 static_assert(kSmem <= 232448, "shared memory of a block");
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         Work w;
         for (uint32_t i = 0; ok && work_at(i, w); ++i) {
             const int row = w.m * kTile + (int)rank * kHalf, col = w.n * a.bn + (int)rank * a.bn / 2;
-            const int chain = kPromote ? kChain<kP, T> : w.k1 - w.k0;
+            const int chain = kPromote ? kChain<T> : w.k1 - w.k0;
             for (int kc = w.k0; kc < w.k1 && ok; kc += chain)
                 for (int p = 0; p < products && ok; ++p) {
                     const int pa = plane_a(a.planes, p), pb = plane_b(a.planes, p);
@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // A of dW is G read along its columns
                 const uint32_t idesc = idesc0 | (w.weight ? 1u << 15 : 0u);
                 const uint32_t lbo = w.weight ? kOperandBytes / 2 : 16, step = w.weight ? 128 : 2;
-                const int chain = kPromote ? kChain<kP, T> : w.k1 - w.k0;
+                const int chain = kPromote ? kChain<T> : w.k1 - w.k0;
                 int kc = w.k0;
                 do {  // an empty sum of bf16 operands still passes its accumulator on
                     if (kPromote && kc >= w.k1) break;
@@ -934,7 +934,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             };
             // one accumulator holds the whole sum, or its chains are added up here
-            if (!kPromote || (w.k1 > w.k0 && w.k1 - w.k0 <= kChain<kP, T>)) {
+            if (!kPromote || (w.k1 > w.k0 && w.k1 - w.k0 <= kChain<T>)) {
                 next();
                 if (!ok) break;
                 if (mine)
@@ -956,7 +956,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 float sums[kCols];
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) sums[j] = 0.f;
-                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<kP, T>) {
+                for (int kc = w.k0; kc < w.k1 && ok; kc += kChain<T>) {
                     next();
                     if (!ok) break;
                     if (!mine) {

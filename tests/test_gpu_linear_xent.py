@@ -320,6 +320,21 @@ def test_equal_weights():
         within(o["dbias"], G.sum(0), ((tp + 4 * U * at) * w).sum(0) + (n + 8) * U * G.abs().sum(0), "dbias")
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_sums_of_gradients_over_classes(dtype):
+    """dbias adds up to the tokens' dloss times what their probabilities miss of
+    one: logits and lse are rounded alike, whatever the length of the sums. A
+    probability off by the exponential (2^-22), a rounded product (2 U d, d up to 30
+    here) and difference (U of lse, up to 16): 100 U in all, and the chains' 512
+    channels, which may be cut off differently by their order alone: 16 U of the logit's
+    magnitudes (up to 40) over the 4 chains or more that it has."""
+    n, V, C = 200, 700, 2056
+    x, W, b, t, _ = inputs(14, n, V, C, dtype, ignored=0.0)
+    dloss = torch.full((n,), 1.0, device="cuda")
+    o = run_all(x, W, b, t, dloss, None)
+    assert abs(float(o["dbias"].to(D64).sum())) <= n * (100 + 16 * 40) * U
+
+
 def test_first_weight_special():
     """The first token's dloss of zero, infinite, or below the normal numbers:
     the others' gradients are as without it."""
