@@ -1027,144 +1027,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
-// ---------------------------------------------------------------- few tokens
-// Up to kFew tokens (a scoring or decoding step): bound by the one read of W,
-// so the sums are taken on the CUDA cores straight from the rows as they are. A
-// warp takes kFewRows classes at a time, 16 bytes of each a lane, against the
-// tokens' rows in shared memory (fp32; the 16-byte pieces of a lane's channels
-// lie 512 bytes apart, so that neither side has bank conflicts).
-constexpr int kFew = 4;
-constexpr int kFewThreads = 256;
-constexpr int kFewRows = 4;
-
-template <typename T, int VEC>
-__device__ __forceinline__ int few_at(int c) {
-    if (VEC < 8) return c;
-    return (c & ~255) + (c & 4) * 32 + ((c & 255) >> 3) * 4 + (c & 3);
-}
-
-template <typename T, int VEC, int kTokens>
-__global__ void __launch_bounds__(kFewThreads, kTokens == 1 ? 4 : kTokens == 2 ? 3 : 2)
-    xent_few_kernel(const T* __restrict__ x, const T* __restrict__ W, const float* __restrict__ bias,
-                    const int32_t* targets, int C, int V, float2* __restrict__ pairs,
-                    float* __restrict__ at_target) {
-    extern __shared__ __align__(16) float rows[];  // [kTokens][up to a multiple of 256]
-    __shared__ float2 sh[kFewThreads / 32][kTokens];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int pitch = (C + 255) & ~255;
-    const float least = -__int_as_float(0x7f800000);
-    pdl_wait();
-    pdl_trigger();
-    int target[kTokens];
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t) {
-        target[t] = targets[t];
-        for (int c = threadIdx.x; c < C; c += kFewThreads)
-            rows[t * pitch + few_at<T, VEC>(c)] = to_f32(x[(long long)t * C + c]);
-    }
-    __syncthreads();
-    // Of the kValues sums of a round (class r, token t) a lane keeps one, the
-    // lane's upper bits being r and t: its class's running pair
-    constexpr int kT = kTokens == 3 ? 4 : kTokens, kValues = kFewRows * kT;
-    constexpr int kSame = 32 / kValues;  // lanes with the same value
-    const int my_r = lane / (32 / kFewRows), my_t = lane / kSame % kT;
-    int my_target = -1;
-#pragma unroll
-    for (int t = 0; t < kTokens; ++t) my_target = my_t == t ? target[t] : my_target;
-    float2 mine = make_float2(least, 0.f);
-    // whole rounds of kFewRows classes a warp, then what is left in one round of
-    // as few as it takes: every warp ends at the same time
-    const int warps = gridDim.x * (kFewThreads / 32), w = (int)blockIdx.x * (kFewThreads / 32) + warp;
-    const int whole = V / (warps * kFewRows), left = V - whole * warps * kFewRows;
-    const int last = (left + warps - 1) / warps;
-    for (int i = 0; i <= whole; ++i) {
-        const int take = i < whole ? kFewRows : last;
-        const long long v0 = (long long)i * warps * kFewRows + (long long)w * take;
-        if (v0 >= V || take == 0) break;
-        float s[kFewRows][kTokens] = {};
-#pragma unroll 2
-        for (int c = lane * VEC; c < C; c += 32 * VEC) {
-            Piece<T, VEC> p[kFewRows];
-#pragma unroll
-            for (int r = 0; r < kFewRows; ++r)
-                if (r < take && v0 + r < V) p[r].load(W + (v0 + r) * C + c);
-#pragma unroll
-            for (int t = 0; t < kTokens; ++t) {
-                float f[VEC];
-                if constexpr (VEC == 1) {
-                    f[0] = rows[t * pitch + c];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < VEC; e += 4) {
-                        const float4 q = *reinterpret_cast<const float4*>(rows + t * pitch + few_at<T, VEC>(c + e));
-                        f[e] = q.x, f[e + 1] = q.y, f[e + 2] = q.z, f[e + 3] = q.w;
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < kFewRows; ++r)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) s[r][t] = fmaf(p[r].get(e), f[e], s[r][t]);
-            }
-        }
-        // sums over the lanes, half of the values left to each at every step
-        float v[kValues];
-#pragma unroll
-        for (int k = 0; k < kValues; ++k) v[k] = k % kT < kTokens ? s[k / kT][k % kT] : 0.f;
-        int o = 16;
-#pragma unroll
-        for (int half = kValues / 2; half > 0; half /= 2, o /= 2) {
-            const bool up = lane & o;
-#pragma unroll
-            for (int k = 0; k < half; ++k) {
-                const float send = up ? v[k] : v[k + half], keep = up ? v[k + half] : v[k];
-                v[k] = keep + __shfl_xor_sync(0xffffffffu, send, o);
-            }
-        }
-#pragma unroll
-        for (int q = kSame / 2; q > 0; q /= 2) v[0] += __shfl_xor_sync(0xffffffffu, v[0], q);
-        const long long cls = v0 + my_r;
-        if (my_r < take && cls < V && my_t < kTokens) {
-            const float l = v[0] + (bias ? __ldg(bias + cls) : 0.f);
-            if (lane % kSame == 0 && cls == my_target) at_target[my_t] = l;
-            mine = join_pairs(mine, make_float2(l, 1.f));
-        }
-    }
-#pragma unroll
-    for (int o = 16; o >= 32 / kFewRows; o /= 2)  // the classes of a token
-        mine = join_pairs(mine, make_float2(__shfl_xor_sync(0xffffffffu, mine.x, o),
-                                            __shfl_xor_sync(0xffffffffu, mine.y, o)));
-    if (my_r == 0 && lane % kSame == 0 && my_t < kTokens) sh[warp][my_t] = mine;
-    __syncthreads();
-    if (threadIdx.x < kTokens) {
-        float2 p = sh[0][threadIdx.x];
-        for (int w = 1; w < kFewThreads / 32; ++w) p = join_pairs(p, sh[w][threadIdx.x]);
-        pairs[(long long)blockIdx.x * kFew + threadIdx.x] = p;
-    }
-}
-
-// The blocks' pairs of a token -> loss and lse, a warp per token.
-__global__ void __launch_bounds__(kFew * 32)
-    xent_few_join_kernel(const int32_t* count, long long capacity, const int32_t* targets, int V,
-                         const float2* __restrict__ pairs, int blocks, const float* at_target, float* loss,
-                         float* lse, unsigned* status) {
-    pdl_wait();
-    pdl_trigger();
-    const float least = -__int_as_float(0x7f800000);
-    const int n = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (n >= token_rows(count, capacity, status)) return;
-    const int t = targets[n];
-    const bool in = t >= 0 && t < V;
-    if (!in && t != -1 && lane == 0) report(status, kErrIndex);
-    float2 p = make_float2(least, 0.f);
-#pragma unroll 8
-    for (int b = lane; b < blocks; b += 32) p = join_pairs(p, pairs[(long long)b * kFew + n]);
-    p = join_lanes<32>(p);
-    if (lane != 0) return;
-    const float all = p.x + logf(p.y);
-    if (lse) lse[n] = in ? all : 0.f;
-    if (loss) loss[n] = in ? all - at_target[n] : 0.f;
-}
-
 // ---------------------------------------------------------------- joins
 // The pairs of a row -> loss and lse: 8 rows a block (64 neighbouring bytes of a
 // part), every 128th part a thread; then a warp per row. Rows may be few
@@ -1401,39 +1263,6 @@ struct Call {
                       direct ? a.C : pitch, box);
     }
 
-    template <int VEC, int kTokens>
-    hc_status few_tokens(float2* pairs, float* at_target, int blocks) {
-        const size_t smem = (size_t)kTokens * ((a.C + 255) / 256 * 256) * 4;
-        return launch_pdl(xent_few_kernel<T, VEC, kTokens>, dim3((unsigned)blocks), dim3(kFewThreads), smem, s,
-                          "xent_few_kernel", (const T*)a.x, (const T*)a.W, a.bias, a.targets, a.C, a.V, pairs,
-                          at_target);
-    }
-    template <int VEC>
-    hc_status few_tokens(float2* pairs, float* at_target, int blocks) {
-        switch (a.capacity) {
-            case 1: return few_tokens<VEC, 1>(pairs, at_target, blocks);
-            case 2: return few_tokens<VEC, 2>(pairs, at_target, blocks);
-            case 3: return few_tokens<VEC, 3>(pairs, at_target, blocks);
-            default: return few_tokens<VEC, 4>(pairs, at_target, blocks);
-        }
-    }
-    hc_status forward_few() {
-        constexpr int kVec = 16 / (int)sizeof(T);
-        // as many blocks as run at a time, a class a warp at least
-        const long long need = ((long long)a.V + kFewThreads / 32 - 1) / (kFewThreads / 32);
-        const long long cap = (a.capacity == 1 ? 4ll : a.capacity == 2 ? 3ll : 2ll) * ctx->num_sms;
-        const int blocks = (int)(need < cap ? need : cap);
-        float2* const pairs = (float2*)stream_workspace(s, ((size_t)blocks * kFew + kFew) * sizeof(float2));
-        if (!pairs) return HC_ERR_CUDA;
-        float* const at_target = reinterpret_cast<float*>(pairs + (size_t)blocks * kFew);
-        const bool wide = a.C % kVec == 0 && (reinterpret_cast<uintptr_t>(a.W) & 15) == 0;
-        const hc_status st = wide ? few_tokens<kVec>(pairs, at_target, blocks) : few_tokens<1>(pairs, at_target, blocks);
-        if (st != HC_OK) return st;
-        return launch_pdl(xent_few_join_kernel, dim3(1), dim3(kFew * 32), 0, s, "xent_few_join_kernel", a.count,
-                          (long long)a.capacity, a.targets, a.V, (const float2*)pairs, blocks,
-                          (const float*)at_target, a.loss_out, a.lse_out, ctx->status);
-    }
-
     // Columns of a tile of logits: the ones whose rounds over the pairs of SMs take
     // least. A block of the sum takes 512 clocks with 256 columns, about 380 and
     // 320 with 128 and 64, which the loads bound (79 tokens of 113 x 2036 fp32: 63 us in
@@ -1464,8 +1293,6 @@ struct Call {
     }
 
     hc_status forward() {
-        // their rows have to fit the 48 KiB of shared memory that every launch may have
-        if (a.capacity <= kFew && (long long)a.capacity * up(a.C, 256) * 4 <= 47 * 1024) return forward_few();
         const int bn = columns(a.V);
         const int parts = (int)(((long long)a.V + kCols - 1) / kCols);
         float2* pairs = nullptr;
@@ -1604,11 +1431,13 @@ struct Call {
 
 hc_status launch_linear_xent_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
     if (xent_small_supported(a)) return launch_xent_small_fwd(ctx, a, s);
+    if (xent_few_supported(a)) return launch_xent_few_fwd(ctx, a, s);
     return a.dt == HC_BF16 ? Call<__nv_bfloat16>(ctx, a, s).forward() : Call<float>(ctx, a, s).forward();
 }
 
 hc_status launch_linear_xent_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
     if (xent_small_supported(a)) return launch_xent_small_bwd(ctx, a, s);
+    if (xent_few_supported(a)) return launch_xent_few_bwd(ctx, a, s);
     return a.dt == HC_BF16 ? Call<__nv_bfloat16>(ctx, a, s).backward() : Call<float>(ctx, a, s).backward();
 }
 

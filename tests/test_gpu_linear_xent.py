@@ -335,6 +335,48 @@ def test_sums_of_gradients_over_classes(dtype):
     assert abs(float(o["dbias"].to(D64).sum())) <= n * (100 + 16 * 40) * U
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n,slack,V,C", [
+    (1, 0, 5003, 2056), (1, 0, 1000, 11520), (1, 1, 700, 333), (2, 0, 511, 4104), (2, 1, 40000, 264),
+    (3, 0, 129, 1000), (3, 1, 2049, 130), (4, 0, 33, 2048), (4, 0, 6000, 65), (0, 4, 300, 520)])
+def test_few_tokens(n, slack, V, C, dtype):
+    """Up to four tokens, and the same bits of each gradient alone."""
+    x, W, b, t, dloss = inputs(n + V + C, n + slack, V, C, dtype, ignored=0.0)
+    if n == 4:
+        t[1] = -1
+        x[1], dloss[1] = float("nan"), float("inf")
+    x[n:], dloss[n:] = float("nan"), float("nan")
+    o = run_all(x, W, b, t, dloss, n)
+    check(x, W, b, t, dloss, n, o)
+    for name in ("dx", "dW", "dbias"):
+        alone = full(o[name].shape, o[name].dtype)
+        hc.hc_linear_cross_entropy_bwd(x, W, b, t, o["lse"], dloss, count=count_of(n), **{name: alone})
+        assert torch.equal(alone, o[name]), name
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("cap", [1, 2, 3, 4])
+def test_few_sure_tokens(cap, dtype):
+    """A logit of about 1000, the others' below 200: their probabilities are zero in fp32
+    (exp(-104) is), lse is the logit to the last bit and so every gradient zero."""
+    V, C = 700, 2056
+    g = gen(cap)
+    W = (randn(g, V, C) * C ** -0.5).to(dtype)
+    t = torch.randint(0, V, (cap,), generator=g, device="cuda")
+    x, b = (1000 * W[t].float()).to(dtype), 0.3 * randn(g, V)
+    o = run_all(x, W, b, t.int(), torch.full((cap,), 3.0, device="cuda"), None)
+    for name in ("loss", "dx", "dW", "dbias"):
+        assert (o[name] == 0).all(), name
+
+
+def test_few_tokens_in_place():
+    """dx may be x."""
+    x, W, b, t, dloss = inputs(3, 4, 900, 520, BF, ignored=0.0)
+    o = run_all(x, W, b, t, dloss, None)
+    hc.hc_linear_cross_entropy_bwd(x, W, b, t, o["lse"], dloss, dx=x)
+    assert torch.equal(x, o["dx"])
+
+
 def test_first_weight_special():
     """The first token's dloss of zero, infinite, or below the normal numbers:
     the others' gradients are as without it."""
