@@ -12,7 +12,7 @@
 // L2), a thread for the same channels of all of them: dW is written, dx added up in
 // shared memory and, over the blocks, by a last kernel.
 //
-// One of 32000 x 4096 bf16: 48 us, 39 at the copy rate; its gradients 153 us, 77 at
+// One of 32000 x 4096 bf16: 48 us, 39 at the copy rate; its gradients 152 us, 77 at
 // the copy rate (286 on the tensor cores, whose W is split or read once for the
 // logits and once for dx): a block's two phases alternate behind barriers. Four of
 // 32000 x 1024 fp32: 92 us (303).
@@ -208,13 +208,23 @@ struct GradArgs {
 
 constexpr int kBatch = kWarps * kRows;  // classes of a block at a time
 
+// Groups of threads, each of which holds all channels and takes its share of a
+// batch's classes (three of 121848 x 152 bf16: 49 us, 74 with one group).
+__host__ __device__ __forceinline__ int groups_of(int C, int vec) {
+    const int units = (C + vec - 1) / vec, n = kThreads / units;
+    return n < 1 ? 1 : n < 8 ? n : 8;
+}
+
 template <typename T, int VEC, int kTokens>
 __global__ void __launch_bounds__(kThreads)
     xent_few_bwd_kernel(const GradArgs a) {
-    extern __shared__ __align__(16) float smem[];  // the rows of x, then those of dx
+    extern __shared__ __align__(16) float smem[];  // the rows of x, then each group's of dx
     __shared__ float g[kBatch][kTokens];
     const int warp = threadIdx.x >> 5, C = a.C, V = a.V, pitch = pitch_of(C);
-    float *const rows = smem, *const dx = smem + kTokens * pitch;
+    const int groups = groups_of(C, VEC), span = groups > 1 ? (C + VEC - 1) / VEC : kThreads;
+    const int group = (int)threadIdx.x / span;
+    float *const rows = smem, *const sum_dx = smem + kTokens * pitch;
+    float* const dx = sum_dx + group * kTokens * pitch;  // of the threads with group < groups
     pdl_wait();
     pdl_trigger();
     const long long used = token_rows(a.count, kTokens, a.status);
@@ -237,9 +247,9 @@ __global__ void __launch_bounds__(kThreads)
         // zero for a token that takes no part, whatever it holds
         for (int c = threadIdx.x; c < pitch; c += kThreads) {
             rows[t * pitch + place<VEC>(c)] = target >= 0 && c < C ? to_f32(x[(long long)t * C + c]) : 0.f;
-            dx[t * pitch + c] = 0.f;
         }
     }
+    for (int i = threadIdx.x; i < groups * kTokens * pitch; i += kThreads) sum_dx[i] = 0.f;
     for (long long b0 = (long long)blockIdx.x * kBatch; b0 < V; b0 += (long long)gridDim.x * kBatch) {
         __syncthreads();  // the rows are there, or the last batch's G has been used
         {
@@ -262,7 +272,7 @@ __global__ void __launch_bounds__(kThreads)
             for (int t = 0; t < kTokens; ++t) s += g[threadIdx.x][t];
             a.dbias[b0 + threadIdx.x] = s;
         }
-        for (int c = threadIdx.x * VEC; c < C; c += kThreads * VEC) {
+        for (int c = (threadIdx.x - group * span) * VEC; c < C && group < groups; c += span * VEC) {
             float f[kTokens][VEC], d[kTokens][VEC];
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) {
@@ -270,7 +280,7 @@ __global__ void __launch_bounds__(kThreads)
                 get<VEC>(dx + t * pitch, c, d[t]);
             }
 #pragma unroll 4
-            for (int k = 0; k < classes; ++k) {
+            for (int k = group; k < classes; k += groups) {
                 const long long at = (b0 + k) * C + c;
                 float gk[kTokens];
 #pragma unroll
@@ -303,8 +313,11 @@ __global__ void __launch_bounds__(kThreads)
     if (!a.part) return;
     __syncthreads();
     for (int t = 0; t < kTokens; ++t)
-        for (int c = threadIdx.x; c < C; c += kThreads)
-            a.part[((long long)blockIdx.x * kTokens + t) * C + c] = dx[t * pitch + place<VEC>(c)];
+        for (int c = threadIdx.x; c < C; c += kThreads) {
+            float v = 0.f;
+            for (int k = 0; k < groups; ++k) v += sum_dx[(k * kTokens + t) * pitch + place<VEC>(c)];
+            a.part[((long long)blockIdx.x * kTokens + t) * C + c] = v;
+        }
 }
 
 // dx from the blocks' sums, 32 channels of a token a block: every 32nd part a
@@ -369,8 +382,9 @@ hc_status backward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s
         g.part = (float*)stream_workspace(s, (size_t)blocks * kTokens * a.C * 4);
         if (!g.part) return HC_ERR_CUDA;
     }
-    // both rows of every token: at most 94 KiB
-    const size_t smem = 2 * (size_t)kTokens * pitch_of(a.C) * 4;
+    // At most 92 KiB with one group; more groups have C <= 128 * VEC: 9 rows of each
+    // token of C <= 256, 5 of 512, 3 of 1024, 48 KiB
+    const size_t smem = (1 + groups_of(a.C, VEC)) * (size_t)kTokens * pitch_of(a.C) * 4;
     auto kern = xent_few_bwd_kernel<T, VEC, kTokens>;
     static bool done[64];
     if (smem > 47 * 1024 && !done[ctx->device]) {
