@@ -12,10 +12,10 @@
 // L2), a thread for the same channels of all of them: dW is written, dx added up in
 // shared memory and, over the blocks, by a last kernel.
 //
-// One of 32000 x 4096 bf16: 48 us, 39 at the copy rate; its gradients 152 us, 77 at
-// the copy rate (286 on the tensor cores, whose W is split or read once for the
-// logits and once for dx): a block's two phases alternate behind barriers. Four of
-// 32000 x 1024 fp32: 92 us (303).
+// One of 32000 x 4096 bf16: 49 us, 39 at the copy rate; its gradients 150 us, 77 at
+// the copy rate (286 on the tensor cores, which take 256 tokens at a time). There a
+// block's two phases alternate behind barriers, and half of W's second read comes
+// from memory (405 MB are read for 262). Four of 32000 x 1024 fp32: 94 us (303).
 #include "xent.cuh"
 
 namespace hc {
@@ -208,6 +208,10 @@ struct GradArgs {
 
 constexpr int kBatch = kWarps * kRows;  // classes of a block at a time
 
+// Blocks of a multiprocessor backward. Three have 80 registers a thread: one of
+// 32000 x 4096 bf16 156 us against 150, two of 131072 x 4096 633 against 543.
+constexpr int kBackBlocks = 2;
+
 // Groups of threads, each of which holds all channels and takes its share of a
 // batch's classes (three of 121848 x 152 bf16: 49 us, 74 with one group).
 __host__ __device__ __forceinline__ int groups_of(int C, int vec) {
@@ -216,7 +220,7 @@ __host__ __device__ __forceinline__ int groups_of(int C, int vec) {
 }
 
 template <typename T, int VEC, int kTokens>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBackBlocks)
     xent_few_bwd_kernel(const GradArgs a) {
     extern __shared__ __align__(16) float smem[];  // the rows of x, then each group's of dx
     __shared__ float g[kBatch][kTokens];
@@ -371,10 +375,8 @@ hc_status forward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s)
 
 template <typename T, int VEC, int kTokens>
 hc_status backward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
-    // one of 32000 x 4096 bf16: 153 us with 4 blocks a multiprocessor, 166 with 2; three of
-    // 121848 x 152: 78 and 74
     const long long need = ((long long)a.V + kBatch - 1) / kBatch;
-    const long long cap = (kTokens <= 2 ? 4ll : 2ll) * ctx->num_sms;
+    const long long cap = (long long)kBackBlocks * ctx->num_sms;
     const int blocks = (int)(need < cap ? need : cap);
     GradArgs g{a.x, a.W, a.bias, a.targets, a.count, a.lse, a.dloss, a.C, a.V, a.dW, a.dbias, nullptr,
                ctx->status};
