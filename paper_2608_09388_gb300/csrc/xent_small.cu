@@ -21,6 +21,14 @@ constexpr int kThreads = 256;
 constexpr int kTokens = 32;
 constexpr int kMaxPerThread = 8;  // VJ * CJ: 32 sums of dW a thread
 
+// Blocks of a multiprocessor, by the registers of a thread's sums (64 where there are
+// four). Loss and gradients of 16763 of 42 x 64 fp32: 30 us so, 33 with four blocks
+// backward, 36 with three of both; of a million of 5 x 16 418 us, 504 with two backward.
+template <int VJ, int CJ>
+constexpr int kForward = VJ * CJ <= 4 ? 4 : 2;
+template <int VJ, int CJ>
+constexpr int kBackward = VJ * CJ <= 2 ? 4 : 2;
+
 struct SmallArgs {
     const void* x;
     const void* W;
@@ -130,7 +138,7 @@ struct Head {
 };
 
 template <typename T, int VJ, int CJ>
-__global__ void __launch_bounds__(kThreads) xent_small_fwd_kernel(const SmallArgs a) {
+__global__ void __launch_bounds__(kThreads, kForward<VJ, CJ>) xent_small_fwd_kernel(const SmallArgs a) {
     using H = Head<T, VJ, CJ>;
     extern __shared__ __align__(16) float smem[];
     float *const w = smem, *const x = w + 16 * VJ * H::kRow;
@@ -177,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) xent_small_fwd_kernel(const SmallArg
 }
 
 template <typename T, int VJ, int CJ>
-__global__ void __launch_bounds__(kThreads) xent_small_bwd_kernel(const SmallArgs a) {
+__global__ void __launch_bounds__(kThreads, kBackward<VJ, CJ>) xent_small_bwd_kernel(const SmallArgs a) {
     using H = Head<T, VJ, CJ>;
     extern __shared__ __align__(16) float smem[];
     float *const w = smem, *const x = w + 16 * VJ * H::kRow, *const g = x + kTokens * H::kRow;
@@ -362,18 +370,14 @@ SmallArgs args_of(const DeviceCtx* ctx, const LinearXentArgs& a, size_t size) {
     return s;
 }
 
-// Two blocks an SM: with W, a tile and its G each has at most 60 KB.
-unsigned grid_of(const DeviceCtx* ctx, const LinearXentArgs& a) {
-    const long long tiles = ((long long)a.capacity + kTokens - 1) / kTokens, cap = 3ll * ctx->num_sms;
-    return (unsigned)(tiles < 1 ? 1 : tiles < cap ? tiles : cap);
-}
-
 template <typename T, int VJ, int CJ>
 hc_status run(const DeviceCtx* ctx, const LinearXentArgs& a, bool back, cudaStream_t s) {
     using H = Head<T, VJ, CJ>;
     static_assert(VJ * CJ <= kMaxPerThread, "sums of dW a thread");
     SmallArgs k = args_of(ctx, a, sizeof(T));
-    const unsigned grid = grid_of(ctx, a);
+    const long long tiles = ((long long)a.capacity + kTokens - 1) / kTokens;
+    const long long cap = (long long)(back ? kBackward<VJ, CJ> : kForward<VJ, CJ>)*ctx->num_sms;
+    const unsigned grid = (unsigned)(tiles < 1 ? 1 : tiles < cap ? tiles : cap);
     auto kern = back ? xent_small_bwd_kernel<T, VJ, CJ> : xent_small_fwd_kernel<T, VJ, CJ>;
     static bool done[2][64];
     if (H::kSmem > 48 * 1024 && !done[back][ctx->device]) {
@@ -419,13 +423,11 @@ hc_status by_classes(const DeviceCtx* ctx, const LinearXentArgs& a, bool back, c
 
 }  // namespace
 
-// Forward and gradients of a head of 42 x 64 against the tensor-core path: 2048
-// tokens 34 and 50 us (the host's time), 65536 85 and 155 (fp32 227), a million 1.11
-// and 2.02 ms. Larger heads of many bf16 tokens lose: 128 x 64 of 16384 tokens
-// 70 and 77 us, of 65536 173 and 157, of a million 2.53 and 2.09 ms; in fp32 they
-// do not (2.54 and 2.84 ms).
+// Forward and gradients against the tensor-core path: 42 x 64 bf16, 2048 tokens 34 and 52
+// us (the host's time), 65536 78 and 187 (fp32 241), a million 1.06 and 2.79 ms; the
+// largest heads, 128 x 64 bf16, 16384 tokens 55 and 84 us, a million 2.26 and 2.86 ms, and
+// 32 x 256, 66 and 99 us, 3.12 and 3.52 ms.
 bool xent_small_supported(const LinearXentArgs& a) {
-    if (a.dt == HC_BF16 && (long long)a.V * a.C > 4096 && a.capacity > 32768) return false;
     if (a.V <= 32) return a.C <= 256;
     if (a.V <= 64) return a.C <= 128;
     return a.V <= 128 && a.C <= 64;
