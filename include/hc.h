@@ -671,12 +671,12 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
  *   loss, lse [capacity] fp32, or NULL each; at least one is required. lse is
  *             what hc_linear_cross_entropy_bwd reads
  * fp32 operands keep fp32's precision: each is split into three bf16 numbers,
- * and the products that matter are summed (plain fp32 for up to four rows and for few
- * classes of few channels). Uses the library's per-stream workspace: with planes = 1
- * (bf16) or 3 (fp32), 2 * planes * C + 16 bytes a row of the capacity (rounded up
- * to 256 rows), 8 bytes a row and 64 classes, and 2 * planes * C bytes a class for
- * fp32 and for rows of W that are not 16-byte aligned. Four rows and small heads take
- * less than a megabyte.
+ * and the products that matter are summed. Up to four rows, up to eight where
+ * they or W are short, and few classes of few channels are summed in plain fp32.
+ * Uses the library's per-stream workspace: with planes = 1 (bf16) or 3 (fp32),
+ * 2 * planes * C + 16 bytes a row of the capacity (rounded up to 256 rows), 8
+ * bytes a row and 64 classes, and 2 * planes * C bytes a class for fp32 and for
+ * rows of W that are not 16-byte aligned; in plain fp32 less than a megabyte.
  */
 hc_status hc_linear_cross_entropy_fwd(const void* x, const void* W, hc_dtype dt, const float* bias,
                                       const int32_t* targets, const int32_t* count, int capacity,
@@ -696,10 +696,11 @@ hc_status hc_linear_cross_entropy_fwd(const void* x, const void* W, hc_dtype dt,
  *   dW        [V, C] of dtype dt, or NULL; may not overlap W
  *   dbias     [V] fp32, or NULL; at least one output is required
  * G is held in bf16 for bf16 operands (a rounding of 2^-8 at most), in three bf16
- * numbers for fp32 (in fp32 for up to four rows and small heads); sums are in fp32. The vocabulary is taken in pieces whose G
- * takes at most 512 MiB of the workspace (2048 classes at least); the sums of dx
- * take 4 * C bytes a row of the capacity and 30 MB more than the forward, those of dW and
- * dbias 52 MB, all of it at most 15 MB for up to four rows and small heads.
+ * numbers for fp32, in fp32 where the forward is plain fp32; sums are in fp32.
+ * The vocabulary is taken in pieces whose G takes at most 512 MiB of the workspace
+ * (2048 classes at least); the sums of dx take 4 * C bytes a row of the capacity
+ * and 30 MB more than the forward, those of dW and dbias 52 MB. In plain fp32
+ * all of it is at most 15 MB.
  */
 hc_status hc_linear_cross_entropy_bwd(const void* x, const void* W, hc_dtype dt, const float* bias,
                                       const int32_t* targets, const float* lse, const float* dloss,

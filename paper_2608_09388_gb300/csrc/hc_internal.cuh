@@ -294,7 +294,7 @@ struct LinearXentArgs {
 hc_status launch_linear_xent_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
 hc_status launch_linear_xent_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
 
-// The same for up to four tokens (xent_few.cu).
+// The same for up to eight tokens (xent_few.cu).
 bool xent_few_supported(const LinearXentArgs& a);
 hc_status launch_xent_few_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);
 hc_status launch_xent_few_bwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s);

@@ -28,7 +28,7 @@
 // 10.8 ms (17.6 TFLOP at 1.63 to 1.70 PFLOP/s; a plain product sustains 1.72 at the
 // power limit), of 2048 of 32000 x 1024 371 to 377 us (284 at the burst rate). There
 // the tensor pipe is busy 74 to 83% of the products' time: 13.2 rounds of tiles in
-// 14, and a tile of 16 blocks is not much longer than its epilogue. Up to four tokens go
+// 14, and a tile of 16 blocks is not much longer than its epilogue. Up to eight tokens go
 // to xent_few.cu, small heads to xent_small.cu.
 #include "pipeline.cuh"
 #include "xent.cuh"

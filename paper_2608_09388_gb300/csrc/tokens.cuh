@@ -218,6 +218,13 @@ struct Piece<__nv_bfloat16, 4> {
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
         v = *reinterpret_cast<const uint2*>(p);
     }
+    __device__ __forceinline__ void store(__nv_bfloat16* p) const {
+        *reinterpret_cast<uint2*>(p) = v;
+    }
+    __device__ __forceinline__ void set_all(const float (&f)[4]) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+        v = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    }
     __device__ __forceinline__ float get(int i) const {
         const uint32_t w = i >> 1 ? v.y : v.x;
         return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);

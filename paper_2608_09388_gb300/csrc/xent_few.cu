@@ -1,4 +1,4 @@
-// The cross entropy behind a linear layer for up to four tokens (a scoring or
+// The cross entropy behind a linear layer for up to eight tokens (a scoring or
 // decoding step, and the gradients of one). The formulas are those of
 // linear_xent.cu. Bound by the one read of W, and backward the write of dW, so the sums
 // are taken on the CUDA cores, in fp32 throughout, straight from the rows as
@@ -21,7 +21,7 @@
 namespace hc {
 namespace {
 
-constexpr int kFew = 4;
+constexpr int kFew = 8;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kRows = 4;
@@ -34,26 +34,26 @@ __device__ __forceinline__ int place(int c) {
 __host__ __device__ __forceinline__ int pitch_of(int C) {
     return (C + 255) & ~255;
 }
-// VEC floats of a row in shared memory, channels c .. of a piece.
-template <int VEC>
-__device__ __forceinline__ void get(const float* row, int c, float (&f)[VEC]) {
+// N floats of a row in shared memory from channel c on.
+template <int VEC, int N>
+__device__ __forceinline__ void get(const float* row, int c, float (&f)[N]) {
     if constexpr (VEC == 1) {
         f[0] = row[c];
     } else {
 #pragma unroll
-        for (int e = 0; e < VEC; e += 4) {
+        for (int e = 0; e < N; e += 4) {
             const float4 q = *reinterpret_cast<const float4*>(row + place<VEC>(c + e));
             f[e] = q.x, f[e + 1] = q.y, f[e + 2] = q.z, f[e + 3] = q.w;
         }
     }
 }
-template <int VEC>
-__device__ __forceinline__ void set(float* row, int c, const float (&f)[VEC]) {
+template <int VEC, int N>
+__device__ __forceinline__ void set(float* row, int c, const float (&f)[N]) {
     if constexpr (VEC == 1) {
         row[c] = f[0];
     } else {
 #pragma unroll
-        for (int e = 0; e < VEC; e += 4)
+        for (int e = 0; e < N; e += 4)
             *reinterpret_cast<float4*>(row + place<VEC>(c + e)) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
     }
 }
@@ -62,7 +62,7 @@ __device__ __forceinline__ void set(float* row, int c, const float (&f)[VEC]) {
 // lane's upper bits being r and t.
 template <int kTokens>
 struct Lanes {
-    static constexpr int kT = kTokens == 3 ? 4 : kTokens, kValues = kRows * kT;
+    static constexpr int kT = kTokens == 3 ? 4 : kTokens == 6 ? 8 : kTokens, kValues = kRows * kT;
     static constexpr int kSame = 32 / kValues;  // lanes with the same value
     int r, t;
     bool first;
@@ -81,7 +81,7 @@ __device__ __forceinline__ float sums(const float* rows, int pitch, const T* __r
     using L = Lanes<kTokens>;
     const int lane = threadIdx.x & 31;
     float s[kRows][kTokens] = {};
-#pragma unroll 2
+#pragma unroll kTokens <= 4 ? 2 : 1
     for (int c = lane * VEC; c < C; c += 32 * VEC) {
         Piece<T, VEC> p[kRows];
 #pragma unroll
@@ -119,7 +119,7 @@ __device__ __forceinline__ float sums(const float* rows, int pitch, const T* __r
 template <typename T, int VEC, int kTokens>
 __global__ void __launch_bounds__(kThreads, kTokens == 1 ? 4 : kTokens == 2 ? 3 : 2)
     xent_few_kernel(const T* __restrict__ x, const T* __restrict__ W, const float* __restrict__ bias,
-                    const int32_t* targets, int C, int V, float2* __restrict__ pairs,
+                    const int32_t* targets, int tokens, int C, int V, float2* __restrict__ pairs,
                     float* __restrict__ at_target) {
     extern __shared__ __align__(16) float rows[];  // [kTokens][pitch]
     __shared__ float2 sh[kWarps][kTokens];
@@ -131,10 +131,10 @@ __global__ void __launch_bounds__(kThreads, kTokens == 1 ? 4 : kTokens == 2 ? 3 
     int my_target = -1;
 #pragma unroll
     for (int t = 0; t < kTokens; ++t) {
-        const int target = targets[t];
+        const int target = t < tokens ? targets[t] : -1;
         my_target = me.t == t ? target : my_target;
         for (int c = threadIdx.x; c < C; c += kThreads)
-            rows[t * pitch + place<VEC>(c)] = to_f32(x[(long long)t * C + c]);
+            rows[t * pitch + place<VEC>(c)] = t < tokens ? to_f32(x[(long long)t * C + c]) : 0.f;
     }
     __syncthreads();
     float2 mine = make_float2(least, 0.f);
@@ -199,7 +199,7 @@ struct GradArgs {
     const int32_t* count;
     const float* lse;
     const float* dloss;
-    int C, V;
+    int capacity, C, V;
     void* dW;      // or NULL
     float* dbias;  // or NULL
     float* part;   // [blocks][kTokens][C]: the blocks' sums of dx, or NULL
@@ -219,19 +219,24 @@ __host__ __device__ __forceinline__ int groups_of(int C, int vec) {
     return n < 1 ? 1 : n < 8 ? n : 8;
 }
 
+// Channels a thread takes at a time there: those of all tokens, and of dx, are in registers.
+template <int VEC, int kTokens>
+constexpr int kChannels = kTokens > 4 && VEC > 4 ? 4 : VEC;
+
 template <typename T, int VEC, int kTokens>
 __global__ void __launch_bounds__(kThreads, kBackBlocks)
     xent_few_bwd_kernel(const GradArgs a) {
     extern __shared__ __align__(16) float smem[];  // the rows of x, then each group's of dx
     __shared__ float g[kBatch][kTokens];
     const int warp = threadIdx.x >> 5, C = a.C, V = a.V, pitch = pitch_of(C);
-    const int groups = groups_of(C, VEC), span = groups > 1 ? (C + VEC - 1) / VEC : kThreads;
+    constexpr int kC = kChannels<VEC, kTokens>;
+    const int groups = groups_of(C, kC), span = groups > 1 ? (C + kC - 1) / kC : kThreads;
     const int group = (int)threadIdx.x / span;
     float *const rows = smem, *const sum_dx = smem + kTokens * pitch;
     float* const dx = sum_dx + group * kTokens * pitch;  // of the threads with group < groups
     pdl_wait();
     pdl_trigger();
-    const long long used = token_rows(a.count, kTokens, a.status);
+    const long long used = token_rows(a.count, a.capacity, a.status);
     const T *const x = static_cast<const T*>(a.x), *const W = static_cast<const T*>(a.W);
     const Lanes<kTokens> me;
     int my_target = -1;
@@ -276,8 +281,8 @@ __global__ void __launch_bounds__(kThreads, kBackBlocks)
             for (int t = 0; t < kTokens; ++t) s += g[threadIdx.x][t];
             a.dbias[b0 + threadIdx.x] = s;
         }
-        for (int c = (threadIdx.x - group * span) * VEC; c < C && group < groups; c += span * VEC) {
-            float f[kTokens][VEC], d[kTokens][VEC];
+        for (int c = (threadIdx.x - group * span) * kC; c < C && group < groups; c += span * kC) {
+            float f[kTokens][kC], d[kTokens][kC];
 #pragma unroll
             for (int t = 0; t < kTokens; ++t) {
                 get<VEC>(rows + t * pitch, c, f[t]);
@@ -290,22 +295,22 @@ __global__ void __launch_bounds__(kThreads, kBackBlocks)
 #pragma unroll
                 for (int t = 0; t < kTokens; ++t) gk[t] = g[k][t];
                 if (a.part) {
-                    Piece<T, VEC> p;
+                    Piece<T, kC> p;
                     p.load(W + at);
 #pragma unroll
                     for (int t = 0; t < kTokens; ++t)
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) d[t][e] = fmaf(gk[t], p.get(e), d[t][e]);
+                        for (int e = 0; e < kC; ++e) d[t][e] = fmaf(gk[t], p.get(e), d[t][e]);
                 }
                 if (a.dW) {
-                    float o[VEC];
+                    float o[kC];
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
+                    for (int e = 0; e < kC; ++e) {
                         o[e] = gk[0] * f[0][e];
 #pragma unroll
                         for (int t = 1; t < kTokens; ++t) o[e] = fmaf(gk[t], f[t][e], o[e]);
                     }
-                    Piece<T, VEC> p;
+                    Piece<T, kC> p;
                     p.set_all(o);
                     p.store(static_cast<T*>(a.dW) + at);
                 }
@@ -328,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, kBackBlocks)
 // warp, then the warps in order; zero for a token that takes no part.
 template <typename T>
 __global__ void __launch_bounds__(1024)
-    xent_few_input_kernel(const float* __restrict__ part, int blocks, const int32_t* count, int capacity,
+    xent_few_input_kernel(const float* __restrict__ part, int blocks, int slots, const int32_t* count, int capacity,
                           const int32_t* targets, int C, int V, T* dx, unsigned* status) {
     __shared__ float sh[32][33];
     pdl_wait();
@@ -341,7 +346,7 @@ __global__ void __launch_bounds__(1024)
     float v = 0.f;
     if (in && c < C) {
 #pragma unroll 8
-        for (int p = warp; p < blocks; p += 32) v += part[((long long)p * capacity + n) * C + c];
+        for (int p = warp; p < blocks; p += 32) v += part[((long long)p * slots + n) * C + c];
     }
     sh[warp][lane] = v;
     __syncthreads();
@@ -366,7 +371,7 @@ hc_status forward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s)
     const hc_status st =
         launch_pdl(xent_few_kernel<T, VEC, kTokens>, dim3((unsigned)blocks), dim3(kThreads),
                    (size_t)kTokens * pitch_of(a.C) * 4, s, "xent_few_kernel", (const T*)a.x,
-                   (const T*)a.W, a.bias, a.targets, a.C, a.V, pairs, at_target);
+                   (const T*)a.W, a.bias, a.targets, a.capacity, a.C, a.V, pairs, at_target);
     if (st != HC_OK) return st;
     return launch_pdl(xent_few_join_kernel, dim3(1), dim3(kFew * 32), 0, s, "xent_few_join_kernel",
                       a.count, (long long)a.capacity, a.targets, a.V, (const float2*)pairs, blocks,
@@ -378,15 +383,15 @@ hc_status backward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s
     const long long need = ((long long)a.V + kBatch - 1) / kBatch;
     const long long cap = (long long)kBackBlocks * ctx->num_sms;
     const int blocks = (int)(need < cap ? need : cap);
-    GradArgs g{a.x, a.W, a.bias, a.targets, a.count, a.lse, a.dloss, a.C, a.V, a.dW, a.dbias, nullptr,
+    GradArgs g{a.x, a.W, a.bias, a.targets, a.count, a.lse, a.dloss, a.capacity, a.C, a.V, a.dW, a.dbias, nullptr,
                ctx->status};
     if (a.dx) {
         g.part = (float*)stream_workspace(s, (size_t)blocks * kTokens * a.C * 4);
         if (!g.part) return HC_ERR_CUDA;
     }
-    // At most 92 KiB with one group; more groups have C <= 128 * VEC: 9 rows of each
-    // token of C <= 256, 5 of 512, 3 of 1024, 48 KiB
-    const size_t smem = (1 + groups_of(a.C, VEC)) * (size_t)kTokens * pitch_of(a.C) * 4;
+    // At most 92 KiB: with one group twice what xent_few_supported allows, with more, which
+    // have C <= 1024 (512 with five tokens or more), 72 KiB
+    const size_t smem = (1 + groups_of(a.C, kChannels<VEC, kTokens>)) * (size_t)kTokens * pitch_of(a.C) * 4;
     auto kern = xent_few_bwd_kernel<T, VEC, kTokens>;
     static bool done[64];
     if (smem > 47 * 1024 && !done[ctx->device]) {
@@ -399,8 +404,8 @@ hc_status backward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s
     const hc_status st = launch_pdl(kern, dim3((unsigned)blocks), dim3(kThreads), smem, s,
                                     "xent_few_bwd_kernel", g);
     if (st != HC_OK || !a.dx) return st;
-    return launch_pdl(xent_few_input_kernel<T>, dim3((unsigned)((a.C + 31) / 32), (unsigned)kTokens),
-                      dim3(1024), 0, s, "xent_few_input_kernel", (const float*)g.part, blocks, a.count,
+    return launch_pdl(xent_few_input_kernel<T>, dim3((unsigned)((a.C + 31) / 32), (unsigned)a.capacity),
+                      dim3(1024), 0, s, "xent_few_input_kernel", (const float*)g.part, blocks, kTokens, a.count,
                       a.capacity, a.targets, a.C, a.V, (T*)a.dx, ctx->status);
 }
 
@@ -410,7 +415,10 @@ hc_status by_tokens(const DeviceCtx* ctx, const LinearXentArgs& a, bool back, cu
         case 1: return back ? backward<T, VEC, 1>(ctx, a, s) : forward<T, VEC, 1>(ctx, a, s);
         case 2: return back ? backward<T, VEC, 2>(ctx, a, s) : forward<T, VEC, 2>(ctx, a, s);
         case 3: return back ? backward<T, VEC, 3>(ctx, a, s) : forward<T, VEC, 3>(ctx, a, s);
-        default: return back ? backward<T, VEC, 4>(ctx, a, s) : forward<T, VEC, 4>(ctx, a, s);
+        case 4: return back ? backward<T, VEC, 4>(ctx, a, s) : forward<T, VEC, 4>(ctx, a, s);
+        case 5:
+        case 6: return back ? backward<T, VEC, 6>(ctx, a, s) : forward<T, VEC, 6>(ctx, a, s);
+        default: return back ? backward<T, VEC, 8>(ctx, a, s) : forward<T, VEC, 8>(ctx, a, s);
     }
 }
 
@@ -425,8 +433,15 @@ hc_status run(const DeviceCtx* ctx, const LinearXentArgs& a, bool back, cudaStre
 }  // namespace
 
 // Their rows in fp32 have to fit the 48 KiB of shared memory that every launch may have.
+// Forward and gradients against the tensor cores: eight of 33776 x 1168 fp32 226 and 544
+// us, of 32000 x 1024 bf16 125 and 135, six 110 and 137. More than four of a bf16 W that is
+// larger than the L2 lose, the products being cheap there and W read twice: six of
+// 131072 x 1280 465 and 432, eight 524 and 434.
 bool xent_few_supported(const LinearXentArgs& a) {
-    return a.capacity >= 1 && a.capacity <= kFew && (long long)a.capacity * ((a.C + 255ll) / 256 * 256) * 4 <= 46 * 1024;
+    if (a.capacity < 1 || a.capacity > kFew) return false;
+    if (a.dt == HC_BF16 && a.capacity > 4 && (long long)a.V * a.C > 1ll << 26) return false;
+    const long long slots = a.capacity <= 4 ? a.capacity : (a.capacity + 1) / 2 * 2;
+    return slots * ((a.C + 255ll) / 256 * 256) * 4 <= 46 * 1024;
 }
 
 hc_status launch_xent_few_fwd(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
