@@ -371,6 +371,49 @@ def test_few_sure_tokens(cap, C, dtype):
         assert (o[name] == 0).all(), name
 
 
+@pytest.mark.parametrize("cap,V,C,dtype", [(1, 3000, 520, BF), (4, 900, 264, F), (8, 2000, 1032, BF)])
+def test_few_tokens_replayed(cap, V, C, dtype):
+    """On two streams at a time, and captured, replayed with other rows and targets."""
+    x, W, b, t, dloss = inputs(cap + V, cap, V, C, dtype, ignored=0.0)
+    want = run_all(x, W, b, t, dloss, None)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [run_all(x, W, b, t, dloss, None, s) for s in streams]
+    torch.cuda.synchronize()
+    for o in outs:
+        assert all(torch.equal(o[k], want[k]) for k in want)
+    side, cnt, o = streams[0], count_of(cap), outs[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        hc.hc_linear_cross_entropy_fwd(x, W, b, t, o["loss"], o["lse"], count=cnt, stream=side)
+        hc.hc_linear_cross_entropy_bwd(x, W, b, t, o["lse"], dloss, dx=o["dx"], dW=o["dW"],
+                                       dbias=o["dbias"], count=cnt, stream=side)
+    for m in (cap, cap - 1):
+        cnt.fill_(m)
+        x.copy_(x.flip(1))
+        t.copy_((t + 17) % V)
+        for v in o.values():
+            v.fill_(77)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(x, W, b, t, dloss, m, o)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_few_tokens_bad_target(dtype):
+    """A target outside the classes is reported by either direction, and the token
+    takes no part."""
+    x, W, b, t, dloss = inputs(5, 3, 900, 264, dtype, ignored=0.0)
+    t[1] = -1
+    want = run_all(x, W, b, t, dloss, None)
+    t[1] = 900
+    o = run_all(x, W, b, t, dloss, None)
+    assert hc.hc_get_device_status() == hc.HC_ERR_INVALID_INDEX
+    assert all(torch.equal(o[k], want[k]) for k in want)
+    hc.hc_linear_cross_entropy_bwd(x, W, b, t, o["lse"], dloss, dbias=o["dbias"])
+    assert hc.hc_get_device_status() == hc.HC_ERR_INVALID_INDEX
+
+
 def test_few_tokens_in_place():
     """dx may be x."""
     x, W, b, t, dloss = inputs(3, 4, 900, 520, BF, ignored=0.0)
