@@ -116,8 +116,15 @@ __device__ __forceinline__ float sums(const float* rows, int pitch, const T* __r
     return v[0];
 }
 
+// Blocks of a multiprocessor forward: the sums of more tokens, or of eight channels for
+// three, take more registers than four blocks have (two of 32000 x 4096 bf16 70 us, 74
+// with three, of 121848 x 152 25 and 29, though of 131072 x 4096 201 and 192; four of 32000 x 1024 fp32 43, 47 with two, of 121848 x 151 bf16 33, 45 with
+// two; four of 32000 x 2048 bf16 49 with two, 70 with four).
+template <int VEC, int kTokens>
+constexpr int kForwardBlocks = kTokens <= 2 || (kTokens <= 4 && VEC < 8) ? 4 : 2;
+
 template <typename T, int VEC, int kTokens>
-__global__ void __launch_bounds__(kThreads, kTokens == 1 ? 4 : kTokens == 2 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, kForwardBlocks<VEC, kTokens>)
     xent_few_kernel(const T* __restrict__ x, const T* __restrict__ W, const float* __restrict__ bias,
                     const int32_t* targets, int tokens, int C, int V, float2* __restrict__ pairs,
                     float* __restrict__ at_target) {
@@ -363,7 +370,7 @@ template <typename T, int VEC, int kTokens>
 hc_status forward(const DeviceCtx* ctx, const LinearXentArgs& a, cudaStream_t s) {
     // as many blocks as run at a time, a class a warp at least
     const long long need = ((long long)a.V + kWarps - 1) / kWarps;
-    const long long cap = (kTokens == 1 ? 4ll : kTokens == 2 ? 3ll : 2ll) * ctx->num_sms;
+    const long long cap = (long long)kForwardBlocks<VEC, kTokens> * ctx->num_sms;
     const int blocks = (int)(need < cap ? need : cap);
     float2* const pairs = (float2*)stream_workspace(s, ((size_t)blocks * kFew + kFew) * sizeof(float2));
     if (!pairs) return HC_ERR_CUDA;
