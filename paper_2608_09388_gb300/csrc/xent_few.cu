@@ -118,8 +118,9 @@ __device__ __forceinline__ float sums(const float* rows, int pitch, const T* __r
 
 // Blocks of a multiprocessor forward: the sums of more tokens, or of eight channels for
 // three, take more registers than four blocks have (two of 32000 x 4096 bf16 70 us, 74
-// with three, of 121848 x 152 25 and 29, though of 131072 x 4096 201 and 192; four of 32000 x 1024 fp32 43, 47 with two, of 121848 x 151 bf16 33, 45 with
-// two; four of 32000 x 2048 bf16 49 with two, 70 with four).
+// with three, of 121848 x 152 25 and 29, though of 131072 x 4096 201 and 192; four of
+// 32000 x 1024 fp32 43, 47 with two, of 121848 x 151 bf16 33, 45 with two; four of
+// 32000 x 2048 bf16 49 with two, 70 with four).
 template <int VEC, int kTokens>
 constexpr int kForwardBlocks = kTokens <= 2 || (kTokens <= 4 && VEC < 8) ? 4 : 2;
 
