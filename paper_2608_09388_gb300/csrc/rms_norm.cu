@@ -604,11 +604,22 @@ hc_status launch_fwd_rows(const DeviceCtx* ctx, const RmsNormArgs& a, cudaStream
     constexpr int kGroups = kGroupThreads / TPR;
     const long long need = ((long long)a.capacity + kGroups - 1) / kGroups;
     const long long cap = (long long)ctx->num_sms;
-    // a row of v a group: at most 512 * 16 channels' 4 bytes and, below 128
-    // channels, the padding of 64 groups' rows to 128: 32 KiB both
+    // a row of v a group, padded to whole blocks of 128: 4 bytes for each of the at
+    // most 512 * VEC * NV channels held (64 KiB with 16 pairs a thread, 32 with
+    // single elements) or, below 128 channels, for the 128 of 64 groups' rows (32
+    // KiB). More than 48 KiB, the sums' 128 bytes among them, have to be allowed.
     const size_t smem = kQ && VEC <= 2 ? (size_t)kGroups * ((a.C + 127) / 128 * 128) * 4 : 0;
-    return launch_pdl(rms_fwd_rows_kernel<T, VEC, TPR, NV, kQ>,
-                      dim3((unsigned)(need < cap ? need : cap)), dim3(kGroupThreads), smem, s,
+    auto kern = rms_fwd_rows_kernel<T, VEC, TPR, NV, kQ>;
+    constexpr size_t kMost = (size_t)4 * kGroupThreads * VEC * NV;
+    static bool done[64];
+    if (kQ && VEC <= 2 && kMost > 47 * 1024 && smem > 47 * 1024 && !done[ctx->device]) {
+        const hc_status st = check_cuda(
+            cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost),
+            "rms_fwd_rows_kernel");
+        if (st != HC_OK) return st;
+        done[ctx->device] = true;
+    }
+    return launch_pdl(kern, dim3((unsigned)(need < cap ? need : cap)), dim3(kGroupThreads), smem, s,
                       "rms_fwd_rows_kernel", (const T*)a.x, (const T*)a.res, a.count,
                       (long long)a.capacity, a.C, a.eps, a.gamma, (T*)a.h, (T*)a.y, a.rstd_out,
                       out8(a), ctx->status);

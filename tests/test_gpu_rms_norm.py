@@ -121,6 +121,42 @@ def test_all_outputs(C, dtype):
     assert (dx[n:] == 77).all()
 
 
+def two_past(t):
+    """A copy whose first element lies two past a 16-byte boundary."""
+    s = torch.empty(t.numel() + 2, dtype=t.dtype, device="cuda")[2:].view(t.shape)
+    return s.copy_(t)
+
+
+# rows that allow 4-byte loads and no wider ones: by their width, by gamma's place
+# alone, by theirs; around the widths where a block's rows of v pass 32 and 48 KiB
+@pytest.mark.parametrize("C,moved", [(C, "none") for C in (514, 642, 770, 1022, 2050, 2946, 3078, 4094, 4098, 6018, 6150, 8190)]
+                         + [(C, m) for C in (1024, 4096, 8192) for m in ("gamma", "rows")])
+def test_8_bits_of_even_rows(C, moved):
+    n, cap = 203, 211
+    x, res, _, _, gamma = inputs(C + 2, cap, C, BF)
+    h, y = full((cap, C), BF), full((cap, C), BF)
+    if moved == "gamma":
+        gamma = two_past(gamma)
+    if moved == "rows":
+        x, res, h, y = (two_past(t) for t in (x, res, h, y))
+    rstd, q = full((cap,)), full((cap, hc.HC_FP8_PITCH(C)), torch.uint8, 77)
+    sc = full(((C + 127) // 128, cap))
+    hc.hc_rms_norm_fwd(x, 1e-5, gamma, res=res, h=h, y=y, rstd=rstd, q=q, scales=sc, count=count_of(n))
+    want = stored(x, res)
+    assert torch.equal(h[:n], want[:n])
+    v, rr, tv, tr = fwd_ref(want[:n], gamma, 1e-5)
+    within(rstd[:n], rr, tr, "rstd")
+    within(y[:n], v, tv + rounding(BF, v), "y")
+    q_ref, s_ref = quant_ref(want[:n].float() * rstd[:n, None] * gamma)
+    assert torch.equal(sc[:, :n], s_ref) and torch.equal(q[:n], q_ref)
+    assert (h[n:] == 77).all() and (y[n:] == 77).all() and (rstd[n:] == 77).all()
+    assert (q[n:] == 77).all() and (sc[:, n:] == 77).all()
+    # the 8-bit rows alone, of the stored sums
+    q1, sc1 = torch.full_like(q, 77), torch.full_like(sc, 77)
+    hc.hc_rms_norm_fwd(h, 1e-5, gamma, q=q1, scales=sc1, count=count_of(n))
+    assert torch.equal(q1, q) and torch.equal(sc1, sc)
+
+
 @pytest.mark.parametrize("n", [0, 1, 2, 3, 127, 128, 129, 5000])
 @pytest.mark.parametrize("C,dtype", [(64, BF), (131, F), (1024, BF), (4096, F), (8200, BF)])
 def test_rows(n, C, dtype):
