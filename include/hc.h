@@ -733,8 +733,8 @@ hc_status hc_tensor_list_fill(const void* const* in, void* const* out, const lon
  * hc_grad_norm -- the norm over all inputs of a list:
  *   norm = sqrt(sum over all tensors of in^2)      (one fp32; 0 for no elements)
  * Sums of more than 32 squares are taken in more than fp32 and in a fixed
- * order; squares above the range of fp32 are taken in 64 bits, what is smaller
- * than 2^-75 counts as 0. Uses the library's per-stream workspace (8 bytes
+ * order; squares and sums above the range of fp32 are taken in 64 bits, what is
+ * smaller than 2^-75 counts as 0. Uses the library's per-stream workspace (8 bytes
  * for each of at most 32 blocks per SM).
  */
 hc_status hc_grad_norm(const hc_tensor_list* list, float* norm, hc_stream_t stream);

@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kThreads, kResident)
     const long long u1 = units * (blockIdx.x + 1) / gridDim.x;
     long long u = units * blockIdx.x / gridDim.x;
     float hi = 0.f, lo = 0.f;
-    double far = 0.0;  // squares that fp32 does not hold
+    double far = 0.0;  // squares and sums that fp32 does not hold
     // the table has been there since before the first call: its look-up runs
     // while the kernel before ends
     int t = u < u1 ? find_entry(table, n, u) : 0;
@@ -148,12 +148,17 @@ __global__ void __launch_bounds__(kThreads, kResident)
                         s1 = fmaf(f.y, f.y, s1);
                     }
                 }
-                const float s = s0 + s1;
-                if (s < __int_as_float(0x7f800000)) {
+                const float s = s0 + s1, sum = hi + s;
+                if (sum < __int_as_float(0x7f800000)) {
                     // hi + s, and what the addition rounds off
-                    const float sum = hi + s, b = sum - hi;
+                    const float b = sum - hi;
                     lo += (hi - (sum - b)) + (s - b);
                     hi = sum;
+                } else if (s < __int_as_float(0x7f800000)) {
+                    // the sums so far go to 64 bits, and begin again here
+                    far += (double)hi + lo;
+                    hi = s;
+                    lo = 0.f;
                 } else {
 #pragma unroll 1
                     for (int i = 0; i < 4 * kPieces; ++i) {

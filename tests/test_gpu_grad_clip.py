@@ -159,6 +159,25 @@ def test_values():
     assert torch.equal(outs[0], a)
 
 
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("size", [2e17, 1e18, 4e18, 5e18, 6.5e18, 1.2e19])
+def test_running_sums_past_fp32(size, kind):
+    """20 M values whose squares fit fp32, as a thread's sum over a unit does at all
+    sizes but the largest (for bf16 the three largest), while its sum over all its
+    units does not from 4e18 on."""
+    g = gen(11)
+    n = {"f32": (20000001, 0), "bf16": (0, 20000001), "mixed": (7000003, 13000001)}[kind]
+    ts = [size * (0.9 + 0.1 * torch.rand(k, generator=g, device="cuda")) for k in n]
+    ts = [ts[0], ts[1].to(BF)]
+    norm, outs = clip_of(ts, 1.0)
+    assert norm.isfinite()
+    check(ts, outs, norm, 1.0)
+    # small ones before and behind the large ones still count
+    ones = [torch.full((50000,), size / 1024, device="cuda") for _ in range(2)]
+    norm, outs = clip_of([ones[0], *ts, ones[1]], 1.0)
+    check([ones[0], *ts, ones[1]], outs, norm, 1.0)
+
+
 def test_long_sum():
     """2^28 equal values: a plain fp32 chain would stop growing."""
     t = torch.full((2 ** 28,), 0.1, device="cuda")
