@@ -628,7 +628,9 @@ class hc_tensor_list(ctypes.Structure):
     """A list of tensors for hc_grad_norm and hc_grad_clip, made once: grads (fp32
     or bf16, any shapes, contiguous, on one device) and outs like them (None: in
     place). It holds them and its table on their device. Waits for the table's
-    copy, so that every stream may use it; not to be made during a capture."""
+    copy, so that every stream may use it; not to be made during a capture. It may
+    go once the last call with it has been made, but stays for as long as a captured
+    graph has one, and until calls on a stream given as a bare handle have run."""
     _fields_ = [("table", ctypes.c_void_p), ("units", ctypes.c_longlong),
                 ("tensors", ctypes.c_int)]
 
@@ -659,23 +661,32 @@ class hc_tensor_list(ctypes.Structure):
                "hc_tensor_list_fill")
         self.memory.copy_(host)
         torch.cuda.current_stream(self.device).synchronize()
+        # the streams whose work the table's memory outlives: the one it was allocated
+        # on, and those that _list adds
+        self.streams = {torch._C._cuda_getCurrentRawStream(self.device)}
 
 
-def _list(tensors):
+def _list(tensors, stream):
+    """The list's and the stream's arguments of a call."""
     import torch
     if not isinstance(tensors, hc_tensor_list):
         raise TypeError("an hc_tensor_list is expected")
     if tensors.device != torch._C._cuda_getDevice():
         raise ValueError(f"the list is of device {tensors.device}, which is not the current one")
-    return ctypes.byref(tensors)
+    s = _s(stream)
+    raw = s if stream is None else s.value or 0
+    if raw not in tensors.streams and (stream is None or isinstance(stream, torch.cuda.Stream)):
+        tensors.memory.record_stream(torch.cuda.current_stream() if stream is None else stream)
+        tensors.streams.add(raw)
+    return ctypes.byref(tensors), s
 
 
 def hc_grad_norm(tensors, norm, stream=None):
     """norm fp32 [1] = the norm over all grads of an hc_tensor_list."""
     f32 = _token_types()[0]
     _on_current_device(norm)
-    _check(load_library().hc_grad_norm(_list(tensors), _arg("norm", norm, (1,), f32), _s(stream)),
-           "hc_grad_norm")
+    lst, s = _list(tensors, stream)
+    _check(load_library().hc_grad_norm(lst, _arg("norm", norm, (1,), f32), s), "hc_grad_norm")
 
 
 def hc_grad_clip(tensors, norm, max_norm, stream=None):
@@ -683,8 +694,8 @@ def hc_grad_clip(tensors, norm, max_norm, stream=None):
     on the device."""
     f32 = _token_types()[0]
     _on_current_device(norm)
-    _check(load_library().hc_grad_clip(_list(tensors), _arg("norm", norm, (1,), f32), max_norm,
-                                       _s(stream)), "hc_grad_clip")
+    lst, s = _list(tensors, stream)
+    _check(load_library().hc_grad_clip(lst, _arg("norm", norm, (1,), f32), max_norm, s), "hc_grad_clip")
 
 
 def hc_test_set_option(option: int, value: int):

@@ -218,6 +218,39 @@ def test_stream_graph_and_shapes():
     assert shifted(sets[0][0]).shape == sets[0][0].shape
 
 
+@pytest.mark.parametrize("given", [True, False])
+def test_list_dropped_while_another_stream_uses_it(given):
+    """A list that goes right behind its calls on another stream than the one it was
+    made on: its table's memory goes to nobody before they have run."""
+    g = gen(13)
+    grads = [randn(g, 300), randn(g, 5000, dtype=BF)]
+    outs = [torch.full_like(t, 77) for t in grads]
+    norm, side = full((1,)), torch.cuda.Stream()
+    # the stream's workspace and the kernels are there: making them would wait
+    first = hc.hc_tensor_list(grads, outs)
+    hc.hc_grad_norm(first, norm, stream=side)
+    hc.hc_grad_clip(first, norm, 1.0, stream=side)
+    lst = hc.hc_tensor_list(grads, outs)
+    at, size = lst.memory.data_ptr(), lst.memory.numel()
+    torch.cuda.synchronize()
+    if given:
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(400_000_000)  # about 0.2 s
+        hc.hc_grad_norm(lst, norm, stream=side)
+        hc.hc_grad_clip(lst, norm, 1.0, stream=side)
+    else:
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(400_000_000)
+            hc.hc_grad_norm(lst, norm)
+            hc.hc_grad_clip(lst, norm, 1.0)
+    del lst
+    new = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    assert not side.query()  # still asleep: nothing below is late
+    assert all(t.data_ptr() + size <= at or at + size <= t.data_ptr() for t in new)
+    torch.cuda.synchronize()
+    check(grads, outs, norm, 1.0)
+
+
 def test_other_device_is_refused():
     lst = hc.hc_tensor_list([torch.zeros(3, device="cuda")])
     lst.device += 1
