@@ -531,7 +531,9 @@ hc_status hc_layer_norm_bwd(const void* x, const void* dy, hc_dtype dt, const in
  *             [ceil(C / 128), capacity] fp32, or both NULL
  * One of y and q is required. C >= 1, eps >= 0. Rows whose squares would pass
  * the range of fp32 are summed with their values scaled by a power of two. A
- * row of zeros gives zeros; with eps = 0 it is NaN.
+ * row of zeros gives zeros. With eps = 0 it is NaN, and a row whose root mean
+ * square is below 2^-128 has an infinite rstd, outputs and gradients that are
+ * infinite or NaN.
  */
 hc_status hc_rms_norm_fwd(const void* x, const void* res, hc_dtype dt, const int32_t* count,
                           int capacity, int C, float eps, const float* gamma, void* h, void* y,

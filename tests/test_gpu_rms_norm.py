@@ -269,6 +269,29 @@ def test_values(C, dtype):
     assert y[0].isnan().all() and (y[1:5].isfinite()).all() and (y[7:].isfinite()).all()
 
 
+@pytest.mark.parametrize("C,dtype", [(24, F), (24, BF), (131, F), (264, BF), (602, BF), (2048, F), (2051, BF), (8200, F),
+                                     (20001, BF)])
+def test_smallest_rows(C, dtype):
+    """Without eps: rows whose rstd fp32 just holds are normed like any others; below
+    that rstd is infinite, and no finite output pretends otherwise. Rows of the
+    ordinary size beside them stay what they are."""
+    x, _, _, _, gamma = inputs(C, 12, C, F)
+    x[::3] *= 2.0 ** -125
+    x[1::3] *= 2.0 ** -132
+    x = x.to(dtype)
+    y, rstd = full((12, C), dtype), full((12,))
+    q, sc = full((12, hc.HC_FP8_PITCH(C)), torch.uint8, 77), full(((C + 127) // 128, 12))
+    hc.hc_rms_norm_fwd(x, 0.0, gamma, y=y, rstd=rstd, q=q, scales=sc)
+    v, rr, tv, tr = fwd_ref(x, gamma, 0.0)
+    past = rr >= 2.0 ** 128
+    assert past[1::3].all() and not past[::3].any() and not past[2::3].any()
+    within(rstd[~past], rr[~past], tr[~past], "rstd")
+    within(y[~past], v[~past], (tv + rounding(dtype, v))[~past], "y")
+    assert (rstd[past] == float("inf")).all() and not y[past].isfinite().any()
+    top = (x[~past].float() * rstd[~past, None] * gamma).abs().amax(1)
+    assert torch.equal(sc[:, ~past].amax(0), top / torch.full_like(top, 448.0))
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("C", [64, 131])
 def test_stored_sums(C, dtype):
