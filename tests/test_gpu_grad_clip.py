@@ -251,6 +251,35 @@ def test_list_dropped_while_another_stream_uses_it(given):
     check(grads, outs, norm, 1.0)
 
 
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_clips_one_after_another(dtype):
+    """Each call writes the outputs anew from the gradients, which stay; in place it
+    goes on from what it left; rows that start one past 16 bytes in and out."""
+    g = gen(17)
+    grads = [randn(g, 300, 70, dtype=dtype), randn(g, 4097, dtype=dtype), shifted(randn(g, 211, 3, dtype=dtype))]
+    keep = [t.clone() for t in grads]
+    outs = [shifted(torch.zeros_like(t)) for t in grads]
+    lst, norm = hc.hc_tensor_list(grads, outs), full((1,))
+    hc.hc_grad_norm(lst, norm)
+    ref = norm_ref(grads)
+    done = []
+    for part in (0.5, 2.0, 0.25):
+        hc.hc_grad_clip(lst, norm, part * ref)
+        check(grads, outs, norm, part * ref)
+        done.append([o.clone() for o in outs])
+    assert all(torch.equal(a, b) for a, b in zip(grads, keep))
+    assert all(torch.equal(a, b) for a, b in zip(done[1], keep))
+    assert not any(torch.equal(a, b) for a, b in zip(done[0], done[2]))
+    inp = hc.hc_tensor_list(grads)
+    hc.hc_grad_clip(inp, norm, 0.5 * ref)
+    check(grads, grads, norm, 0.5 * ref, before=keep)
+    assert all(torch.equal(a, b) for a, b in zip(grads, done[0]))
+    hc.hc_grad_clip(inp, norm, 0.5 * ref)  # the norm given is the same: halved once more
+    for t, d in zip(grads, done[0]):
+        want = d.to(D64) / 2
+        within(t, want, 13 * U * want.abs() + rounding(dtype, want), "halved twice")
+
+
 def test_other_device_is_refused():
     lst = hc.hc_tensor_list([torch.zeros(3, device="cuda")])
     lst.device += 1
