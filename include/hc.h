@@ -667,13 +667,14 @@ hc_status hc_fp8_linear_fwd(const uint8_t* xq, const float* xs, const int32_t* c
  *   x         [capacity, C] of dtype dt
  *   W         [V, C] of dtype dt: a row per class, as an embedding table has
  *             (the same table may serve both)
- *   bias      [V] fp32, or NULL (0); -infinity excludes a class (a token whose
- *             classes are all excluded has the loss NaN)
+ *   bias      [V] fp32, or NULL (0); -infinity excludes a class, whose row of W
+ *             has to be finite all the same (a token whose classes are all
+ *             excluded has the loss NaN)
  *   targets   [capacity] int32
  *   loss, lse [capacity] fp32, or NULL each; at least one is required. lse is
  *             what hc_linear_cross_entropy_bwd reads
  * fp32 operands keep fp32's precision: each is split into three bf16 numbers,
- * and the products that matter are summed. Up to four rows, up to eight where
+ * and the products that matter are summed (one with an infinity is NaN). Up to four rows, up to eight where
  * they or W are short, and few classes of few channels are summed in plain fp32.
  * Uses the library's per-stream workspace: with planes = 1 (bf16) or 3 (fp32),
  * 2 * planes * C + 16 bytes a row of the capacity (rounded up to 256 rows), 8
@@ -698,11 +699,15 @@ hc_status hc_linear_cross_entropy_fwd(const void* x, const void* W, hc_dtype dt,
  *   dW        [V, C] of dtype dt, or NULL; may not overlap W
  *   dbias     [V] fp32, or NULL; at least one output is required
  * G is held in bf16 for bf16 operands (a rounding of 2^-8 at most), in three bf16
- * numbers for fp32, in fp32 where the forward is plain fp32; sums are in fp32.
- * The vocabulary is taken in pieces whose G takes at most 512 MiB of the workspace
- * (2048 classes at least); the sums of dx take 4 * C bytes a row of the capacity
- * and 30 MB more than the forward, those of dW and dbias 52 MB. In plain fp32
- * all of it is at most 15 MB.
+ * numbers for fp32, in fp32 where the forward is plain fp32. Sums are in fp32; those
+ * of bf16 operands stay in one accumulator of the tensor cores, which cuts off 2^-25
+ * or so of a sum for every 16 terms (tokens for dW, classes of a piece for dx).
+ * The workspace follows the capacity, not N': besides the forward's rows and W,
+ * the vocabulary is taken in pieces whose G, 2 * planes bytes a row and class, takes
+ * at most 512 MiB (but 2048 classes at least: 4.1 GB for 335200 rows of fp32); the
+ * sums of dx take 4 * C bytes a row of the capacity and 30 MB, those of dW 20 MB,
+ * those of dbias 4 bytes for 32 rows and a class of a piece (34 MB while G is
+ * within 512 MiB). In plain fp32 all of it is at most 15 MB.
  */
 hc_status hc_linear_cross_entropy_bwd(const void* x, const void* W, hc_dtype dt, const float* bias,
                                       const int32_t* targets, const float* lse, const float* dloss,
@@ -748,6 +753,7 @@ hc_status hc_grad_norm(const hc_tensor_list* list, float* norm, hc_stream_t stre
  * norm is read on the device: hc_grad_norm's, or one that a caller has combined
  * from several. An infinite norm gives 0 (NaN where in is infinite), a NaN fills
  * all outputs. Tensors in place whose norm is not above max_norm are not touched.
+ * norm may not lie in one of the list's tensors.
  */
 hc_status hc_grad_clip(const hc_tensor_list* list, const float* norm, float max_norm,
                        hc_stream_t stream);

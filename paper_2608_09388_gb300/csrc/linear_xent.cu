@@ -333,9 +333,13 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
         "h"((unsigned short)3)
         : "memory");
 }
-// An arrival that orders no memory: what it tells has been read from TMEM (and
-// waited for) already. With release semantics it waited for the global stores
-// of the tile before, 1000 clocks a tile.
+// Gives the accumulator back. All that has to come before it are the warp's loads
+// from TMEM, and those are not ordered by the barrier's memory semantics: they are
+// done at tcgen05.wait::ld (by the whole warp), tcgen05.fence::before_thread_sync
+// puts them before the arrival, and tcgen05.fence::after_thread_sync behind the
+// wait puts the products after it; with that pair of fences the arrival may be
+// relaxed. With release semantics it also waited for the global stores of the
+// tile before, which nobody waits for here: 1000 clocks a tile.
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar)
                  : "memory");
