@@ -664,6 +664,7 @@ class hc_tensor_list(ctypes.Structure):
         # the streams whose work the table's memory outlives: the one it was allocated
         # on, and those that _list adds
         self.streams = {torch._C._cuda_getCurrentRawStream(self.device)}
+        self.at = ctypes.addressof(self)
 
 
 def _list(tensors, stream):
@@ -671,14 +672,18 @@ def _list(tensors, stream):
     import torch
     if not isinstance(tensors, hc_tensor_list):
         raise TypeError("an hc_tensor_list is expected")
-    if tensors.device != torch._C._cuda_getDevice():
+    device = torch._C._cuda_getDevice()
+    if tensors.device != device:
         raise ValueError(f"the list is of device {tensors.device}, which is not the current one")
-    s = _s(stream)
-    raw = s if stream is None else s.value or 0
+    if stream is None:
+        s = raw = torch._C._cuda_getCurrentRawStream(device)
+    else:
+        s = _s(stream)
+        raw = s.value or 0
     if raw not in tensors.streams and (stream is None or isinstance(stream, torch.cuda.Stream)):
         tensors.memory.record_stream(torch.cuda.current_stream() if stream is None else stream)
         tensors.streams.add(raw)
-    return ctypes.byref(tensors), s
+    return tensors.at, s
 
 
 def hc_grad_norm(tensors, norm, stream=None):
